@@ -11,7 +11,8 @@
  *   spf_select_topk    Appendix A.1.2 / Algorithm 1 "TopKChunks".
  *   spf_compact_spans  Section 3.2 / Algorithm 1 "MergeAdjacentChunks" + "MapDraftChunksToTextSpans".
  *
- * Around them: spf_keep_count / spf_keep_rate / spf_snap_budget (Section 3.1, keep rate) and spf_concat_with_delim
+ * Before them, on the draft model's side: spf_kv_append (rotates a step's queries and keys and writes a paged cache) and
+ * spf_attend (the step's attention over it).  Around them: spf_keep_count / spf_keep_rate / spf_snap_budget (Section 3.1, keep rate) and spf_concat_with_delim
  * (Algorithm 1 "ConcatWithDelim") on the host; spf_score_paged (paged key cache), spf_score_fp8 (8-bit key cache),
  * spf_score_shard_lse /
  * spf_score_shard_apply (one prompt's keys over several GPUs); spf_score_extra, spf_chunk_pool_edge,
@@ -56,7 +57,8 @@ typedef enum {
   SPF_ERR_WORKSPACE = -3,   /* workspace missing, misaligned or smaller than the size query says    */
   SPF_ERR_CUDA = -4,        /* a CUDA runtime call failed (no device, launch error)                 */
   SPF_ERR_TIMEOUT = -5,     /* device status only: a bounded wait inside a kernel ran out           */
-  SPF_ERR_RANGE = -6        /* device status only: a softmax row sum overflowed fp32 in the fused path */
+  SPF_ERR_RANGE = -6,       /* device status only: a softmax row sum overflowed fp32 in the fused path */
+  SPF_ERR_CACHE = -7        /* device status only: a length, position or block-table entry outside the cache */
 } spf_status;
 
 /* Draft-model attention geometry shared by all prompts of a call. */
@@ -213,6 +215,99 @@ typedef struct {
 SPF_API size_t spf_score_fp8_workspace_bytes(const spf_shape* shape, const spf_fp8_prompt* prompts, int32_t n_prompts);
 SPF_API int32_t spf_score_fp8(const spf_shape* shape, const spf_fp8_prompt* prompts, int32_t n_prompts, void* workspace,
                               size_t workspace_bytes, int32_t* dev_status, void* cuda_stream);
+
+/*
+ * The draft model's paged cache of ONE layer, keys and values, as spf_kv_append writes and spf_attend reads it.  The key pool
+ * is the pool that spf_score_paged (bf16) and spf_score_paged_fp8 (8 bits) score.
+ *
+ *   k_pool, v_pool     DEVICE, contiguous [n_pool_blocks][Hkv][block_tokens][d], 16-byte aligned; keys after the rotation.
+ *                      bf16 when the scales are NULL, else E4M3 bytes (see spf_score_fp8)
+ *   k_scale, v_scale   DEVICE fp32 [n_pool_blocks][Hkv][block_tokens / SPF_KV_SCALE_TOKENS]: what the bytes of that many
+ *                      consecutive tokens of a block and head are multiplied by, positive and finite; both NULL: bf16 pools
+ *   block_tokens       a positive multiple of 128
+ *   head_dim           d: 64 or 128
+ * Limit: n_pool_blocks * Hkv * block_tokens < 2^31.
+ */
+#define SPF_KV_SCALE_TOKENS 64
+typedef struct {
+  void* k_pool;
+  void* v_pool;
+  float* k_scale;
+  float* v_scale;
+  int64_t n_pool_blocks;
+  int32_t block_tokens;
+  int32_t n_kv_heads;
+  int32_t head_dim;
+} spf_kv_cache;
+
+/*
+ * A step of the draft model: some new tokens of each of n_seqs sequences (one, when it generates; a chunk of the prompt;
+ * none).  The new tokens of sequence b are rows row_start[b] ... row_start[b + 1] - 1 of the step's arrays and the LAST
+ * row_start[b + 1] - row_start[b] of the sequence's seq_lens[b] tokens.  All arrays are DEVICE memory, so that a captured
+ * graph can be replayed with other lengths.
+ *
+ *   n_rows        rows of the step's arrays; rows behind row_start[n_seqs] are not read and left as they were
+ *   max_new       HOST hint, >= 1: new tokens of the sequence that has most.  It picks the kernels; sequences with more are
+ *                 computed all the same, only slower
+ *   row_start     int32 [n_seqs + 1], ascending from 0, the last one at most n_rows
+ *   seq_lens      int32 [n_seqs], the new tokens included, at most table_stride * block_tokens
+ *   block_table   int32 [n_seqs][table_stride]: logical block j of sequence b is pool block block_table[b][j]; entries behind
+ *                 a sequence's length are not read
+ */
+typedef struct {
+  int32_t n_seqs;
+  int32_t n_rows;
+  int32_t max_new;
+  int32_t table_stride;
+  const int32_t* row_start;
+  const int32_t* seq_lens;
+  const int32_t* block_table;
+} spf_kv_step;
+
+/*
+ * Rotation by position.  `table` is DEVICE fp32 [n_positions][rot_dim], row p = the cosines of position p's rot_dim / 2
+ * angles, then their sines (whatever base or scaling they were made with).  Pair j of a head, elements (j, j + rot_dim / 2),
+ * or (2 j, 2 j + 1) where `interleaved`, becomes
+ *     (x cos_j - y sin_j, y cos_j + x sin_j),
+ * in fp32 with each product rounded; elements from rot_dim on stay.  rot_dim: a multiple of 16, at most d.  `positions`:
+ * DEVICE int32 [n_rows], the table's row for every row of the step, or NULL for a token's place in its sequence.
+ */
+typedef struct {
+  const float* table;
+  const int32_t* positions;
+  int32_t n_positions;
+  int32_t rot_dim;
+  int32_t interleaved;
+} spf_rope;
+
+/* Rows of a step, element (row, head, j) at row * stride_row + head * stride_head + j; strides in elements, multiples of 8,
+ * data 16-byte aligned: a slice of a fused projection's output, or one lookahead token of the [L][Hq][m][d] queries that
+ * spf_score reads. */
+typedef struct {
+  void* data;
+  int64_t stride_row;
+  int64_t stride_head;
+} spf_rows;
+
+/*
+ * Appends a step's keys and values to the cache, rotating keys (and queries) on the way.
+ *   k, v          bf16, n_kv_heads heads a row
+ *   q, q_out      bf16, n_q_heads heads a row: the rotated queries go to q_out, which may be q itself (same strides) and must
+ *                 not overlap it otherwise; both NULL: the step's queries are handled elsewhere
+ *   rope          NULL: nothing is rotated (q, where given, is copied)
+ * bf16 pools: rotated values are rounded to bf16 once.  8-bit pools, for each group of SPF_KV_SCALE_TOKENS tokens and head that
+ * receives tokens: scale = the smallest power of two that keeps the new tokens' finite values within 448 times it (at least
+ * 2^-100), and no smaller than the scale that tokens of the group from before the step have; where it grows, their bytes are
+ * rounded again to the new scale (exact unless they become subnormal).  New values are rounded once, from fp32; infinities
+ * become +-448 times the scale, NaN stays NaN (0x7F).
+ * A block that receives tokens belongs to one sequence of the step only (two that write the same block race).
+ * Device conditions: SPF_ERR_CACHE in dev_status (may be NULL) for a row whose position, table row or block lies outside; that
+ * row is left out, the others are not affected.
+ * Errors: SPF_ERR_INVALID_ARG, SPF_ERR_UNSUPPORTED (head_dim, the limit above), SPF_ERR_CUDA.
+ */
+SPF_API int32_t spf_kv_append(const spf_kv_cache* cache, const spf_kv_step* step, const spf_rope* rope, const spf_rows* k,
+                              const spf_rows* v, const spf_rows* q, const spf_rows* q_out, int32_t n_q_heads,
+                              int32_t* dev_status, void* cuda_stream);
 
 /*
  * One long prompt over several GPUs (Appendix A.1.1 is per prompt; this shards its keys).  Each rank holds a contiguous

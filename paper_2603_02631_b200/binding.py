@@ -66,6 +66,26 @@ class _PagedPrompt(ctypes.Structure):
                 ("q", ctypes.c_void_p), ("importance", ctypes.c_void_p), ("lse", ctypes.c_void_p)]
 
 
+class _KvCache(ctypes.Structure):
+    _fields_ = [("k_pool", ctypes.c_void_p), ("v_pool", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("n_pool_blocks", ctypes.c_int64), ("block_tokens", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32)]
+
+
+class _KvStep(ctypes.Structure):
+    _fields_ = [("n_seqs", ctypes.c_int32), ("n_rows", ctypes.c_int32), ("max_new", ctypes.c_int32), ("table_stride", ctypes.c_int32),
+                ("row_start", ctypes.c_void_p), ("seq_lens", ctypes.c_void_p), ("block_table", ctypes.c_void_p)]
+
+
+class _Rope(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("positions", ctypes.c_void_p), ("n_positions", ctypes.c_int32), ("rot_dim", ctypes.c_int32),
+                ("interleaved", ctypes.c_int32)]
+
+
+class _Rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("stride_row", ctypes.c_int64), ("stride_head", ctypes.c_int64)]
+
+
 def _load() -> ctypes.CDLL:
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"{LIB_PATH} is missing: build it with `python -m paper_2603_02631_b200.build` "
@@ -123,6 +143,9 @@ def _load() -> ctypes.CDLL:
     dll.spf_select_topk_batch.argtypes = [ctypes.POINTER(_TopkItem), i32, vp]
     dll.spf_compact_spans_batch.restype = i32
     dll.spf_compact_spans_batch.argtypes = [ctypes.POINTER(_CompactItem), i32, i32, vp]
+    dll.spf_kv_append.restype = i32
+    dll.spf_kv_append.argtypes = [ctypes.POINTER(_KvCache), ctypes.POINTER(_KvStep), ctypes.POINTER(_Rope), ctypes.POINTER(_Rows),
+                                  ctypes.POINTER(_Rows), ctypes.POINTER(_Rows), ctypes.POINTER(_Rows), i32, vp, vp]
     dll.spf_keep_count.restype = i64
     dll.spf_keep_count.argtypes = [i64, ctypes.c_double]
     dll.spf_keep_rate.restype = ctypes.c_double
@@ -626,6 +649,41 @@ def spf_compress_host(q: torch.Tensor, k_layers: Sequence[torch.Tensor], token_i
     stream.  See spf_compress_host in include/spf.h for sizes."""
     _check(_native.compress_host(q, k_layers, token_ids, char_start, char_end, chunk, pool_kernel, keep, arena, out_ids, out_pos,
                                  out_tok_spans, out_char_spans, out_counts, softmax_scale, stream), "spf_compress_host")
+
+
+@dataclasses.dataclass
+class KvCache:
+    """One layer's paged cache (see spf_kv_cache in include/spf.h): bf16 pools, or uint8 pools (E4M3 bytes) with their scales."""
+    k_pool: torch.Tensor                      # [n_pool_blocks, Hkv, block_tokens, d], contiguous
+    v_pool: torch.Tensor
+    k_scale: Optional[torch.Tensor] = None    # fp32 [n_pool_blocks, Hkv, block_tokens / 64]
+    v_scale: Optional[torch.Tensor] = None
+
+
+@dataclasses.dataclass
+class KvStep:
+    """The new tokens of a step (see spf_kv_step in include/spf.h): rows row_start[b] .. row_start[b + 1] - 1 of the step's arrays
+    are the last of sequence b's seq_lens[b] tokens."""
+    row_start: torch.Tensor                   # int32 [n_seqs + 1]
+    seq_lens: torch.Tensor                    # int32 [n_seqs]
+    block_table: torch.Tensor                 # int32 [n_seqs, blocks]
+    max_new: int = 1                          # hint: new tokens of the sequence that has most
+
+
+@dataclasses.dataclass
+class Rope:
+    """Rotation by position (see spf_rope in include/spf.h)."""
+    table: torch.Tensor                       # fp32 [n_positions, rot_dim]: cosines, then sines
+    positions: Optional[torch.Tensor] = None  # int32 [rows]; None: a token's place in its sequence
+    interleaved: bool = False                 # pairs (2 j, 2 j + 1) instead of (j, j + rot_dim / 2)
+
+
+def spf_kv_append(cache: KvCache, step: KvStep, k: torch.Tensor, v: torch.Tensor, q: Optional[torch.Tensor] = None,
+                  q_out: Optional[torch.Tensor] = None, rope: Optional[Rope] = None, dev_status: Optional[torch.Tensor] = None,
+                  stream: Optional[torch.cuda.Stream] = None) -> None:
+    """Rotates a step's keys (and queries, into ``q_out``) and appends keys and values to the cache.  k, v: bf16 [rows, Hkv, d];
+    q, q_out: bf16 [rows, Hq, d]; rows and heads may have any strides that are multiples of 8."""
+    _check(_native.kv_append(cache, step, k, v, q, q_out, rope, dev_status, stream), "spf_kv_append")
 
 
 @dataclasses.dataclass

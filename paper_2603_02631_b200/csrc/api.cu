@@ -8,6 +8,7 @@
 #include <mutex>
 
 #include "common.cuh"
+#include "kv.cuh"
 #include "score.cuh"
 
 namespace spf {
@@ -73,18 +74,6 @@ int32_t make_problem(const spf_shape* shape, const spf_prompt& pr, int32_t index
   p.block_tokens = 0;
   p.n_pool_blocks = 0;
   *out = p;
-  return SPF_OK;
-}
-
-int32_t device_sm_count(int* out) {
-  int dev = 0;
-  SPF_CUDA_CHECK(cudaGetDevice(&dev));
-  static std::mutex mu;
-  static int cached[64];
-  std::lock_guard<std::mutex> lock(mu);
-  if (dev < 0 || dev >= 64) return fail(SPF_ERR_CUDA, "device ordinal %d out of range", dev);
-  if (cached[dev] == 0) SPF_CUDA_CHECK(cudaDeviceGetAttribute(&cached[dev], cudaDevAttrMultiProcessorCount, dev));
-  *out = cached[dev];
   return SPF_OK;
 }
 
@@ -174,6 +163,18 @@ int32_t score_prompts(const char* who, const spf_shape* shape, const Prompt* pro
 }
 
 }  // namespace
+
+int32_t device_sm_count(int* out) {
+  int dev = 0;
+  SPF_CUDA_CHECK(cudaGetDevice(&dev));
+  static std::mutex mu;
+  static int cached[64];
+  std::lock_guard<std::mutex> lock(mu);
+  if (dev < 0 || dev >= 64) return fail(SPF_ERR_CUDA, "device ordinal %d out of range", dev);
+  if (cached[dev] == 0) SPF_CUDA_CHECK(cudaDeviceGetAttribute(&cached[dev], cudaDevAttrMultiProcessorCount, dev));
+  *out = cached[dev];
+  return SPF_OK;
+}
 
 int32_t fail(int32_t code, const char* fmt, ...) {
   va_list ap;
@@ -443,6 +444,7 @@ extern "C" const char* spf_status_string(int32_t status) {
     case SPF_ERR_CUDA: return "CUDA runtime error";
     case SPF_ERR_TIMEOUT: return "bounded device-side wait ran out";
     case SPF_ERR_RANGE: return "a softmax row overflowed fp32 in the fused path";
+    case SPF_ERR_CACHE: return "a length, position or block-table entry lies outside the cache";
     default: return "unknown status";
   }
 }

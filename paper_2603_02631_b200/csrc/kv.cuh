@@ -1,0 +1,57 @@
+// The draft model's paged cache and a step's tokens, as the kernels that write and read them see them, and the host's checks.
+#pragma once
+
+#include "common.cuh"
+
+namespace spf {
+
+constexpr int kScaleTokens = SPF_KV_SCALE_TOKENS;
+
+struct KvView {
+  uint8_t *k, *v;              // pools: bf16 or E4M3 [n_blocks][n_kv_heads][block_tokens][d]
+  float *k_scale, *v_scale;    // 8-bit pools: [n_blocks][n_kv_heads][block_tokens / 64]
+  int64_t n_blocks;
+  int block_tokens, n_kv_heads;
+};
+
+struct StepView {
+  const int32_t *row_start, *seq_lens, *table;
+  int n_seqs, n_rows, table_stride;
+};
+
+struct RowsView {
+  __nv_bfloat16* data;
+  int64_t stride_row, stride_head;
+};
+
+// Device-side conditions of the cache calls: the first one stays.
+__device__ __forceinline__ void report_cache(int32_t* dev_status) {
+  if (dev_status != nullptr) atomicCAS(dev_status, 0, (int32_t)SPF_ERR_CACHE);
+}
+
+// The sequence of a row: the last one that starts at or before it (-1: none does).  Empty sequences start where the next does.
+__device__ __forceinline__ int sequence_of(const StepView& st, int row) {
+  int lo = 0, hi = st.n_seqs;                       // the answer is below hi, and at least lo - 1
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if (__ldg(st.row_start + mid) <= row) lo = mid + 1;
+    else hi = mid;
+  }
+  return lo - 1;
+}
+
+// Pool block of a token, -1 where the table or the pool has no such place.
+__device__ __forceinline__ int64_t pool_block(const KvView& kv, const StepView& st, int seq, int pos) {
+  const int j = pos / kv.block_tokens;
+  if (pos < 0 || j >= st.table_stride) return -1;
+  const int b = __ldg(st.table + (int64_t)seq * st.table_stride + j);
+  return b >= 0 && b < kv.n_blocks ? b : -1;
+}
+
+// Host checks, shared by the calls on the cache; they leave the reason in the error text.
+int32_t check_cache(const char* who, const spf_kv_cache* cache, KvView* out);
+int32_t check_step(const char* who, const spf_kv_step* step, StepView* out);
+int32_t check_rows(const char* who, const char* name, const spf_rows* rows, int n_heads, int head_dim, bool written, RowsView* out);
+int32_t device_sm_count(int* out);
+
+}  // namespace spf

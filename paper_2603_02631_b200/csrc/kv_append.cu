@@ -1,0 +1,444 @@
+// Rotation of a step's queries and keys by position, and the append of keys and values to the paged cache.
+//
+//   q'[t, h] = R(p_t) q[t, h],  k'[t, h] = R(p_t) k[t, h],  R(p): pairs (x, y) -> (x cos - y sin, y cos + x sin), fp32, each
+//   product rounded by itself (no fused multiply-add: the result is then the same wherever the formula is written out).
+//
+// bf16 pools: one rounding, straight to the token's place.  8-bit pools: a scale belongs to 64 tokens of a block and head, so
+// one CTA makes the new tokens of such a group, their largest magnitude, the scale, and the bytes:
+//   s' = max(s of the tokens that the group holds already, 2^ceil(log2(max |x| / 448))),   byte = E4M3(x / s'),
+// and rounds the bytes held already from s to s' where it grew.  Powers of two: that second rounding is then exact but for
+// bytes that become subnormal.
+//
+// Bounds: bytes for a prompt, a launch and four dependent loads (row_start, seq_lens, table, the data) for single tokens.
+#include <algorithm>
+
+#include <cuda_fp16.h>
+
+#include "kv.cuh"
+
+namespace spf {
+namespace {
+
+constexpr int kAppendThreads = 128;
+
+struct AppendArgs {
+  KvView kv;
+  StepView step;
+  RowsView k, v, q, q_out;
+  const float* rope;            // null: no rotation
+  const int32_t* positions;     // null: a token's place in its sequence
+  int n_positions, rot_dim, interleaved;
+  int n_q_heads;                // 0: no queries in this call
+  int rotate_ctas;              // CTAs that move whole rows; behind them, those that fill 8-bit groups
+  int32_t* dev_status;
+};
+
+union Pack8 {
+  uint4 u;
+  __nv_bfloat162 h[4];
+};
+
+__device__ __forceinline__ uint4 load_raw(const __nv_bfloat16* p) { return __ldg(reinterpret_cast<const uint4*>(p)); }
+
+__device__ __forceinline__ void widen8(const uint4& raw, float (&x)[8]) {
+  Pack8 v;
+  v.u = raw;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 f = __bfloat1622float2(v.h[i]);
+    x[2 * i] = f.x;
+    x[2 * i + 1] = f.y;
+  }
+}
+
+__device__ __forceinline__ uint4 narrow8(const float (&x)[8]) {
+  Pack8 v;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v.h[i] = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+  return v.u;
+}
+
+// A head is moved in units of 16 elements, two runs of 8: where the unit's halves lie, and which angles turn them (angle < 0:
+// the unit is not rotated).  Units of the split form pair element j with j + rot_dim / 2.
+struct Unit {
+  int first, second, angle;
+};
+__device__ __forceinline__ Unit unit_of(int u, int rot_dim, int interleaved) {
+  if (u * 16 >= rot_dim) return Unit{u * 16, u * 16 + 8, -1};
+  if (interleaved) return Unit{u * 16, u * 16 + 8, u * 8};
+  return Unit{u * 8, rot_dim / 2 + u * 8, u * 8};
+}
+
+struct Angles {
+  float c[8], s[8];
+};
+__device__ __forceinline__ void load_angles(const float* table, int64_t row, int rot_dim, int angle, Angles& a) {
+  const float4* c = reinterpret_cast<const float4*>(table + row * rot_dim + angle);
+  const float4* s = reinterpret_cast<const float4*>(table + row * rot_dim + rot_dim / 2 + angle);
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const float4 x = __ldg(c + i), y = __ldg(s + i);
+    a.c[4 * i] = x.x, a.c[4 * i + 1] = x.y, a.c[4 * i + 2] = x.z, a.c[4 * i + 3] = x.w;
+    a.s[4 * i] = y.x, a.s[4 * i + 1] = y.y, a.s[4 * i + 2] = y.z, a.s[4 * i + 3] = y.w;
+  }
+}
+
+__device__ __forceinline__ void turn(float& x, float& y, float c, float s) {
+  const float nx = __fsub_rn(__fmul_rn(x, c), __fmul_rn(y, s));
+  y = __fadd_rn(__fmul_rn(y, c), __fmul_rn(x, s));
+  x = nx;
+}
+__device__ __forceinline__ void rotate(float (&a)[8], float (&b)[8], const Angles& t, int interleaved) {
+  if (interleaved) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      turn(a[2 * i], a[2 * i + 1], t.c[i], t.s[i]);
+      turn(b[2 * i], b[2 * i + 1], t.c[4 + i], t.s[4 + i]);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) turn(a[i], b[i], t.c[i], t.s[i]);
+  }
+}
+
+// Position in the sequence and row of the angles' table; false (and reported) where one lies outside.
+__device__ __forceinline__ bool place_of(const AppendArgs& a, int seq, int row, int* pos, int64_t* angle_row) {
+  const int start = __ldg(a.step.row_start + seq), end = __ldg(a.step.row_start + seq + 1), len = __ldg(a.step.seq_lens + seq);
+  *pos = len - (end - row);
+  *angle_row = a.positions != nullptr ? __ldg(a.positions + row) : *pos;
+  const bool fine = row >= start && *pos >= 0 && (a.rope == nullptr || (*angle_row >= 0 && *angle_row < a.n_positions));
+  if (!fine) report_cache(a.dev_status);
+  return fine;
+}
+
+// Rows as they are: queries (always), keys and values (bf16 pools).  A thread has one unit of HPT heads of a row, so that a
+// row's angles are read once for HPT heads.
+template <int D, int HPT, bool FP8>
+__device__ __forceinline__ void move_rows(const AppendArgs& a) {
+  constexpr int kUnits = D / 16;
+  const int turned = a.n_q_heads + (FP8 ? 0 : a.kv.n_kv_heads), copied = FP8 ? 0 : a.kv.n_kv_heads;
+  const int turned_groups = (turned + HPT - 1) / HPT, groups = turned_groups + (copied + HPT - 1) / HPT;
+  const int per_row = groups * kUnits;
+  const int64_t first = (int64_t)blockIdx.x * kAppendThreads, item = first + threadIdx.x;
+  // the sequences of the CTA's first and last row, by one look of all threads at the starts; a thread's own lies between
+  const int row_lo = (int)(first / per_row), row_hi = (int)min((first + kAppendThreads - 1) / per_row, (int64_t)a.step.n_rows - 1);
+  int lo = 0, hi = 0;
+  for (int b = 0; b < a.step.n_seqs; b += kAppendThreads) {
+    const int start = b + (int)threadIdx.x < a.step.n_seqs ? __ldg(a.step.row_start + b + threadIdx.x) : 0x7fffffff;
+    lo += __syncthreads_count(start <= row_lo);
+    hi += __syncthreads_count(start <= row_hi);
+  }
+  const int row = (int)(item / per_row);
+  if (row >= a.step.n_rows || row >= __ldg(a.step.row_start + a.step.n_seqs)) return;
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if (__ldg(a.step.row_start + mid) <= row) lo = mid + 1;
+    else hi = mid;
+  }
+  const int seq = lo - 1;
+  if (seq < 0) return;
+  int pos;
+  int64_t angle_row;
+  if (!place_of(a, seq, row, &pos, &angle_row)) return;
+  const int in_row = (int)(item - (int64_t)row * per_row), group = in_row / kUnits;
+  const Unit u = unit_of(in_row % kUnits, a.rope != nullptr ? a.rot_dim : 0, a.interleaved);
+  const bool copy = group >= turned_groups;
+  const int head0 = (copy ? group - turned_groups : group) * HPT, heads = copy ? copied : turned;
+
+  const int64_t block = pool_block(a.kv, a.step, seq, pos);
+  if (block < 0) {
+    report_cache(a.dev_status);
+    return;
+  }
+  // offset of the token's row in a bf16 pool, but for the head
+  const int64_t cell = (block * a.kv.n_kv_heads * a.kv.block_tokens + pos % a.kv.block_tokens) * D;
+  const bool turns = !copy && u.angle >= 0;
+  uint4 x[HPT][2];                                  // what is not turned is copied as it is
+  Angles t;
+  if (turns) load_angles(a.rope, angle_row, a.rot_dim, u.angle, t);
+#pragma unroll
+  for (int i = 0; i < HPT; ++i) {
+    const int h = head0 + i;
+    if (h < heads) {
+      const __nv_bfloat16* src = copy ? a.v.data + row * a.v.stride_row + h * a.v.stride_head
+                                 : h < a.n_q_heads ? a.q.data + row * a.q.stride_row + h * a.q.stride_head
+                                                   : a.k.data + row * a.k.stride_row + (h - a.n_q_heads) * a.k.stride_head;
+      x[i][0] = load_raw(src + u.first);
+      x[i][1] = load_raw(src + u.second);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < HPT; ++i) {
+    const int h = head0 + i;
+    if (h < heads) {
+      if (turns) {
+        float f[8], g[8];
+        widen8(x[i][0], f);
+        widen8(x[i][1], g);
+        rotate(f, g, t, a.interleaved);
+        x[i][0] = narrow8(f);
+        x[i][1] = narrow8(g);
+      }
+      __nv_bfloat16* dst;
+      if (copy) dst = reinterpret_cast<__nv_bfloat16*>(a.kv.v) + cell + (int64_t)h * a.kv.block_tokens * D;
+      else if (h < a.n_q_heads) dst = a.q_out.data + row * a.q_out.stride_row + h * a.q_out.stride_head;
+      else dst = reinterpret_cast<__nv_bfloat16*>(a.kv.k) + cell + (int64_t)(h - a.n_q_heads) * a.kv.block_tokens * D;
+      *reinterpret_cast<uint4*>(dst + u.first) = x[i][0];
+      *reinterpret_cast<uint4*>(dst + u.second) = x[i][1];
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------------------------- 8-bit groups
+// The smallest power of two s >= 2^-100 with m / s <= 448 (448 = 1.75 * 2^8), m finite and not negative.
+__device__ __forceinline__ float scale_for(float m) {
+  const uint32_t bits = __float_as_uint(m);
+  const int exponent = (int)(bits >> 23) - 127;
+  const int e = max(exponent - 8 + ((bits & 0x7fffffu) > 0x600000u ? 1 : 0), -100);
+  return __uint_as_float((uint32_t)(e + 127) << 23);
+}
+
+// Two values as E4M3 bytes, to nearest, clipped at 448 (NaN: 0x7F).
+__device__ __forceinline__ uint32_t e4m3_pair(float lo, float hi) {
+  uint16_t r;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ float2 e4m3_pair_value(uint32_t two) {
+  uint32_t h2;
+  asm("{\n.reg .b16 b;\ncvt.u16.u32 b, %1;\ncvt.rn.f16x2.e4m3x2 %0, b;\n}" : "=r"(h2) : "r"(two));
+  return __half22float2(*reinterpret_cast<const __half2*>(&h2));
+}
+
+// x / scale: a product where the scale is a power of two (as every scale that this kernel makes), which is the same value.
+struct Divider {
+  float scale, inverse;
+  bool exact;
+  __device__ __forceinline__ float operator()(float x) const { return exact ? x * inverse : __fdiv_rn(x, scale); }
+};
+
+__device__ __forceinline__ uint2 bytes8(const float (&x)[8], const Divider& by) {
+  uint2 r;
+  r.x = e4m3_pair(by(x[0]), by(x[1])) | (e4m3_pair(by(x[2]), by(x[3])) << 16);
+  r.y = e4m3_pair(by(x[4]), by(x[5])) | (e4m3_pair(by(x[6]), by(x[7])) << 16);
+  return r;
+}
+
+__device__ __forceinline__ float finite_magnitude(float x) {
+  const float m = fabsf(x);
+  return m <= 3.402823466e38f ? m : 0.f;            // neither infinities nor NaN set a scale
+}
+
+// One group of 64 tokens (of a sequence, in a pool block), one head, keys or values.  Group slots of the grid: sequence b owns
+// those from row_start[b] / 64 + 2 b on, which is at least as many as its new tokens can touch (n tokens touch at most
+// n / 64 + 2 groups).
+template <int D>
+__device__ __forceinline__ void fill_group(const AppendArgs& a) {
+  constexpr int kUnits = D / 16, kPer = kScaleTokens * kUnits / kAppendThreads;
+  __shared__ float warp_max[kAppendThreads / 32];
+  const int index = (int)blockIdx.x - a.rotate_ctas;
+  const int lanes = 2 * a.kv.n_kv_heads, slot = index / lanes, head = (index % lanes) >> 1, is_v = index & 1;
+  int count = 0;
+  for (int b = 0; b < a.step.n_seqs; b += kAppendThreads) {
+    const int at = b + (int)threadIdx.x;
+    count += __syncthreads_count(at < a.step.n_seqs && __ldg(a.step.row_start + min(at, a.step.n_seqs)) / kScaleTokens + 2 * at <= slot);
+  }
+  const int seq = count - 1;
+  if (seq < 0) return;
+  const int start = __ldg(a.step.row_start + seq), end = min(__ldg(a.step.row_start + seq + 1), a.step.n_rows), len = __ldg(a.step.seq_lens + seq);
+  const int behind = __ldg(a.step.row_start + seq + 1);
+  const int old_len = len - (behind - start);        // tokens before the step
+  const int group = max(old_len, 0) / kScaleTokens + slot - (start / kScaleTokens + 2 * seq);
+  const int first = group * kScaleTokens;           // position of the group's first token
+  const int lo = max(first, max(old_len, 0)), hi = min(first + kScaleTokens, min(len, old_len + (end - start)));
+  if (start < 0 || lo >= hi) {
+    if (threadIdx.x == 0 && old_len < 0) report_cache(a.dev_status);
+    return;
+  }
+  const int64_t block = pool_block(a.kv, a.step, seq, first);
+  if (block < 0 || old_len < 0) {
+    if (threadIdx.x == 0) report_cache(a.dev_status);
+    if (block < 0) return;
+  }
+  const int off = first % a.kv.block_tokens;
+  const int64_t slab = block * a.kv.n_kv_heads + head;
+  uint8_t* cells = (is_v ? a.kv.v : a.kv.k) + (slab * a.kv.block_tokens + off) * D;
+  float* scale_at = (is_v ? a.kv.v_scale : a.kv.k_scale) + slab * (a.kv.block_tokens / kScaleTokens) + off / kScaleTokens;
+  const RowsView& rows = is_v ? a.v : a.k;
+  const int rot_dim = !is_v && a.rope != nullptr ? a.rot_dim : 0;
+
+  float x[kPer][2][8];
+  bool live[kPer];
+  float top = 0.f;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const int item = i * kAppendThreads + threadIdx.x, pos = first + item / kUnits;
+    const int row = start + (pos - old_len);
+    live[i] = pos >= lo && pos < hi;
+    if (!live[i]) continue;
+    const Unit u = unit_of(item % kUnits, rot_dim, a.interleaved);
+    const int64_t angle_row = a.positions != nullptr ? __ldg(a.positions + row) : pos;
+    if (a.rope != nullptr && (angle_row < 0 || angle_row >= a.n_positions)) {
+      live[i] = false;
+      report_cache(a.dev_status);
+      continue;
+    }
+    const __nv_bfloat16* src = rows.data + row * rows.stride_row + head * rows.stride_head;
+    widen8(load_raw(src + u.first), x[i][0]);
+    widen8(load_raw(src + u.second), x[i][1]);
+    if (u.angle >= 0) {
+      Angles t;
+      load_angles(a.rope, angle_row, a.rot_dim, u.angle, t);
+      rotate(x[i][0], x[i][1], t, a.interleaved);
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) top = fmaxf(top, fmaxf(finite_magnitude(x[i][0][e]), finite_magnitude(x[i][1][e])));
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+  if ((threadIdx.x & 31) == 0) warp_max[threadIdx.x >> 5] = top;
+  const bool partly = lo > first;                   // the group holds tokens from before the step
+  const float held = partly ? *scale_at : 0.f;
+  __syncthreads();                                  // every thread has the old scale before one of them writes the new one
+#pragma unroll
+  for (int w = 0; w < kAppendThreads / 32; ++w) top = fmaxf(top, warp_max[w]);
+  const float scale = fmaxf(held, scale_for(top));
+  if (threadIdx.x == 0 && scale != held) *scale_at = scale;
+  const Divider by{scale, 1.f / scale, (__float_as_uint(scale) & 0x7fffffu) == 0};
+  if (partly && scale != held) {
+    const float ratio = __fdiv_rn(held, scale);
+    for (int i = threadIdx.x; i < (lo - first) * (D / 16); i += kAppendThreads) {
+      uint4* at = reinterpret_cast<uint4*>(cells) + i;
+      uint4 v = *at;
+      uint32_t* w = &v.x;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float2 p = e4m3_pair_value(w[j] & 0xffffu), r = e4m3_pair_value(w[j] >> 16);
+        w[j] = e4m3_pair(p.x * ratio, p.y * ratio) | (e4m3_pair(r.x * ratio, r.y * ratio) << 16);
+      }
+      *at = v;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    if (!live[i]) continue;
+    const int item = i * kAppendThreads + threadIdx.x;
+    const Unit u = unit_of(item % kUnits, rot_dim, a.interleaved);
+    uint8_t* dst = cells + (item / kUnits) * D;
+    *reinterpret_cast<uint2*>(dst + u.first) = bytes8(x[i][0], by);
+    *reinterpret_cast<uint2*>(dst + u.second) = bytes8(x[i][1], by);
+  }
+}
+
+template <int D, int HPT, bool FP8>
+__global__ void __launch_bounds__(kAppendThreads) append_kernel(const __grid_constant__ AppendArgs a) {
+  if (FP8 && (int)blockIdx.x >= a.rotate_ctas) fill_group<D>(a);
+  else move_rows<D, HPT, FP8>(a);
+}
+
+template <int D, bool FP8>
+int32_t launch_append(AppendArgs& a, cudaStream_t stream) {
+  const int turned = a.n_q_heads + (FP8 ? 0 : a.kv.n_kv_heads), copied = FP8 ? 0 : a.kv.n_kv_heads;
+  // one head a thread while that does not fill the chip, four where it does: a row's angles are then read once for four heads
+  const int64_t items1 = (int64_t)a.step.n_rows * (turned + copied) * (D / 16);
+  const bool many = items1 > 148 * 2048;
+  const int hpt = many ? 4 : 1;
+  const int64_t items = (int64_t)a.step.n_rows * (ceil_div(turned, hpt) + ceil_div(copied, hpt)) * (D / 16);
+  const int64_t rotate = ceil_div(items, kAppendThreads);
+  const int64_t groups = FP8 ? (a.step.n_rows / kScaleTokens + 2 * (int64_t)a.step.n_seqs) * 2 * a.kv.n_kv_heads : 0;
+  if (rotate + groups > 0x7fffffffLL) return fail(SPF_ERR_UNSUPPORTED, "spf_kv_append: too many rows for one launch");
+  if (rotate + groups == 0) return SPF_OK;
+  a.rotate_ctas = (int)rotate;
+  if (many) append_kernel<D, 4, FP8><<<(unsigned)(rotate + groups), kAppendThreads, 0, stream>>>(a);
+  else append_kernel<D, 1, FP8><<<(unsigned)(rotate + groups), kAppendThreads, 0, stream>>>(a);
+  SPF_CUDA_CHECK(cudaGetLastError());
+  return SPF_OK;
+}
+
+}  // namespace
+
+int32_t check_cache(const char* who, const spf_kv_cache* c, KvView* out) {
+  if (c == nullptr) return fail(SPF_ERR_INVALID_ARG, "%s: cache is null", who);
+  if (c->k_pool == nullptr || c->v_pool == nullptr) return fail(SPF_ERR_INVALID_ARG, "%s: k_pool or v_pool is null", who);
+  if ((c->k_scale == nullptr) != (c->v_scale == nullptr))
+    return fail(SPF_ERR_INVALID_ARG, "%s: k_scale and v_scale are both given (8-bit pools) or both null (bf16 pools)", who);
+  if (reinterpret_cast<uintptr_t>(c->k_pool) % 16 != 0 || reinterpret_cast<uintptr_t>(c->v_pool) % 16 != 0)
+    return fail(SPF_ERR_INVALID_ARG, "%s: k_pool or v_pool is not 16-byte aligned", who);
+  if (reinterpret_cast<uintptr_t>(c->k_scale) % 4 != 0 || reinterpret_cast<uintptr_t>(c->v_scale) % 4 != 0)
+    return fail(SPF_ERR_INVALID_ARG, "%s: k_scale or v_scale is not 4-byte aligned", who);
+  if (c->n_pool_blocks < 1 || c->n_kv_heads < 1) return fail(SPF_ERR_INVALID_ARG, "%s: the pool has no blocks or no heads", who);
+  if (c->block_tokens < 128 || c->block_tokens % 128 != 0)
+    return fail(SPF_ERR_INVALID_ARG, "%s: block_tokens must be a positive multiple of 128 (got %d)", who, c->block_tokens);
+  if (c->head_dim != 64 && c->head_dim != 128)
+    return fail(SPF_ERR_UNSUPPORTED, "%s: head_dim must be 64 or 128 (got %d)", who, c->head_dim);
+  const int64_t per_block = (int64_t)c->n_kv_heads * c->block_tokens;
+  if (per_block > 0x7fffffffLL || c->n_pool_blocks > 0x7fffffffLL / per_block)
+    return fail(SPF_ERR_UNSUPPORTED, "%s: n_pool_blocks * n_kv_heads * block_tokens is 2^31 or more", who);
+  *out = KvView{static_cast<uint8_t*>(c->k_pool), static_cast<uint8_t*>(c->v_pool), c->k_scale, c->v_scale, c->n_pool_blocks,
+                c->block_tokens, c->n_kv_heads};
+  return SPF_OK;
+}
+
+int32_t check_step(const char* who, const spf_kv_step* s, StepView* out) {
+  if (s == nullptr) return fail(SPF_ERR_INVALID_ARG, "%s: step is null", who);
+  if (s->n_seqs < 1 || s->n_seqs > (1 << 20) || s->n_rows < 0 || s->n_rows > (1 << 30) || s->max_new < 1 || s->table_stride < 1)
+    return fail(SPF_ERR_INVALID_ARG, "%s: n_seqs, max_new and table_stride must be positive (n_seqs at most 2^20), n_rows in [0, 2^30]", who);
+  if (s->row_start == nullptr || s->seq_lens == nullptr || s->block_table == nullptr)
+    return fail(SPF_ERR_INVALID_ARG, "%s: row_start, seq_lens or block_table is null", who);
+  *out = StepView{s->row_start, s->seq_lens, s->block_table, s->n_seqs, s->n_rows, s->table_stride};
+  return SPF_OK;
+}
+
+int32_t check_rows(const char* who, const char* name, const spf_rows* r, int n_heads, int head_dim, bool written, RowsView* out) {
+  if (r == nullptr || r->data == nullptr) return fail(SPF_ERR_INVALID_ARG, "%s: %s is null", who, name);
+  if (reinterpret_cast<uintptr_t>(r->data) % 16 != 0) return fail(SPF_ERR_INVALID_ARG, "%s: %s is not 16-byte aligned", who, name);
+  if (r->stride_row % 8 != 0 || r->stride_head % 8 != 0 || r->stride_row < 0 || r->stride_head < 0)
+    return fail(SPF_ERR_INVALID_ARG, "%s: the strides of %s must be multiples of 8, not negative", who, name);
+  if (written && (r->stride_row < head_dim || (n_heads > 1 && r->stride_head < head_dim)))
+    return fail(SPF_ERR_INVALID_ARG, "%s: heads or rows of %s overlap", who, name);
+  *out = RowsView{static_cast<__nv_bfloat16*>(r->data), r->stride_row, r->stride_head};
+  return SPF_OK;
+}
+
+}  // namespace spf
+
+using namespace spf;
+
+extern "C" int32_t spf_kv_append(const spf_kv_cache* cache, const spf_kv_step* step, const spf_rope* rope, const spf_rows* k,
+                                 const spf_rows* v, const spf_rows* q, const spf_rows* q_out, int32_t n_q_heads,
+                                 int32_t* dev_status, void* cuda_stream) {
+  const char* who = "spf_kv_append";
+  clear_error();
+  AppendArgs a{};
+  int32_t st = check_cache(who, cache, &a.kv);
+  if (st == SPF_OK) st = check_step(who, step, &a.step);
+  if (st == SPF_OK && step->n_rows == 0) return SPF_OK;
+  if (st == SPF_OK) st = check_rows(who, "k", k, cache->n_kv_heads, cache->head_dim, false, &a.k);
+  if (st == SPF_OK) st = check_rows(who, "v", v, cache->n_kv_heads, cache->head_dim, false, &a.v);
+  if (st != SPF_OK) return st;
+  if ((q == nullptr) != (q_out == nullptr)) return fail(SPF_ERR_INVALID_ARG, "%s: q and q_out are both given or both null", who);
+  if (q != nullptr) {
+    if (n_q_heads < 1) return fail(SPF_ERR_INVALID_ARG, "%s: n_q_heads must be positive", who);
+    st = check_rows(who, "q", q, n_q_heads, cache->head_dim, false, &a.q);
+    if (st == SPF_OK) st = check_rows(who, "q_out", q_out, n_q_heads, cache->head_dim, true, &a.q_out);
+    if (st != SPF_OK) return st;
+    if (q->data == q_out->data && (q->stride_row != q_out->stride_row || q->stride_head != q_out->stride_head))
+      return fail(SPF_ERR_INVALID_ARG, "%s: q_out overlaps q with other strides", who);
+    a.n_q_heads = n_q_heads;
+  }
+  if (rope != nullptr) {
+    if (rope->table == nullptr || reinterpret_cast<uintptr_t>(rope->table) % 16 != 0)
+      return fail(SPF_ERR_INVALID_ARG, "%s: the rotation's table is null or not 16-byte aligned", who);
+    if (rope->n_positions < 1 || rope->rot_dim < 16 || rope->rot_dim % 16 != 0 || rope->rot_dim > cache->head_dim)
+      return fail(SPF_ERR_INVALID_ARG, "%s: rot_dim must be a multiple of 16 in [16, head_dim] and n_positions positive", who);
+    a.rope = rope->table;
+    a.positions = rope->positions;
+    a.n_positions = rope->n_positions;
+    a.rot_dim = rope->rot_dim;
+    a.interleaved = rope->interleaved != 0;
+  }
+  a.dev_status = dev_status;
+  const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+  if (cache->k_scale != nullptr) return cache->head_dim == 64 ? launch_append<64, true>(a, stream) : launch_append<128, true>(a, stream);
+  return cache->head_dim == 64 ? launch_append<64, false>(a, stream) : launch_append<128, false>(a, stream);
+}

@@ -8,6 +8,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <ATen/ATen.h>
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 
 #include <string>
@@ -61,7 +62,7 @@ const at::Tensor& device_tensor(PyObject* o, at::ScalarType dtype, const char* n
 struct Names {
   PyObject *importance, *lse, *chunk_scores, *kept, *out_ids, *out_pos, *tok_spans, *char_spans, *counts, *dev_status, *workspace, *chunk,
       *pool_kernel, *softmax_scale, *pool_edge_rule, *force_first, *force_last, *max_tokens, *slots, *q, *k, *token_ids, *char_start,
-      *char_end, *n_tokens;
+      *char_end, *n_tokens, *k_pool, *v_pool, *k_scale, *v_scale, *row_start, *seq_lens, *block_table, *max_new, *table, *positions, *interleaved;
 };
 Names N;
 
@@ -451,7 +452,141 @@ PyObject* compress_host(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
   }
 }
 
+// ---------------------------------------------------------------------------------------------- the draft model's cache
+// The tensors of one call on a cache, all of them on one device, held until its kernels are enqueued.
+struct Held {
+  std::vector<at::Tensor> tensors;
+  const at::Tensor& keep(const at::Tensor& t, const char* name) {
+    if (!tensors.empty() && t.device() != tensors.front().device())
+      raise(PyExc_ValueError, std::string(name) + " is on another device than the cache");
+    tensors.push_back(t);
+    return tensors.back();
+  }
+  const at::Tensor& keep_attr(PyObject* o, PyObject* name, at::ScalarType dtype, const char* what) {
+    return keep(device_tensor(attr(o, name).p, dtype, what), what);
+  }
+};
+
+spf_kv_cache read_cache(PyObject* o, Held* held) {
+  spf_kv_cache c{};
+  const Ref scale(attr(o, N.k_scale)), v_scale(attr(o, N.v_scale));
+  if ((scale.p == Py_None) != (v_scale.p == Py_None)) raise(PyExc_ValueError, "k_scale and v_scale are both given (8-bit pools) or both None (bf16 pools)");
+  const bool bits8 = scale.p != Py_None;
+  const at::ScalarType type = bits8 ? at::kByte : at::kBFloat16;
+  held->tensors.reserve(16);
+  const at::Tensor& k = held->keep_attr(o, N.k_pool, type, "k_pool");
+  const at::Tensor& v = held->keep_attr(o, N.v_pool, type, "v_pool");
+  if (k.dim() != 4 || k.sizes() != v.sizes() || !k.is_contiguous() || !v.is_contiguous())
+    raise(PyExc_ValueError, "k_pool and v_pool must be contiguous [n_pool_blocks, Hkv, block_tokens, d] of one shape");
+  if (k.size(1) > INT32_MAX || k.size(2) > INT32_MAX || k.size(3) > INT32_MAX) raise(PyExc_ValueError, "the pool is too large");
+  c.k_pool = k.data_ptr();
+  c.v_pool = v.data_ptr();
+  c.n_pool_blocks = k.size(0);
+  c.n_kv_heads = (int32_t)k.size(1);
+  c.block_tokens = (int32_t)k.size(2);
+  c.head_dim = (int32_t)k.size(3);
+  if (bits8) {
+    const at::Tensor* scales[2] = {&held->keep(device_tensor(scale.p, at::kFloat, "k_scale"), "k_scale"),
+                                   &held->keep(device_tensor(v_scale.p, at::kFloat, "v_scale"), "v_scale")};
+    for (const at::Tensor* t : scales)
+      if (t->dim() != 3 || !t->is_contiguous() || t->size(0) != k.size(0) || t->size(1) != k.size(1) || t->size(2) != k.size(2) / SPF_KV_SCALE_TOKENS)
+        raise(PyExc_ValueError, "k_scale and v_scale must be contiguous fp32 [n_pool_blocks, Hkv, block_tokens / 64]");
+    c.k_scale = scales[0]->data_ptr<float>();
+    c.v_scale = scales[1]->data_ptr<float>();
+  }
+  return c;
+}
+
+spf_kv_step read_step(PyObject* o, int64_t n_rows, Held* held) {
+  spf_kv_step s{};
+  const at::Tensor& start = held->keep_attr(o, N.row_start, at::kInt, "row_start");
+  const at::Tensor& lens = held->keep_attr(o, N.seq_lens, at::kInt, "seq_lens");
+  const at::Tensor& table = held->keep_attr(o, N.block_table, at::kInt, "block_table");
+  const int64_t n = lens.numel(), max_new = attr_int(o, N.max_new);
+  if (start.dim() != 1 || lens.dim() != 1 || start.numel() != n + 1 || !start.is_contiguous() || !lens.is_contiguous())
+    raise(PyExc_ValueError, "row_start must be contiguous [n_seqs + 1] and seq_lens contiguous [n_seqs]");
+  if (table.dim() != 2 || table.size(0) != n || !table.is_contiguous() || table.size(1) > INT32_MAX)
+    raise(PyExc_ValueError, "block_table must be contiguous [n_seqs, blocks]");
+  if (n > INT32_MAX || n_rows > INT32_MAX || max_new < 1 || max_new > INT32_MAX) raise(PyExc_ValueError, "max_new must be positive, and the step smaller");
+  s.n_seqs = (int32_t)n;
+  s.n_rows = (int32_t)n_rows;
+  s.max_new = (int32_t)max_new;
+  s.table_stride = (int32_t)table.size(1);
+  s.row_start = start.data_ptr<int32_t>();
+  s.seq_lens = lens.data_ptr<int32_t>();
+  s.block_table = table.data_ptr<int32_t>();
+  return s;
+}
+
+// bf16 [rows, heads, d] with any strides of rows and heads.  A dimension of one element has no stride of its own.
+spf_rows read_rows(PyObject* o, const char* name, int64_t n_rows, int64_t n_heads, int64_t d, Held* held) {
+  const at::Tensor& t = held->keep(device_tensor(o, at::kBFloat16, name), name);
+  if (t.dim() != 3 || t.size(0) != n_rows || (n_heads >= 0 && t.size(1) != n_heads) || t.size(2) != d || t.stride(2) != 1)
+    raise(PyExc_ValueError, std::string(name) + " must be [rows, heads, d] of the step and the cache, the last dimension contiguous");
+  return spf_rows{t.data_ptr(), t.size(0) > 1 ? t.stride(0) : d, t.size(1) > 1 ? t.stride(1) : d};
+}
+
+int32_t* read_status(PyObject* o, Held* held) {
+  if (o == Py_None) return nullptr;
+  const at::Tensor& t = held->keep(device_tensor(o, at::kInt, "dev_status"), "dev_status");
+  if (t.numel() < 1) raise(PyExc_ValueError, "dev_status must hold one int32");
+  return t.data_ptr<int32_t>();
+}
+
+// The stream of a call on a cache: the one given, else the current one of the cache's device (not of the current device).
+void* stream_on(PyObject* stream, const Held& held) {
+  if (stream == Py_None) return c10::cuda::getCurrentCUDAStream(held.tensors.front().device().index()).stream();
+  return stream_of(stream);
+}
+
+// kv_append(cache, step, k, v, q, q_out, rope, dev_status, stream) -> status
+PyObject* kv_append(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
+  try {
+    if (n_args != 9) raise(PyExc_TypeError, "kv_append takes 9 arguments");
+    Held held;
+    const spf_kv_cache cache = read_cache(args[0], &held);
+    const at::Tensor& k0 = device_tensor(args[2], at::kBFloat16, "k");
+    const int64_t n_rows = k0.dim() > 0 ? k0.size(0) : 0;
+    const spf_kv_step step = read_step(args[1], n_rows, &held);
+    const spf_rows k = read_rows(args[2], "k", n_rows, cache.n_kv_heads, cache.head_dim, &held);
+    const spf_rows v = read_rows(args[3], "v", n_rows, cache.n_kv_heads, cache.head_dim, &held);
+    spf_rows q{}, q_out{};
+    int64_t n_q_heads = 0;
+    if ((args[4] == Py_None) != (args[5] == Py_None)) raise(PyExc_ValueError, "q and q_out are both given or both None");
+    const bool queries = args[4] != Py_None;
+    if (queries) {
+      q = read_rows(args[4], "q", n_rows, -1, cache.head_dim, &held);
+      n_q_heads = held.tensors.back().size(1);
+      q_out = read_rows(args[5], "q_out", n_rows, n_q_heads, cache.head_dim, &held);
+    }
+    spf_rope rope{};
+    if (args[6] != Py_None) {
+      const at::Tensor& table = held.keep_attr(args[6], N.table, at::kFloat, "rope.table");
+      if (table.dim() != 2 || !table.is_contiguous() || table.size(0) > INT32_MAX || table.size(1) > INT32_MAX)
+        raise(PyExc_ValueError, "rope.table must be contiguous fp32 [n_positions, rot_dim]");
+      rope = spf_rope{table.data_ptr<float>(), nullptr, (int32_t)table.size(0), (int32_t)table.size(1), attr_true(args[6], N.interleaved)};
+      const Ref positions(attr(args[6], N.positions));
+      if (positions.p != Py_None) {
+        const at::Tensor& t = held.keep(device_tensor(positions.p, at::kInt, "rope.positions"), "rope.positions");
+        if (t.numel() != n_rows || !t.is_contiguous()) raise(PyExc_ValueError, "rope.positions must be contiguous int32 [rows]");
+        rope.positions = t.data_ptr<int32_t>();
+      }
+    }
+    int32_t* status = read_status(args[7], &held);
+    const c10::cuda::CUDAGuard guard(held.tensors.front().device());
+    void* stream = stream_on(args[8], held);
+    return PyLong_FromLong(spf_kv_append(&cache, &step, args[6] != Py_None ? &rope : nullptr, &k, &v, queries ? &q : nullptr,
+                                         queries ? &q_out : nullptr, (int32_t)n_q_heads, status, stream));
+  } catch (const PyFailure&) {
+    return nullptr;
+  } catch (const std::exception& e) {
+    PyErr_SetString(PyExc_RuntimeError, e.what());
+    return nullptr;
+  }
+}
+
 PyMethodDef kMethods[] = {
+    {"kv_append", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(kv_append)), METH_FASTCALL, "A step's keys and values into the cache."},
     {"select", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(select_one)), METH_FASTCALL, "The path for one prompt."},
     {"select_batch", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(select_batch)), METH_FASTCALL, "The path for a batch of prompts."},
     {"compress_host", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(compress_host)), METH_FASTCALL, "The path for one prompt in host tensors."},
@@ -467,6 +602,8 @@ PyMODINIT_FUNC PyInit__native() {
   SPF_NAME(char_spans); SPF_NAME(counts); SPF_NAME(dev_status); SPF_NAME(workspace); SPF_NAME(chunk); SPF_NAME(pool_kernel);
   SPF_NAME(softmax_scale); SPF_NAME(pool_edge_rule); SPF_NAME(force_first); SPF_NAME(force_last); SPF_NAME(max_tokens); SPF_NAME(slots);
   SPF_NAME(q); SPF_NAME(k); SPF_NAME(token_ids); SPF_NAME(char_start); SPF_NAME(char_end); SPF_NAME(n_tokens);
+  SPF_NAME(k_pool); SPF_NAME(v_pool); SPF_NAME(k_scale); SPF_NAME(v_scale); SPF_NAME(row_start); SPF_NAME(seq_lens); SPF_NAME(block_table);
+  SPF_NAME(max_new); SPF_NAME(table); SPF_NAME(positions); SPF_NAME(interleaved);
 #undef SPF_NAME
   return PyModule_Create(&kModule);
 }
