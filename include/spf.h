@@ -310,6 +310,41 @@ SPF_API int32_t spf_kv_append(const spf_kv_cache* cache, const spf_kv_step* step
                               int32_t* dev_status, void* cuda_stream);
 
 /*
+ * Attention of a step's tokens over the cache (the new tokens' own keys and values are in it already: spf_kv_append comes
+ * first).  Row t, place p in its sequence of n tokens, head h:
+ *     out[t,h] = sum_s w_s V[h / G, s],   w = softmax over s of softmax_scale * q[t,h] . K[h / G, s],
+ *     s from first_key to p (to n - 1 where see_all)
+ * A row without keys gets zeros, and -inf as its lse.  bf16 queries and outputs, fp32 softmax and sums.
+ *   q, out        bf16, n_q_heads heads a row (a multiple of the cache's heads); out must not overlap q
+ *   softmax_scale <= 0 selects 1/sqrt(d)
+ *   options       NULL: causal, from key 0 on, without lse
+ *     lse         fp32, element (row, head) at row * lse_stride_row + head * lse_stride_head: the natural log of the sum of
+ *                 exp over the keys that the row sees; may be NULL.  With first_keys = the prompt's length it is what
+ *                 spf_score_extra takes.
+ *     first_keys  DEVICE int32 [n_seqs], may be NULL: the first key that rows of a sequence see (negative: 0)
+ *     see_all     nonzero: rows see all n keys, also those behind them (lookahead queries over a prompt)
+ *   workspace     DEVICE, 256-byte aligned, spf_attend_workspace_bytes() of a step whose max_new is at least this one's;
+ *                 contents irrelevant on entry, unspecified on exit.  Calls that share one must be ordered on one stream.
+ * What the pools hold behind a sequence's tokens, or before its first key, does not matter.
+ * 8-bit pools: values of bytes times scales are exact; their scales should lie within 2^-100 ... 2^100.
+ * Device conditions (dev_status, may be NULL): SPF_ERR_CACHE: a length beyond the block table, more new tokens than the
+ * sequence is long, or a block outside the pool, whose keys and values then read as zeros; SPF_ERR_TIMEOUT as for spf_score.
+ * Errors: SPF_ERR_INVALID_ARG, SPF_ERR_UNSUPPORTED (head_dim, heads, the cache's limit), SPF_ERR_WORKSPACE, SPF_ERR_CUDA.
+ */
+typedef struct {
+  float* lse;
+  int64_t lse_stride_row;
+  int64_t lse_stride_head;
+  const int32_t* first_keys;
+  int32_t see_all;
+} spf_attend_options;
+
+SPF_API size_t spf_attend_workspace_bytes(const spf_kv_cache* cache, int32_t n_q_heads, int32_t max_new);
+SPF_API int32_t spf_attend(const spf_kv_cache* cache, const spf_kv_step* step, const spf_rows* q, const spf_rows* out,
+                           int32_t n_q_heads, float softmax_scale, const spf_attend_options* options, void* workspace,
+                           size_t workspace_bytes, int32_t* dev_status, void* cuda_stream);
+
+/*
  * One long prompt over several GPUs (Appendix A.1.1 is per prompt; this shards its keys).  Each rank holds a contiguous
  * range of the prompt's keys for all layers and describes it as an spf_prompt of its own (n_tokens = the range's
  * length).  A softmax row spans all ranks, so scoring takes two calls with one exchange between them:

@@ -86,6 +86,11 @@ class _Rows(ctypes.Structure):
     _fields_ = [("data", ctypes.c_void_p), ("stride_row", ctypes.c_int64), ("stride_head", ctypes.c_int64)]
 
 
+class _AttendOptions(ctypes.Structure):
+    _fields_ = [("lse", ctypes.c_void_p), ("lse_stride_row", ctypes.c_int64), ("lse_stride_head", ctypes.c_int64),
+                ("first_keys", ctypes.c_void_p), ("see_all", ctypes.c_int32)]
+
+
 def _load() -> ctypes.CDLL:
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"{LIB_PATH} is missing: build it with `python -m paper_2603_02631_b200.build` "
@@ -146,6 +151,11 @@ def _load() -> ctypes.CDLL:
     dll.spf_kv_append.restype = i32
     dll.spf_kv_append.argtypes = [ctypes.POINTER(_KvCache), ctypes.POINTER(_KvStep), ctypes.POINTER(_Rope), ctypes.POINTER(_Rows),
                                   ctypes.POINTER(_Rows), ctypes.POINTER(_Rows), ctypes.POINTER(_Rows), i32, vp, vp]
+    dll.spf_attend_workspace_bytes.restype = ctypes.c_size_t
+    dll.spf_attend_workspace_bytes.argtypes = [ctypes.POINTER(_KvCache), i32, i32]
+    dll.spf_attend.restype = i32
+    dll.spf_attend.argtypes = [ctypes.POINTER(_KvCache), ctypes.POINTER(_KvStep), ctypes.POINTER(_Rows), ctypes.POINTER(_Rows), i32,
+                               ctypes.c_float, ctypes.POINTER(_AttendOptions), vp, ctypes.c_size_t, vp, vp]
     dll.spf_keep_count.restype = i64
     dll.spf_keep_count.argtypes = [i64, ctypes.c_double]
     dll.spf_keep_rate.restype = ctypes.c_double
@@ -684,6 +694,23 @@ def spf_kv_append(cache: KvCache, step: KvStep, k: torch.Tensor, v: torch.Tensor
     """Rotates a step's keys (and queries, into ``q_out``) and appends keys and values to the cache.  k, v: bf16 [rows, Hkv, d];
     q, q_out: bf16 [rows, Hq, d]; rows and heads may have any strides that are multiples of 8."""
     _check(_native.kv_append(cache, step, k, v, q, q_out, rope, dev_status, stream), "spf_kv_append")
+
+
+def spf_attend_workspace_bytes(cache: KvCache, step: KvStep, q: torch.Tensor) -> int:
+    """Bytes of workspace for steps like this one, whose ``max_new`` is no larger."""
+    n = int(_native.attend_workspace_bytes(cache, step, q))
+    if n == 0:
+        raise SpfError(-1, "spf_attend_workspace_bytes", spf_last_error())
+    return n
+
+
+def spf_attend(cache: KvCache, step: KvStep, q: torch.Tensor, out: torch.Tensor, workspace: torch.Tensor,
+               lse: Optional[torch.Tensor] = None, first_keys: Optional[torch.Tensor] = None, causal: bool = True,
+               softmax_scale: float = 0.0, dev_status: Optional[torch.Tensor] = None,
+               stream: Optional[torch.cuda.Stream] = None) -> None:
+    """Attention of a step's tokens over the cache, their own keys and values (spf_kv_append) included.  q, out: bf16
+    [rows, Hq, d]; lse: fp32 [rows, Hq] of any strides; first_keys: int32 [n_seqs], the first key that a sequence's rows see."""
+    _check(_native.attend(cache, step, q, out, workspace, lse, first_keys, causal, softmax_scale, dev_status, stream), "spf_attend")
 
 
 @dataclasses.dataclass

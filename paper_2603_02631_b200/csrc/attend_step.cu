@@ -1,0 +1,806 @@
+// Attention of a step with few rows per key head (single tokens, lookahead tokens) over the paged cache, bf16 or 8 bits.
+//
+//   z[r, s] = c q[r] . k[s]  (base-2 logits),   out[r] = sum_s 2^(z[r,s] - m_r) v[s] / l_r,   l_r = sum_s 2^(z[r,s] - m_r),
+//   lse[r] = (m_r + log2 l_r) ln 2;   rows r = (new token i, head g of the key head's group), r = i G + g, in tiles of R.
+//
+// One pass over keys and values, each read once for all rows of a tile.  What bounds it is that read, so the work is dealt out
+// by key tiles, not by sequences: the tiles of all (sequence, row tile, key head) triples, 64 keys each, form one list, and CTA
+// c takes its c-th part, wherever that begins and ends.  A triple that one CTA has from end to end is written at once; one that
+// several share leaves partial sums in the workspace, and a second kernel (launched behind the first without waiting for the
+// host) joins them in the order of the keys.  All of it is worked out on the device from the lengths there.
+//
+// A CTA: one warp copies tiles into a ring (TMA, 64 keys and their values a stage) and runs ahead across the triples' borders;
+// four warps compute, each on its own 16 keys of every tile (32 with 64 rows: two warps share a row half), with maxima, sums and
+// outputs of their own in registers, so that nothing is exchanged between them until a triple ends.  Products are warp-level
+// (m16n8k16): with at most 16 rows in a tile the tensor cores' big instruction would be idle for the most part, and the keys'
+// read takes longer than these.
+//
+// The reference m_r moves only when a logit exceeds it by 8 (2^8 is far from any format's limit): most tiles need no exchange
+// of maxima and no rescaling of the output.  Weights are rounded to the format of the second product's operands: bf16 (8 bits;
+// the output is bf16 too) over bf16 values, fp16 (11 bits) over 8-bit ones; their sum l is taken in fp32 before that.
+//
+// 8 bits: E4M3 is widened to fp16, exactly, next to the products.  Queries become fp16 after a power of two per row that puts
+// the largest element in [2^14, 2^15): exact for elements within 2^-29 of it.  A tile's value scale s_v joins its logits, so that the
+// weights are p s_v / (the largest such so far) and never leave fp16's range, and l takes them divided by s_v again:
+//   z'[r,s] = z[r,s] + log2 s_v,  w = 2^(z' - m' + 7),  out = sum w byte / l,  l = sum w / s_v,  lse = (m' - 7 + log2 l) ln 2.
+//
+// Keys that no row may see (behind the sequence's end, before its first key) take part with logits of -inf and values of zero,
+// whatever the pool holds there.  Keys that only later rows of the step may see have weight zero; if their values are not
+// finite, the tile's second product is made row by row, so that they reach the rows that see them and no others.
+#include <algorithm>
+
+#include "attend.cuh"
+
+namespace spf {
+namespace {
+
+constexpr int kKeys = 64;               // keys of a tile: one scale's worth
+constexpr int kWarps = 4;               // that compute
+constexpr int kThreads = (kWarps + 1) * 32;
+constexpr int kCtasPerSm = 2;
+constexpr int kMaxStages = 8;
+constexpr float kLazy = 8.f;            // how far logits may exceed their reference
+constexpr float kShift = 7.f;           // 8-bit values: weights reach 2^(kLazy + kShift) = 2^15, below fp16's 65504
+
+// What the copying warp tells the computing ones about a stage.
+struct TileDesc {
+  int row0, n_new, pos0, first, end, head, row_tile, key0;
+  float k_scale, v_log2, v_inverse;     // 8 bits
+  int flags;                            // kFirst, kLast, kNoKeys; bits 8 ...: CTAs behind this one with parts of the triple
+};
+enum : int { kFirst = 1, kLast = 2, kNoKeys = 4, kFromStart = 8, kToEnd = 16 };
+
+template <int D_, bool FP8_, int R_>
+struct Traits {
+  static constexpr int D = D_, R = R_;
+  static constexpr bool FP8 = FP8_;
+  static constexpr int WR = R == 64 ? 2 : 1, WK = kWarps / WR;        // warps over rows, over keys
+  static constexpr int MT = R / (16 * WR);                            // 16-row tiles of a warp
+  static constexpr int KW = kKeys / WK, NT = KW / 8;                  // keys of a warp in a tile
+  static constexpr int ROWB = FP8 ? D : 2 * D, SPAN = ROWB < 128 ? ROWB : 128, SPANS = ROWB / SPAN;
+  static constexpr int TILE = kKeys * ROWB, STAGE = 2 * TILE;
+  static constexpr int QBYTES = R * D * 2;
+  static constexpr int FIT = (112 * 1024 - 4096 - QBYTES) / STAGE;
+  static constexpr int STAGES = FIT < kMaxStages ? FIT : kMaxStages;
+  static constexpr int JOIN = D * WK * R * 4 <= STAGE ? D : STAGE / (WK * R * 4);   // output columns joined at a time
+};
+
+struct SmallSmem {
+  unsigned long long full[kMaxStages], empty[kMaxStages], join;
+  TileDesc desc[kMaxStages];
+  float2 stats[kWarps][64];             // (m, l) of the warps' rows
+  int64_t scan[kThreads / 32];
+  int64_t total, start_base;
+  int start_seq;
+  int abort;
+};
+
+template <class T>
+constexpr int smem_bytes() { return T::STAGES * T::STAGE + T::QBYTES + (int)sizeof(SmallSmem) + 1024; }
+
+struct StepArgs {
+  AttendArgs a;
+  CUtensorMap k_map, v_map;
+  float* partial;                 // [2 ctas][R][D], [2 ctas][R] (m, l), headers
+  float2* partial_stats;
+  int4* headers;                  // per CTA: (CTAs behind it with parts of its last triple, row0, head, row tile), rows in .y2
+  int min_tiles;
+};
+
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+  const __half2 v = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+__device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
+}
+__device__ __forceinline__ void ldsm4_t(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
+}
+
+template <bool FP8>
+__device__ __forceinline__ void mma16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  if constexpr (FP8)
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+  else
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+// Four E4M3 bytes as two pairs of fp16, in order.
+__device__ __forceinline__ void widen4(uint32_t four, uint32_t& lo, uint32_t& hi) {
+  asm("{\n.reg .b16 a, b;\nmov.b32 {a, b}, %2;\ncvt.rn.f16x2.e4m3x2 %0, a;\ncvt.rn.f16x2.e4m3x2 %1, b;\n}" : "=r"(lo), "=r"(hi) : "r"(four));
+}
+
+// Byte offset of the 16-byte chunk `chunk` of row `row` in a tile, as the copies' swizzle lays it: spans of 128 (or 64) bytes
+// one after the other, the chunk's place in its span exchanged by the row.
+template <class T>
+__device__ __forceinline__ uint32_t tile_chunk(int row, int chunk) {
+  if constexpr (T::SPAN == 64) return (uint32_t)(row * 64 + ((chunk ^ (row >> 1)) & 3) * 16);
+  return (uint32_t)((chunk >> 3) * (kKeys * 128) + row * 128 + ((chunk ^ row) & 7) * 16);
+}
+// The same for the query tile, rows of 2 D bytes.
+template <class T>
+__device__ __forceinline__ uint32_t q_chunk(int row, int chunk) {
+  return (uint32_t)(row * (2 * T::D) + ((chunk & ~7) | ((chunk ^ row) & 7)) * 16);
+}
+
+// ---------------------------------------------------------------------------------------------- the list of tiles
+__device__ __forceinline__ int tiles_of(const SeqSpan& s) { return max((s.end + kKeys - 1) / kKeys - s.first / kKeys, 1); }
+template <class T>
+__device__ __forceinline__ int row_tiles_of(const AttendArgs& a, const SeqSpan& s) {
+  return (int)(((int64_t)s.n_new * a.group + T::R - 1) / T::R);
+}
+template <class T>
+__device__ __forceinline__ int64_t cost_of(const AttendArgs& a, int b) {
+  const SeqSpan s = seq_span(a, b);
+  return (int64_t)row_tiles_of<T>(a, s) * a.kv.n_kv_heads * tiles_of(s);
+}
+
+// Length of the list, and the sequence that holds the CTA's first tile.  Every thread sums up a run of sequences.
+template <class T>
+__device__ __forceinline__ void find_start(const StepArgs& args, SmallSmem& sm) {
+  const AttendArgs& a = args.a;
+  const int run = (a.step.n_seqs + kThreads - 1) / kThreads, lo = min((int)threadIdx.x * run, a.step.n_seqs), hi = min(lo + run, a.step.n_seqs);
+  int64_t mine = 0;
+  for (int b = lo; b < hi; ++b) mine += cost_of<T>(a, b);
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int64_t upto = mine;                                   // sum over the threads up to this one
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int64_t v = __shfl_up_sync(0xffffffffu, upto, o);
+    if (lane >= o) upto += v;
+  }
+  if (lane == 31) sm.scan[warp] = upto;
+  __syncthreads();
+  int64_t total = 0;
+#pragma unroll
+  for (int w = 0; w < kThreads / 32; ++w) {
+    if (w < warp) upto += sm.scan[w];
+    total += sm.scan[w];
+  }
+  const int64_t per = max((int64_t)args.min_tiles, (total + gridDim.x - 1) / gridDim.x), w0 = per * blockIdx.x;
+  if (threadIdx.x == 0) sm.total = total;
+  if (w0 >= upto - mine && w0 < upto) {
+    int64_t base = upto - mine;
+    int b = lo;
+    for (; b < hi - 1; ++b) {
+      const int64_t c = cost_of<T>(a, b);
+      if (w0 < base + c) break;
+      base += c;
+    }
+    sm.start_seq = b;
+    sm.start_base = base;
+  }
+  __syncthreads();
+}
+
+// The copying warp.  Each lane works out one of the next 32 tiles (block table, scales: loads in parallel), then the tiles are
+// put into the ring one by one.
+template <class T>
+__device__ __forceinline__ void copy_tiles(const StepArgs& args, SmallSmem& sm, uint32_t ring, int64_t w0, int64_t w1, int64_t per, const Abort& ab) {
+  const AttendArgs& a = args.a;
+  const int lane = threadIdx.x & 31;
+  const int64_t pool_rows = a.kv.n_blocks * a.kv.n_kv_heads * a.kv.block_tokens;
+  int seq = sm.start_seq;
+  int64_t base = sm.start_base;
+  int stage = 0;
+  int64_t issued = 0;
+  uint32_t parity = 1;                                    // the ring's stages start out empty
+  for (int64_t w = w0; w < w1; w += 32) {
+    const int64_t mine = w + lane;
+    TileDesc d{};
+    int row = 0;
+    if (mine < w1) {
+      SeqSpan s = seq_span(a, seq);
+      int tiles = tiles_of(s), row_tiles = row_tiles_of<T>(a, s);
+      int64_t cost = (int64_t)row_tiles * a.kv.n_kv_heads * tiles;
+      while (mine >= base + cost && seq < a.step.n_seqs - 1) {
+        base += cost;
+        s = seq_span(a, ++seq);
+        tiles = tiles_of(s);
+        row_tiles = row_tiles_of<T>(a, s);
+        cost = (int64_t)row_tiles * a.kv.n_kv_heads * tiles;
+      }
+      const int64_t in_seq = mine - base, triple = in_seq / tiles;
+      const int tile = (int)(in_seq - triple * tiles);
+      const int64_t from = base + triple * tiles, to = from + tiles;      // the triple's place in the list
+      d.row0 = s.row0;
+      d.n_new = s.n_new;
+      d.pos0 = s.pos0;
+      d.first = s.first;
+      d.end = s.end;
+      d.head = (int)(triple / row_tiles);
+      d.row_tile = (int)(triple - (int64_t)d.head * row_tiles);
+      d.key0 = (s.first / kKeys + tile) * kKeys;
+      d.flags = (mine == max(from, w0) ? kFirst : 0) | (mine == min(to, w1) - 1 ? kLast : 0) | (s.first >= s.end ? kNoKeys : 0) |
+                (from >= w0 ? kFromStart : 0) | (to <= w1 ? kToEnd : 0) | ((int)((to - 1) / per - blockIdx.x) << 8);
+      if (s.first < s.end) {
+        row = pool_row(a, seq, d.head, d.key0);
+        if constexpr (T::FP8) {
+          const float v = group_scale(a.kv.v_scale, row, pool_rows);
+          d.k_scale = a.c * group_scale(a.kv.k_scale, row, pool_rows);
+          d.v_log2 = log2f(v);
+          d.v_inverse = 1.f / v;
+        }
+      }
+    }
+    const int count = (int)min((int64_t)32, w1 - w);
+    for (int j = 0; j < count; ++j) {
+      if (!mbar_wait_warp(smem_u32(&sm.empty[stage]), parity, ab)) {
+        // a stage's last copy was its (issued - stage) / STAGES-th, rounded up
+        if (lane < T::STAGES && issued > lane)
+          drain_copy(smem_u32(&sm.full[lane]), (uint32_t)((issued - lane + T::STAGES - 1) / T::STAGES - 1) & 1u);
+        return;
+      }
+      ++issued;
+      if (lane == j) {
+        sm.desc[stage] = d;
+        const uint32_t bar = smem_u32(&sm.full[stage]), at = ring + stage * T::STAGE;
+        if (d.flags & kNoKeys) {
+          mbar_arrive(bar);
+        } else {
+          mbar_expect_tx(bar, T::STAGE);
+          tma_load_3d(at, &args.k_map, 0, row, 0, bar);
+          tma_load_3d(at + T::TILE, &args.v_map, 0, row, 0, bar);
+        }
+      }
+      if (++stage == T::STAGES) stage = 0, parity ^= 1;
+    }
+    seq = __shfl_sync(0xffffffffu, seq, count - 1);
+    base = __shfl_sync(0xffffffffu, base, count - 1);
+  }
+}
+
+// ---------------------------------------------------------------------------------------------- the computing warps
+// Barrier of the computing warps (bounded, as every wait here).
+struct Join {
+  uint32_t bar, parity;
+  __device__ __forceinline__ bool wait(const Abort& ab) {
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) mbar_arrive(bar);
+    const bool ok = mbar_wait_warp(bar, parity, ab);
+    parity ^= 1;
+    return ok;
+  }
+};
+
+// The triple's query rows into shared memory, rows that do not exist as zeros.  8 bits: fp16, scaled per row, and in the order
+// in which 16 bytes of a key meet a product's operand: element 4 c + 2 s + e of 16 at place 2 c + 8 s + e.
+template <class T>
+__device__ __forceinline__ void load_queries(const AttendArgs& a, const TileDesc& d, unsigned char* q_tile, float* q_factor) {
+  constexpr int kChunks = T::D / 8, kLanes = T::FP8 ? T::D / 16 : T::D / 8;     // threads of a row
+  const int total = d.n_new * a.group;
+  for (int item = threadIdx.x; item < T::R * kLanes; item += kWarps * 32) {
+    const int r = item / kLanes, part = item % kLanes, rr = d.row_tile * T::R + r;
+    const __nv_bfloat16* src = a.q.data + (int64_t)(d.row0 + rr / a.group) * a.q.stride_row + (int64_t)(d.head * a.group + rr % a.group) * a.q.stride_head;
+    if constexpr (!T::FP8) {
+      uint4 v = make_uint4(0, 0, 0, 0);
+      if (rr < total) v = __ldg(reinterpret_cast<const uint4*>(src) + part);
+      *reinterpret_cast<uint4*>(q_tile + q_chunk<T>(r, part)) = v;
+    } else {
+      union { uint4 u[2]; __nv_bfloat162 h[8]; } v;
+      v.u[0] = v.u[1] = make_uint4(0, 0, 0, 0);
+      if (rr < total) {
+        v.u[0] = __ldg(reinterpret_cast<const uint4*>(src) + 2 * part);
+        v.u[1] = __ldg(reinterpret_cast<const uint4*>(src) + 2 * part + 1);
+      }
+      float2 f[8];
+      float top = 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        f[i] = __bfloat1622float2(v.h[i]);
+        top = fmaxf(top, fmaxf(fabsf(f[i].x), fabsf(f[i].y)));
+      }
+#pragma unroll
+      for (int o = kLanes / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o, kLanes));
+      // 2^e with top * 2^e in [2^14, 2^15), e clipped where the factor or its inverse would leave fp32's normal range
+      const int e = top > 0.f && top < INFINITY ? min(max(14 - ((int)(__float_as_uint(top) >> 23) - 127), -120), 120) : 0;
+      const float up = __uint_as_float((uint32_t)(e + 127) << 23);
+      union { uint4 u[2]; uint32_t w[8]; } o;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) o.w[(i >> 1) + 4 * (i & 1)] = pack_f16(f[i].x * up, f[i].y * up);
+      *reinterpret_cast<uint4*>(q_tile + q_chunk<T>(r, 2 * part)) = o.u[0];
+      *reinterpret_cast<uint4*>(q_tile + q_chunk<T>(r, 2 * part + 1)) = o.u[1];
+      if (part == 0) q_factor[r] = __uint_as_float((uint32_t)(127 - e) << 23);
+    }
+  }
+  (void)kChunks;
+}
+
+// Values of 16 keys and 16 dimensions as the second product's operands: b[n][0..1] of two 8-wide column tiles.  The columns of
+// bf16 tiles are 16 * np + 8 * n + ..., of 8-bit ones the even and the odd dimensions.
+template <class T>
+__device__ __forceinline__ void load_values(uint32_t v_tile, int key, int np, int lane, uint32_t (&b)[2][2]) {
+  if constexpr (!T::FP8) {
+    uint32_t r[4];
+    ldsm4_t(v_tile + tile_chunk<T>(key + ((lane >> 3) & 1) * 8 + (lane & 7), 2 * np + (lane >> 4)), r);
+    b[0][0] = r[0], b[0][1] = r[1], b[1][0] = r[2], b[1][1] = r[3];
+  }
+}
+template <class T>
+__device__ __forceinline__ void load_values8(uint32_t v_tile, int key, int np2, int lane, uint32_t (&b)[4][2]) {
+  uint32_t r[4];                                         // 16 keys x 32 dimensions
+  ldsm4_t(v_tile + tile_chunk<T>(key + ((lane >> 3) & 1) * 8 + (lane & 7), 2 * np2 + (lane >> 4)), r);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) widen4(__byte_perm(r[i], 0, 0x3120), b[(i >> 1) * 2][i & 1], b[(i >> 1) * 2 + 1][i & 1]);
+}
+
+// Zeroes what belongs to keys outside [lo, hi): the halves of an operand register are keys `key` and `key` + 1.
+__device__ __forceinline__ uint32_t keep_keys(uint32_t pair, int key, int lo, int hi) {
+  uint32_t mask = 0;
+  if (key >= lo && key < hi) mask |= 0x0000ffffu;
+  if (key + 1 >= lo && key + 1 < hi) mask |= 0xffff0000u;
+  return pair & mask;
+}
+template <bool FP8>
+__device__ __forceinline__ bool not_finite(uint32_t pair) {
+  constexpr uint32_t kExp = FP8 ? 0x7c00u : 0x7f80u;
+  return (pair & kExp) == kExp || ((pair >> 16) & kExp) == kExp;
+}
+
+template <class T>
+struct State {
+  float o[T::MT][T::D / 8][4];
+  float m[T::MT][2], l[T::MT][2];
+};
+
+// out += weights . values of the warp's keys.  `guard`: the tile has keys that not every row may see, or keys outside the
+// sequence's range [first, end).
+template <class T>
+__device__ __forceinline__ void add_values(State<T>& st, const uint32_t (&p)[T::MT][T::NT / 2][4], uint32_t v_tile, int key_in_tile, int key0,
+                                           const TileDesc& d, int group, int causal, int row_in_triple, bool guard, int lane) {
+  constexpr int kStep = T::FP8 ? 4 : 2;                  // 8-wide column tiles of one load
+#pragma unroll
+  for (int ks = 0; ks < T::NT / 2; ++ks) {
+#pragma unroll
+    for (int np = 0; np < T::D / 8 / kStep; ++np) {
+      uint32_t b[kStep][2];
+      if constexpr (T::FP8) load_values8<T>(v_tile, key_in_tile + ks * 16, np, lane, b);
+      else load_values<T>(v_tile, key_in_tile + ks * 16, np, lane, b);
+      bool odd = false;
+      if (guard) {
+        const int key = key0 + key_in_tile + ks * 16 + (lane & 3) * 2;
+#pragma unroll
+        for (int n = 0; n < kStep; ++n)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            b[n][h] = keep_keys(b[n][h], key + 8 * h, d.first, d.end);
+            odd |= not_finite<T::FP8>(b[n][h]);
+          }
+        odd = __any_sync(0xffffffffu, odd);
+      }
+      if (!odd) {
+#pragma unroll
+        for (int mt = 0; mt < T::MT; ++mt)
+#pragma unroll
+          for (int n = 0; n < kStep; ++n) mma16<T::FP8>(st.o[mt][np * kStep + n], p[mt][ks], b[n][0], b[n][1]);
+      } else {
+        // values that are not finite, some of which only some rows may see: row by row, each with the values that it sees
+        const int key = key0 + key_in_tile + ks * 16 + (lane & 3) * 2;
+        for (int r = 0; r < 16; ++r)
+#pragma unroll
+          for (int mt = 0; mt < T::MT; ++mt) {
+            const int hi = causal ? min(d.end, d.pos0 + (row_in_triple + mt * 16 + r) / group + 1) : d.end;
+            uint32_t pr[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) pr[e] = (lane >> 2) + 8 * (e & 1) == r ? p[mt][ks][e] : 0u;
+#pragma unroll
+            for (int n = 0; n < kStep; ++n) {
+              float part[4] = {0.f, 0.f, 0.f, 0.f};
+              mma16<T::FP8>(part, pr, keep_keys(b[n][0], key, d.first, hi), keep_keys(b[n][1], key + 8, d.first, hi));
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                if ((lane >> 2) + 8 * (e >> 1) == r) st.o[mt][np * kStep + n][e] += part[e];
+            }
+          }
+      }
+    }
+  }
+}
+
+template <class T>
+__device__ __forceinline__ void compute_tiles(const StepArgs& args, SmallSmem& sm, unsigned char* ring_ptr, uint32_t ring, unsigned char* q_tile,
+                                              int64_t n_tiles, const Abort& ab) {
+  constexpr int D = T::D, R = T::R, MT = T::MT, NT = T::NT;
+  const AttendArgs& a = args.a;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int row_warp = warp % T::WR, key_warp = warp / T::WR, row_off = row_warp * MT * 16, key_off = key_warp * T::KW;
+  const uint32_t q_addr = smem_u32(q_tile);
+  __shared__ float q_factor[R];
+  Join join{smem_u32(&sm.join), 0};
+  State<T> st;
+  float qf[MT][2];
+  uint32_t q[MT == 1 ? D / 16 : 1][4];
+  int stage = 0;
+  uint32_t parity = 0;
+  for (int64_t tile = 0; tile < n_tiles; ++tile) {
+    if (!mbar_wait_warp(smem_u32(&sm.full[stage]), parity, ab)) return;
+    const TileDesc& d = sm.desc[stage];
+    const int flags = d.flags;
+    if (flags & kFirst) {
+      load_queries<T>(a, d, q_tile, q_factor);
+      if (!join.wait(ab)) return;
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          st.m[mt][b] = -INFINITY;
+          st.l[mt][b] = 0.f;
+          if constexpr (T::FP8) qf[mt][b] = q_factor[row_off + mt * 16 + (lane >> 2) + 8 * b];
+        }
+#pragma unroll
+        for (int n = 0; n < D / 8; ++n)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) st.o[mt][n][e] = 0.f;
+      }
+      if constexpr (MT == 1)
+#pragma unroll
+        for (int kk = 0; kk < D / 16; ++kk)
+          ldsm4(q_addr + q_chunk<T>(row_off + (lane & 7) + ((lane >> 3) & 1) * 8, 2 * kk + (lane >> 4)), q[kk]);
+    }
+    if (!(flags & kNoKeys)) {
+      const uint32_t k_tile = ring + stage * T::STAGE, v_tile = k_tile + T::TILE;
+      // logits of the warp's rows and keys
+      float z[MT][NT][4];
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) z[mt][n][e] = 0.f;
+#pragma unroll
+      for (int kk = 0; kk < D / 16; ++kk) {
+        uint32_t qa[MT][4];
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+          if constexpr (MT == 1) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) qa[mt][e] = q[kk][e];
+          } else {
+            ldsm4(q_addr + q_chunk<T>(row_off + mt * 16 + (lane & 7) + ((lane >> 3) & 1) * 8, 2 * kk + (lane >> 4)), qa[mt]);
+          }
+        }
+        if constexpr (T::FP8) {
+          if (kk % 2 == 0) {
+#pragma unroll
+            for (int np = 0; np < NT / 2; ++np) {
+              uint32_t r[4];                             // 16 keys x 32 dimensions: chunks kk, kk + 1
+              ldsm4(k_tile + tile_chunk<T>(key_off + np * 16 + (lane >> 4) * 8 + (lane & 7), kk + ((lane >> 3) & 1)), r);
+              uint32_t qb[MT][4];
+#pragma unroll
+              for (int mt = 0; mt < MT; ++mt) {
+                if constexpr (MT == 1) {
+#pragma unroll
+                  for (int e = 0; e < 4; ++e) qb[mt][e] = q[kk + 1][e];
+                } else {
+                  ldsm4(q_addr + q_chunk<T>(row_off + mt * 16 + (lane & 7) + ((lane >> 3) & 1) * 8, 2 * (kk + 1) + (lane >> 4)), qb[mt]);
+                }
+              }
+#pragma unroll
+              for (int h = 0; h < 2; ++h) {
+                uint32_t b0, b1, c0, c1;
+                widen4(r[2 * h], b0, b1);
+                widen4(r[2 * h + 1], c0, c1);
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt) {
+                  mma16<true>(z[mt][2 * np + h], qa[mt], b0, b1);
+                  mma16<true>(z[mt][2 * np + h], qb[mt], c0, c1);
+                }
+              }
+            }
+          }
+        } else {
+#pragma unroll
+          for (int np = 0; np < NT / 2; ++np) {
+            uint32_t r[4];
+            ldsm4(k_tile + tile_chunk<T>(key_off + np * 16 + (lane >> 4) * 8 + (lane & 7), 2 * kk + ((lane >> 3) & 1)), r);
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+              mma16<false>(z[mt][2 * np], qa[mt], r[0], r[1]);
+              mma16<false>(z[mt][2 * np + 1], qa[mt], r[2], r[3]);
+            }
+          }
+        }
+      }
+      // base-2 logits, masked
+      const int key0 = d.key0;
+      const int row_first = d.row_tile * R;
+      const bool guard = key0 < d.first || key0 + kKeys > d.end || (a.causal && key0 + kKeys - 1 > d.pos0 + row_first / a.group);
+      bool over = false;
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          const float f = T::FP8 ? d.k_scale * qf[mt][b] : a.c;
+          const float add = T::FP8 ? d.v_log2 : 0.f;
+          int hi = d.end;
+          if (guard && a.causal) hi = min(hi, d.pos0 + (row_first + row_off + mt * 16 + (lane >> 2) + 8 * b) / a.group + 1);
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              float x = T::FP8 ? fmaf(z[mt][n][2 * b + e], f, add) : z[mt][n][2 * b + e] * f;
+              if (guard) {
+                const int key = key0 + key_off + n * 8 + (lane & 3) * 2 + e;
+                if (key < d.first || key >= hi) x = -INFINITY;
+              }
+              z[mt][n][2 * b + e] = x;
+              over |= x > st.m[mt][b] + kLazy;
+            }
+        }
+      if (__any_sync(0xffffffffu, over)) {
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+          for (int b = 0; b < 2; ++b) {
+            float top = st.m[mt][b];
+#pragma unroll
+            for (int n = 0; n < NT; ++n) top = fmaxf(top, fmaxf(z[mt][n][2 * b], z[mt][n][2 * b + 1]));
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+            const float f = top == st.m[mt][b] ? 1.f : fast_exp2(st.m[mt][b] - top);
+            st.m[mt][b] = top;
+            st.l[mt][b] *= f;
+#pragma unroll
+            for (int n = 0; n < D / 8; ++n) st.o[mt][n][2 * b] *= f, st.o[mt][n][2 * b + 1] *= f;
+          }
+      }
+      uint32_t p[MT][NT / 2][4];
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          const float ref = (st.m[mt][b] == -INFINITY ? 0.f : st.m[mt][b]) - (T::FP8 ? kShift : 0.f);
+          float sum = 0.f;
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            const float x = fast_exp2(z[mt][n][2 * b] - ref), y = fast_exp2(z[mt][n][2 * b + 1] - ref);
+            sum += x + y;
+            p[mt][n >> 1][b + 2 * (n & 1)] = T::FP8 ? pack_f16(x, y) : pack_bf16(x, y);
+          }
+          if constexpr (T::FP8) st.l[mt][b] = fmaf(sum, d.v_inverse, st.l[mt][b]);
+          else st.l[mt][b] += sum;
+        }
+      add_values<T>(st, p, v_tile, key_off, key0, d, a.group, a.causal, row_first + row_off, guard, lane);
+    }
+    if (flags & kLast) {
+      // the warps' sums of a row, each against its own reference
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          float l = st.l[mt][b];
+          l += __shfl_xor_sync(0xffffffffu, l, 1);
+          l += __shfl_xor_sync(0xffffffffu, l, 2);
+          if ((lane & 3) == 0) sm.stats[key_warp][row_off + mt * 16 + (lane >> 2) + 8 * b] = make_float2(st.m[mt][b], l);
+        }
+      if (!join.wait(ab)) return;                        // statistics are there, and the stage's tile is read
+      float f[MT][2];
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          const int r = row_off + mt * 16 + (lane >> 2) + 8 * b;
+          float top = -INFINITY;
+#pragma unroll
+          for (int w = 0; w < T::WK; ++w) top = fmaxf(top, sm.stats[w][r].x);
+          f[mt][b] = st.m[mt][b] == -INFINITY ? 0.f : fast_exp2(st.m[mt][b] - top);
+        }
+      const bool whole = (flags & kFromStart) && (flags & kToEnd);
+      const int slot = 2 * blockIdx.x + ((flags & kFromStart) ? 1 : 0);
+      const int live = min(R, d.n_new * a.group - d.row_tile * R);
+      float* buf = reinterpret_cast<float*>(ring_ptr + stage * T::STAGE);
+      constexpr int kSwizzle = (T::JOIN / 8 < 4 ? T::JOIN / 8 : 4) - 1;
+      for (int c0 = 0; c0 < D; c0 += T::JOIN) {
+#pragma unroll
+        for (int n = 0; n < D / 8; ++n) {
+          // columns of the thread's pair in the tile: bf16 8 n + 2 c, + 1; 8 bits 16 (n / 2) + 4 c + (n % 2), + 2
+          const int first = T::FP8 ? (n >> 1) * 16 + (lane & 3) * 4 + (n & 1) : n * 8 + (lane & 3) * 2;
+          if (first < c0 || first >= c0 + T::JOIN) continue;
+#pragma unroll
+          for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+              const int r = row_off + mt * 16 + (lane >> 2) + 8 * b, col = (first - c0) ^ ((r & kSwizzle) << 3);
+              float* at = buf + (key_warp * R + r) * T::JOIN + col;
+              at[0] = st.o[mt][n][2 * b] * f[mt][b];
+              at[T::FP8 ? 2 : 1] = st.o[mt][n][2 * b + 1] * f[mt][b];
+            }
+        }
+        if (!join.wait(ab)) return;
+        for (int item = threadIdx.x; item < live * (T::JOIN / 8); item += kWarps * 32) {
+          const int r = item / (T::JOIN / 8), col = item % (T::JOIN / 8) * 8, at = col ^ ((r & kSwizzle) << 3);
+          float x[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) x[i] = 0.f;
+#pragma unroll
+          for (int w = 0; w < T::WK; ++w) {
+            const float4* src = reinterpret_cast<const float4*>(buf + (w * R + r) * T::JOIN + at);
+            const float4 u = src[0], v = src[1];
+            x[0] += u.x, x[1] += u.y, x[2] += u.z, x[3] += u.w, x[4] += v.x, x[5] += v.y, x[6] += v.z, x[7] += v.w;
+          }
+          float top = -INFINITY, l = 0.f;
+#pragma unroll
+          for (int w = 0; w < T::WK; ++w) top = fmaxf(top, sm.stats[w][r].x);
+#pragma unroll
+          for (int w = 0; w < T::WK; ++w)
+            if (sm.stats[w][r].x != -INFINITY) l += sm.stats[w][r].y * fast_exp2(sm.stats[w][r].x - top);
+          if (whole) {
+            const int rr = d.row_tile * R + r;
+            const int64_t row = d.row0 + rr / a.group;
+            const int head = d.head * a.group + rr % a.group;
+            const float inv = l == 0.f ? 0.f : 1.f / l;
+            uint4 v;
+            v.x = pack_bf16(x[0] * inv, x[1] * inv), v.y = pack_bf16(x[2] * inv, x[3] * inv);
+            v.z = pack_bf16(x[4] * inv, x[5] * inv), v.w = pack_bf16(x[6] * inv, x[7] * inv);
+            *reinterpret_cast<uint4*>(a.out.data + row * a.out.stride_row + head * a.out.stride_head + c0 + col) = v;
+            if (a.lse != nullptr && c0 + col == 0)
+              a.lse[row * a.lse_stride_row + head * a.lse_stride_head] = l == 0.f ? -INFINITY : (top - (T::FP8 ? kShift : 0.f) + log2f(l)) * kLn2;
+          } else {
+            float4* dst = reinterpret_cast<float4*>(args.partial + ((int64_t)slot * R + r) * D + c0 + col);
+            dst[0] = make_float4(x[0], x[1], x[2], x[3]);
+            dst[1] = make_float4(x[4], x[5], x[6], x[7]);
+            if (c0 + col == 0) args.partial_stats[slot * R + r] = make_float2(top, l);
+          }
+        }
+        if (!join.wait(ab)) return;
+      }
+      if ((flags & kFromStart) && !(flags & kToEnd) && threadIdx.x == 0) {
+        args.headers[2 * blockIdx.x] = make_int4(flags >> 8, d.row0, d.head, d.row_tile);
+        args.headers[2 * blockIdx.x + 1] = make_int4(live, 0, 0, 0);
+      }
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // the stage was written with ordinary stores; copies follow
+    }
+    __syncwarp();
+    if (lane == 0) mbar_arrive(smem_u32(&sm.empty[stage]));
+    if (++stage == T::STAGES) stage = 0, parity ^= 1;
+  }
+}
+
+template <int D, bool FP8, int R>
+__global__ void __launch_bounds__(kThreads, kCtasPerSm) attend_step_kernel(const __grid_constant__ StepArgs args) {
+  using T = Traits<D, FP8, R>;
+  extern __shared__ unsigned char smem_raw[];
+  unsigned char* ring_ptr = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
+  unsigned char* q_tile = ring_ptr + T::STAGES * T::STAGE;
+  SmallSmem& sm = *reinterpret_cast<SmallSmem*>(q_tile + T::QBYTES);
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < T::STAGES; ++i) {
+      mbar_init(smem_u32(&sm.full[i]), 1);
+      mbar_init(smem_u32(&sm.empty[i]), kWarps);
+    }
+    mbar_init(smem_u32(&sm.join), kWarps);
+    sm.abort = 0;
+    args.headers[2 * blockIdx.x] = make_int4(0, 0, 0, 0);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  find_start<T>(args, sm);                               // ends with a barrier of the CTA
+  const int64_t total = sm.total;
+  const int64_t per = max((int64_t)args.min_tiles, (total + gridDim.x - 1) / gridDim.x);
+  const int64_t w0 = per * blockIdx.x, w1 = min(w0 + per, total);
+  if (w0 < w1) {
+    const Abort ab{&sm.abort, args.a.dev_status};
+    if (threadIdx.x < kWarps * 32) compute_tiles<T>(args, sm, ring_ptr, smem_u32(ring_ptr), q_tile, w1 - w0, ab);
+    else copy_tiles<T>(args, sm, smem_u32(ring_ptr), w0, w1, per, ab);
+  }
+  grid_launch_dependents();
+}
+
+// Joins the parts of the triples that CTA blockIdx.x began and others went on with: a warp per row.
+template <int D, bool FP8, int R>
+__global__ void __launch_bounds__(128) attend_join_kernel(const __grid_constant__ StepArgs args) {
+  const AttendArgs& a = args.a;
+  grid_wait();
+  const int4 head = args.headers[2 * blockIdx.x];
+  const int r = blockIdx.y * 4 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+  if (head.x <= 0 || r >= args.headers[2 * blockIdx.x + 1].x) return;
+  const int parts = head.x + 1;
+  auto slot = [&](int i) { return i == 0 ? 2 * (int)blockIdx.x + 1 : 2 * ((int)blockIdx.x + i); };
+  float top = -INFINITY;
+  for (int i = lane; i < parts; i += 32) top = fmaxf(top, args.partial_stats[slot(i) * R + r].x);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+  constexpr int V = D / 32;                              // columns of a lane
+  float x[V] = {}, l = 0.f;
+#pragma unroll 4
+  for (int i = 0; i < parts; ++i) {
+    const float2 s = args.partial_stats[slot(i) * R + r];
+    const float f = s.x == -INFINITY ? 0.f : fast_exp2(s.x - top);
+    const float* src = args.partial + ((int64_t)slot(i) * R + r) * D + lane * V;
+    l += s.y * f;
+#pragma unroll
+    for (int j = 0; j < V; ++j) x[j] += src[j] * f;
+  }
+  const int rr = head.w * R + r;
+  const int64_t row = head.y + rr / a.group;
+  const int h = head.z * a.group + rr % a.group;
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  uint32_t* dst = reinterpret_cast<uint32_t*>(a.out.data + row * a.out.stride_row + h * a.out.stride_head) + lane * (V / 2);
+#pragma unroll
+  for (int j = 0; j < V / 2; ++j) dst[j] = pack_bf16(x[2 * j] * inv, x[2 * j + 1] * inv);
+  if (a.lse != nullptr && lane == 0)
+    a.lse[row * a.lse_stride_row + h * a.lse_stride_head] = l == 0.f ? -INFINITY : (top - (FP8 ? kShift : 0.f) + log2f(l)) * kLn2;
+}
+
+struct StepWorkspace {
+  size_t partial, stats, headers, total;
+};
+StepWorkspace step_workspace(int rows, int d, int ctas) {
+  StepWorkspace w;
+  w.partial = 0;
+  w.stats = align_up((size_t)2 * ctas * rows * d * sizeof(float), 256);
+  w.headers = w.stats + align_up((size_t)2 * ctas * rows * sizeof(float2), 256);
+  w.total = w.headers + align_up((size_t)2 * ctas * sizeof(int4), 256);
+  return w;
+}
+
+// Rows of a tile: the fewest that hold the rows of a sequence and key head, up to 64.
+int tile_rows(int group, int max_new) {
+  const int64_t rows = (int64_t)group * max_new;
+  return rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
+}
+
+template <int D, bool FP8, int R>
+int32_t launch_step(const StepArgs& args, int ctas, cudaStream_t stream) {
+  using T = Traits<D, FP8, R>;
+  static ContextSet done;
+  const int32_t st = allow_shared_memory(reinterpret_cast<const void*>(attend_step_kernel<D, FP8, R>), smem_bytes<T>(), done);
+  if (st != SPF_OK) return st;
+  attend_step_kernel<D, FP8, R><<<ctas, kThreads, smem_bytes<T>(), stream>>>(args);
+  SPF_CUDA_CHECK(cudaGetLastError());
+  cudaLaunchConfig_t config{};
+  config.gridDim = dim3((unsigned)ctas, R / 4);
+  config.blockDim = dim3(128);
+  config.stream = stream;
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  config.attrs = &attr;
+  config.numAttrs = 1;
+  SPF_CUDA_CHECK(cudaLaunchKernelEx(&config, attend_join_kernel<D, FP8, R>, args));
+  return SPF_OK;
+}
+
+template <int D, bool FP8>
+int32_t launch_rows(const StepArgs& args, int rows, int ctas, cudaStream_t stream) {
+  switch (rows) {
+    case 16: return launch_step<D, FP8, 16>(args, ctas, stream);
+    case 32: return launch_step<D, FP8, 32>(args, ctas, stream);
+    default: return launch_step<D, FP8, 64>(args, ctas, stream);
+  }
+}
+
+}  // namespace
+
+size_t attend_step_workspace_bytes(const spf_kv_cache* cache, int group, int max_new, int sm_count) {
+  return step_workspace(tile_rows(group, max_new), cache->head_dim, sm_count * kCtasPerSm).total;
+}
+
+int32_t attend_step_launch(const AttendArgs& a, const spf_kv_cache* cache, int max_new, int sm_count, void* workspace, cudaStream_t stream) {
+  StepArgs args{};
+  args.a = a;
+  const int rows = tile_rows(a.group, max_new), ctas = sm_count * kCtasPerSm;
+  const StepWorkspace w = step_workspace(rows, cache->head_dim, ctas);
+  char* base = static_cast<char*>(workspace);
+  args.partial = reinterpret_cast<float*>(base + w.partial);
+  args.partial_stats = reinterpret_cast<float2*>(base + w.stats);
+  args.headers = reinterpret_cast<int4*>(base + w.headers);
+  args.min_tiles = 2;
+  int32_t st = encode_pool_map("spf_attend", cache, cache->k_pool, kKeys, &args.k_map);
+  if (st == SPF_OK) st = encode_pool_map("spf_attend", cache, cache->v_pool, kKeys, &args.v_map);
+  if (st != SPF_OK) return st;
+  const bool fp8 = cache->k_scale != nullptr;
+  if (cache->head_dim == 64) return fp8 ? launch_rows<64, true>(args, rows, ctas, stream) : launch_rows<64, false>(args, rows, ctas, stream);
+  return fp8 ? launch_rows<128, true>(args, rows, ctas, stream) : launch_rows<128, false>(args, rows, ctas, stream);
+}
+
+}  // namespace spf

@@ -585,7 +585,71 @@ PyObject* kv_append(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
   }
 }
 
+// attend_workspace_bytes(cache, step, q) -> bytes (0: the reason is in spf_last_error())
+PyObject* attend_workspace_bytes(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
+  try {
+    if (n_args != 3) raise(PyExc_TypeError, "attend_workspace_bytes takes 3 arguments");
+    Held held;
+    const spf_kv_cache cache = read_cache(args[0], &held);
+    const at::Tensor& q = device_tensor(args[2], at::kBFloat16, "q");
+    if (q.dim() != 3) raise(PyExc_ValueError, "q must be [rows, heads, d] of the step and the cache, the last dimension contiguous");
+    const int64_t max_new = attr_int(args[1], N.max_new);
+    const c10::cuda::CUDAGuard guard(held.tensors.front().device());
+    return PyLong_FromSize_t(spf_attend_workspace_bytes(&cache, (int32_t)q.size(1), (int32_t)std::min<int64_t>(max_new, INT32_MAX)));
+  } catch (const PyFailure&) {
+    return nullptr;
+  } catch (const std::exception& e) {
+    PyErr_SetString(PyExc_RuntimeError, e.what());
+    return nullptr;
+  }
+}
+
+// attend(cache, step, q, out, workspace, lse, first_keys, causal, softmax_scale, dev_status, stream) -> status
+PyObject* attend(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
+  try {
+    if (n_args != 11) raise(PyExc_TypeError, "attend takes 11 arguments");
+    Held held;
+    const spf_kv_cache cache = read_cache(args[0], &held);
+    const at::Tensor& q0 = device_tensor(args[2], at::kBFloat16, "q");
+    const int64_t n_rows = q0.dim() > 0 ? q0.size(0) : 0, heads = q0.dim() > 1 ? q0.size(1) : 0;
+    const spf_kv_step step = read_step(args[1], n_rows, &held);
+    const spf_rows q = read_rows(args[2], "q", n_rows, heads, cache.head_dim, &held);
+    const spf_rows out = read_rows(args[3], "out", n_rows, heads, cache.head_dim, &held);
+    const at::Tensor& ws = held.keep(tensor(args[4], "workspace"), "workspace");
+    if (!ws.is_cuda() || !ws.is_contiguous()) raise(PyExc_TypeError, "workspace must be a contiguous CUDA tensor");
+    spf_attend_options options{};
+    if (args[5] != Py_None) {
+      const at::Tensor& lse = held.keep(device_tensor(args[5], at::kFloat, "lse"), "lse");
+      if (lse.dim() != 2 || lse.size(0) != n_rows || lse.size(1) != heads) raise(PyExc_ValueError, "lse must be fp32 [rows, heads]");
+      options.lse = lse.data_ptr<float>();
+      options.lse_stride_row = n_rows > 1 ? lse.stride(0) : 1;
+      options.lse_stride_head = heads > 1 ? lse.stride(1) : 1;
+    }
+    if (args[6] != Py_None) {
+      const at::Tensor& first = held.keep(device_tensor(args[6], at::kInt, "first_keys"), "first_keys");
+      if (first.numel() != step.n_seqs || !first.is_contiguous()) raise(PyExc_ValueError, "first_keys must be contiguous int32 [n_seqs]");
+      options.first_keys = first.data_ptr<int32_t>();
+    }
+    const int causal = PyObject_IsTrue(args[7]);
+    const double scale = PyFloat_AsDouble(args[8]);
+    if (PyErr_Occurred()) throw PyFailure{};
+    options.see_all = !causal;
+    int32_t* status = read_status(args[9], &held);
+    const c10::cuda::CUDAGuard guard(held.tensors.front().device());
+    void* stream = stream_on(args[10], held);
+    return PyLong_FromLong(spf_attend(&cache, &step, &q, &out, (int32_t)heads, (float)scale, &options, ws.data_ptr(),
+                                      (size_t)ws.numel() * ws.element_size(), status, stream));
+  } catch (const PyFailure&) {
+    return nullptr;
+  } catch (const std::exception& e) {
+    PyErr_SetString(PyExc_RuntimeError, e.what());
+    return nullptr;
+  }
+}
+
 PyMethodDef kMethods[] = {
+    {"attend_workspace_bytes", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(attend_workspace_bytes)), METH_FASTCALL, "Workspace of attend."},
+    {"attend", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(attend)), METH_FASTCALL, "A step's attention over the cache."},
     {"kv_append", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(kv_append)), METH_FASTCALL, "A step's keys and values into the cache."},
     {"select", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(select_one)), METH_FASTCALL, "The path for one prompt."},
     {"select_batch", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(select_batch)), METH_FASTCALL, "The path for a batch of prompts."},

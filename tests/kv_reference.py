@@ -121,14 +121,16 @@ def logical(pool, scale, table_row, n):
 
 
 def attention(q, k, v, pos, first=0, causal=True, scale=None):
-    """(out, lse, weight): float64 [rows, heads, d], [rows, heads] and sum p |v|, which bounds what a relative error of the
-    weights does; q [rows, Hq, d], k and v [Hkv, n, d], pos: the rows' places in the sequence."""
+    """(out, lse, weight, terms): float64 [rows, heads, d], [rows, heads], sum p |v|, which bounds what a relative error of the
+    weights does, and the largest sum |scale q k| of a row's logits, which bounds what fp32 sums do to them; q [rows, Hq, d],
+    k and v [Hkv, n, d], pos: the rows' places in the sequence."""
     q = q.double().cpu()
     rows, Hq, d = q.shape
     group = Hq // k.shape[0]
     scale = 1.0 / math.sqrt(d) if scale is None else scale
     out, lse, weight = (torch.zeros((rows, Hq, d), dtype=torch.float64), torch.full((rows, Hq), -math.inf, dtype=torch.float64),
                         torch.zeros((rows, Hq, d), dtype=torch.float64))
+    terms = torch.zeros((rows, Hq), dtype=torch.float64)
     for i in range(rows):
         end = min(k.shape[1], int(pos[i]) + 1) if causal else k.shape[1]
         if end <= first:
@@ -140,4 +142,5 @@ def attention(q, k, v, pos, first=0, causal=True, scale=None):
             p = torch.exp(z - lse[i, h])
             out[i, h] = p @ vv
             weight[i, h] = p @ vv.abs()
-    return out, lse, weight
+            terms[i, h] = (kk.abs() @ q[i, h].abs()).max() * scale
+    return out, lse, weight, terms

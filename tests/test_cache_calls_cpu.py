@@ -73,3 +73,32 @@ def test_append_checks_its_tensors(spf):
         spf.spf_kv_append(spf.KvCache(pool, pool), spf.KvStep(i, i[:1], i[None]), x, x)   # host tensors
     with pytest.raises(ValueError):
         spf.spf_kv_append(spf.KvCache(pool, pool, i), spf.KvStep(i, i[:1], i[None]), x, x)  # one of the two scales
+
+
+def test_attend_refuses(spf):
+    b, cache, step = _structs()
+    q, out = b._Rows(P, 256, 64), b._Rows(2 * P, 256, 64)
+    options = b._AttendOptions(P, 4, 1, None, 0)
+
+    def call(cache=cache, step=step, q=q, out=out, heads=4, options=options, ws=P, ws_bytes=1 << 40):
+        ref = lambda x: None if x is None else ctypes.byref(x)  # noqa: E731
+        return spf.lib.spf_attend(ref(cache), ref(step), ref(q), ref(out), heads, 0.0, ref(options), ws, ws_bytes, None, None)
+
+    for fields, status in BAD_CACHE:
+        assert call(cache=_changed(cache, **fields)) == status, fields
+        assert spf.spf_last_error().startswith("spf_attend")
+    for fields in BAD_STEP:
+        assert call(step=_changed(step, **fields)) == -1, fields
+    for fields in BAD_ROWS:
+        for name in ("q", "out"):
+            assert call(**{name: _changed(q, **fields)}) == -1, (name, fields)
+    assert call(cache=None) == -1 and call(step=None) == -1 and call(q=None) == -1 and call(out=None) == -1
+    assert call(heads=0) == -1 and call(heads=5) == -2
+    assert call(out=q) == -1                                                  # in place
+    assert call(out=_changed(out, stride_head=32)) == -1                      # heads of the output overlap
+    for fields in (dict(lse_stride_row=0), dict(lse_stride_head=0), dict(lse_stride_row=-1)):
+        assert call(options=_changed(options, **fields)) == -1, fields
+    assert call(step=_changed(step, n_rows=0)) == 0                           # nothing to do: nothing is launched
+    assert spf.lib.spf_attend_workspace_bytes(ctypes.byref(_changed(cache, head_dim=96)), 4, 1) == 0
+    assert spf.lib.spf_attend_workspace_bytes(ctypes.byref(cache), 4, 0) == 0
+    assert spf.lib.spf_attend_workspace_bytes(ctypes.byref(cache), 3, 1) == 0
