@@ -13,7 +13,7 @@
  *
  * Before them, on the draft model's side: spf_kv_append (rotates a step's queries and keys and writes a paged cache) and
  * spf_attend (the step's attention over it).  Around them: spf_keep_count / spf_keep_rate / spf_snap_budget (Section 3.1, keep rate) and spf_concat_with_delim
- * (Algorithm 1 "ConcatWithDelim") on the host; spf_score_paged (paged key cache), spf_score_fp8 (8-bit key cache),
+ * (Algorithm 1 "ConcatWithDelim") on the host; spf_score_paged (paged key cache), spf_score_fp8 (8-bit key cache), spf_score_paged_fp8 (both),
  * spf_score_shard_lse /
  * spf_score_shard_apply (one prompt's keys over several GPUs); spf_score_extra, spf_chunk_pool_edge,
  * spf_select_topk_forced (switches for points the paper leaves open); spf_compress_host (the four calls for host
@@ -343,6 +343,33 @@ SPF_API size_t spf_attend_workspace_bytes(const spf_kv_cache* cache, int32_t n_q
 SPF_API int32_t spf_attend(const spf_kv_cache* cache, const spf_kv_step* step, const spf_rows* q, const spf_rows* out,
                            int32_t n_q_heads, float softmax_scale, const spf_attend_options* options, void* workspace,
                            size_t workspace_bytes, int32_t* dev_status, void* cuda_stream);
+
+/*
+ * spf_score on a PAGED 8-bit key cache, as spf_kv_append writes it: blocks as for spf_score_paged, key s of a prompt, in block
+ * block_table[s / block_tokens], worth
+ *     k_scales[l][block][hk][(s % block_tokens) / SPF_KV_SCALE_TOKENS] * E4M3(byte).
+ *
+ *   k_pools    HOST array of L device pointers, layer l uint8 [n_pool_blocks][Hkv][block_tokens][d], contiguous, 16-byte aligned
+ *   k_scales   HOST array of L device pointers, layer l fp32 [n_pool_blocks][Hkv][block_tokens / SPF_KV_SCALE_TOKENS], positive
+ *              and finite where the prompt has tokens
+ *   others     as in spf_paged_prompt
+ * Kernel paths, workspace, errors and dev_status as for spf_score_fp8.
+ */
+typedef struct {
+  int64_t n_tokens;
+  const void* const* k_pools;
+  const float* const* k_scales;
+  int64_t n_pool_blocks;
+  int32_t block_tokens;
+  const int32_t* block_table;
+  const void* q;
+  float* importance;
+  float* lse;
+} spf_paged_fp8_prompt;
+
+SPF_API size_t spf_score_paged_fp8_workspace_bytes(const spf_shape* shape, const spf_paged_fp8_prompt* prompts, int32_t n_prompts);
+SPF_API int32_t spf_score_paged_fp8(const spf_shape* shape, const spf_paged_fp8_prompt* prompts, int32_t n_prompts, void* workspace,
+                                    size_t workspace_bytes, int32_t* dev_status, void* cuda_stream);
 
 /*
  * One long prompt over several GPUs (Appendix A.1.1 is per prompt; this shards its keys).  Each rank holds a contiguous

@@ -66,6 +66,12 @@ class _PagedPrompt(ctypes.Structure):
                 ("q", ctypes.c_void_p), ("importance", ctypes.c_void_p), ("lse", ctypes.c_void_p)]
 
 
+class _PagedFp8Prompt(ctypes.Structure):
+    _fields_ = [("n_tokens", ctypes.c_int64), ("k_pools", ctypes.POINTER(ctypes.c_void_p)), ("k_scales", ctypes.POINTER(ctypes.c_void_p)),
+                ("n_pool_blocks", ctypes.c_int64), ("block_tokens", ctypes.c_int32), ("block_table", ctypes.c_void_p),
+                ("q", ctypes.c_void_p), ("importance", ctypes.c_void_p), ("lse", ctypes.c_void_p)]
+
+
 class _KvCache(ctypes.Structure):
     _fields_ = [("k_pool", ctypes.c_void_p), ("v_pool", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
                 ("n_pool_blocks", ctypes.c_int64), ("block_tokens", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
@@ -107,6 +113,10 @@ def _load() -> ctypes.CDLL:
     dll.spf_score_paged_workspace_bytes.argtypes = [ctypes.POINTER(_Shape), ctypes.POINTER(_PagedPrompt), i32]
     dll.spf_score_paged.restype = i32
     dll.spf_score_paged.argtypes = [ctypes.POINTER(_Shape), ctypes.POINTER(_PagedPrompt), i32, vp, ctypes.c_size_t, vp, vp]
+    dll.spf_score_paged_fp8_workspace_bytes.restype = ctypes.c_size_t
+    dll.spf_score_paged_fp8_workspace_bytes.argtypes = [ctypes.POINTER(_Shape), ctypes.POINTER(_PagedFp8Prompt), i32]
+    dll.spf_score_paged_fp8.restype = i32
+    dll.spf_score_paged_fp8.argtypes = [ctypes.POINTER(_Shape), ctypes.POINTER(_PagedFp8Prompt), i32, vp, ctypes.c_size_t, vp, vp]
     dll.spf_score_fp8_workspace_bytes.restype = ctypes.c_size_t
     dll.spf_score_fp8_workspace_bytes.argtypes = [ctypes.POINTER(_Shape), ctypes.POINTER(_Fp8Prompt), i32]
     dll.spf_score_fp8.restype = i32
@@ -427,6 +437,73 @@ def spf_score_fp8(prompts: Sequence[Fp8PromptBuffers], workspace: torch.Tensor, 
     _check(lib.spf_score_fp8(ctypes.byref(shape), arr, len(prompts), workspace.data_ptr(),
                              workspace.numel() * workspace.element_size(), _ptr(dev_status), _stream_ptr(stream)),
            "spf_score_fp8")
+
+
+@dataclasses.dataclass
+class PagedFp8PromptBuffers:
+    """Device buffers of one prompt whose keys sit in 8-bit block pools (see spf_paged_fp8_prompt in include/spf.h)."""
+    q: torch.Tensor                      # bf16 [L, Hq, m, d]
+    k_pools: Sequence[torch.Tensor]      # L tensors uint8 [n_pool_blocks, Hkv, block_tokens, d] (E4M3 bytes), contiguous
+    k_scales: Sequence[torch.Tensor]     # L tensors fp32 [n_pool_blocks, Hkv, block_tokens / 64], contiguous
+    block_table: torch.Tensor            # int32 [ceil(N / block_tokens)]
+    n_tokens: int
+    importance: torch.Tensor             # fp32 [N] (out)
+    lse: Optional[torch.Tensor] = None   # fp32 [L, Hq, m] (out)
+
+
+def _marshal_paged_fp8(prompts: Sequence[PagedFp8PromptBuffers], softmax_scale: float):
+    L, Hq, m, d = prompts[0].q.shape
+    Hkv = prompts[0].k_pools[0].shape[1]
+    shape = _Shape(L, Hq, Hkv, d, m, float(softmax_scale))
+    arr = (_PagedFp8Prompt * len(prompts))()
+    keep = []
+    for i, p in enumerate(prompts):
+        _dev(p.q, torch.bfloat16, "q")
+        _dev(p.block_table, torch.int32, "block_table")
+        _dev(p.importance, torch.float32, "importance")
+        if len(p.k_pools) != L or len(p.k_scales) != L or tuple(p.q.shape) != (L, Hq, m, d) or not p.q.is_contiguous() or \
+                not p.block_table.is_contiguous():
+            raise ValueError("one contiguous pool and one of scales per layer, contiguous q of the batch's shape and block_table")
+        nb, hk, bt, dd = p.k_pools[0].shape
+        for pool, scale in zip(p.k_pools, p.k_scales):
+            _dev(pool, torch.uint8, "k_pools[l]")
+            _dev(scale, torch.float32, "k_scales[l]")
+            if tuple(pool.shape) != (nb, hk, bt, dd) or not pool.is_contiguous() or hk != Hkv or dd != d:
+                raise ValueError("every pool must be contiguous uint8 [n_pool_blocks, Hkv, block_tokens, d]")
+            if tuple(scale.shape) != (nb, hk, bt // 64) or not scale.is_contiguous():
+                raise ValueError("every k_scales[l] must be contiguous fp32 [n_pool_blocks, Hkv, block_tokens / 64]")
+        if p.block_table.numel() < (p.n_tokens + bt - 1) // bt or p.importance.numel() != p.n_tokens or not p.importance.is_contiguous():
+            raise ValueError("block_table or importance has the wrong size")
+        if p.lse is not None:
+            _dev(p.lse, torch.float32, "lse")
+            if p.lse.numel() != L * Hq * m or not p.lse.is_contiguous():
+                raise ValueError("lse must be contiguous fp32 [L, Hq, m]")
+        pools = (ctypes.c_void_p * L)(*[x.data_ptr() for x in p.k_pools])
+        scales = (ctypes.c_void_p * L)(*[x.data_ptr() for x in p.k_scales])
+        keep += [pools, scales]
+        ptr = ctypes.POINTER(ctypes.c_void_p)
+        arr[i] = _PagedFp8Prompt(p.n_tokens, ctypes.cast(pools, ptr), ctypes.cast(scales, ptr), nb, bt, p.block_table.data_ptr(),
+                                 p.q.data_ptr(), p.importance.data_ptr(), _ptr(p.lse))
+    return shape, arr, keep
+
+
+def spf_score_paged_fp8_workspace_bytes(prompts: Sequence[PagedFp8PromptBuffers], softmax_scale: float = 0.0) -> int:
+    shape, arr, _keep = _marshal_paged_fp8(prompts, softmax_scale)
+    n = int(lib.spf_score_paged_fp8_workspace_bytes(ctypes.byref(shape), arr, len(prompts)))
+    if n == 0:
+        raise SpfError(-1, "spf_score_paged_fp8_workspace_bytes", spf_last_error())
+    return n
+
+
+def spf_score_paged_fp8(prompts: Sequence[PagedFp8PromptBuffers], workspace: torch.Tensor, softmax_scale: float = 0.0,
+                        dev_status: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """spf_score for keys in 8-bit block pools, as spf_kv_append writes them."""
+    shape, arr, _keep = _marshal_paged_fp8(prompts, softmax_scale)
+    if not workspace.is_cuda:
+        raise TypeError("workspace must be a CUDA tensor")
+    _check(lib.spf_score_paged_fp8(ctypes.byref(shape), arr, len(prompts), workspace.data_ptr(),
+                                   workspace.numel() * workspace.element_size(), _ptr(dev_status), _stream_ptr(stream)),
+           "spf_score_paged_fp8")
 
 
 def spf_score_shard_lse(prompt: PromptBuffers, workspace: torch.Tensor, softmax_scale: float = 0.0,

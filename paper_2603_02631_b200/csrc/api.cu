@@ -70,6 +70,7 @@ int32_t make_problem(const spf_shape* shape, const spf_prompt& pr, int32_t index
   p.lse_out = pr.lse;
   p.extra_lse = nullptr;
   p.k_scale = nullptr;
+  p.scale_blocks = false;
   p.block_table = nullptr;
   p.block_tokens = 0;
   p.n_pool_blocks = 0;
@@ -296,6 +297,31 @@ extern "C" int32_t spf_score_fp8(const spf_shape* shape, const spf_fp8_prompt* p
                                    size_t workspace_bytes, int32_t* dev_status, void* cuda_stream) {
   return score_prompts("spf_score_fp8", shape, prompts, n_prompts, make_fp8_problem, g_score_path.load(std::memory_order_relaxed), nullptr,
                        workspace, workspace_bytes, dev_status, static_cast<cudaStream_t>(cuda_stream));
+}
+
+// Paged 8-bit key cache: a paged prompt over pools of bytes, marked with its scale pools.
+static int32_t make_paged_fp8_problem(const spf_shape* shape, const spf_paged_fp8_prompt& pp, int32_t index, ScoreProblem* out) {
+  const spf_paged_prompt paged{pp.n_tokens, pp.k_pools, pp.n_pool_blocks, pp.block_tokens, pp.block_table, pp.q, pp.importance, pp.lse};
+  const int32_t st = make_paged_problem(shape, paged, index, out);
+  if (st != SPF_OK) return st;
+  if (pp.k_scales == nullptr) return fail(SPF_ERR_INVALID_ARG, "spf_score_paged_fp8: prompt %d: k_scales is null", index);
+  for (int l = 0; l < out->n_layers; ++l) {
+    if (pp.k_scales[l] == nullptr || reinterpret_cast<uintptr_t>(pp.k_scales[l]) % 4 != 0)
+      return fail(SPF_ERR_INVALID_ARG, "spf_score_paged_fp8: prompt %d: k_scales[%d] is null or not 4-byte aligned", index, l);
+    out->k_scale_pools.p[l] = pp.k_scales[l];
+  }
+  out->scale_blocks = true;
+  return SPF_OK;
+}
+
+extern "C" size_t spf_score_paged_fp8_workspace_bytes(const spf_shape* shape, const spf_paged_fp8_prompt* prompts, int32_t n_prompts) {
+  return workspace_bytes_for("spf_score_paged_fp8_workspace_bytes", shape, prompts, n_prompts, make_paged_fp8_problem);
+}
+
+extern "C" int32_t spf_score_paged_fp8(const spf_shape* shape, const spf_paged_fp8_prompt* prompts, int32_t n_prompts, void* workspace,
+                                       size_t workspace_bytes, int32_t* dev_status, void* cuda_stream) {
+  return score_prompts("spf_score_paged_fp8", shape, prompts, n_prompts, make_paged_fp8_problem, g_score_path.load(std::memory_order_relaxed),
+                       nullptr, workspace, workspace_bytes, dev_status, static_cast<cudaStream_t>(cuda_stream));
 }
 
 // Key-sharded scoring: the two sweeps of the general path as separate calls.

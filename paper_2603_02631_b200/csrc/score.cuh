@@ -5,6 +5,11 @@
 
 namespace spf {
 
+// Per-layer scale pools of a paged 8-bit key cache.
+struct ScalePools {
+  const float* p[kMaxLayers];
+};
+
 struct ScoreProblem {
   int n_layers, n_q_heads, n_kv_heads, group, head_dim, n_lookahead;
   int m_pad;     // n_lookahead rounded up to a multiple of 8
@@ -18,6 +23,11 @@ struct ScoreProblem {
   // 8-bit key cache (k_scale != null): the layer pointers hold E4M3 bytes, strides count bytes, key (l, hk, s, j) has the
   // value k_scale[l * Hkv + hk] * E4M3(byte)
   const float* k_scale;
+  // paged 8-bit key cache (scale_blocks): bytes in block pools, key = scale * E4M3(byte) with layer l's scales, fp32
+  // [n_pool_blocks][Hkv][block_tokens / 64], in k_scale_pools.p[l]; k_scale is null
+  bool scale_blocks;
+  ScalePools k_scale_pools;
+  int key_format() const { return scale_blocks ? 2 : k_scale != nullptr ? 1 : 0; }
   const float* extra_lse;  // may be null: fp32 [L][Hq][m], natural log of what the row's denominator holds besides the prompt keys
   // paged key cache (block_tokens > 0): k.p[l] is layer l's block pool, bf16 [n_pool_blocks][Hkv][block_tokens][d];
   // logical block b of the prompt sits in pool block block_table[b] (device memory)

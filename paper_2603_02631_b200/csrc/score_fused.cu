@@ -265,6 +265,7 @@ struct Geometry {
 
 Geometry geometry(const ScoreProblem& p, int sm_count) {
   Geometry g;
+  if (p.scale_blocks) return g;                       // scales for groups of keys: the general path
   g.fp8 = p.k_scale != nullptr;
   // 8-bit key caches: contiguous only, and the TMA wants 16-byte aligned layer pointers and strides (the general path reads
   // them 8 bytes at a time and takes what this refuses)

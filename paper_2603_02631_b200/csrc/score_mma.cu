@@ -95,6 +95,21 @@ __device__ __forceinline__ int64_t tile_offset(int64_t key0, int64_t stride_tok,
   return block * pv.stride_block + (key0 % pv.block_tokens) * stride_tok;
 }
 
+// The kernels' FP8: 0 bf16 keys; 1 E4M3 bytes with a scale per (layer, kv-head); 2 E4M3 bytes in block pools with a scale for each
+// 64 tokens of a block and head.  Layer l's scales, fp32 [blocks][Hkv][block_tokens / 64], belong to 2 only.
+template <int FP8>
+struct TileScales {};
+template <>
+struct TileScales<2> {
+  const float* p[kMaxLayers];
+};
+// Scale of the tile whose first row lies `offset` elements into the layer's pool (a tile never straddles 64 tokens).
+template <int D, int FP8>
+__device__ __forceinline__ float tile_scale(const TileScales<FP8>& ts, int layer, int64_t offset) {
+  if constexpr (FP8 == 2) return __ldg(ts.p[layer] + offset / (D * SPF_KV_SCALE_TOKENS));
+  return 1.f;
+}
+
 // FP8: the cache holds E4M3 bytes (strides then count bytes); the tile is widened to bf16 as it is loaded.
 template <int D, bool FP8>
 __device__ __forceinline__ void load_key_tile(KeyTile<D>& t, const __nv_bfloat16* slab, int64_t tile_off, int64_t key0,
@@ -184,15 +199,15 @@ __global__ void pack_q_kernel(const __nv_bfloat16* __restrict__ q, uint4* __rest
 }
 
 // Sweep 1.  grid = (n_split, n_slabs); every warp strides over the slab's 32-key tiles.
-template <int D, int MT, bool FP8>
+template <int D, int MT, int FP8>
 __global__ void __launch_bounds__(kThreads) score_lse_kernel(LayerPtrs kp, const uint4* __restrict__ qf,
                                                               float2* __restrict__ partial, int64_t n_tokens,
                                                               int64_t stride_head, int64_t stride_tok, int n_kv_heads,
-                                                              float c, const float* __restrict__ k_scale, PagedView pv) {
+                                                              float c, const float* __restrict__ k_scale, PagedView pv, TileScales<FP8> ts) {
   const int slab = blockIdx.y;
   const int layer = slab / n_kv_heads, hk = slab % n_kv_heads;
-  const __nv_bfloat16* kslab = slab_base<FP8>(kp.p[layer], hk * stride_head);
-  if (FP8) c *= __ldg(k_scale + slab);                 // the slab's key scale multiplies every logit
+  const __nv_bfloat16* kslab = slab_base<FP8 != 0>(kp.p[layer], hk * stride_head);
+  if (FP8 == 1) c *= __ldg(k_scale + slab);            // the slab's key scale multiplies every logit
   const uint4* qslab = qf + (int64_t)slab * (MT * (D / 16) * 32);
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int64_t n_tiles = (n_tokens + kTileKeys - 1) / kTileKeys;
@@ -206,11 +221,18 @@ __global__ void __launch_bounds__(kThreads) score_lse_kernel(LayerPtrs kp, const
 
   int64_t tile = (int64_t)blockIdx.x * kWarpsPerCta + warp;
   KeyTile<D> cur;
-  if (tile < n_tiles) load_key_tile<D, FP8>(cur, kslab, tile_offset(tile * kTileKeys, stride_tok, pv), tile * kTileKeys, n_tokens, stride_tok, lane);
+  float cur_scale = 1.f, nxt_scale = 1.f;              // FP8 == 2: the tile's
+  auto load = [&](KeyTile<D>& t, float& scale, int64_t which) {
+    const int64_t offset = tile_offset(which * kTileKeys, stride_tok, pv);
+    scale = tile_scale<D>(ts, layer, hk * stride_head + offset);
+    load_key_tile<D, FP8 != 0>(t, kslab, offset, which * kTileKeys, n_tokens, stride_tok, lane);
+  };
+  if (tile < n_tiles) load(cur, cur_scale, tile);
   while (tile < n_tiles) {
     const int64_t next = tile + stride;
     KeyTile<D> nxt;
-    if (next < n_tiles) load_key_tile<D, FP8>(nxt, kslab, tile_offset(next * kTileKeys, stride_tok, pv), next * kTileKeys, n_tokens, stride_tok, lane);
+    if (next < n_tiles) load(nxt, nxt_scale, next);
+    const float ct = FP8 == 2 ? c * cur_scale : c;
 
     float acc[MT][4][4];
     tile_logits<D, MT>(acc, cur, qslab, lane);
@@ -227,7 +249,7 @@ __global__ void __launch_bounds__(kThreads) score_lse_kernel(LayerPtrs kp, const
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
             const int key = nt * 8 + (lane & 3) * 2 + e;
-            const float t = key < left ? acc[mt][nt][2 * b + e] * c : -INFINITY;
+            const float t = key < left ? acc[mt][nt][2 * b + e] * ct : -INFINITY;
             v[nt * 2 + e] = t;
             mx = fmaxf(mx, t);
           }
@@ -240,6 +262,7 @@ __global__ void __launch_bounds__(kThreads) score_lse_kernel(LayerPtrs kp, const
         run_m[mt][b] = m_new;
       }
     cur = nxt;
+    cur_scale = nxt_scale;
     tile = next;
   }
 
@@ -319,12 +342,12 @@ __global__ void load_lse_kernel(const float* __restrict__ lse_in, float* __restr
 }
 
 // Sweep 2.  One warp owns 32 keys for all slabs.  NI = m_pad / 8 lookahead indices live in a thread.
-template <int D, int MT, int NI, bool FP8>
+template <int D, int MT, int NI, int FP8>
 __global__ void __launch_bounds__(kThreads) score_max_kernel(LayerPtrs kp, const uint4* __restrict__ qf,
                                                               const float* __restrict__ lse2, float* __restrict__ importance,
                                                               int64_t n_tokens, int64_t stride_head, int64_t stride_tok,
                                                               int n_layers, int n_kv_heads, int group, int n_lookahead,
-                                                              float c, const float* __restrict__ k_scale, PagedView pv) {
+                                                              float c, const float* __restrict__ k_scale, PagedView pv, TileScales<FP8> ts) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int64_t tile = (int64_t)blockIdx.x * kWarpsPerCta + warp;
   const int64_t n_tiles = (n_tokens + kTileKeys - 1) / kTileKeys;
@@ -340,16 +363,18 @@ __global__ void __launch_bounds__(kThreads) score_max_kernel(LayerPtrs kp, const
 
   KeyTile<D> cur;
   const int64_t tile_off = tile_offset(key0, stride_tok, pv);   // the same for every layer and kv-head
-  load_key_tile<D, FP8>(cur, kp.p[0], tile_off, key0, n_tokens, stride_tok, lane);
+  load_key_tile<D, FP8 != 0>(cur, kp.p[0], tile_off, key0, n_tokens, stride_tok, lane);
+  float cur_scale = tile_scale<D>(ts, 0, tile_off), nxt_scale = 1.f;
   for (int slab = 0; slab < n_slabs; ++slab) {
     KeyTile<D> nxt;
     if (slab + 1 < n_slabs) {
       const int l2 = (slab + 1) / n_kv_heads, h2 = (slab + 1) % n_kv_heads;
-      load_key_tile<D, FP8>(nxt, slab_base<FP8>(kp.p[l2], h2 * stride_head), tile_off, key0, n_tokens, stride_tok, lane);
+      load_key_tile<D, FP8 != 0>(nxt, slab_base<FP8 != 0>(kp.p[l2], h2 * stride_head), tile_off, key0, n_tokens, stride_tok, lane);
+      nxt_scale = tile_scale<D>(ts, l2, h2 * stride_head + tile_off);
     }
     float acc[MT][4][4];
     tile_logits<D, MT>(acc, cur, qf + (int64_t)slab * (MT * (D / 16) * 32), lane);
-    const float cs = FP8 ? c * __ldg(k_scale + slab) : c;
+    const float cs = FP8 == 1 ? c * __ldg(k_scale + slab) : FP8 == 2 ? c * cur_scale : c;
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
@@ -366,6 +391,7 @@ __global__ void __launch_bounds__(kThreads) score_max_kernel(LayerPtrs kp, const
             amax[slot][nt * 2 + e] = fmaxf(amax[slot][nt * 2 + e], fmaf(acc[mt][nt][2 * b + e], cs, -lse));
       }
     cur = nxt;
+    cur_scale = nxt_scale;
   }
 
   const float inv_m = 1.f / (float)n_lookahead;
@@ -382,29 +408,43 @@ __global__ void __launch_bounds__(kThreads) score_max_kernel(LayerPtrs kp, const
   }
 }
 
-template <int D, int MT>
-void launch_lse(const ScoreProblem& p, const uint4* qf, float2* partial, int n_split, cudaStream_t stream) {
-  dim3 grid(n_split, p.n_layers * p.n_kv_heads);
-  if (p.k_scale != nullptr)
-    score_lse_kernel<D, MT, true><<<grid, kThreads, 0, stream>>>(p.k, qf, partial, p.n_tokens, p.stride_head, p.stride_tok,
-                                                                 p.n_kv_heads, p.c_log2, p.k_scale, paged_view(p));
-  else
-    score_lse_kernel<D, MT, false><<<grid, kThreads, 0, stream>>>(p.k, qf, partial, p.n_tokens, p.stride_head, p.stride_tok,
-                                                                  p.n_kv_heads, p.c_log2, nullptr, paged_view(p));
+template <int FP8>
+TileScales<FP8> tile_scales(const ScoreProblem& p) {
+  TileScales<FP8> ts{};
+  if constexpr (FP8 == 2)
+    for (int l = 0; l < p.n_layers; ++l) ts.p[l] = p.k_scale_pools.p[l];
+  return ts;
 }
 
+template <int D, int MT, int FP8>
+void launch_lse_as(const ScoreProblem& p, const uint4* qf, float2* partial, int n_split, cudaStream_t stream) {
+  const dim3 grid(n_split, p.n_layers * p.n_kv_heads);
+  score_lse_kernel<D, MT, FP8><<<grid, kThreads, 0, stream>>>(p.k, qf, partial, p.n_tokens, p.stride_head, p.stride_tok, p.n_kv_heads, p.c_log2,
+                                                              p.k_scale, paged_view(p), tile_scales<FP8>(p));
+}
+template <int D, int MT>
+void launch_lse(const ScoreProblem& p, const uint4* qf, float2* partial, int n_split, cudaStream_t stream) {
+  switch (p.key_format()) {
+    case 0: return launch_lse_as<D, MT, 0>(p, qf, partial, n_split, stream);
+    case 1: return launch_lse_as<D, MT, 1>(p, qf, partial, n_split, stream);
+    default: return launch_lse_as<D, MT, 2>(p, qf, partial, n_split, stream);
+  }
+}
+
+template <int D, int MT, int NI, int FP8>
+void launch_max_as(const ScoreProblem& p, const uint4* qf, const float* lse2, cudaStream_t stream) {
+  const unsigned grid = (unsigned)ceil_div(ceil_div(p.n_tokens, kTileKeys), kWarpsPerCta);
+  score_max_kernel<D, MT, NI, FP8><<<grid, kThreads, 0, stream>>>(p.k, qf, lse2, p.importance, p.n_tokens, p.stride_head, p.stride_tok, p.n_layers,
+                                                                  p.n_kv_heads, p.group, p.n_lookahead, p.c_log2, p.k_scale, paged_view(p),
+                                                                  tile_scales<FP8>(p));
+}
 template <int D, int MT, int NI>
 void launch_max(const ScoreProblem& p, const uint4* qf, const float* lse2, cudaStream_t stream) {
-  const int64_t n_tiles = ceil_div(p.n_tokens, kTileKeys);
-  const unsigned grid = (unsigned)ceil_div(n_tiles, kWarpsPerCta);
-  if (p.k_scale != nullptr)
-    score_max_kernel<D, MT, NI, true><<<grid, kThreads, 0, stream>>>(p.k, qf, lse2, p.importance, p.n_tokens, p.stride_head,
-                                                                       p.stride_tok, p.n_layers, p.n_kv_heads, p.group,
-                                                                       p.n_lookahead, p.c_log2, p.k_scale, paged_view(p));
-  else
-    score_max_kernel<D, MT, NI, false><<<grid, kThreads, 0, stream>>>(p.k, qf, lse2, p.importance, p.n_tokens, p.stride_head,
-                                                                        p.stride_tok, p.n_layers, p.n_kv_heads, p.group,
-                                                                        p.n_lookahead, p.c_log2, nullptr, paged_view(p));
+  switch (p.key_format()) {
+    case 0: return launch_max_as<D, MT, NI, 0>(p, qf, lse2, stream);
+    case 1: return launch_max_as<D, MT, NI, 1>(p, qf, lse2, stream);
+    default: return launch_max_as<D, MT, NI, 2>(p, qf, lse2, stream);
+  }
 }
 
 template <int D, int MT>

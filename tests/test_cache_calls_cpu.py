@@ -102,3 +102,25 @@ def test_attend_refuses(spf):
     assert spf.lib.spf_attend_workspace_bytes(ctypes.byref(_changed(cache, head_dim=96)), 4, 1) == 0
     assert spf.lib.spf_attend_workspace_bytes(ctypes.byref(cache), 4, 0) == 0
     assert spf.lib.spf_attend_workspace_bytes(ctypes.byref(cache), 3, 1) == 0
+
+
+def test_score_paged_fp8_refuses(spf):
+    b, _, _ = _structs()
+    ptrs = (ctypes.c_void_p * 2)(P, 2 * P)
+    odd = (ctypes.c_void_p * 2)(P, P + 2)
+    none = (ctypes.c_void_p * 2)(P, None)
+    lp = lambda x: ctypes.cast(x, ctypes.POINTER(ctypes.c_void_p))  # noqa: E731
+    shape = b._Shape(2, 4, 2, 64, 8, 0.0)
+    good = b._PagedFp8Prompt(1000, lp(ptrs), lp(ptrs), 10, 256, P, P, P, None)
+
+    def call(prompt, shape=shape):
+        arr = (b._PagedFp8Prompt * 1)(prompt)
+        return spf.lib.spf_score_paged_fp8(ctypes.byref(shape), arr, 1, P, 1 << 40, None, None)
+
+    for fields in (dict(n_tokens=0), dict(k_pools=lp(none)), dict(k_scales=None), dict(k_scales=lp(none)), dict(k_scales=lp(odd)), dict(n_pool_blocks=0),
+                   dict(block_tokens=64), dict(block_tokens=200), dict(block_table=None), dict(q=None), dict(importance=None)):
+        assert call(_changed(good, **fields)) == -1, fields
+    assert call(good, b._Shape(2, 4, 2, 96, 8, 0.0)) == -2
+    arr = (b._PagedFp8Prompt * 1)(good)
+    assert spf.lib.spf_score_paged_fp8(ctypes.byref(shape), arr, 1, None, 0, None, None) == -3
+    assert spf.lib.spf_score_paged_fp8_workspace_bytes(ctypes.byref(shape), arr, 1) > 0
