@@ -451,45 +451,8 @@ class PagedFp8PromptBuffers:
     lse: Optional[torch.Tensor] = None   # fp32 [L, Hq, m] (out)
 
 
-def _marshal_paged_fp8(prompts: Sequence[PagedFp8PromptBuffers], softmax_scale: float):
-    L, Hq, m, d = prompts[0].q.shape
-    Hkv = prompts[0].k_pools[0].shape[1]
-    shape = _Shape(L, Hq, Hkv, d, m, float(softmax_scale))
-    arr = (_PagedFp8Prompt * len(prompts))()
-    keep = []
-    for i, p in enumerate(prompts):
-        _dev(p.q, torch.bfloat16, "q")
-        _dev(p.block_table, torch.int32, "block_table")
-        _dev(p.importance, torch.float32, "importance")
-        if len(p.k_pools) != L or len(p.k_scales) != L or tuple(p.q.shape) != (L, Hq, m, d) or not p.q.is_contiguous() or \
-                not p.block_table.is_contiguous():
-            raise ValueError("one contiguous pool and one of scales per layer, contiguous q of the batch's shape and block_table")
-        nb, hk, bt, dd = p.k_pools[0].shape
-        for pool, scale in zip(p.k_pools, p.k_scales):
-            _dev(pool, torch.uint8, "k_pools[l]")
-            _dev(scale, torch.float32, "k_scales[l]")
-            if tuple(pool.shape) != (nb, hk, bt, dd) or not pool.is_contiguous() or hk != Hkv or dd != d:
-                raise ValueError("every pool must be contiguous uint8 [n_pool_blocks, Hkv, block_tokens, d]")
-            if tuple(scale.shape) != (nb, hk, bt // 64) or not scale.is_contiguous():
-                raise ValueError("every k_scales[l] must be contiguous fp32 [n_pool_blocks, Hkv, block_tokens / 64]")
-        if p.block_table.numel() < (p.n_tokens + bt - 1) // bt or p.importance.numel() != p.n_tokens or not p.importance.is_contiguous():
-            raise ValueError("block_table or importance has the wrong size")
-        if p.lse is not None:
-            _dev(p.lse, torch.float32, "lse")
-            if p.lse.numel() != L * Hq * m or not p.lse.is_contiguous():
-                raise ValueError("lse must be contiguous fp32 [L, Hq, m]")
-        pools = (ctypes.c_void_p * L)(*[x.data_ptr() for x in p.k_pools])
-        scales = (ctypes.c_void_p * L)(*[x.data_ptr() for x in p.k_scales])
-        keep += [pools, scales]
-        ptr = ctypes.POINTER(ctypes.c_void_p)
-        arr[i] = _PagedFp8Prompt(p.n_tokens, ctypes.cast(pools, ptr), ctypes.cast(scales, ptr), nb, bt, p.block_table.data_ptr(),
-                                 p.q.data_ptr(), p.importance.data_ptr(), _ptr(p.lse))
-    return shape, arr, keep
-
-
 def spf_score_paged_fp8_workspace_bytes(prompts: Sequence[PagedFp8PromptBuffers], softmax_scale: float = 0.0) -> int:
-    shape, arr, _keep = _marshal_paged_fp8(prompts, softmax_scale)
-    n = int(lib.spf_score_paged_fp8_workspace_bytes(ctypes.byref(shape), arr, len(prompts)))
+    n = int(_native.score_paged_fp8_workspace_bytes(prompts, softmax_scale))
     if n == 0:
         raise SpfError(-1, "spf_score_paged_fp8_workspace_bytes", spf_last_error())
     return n
@@ -498,12 +461,7 @@ def spf_score_paged_fp8_workspace_bytes(prompts: Sequence[PagedFp8PromptBuffers]
 def spf_score_paged_fp8(prompts: Sequence[PagedFp8PromptBuffers], workspace: torch.Tensor, softmax_scale: float = 0.0,
                         dev_status: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> None:
     """spf_score for keys in 8-bit block pools, as spf_kv_append writes them."""
-    shape, arr, _keep = _marshal_paged_fp8(prompts, softmax_scale)
-    if not workspace.is_cuda:
-        raise TypeError("workspace must be a CUDA tensor")
-    _check(lib.spf_score_paged_fp8(ctypes.byref(shape), arr, len(prompts), workspace.data_ptr(),
-                                   workspace.numel() * workspace.element_size(), _ptr(dev_status), _stream_ptr(stream)),
-           "spf_score_paged_fp8")
+    _check(_native.score_paged_fp8(prompts, workspace, softmax_scale, dev_status, stream), "spf_score_paged_fp8")
 
 
 def spf_score_shard_lse(prompt: PromptBuffers, workspace: torch.Tensor, softmax_scale: float = 0.0,
@@ -851,7 +809,8 @@ class Selector:
         return self.workspace
 
     def _run(self, kind: int, q, keys, aux, n_tokens: int, token_ids, char_start, char_end, keep: float, stream) -> Selection:
-        """Scoring, pooling, top-k and compaction enqueued by one native call (kind 0: contiguous, 1: paged, 2: 8-bit keys)."""
+        """Scoring, pooling, top-k and compaction enqueued by one native call (kind 0: contiguous, 1: paged, 2: 8-bit keys,
+        3: paged 8-bit keys)."""
         status, where, results = _native.select(self, kind, q, keys, aux, n_tokens, token_ids, char_start, char_end, keep, stream)
         _check(status, where)
         importance, lse, chunk_scores, k = results[0]
@@ -877,6 +836,12 @@ class Selector:
                 stream: Optional[torch.cuda.Stream] = None) -> Selection:
         """run() for a prompt whose key cache is held as E4M3 bytes (see Fp8PromptBuffers)."""
         return self._run(2, q, k_layers, k_scale, 0, token_ids, char_start, char_end, keep, stream)
+
+    def run_paged_fp8(self, q: torch.Tensor, k_pools: Sequence[torch.Tensor], k_scales: Sequence[torch.Tensor],
+                      block_table: torch.Tensor, n_tokens: int, token_ids: torch.Tensor, char_start: torch.Tensor,
+                      char_end: torch.Tensor, keep: float, stream: Optional[torch.cuda.Stream] = None) -> Selection:
+        """run() for a prompt whose keys sit in 8-bit block pools (see PagedFp8PromptBuffers)."""
+        return self._run(3, q, k_pools, (block_table, k_scales), n_tokens, token_ids, char_start, char_end, keep, stream)
 
     # device conditions after which the general path is tried: a row sum beyond fp32 (-6), a bounded wait that ran
     # out (-5); and the host refusal of a grid that cannot be co-resident (-2, raised as SpfError)

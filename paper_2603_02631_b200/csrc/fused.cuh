@@ -131,6 +131,7 @@ struct FusedPrompt {
   unsigned long long* lse;     // [slab][NCOLS] {log-sum-exp in base-2 units, 1} once known
   const float* refs;           // [slab] reference of visit 1
   const float* slab_c;         // [slab] 8-bit keys: accumulated dot product -> base-2 logit; null: FusedArgs::c for all
+  const float* tile_scales;    // [slab][n_tiles][2] 8-bit keys in blocks with scales: those of a tile's two groups of 64 keys
   unsigned* amax;              // [m][n_tiles * 128] order-preserving bits of the running maxima (parts > 1)
   unsigned* finished;          // [n_tiles][4] arrivals at `amax` (parts > 1)
   float* importance;           // [N]
@@ -230,7 +231,8 @@ __device__ __forceinline__ float from_order_bits(unsigned u) {
   return __uint_as_float((u & 0x80000000u) ? (u & 0x7fffffffu) : ~u);
 }
 
-template <int D, int NCOLS, int G, bool FP8, bool ONCE>
+// FP8: 0 bf16 keys; 1 E4M3 keys with a scale per slab, part of slab_c; 2 E4M3 keys with scales for groups of 64 (tile_scales).
+template <int D, int NCOLS, int G, int FP8, bool ONCE>
 struct FusedTraits {
   static constexpr int QS = ONCE ? kMaxQStages : 2;                // query tiles in flight per visit
   static constexpr int CW = NCOLS < 32 ? NCOLS : 32;               // visit 2: accumulators per tensor-memory load
@@ -258,6 +260,45 @@ struct FusedShare {
   int n_slabs, n_tiles;           // how many of each
   __device__ int slab(int n) const { return part + n * parts; }
   __device__ int tile(int lt) const { return first + lt * step; }
+};
+
+// Scales of groups of keys.  The 32 keys of a tile that a warp has (a quadrant of the lanes; with query rows as lanes, what
+// its quadrant has of the columns: 32, or the half of 64 keys) share one: lane j holds that of the CTA's tile 32 * chunk + j.
+// The next slab's are asked for a slab ahead; from the 33rd tile of a slab on they are fetched when they are needed.
+template <int FP8>
+struct GroupScales {
+  const float* at;
+  int first, step, n_tiles, stride, lane, chunk;
+  float now, next;
+  __device__ __forceinline__ float fetch(int slab, int c) const {
+    const int lt = 32 * c + lane;
+    return lt < n_tiles ? produced(at + (int64_t)slab * stride + 2 * (first + lt * step)) : 1.f;
+  }
+  __device__ __forceinline__ GroupScales(const FusedShare& sh, int quad, int lane_) {
+    if constexpr (FP8 == 2) {
+      at = sh.p->tile_scales + (quad >> 1);
+      first = sh.first, step = sh.step, n_tiles = sh.n_tiles, stride = 2 * sh.p->n_tiles, lane = lane_;
+      next = fetch(sh.slab(0), 0);
+    }
+  }
+  __device__ __forceinline__ void begin(const FusedShare& sh, int n) {
+    if constexpr (FP8 == 2) {
+      now = next;
+      chunk = 0;
+      if (n + 1 < sh.n_slabs) next = fetch(sh.slab(n + 1), 0);
+    }
+  }
+  // c times the scale of tile lt of slab n
+  __device__ __forceinline__ float times(float c, const FusedShare& sh, int n, int lt) {
+    if constexpr (FP8 == 2) {
+      if (lt >> 5 != chunk) {
+        chunk = lt >> 5;
+        now = fetch(sh.slab(n), chunk);
+      }
+      return c * __shfl_sync(0xffffffffu, now, lt & 31);
+    }
+    return c;
+  }
 };
 
 // ---------------------------------------------------------------------------------------------- TMA producer of one visit
@@ -330,11 +371,13 @@ __device__ __forceinline__ void fused_produce(const FusedArgs& a, const FusedSha
 // each of the two sets of epilogue warps, the odd tiles' behind the even tiles': a tile's maxima belong to one set, so with an
 // odd number of tiles a set skips two, and in a common ring of two stages it could take the tile before the one that it
 // skipped for its own (a barrier's parity tells one round from the next only).
-template <class T, int NCOLS, bool FP8, bool ROWS, bool SETS>
+template <class T, int NCOLS, int FP8, bool ROWS, bool SETS>
 __device__ __forceinline__ void fused_multiply(const FusedArgs& a, const FusedShare& sh, int v, const unsigned char* k_tiles,
                                                const unsigned char* q_tiles, uint32_t tmem, const FusedBars& bars, const Abort& ab) {
   if (!elect_one()) return;
   constexpr uint32_t idesc = ROWS ? instr_desc(NCOLS, kTileKeys, FP8) : instr_desc(kTileKeys, NCOLS, FP8);
+  // keys with scales for groups: the queries' second term is E5M2 (see the preparing kernel), format 1 of its operand
+  constexpr uint32_t idesc_low = FP8 == 2 ? idesc | (1u << (ROWS ? 7 : 10)) : idesc;
   const uint64_t k_desc0 = smem_desc<T::SUBROW>(smem_u32(k_tiles));
   const uint64_t q_desc0 = smem_desc<T::SUBROW>(smem_u32(q_tiles));
   Ring kr(a.k_stages[v]), qr(T::QS), even(SETS ? (a.t_stages[v] + 1) / 2 : a.t_stages[v]), odd(a.t_stages[v] / 2);
@@ -357,7 +400,7 @@ __device__ __forceinline__ void fused_multiply(const FusedArgs& a, const FusedSh
           for (int ks = 0; ks < T::KSTEPS; ++ks) {
             const uint64_t kd = kd0 + (uint64_t)((h * T::kSubTileBytes) >> 4) + 2u * ks;
             const uint64_t qd = qd0 + (uint64_t)(((part * T::KSUB + h) * T::kQSub) >> 4) + 2u * ks;
-            tc_mma<FP8, ROWS>(d_tmem, ROWS ? qd : kd, ROWS ? kd : qd, idesc, (uint32_t)((part | h | ks) != 0));
+            tc_mma<FP8 != 0, ROWS>(d_tmem, ROWS ? qd : kd, ROWS ? kd : qd, part == 0 ? idesc : idesc_low, (uint32_t)((part | h | ks) != 0));
           }
       tc_commit(bars.k_empty(v, kr.stage));
       tc_commit(bars.t_full(v, stage));
@@ -381,7 +424,7 @@ __device__ __forceinline__ void fused_multiply(const FusedArgs& a, const FusedSh
 // half; 32 rows: a quarter of the keys per quadrant).  Bound by the exp2 unit (16 results a cycle and SM: 512 cycles per
 // tile of 64 rows; the loop alone with its MMAs takes 645).  One load of 32 columns at a time, computed before the next is
 // asked for: the other set's warps fill the gap, and keeping a load in flight across the arithmetic measured 8 to 15 % slower.
-template <class T, int NCOLS, bool FP8>
+template <class T, int NCOLS, int FP8>
 __device__ __forceinline__ void sum_by_rows(const FusedArgs& a, const FusedShare& sh, int warp, int lane, uint32_t tmem, float* sums,
                                           const FusedBars& bars, const Abort& ab) {
   constexpr int NL = NCOLS / 32;                                   // tensor-memory loads of 32 columns per tile
@@ -398,9 +441,12 @@ __device__ __forceinline__ void sum_by_rows(const FusedArgs& a, const FusedShare
   int lt = set;                                                    // this set's next tile, counted from the slab's first
   bool ready = false;                                              // that tile's logits are there: asked before this one's arithmetic
   float next_ref = produced(refs + sh.slab(0)), next_c = FP8 ? produced(slab_c + sh.slab(0)) : a.c;
+  GroupScales<FP8> group(sh, quad, lane);
 #pragma unroll 1
   for (int n = 0; n < n_slabs; ++n) {
-    const uint64_t nref = pack2(-next_ref, -next_ref), cc = pack2(next_c, next_c);
+    const uint64_t nref = pack2(-next_ref, -next_ref), slab_cc = pack2(next_c, next_c);
+    const float slab_scale = next_c;
+    group.begin(sh, n);
     if (n + 1 < n_slabs) {
       next_ref = produced(refs + sh.slab(n + 1));
       if constexpr (FP8) next_c = produced(slab_c + sh.slab(n + 1));
@@ -408,6 +454,11 @@ __device__ __forceinline__ void sum_by_rows(const FusedArgs& a, const FusedShare
     uint64_t acc[4] = {0ull, 0ull, 0ull, 0ull};
 #pragma unroll 1
     for (; lt < n_tiles; lt += 2) {
+      uint64_t cc = slab_cc;
+      if constexpr (FP8 == 2) {
+        const float tile_c = group.times(slab_scale, sh, n, lt);
+        cc = pack2(tile_c, tile_c);
+      }
       if (!__all_sync(0xffffffffu, ready) && !mbar_wait_warp(bars.t_full(0, tr.stage), tr.phase, ab)) return;
       tc_fence_after();
       const uint32_t taddr = lane_addr + (uint32_t)(tr.stage * NCOLS);
@@ -463,7 +514,7 @@ __device__ __forceinline__ void sum_by_rows(const FusedArgs& a, const FusedShare
 // With 16 rows keys are the quicker ones, 960 -> 910 us for 16 layers x 8 heads at 340942 tokens, and its columns are half as many:
 // 28 tiles a CTA at 16 slots a key instead of 26, where the general path takes 152 us for two layers at 511438 tokens and this one
 // 105.)
-template <class T, int NCOLS, bool FP8, bool ONCE>
+template <class T, int NCOLS, int FP8, bool ONCE>
 __device__ __forceinline__ void sum_by_keys(const FusedArgs& a, const FusedShare& sh, int warp, int lane, uint32_t tmem, float* sums,
                                              const FusedBars& bars, const Abort& ab) {
   constexpr int CT = NCOLS / 4;
@@ -481,9 +532,12 @@ __device__ __forceinline__ void sum_by_keys(const FusedArgs& a, const FusedShare
   tr.advance(set);
   int lt = set;                                                    // this set's next tile, counted from the slab's first
   float next_ref = produced(refs + sh.slab(0)), next_c = FP8 ? produced(slab_c + sh.slab(0)) : a.c;
+  GroupScales<FP8> group(sh, quad, lane);
 #pragma unroll 1
   for (int n = 0; n < n_slabs; ++n) {
-    const uint64_t nref = pack2(-next_ref, -next_ref), cc = pack2(next_c, next_c);
+    const uint64_t nref = pack2(-next_ref, -next_ref), slab_cc = pack2(next_c, next_c);
+    const float slab_scale = next_c;
+    group.begin(sh, n);
     if (n + 1 < n_slabs) {
       next_ref = produced(refs + sh.slab(n + 1));
       if constexpr (FP8) next_c = produced(slab_c + sh.slab(n + 1));
@@ -493,6 +547,11 @@ __device__ __forceinline__ void sum_by_keys(const FusedArgs& a, const FusedShare
     for (int j = 0; j < CT; ++j) acc[j] = 0ull;
 #pragma unroll 1
     for (; lt < n_tiles; lt += 2) {
+      uint64_t cc = slab_cc;
+      if constexpr (FP8 == 2) {
+        const float tile_c = group.times(slab_scale, sh, n, lt);
+        cc = pack2(tile_c, tile_c);
+      }
       if (!mbar_wait_warp(bars.t_full(0, tr.stage), tr.phase, ab)) return;
       tc_fence_after();
       uint32_t r[NCOLS];
@@ -726,7 +785,7 @@ __device__ __forceinline__ void fused_store(const FusedShare& sh, int lane, cons
   }
 }
 
-template <class T, int NCOLS, int G, bool FP8, int TEAMS>
+template <class T, int NCOLS, int G, int FP8, int TEAMS>
 __device__ __forceinline__ void fused_gather(const FusedArgs& a, const FusedShare& sh, int which, int lane, const Stored& stored, float* off,
                                              float* off_c, const FusedBars& bars, const Abort& ab) {
   constexpr int LANES = NCOLS / 4 / kTeamWarps;                    // quads of this warp
@@ -805,7 +864,7 @@ __device__ __forceinline__ void fused_publish(const FusedArgs& a, const FusedSha
 
 // ---------------------------------------------------------------------------------------------- log-sum-exps for visit 2
 // Fetches each slab's log-sum-exps in turn and hands them to the max warps through shared memory (negated: what visit 2 adds).
-template <class T, int NCOLS, int G, bool FP8>
+template <class T, int NCOLS, int G, int FP8>
 __device__ __forceinline__ void fused_fetch_lse(const FusedArgs& a, const FusedShare& sh, int lane, const Stored& stored, float* off, float* off_c,
                                                 const FusedBars& bars, const Abort& ab) {
   const FusedPrompt& p = *sh.p;
@@ -978,7 +1037,7 @@ __device__ __forceinline__ void clear_maxima(uint32_t amax_addr, int set, int n_
 // ---------------------------------------------------------------------------------------------- visit 2: maxima of the tiles
 // Begins a slab once its log-sum-exps are there.  A tile's maxima always belong to the same warps (lt mod 2 == set).  REGS: up
 // to kRegTiles tiles, whose maxima stay in registers and leave all of tensor memory to the logits.
-template <class T, int NCOLS, int G, bool FP8, bool ONCE, bool REGS>
+template <class T, int NCOLS, int G, int FP8, bool ONCE, bool REGS>
 __device__ __forceinline__ void fused_max(const FusedArgs& a, const FusedShare& sh, int warp, int lane, uint32_t tmem, uint32_t amax_tmem,
                                           const float* off, const float* off_c, const FusedBars& bars, const Abort& ab) {
   constexpr int V = ONCE ? 0 : 1;                                  // whose logits: resident: those that were summed
@@ -1002,9 +1061,11 @@ __device__ __forceinline__ void fused_max(const FusedArgs& a, const FusedShare& 
   Ring last = first, end = first;                                  // resident: that of the slab before, and the slab's last tile's
   bool ready = false;
   const int stage0 = ONCE ? 0 : set * ((a.t_stages[V] + 1) / 2);
+  GroupScales<FP8> group(sh, quad, lane);
 #pragma unroll 1
   for (int n = 0; n < sh.n_slabs; ++n) {
     const int slot = n % kOffSlots;
+    group.begin(sh, n);
     if (ONCE) {
       // That the log-sum-exps contain these logits orders nothing (they come by way of relaxed words in global memory).  For the
       // products, the barrier of the slab's last tile does, whose commit tracks everything issued before it: asked ahead of the
@@ -1032,6 +1093,7 @@ __device__ __forceinline__ void fused_max(const FusedArgs& a, const FusedShare& 
         if (!__all_sync(0xffffffffu, ready) && !mbar_wait_warp(bars.t_full(V, stage0 + tr.stage), tr.phase, ab)) return false;
         tc_fence_after();
       }
+      const float tile_c = group.times(c, sh, n, lt);
       if (!REGS) tmem_store_wait();                                // the maxima read below may be this warp's last stores
 #pragma unroll
       for (int ch = 0; ch < NCH; ++ch) {
@@ -1050,7 +1112,7 @@ __device__ __forceinline__ void fused_max(const FusedArgs& a, const FusedShare& 
           if (!ONCE) ready = mbar_test_wait(bars.t_full(V, stage0 + tr.stage), tr.phase);   // the next tile's, before this one's arithmetic
         }
         if (NCH > 1) load_off(ch);
-        fold_maxima<T, G>(r, m, o, c, lane);
+        fold_maxima<T, G>(r, m, o, tile_c, lane);
         if (!REGS) tmem_store<NIW>(m_addr, m);
       }
       return true;
@@ -1093,7 +1155,7 @@ __device__ __forceinline__ void fused_max(const FusedArgs& a, const FusedShare& 
 }
 
 // ---------------------------------------------------------------------------------------------- kernel
-template <int D, int NCOLS, int G, bool FP8, bool ONCE>
+template <int D, int NCOLS, int G, int FP8, bool ONCE>
 __global__ void __launch_bounds__(kFusedThreads, 1) score_fused_kernel(const __grid_constant__ FusedArgs a) {
   using T = FusedTraits<D, NCOLS, G, FP8, ONCE>;
   static_assert(T::CW % G == 0, "a load's accumulators must hold whole GQA groups");
@@ -1237,13 +1299,15 @@ int32_t fused_launch_d64(const FusedArgs& args, const FusedLaunch& l, cudaStream
 int32_t fused_launch_d128(const FusedArgs& args, const FusedLaunch& l, cudaStream_t stream);
 int32_t fused_launch_d64_fp8(const FusedArgs& args, const FusedLaunch& l, cudaStream_t stream);
 int32_t fused_launch_d128_fp8(const FusedArgs& args, const FusedLaunch& l, cudaStream_t stream);
+int32_t fused_launch_d64_fp8_groups(const FusedArgs& args, const FusedLaunch& l, cudaStream_t stream);
+int32_t fused_launch_d128_fp8_groups(const FusedArgs& args, const FusedLaunch& l, cudaStream_t stream);
 
 // The kernel's cross-CTA hand-over needs every CTA of the grid on an SM at the same time.  The launch therefore asks the
 // runtime for exactly that guarantee (a cooperative launch; no grid-wide barrier is used): a grid that cannot be
 // co-resident -- fewer SMs available than the device reports, e.g. under MPS with a limited SM share -- is refused here
 // instead of spinning into the bounded waits.  SMs that are merely busy with other kernels delay the launch; they do not
 // break it.
-template <int D, int NCOLS, int G, bool FP8, bool ONCE>
+template <int D, int NCOLS, int G, int FP8, bool ONCE>
 int32_t fused_launch_one(const FusedArgs& args, const FusedLaunch& l, cudaStream_t stream) {
   auto kern = score_fused_kernel<D, NCOLS, G, FP8, ONCE>;
   static ContextSet allowed;
@@ -1273,7 +1337,7 @@ int32_t fused_launch_one(const FusedArgs& args, const FusedLaunch& l, cudaStream
   return SPF_OK;
 }
 
-template <int D, int NCOLS, bool FP8, bool ONCE>
+template <int D, int NCOLS, int FP8, bool ONCE>
 int32_t fused_launch_group(const FusedArgs& args, const FusedLaunch& l, cudaStream_t stream) {
   if constexpr (NCOLS <= 32) {                                     // one head per group: at most 32 lookahead queries
     if (l.padded_group == 1) return fused_launch_one<D, NCOLS, 1, FP8, ONCE>(args, l, stream);
@@ -1285,7 +1349,7 @@ int32_t fused_launch_group(const FusedArgs& args, const FusedLaunch& l, cudaStre
   }
 }
 
-template <int D, bool FP8>
+template <int D, int FP8>
 int32_t fused_launch(const FusedArgs& args, const FusedLaunch& l, cudaStream_t stream) {
   switch (l.ncols) {
     case 16: return l.once ? fused_launch_group<D, 16, FP8, true>(args, l, stream) : fused_launch_group<D, 16, FP8, false>(args, l, stream);

@@ -2,5 +2,5 @@
 #include "fused.cuh"
 
 namespace spf {
-int32_t fused_launch_d128_fp8(const FusedArgs& args, const FusedLaunch& l, cudaStream_t stream) { return fused_launch<128, true>(args, l, stream); }
+int32_t fused_launch_d128_fp8(const FusedArgs& args, const FusedLaunch& l, cudaStream_t stream) { return fused_launch<128, 1>(args, l, stream); }
 }  // namespace spf

@@ -2,5 +2,5 @@
 #include "fused.cuh"
 
 namespace spf {
-int32_t fused_launch_d64(const FusedArgs& args, const FusedLaunch& l, cudaStream_t stream) { return fused_launch<64, false>(args, l, stream); }
+int32_t fused_launch_d64(const FusedArgs& args, const FusedLaunch& l, cudaStream_t stream) { return fused_launch<64, 0>(args, l, stream); }
 }  // namespace spf

@@ -62,7 +62,8 @@ const at::Tensor& device_tensor(PyObject* o, at::ScalarType dtype, const char* n
 struct Names {
   PyObject *importance, *lse, *chunk_scores, *kept, *out_ids, *out_pos, *tok_spans, *char_spans, *counts, *dev_status, *workspace, *chunk,
       *pool_kernel, *softmax_scale, *pool_edge_rule, *force_first, *force_last, *max_tokens, *slots, *q, *k, *token_ids, *char_start,
-      *char_end, *n_tokens, *k_pool, *v_pool, *k_scale, *v_scale, *row_start, *seq_lens, *block_table, *max_new, *table, *positions, *interleaved;
+      *char_end, *n_tokens, *k_pool, *v_pool, *k_scale, *v_scale, *row_start, *seq_lens, *block_table, *max_new, *table, *positions, *interleaved,
+      *k_pools, *k_scales;
 };
 Names N;
 
@@ -92,7 +93,7 @@ bool attr_true(PyObject* o, PyObject* name) {
   return v != 0;
 }
 
-enum Kind { kPlain = 0, kPaged = 1, kFp8 = 2 };
+enum Kind { kPlain = 0, kPaged = 1, kFp8 = 2, kPagedFp8 = 3 };
 
 // One prompt's scoring inputs in the form of its kind.  `held` keeps the tensors behind the pointers until the kernels are
 // enqueued: what the caller handed over may be temporary (a property that casts, a sequence that makes its items), and memory
@@ -100,13 +101,15 @@ enum Kind { kPlain = 0, kPaged = 1, kFp8 = 2 };
 struct Inputs {
   std::vector<at::Tensor> held;
   std::vector<const void*> layers;
+  std::vector<const float*> scales;            // per layer (paged 8-bit keys)
   int64_t n = 0;
   const void *q = nullptr, *aux = nullptr;     // aux: block table or key scales
   int64_t stride_head = 0, stride_tok = 0, pool_blocks = 0;
   int block_tokens = 0;
 };
 
-// Checks q and the layers' key tensors; the first prompt of a call fixes the shape.  `n_paged`: tokens of a paged prompt.
+// Checks q and the layers' key tensors; the first prompt of a call fixes the shape.  `n_paged`: tokens of a paged prompt.  `aux`: the
+// block table (paged), the key scales (8 bits), or a tuple of the block table and a sequence of the layers' scales (both).
 void read_inputs(Kind kind, PyObject* q_obj, PyObject* layers_obj, PyObject* aux_obj, int64_t n_paged, double scale, bool first,
                  spf_shape* shape, Inputs* in) {
   const at::Tensor& q = device_tensor(q_obj, at::kBFloat16, "q");
@@ -115,12 +118,13 @@ void read_inputs(Kind kind, PyObject* q_obj, PyObject* layers_obj, PyObject* aux
   Ref layers(PySequence_Fast(layers_obj, "the key tensors must be a sequence"));
   const Py_ssize_t count = PySequence_Fast_GET_SIZE(layers.p);
   PyObject** items = PySequence_Fast_ITEMS(layers.p);
-  const at::ScalarType dtype = kind == kFp8 ? at::kByte : at::kBFloat16;
+  const bool paged = kind == kPaged || kind == kPagedFp8;
+  const at::ScalarType dtype = kind == kFp8 || kind == kPagedFp8 ? at::kByte : at::kBFloat16;
   if (count < 1) raise(PyExc_ValueError, "k_layers must hold one tensor per layer");
   const at::Tensor& k0 = device_tensor(items[0], dtype, "k_layers[l]");
-  const int64_t dims = kind == kPaged ? 4 : 3;
+  const int64_t dims = paged ? 4 : 3;
   if (k0.dim() != dims) raise(PyExc_ValueError, "a key tensor has the wrong number of dimensions");
-  const int64_t hkv = kind == kPaged ? k0.size(1) : k0.size(0);
+  const int64_t hkv = paged ? k0.size(1) : k0.size(0);
   if (first) {
     shape->n_layers = (int32_t)q.size(0);
     shape->n_q_heads = (int32_t)q.size(1);
@@ -140,16 +144,33 @@ void read_inputs(Kind kind, PyObject* q_obj, PyObject* layers_obj, PyObject* aux
     const at::Tensor& kl = device_tensor(items[l], dtype, "k_layers[l]");
     in->held.push_back(kl);
     bool fine = kl.dim() == dims && kl.sizes() == k0.sizes() && kl.size(dims - 1) == shape->head_dim && hkv == shape->n_kv_heads;
-    if (kind == kPaged) fine = fine && kl.is_contiguous();
+    if (paged) fine = fine && kl.is_contiguous();
     else fine = fine && kl.stride(2) == 1 && kl.strides() == k0.strides();
     if (!fine)
-      raise(PyExc_ValueError, kind == kPaged ? "every pool must be contiguous bf16 [n_pool_blocks, Hkv, block_tokens, d]"
-                                             : "every k_layers[l] must be [Hkv, N, d] with a contiguous last dim and equal strides");
+      raise(PyExc_ValueError, kind == kPaged      ? "every pool must be contiguous bf16 [n_pool_blocks, Hkv, block_tokens, d]"
+                              : kind == kPagedFp8 ? "every pool must be contiguous uint8 [n_pool_blocks, Hkv, block_tokens, d]"
+                                                  : "every k_layers[l] must be [Hkv, N, d] with a contiguous last dim and equal strides");
     in->layers[(size_t)l] = kl.data_ptr();
   }
   in->q = q.data_ptr();
-  if (kind == kPaged) {
-    const at::Tensor& table = device_tensor(aux_obj, at::kInt, "block_table");
+  if (paged) {
+    PyObject* table_obj = aux_obj;
+    if (kind == kPagedFp8) {
+      if (!PyTuple_Check(aux_obj) || PyTuple_GET_SIZE(aux_obj) != 2) raise(PyExc_TypeError, "block_table and k_scales are wanted");
+      table_obj = PyTuple_GET_ITEM(aux_obj, 0);
+      PyObject* scales_obj = PyTuple_GET_ITEM(aux_obj, 1);
+      if (PyIter_Check(scales_obj)) raise(PyExc_TypeError, "k_scales must be a sequence");
+      Ref scales(PySequence_Fast(scales_obj, "k_scales must be a sequence"));
+      if (PySequence_Fast_GET_SIZE(scales.p) != count) raise(PyExc_ValueError, "k_scales must hold one tensor per layer");
+      for (Py_ssize_t l = 0; l < count; ++l) {
+        const at::Tensor& t = device_tensor(PySequence_Fast_GET_ITEM(scales.p, l), at::kFloat, "k_scales[l]");
+        in->held.push_back(t);
+        if (t.dim() != 3 || !t.is_contiguous() || t.size(0) != k0.size(0) || t.size(1) != hkv || t.size(2) != k0.size(2) / SPF_KV_SCALE_TOKENS)
+          raise(PyExc_ValueError, "every k_scales[l] must be contiguous fp32 [n_pool_blocks, Hkv, block_tokens / 64]");
+        in->scales.push_back(t.data_ptr<float>());
+      }
+    }
+    const at::Tensor& table = device_tensor(table_obj, at::kInt, "block_table");
     in->n = n_paged;
     in->block_tokens = (int)k0.size(2);
     in->pool_blocks = k0.size(0);
@@ -292,9 +313,12 @@ PyObject* select_one(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
     spf_prompt plain{in.n, in.layers.data(), in.stride_head, in.stride_tok, in.q, b.importance_ptr, b.lse_ptr};
     spf_paged_prompt paged{in.n, in.layers.data(), in.pool_blocks, in.block_tokens, static_cast<const int32_t*>(in.aux), in.q, b.importance_ptr, b.lse_ptr};
     spf_fp8_prompt fp8{in.n, in.layers.data(), in.stride_head, in.stride_tok, static_cast<const float*>(in.aux), in.q, b.importance_ptr, b.lse_ptr};
+    spf_paged_fp8_prompt paged_fp8{in.n, in.layers.data(), in.scales.data(), in.pool_blocks, in.block_tokens, static_cast<const int32_t*>(in.aux), in.q,
+                                   b.importance_ptr, b.lse_ptr};
     const size_t need = kind == kPlain ? spf_score_workspace_bytes(&shape, &plain, 1)
                         : kind == kPaged ? spf_score_paged_workspace_bytes(&shape, &paged, 1)
-                                         : spf_score_fp8_workspace_bytes(&shape, &fp8, 1);
+                        : kind == kFp8   ? spf_score_fp8_workspace_bytes(&shape, &fp8, 1)
+                                         : spf_score_paged_fp8_workspace_bytes(&shape, &paged_fp8, 1);
     if (need == 0) return result_tuple(SPF_ERR_INVALID_ARG, "spf_score_workspace_bytes", nullptr, 0);
     const at::Tensor ws = workspace_of(selector, need, b.importance);
     const size_t ws_bytes = (size_t)ws.numel() * ws.element_size();
@@ -303,10 +327,11 @@ PyObject* select_one(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
     int32_t st;
     const char* where;
     Py_BEGIN_ALLOW_THREADS;
-    where = kind == kPlain ? "spf_score" : kind == kPaged ? "spf_score_paged" : "spf_score_fp8";
+    where = kind == kPlain ? "spf_score" : kind == kPaged ? "spf_score_paged" : kind == kFp8 ? "spf_score_fp8" : "spf_score_paged_fp8";
     st = kind == kPlain ? spf_score(&shape, &plain, 1, ws_ptr, ws_bytes, status, stream)
          : kind == kPaged ? spf_score_paged(&shape, &paged, 1, ws_ptr, ws_bytes, status, stream)
-                          : spf_score_fp8(&shape, &fp8, 1, ws_ptr, ws_bytes, status, stream);
+         : kind == kFp8   ? spf_score_fp8(&shape, &fp8, 1, ws_ptr, ws_bytes, status, stream)
+                          : spf_score_paged_fp8(&shape, &paged_fp8, 1, ws_ptr, ws_bytes, status, stream);
     if (st == SPF_OK) {
       where = "spf_pool_select_compact";
       const spf_path_item item = path_item(b, in.n);
@@ -585,6 +610,82 @@ PyObject* kv_append(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
   }
 }
 
+// The prompts of a call on 8-bit block pools (PagedFp8PromptBuffers).
+struct PagedFp8Call {
+  spf_shape shape{};
+  std::vector<Inputs> in;
+  std::vector<spf_paged_fp8_prompt> prompts;
+  std::vector<at::Tensor> held;
+  PagedFp8Call(PyObject* list, double scale) {
+    Ref seq(PySequence_Fast(list, "prompts must be a sequence"));
+    const size_t count = (size_t)PySequence_Fast_GET_SIZE(seq.p);
+    if (count == 0) raise(PyExc_IndexError, "no prompts");
+    in.resize(count);
+    prompts.resize(count);
+    for (size_t i = 0; i < count; ++i) {
+      PyObject* o = PySequence_Fast_GET_ITEM(seq.p, (Py_ssize_t)i);
+      const Ref q(attr(o, N.q)), pools(attr(o, N.k_pools)), table(attr(o, N.block_table)), scales(attr(o, N.k_scales));
+      const Ref aux(PyTuple_Pack(2, table.p, scales.p));
+      const int64_t n = attr_int(o, N.n_tokens);
+      if (n < 0) raise(PyExc_ValueError, "n_tokens must not be negative");
+      read_inputs(kPagedFp8, q.p, pools.p, aux.p, n, scale, i == 0, &shape, &in[i]);
+      const at::Tensor importance = attr_tensor(o, N.importance, at::kFloat, "importance"), lse = attr_tensor_or_none(o, N.lse, at::kFloat, "lse");
+      if (importance.numel() != n || !importance.is_contiguous()) raise(PyExc_ValueError, "block_table or importance has the wrong size");
+      if (lse.defined() && (lse.numel() != (int64_t)shape.n_layers * shape.n_q_heads * shape.n_lookahead || !lse.is_contiguous()))
+        raise(PyExc_ValueError, "lse must be contiguous fp32 [L, Hq, m]");
+      held.push_back(importance);
+      held.push_back(lse);
+      prompts[i] = spf_paged_fp8_prompt{n, in[i].layers.data(), in[i].scales.data(), in[i].pool_blocks, in[i].block_tokens,
+                                        static_cast<const int32_t*>(in[i].aux), in[i].q, importance.data_ptr<float>(),
+                                        lse.defined() ? lse.data_ptr<float>() : nullptr};
+    }
+  }
+};
+
+// score_paged_fp8_workspace_bytes(prompts, softmax_scale) -> bytes (0: the reason is in spf_last_error())
+PyObject* score_paged_fp8_workspace_bytes(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
+  try {
+    if (n_args != 2) raise(PyExc_TypeError, "score_paged_fp8_workspace_bytes takes 2 arguments");
+    const double scale = PyFloat_AsDouble(args[1]);
+    if (PyErr_Occurred()) throw PyFailure{};
+    const PagedFp8Call call(args[0], scale);
+    return PyLong_FromSize_t(spf_score_paged_fp8_workspace_bytes(&call.shape, call.prompts.data(), (int32_t)call.prompts.size()));
+  } catch (const PyFailure&) {
+    return nullptr;
+  } catch (const std::exception& e) {
+    PyErr_SetString(PyExc_RuntimeError, e.what());
+    return nullptr;
+  }
+}
+
+// score_paged_fp8(prompts, workspace, softmax_scale, dev_status, stream) -> status
+PyObject* score_paged_fp8(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
+  try {
+    if (n_args != 5) raise(PyExc_TypeError, "score_paged_fp8 takes 5 arguments");
+    const double scale = PyFloat_AsDouble(args[2]);
+    if (PyErr_Occurred()) throw PyFailure{};
+    const PagedFp8Call call(args[0], scale);
+    const at::Tensor ws = tensor(args[1], "workspace");
+    if (!ws.is_cuda()) raise(PyExc_TypeError, "workspace must be a CUDA tensor");
+    at::Tensor status;
+    if (args[3] != Py_None) status = device_tensor(args[3], at::kInt, "dev_status");
+    void* stream = stream_of(args[4]);
+    void* ws_ptr = ws.data_ptr();
+    const size_t ws_bytes = (size_t)ws.numel() * ws.element_size();
+    int32_t st;
+    Py_BEGIN_ALLOW_THREADS;
+    st = spf_score_paged_fp8(&call.shape, call.prompts.data(), (int32_t)call.prompts.size(), ws_ptr, ws_bytes,
+                             status.defined() ? status.data_ptr<int32_t>() : nullptr, stream);
+    Py_END_ALLOW_THREADS;
+    return PyLong_FromLong(st);
+  } catch (const PyFailure&) {
+    return nullptr;
+  } catch (const std::exception& e) {
+    PyErr_SetString(PyExc_RuntimeError, e.what());
+    return nullptr;
+  }
+}
+
 // attend_workspace_bytes(cache, step, q) -> bytes (0: the reason is in spf_last_error())
 PyObject* attend_workspace_bytes(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
   try {
@@ -648,6 +749,9 @@ PyObject* attend(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
 }
 
 PyMethodDef kMethods[] = {
+    {"score_paged_fp8_workspace_bytes", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(score_paged_fp8_workspace_bytes)), METH_FASTCALL,
+     "Workspace of score_paged_fp8."},
+    {"score_paged_fp8", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(score_paged_fp8)), METH_FASTCALL, "Scores prompts in 8-bit block pools."},
     {"attend_workspace_bytes", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(attend_workspace_bytes)), METH_FASTCALL, "Workspace of attend."},
     {"attend", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(attend)), METH_FASTCALL, "A step's attention over the cache."},
     {"kv_append", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(kv_append)), METH_FASTCALL, "A step's keys and values into the cache."},
@@ -668,6 +772,7 @@ PyMODINIT_FUNC PyInit__native() {
   SPF_NAME(q); SPF_NAME(k); SPF_NAME(token_ids); SPF_NAME(char_start); SPF_NAME(char_end); SPF_NAME(n_tokens);
   SPF_NAME(k_pool); SPF_NAME(v_pool); SPF_NAME(k_scale); SPF_NAME(v_scale); SPF_NAME(row_start); SPF_NAME(seq_lens); SPF_NAME(block_table);
   SPF_NAME(max_new); SPF_NAME(table); SPF_NAME(positions); SPF_NAME(interleaved);
+  SPF_NAME(k_pools); SPF_NAME(k_scales);
 #undef SPF_NAME
   return PyModule_Create(&kModule);
 }

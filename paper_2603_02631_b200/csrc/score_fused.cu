@@ -21,7 +21,19 @@ namespace {
 // bits and each term carries 4, so the pair is exact for every element within 2^9 of the slab's largest and off by at most
 // 2^-17 of that largest value below (the remainder's last bits fall under the format's smallest step, 2^-9).  Next to
 // them goes the slab's factor from accumulated dot product to base-2 logit: softmax scale * log2(e) * key scale / S.
+//
+// Keys with scales for groups of 64: the second term is E5M2.  What the first leaves is at most half a step of its own, so three
+// significant bits hold it, and E5M2 goes on where E4M3's steps end: exact for every element within 2^13 of the slab's largest |q|,
+// off by at most 2^-21 of that largest below.  (E4M3 terms: 2^9 and 2^-17, which at 131072 tokens was half of the importance's
+// error, 1.0e-6 instead of 6.3e-7 in the 2-norm.)
 constexpr int kPrepThreads = 256;
+
+// fp32 to the nearest E5M2 byte (saturating).
+__device__ __forceinline__ uint32_t float_to_e5m2(float x) {
+  uint32_t out;
+  asm("{\n.reg .b16 r;\ncvt.rn.satfinite.e5m2x2.f32 r, %1, %2;\ncvt.u32.u16 %0, r;\n}" : "=r"(out) : "f"(0.f), "f"(x));
+  return out & 0xffu;
+}
 
 struct PrepPrompt {
   CUtensorMap k_map;
@@ -38,15 +50,25 @@ struct PrepPrompt {
   int block_tokens;
 };
 
-template <int N>
+// 8-bit keys with scales for groups of 64: the layers' scale pools, and where each slab's are laid out tile by tile.
+template <bool GROUPS>
+struct PrepScales {};
+template <>
+struct PrepScales<true> {
+  const float* pools[kFusedMaxLayers];
+  float* tile_scales;              // [slab][n_tiles][2]
+};
+
+template <int N, bool GROUPS>
 struct PrepArgs {
   PrepPrompt prompt[N];
+  PrepScales<GROUPS> scales[N];
   int n_kv_heads, group, padded_group, n_lookahead, ncols;
   float c;
 };
 
-template <int D, bool FP8, int N>
-__global__ void __launch_bounds__(kPrepThreads) fused_prep_kernel(const __grid_constant__ PrepArgs<N> a) {
+template <int D, int FP8, int N>
+__global__ void __launch_bounds__(kPrepThreads) fused_prep_kernel(const __grid_constant__ PrepArgs<N, FP8 == 2> a) {
   const PrepPrompt& p = a.prompt[blockIdx.y];
   const int slab = blockIdx.x, n_slabs = gridDim.x;
   const int layer = slab / a.n_kv_heads, hk = slab - layer * a.n_kv_heads;
@@ -100,7 +122,8 @@ __global__ void __launch_bounds__(kPrepThreads) fused_prep_kernel(const __grid_c
               const float s = ((x & 1) ? f.y : f.x) * S;
               const uint32_t t = float_to_e4m3(s);
               hi[2 * half + (x >> 2)] |= t << (8 * (x & 3));
-              lo[2 * half + (x >> 2)] |= float_to_e4m3(s - e4m3_to_float(t)) << (8 * (x & 3));
+              const float rest = s - e4m3_to_float(t);
+              lo[2 * half + (x >> 2)] |= (FP8 == 2 ? float_to_e5m2(rest) : float_to_e4m3(rest)) << (8 * (x & 3));
             }
           }
         }
@@ -118,6 +141,25 @@ __global__ void __launch_bounds__(kPrepThreads) fused_prep_kernel(const __grid_c
   if (p.block_tokens > 0) {
     sample_block = min(max((int64_t)__ldg(p.block_table + sample_key / p.block_tokens), (int64_t)0), p.n_pool_blocks - 1);
     sample_row = sample_key % p.block_tokens;
+  }
+  float key_scale = 1.f;                                            // of the sample key
+  if constexpr (FP8 == 1) key_scale = __ldg(p.key_scale + slab);
+  if constexpr (FP8 == 2) {
+    const PrepScales<true>& ps = a.scales[blockIdx.y];
+    const int groups = p.block_tokens / SPF_KV_SCALE_TOKENS, total = (int)((p.n_tokens + kTileKeys - 1) / kTileKeys) * 2;
+    const float* pool = ps.pools[layer] + (int64_t)hk * groups;
+    key_scale = __ldg(pool + sample_block * a.n_kv_heads * groups + sample_row / SPF_KV_SCALE_TOKENS);
+#pragma unroll 4
+    for (int i = threadIdx.x; i < total; i += kPrepThreads) {
+      const int64_t key0 = (int64_t)i * SPF_KV_SCALE_TOKENS;
+      float s = 1.f;                                                // behind the prompt's end, and for blocks outside the pool (zeros)
+      if (key0 < p.n_tokens) {
+        const int64_t block = __ldg(p.block_table + key0 / p.block_tokens);
+        if (block >= 0 && block < p.n_pool_blocks)
+          s = __ldg(pool + block * a.n_kv_heads * groups + key0 % p.block_tokens / SPF_KV_SCALE_TOKENS);
+      }
+      ps.tile_scales[(int64_t)slab * total + i] = s;
+    }
   }
   constexpr int LPR = D / 8;                                        // lanes per row: 8 elements of it each
   const int rows = a.group * a.n_lookahead;
@@ -167,7 +209,7 @@ __global__ void __launch_bounds__(kPrepThreads) fused_prep_kernel(const __grid_c
   if (threadIdx.x == 0) {
     for (int w = 1; w < kPrepThreads / 32; ++w) ref = fminf(ref, red[w]);
     // a softmax scale (and a key scale) is positive, so the smallest q.k is the smallest logit
-    p.refs[slab] = fmaf(ref, FP8 ? a.c * __ldg(p.key_scale + slab) : a.c, kRefMargin);
+    p.refs[slab] = fmaf(ref, FP8 ? a.c * key_scale : a.c, kRefMargin);
   }
   if constexpr (FP8) {
     __syncthreads();
@@ -183,22 +225,25 @@ __global__ void __launch_bounds__(kPrepThreads) fused_prep_kernel(const __grid_c
         S = ldexpf(1.f, max(-100, min(ex - 1, 100)));
       }
       s_scale = S;
-      p.slab_c[slab] = a.c * __ldg(p.key_scale + slab) / S;
+      p.slab_c[slab] = a.c * (FP8 == 1 ? key_scale : 1.f) / S;
     }
     __syncthreads();
   }
   if constexpr (FP8) write_image(s_scale);
 }
 
-template <int N>
-int32_t launch_prep(const PrepArgs<N>& args, int d, bool fp8, int n_slabs, int n_prompts, cudaStream_t stream) {
+template <int N, bool GROUPS>
+int32_t launch_prep(const PrepArgs<N, GROUPS>& args, int d, bool fp8, int n_slabs, int n_prompts, cudaStream_t stream) {
   const dim3 grid((unsigned)n_slabs, (unsigned)n_prompts);
-  if (fp8) {
-    if (d == 64) fused_prep_kernel<64, true, N><<<grid, kPrepThreads, 0, stream>>>(args);
-    else fused_prep_kernel<128, true, N><<<grid, kPrepThreads, 0, stream>>>(args);
+  if constexpr (GROUPS) {
+    if (d == 64) fused_prep_kernel<64, 2, N><<<grid, kPrepThreads, 0, stream>>>(args);
+    else fused_prep_kernel<128, 2, N><<<grid, kPrepThreads, 0, stream>>>(args);
+  } else if (fp8) {
+    if (d == 64) fused_prep_kernel<64, 1, N><<<grid, kPrepThreads, 0, stream>>>(args);
+    else fused_prep_kernel<128, 1, N><<<grid, kPrepThreads, 0, stream>>>(args);
   } else {
-    if (d == 64) fused_prep_kernel<64, false, N><<<grid, kPrepThreads, 0, stream>>>(args);
-    else fused_prep_kernel<128, false, N><<<grid, kPrepThreads, 0, stream>>>(args);
+    if (d == 64) fused_prep_kernel<64, 0, N><<<grid, kPrepThreads, 0, stream>>>(args);
+    else fused_prep_kernel<128, 0, N><<<grid, kPrepThreads, 0, stream>>>(args);
   }
   SPF_CUDA_CHECK(cudaGetLastError());
   return SPF_OK;
@@ -265,11 +310,10 @@ struct Geometry {
 
 Geometry geometry(const ScoreProblem& p, int sm_count) {
   Geometry g;
-  if (p.scale_blocks) return g;                       // scales for groups of keys: the general path
-  g.fp8 = p.k_scale != nullptr;
-  // 8-bit key caches: contiguous only, and the TMA wants 16-byte aligned layer pointers and strides (the general path reads
-  // them 8 bytes at a time and takes what this refuses)
-  if (g.fp8) {
+  g.fp8 = p.k_scale != nullptr || p.scale_blocks;
+  // 8-bit key caches with a scale per slab: contiguous only, and the TMA wants 16-byte aligned layer pointers and strides (the
+  // general path reads them 8 bytes at a time and takes what this refuses)
+  if (g.fp8 && !p.scale_blocks) {
     if (p.block_tokens > 0 || p.stride_tok % 16 != 0 || p.stride_head % 16 != 0) return g;
     for (int l = 0; l < p.n_layers; ++l)
       if (reinterpret_cast<uintptr_t>(p.k.p[l]) % 16 != 0) return g;
@@ -446,7 +490,7 @@ bool pick_stages(const Geometry& g, int d, int tiles, bool paged, FusedArgs* a, 
 
 // ---------------------------------------------------------------------------------------------- workspace
 struct FusedWorkspace {
-  size_t k_maps, refs, slab_c, q_tiles;              // written by the preparing kernel
+  size_t k_maps, refs, slab_c, tile_scales, q_tiles;  // written by the preparing kernel
   size_t row_sums, lse;                              // cleared by it, the sums as far as used
   size_t finished, amax;                             // cleared by it where groups meet
   size_t total;
@@ -464,7 +508,8 @@ FusedWorkspace fused_workspace(const ScoreProblem& p) {
   };
   w.k_maps = take((size_t)p.n_layers * sizeof(CUtensorMap));
   w.refs = take(n_slabs * sizeof(float));
-  w.slab_c = take(p.k_scale != nullptr ? n_slabs * sizeof(float) : 0);
+  w.slab_c = take(p.k_scale != nullptr || p.scale_blocks ? n_slabs * sizeof(float) : 0);
+  w.tile_scales = take(p.scale_blocks ? n_slabs * n_tiles * 2 * sizeof(float) : 0);
   w.q_tiles = take(n_slabs * 2 * ncols * (size_t)p.head_dim);     // bf16, or two 8-bit terms
   w.row_sums = take(n_slabs * std::min<size_t>(n_tiles, kFusedMaxCtas) * ncols * sizeof(float));
   w.lse = take(n_slabs * ncols * sizeof(unsigned long long));
@@ -517,10 +562,10 @@ int32_t encode_key_map(const ScoreProblem& p, const Geometry& g, CUtensorMap* ma
   return SPF_OK;
 }
 
-template <int N>
+template <int N, bool GROUPS>
 int32_t launch_group(const ScoreProblem* p, int n, const Geometry* geometries, const Split* split, char* base, int sm_count, int32_t* dev_status,
                      cudaStream_t stream, int mode, const float* lse_in) {
-  PrepArgs<N> prep{};
+  PrepArgs<N, GROUPS> prep{};
   FusedArgs args{};
   const ScoreProblem& p0 = p[0];
   const Geometry& g = geometries[0];                                 // the prompts' differ in lead alone
@@ -556,6 +601,11 @@ int32_t launch_group(const ScoreProblem* p, int n, const Geometry* geometries, c
     pp.slab_c = reinterpret_cast<float*>(base + w.slab_c);
     pp.q_tiles = reinterpret_cast<unsigned char*>(base + w.q_tiles);
     pp.key_scale = q.k_scale;
+    if constexpr (GROUPS) {
+      for (int layer = 0; layer < q.n_layers; ++layer) prep.scales[i].pools[layer] = q.k_scale_pools.p[layer];
+      prep.scales[i].tile_scales = reinterpret_cast<float*>(base + w.tile_scales);
+      fp.tile_scales = prep.scales[i].tile_scales;
+    }
     pp.block_table = q.block_table;
     pp.n_tokens = q.n_tokens;
     pp.stride_head = q.stride_head;
@@ -592,8 +642,9 @@ int32_t launch_group(const ScoreProblem* p, int n, const Geometry* geometries, c
   }
   if (!pick_stages(g, p0.head_dim, most_tiles, p0.block_tokens > 0, &args, &l.smem_bytes))
     return fail(SPF_ERR_UNSUPPORTED, "spf_score: shape not covered by the fused path");
-  const int32_t st = launch_prep<N>(prep, p0.head_dim, g.fp8, g.n_slabs, n, stream);
+  const int32_t st = launch_prep<N, GROUPS>(prep, p0.head_dim, g.fp8, g.n_slabs, n, stream);
   if (st != SPF_OK) return st;
+  if constexpr (GROUPS) return p0.head_dim == 64 ? fused_launch_d64_fp8_groups(args, l, stream) : fused_launch_d128_fp8_groups(args, l, stream);
   if (p0.head_dim == 64) return g.fp8 ? fused_launch_d64_fp8(args, l, stream) : fused_launch_d64(args, l, stream);
   return g.fp8 ? fused_launch_d128_fp8(args, l, stream) : fused_launch_d128(args, l, stream);
 }
@@ -643,8 +694,11 @@ int32_t score_fused_launch(const ScoreProblem* p, int n_prompts, void* workspace
   if (!split_group(g, n_tiles, n, sm_count, split)) return fail(SPF_ERR_UNSUPPORTED, "spf_score: shape not covered by the fused path");
   if (done != nullptr) *done = n;
   char* base = static_cast<char*>(workspace);
-  return n == 1 ? launch_group<1>(p, n, g, split, base, sm_count, dev_status, stream, mode, lse_in)
-                : launch_group<kFusedMaxBatch>(p, n, g, split, base, sm_count, dev_status, stream, mode, lse_in);
+  if (p[0].scale_blocks)
+    return n == 1 ? launch_group<1, true>(p, n, g, split, base, sm_count, dev_status, stream, mode, lse_in)
+                  : launch_group<kFusedMaxBatch, true>(p, n, g, split, base, sm_count, dev_status, stream, mode, lse_in);
+  return n == 1 ? launch_group<1, false>(p, n, g, split, base, sm_count, dev_status, stream, mode, lse_in)
+                : launch_group<kFusedMaxBatch, false>(p, n, g, split, base, sm_count, dev_status, stream, mode, lse_in);
 }
 
 }  // namespace spf

@@ -103,3 +103,31 @@ def test_batch_of_prompts(path):
     for b, want in zip(bufs, wants):
         got = b.importance.cpu().numpy()
         assert np.max(np.abs(got - want) / np.maximum(want, 1e-30)) <= 1e-3
+
+
+def test_selector():
+    """Selector.run_paged_fp8 gives what the calls one by one give."""
+    import paper_2603_02631_b200 as spf
+    L, Hq, Hkv, d, m, N, block = 2, 8, 2, 64, 8, 5000, 256
+    prompt = _prompt(L, Hq, Hkv, d, m, N, block)
+    pools, scales, table, _ = make_pools(prompt.k, N, block, seed=1)
+    dp = prompt.to("cuda:0")
+    imp = torch.empty(N, device="cuda")
+    _score(spf, [spf.PagedFp8PromptBuffers(dp.q, pools, scales, table, N, imp)], 0)
+    sel = spf.Selector(L, Hq, Hkv, d, m, N)
+    got = sel.run_paged_fp8(dp.q, pools, scales, table, N, dp.token_ids, dp.char_start, dp.char_end, 0.25)
+    torch.cuda.synchronize()
+    assert int(sel.dev_status.item()) == 0
+    assert torch.equal(got.importance, imp)
+    scores = torch.empty((N + 31) // 32, device="cuda")
+    kept = torch.empty(got.k, dtype=torch.int32, device="cuda")
+    spf.spf_chunk_pool(imp, 13, 32, scores)
+    spf.spf_select_topk(scores, scores.numel(), got.k, kept)
+    torch.cuda.synchronize()
+    assert torch.equal(kept, got.kept_chunks[:got.k])
+    with pytest.raises(ValueError):
+        sel.run_paged_fp8(dp.q, pools, scales[:1], table, N, dp.token_ids, dp.char_start, dp.char_end, 0.25)
+    with pytest.raises(TypeError):
+        sel.run_paged_fp8(dp.q, pools, [s.double() for s in scales], table, N, dp.token_ids, dp.char_start, dp.char_end, 0.25)
+    with pytest.raises(ValueError):
+        spf.spf_score_paged_fp8_workspace_bytes([spf.PagedFp8PromptBuffers(dp.q, pools, [s[:, :, :1] for s in scales], table, N, imp)])
