@@ -10,18 +10,23 @@
 // host) joins them in the order of the keys.  All of it is worked out on the device from the lengths there.
 //
 // A CTA: one warp copies tiles into a ring (TMA, 64 keys and their values a stage) and runs ahead across the triples' borders;
-// four warps compute, each on its own 16 keys of every tile (32 with 64 rows: two warps share a row half), with maxima, sums and
-// outputs of their own in registers, so that nothing is exchanged between them until a triple ends.  Products are warp-level
-// (m16n8k16): with at most 16 rows in a tile the tensor cores' big instruction would be idle for the most part, and the keys'
-// read takes longer than these.
+// four warps compute, each on its own 16 keys of every tile (many rows: some of the rows and more of the keys), with maxima, sums
+// and outputs of their own in registers, so that nothing is exchanged between them until a triple ends.  Products are warp-level, with
+// the keys (then the dimensions of the values) as the 16 rows of the left operand and the query rows as the 8 columns of the right
+// one: a single token's few heads fill a product, where they would be half or less of the left operand's rows, and the tensor
+// cores' big instruction would be idle for the most part; the keys' read takes longer than these.  Logits have keys as
+// rows and queries as columns; a weight is wanted the other way round, which one movmatrix per 8 x 8 does.
 //
 // The reference m_r moves only when a logit exceeds it by 8 (2^8 is far from any format's limit): most tiles need no exchange
 // of maxima and no rescaling of the output.  Weights are rounded to the format of the second product's operands: bf16 (8 bits;
 // the output is bf16 too) over bf16 values, fp16 (11 bits) over 8-bit ones; their sum l is taken in fp32 before that.
 //
-// 8 bits: E4M3 is widened to fp16, exactly, next to the products.  Queries become fp16 after a power of two per row that puts
-// the largest element in [2^14, 2^15): exact for elements within 2^-29 of it.  A tile's value scale s_v joins its logits, so that the
-// weights are p s_v / (the largest such so far) and never leave fp16's range, and l takes them divided by s_v again:
+// 8 bits, keys: multiplied as they are (m16n8k32, E4M3) by queries in two terms, E4M3 and E5M2: q 2^e = hi + lo, with the power of
+// two e of a row that takes its largest element to (224, 448].  Exact for elements within 2^13 of that one, off by at most 2^-21 of
+// it below: hi has 4 significant bits, what it leaves is at most half its step and fits lo's 3.
+// 8 bits, values: widened to fp16, exactly, next to the products (widen4; both operands by the conversion instruction, which is
+// slow: 697 instead of 384 us for four sequences of 131 to 250 thousand tokens).  A tile's value scale s_v joins its logits, so that the weights are p s_v / (the largest such so far) and never
+// leave fp16's range, and l takes them divided by s_v again:
 //   z'[r,s] = z[r,s] + log2 s_v,  w = 2^(z' - m' + 7),  out = sum w byte / l,  l = sum w / s_v,  lse = (m' - 7 + log2 l) ln 2.
 //
 // Keys that no row may see (behind the sequence's end, before its first key) take part with logits of -inf and values of zero,
@@ -36,8 +41,9 @@ namespace {
 
 constexpr int kKeys = 64;               // keys of a tile: one scale's worth
 constexpr int kWarps = 4;               // that compute
-constexpr int kThreads = (kWarps + 1) * 32;
-constexpr int kCtasPerSm = 2;
+// From 16 rows on a second warpgroup, whose first warp copies, lends registers of the 128 a thread that the launch has,
+// 128 x (192 + 64) = 256 x 128.
+constexpr int kComputeRegs = 192, kOtherRegs = 64;
 constexpr int kMaxStages = 8;
 constexpr float kLazy = 8.f;            // how far logits may exceed their reference
 constexpr float kShift = 7.f;           // 8-bit values: weights reach 2^(kLazy + kShift) = 2^15, below fp16's 65504
@@ -54,13 +60,18 @@ template <int D_, bool FP8_, int R_>
 struct Traits {
   static constexpr int D = D_, R = R_;
   static constexpr bool FP8 = FP8_;
-  static constexpr int WR = R == 64 ? 2 : 1, WK = kWarps / WR;        // warps over rows, over keys
-  static constexpr int MT = R / (16 * WR);                            // 16-row tiles of a warp
-  static constexpr int KW = kKeys / WK, NT = KW / 8;                  // keys of a warp in a tile
-  static constexpr int ROWB = FP8 ? D : 2 * D, SPAN = ROWB < 128 ? ROWB : 128, SPANS = ROWB / SPAN;
+  // warps over rows (16 rows of 128 dimensions, 32 of 64, are 64 registers of outputs), and over keys
+  static constexpr int WR = R * D <= 2048 ? 1 : R * D / 2048, WK = kWarps / WR;
+  static constexpr int NT = R / (8 * WR);                             // 8-row tiles of a warp
+  static constexpr int KW = kKeys / WK, KT = KW / 16;                 // keys of a warp in a tile, in sixteens
+  static constexpr bool LEND = R >= 16;                               // registers move between warpgroups
+  static constexpr int THREADS = LEND ? 2 * kWarps * 32 : (kWarps + 1) * 32;
+  static constexpr int CTAS = R == 8 ? 3 : 2;                         // per SM
+  static constexpr bool QREGS = R <= 16;                              // queries stay in registers
+  static constexpr int ROWB = FP8 ? D : 2 * D, SPAN = ROWB < 128 ? ROWB : 128;
   static constexpr int TILE = kKeys * ROWB, STAGE = 2 * TILE;
   static constexpr int QBYTES = R * D * 2;
-  static constexpr int FIT = (112 * 1024 - 4096 - QBYTES) / STAGE;
+  static constexpr int FIT = ((CTAS == 3 ? 74 : 112) * 1024 - 4096 - QBYTES) / STAGE;
   static constexpr int STAGES = FIT < kMaxStages ? FIT : kMaxStages;
   static constexpr int JOIN = D * WK * R * 4 <= STAGE ? D : STAGE / (WK * R * 4);   // output columns joined at a time
 };
@@ -69,7 +80,7 @@ struct SmallSmem {
   unsigned long long full[kMaxStages], empty[kMaxStages], join;
   TileDesc desc[kMaxStages];
   float2 stats[kWarps][64];             // (m, l) of the warps' rows
-  int64_t scan[kThreads / 32];
+  int64_t scan[2 * kWarps];
   int64_t total, start_base;
   int start_seq;
   int abort;
@@ -115,9 +126,35 @@ __device__ __forceinline__ void mma16(float (&d)[4], const uint32_t (&a)[4], uin
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// Four E4M3 bytes as two pairs of fp16, in order.
-__device__ __forceinline__ void widen4(uint32_t four, uint32_t& lo, uint32_t& hi) {
-  asm("{\n.reg .b16 a, b;\nmov.b32 {a, b}, %2;\ncvt.rn.f16x2.e4m3x2 %0, a;\ncvt.rn.f16x2.e4m3x2 %1, b;\n}" : "=r"(lo), "=r"(hi) : "r"(four));
+// 8-bit keys by the E4M3 (LOW: E5M2) term of 8-bit queries.
+template <bool LOW>
+__device__ __forceinline__ void mma32(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  if constexpr (LOW)
+    asm volatile("mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e5m2.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+  else
+    asm volatile("mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+// Four E4M3 bytes as two pairs of fp16, bytes 0 and 2, bytes 1 and 3, each times kWiden.  A byte s eeee mmm moved to the bits
+// s 0eeee mmm0000000 of a half is its value times 2^-8, subnormals included.  The product with 9 * 2^12 (exact: 4 + 4 significant
+// bits) leaves 448 at 64512, inside fp16, and takes the NaN patterns, which look like 480, to infinity.
+constexpr float kWiden = 144.f, kLog2Widen = 7.169925001442312f;
+__device__ __forceinline__ void widen4(uint32_t four, uint32_t& even, uint32_t& odd) {
+  const __half2 up = __half2half2(__ushort_as_half(0x7880));
+  const uint32_t e = (four & 0x00ff00ffu) * 128u + (four & 0x00800080u) * 128u;
+  const uint32_t o = ((four >> 1) & 0x3f803f80u) | (four & 0x80008000u);
+  const __half2 he = __hmul2(*reinterpret_cast<const __half2*>(&e), up), ho = __hmul2(*reinterpret_cast<const __half2*>(&o), up);
+  even = *reinterpret_cast<const uint32_t*>(&he);
+  odd = *reinterpret_cast<const uint32_t*>(&ho);
+}
+// What is not finite in an 8-bit pool can only have been NaN.
+template <bool FP8>
+__device__ __forceinline__ float nan_if_infinite(float x) {
+  return FP8 && !(fabsf(x) <= 3.402823466e38f) ? __int_as_float(0x7fffffff) : x;
 }
 
 // Byte offset of the 16-byte chunk `chunk` of row `row` in a tile, as the copies' swizzle lays it: spans of 128 (or 64) bytes
@@ -131,6 +168,19 @@ __device__ __forceinline__ uint32_t tile_chunk(int row, int chunk) {
 template <class T>
 __device__ __forceinline__ uint32_t q_chunk(int row, int chunk) {
   return (uint32_t)(row * (2 * T::D) + ((chunk & ~7) | ((chunk ^ row) & 7)) * 16);
+}
+
+// One term of 8-bit queries, rows of D bytes: eight rows' chunks of one column on banks of their own.
+template <class T>
+__device__ __forceinline__ uint32_t q8_chunk(int row, int chunk) {
+  if constexpr (T::D == 64) return (uint32_t)(row * 64 + ((chunk ^ (row >> 1)) & 3) * 16);
+  return (uint32_t)(row * 128 + ((chunk ^ row) & 7) * 16);
+}
+
+// Log-sum-exp (natural) of a row from its reference and sum.
+template <bool FP8>
+__device__ __forceinline__ float row_lse(float m, float l) {
+  return l == 0.f ? -INFINITY : (m - (FP8 ? kShift + kLog2Widen : 0.f) + log2f(l)) * kLn2;
 }
 
 // ---------------------------------------------------------------------------------------------- the list of tiles
@@ -149,7 +199,7 @@ __device__ __forceinline__ int64_t cost_of(const AttendArgs& a, int b) {
 template <class T>
 __device__ __forceinline__ void find_start(const StepArgs& args, SmallSmem& sm) {
   const AttendArgs& a = args.a;
-  const int run = (a.step.n_seqs + kThreads - 1) / kThreads, lo = min((int)threadIdx.x * run, a.step.n_seqs), hi = min(lo + run, a.step.n_seqs);
+  const int run = (a.step.n_seqs + T::THREADS - 1) / T::THREADS, lo = min((int)threadIdx.x * run, a.step.n_seqs), hi = min(lo + run, a.step.n_seqs);
   int64_t mine = 0;
   for (int b = lo; b < hi; ++b) mine += cost_of<T>(a, b);
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -163,7 +213,7 @@ __device__ __forceinline__ void find_start(const StepArgs& args, SmallSmem& sm) 
   __syncthreads();
   int64_t total = 0;
 #pragma unroll
-  for (int w = 0; w < kThreads / 32; ++w) {
+  for (int w = 0; w < T::THREADS / 32; ++w) {
     if (w < warp) upto += sm.scan[w];
     total += sm.scan[w];
   }
@@ -229,7 +279,7 @@ __device__ __forceinline__ void copy_tiles(const StepArgs& args, SmallSmem& sm, 
           const float v = group_scale(a.kv.v_scale, row, pool_rows);
           d.k_scale = a.c * group_scale(a.kv.k_scale, row, pool_rows);
           d.v_log2 = log2f(v);
-          d.v_inverse = 1.f / v;
+          d.v_inverse = kWiden / v;                       // l comes out times kWiden, as the values do
         }
       }
     }
@@ -273,72 +323,100 @@ struct Join {
   }
 };
 
-// The triple's query rows into shared memory, rows that do not exist as zeros.  8 bits: fp16, scaled per row, and in the order
-// in which 16 bytes of a key meet a product's operand: element 4 c + 2 s + e of 16 at place 2 c + 8 s + e.
+// The triple's query rows into shared memory, rows that do not exist as zeros.  8 bits: the two terms, one tile behind the other, and
+// the rows' factors 2^-e.
 template <class T>
 __device__ __forceinline__ void load_queries(const AttendArgs& a, const TileDesc& d, unsigned char* q_tile, float* q_factor) {
-  constexpr int kChunks = T::D / 8, kLanes = T::FP8 ? T::D / 16 : T::D / 8;     // threads of a row
+  constexpr int kLanes = T::D / 8;                       // threads of a row
   const int total = d.n_new * a.group;
   for (int item = threadIdx.x; item < T::R * kLanes; item += kWarps * 32) {
     const int r = item / kLanes, part = item % kLanes, rr = d.row_tile * T::R + r;
     const __nv_bfloat16* src = a.q.data + (int64_t)(d.row0 + rr / a.group) * a.q.stride_row + (int64_t)(d.head * a.group + rr % a.group) * a.q.stride_head;
+    union { uint4 u; __nv_bfloat162 h[4]; } v;
+    v.u = make_uint4(0, 0, 0, 0);
+    if (rr < total) v.u = __ldg(reinterpret_cast<const uint4*>(src) + part);
     if constexpr (!T::FP8) {
-      uint4 v = make_uint4(0, 0, 0, 0);
-      if (rr < total) v = __ldg(reinterpret_cast<const uint4*>(src) + part);
-      *reinterpret_cast<uint4*>(q_tile + q_chunk<T>(r, part)) = v;
+      *reinterpret_cast<uint4*>(q_tile + q_chunk<T>(r, part)) = v.u;
     } else {
-      union { uint4 u[2]; __nv_bfloat162 h[8]; } v;
-      v.u[0] = v.u[1] = make_uint4(0, 0, 0, 0);
-      if (rr < total) {
-        v.u[0] = __ldg(reinterpret_cast<const uint4*>(src) + 2 * part);
-        v.u[1] = __ldg(reinterpret_cast<const uint4*>(src) + 2 * part + 1);
-      }
-      float2 f[8];
+      float f[8];
       float top = 0.f;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        f[i] = __bfloat1622float2(v.h[i]);
-        top = fmaxf(top, fmaxf(fabsf(f[i].x), fabsf(f[i].y)));
+      for (int i = 0; i < 4; ++i) {
+        const float2 p = __bfloat1622float2(v.h[i]);
+        f[2 * i] = p.x, f[2 * i + 1] = p.y;
+        top = fmaxf(top, fmaxf(fabsf(p.x), fabsf(p.y)));
       }
 #pragma unroll
       for (int o = kLanes / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o, kLanes));
-      // 2^e with top * 2^e in [2^14, 2^15), e clipped where the factor or its inverse would leave fp32's normal range
-      const int e = top > 0.f && top < INFINITY ? min(max(14 - ((int)(__float_as_uint(top) >> 23) - 127), -120), 120) : 0;
+      // 2^e takes `top` to (224, 448]; e clipped where the factor or its inverse would leave fp32's normal range
+      const uint32_t bits = __float_as_uint(top);
+      const int e = top > 0.f && top < INFINITY ? min(max(135 - (int)(bits >> 23) - ((bits & 0x7fffffu) > 0x600000u ? 1 : 0), -120), 120) : 0;
       const float up = __uint_as_float((uint32_t)(e + 127) << 23);
-      union { uint4 u[2]; uint32_t w[8]; } o;
+      uint32_t hi[2] = {0, 0}, lo[2] = {0, 0};
 #pragma unroll
-      for (int i = 0; i < 8; ++i) o.w[(i >> 1) + 4 * (i & 1)] = pack_f16(f[i].x * up, f[i].y * up);
-      *reinterpret_cast<uint4*>(q_tile + q_chunk<T>(r, 2 * part)) = o.u[0];
-      *reinterpret_cast<uint4*>(q_tile + q_chunk<T>(r, 2 * part + 1)) = o.u[1];
+      for (int i = 0; i < 8; ++i) {
+        const float x = f[i] * up;
+        const uint32_t t = float_to_e4m3(x);
+        uint32_t rest;
+        asm("{\n.reg .b16 r;\ncvt.rn.satfinite.e5m2x2.f32 r, %1, %2;\ncvt.u32.u16 %0, r;\n}" : "=r"(rest) : "f"(0.f), "f"(x - e4m3_to_float(t)));
+        hi[i >> 2] |= t << (8 * (i & 3));
+        lo[i >> 2] |= (rest & 0xffu) << (8 * (i & 3));
+      }
+      *reinterpret_cast<uint2*>(q_tile + q8_chunk<T>(r, part >> 1) + 8 * (part & 1)) = make_uint2(hi[0], hi[1]);
+      *reinterpret_cast<uint2*>(q_tile + T::R * T::D + q8_chunk<T>(r, part >> 1) + 8 * (part & 1)) = make_uint2(lo[0], lo[1]);
       if (part == 0) q_factor[r] = __uint_as_float((uint32_t)(127 - e) << 23);
     }
   }
-  (void)kChunks;
 }
 
-// Values of 16 keys and 16 dimensions as the second product's operands: b[n][0..1] of two 8-wide column tiles.  The columns of
-// bf16 tiles are 16 * np + 8 * n + ..., of 8-bit ones the even and the odd dimensions.
+// The queries of 8 rows as right operands for 32 (8 bits: 64) dimensions: b[0..1] of two products; 8 bits: first[0..1], second[2..3]
+// of one term.
 template <class T>
-__device__ __forceinline__ void load_values(uint32_t v_tile, int key, int np, int lane, uint32_t (&b)[2][2]) {
-  if constexpr (!T::FP8) {
+__device__ __forceinline__ void query_operand(uint32_t q_addr, int row, int step, int lane, uint32_t (&b)[4]) {
+  if constexpr (T::FP8) ldsm4(q_addr + q8_chunk<T>(row + (lane & 7), 4 * step + (lane >> 3)), b);
+  else ldsm4(q_addr + q_chunk<T>(row + (lane & 7), 4 * step + (lane >> 3)), b);
+}
+
+// The 16 keys from `key` on as the left operand: bf16 16 dimensions (of chunk pair `step`), 8 bits 32.  Rows 0-7 and 8-15 of the
+// operand are keys 0-7 and 8-15; 8 bits: the even and the odd keys, as the values' bytes come.
+template <class T>
+__device__ __forceinline__ void key_operand(uint32_t k_tile, int key, int step, int lane, uint32_t (&a)[4]) {
+  const int in8 = lane & 7, second = (lane >> 3) & 1;
+  ldsm4(k_tile + tile_chunk<T>(key + (T::FP8 ? 2 * in8 + second : 8 * second + in8), 2 * step + (lane >> 4)), a);
+}
+// The key (from the warp's sixteen) of a thread's logits 0, 1 (half = 0) and 2, 3 (half = 1).
+template <class T>
+__device__ __forceinline__ int key_of(int lane, int half) { return T::FP8 ? 2 * (lane >> 2) + half : (lane >> 2) + 8 * half; }
+
+// 16 dimensions of the values of 16 keys as the left operand: a[0], a[2] dimensions 0-7, a[1], a[3] 8-15.  The halves of a register
+// are two keys (value_key).  8 bits: two such, for the 16 dimensions behind as well.
+template <class T>
+__device__ __forceinline__ void value_operand(uint32_t v_tile, int key, int mt, int lane, uint32_t (&a)[T::FP8 ? 2 : 1][4]) {
+  if constexpr (T::FP8) {
     uint32_t r[4];
-    ldsm4_t(v_tile + tile_chunk<T>(key + ((lane >> 3) & 1) * 8 + (lane & 7), 2 * np + (lane >> 4)), r);
-    b[0][0] = r[0], b[0][1] = r[1], b[1][0] = r[2], b[1][1] = r[3];
+    // two 16 x 16 byte matrices, transposed: r[0] the four keys 4 c ... of dimension lane / 4, r[1] of the one 8 behind it
+    asm volatile("ldmatrix.sync.aligned.m16n16.x2.trans.shared.b8 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+                 : "r"(v_tile + tile_chunk<T>(key + (lane & 15), mt + (lane >> 4))));
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      widen4(r[2 * i], a[i][0], a[i][2]);
+      widen4(r[2 * i + 1], a[i][1], a[i][3]);
+    }
+  } else {
+    ldsm4_t(v_tile + tile_chunk<T>(key + (lane >> 4) * 8 + (lane & 7), 2 * mt + ((lane >> 3) & 1)), a[0]);
   }
 }
+// The two keys in register e of a value operand.
 template <class T>
-__device__ __forceinline__ void load_values8(uint32_t v_tile, int key, int np2, int lane, uint32_t (&b)[4][2]) {
-  uint32_t r[4];                                         // 16 keys x 32 dimensions
-  ldsm4_t(v_tile + tile_chunk<T>(key + ((lane >> 3) & 1) * 8 + (lane & 7), 2 * np2 + (lane >> 4)), r);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) widen4(__byte_perm(r[i], 0, 0x3120), b[(i >> 1) * 2][i & 1], b[(i >> 1) * 2 + 1][i & 1]);
+__device__ __forceinline__ int value_key(int lane, int e, int half) {
+  return T::FP8 ? 4 * (lane & 3) + (e >> 1) + 2 * half : 2 * (lane & 3) + half + 8 * (e >> 1);
 }
 
-// Zeroes what belongs to keys outside [lo, hi): the halves of an operand register are keys `key` and `key` + 1.
-__device__ __forceinline__ uint32_t keep_keys(uint32_t pair, int key, int lo, int hi) {
+// Zeroes the halves of an operand register whose keys lie outside [lo, hi).
+__device__ __forceinline__ uint32_t keep_keys(uint32_t pair, int key_low, int key_high, int lo, int hi) {
   uint32_t mask = 0;
-  if (key >= lo && key < hi) mask |= 0x0000ffffu;
-  if (key + 1 >= lo && key + 1 < hi) mask |= 0xffff0000u;
+  if (key_low >= lo && key_low < hi) mask |= 0x0000ffffu;
+  if (key_high >= lo && key_high < hi) mask |= 0xffff0000u;
   return pair & mask;
 }
 template <bool FP8>
@@ -347,62 +425,67 @@ __device__ __forceinline__ bool not_finite(uint32_t pair) {
   return (pair & kExp) == kExp || ((pair >> 16) & kExp) == kExp;
 }
 
+__device__ __forceinline__ uint32_t transpose8(uint32_t x) {
+  uint32_t y;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+
+// What a warp has of a triple: outputs (dimensions lane / 4 and 8 behind it of every 16, query rows 2 (lane % 4) and the next of
+// every 8), references and sums of its rows.
 template <class T>
 struct State {
-  float o[T::MT][T::D / 8][4];
-  float m[T::MT][2], l[T::MT][2];
+  float o[T::D / 16][T::NT][4];
+  float m[T::NT][2], l[T::NT][2];
 };
 
-// out += weights . values of the warp's keys.  `guard`: the tile has keys that not every row may see, or keys outside the
-// sequence's range [first, end).
+// out += values . weights of 16 keys, p[nt] being the weights of 8 rows.  `guard`: the tile has keys that not every row may see,
+// or keys outside the sequence's range [first, end).
 template <class T>
-__device__ __forceinline__ void add_values(State<T>& st, const uint32_t (&p)[T::MT][T::NT / 2][4], uint32_t v_tile, int key_in_tile, int key0,
-                                           const TileDesc& d, int group, int causal, int row_in_triple, bool guard, int lane) {
-  constexpr int kStep = T::FP8 ? 4 : 2;                  // 8-wide column tiles of one load
+__device__ __forceinline__ void add_values(State<T>& st, const uint32_t (&p)[T::NT][2], uint32_t v_tile, int key_in_tile, int key0, const TileDesc& d,
+                                           int group, int causal, int row_in_triple, bool guard, int lane) {
+  constexpr int kStep = T::FP8 ? 2 : 1;
 #pragma unroll
-  for (int ks = 0; ks < T::NT / 2; ++ks) {
+  for (int m0 = 0; m0 < T::D / 16; m0 += kStep) {
+    uint32_t v[kStep][4];
+    value_operand<T>(v_tile, key_in_tile, m0, lane, v);
+    bool odd = false;
+    if (guard) {
 #pragma unroll
-    for (int np = 0; np < T::D / 8 / kStep; ++np) {
-      uint32_t b[kStep][2];
-      if constexpr (T::FP8) load_values8<T>(v_tile, key_in_tile + ks * 16, np, lane, b);
-      else load_values<T>(v_tile, key_in_tile + ks * 16, np, lane, b);
-      bool odd = false;
-      if (guard) {
-        const int key = key0 + key_in_tile + ks * 16 + (lane & 3) * 2;
+      for (int i = 0; i < kStep; ++i)
 #pragma unroll
-        for (int n = 0; n < kStep; ++n)
+        for (int e = 0; e < 4; ++e) {
+          const int base = key0 + key_in_tile;
+          v[i][e] = keep_keys(v[i][e], base + value_key<T>(lane, e, 0), base + value_key<T>(lane, e, 1), d.first, d.end);
+          odd |= not_finite<T::FP8>(v[i][e]);
+        }
+      odd = __any_sync(0xffffffffu, odd);
+    }
+    if (!odd) {
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            b[n][h] = keep_keys(b[n][h], key + 8 * h, d.first, d.end);
-            odd |= not_finite<T::FP8>(b[n][h]);
+      for (int i = 0; i < kStep; ++i)
+#pragma unroll
+        for (int nt = 0; nt < T::NT; ++nt) mma16<T::FP8>(st.o[m0 + i][nt], v[i], p[nt][0], p[nt][1]);
+    } else {
+      // values that are not finite, some of which only some rows may see: row by row, each with the values that it sees
+#pragma unroll 1
+      for (int r = 0; r < 8; ++r)
+#pragma unroll
+        for (int nt = 0; nt < T::NT; ++nt) {
+          const int hi = causal ? min(d.end, d.pos0 + (row_in_triple + nt * 8 + r) / group + 1) : d.end, base = key0 + key_in_tile;
+          const bool mine = (lane >> 2) == r;
+#pragma unroll
+          for (int i = 0; i < kStep; ++i) {
+            float part[4] = {0.f, 0.f, 0.f, 0.f};
+            uint32_t vr[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) vr[e] = keep_keys(v[i][e], base + value_key<T>(lane, e, 0), base + value_key<T>(lane, e, 1), d.first, hi);
+            mma16<T::FP8>(part, vr, mine ? p[nt][0] : 0u, mine ? p[nt][1] : 0u);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (2 * (lane & 3) + (e & 1) == r) st.o[m0 + i][nt][e] += part[e];
           }
-        odd = __any_sync(0xffffffffu, odd);
-      }
-      if (!odd) {
-#pragma unroll
-        for (int mt = 0; mt < T::MT; ++mt)
-#pragma unroll
-          for (int n = 0; n < kStep; ++n) mma16<T::FP8>(st.o[mt][np * kStep + n], p[mt][ks], b[n][0], b[n][1]);
-      } else {
-        // values that are not finite, some of which only some rows may see: row by row, each with the values that it sees
-        const int key = key0 + key_in_tile + ks * 16 + (lane & 3) * 2;
-        for (int r = 0; r < 16; ++r)
-#pragma unroll
-          for (int mt = 0; mt < T::MT; ++mt) {
-            const int hi = causal ? min(d.end, d.pos0 + (row_in_triple + mt * 16 + r) / group + 1) : d.end;
-            uint32_t pr[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) pr[e] = (lane >> 2) + 8 * (e & 1) == r ? p[mt][ks][e] : 0u;
-#pragma unroll
-            for (int n = 0; n < kStep; ++n) {
-              float part[4] = {0.f, 0.f, 0.f, 0.f};
-              mma16<T::FP8>(part, pr, keep_keys(b[n][0], key, d.first, hi), keep_keys(b[n][1], key + 8, d.first, hi));
-#pragma unroll
-              for (int e = 0; e < 4; ++e)
-                if ((lane >> 2) + 8 * (e >> 1) == r) st.o[mt][np * kStep + n][e] += part[e];
-            }
-          }
-      }
+        }
     }
   }
 }
@@ -410,16 +493,17 @@ __device__ __forceinline__ void add_values(State<T>& st, const uint32_t (&p)[T::
 template <class T>
 __device__ __forceinline__ void compute_tiles(const StepArgs& args, SmallSmem& sm, unsigned char* ring_ptr, uint32_t ring, unsigned char* q_tile,
                                               int64_t n_tiles, const Abort& ab) {
-  constexpr int D = T::D, R = T::R, MT = T::MT, NT = T::NT;
+  constexpr int D = T::D, R = T::R, NT = T::NT, KT = T::KT;
+  constexpr int kTerms = T::FP8 ? 2 : 1, kSteps = T::FP8 ? D / 64 : D / 32;   // four registers of queries each
   const AttendArgs& a = args.a;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int row_warp = warp % T::WR, key_warp = warp / T::WR, row_off = row_warp * MT * 16, key_off = key_warp * T::KW;
+  const int row_off = warp % T::WR * NT * 8, key_warp = warp / T::WR, key_off = key_warp * T::KW;
   const uint32_t q_addr = smem_u32(q_tile);
   __shared__ float q_factor[R];
   Join join{smem_u32(&sm.join), 0};
   State<T> st;
-  float qf[MT][2];
-  uint32_t q[MT == 1 ? D / 16 : 1][4];
+  float qf[NT][2];
+  uint32_t q[T::QREGS ? kTerms * kSteps * NT : 1][4];
   int stage = 0;
   uint32_t parity = 0;
   for (int64_t tile = 0; tile < n_tiles; ++tile) {
@@ -430,195 +514,174 @@ __device__ __forceinline__ void compute_tiles(const StepArgs& args, SmallSmem& s
       load_queries<T>(a, d, q_tile, q_factor);
       if (!join.wait(ab)) return;
 #pragma unroll
-      for (int mt = 0; mt < MT; ++mt) {
+      for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
-          st.m[mt][b] = -INFINITY;
-          st.l[mt][b] = 0.f;
-          if constexpr (T::FP8) qf[mt][b] = q_factor[row_off + mt * 16 + (lane >> 2) + 8 * b];
+        for (int e = 0; e < 2; ++e) {
+          st.m[nt][e] = -INFINITY;
+          st.l[nt][e] = 0.f;
+          if constexpr (T::FP8) qf[nt][e] = q_factor[row_off + nt * 8 + 2 * (lane & 3) + e];
         }
 #pragma unroll
-        for (int n = 0; n < D / 8; ++n)
+        for (int m = 0; m < D / 16; ++m)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) st.o[mt][n][e] = 0.f;
+          for (int e = 0; e < 4; ++e) st.o[m][nt][e] = 0.f;
       }
-      if constexpr (MT == 1)
+      if constexpr (T::QREGS) {
 #pragma unroll
-        for (int kk = 0; kk < D / 16; ++kk)
-          ldsm4(q_addr + q_chunk<T>(row_off + (lane & 7) + ((lane >> 3) & 1) * 8, 2 * kk + (lane >> 4)), q[kk]);
+        for (int t = 0; t < kTerms; ++t)
+#pragma unroll
+          for (int x = 0; x < kSteps; ++x)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) query_operand<T>(q_addr + t * R * D, row_off + nt * 8, x, lane, q[(t * kSteps + x) * NT + nt]);
+      }
     }
     if (!(flags & kNoKeys)) {
       const uint32_t k_tile = ring + stage * T::STAGE, v_tile = k_tile + T::TILE;
-      // logits of the warp's rows and keys
-      float z[MT][NT][4];
+      const int key0 = d.key0, row_first = d.row_tile * R;
+      const bool guard = key0 < d.first || key0 + kKeys > d.end || (a.causal && key0 + kKeys - 1 > d.pos0 + row_first / a.group);
+      // logits of the warp's keys and rows
+      float z[KT][NT][4];
 #pragma unroll
-      for (int mt = 0; mt < MT; ++mt)
+      for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) z[mt][n][e] = 0.f;
+          for (int e = 0; e < 4; ++e) z[kt][nt][e] = 0.f;
 #pragma unroll
-      for (int kk = 0; kk < D / 16; ++kk) {
-        uint32_t qa[MT][4];
+      for (int x = 0; x < kSteps; ++x) {
+        uint32_t k[KT][2][4];
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-          if constexpr (MT == 1) {
+        for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) qa[mt][e] = q[kk][e];
-          } else {
-            ldsm4(q_addr + q_chunk<T>(row_off + mt * 16 + (lane & 7) + ((lane >> 3) & 1) * 8, 2 * kk + (lane >> 4)), qa[mt]);
-          }
-        }
-        if constexpr (T::FP8) {
-          if (kk % 2 == 0) {
+          for (int h = 0; h < 2; ++h) key_operand<T>(k_tile, key_off + kt * 16, 2 * x + h, lane, k[kt][h]);
 #pragma unroll
-            for (int np = 0; np < NT / 2; ++np) {
-              uint32_t r[4];                             // 16 keys x 32 dimensions: chunks kk, kk + 1
-              ldsm4(k_tile + tile_chunk<T>(key_off + np * 16 + (lane >> 4) * 8 + (lane & 7), kk + ((lane >> 3) & 1)), r);
-              uint32_t qb[MT][4];
+        for (int t = 0; t < kTerms; ++t)
 #pragma unroll
-              for (int mt = 0; mt < MT; ++mt) {
-                if constexpr (MT == 1) {
+          for (int nt = 0; nt < NT; ++nt) {
+            uint32_t b[4];
+            if constexpr (T::QREGS) {
 #pragma unroll
-                  for (int e = 0; e < 4; ++e) qb[mt][e] = q[kk + 1][e];
-                } else {
-                  ldsm4(q_addr + q_chunk<T>(row_off + mt * 16 + (lane & 7) + ((lane >> 3) & 1) * 8, 2 * (kk + 1) + (lane >> 4)), qb[mt]);
-                }
-              }
+              for (int e = 0; e < 4; ++e) b[e] = q[(t * kSteps + x) * NT + nt][e];
+            } else {
+              query_operand<T>(q_addr + t * R * D, row_off + nt * 8, x, lane, b);
+            }
+#pragma unroll
+            for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
               for (int h = 0; h < 2; ++h) {
-                uint32_t b0, b1, c0, c1;
-                widen4(r[2 * h], b0, b1);
-                widen4(r[2 * h + 1], c0, c1);
-#pragma unroll
-                for (int mt = 0; mt < MT; ++mt) {
-                  mma16<true>(z[mt][2 * np + h], qa[mt], b0, b1);
-                  mma16<true>(z[mt][2 * np + h], qb[mt], c0, c1);
-                }
+                if constexpr (!T::FP8) mma16<false>(z[kt][nt], k[kt][h], b[2 * h], b[2 * h + 1]);
+                else if (t == 0) mma32<false>(z[kt][nt], k[kt][h], b[2 * h], b[2 * h + 1]);
+                else mma32<true>(z[kt][nt], k[kt][h], b[2 * h], b[2 * h + 1]);
               }
-            }
           }
-        } else {
-#pragma unroll
-          for (int np = 0; np < NT / 2; ++np) {
-            uint32_t r[4];
-            ldsm4(k_tile + tile_chunk<T>(key_off + np * 16 + (lane >> 4) * 8 + (lane & 7), 2 * kk + ((lane >> 3) & 1)), r);
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
-              mma16<false>(z[mt][2 * np], qa[mt], r[0], r[1]);
-              mma16<false>(z[mt][2 * np + 1], qa[mt], r[2], r[3]);
-            }
-          }
-        }
       }
       // base-2 logits, masked
-      const int key0 = d.key0;
-      const int row_first = d.row_tile * R;
-      const bool guard = key0 < d.first || key0 + kKeys > d.end || (a.causal && key0 + kKeys - 1 > d.pos0 + row_first / a.group);
       bool over = false;
 #pragma unroll
-      for (int mt = 0; mt < MT; ++mt)
+      for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
-          const float f = T::FP8 ? d.k_scale * qf[mt][b] : a.c;
+        for (int e = 0; e < 2; ++e) {
+          const float f = T::FP8 ? d.k_scale * qf[nt][e] : a.c;
           const float add = T::FP8 ? d.v_log2 : 0.f;
           int hi = d.end;
-          if (guard && a.causal) hi = min(hi, d.pos0 + (row_first + row_off + mt * 16 + (lane >> 2) + 8 * b) / a.group + 1);
+          if (guard && a.causal) hi = min(hi, d.pos0 + (row_first + row_off + nt * 8 + 2 * (lane & 3) + e) / a.group + 1);
+          const float limit = st.m[nt][e] + kLazy;
 #pragma unroll
-          for (int n = 0; n < NT; ++n)
+          for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              float x = T::FP8 ? fmaf(z[mt][n][2 * b + e], f, add) : z[mt][n][2 * b + e] * f;
+            for (int h = 0; h < 2; ++h) {
+              float x = T::FP8 ? fmaf(z[kt][nt][2 * h + e], f, add) : z[kt][nt][2 * h + e] * f;
               if (guard) {
-                const int key = key0 + key_off + n * 8 + (lane & 3) * 2 + e;
+                const int key = key0 + key_off + kt * 16 + key_of<T>(lane, h);
                 if (key < d.first || key >= hi) x = -INFINITY;
               }
-              z[mt][n][2 * b + e] = x;
-              over |= x > st.m[mt][b] + kLazy;
+              z[kt][nt][2 * h + e] = x;
+              over |= x > limit;
             }
         }
       if (__any_sync(0xffffffffu, over)) {
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
+        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int b = 0; b < 2; ++b) {
-            float top = st.m[mt][b];
+          for (int e = 0; e < 2; ++e) {
+            float top = st.m[nt][e];
 #pragma unroll
-            for (int n = 0; n < NT; ++n) top = fmaxf(top, fmaxf(z[mt][n][2 * b], z[mt][n][2 * b + 1]));
-            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-            const float f = top == st.m[mt][b] ? 1.f : fast_exp2(st.m[mt][b] - top);
-            st.m[mt][b] = top;
-            st.l[mt][b] *= f;
+            for (int kt = 0; kt < KT; ++kt) top = fmaxf(top, fmaxf(z[kt][nt][e], z[kt][nt][2 + e]));
 #pragma unroll
-            for (int n = 0; n < D / 8; ++n) st.o[mt][n][2 * b] *= f, st.o[mt][n][2 * b + 1] *= f;
+            for (int o = 4; o < 32; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+            const float f = top == st.m[nt][e] ? 1.f : fast_exp2(st.m[nt][e] - top);
+            st.m[nt][e] = top;
+            st.l[nt][e] *= f;
+#pragma unroll
+            for (int m = 0; m < D / 16; ++m) st.o[m][nt][e] *= f, st.o[m][nt][2 + e] *= f;
           }
       }
-      uint32_t p[MT][NT / 2][4];
+      uint32_t p[KT][NT][2];
 #pragma unroll
-      for (int mt = 0; mt < MT; ++mt)
+      for (int nt = 0; nt < NT; ++nt) {
+        float ref[2], sum[2] = {0.f, 0.f};
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
-          const float ref = (st.m[mt][b] == -INFINITY ? 0.f : st.m[mt][b]) - (T::FP8 ? kShift : 0.f);
-          float sum = 0.f;
+        for (int e = 0; e < 2; ++e) ref[e] = (st.m[nt][e] == -INFINITY ? 0.f : st.m[nt][e]) - (T::FP8 ? kShift : 0.f);
 #pragma unroll
-          for (int n = 0; n < NT; ++n) {
-            const float x = fast_exp2(z[mt][n][2 * b] - ref), y = fast_exp2(z[mt][n][2 * b + 1] - ref);
-            sum += x + y;
-            p[mt][n >> 1][b + 2 * (n & 1)] = T::FP8 ? pack_f16(x, y) : pack_bf16(x, y);
+        for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const float x = fast_exp2(z[kt][nt][2 * h] - ref[0]), y = fast_exp2(z[kt][nt][2 * h + 1] - ref[1]);
+            sum[0] += x;
+            sum[1] += y;
+            p[kt][nt][h] = transpose8(T::FP8 ? pack_f16(x, y) : pack_bf16(x, y));
           }
-          if constexpr (T::FP8) st.l[mt][b] = fmaf(sum, d.v_inverse, st.l[mt][b]);
-          else st.l[mt][b] += sum;
-        }
-      add_values<T>(st, p, v_tile, key_off, key0, d, a.group, a.causal, row_first + row_off, guard, lane);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) st.l[nt][e] = T::FP8 ? fmaf(sum[e], d.v_inverse, st.l[nt][e]) : st.l[nt][e] + sum[e];
+      }
+#pragma unroll
+      for (int kt = 0; kt < KT; ++kt)
+        add_values<T>(st, p[kt], v_tile, key_off + kt * 16, key0, d, a.group, a.causal, row_first + row_off, guard, lane);
     }
     if (flags & kLast) {
       // the warps' sums of a row, each against its own reference
 #pragma unroll
-      for (int mt = 0; mt < MT; ++mt)
+      for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
-          float l = st.l[mt][b];
-          l += __shfl_xor_sync(0xffffffffu, l, 1);
-          l += __shfl_xor_sync(0xffffffffu, l, 2);
-          if ((lane & 3) == 0) sm.stats[key_warp][row_off + mt * 16 + (lane >> 2) + 8 * b] = make_float2(st.m[mt][b], l);
+        for (int e = 0; e < 2; ++e) {
+          float l = st.l[nt][e];
+#pragma unroll
+          for (int o = 4; o < 32; o <<= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+          if (lane < 4) sm.stats[key_warp][row_off + nt * 8 + 2 * lane + e] = make_float2(st.m[nt][e], l);
         }
       if (!join.wait(ab)) return;                        // statistics are there, and the stage's tile is read
-      float f[MT][2];
+      float f[NT][2];
 #pragma unroll
-      for (int mt = 0; mt < MT; ++mt)
+      for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
-          const int r = row_off + mt * 16 + (lane >> 2) + 8 * b;
+        for (int e = 0; e < 2; ++e) {
+          const int r = row_off + nt * 8 + 2 * (lane & 3) + e;
           float top = -INFINITY;
 #pragma unroll
           for (int w = 0; w < T::WK; ++w) top = fmaxf(top, sm.stats[w][r].x);
-          f[mt][b] = st.m[mt][b] == -INFINITY ? 0.f : fast_exp2(st.m[mt][b] - top);
+          f[nt][e] = st.m[nt][e] == -INFINITY ? 0.f : fast_exp2(st.m[nt][e] - top);
         }
       const bool whole = (flags & kFromStart) && (flags & kToEnd);
       const int slot = 2 * blockIdx.x + ((flags & kFromStart) ? 1 : 0);
       const int live = min(R, d.n_new * a.group - d.row_tile * R);
       float* buf = reinterpret_cast<float*>(ring_ptr + stage * T::STAGE);
-      constexpr int kSwizzle = (T::JOIN / 8 < 4 ? T::JOIN / 8 : 4) - 1;
+      constexpr int kSwizzle = (T::JOIN / 8 < 4 ? T::JOIN / 8 : 4) - 1;      // rows 2 c share a bank otherwise
+#pragma unroll 1
       for (int c0 = 0; c0 < D; c0 += T::JOIN) {
 #pragma unroll
-        for (int n = 0; n < D / 8; ++n) {
-          // columns of the thread's pair in the tile: bf16 8 n + 2 c, + 1; 8 bits 16 (n / 2) + 4 c + (n % 2), + 2
-          const int first = T::FP8 ? (n >> 1) * 16 + (lane & 3) * 4 + (n & 1) : n * 8 + (lane & 3) * 2;
-          if (first < c0 || first >= c0 + T::JOIN) continue;
+        for (int m = 0; m < D / 16; ++m) {
+          if (16 * m < c0 || 16 * m >= c0 + T::JOIN) continue;
 #pragma unroll
-          for (int mt = 0; mt < MT; ++mt)
+          for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int b = 0; b < 2; ++b) {
-              const int r = row_off + mt * 16 + (lane >> 2) + 8 * b, col = (first - c0) ^ ((r & kSwizzle) << 3);
-              float* at = buf + (key_warp * R + r) * T::JOIN + col;
-              at[0] = st.o[mt][n][2 * b] * f[mt][b];
-              at[T::FP8 ? 2 : 1] = st.o[mt][n][2 * b + 1] * f[mt][b];
+            for (int e = 0; e < 4; ++e) {
+              const int r = row_off + nt * 8 + 2 * (lane & 3) + (e & 1), col = 16 * m - c0 + (lane >> 2) + 8 * (e >> 1);
+              buf[(key_warp * R + r) * T::JOIN + (col ^ (((r >> 1) & kSwizzle) << 3))] = st.o[m][nt][e] * f[nt][e & 1];
             }
         }
         if (!join.wait(ab)) return;
         for (int item = threadIdx.x; item < live * (T::JOIN / 8); item += kWarps * 32) {
-          const int r = item / (T::JOIN / 8), col = item % (T::JOIN / 8) * 8, at = col ^ ((r & kSwizzle) << 3);
+          const int r = item / (T::JOIN / 8), col = item % (T::JOIN / 8) * 8, at = col ^ (((r >> 1) & kSwizzle) << 3);
           float x[8];
 #pragma unroll
           for (int i = 0; i < 8; ++i) x[i] = 0.f;
@@ -639,12 +702,13 @@ __device__ __forceinline__ void compute_tiles(const StepArgs& args, SmallSmem& s
             const int64_t row = d.row0 + rr / a.group;
             const int head = d.head * a.group + rr % a.group;
             const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = nan_if_infinite<T::FP8>(x[i]) * inv;
             uint4 v;
-            v.x = pack_bf16(x[0] * inv, x[1] * inv), v.y = pack_bf16(x[2] * inv, x[3] * inv);
-            v.z = pack_bf16(x[4] * inv, x[5] * inv), v.w = pack_bf16(x[6] * inv, x[7] * inv);
+            v.x = pack_bf16(x[0], x[1]), v.y = pack_bf16(x[2], x[3]);
+            v.z = pack_bf16(x[4], x[5]), v.w = pack_bf16(x[6], x[7]);
             *reinterpret_cast<uint4*>(a.out.data + row * a.out.stride_row + head * a.out.stride_head + c0 + col) = v;
-            if (a.lse != nullptr && c0 + col == 0)
-              a.lse[row * a.lse_stride_row + head * a.lse_stride_head] = l == 0.f ? -INFINITY : (top - (T::FP8 ? kShift : 0.f) + log2f(l)) * kLn2;
+            if (a.lse != nullptr && c0 + col == 0) a.lse[row * a.lse_stride_row + head * a.lse_stride_head] = row_lse<T::FP8>(top, l);
           } else {
             float4* dst = reinterpret_cast<float4*>(args.partial + ((int64_t)slot * R + r) * D + c0 + col);
             dst[0] = make_float4(x[0], x[1], x[2], x[3]);
@@ -667,7 +731,7 @@ __device__ __forceinline__ void compute_tiles(const StepArgs& args, SmallSmem& s
 }
 
 template <int D, bool FP8, int R>
-__global__ void __launch_bounds__(kThreads, kCtasPerSm) attend_step_kernel(const __grid_constant__ StepArgs args) {
+__global__ void __launch_bounds__(Traits<D, FP8, R>::THREADS, Traits<D, FP8, R>::CTAS) attend_step_kernel(const __grid_constant__ StepArgs args) {
   using T = Traits<D, FP8, R>;
   extern __shared__ unsigned char smem_raw[];
   unsigned char* ring_ptr = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
@@ -689,8 +753,13 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) attend_step_kernel(const
   const int64_t w0 = per * blockIdx.x, w1 = min(w0 + per, total);
   if (w0 < w1) {
     const Abort ab{&sm.abort, args.a.dev_status};
-    if (threadIdx.x < kWarps * 32) compute_tiles<T>(args, sm, ring_ptr, smem_u32(ring_ptr), q_tile, w1 - w0, ab);
-    else copy_tiles<T>(args, sm, smem_u32(ring_ptr), w0, w1, per, ab);
+    if (threadIdx.x < kWarps * 32) {
+      if constexpr (T::LEND) reg_inc<kComputeRegs>();
+      compute_tiles<T>(args, sm, ring_ptr, smem_u32(ring_ptr), q_tile, w1 - w0, ab);
+    } else {
+      if constexpr (T::LEND) reg_dec<kOtherRegs>();
+      if (threadIdx.x < (kWarps + 1) * 32) copy_tiles<T>(args, sm, smem_u32(ring_ptr), w0, w1, per, ab);
+    }
   }
   grid_launch_dependents();
 }
@@ -726,9 +795,9 @@ __global__ void __launch_bounds__(128) attend_join_kernel(const __grid_constant_
   const float inv = l == 0.f ? 0.f : 1.f / l;
   uint32_t* dst = reinterpret_cast<uint32_t*>(a.out.data + row * a.out.stride_row + h * a.out.stride_head) + lane * (V / 2);
 #pragma unroll
-  for (int j = 0; j < V / 2; ++j) dst[j] = pack_bf16(x[2 * j] * inv, x[2 * j + 1] * inv);
+  for (int j = 0; j < V / 2; ++j) dst[j] = pack_bf16(nan_if_infinite<FP8>(x[2 * j]) * inv, nan_if_infinite<FP8>(x[2 * j + 1]) * inv);
   if (a.lse != nullptr && lane == 0)
-    a.lse[row * a.lse_stride_row + h * a.lse_stride_head] = l == 0.f ? -INFINITY : (top - (FP8 ? kShift : 0.f) + log2f(l)) * kLn2;
+    a.lse[row * a.lse_stride_row + h * a.lse_stride_head] = row_lse<FP8>(top, l);
 }
 
 struct StepWorkspace {
@@ -746,8 +815,9 @@ StepWorkspace step_workspace(int rows, int d, int ctas) {
 // Rows of a tile: the fewest that hold the rows of a sequence and key head, up to 64.
 int tile_rows(int group, int max_new) {
   const int64_t rows = (int64_t)group * max_new;
-  return rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
+  return rows <= 8 ? 8 : rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
 }
+int ctas_per_sm(int rows) { return rows <= 8 ? 3 : 2; }
 
 template <int D, bool FP8, int R>
 int32_t launch_step(const StepArgs& args, int ctas, cudaStream_t stream) {
@@ -755,7 +825,7 @@ int32_t launch_step(const StepArgs& args, int ctas, cudaStream_t stream) {
   static ContextSet done;
   const int32_t st = allow_shared_memory(reinterpret_cast<const void*>(attend_step_kernel<D, FP8, R>), smem_bytes<T>(), done);
   if (st != SPF_OK) return st;
-  attend_step_kernel<D, FP8, R><<<ctas, kThreads, smem_bytes<T>(), stream>>>(args);
+  attend_step_kernel<D, FP8, R><<<ctas, T::THREADS, smem_bytes<T>(), stream>>>(args);
   SPF_CUDA_CHECK(cudaGetLastError());
   cudaLaunchConfig_t config{};
   config.gridDim = dim3((unsigned)ctas, R / 4);
@@ -773,6 +843,7 @@ int32_t launch_step(const StepArgs& args, int ctas, cudaStream_t stream) {
 template <int D, bool FP8>
 int32_t launch_rows(const StepArgs& args, int rows, int ctas, cudaStream_t stream) {
   switch (rows) {
+    case 8: return launch_step<D, FP8, 8>(args, ctas, stream);
     case 16: return launch_step<D, FP8, 16>(args, ctas, stream);
     case 32: return launch_step<D, FP8, 32>(args, ctas, stream);
     default: return launch_step<D, FP8, 64>(args, ctas, stream);
@@ -782,13 +853,17 @@ int32_t launch_rows(const StepArgs& args, int rows, int ctas, cudaStream_t strea
 }  // namespace
 
 size_t attend_step_workspace_bytes(const spf_kv_cache* cache, int group, int max_new, int sm_count) {
-  return step_workspace(tile_rows(group, max_new), cache->head_dim, sm_count * kCtasPerSm).total;
+  // a step with fewer rows has more CTAs: the most that any with up to this many takes
+  size_t most = 0;
+  for (int rows = 8; rows <= tile_rows(group, max_new); rows *= 2)
+    most = std::max(most, step_workspace(rows, cache->head_dim, sm_count * ctas_per_sm(rows)).total);
+  return most;
 }
 
 int32_t attend_step_launch(const AttendArgs& a, const spf_kv_cache* cache, int max_new, int sm_count, void* workspace, cudaStream_t stream) {
   StepArgs args{};
   args.a = a;
-  const int rows = tile_rows(a.group, max_new), ctas = sm_count * kCtasPerSm;
+  const int rows = tile_rows(a.group, max_new), ctas = sm_count * ctas_per_sm(rows);
   const StepWorkspace w = step_workspace(rows, cache->head_dim, ctas);
   char* base = static_cast<char*>(workspace);
   args.partial = reinterpret_cast<float*>(base + w.partial);
