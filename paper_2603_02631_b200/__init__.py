@@ -20,5 +20,7 @@ __all__ = list(_BINDING_NAMES) + ["binding"]
 def __getattr__(name):
     if name == "binding" or name in _BINDING_NAMES:
         binding = importlib.import_module(".binding", __name__)
-        return binding if name == "binding" else getattr(binding, name)
+        value = binding if name == "binding" else getattr(binding, name)
+        globals()[name] = value                        # found at once from now on: this function costs more than a microsecond
+        return value
     raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

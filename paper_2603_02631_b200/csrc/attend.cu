@@ -28,6 +28,12 @@ int32_t check_heads(const char* who, const spf_kv_cache* cache, int32_t n_q_head
   return SPF_OK;
 }
 
+// Enough for every step with up to `max_new` new tokens a sequence.
+size_t workspace_for(const spf_kv_cache* cache, int group, int max_new, int sm_count) {
+  const size_t few = attend_step_workspace_bytes(cache, group, max_new, sm_count);
+  return (int64_t)group * max_new > kStepRows ? std::max(few, attend_prompt_workspace_bytes(cache, sm_count)) : few;
+}
+
 }  // namespace
 
 int32_t encode_pool_map(const char* who, const spf_kv_cache* cache, void* pool, int tile_rows, CUtensorMap* map) {
@@ -58,7 +64,7 @@ extern "C" size_t spf_attend_workspace_bytes(const spf_kv_cache* cache, int32_t 
   if (check_cache(who, cache, &kv) != SPF_OK || check_heads(who, cache, n_q_heads, &group) != SPF_OK) return 0;
   if (max_new < 1) return fail(SPF_ERR_INVALID_ARG, "%s: max_new must be positive", who), 0;
   if (device_sm_count(&sm_count) != SPF_OK) return 0;
-  return attend_step_workspace_bytes(cache, group, max_new, sm_count);
+  return workspace_for(cache, group, max_new, sm_count);
 }
 
 extern "C" int32_t spf_attend(const spf_kv_cache* cache, const spf_kv_step* step, const spf_rows* q, const spf_rows* out, int32_t n_q_heads,
@@ -93,9 +99,11 @@ extern "C" int32_t spf_attend(const spf_kv_cache* cache, const spf_kv_step* step
   int sm_count = 0;
   st = device_sm_count(&sm_count);
   if (st != SPF_OK) return st;
-  const size_t need = attend_step_workspace_bytes(cache, a.group, step->max_new, sm_count);
+  const size_t need = workspace_for(cache, a.group, step->max_new, sm_count);
   if (workspace == nullptr || reinterpret_cast<uintptr_t>(workspace) % 256 != 0)
     return fail(SPF_ERR_WORKSPACE, "%s: workspace is null or not 256-byte aligned", who);
   if (workspace_bytes < need) return fail(SPF_ERR_WORKSPACE, "%s: workspace has %zu bytes, %zu needed", who, workspace_bytes, need);
-  return attend_step_launch(a, cache, step->max_new, sm_count, workspace, static_cast<cudaStream_t>(cuda_stream));
+  const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+  if ((int64_t)a.group * step->max_new > kStepRows) return attend_prompt_launch(a, cache, sm_count, workspace, stream);
+  return attend_step_launch(a, cache, step->max_new, sm_count, workspace, stream);
 }

@@ -71,7 +71,95 @@ __device__ __forceinline__ void drain_copy(uint32_t bar, uint32_t parity) {
 // Tensor map of a pool: rows of d elements seen as spans of at most 128 bytes, `tile_rows` rows a copy.
 int32_t encode_pool_map(const char* who, const spf_kv_cache* cache, void* pool, int tile_rows, CUtensorMap* map);
 
+// ---------------------------------------------------------------------------------------------- what both kernels compute with
+constexpr float kLazy = 8.f;            // how far logits may exceed their reference
+constexpr float kShift = 7.f;           // 8-bit values: weights reach 2^(kLazy + kShift) = 2^15, below fp16's 65504
+
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+  const __half2 v = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+// Four E4M3 bytes as two pairs of fp16, bytes 0 and 2, bytes 1 and 3, each times kWiden.  A byte s eeee mmm moved to the bits
+// s 0eeee mmm0000000 of a half is its value times 2^-8, subnormals included.  The product with 9 * 2^12 (exact: 4 + 4 significant
+// bits) leaves 448 at 64512, inside fp16, and takes the NaN patterns, which look like 480, to infinity.
+constexpr float kWiden = 144.f, kLog2Widen = 7.169925001442312f;
+__device__ __forceinline__ void widen4(uint32_t four, uint32_t& even, uint32_t& odd) {
+  const __half2 up = __half2half2(__ushort_as_half(0x7880));
+  const uint32_t e = (four & 0x00ff00ffu) * 128u + (four & 0x00800080u) * 128u;
+  const uint32_t o = ((four >> 1) & 0x3f803f80u) | (four & 0x80008000u);
+  const __half2 he = __hmul2(*reinterpret_cast<const __half2*>(&e), up), ho = __hmul2(*reinterpret_cast<const __half2*>(&o), up);
+  even = *reinterpret_cast<const uint32_t*>(&he);
+  odd = *reinterpret_cast<const uint32_t*>(&ho);
+}
+// What is not finite in an 8-bit pool can only have been NaN.
+template <bool FP8>
+__device__ __forceinline__ float nan_if_infinite(float x) {
+  return FP8 && !(fabsf(x) <= 3.402823466e38f) ? __int_as_float(0x7fffffff) : x;
+}
+
+// Eight elements of a query row, whose largest magnitude is `top`, as bytes of two terms: x 2^e = hi (E4M3) + lo (E5M2).  2^e takes
+// `top` to (224, 448]; e is clipped where 2^e or its inverse would leave fp32's normal range.
+__device__ __forceinline__ void two_terms(const float (&f)[8], float top, int* e_out, uint2* hi_out, uint2* lo_out) {
+  const uint32_t bits = __float_as_uint(top);
+  const int e = top > 0.f && top < INFINITY ? min(max(135 - (int)(bits >> 23) - ((bits & 0x7fffffu) > 0x600000u ? 1 : 0), -120), 120) : 0;
+  const float up = __uint_as_float((uint32_t)(e + 127) << 23);
+  uint32_t hi[2] = {0, 0}, lo[2] = {0, 0};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float x = f[i] * up;
+    const uint32_t t = float_to_e4m3(x);
+    uint32_t rest;
+    asm("{\n.reg .b16 r;\ncvt.rn.satfinite.e5m2x2.f32 r, %1, %2;\ncvt.u32.u16 %0, r;\n}" : "=r"(rest) : "f"(0.f), "f"(x - e4m3_to_float(t)));
+    hi[i >> 2] |= t << (8 * (i & 3));
+    lo[i >> 2] |= (rest & 0xffu) << (8 * (i & 3));
+  }
+  *e_out = e;
+  *hi_out = make_uint2(hi[0], hi[1]);
+  *lo_out = make_uint2(lo[0], lo[1]);
+}
+
+// Log-sum-exp (natural) of a row from its reference and sum.
+template <bool FP8>
+__device__ __forceinline__ float row_lse(float m, float l) {
+  return l == 0.f ? -INFINITY : (m - (FP8 ? kShift + kLog2Widen : 0.f) + log2f(l)) * kLn2;
+}
+
+// ---------------------------------------------------------------------------------------------- parts of a triple
+// A triple (sequence, row tile, key head) whose tiles several CTAs share leaves partial sums: slot 2 c of CTA c for what an earlier
+// CTA began, slot 2 c + 1 for what it began itself.
+struct AttendParts {
+  float* sums;                    // [2 ctas][R][D]
+  float2* stats;                  // [2 ctas][R] reference and sum of weights
+  int4* headers;                  // [ctas][2]: CTAs behind this one with parts of its last triple (0: none), row0, head, row tile; rows
+};
+struct PartsLayout {
+  size_t sums, stats, headers, total;
+};
+inline PartsLayout parts_layout(int rows, int d, int ctas) {
+  PartsLayout w;
+  w.sums = 0;
+  w.stats = align_up((size_t)2 * ctas * rows * d * sizeof(float), 256);
+  w.headers = w.stats + align_up((size_t)2 * ctas * rows * sizeof(float2), 256);
+  w.total = w.headers + align_up((size_t)2 * ctas * sizeof(int4), 256);
+  return w;
+}
+inline AttendParts parts_at(void* workspace, int rows, int d, int ctas) {
+  const PartsLayout w = parts_layout(rows, d, ctas);
+  char* base = static_cast<char*>(workspace);
+  return AttendParts{reinterpret_cast<float*>(base + w.sums), reinterpret_cast<float2*>(base + w.stats), reinterpret_cast<int4*>(base + w.headers)};
+}
+// Launches the kernel that joins parts, behind the one that leaves them.
+int32_t attend_join_launch(const AttendArgs& a, const AttendParts& parts, int rows, int head_dim, bool fp8, int ctas, cudaStream_t stream);
+
 // The two kernels: a few rows a head and sequence, keys split over the chip; many rows.
+size_t attend_prompt_workspace_bytes(const spf_kv_cache* cache, int sm_count);
+int32_t attend_prompt_launch(const AttendArgs& a, const spf_kv_cache* cache, int sm_count, void* workspace, cudaStream_t stream);
+constexpr int kStepRows = 64;     // rows a key head and sequence up to which the first is taken
 size_t attend_step_workspace_bytes(const spf_kv_cache* cache, int group, int max_new, int sm_count);
 int32_t attend_step_launch(const AttendArgs& a, const spf_kv_cache* cache, int max_new, int sm_count, void* workspace, cudaStream_t stream);
 

@@ -45,8 +45,7 @@ constexpr int kWarps = 4;               // that compute
 // 128 x (192 + 64) = 256 x 128.
 constexpr int kComputeRegs = 192, kOtherRegs = 64;
 constexpr int kMaxStages = 8;
-constexpr float kLazy = 8.f;            // how far logits may exceed their reference
-constexpr float kShift = 7.f;           // 8-bit values: weights reach 2^(kLazy + kShift) = 2^15, below fp16's 65504
+
 
 // What the copying warp tells the computing ones about a stage.
 struct TileDesc {
@@ -54,7 +53,7 @@ struct TileDesc {
   float k_scale, v_log2, v_inverse;     // 8 bits
   int flags;                            // kFirst, kLast, kNoKeys; bits 8 ...: CTAs behind this one with parts of the triple
 };
-enum : int { kFirst = 1, kLast = 2, kNoKeys = 4, kFromStart = 8, kToEnd = 16 };
+
 
 template <int D_, bool FP8_, int R_>
 struct Traits {
@@ -76,6 +75,8 @@ struct Traits {
   static constexpr int JOIN = D * WK * R * 4 <= STAGE ? D : STAGE / (WK * R * 4);   // output columns joined at a time
 };
 
+enum : int { kFirst = 1, kLast = 2, kNoKeys = 4, kFromStart = 8, kToEnd = 16 };
+
 struct SmallSmem {
   unsigned long long full[kMaxStages], empty[kMaxStages], join;
   TileDesc desc[kMaxStages];
@@ -92,20 +93,9 @@ constexpr int smem_bytes() { return T::STAGES * T::STAGE + T::QBYTES + (int)size
 struct StepArgs {
   AttendArgs a;
   CUtensorMap k_map, v_map;
-  float* partial;                 // [2 ctas][R][D], [2 ctas][R] (m, l), headers
-  float2* partial_stats;
-  int4* headers;                  // per CTA: (CTAs behind it with parts of its last triple, row0, head, row tile), rows in .y2
+  AttendParts parts;
   int min_tiles;
 };
-
-__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
-  const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
-  return *reinterpret_cast<const uint32_t*>(&v);
-}
-__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
-  const __half2 v = __floats2half2_rn(lo, hi);
-  return *reinterpret_cast<const uint32_t*>(&v);
-}
 
 __device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t (&r)[4]) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
@@ -139,24 +129,6 @@ __device__ __forceinline__ void mma32(float (&d)[4], const uint32_t (&a)[4], uin
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// Four E4M3 bytes as two pairs of fp16, bytes 0 and 2, bytes 1 and 3, each times kWiden.  A byte s eeee mmm moved to the bits
-// s 0eeee mmm0000000 of a half is its value times 2^-8, subnormals included.  The product with 9 * 2^12 (exact: 4 + 4 significant
-// bits) leaves 448 at 64512, inside fp16, and takes the NaN patterns, which look like 480, to infinity.
-constexpr float kWiden = 144.f, kLog2Widen = 7.169925001442312f;
-__device__ __forceinline__ void widen4(uint32_t four, uint32_t& even, uint32_t& odd) {
-  const __half2 up = __half2half2(__ushort_as_half(0x7880));
-  const uint32_t e = (four & 0x00ff00ffu) * 128u + (four & 0x00800080u) * 128u;
-  const uint32_t o = ((four >> 1) & 0x3f803f80u) | (four & 0x80008000u);
-  const __half2 he = __hmul2(*reinterpret_cast<const __half2*>(&e), up), ho = __hmul2(*reinterpret_cast<const __half2*>(&o), up);
-  even = *reinterpret_cast<const uint32_t*>(&he);
-  odd = *reinterpret_cast<const uint32_t*>(&ho);
-}
-// What is not finite in an 8-bit pool can only have been NaN.
-template <bool FP8>
-__device__ __forceinline__ float nan_if_infinite(float x) {
-  return FP8 && !(fabsf(x) <= 3.402823466e38f) ? __int_as_float(0x7fffffff) : x;
-}
-
 // Byte offset of the 16-byte chunk `chunk` of row `row` in a tile, as the copies' swizzle lays it: spans of 128 (or 64) bytes
 // one after the other, the chunk's place in its span exchanged by the row.
 template <class T>
@@ -175,12 +147,6 @@ template <class T>
 __device__ __forceinline__ uint32_t q8_chunk(int row, int chunk) {
   if constexpr (T::D == 64) return (uint32_t)(row * 64 + ((chunk ^ (row >> 1)) & 3) * 16);
   return (uint32_t)(row * 128 + ((chunk ^ row) & 7) * 16);
-}
-
-// Log-sum-exp (natural) of a row from its reference and sum.
-template <bool FP8>
-__device__ __forceinline__ float row_lse(float m, float l) {
-  return l == 0.f ? -INFINITY : (m - (FP8 ? kShift + kLog2Widen : 0.f) + log2f(l)) * kLn2;
 }
 
 // ---------------------------------------------------------------------------------------------- the list of tiles
@@ -348,22 +314,11 @@ __device__ __forceinline__ void load_queries(const AttendArgs& a, const TileDesc
       }
 #pragma unroll
       for (int o = kLanes / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o, kLanes));
-      // 2^e takes `top` to (224, 448]; e clipped where the factor or its inverse would leave fp32's normal range
-      const uint32_t bits = __float_as_uint(top);
-      const int e = top > 0.f && top < INFINITY ? min(max(135 - (int)(bits >> 23) - ((bits & 0x7fffffu) > 0x600000u ? 1 : 0), -120), 120) : 0;
-      const float up = __uint_as_float((uint32_t)(e + 127) << 23);
-      uint32_t hi[2] = {0, 0}, lo[2] = {0, 0};
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float x = f[i] * up;
-        const uint32_t t = float_to_e4m3(x);
-        uint32_t rest;
-        asm("{\n.reg .b16 r;\ncvt.rn.satfinite.e5m2x2.f32 r, %1, %2;\ncvt.u32.u16 %0, r;\n}" : "=r"(rest) : "f"(0.f), "f"(x - e4m3_to_float(t)));
-        hi[i >> 2] |= t << (8 * (i & 3));
-        lo[i >> 2] |= (rest & 0xffu) << (8 * (i & 3));
-      }
-      *reinterpret_cast<uint2*>(q_tile + q8_chunk<T>(r, part >> 1) + 8 * (part & 1)) = make_uint2(hi[0], hi[1]);
-      *reinterpret_cast<uint2*>(q_tile + T::R * T::D + q8_chunk<T>(r, part >> 1) + 8 * (part & 1)) = make_uint2(lo[0], lo[1]);
+      int e;
+      uint2 hi, lo;
+      two_terms(f, top, &e, &hi, &lo);
+      *reinterpret_cast<uint2*>(q_tile + q8_chunk<T>(r, part >> 1) + 8 * (part & 1)) = hi;
+      *reinterpret_cast<uint2*>(q_tile + T::R * T::D + q8_chunk<T>(r, part >> 1) + 8 * (part & 1)) = lo;
       if (part == 0) q_factor[r] = __uint_as_float((uint32_t)(127 - e) << 23);
     }
   }
@@ -710,17 +665,17 @@ __device__ __forceinline__ void compute_tiles(const StepArgs& args, SmallSmem& s
             *reinterpret_cast<uint4*>(a.out.data + row * a.out.stride_row + head * a.out.stride_head + c0 + col) = v;
             if (a.lse != nullptr && c0 + col == 0) a.lse[row * a.lse_stride_row + head * a.lse_stride_head] = row_lse<T::FP8>(top, l);
           } else {
-            float4* dst = reinterpret_cast<float4*>(args.partial + ((int64_t)slot * R + r) * D + c0 + col);
+            float4* dst = reinterpret_cast<float4*>(args.parts.sums + ((int64_t)slot * R + r) * D + c0 + col);
             dst[0] = make_float4(x[0], x[1], x[2], x[3]);
             dst[1] = make_float4(x[4], x[5], x[6], x[7]);
-            if (c0 + col == 0) args.partial_stats[slot * R + r] = make_float2(top, l);
+            if (c0 + col == 0) args.parts.stats[slot * R + r] = make_float2(top, l);
           }
         }
         if (!join.wait(ab)) return;
       }
       if ((flags & kFromStart) && !(flags & kToEnd) && threadIdx.x == 0) {
-        args.headers[2 * blockIdx.x] = make_int4(flags >> 8, d.row0, d.head, d.row_tile);
-        args.headers[2 * blockIdx.x + 1] = make_int4(live, 0, 0, 0);
+        args.parts.headers[2 * blockIdx.x] = make_int4(flags >> 8, d.row0, d.head, d.row_tile);
+        args.parts.headers[2 * blockIdx.x + 1] = make_int4(live, 0, 0, 0);
       }
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // the stage was written with ordinary stores; copies follow
     }
@@ -744,10 +699,11 @@ __global__ void __launch_bounds__(Traits<D, FP8, R>::THREADS, Traits<D, FP8, R>:
     }
     mbar_init(smem_u32(&sm.join), kWarps);
     sm.abort = 0;
-    args.headers[2 * blockIdx.x] = make_int4(0, 0, 0, 0);
+    args.parts.headers[2 * blockIdx.x] = make_int4(0, 0, 0, 0);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   find_start<T>(args, sm);                               // ends with a barrier of the CTA
+  grid_launch_dependents();                              // every CTA of this kernel has started: the joining one can take its place
   const int64_t total = sm.total;
   const int64_t per = max((int64_t)args.min_tiles, (total + gridDim.x - 1) / gridDim.x);
   const int64_t w0 = per * blockIdx.x, w1 = min(w0 + per, total);
@@ -761,55 +717,6 @@ __global__ void __launch_bounds__(Traits<D, FP8, R>::THREADS, Traits<D, FP8, R>:
       if (threadIdx.x < (kWarps + 1) * 32) copy_tiles<T>(args, sm, smem_u32(ring_ptr), w0, w1, per, ab);
     }
   }
-  grid_launch_dependents();
-}
-
-// Joins the parts of the triples that CTA blockIdx.x began and others went on with: a warp per row.
-template <int D, bool FP8, int R>
-__global__ void __launch_bounds__(128) attend_join_kernel(const __grid_constant__ StepArgs args) {
-  const AttendArgs& a = args.a;
-  grid_wait();
-  const int4 head = args.headers[2 * blockIdx.x];
-  const int r = blockIdx.y * 4 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
-  if (head.x <= 0 || r >= args.headers[2 * blockIdx.x + 1].x) return;
-  const int parts = head.x + 1;
-  auto slot = [&](int i) { return i == 0 ? 2 * (int)blockIdx.x + 1 : 2 * ((int)blockIdx.x + i); };
-  float top = -INFINITY;
-  for (int i = lane; i < parts; i += 32) top = fmaxf(top, args.partial_stats[slot(i) * R + r].x);
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-  constexpr int V = D / 32;                              // columns of a lane
-  float x[V] = {}, l = 0.f;
-#pragma unroll 4
-  for (int i = 0; i < parts; ++i) {
-    const float2 s = args.partial_stats[slot(i) * R + r];
-    const float f = s.x == -INFINITY ? 0.f : fast_exp2(s.x - top);
-    const float* src = args.partial + ((int64_t)slot(i) * R + r) * D + lane * V;
-    l += s.y * f;
-#pragma unroll
-    for (int j = 0; j < V; ++j) x[j] += src[j] * f;
-  }
-  const int rr = head.w * R + r;
-  const int64_t row = head.y + rr / a.group;
-  const int h = head.z * a.group + rr % a.group;
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  uint32_t* dst = reinterpret_cast<uint32_t*>(a.out.data + row * a.out.stride_row + h * a.out.stride_head) + lane * (V / 2);
-#pragma unroll
-  for (int j = 0; j < V / 2; ++j) dst[j] = pack_bf16(nan_if_infinite<FP8>(x[2 * j]) * inv, nan_if_infinite<FP8>(x[2 * j + 1]) * inv);
-  if (a.lse != nullptr && lane == 0)
-    a.lse[row * a.lse_stride_row + h * a.lse_stride_head] = row_lse<FP8>(top, l);
-}
-
-struct StepWorkspace {
-  size_t partial, stats, headers, total;
-};
-StepWorkspace step_workspace(int rows, int d, int ctas) {
-  StepWorkspace w;
-  w.partial = 0;
-  w.stats = align_up((size_t)2 * ctas * rows * d * sizeof(float), 256);
-  w.headers = w.stats + align_up((size_t)2 * ctas * rows * sizeof(float2), 256);
-  w.total = w.headers + align_up((size_t)2 * ctas * sizeof(int4), 256);
-  return w;
 }
 
 // Rows of a tile: the fewest that hold the rows of a sequence and key head, up to 64.
@@ -827,17 +734,7 @@ int32_t launch_step(const StepArgs& args, int ctas, cudaStream_t stream) {
   if (st != SPF_OK) return st;
   attend_step_kernel<D, FP8, R><<<ctas, T::THREADS, smem_bytes<T>(), stream>>>(args);
   SPF_CUDA_CHECK(cudaGetLastError());
-  cudaLaunchConfig_t config{};
-  config.gridDim = dim3((unsigned)ctas, R / 4);
-  config.blockDim = dim3(128);
-  config.stream = stream;
-  cudaLaunchAttribute attr{};
-  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr.val.programmaticStreamSerializationAllowed = 1;
-  config.attrs = &attr;
-  config.numAttrs = 1;
-  SPF_CUDA_CHECK(cudaLaunchKernelEx(&config, attend_join_kernel<D, FP8, R>, args));
-  return SPF_OK;
+  return attend_join_launch(args.a, args.parts, R, D, FP8, ctas, stream);
 }
 
 template <int D, bool FP8>
@@ -856,7 +753,7 @@ size_t attend_step_workspace_bytes(const spf_kv_cache* cache, int group, int max
   // a step with fewer rows has more CTAs: the most that any with up to this many takes
   size_t most = 0;
   for (int rows = 8; rows <= tile_rows(group, max_new); rows *= 2)
-    most = std::max(most, step_workspace(rows, cache->head_dim, sm_count * ctas_per_sm(rows)).total);
+    most = std::max(most, parts_layout(rows, cache->head_dim, sm_count * ctas_per_sm(rows)).total);
   return most;
 }
 
@@ -864,11 +761,7 @@ int32_t attend_step_launch(const AttendArgs& a, const spf_kv_cache* cache, int m
   StepArgs args{};
   args.a = a;
   const int rows = tile_rows(a.group, max_new), ctas = sm_count * ctas_per_sm(rows);
-  const StepWorkspace w = step_workspace(rows, cache->head_dim, ctas);
-  char* base = static_cast<char*>(workspace);
-  args.partial = reinterpret_cast<float*>(base + w.partial);
-  args.partial_stats = reinterpret_cast<float2*>(base + w.stats);
-  args.headers = reinterpret_cast<int4*>(base + w.headers);
+  args.parts = parts_at(workspace, rows, cache->head_dim, ctas);
   args.min_tiles = 2;
   int32_t st = encode_pool_map("spf_attend", cache, cache->k_pool, kKeys, &args.k_map);
   if (st == SPF_OK) st = encode_pool_map("spf_attend", cache, cache->v_pool, kKeys, &args.v_map);
