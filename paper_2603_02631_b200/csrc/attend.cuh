@@ -153,8 +153,9 @@ inline AttendParts parts_at(void* workspace, int rows, int d, int ctas) {
   char* base = static_cast<char*>(workspace);
   return AttendParts{reinterpret_cast<float*>(base + w.sums), reinterpret_cast<float2*>(base + w.stats), reinterpret_cast<int4*>(base + w.headers)};
 }
-// Launches the kernel that joins parts, behind the one that leaves them.
-int32_t attend_join_launch(const AttendArgs& a, const AttendParts& parts, int rows, int head_dim, bool fp8, int ctas, cudaStream_t stream);
+// Launches the kernel that joins parts, behind the one that leaves them.  `live`: rows that a tile of `rows` is expected to have at
+// most; with more the kernel does its work in several rounds.
+int32_t attend_join_launch(const AttendArgs& a, const AttendParts& parts, int rows, int live, int head_dim, bool fp8, int ctas, cudaStream_t stream);
 
 // The two kernels: a few rows a head and sequence, keys split over the chip; many rows.
 size_t attend_prompt_workspace_bytes(const spf_kv_cache* cache, int sm_count);

@@ -738,7 +738,7 @@ int32_t launch(const PromptArgs& args, int ctas, cudaStream_t stream) {
   if (st != SPF_OK) return st;
   attend_prompt_kernel<D, FP8><<<ctas, kThreads, smem_bytes<T>(), stream>>>(args);
   SPF_CUDA_CHECK(cudaGetLastError());
-  return attend_join_launch(args.a, args.parts, kRows, D, FP8, ctas, stream);
+  return attend_join_launch(args.a, args.parts, kRows, kRows, D, FP8, ctas, stream);
 }
 
 }  // namespace

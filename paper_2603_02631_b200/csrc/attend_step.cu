@@ -39,18 +39,18 @@
 namespace spf {
 namespace {
 
-constexpr int kKeys = 64;               // keys of a tile: one scale's worth
 constexpr int kWarps = 4;               // that compute
 // From 16 rows on a second warpgroup, whose first warp copies, lends registers of the 128 a thread that the launch has,
 // 128 x (192 + 64) = 256 x 128.
 constexpr int kComputeRegs = 192, kOtherRegs = 64;
 constexpr int kMaxStages = 8;
+constexpr float kNoReference = -1.5e38f;   // of a row that has seen no key: finite, so that no difference of two is NaN
 
 
 // What the copying warp tells the computing ones about a stage.
 struct TileDesc {
   int row0, n_new, pos0, first, end, head, row_tile, key0;
-  float k_scale, v_log2, v_inverse;     // 8 bits
+  float k_scale[2], v_log2[2], v_inverse[2];   // 8 bits: of the tile's groups of 64 keys
   int flags;                            // kFirst, kLast, kNoKeys; bits 8 ...: CTAs behind this one with parts of the triple
 };
 
@@ -62,13 +62,17 @@ struct Traits {
   // warps over rows (16 rows of 128 dimensions, 32 of 64, are 64 registers of outputs), and over keys
   static constexpr int WR = R * D <= 2048 ? 1 : R * D / 2048, WK = kWarps / WR;
   static constexpr int NT = R / (8 * WR);                             // 8-row tiles of a warp
-  static constexpr int KW = kKeys / WK, KT = KW / 16;                 // keys of a warp in a tile, in sixteens
+  // Keys of a tile: 128 where their rows are short, so that a warp has two sixteens of them at a time.  (One sixteen is a chain of
+  // dependent steps: with tiles of 64 keys 32 sequences of up to 16k tokens on an 8-bit cache took 136 instead of 111 us, four of up to
+  // 250k 384 instead of 292, eight lookahead tokens over 131072 keys of 64 dimensions 92 instead of 70.)  A warp's keys share a scale, so they are 64 at most.
+  static constexpr int KEYS = (FP8 ? D : 2 * D) <= 128 && WK > 1 ? 128 : 64;
+  static constexpr int KW = KEYS / WK, KT = KW / 16;                  // keys of a warp in a tile, in sixteens
   static constexpr bool LEND = R >= 16;                               // registers move between warpgroups
   static constexpr int THREADS = LEND ? 2 * kWarps * 32 : (kWarps + 1) * 32;
   static constexpr int CTAS = R == 8 ? 3 : 2;                         // per SM
   static constexpr bool QREGS = R <= 16;                              // queries stay in registers
   static constexpr int ROWB = FP8 ? D : 2 * D, SPAN = ROWB < 128 ? ROWB : 128;
-  static constexpr int TILE = kKeys * ROWB, STAGE = 2 * TILE;
+  static constexpr int TILE = KEYS * ROWB, STAGE = 2 * TILE;
   static constexpr int QBYTES = R * D * 2;
   static constexpr int FIT = ((CTAS == 3 ? 74 : 112) * 1024 - 4096 - QBYTES) / STAGE;
   static constexpr int STAGES = FIT < kMaxStages ? FIT : kMaxStages;
@@ -94,7 +98,6 @@ struct StepArgs {
   AttendArgs a;
   CUtensorMap k_map, v_map;
   AttendParts parts;
-  int min_tiles;
 };
 
 __device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t (&r)[4]) {
@@ -134,7 +137,7 @@ __device__ __forceinline__ void mma32(float (&d)[4], const uint32_t (&a)[4], uin
 template <class T>
 __device__ __forceinline__ uint32_t tile_chunk(int row, int chunk) {
   if constexpr (T::SPAN == 64) return (uint32_t)(row * 64 + ((chunk ^ (row >> 1)) & 3) * 16);
-  return (uint32_t)((chunk >> 3) * (kKeys * 128) + row * 128 + ((chunk ^ row) & 7) * 16);
+  return (uint32_t)((chunk >> 3) * (T::KEYS * 128) + row * 128 + ((chunk ^ row) & 7) * 16);
 }
 // The same for the query tile, rows of 2 D bytes.
 template <class T>
@@ -150,7 +153,8 @@ __device__ __forceinline__ uint32_t q8_chunk(int row, int chunk) {
 }
 
 // ---------------------------------------------------------------------------------------------- the list of tiles
-__device__ __forceinline__ int tiles_of(const SeqSpan& s) { return max((s.end + kKeys - 1) / kKeys - s.first / kKeys, 1); }
+template <class T>
+__device__ __forceinline__ int tiles_of(const SeqSpan& s) { return max((s.end + T::KEYS - 1) / T::KEYS - s.first / T::KEYS, 1); }
 template <class T>
 __device__ __forceinline__ int row_tiles_of(const AttendArgs& a, const SeqSpan& s) {
   return (int)(((int64_t)s.n_new * a.group + T::R - 1) / T::R);
@@ -158,7 +162,7 @@ __device__ __forceinline__ int row_tiles_of(const AttendArgs& a, const SeqSpan& 
 template <class T>
 __device__ __forceinline__ int64_t cost_of(const AttendArgs& a, int b) {
   const SeqSpan s = seq_span(a, b);
-  return (int64_t)row_tiles_of<T>(a, s) * a.kv.n_kv_heads * tiles_of(s);
+  return (int64_t)row_tiles_of<T>(a, s) * a.kv.n_kv_heads * tiles_of<T>(s);
 }
 
 // Length of the list, and the sequence that holds the CTA's first tile.  Every thread sums up a run of sequences.
@@ -183,7 +187,7 @@ __device__ __forceinline__ void find_start(const StepArgs& args, SmallSmem& sm) 
     if (w < warp) upto += sm.scan[w];
     total += sm.scan[w];
   }
-  const int64_t per = max((int64_t)args.min_tiles, (total + gridDim.x - 1) / gridDim.x), w0 = per * blockIdx.x;
+  const int64_t w0 = (total + gridDim.x - 1) / gridDim.x * blockIdx.x;
   if (threadIdx.x == 0) sm.total = total;
   if (w0 >= upto - mine && w0 < upto) {
     int64_t base = upto - mine;
@@ -217,12 +221,12 @@ __device__ __forceinline__ void copy_tiles(const StepArgs& args, SmallSmem& sm, 
     int row = 0;
     if (mine < w1) {
       SeqSpan s = seq_span(a, seq);
-      int tiles = tiles_of(s), row_tiles = row_tiles_of<T>(a, s);
+      int tiles = tiles_of<T>(s), row_tiles = row_tiles_of<T>(a, s);
       int64_t cost = (int64_t)row_tiles * a.kv.n_kv_heads * tiles;
       while (mine >= base + cost && seq < a.step.n_seqs - 1) {
         base += cost;
         s = seq_span(a, ++seq);
-        tiles = tiles_of(s);
+        tiles = tiles_of<T>(s);
         row_tiles = row_tiles_of<T>(a, s);
         cost = (int64_t)row_tiles * a.kv.n_kv_heads * tiles;
       }
@@ -236,16 +240,19 @@ __device__ __forceinline__ void copy_tiles(const StepArgs& args, SmallSmem& sm, 
       d.end = s.end;
       d.head = (int)(triple / row_tiles);
       d.row_tile = (int)(triple - (int64_t)d.head * row_tiles);
-      d.key0 = (s.first / kKeys + tile) * kKeys;
+      d.key0 = (s.first / T::KEYS + tile) * T::KEYS;
       d.flags = (mine == max(from, w0) ? kFirst : 0) | (mine == min(to, w1) - 1 ? kLast : 0) | (s.first >= s.end ? kNoKeys : 0) |
                 (from >= w0 ? kFromStart : 0) | (to <= w1 ? kToEnd : 0) | ((int)((to - 1) / per - blockIdx.x) << 8);
       if (s.first < s.end) {
         row = pool_row(a, seq, d.head, d.key0);
         if constexpr (T::FP8) {
-          const float v = group_scale(a.kv.v_scale, row, pool_rows);
-          d.k_scale = a.c * group_scale(a.kv.k_scale, row, pool_rows);
-          d.v_log2 = log2f(v);
-          d.v_inverse = kWiden / v;                       // l comes out times kWiden, as the values do
+#pragma unroll
+          for (int g = 0; g < T::KEYS / kScaleTokens; ++g) {
+            const float v = group_scale(a.kv.v_scale, row + g * kScaleTokens, pool_rows);
+            d.k_scale[g] = a.c * group_scale(a.kv.k_scale, row + g * kScaleTokens, pool_rows);
+            d.v_log2[g] = log2f(v);
+            d.v_inverse[g] = kWiden / v;                  // l comes out times kWiden, as the values do
+          }
         }
       }
     }
@@ -394,60 +401,94 @@ struct State {
   float m[T::NT][2], l[T::NT][2];
 };
 
-// out += values . weights of 16 keys, p[nt] being the weights of 8 rows.  `guard`: the tile has keys that not every row may see,
-// or keys outside the sequence's range [first, end).
-template <class T>
-__device__ __forceinline__ void add_values(State<T>& st, const uint32_t (&p)[T::NT][2], uint32_t v_tile, int key_in_tile, int key0, const TileDesc& d,
-                                           int group, int causal, int row_in_triple, bool guard, int lane) {
+// Keys of a triple that its rows see: [first, end) that some do, below `all` that every one does.
+struct Seen {
+  int first, end, all;
+};
+
+// out += values . weights of the warp's keys from `key` (of the tile, which begins at key0) on, p[kt][nt] being the weights of
+// sixteen keys and eight rows.  GUARD: the tile has keys outside [first, end), whose values are taken as zeros.
+template <class T, bool GUARD>
+__device__ __forceinline__ void add_values(State<T>& st, const uint32_t (&p)[T::KT][T::NT][2], uint32_t v_tile, int key, int key0, const Seen& seen,
+                                           int lane) {
   constexpr int kStep = T::FP8 ? 2 : 1;
 #pragma unroll
-  for (int m0 = 0; m0 < T::D / 16; m0 += kStep) {
-    uint32_t v[kStep][4];
-    value_operand<T>(v_tile, key_in_tile, m0, lane, v);
-    bool odd = false;
-    if (guard) {
+  for (int kt = 0; kt < T::KT; ++kt)
+#pragma unroll
+    for (int m0 = 0; m0 < T::D / 16; m0 += kStep) {
+      uint32_t v[kStep][4];
+      value_operand<T>(v_tile, key + kt * 16, m0, lane, v);
+      if (GUARD) {
+        const int base = key0 + key + kt * 16;
+#pragma unroll
+        for (int i = 0; i < kStep; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            v[i][e] = keep_keys(v[i][e], base + value_key<T>(lane, e, 0), base + value_key<T>(lane, e, 1), seen.first, seen.end);
+      }
 #pragma unroll
       for (int i = 0; i < kStep; ++i)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int base = key0 + key_in_tile;
-          v[i][e] = keep_keys(v[i][e], base + value_key<T>(lane, e, 0), base + value_key<T>(lane, e, 1), d.first, d.end);
-          odd |= not_finite<T::FP8>(v[i][e]);
-        }
-      odd = __any_sync(0xffffffffu, odd);
+        for (int nt = 0; nt < T::NT; ++nt) mma16<T::FP8>(st.o[m0 + i][nt], v[i], p[kt][nt][0], p[kt][nt][1]);
     }
-    if (!odd) {
+}
+
+// Whether the warp has values that are not finite of keys that some row sees and others do not.
+template <class T>
+__device__ __noinline__ bool odd_values(uint32_t v_tile, int key, int key0, int all, int end, int lane) {
+  constexpr int kStep = T::FP8 ? 2 : 1;
+  bool odd = false;
+  for (int kt = 0; kt < T::KT; ++kt)
+    for (int m0 = 0; m0 < T::D / 16; m0 += kStep) {
+      uint32_t v[kStep][4];
+      value_operand<T>(v_tile, key + kt * 16, m0, lane, v);
+      const int base = key0 + key + kt * 16;
 #pragma unroll
       for (int i = 0; i < kStep; ++i)
 #pragma unroll
-        for (int nt = 0; nt < T::NT; ++nt) mma16<T::FP8>(st.o[m0 + i][nt], v[i], p[nt][0], p[nt][1]);
-    } else {
-      // values that are not finite, some of which only some rows may see: row by row, each with the values that it sees
+        for (int e = 0; e < 4; ++e)
+          odd |= not_finite<T::FP8>(keep_keys(v[i][e], base + value_key<T>(lane, e, 0), base + value_key<T>(lane, e, 1), all, end));
+    }
+  return __any_sync(0xffffffffu, odd);
+}
+
+// add_values where there are such: row by row, each with the values that it sees.
+template <class T>
+__device__ __forceinline__ void add_odd_values(State<T>& st, const uint32_t (&p)[T::KT][T::NT][2], uint32_t v_tile, int key, int key0, const Seen& seen,
+                                               const TileDesc& d, int group, int causal, int row_in_triple, int lane) {
+  constexpr int kStep = T::FP8 ? 2 : 1;
 #pragma unroll 1
-      for (int r = 0; r < 8; ++r)
+  for (int r = 0; r < 8; ++r) {
+    const bool mine = (lane >> 2) == r;
+#pragma unroll
+    for (int kt = 0; kt < T::KT; ++kt)
+#pragma unroll
+      for (int m0 = 0; m0 < T::D / 16; m0 += kStep) {
+        uint32_t v[kStep][4];
+        value_operand<T>(v_tile, key + kt * 16, m0, lane, v);
+        const int base = key0 + key + kt * 16;
 #pragma unroll
         for (int nt = 0; nt < T::NT; ++nt) {
-          const int hi = causal ? min(d.end, d.pos0 + (row_in_triple + nt * 8 + r) / group + 1) : d.end, base = key0 + key_in_tile;
-          const bool mine = (lane >> 2) == r;
+          const int hi = causal ? min(seen.end, d.pos0 + (row_in_triple + nt * 8 + r) / group + 1) : seen.end;
 #pragma unroll
           for (int i = 0; i < kStep; ++i) {
             float part[4] = {0.f, 0.f, 0.f, 0.f};
             uint32_t vr[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) vr[e] = keep_keys(v[i][e], base + value_key<T>(lane, e, 0), base + value_key<T>(lane, e, 1), d.first, hi);
-            mma16<T::FP8>(part, vr, mine ? p[nt][0] : 0u, mine ? p[nt][1] : 0u);
+            for (int e = 0; e < 4; ++e) vr[e] = keep_keys(v[i][e], base + value_key<T>(lane, e, 0), base + value_key<T>(lane, e, 1), seen.first, hi);
+            mma16<T::FP8>(part, vr, mine ? p[kt][nt][0] : 0u, mine ? p[kt][nt][1] : 0u);
 #pragma unroll
             for (int e = 0; e < 4; ++e)
               if (2 * (lane & 3) + (e & 1) == r) st.o[m0 + i][nt][e] += part[e];
           }
         }
-    }
+      }
   }
 }
 
 template <class T>
 __device__ __forceinline__ void compute_tiles(const StepArgs& args, SmallSmem& sm, unsigned char* ring_ptr, uint32_t ring, unsigned char* q_tile,
-                                              int64_t n_tiles, const Abort& ab) {
+                                              int64_t w0, int64_t n_tiles, const Abort& ab) {
   constexpr int D = T::D, R = T::R, NT = T::NT, KT = T::KT;
   constexpr int kTerms = T::FP8 ? 2 : 1, kSteps = T::FP8 ? D / 64 : D / 32;   // four registers of queries each
   const AttendArgs& a = args.a;
@@ -458,21 +499,38 @@ __device__ __forceinline__ void compute_tiles(const StepArgs& args, SmallSmem& s
   Join join{smem_u32(&sm.join), 0};
   State<T> st;
   float qf[NT][2];
+  int sees[NT][2];                                       // the key behind the last one that a row sees
+  Seen seen{0, 0, 0};
   uint32_t q[T::QREGS ? kTerms * kSteps * NT : 1][4];
   int stage = 0;
   uint32_t parity = 0;
+  {
+    // the queries of the CTA's first triple, while its first keys are on their way
+    const SeqSpan s = seq_span(a, sm.start_seq);
+    const int64_t triple = (w0 - sm.start_base) / tiles_of<T>(s);
+    TileDesc d;
+    d.row0 = s.row0, d.n_new = s.n_new;
+    d.head = (int)(triple / row_tiles_of<T>(a, s));
+    d.row_tile = (int)(triple - (int64_t)d.head * row_tiles_of<T>(a, s));
+    load_queries<T>(a, d, q_tile, q_factor);
+  }
   for (int64_t tile = 0; tile < n_tiles; ++tile) {
     if (!mbar_wait_warp(smem_u32(&sm.full[stage]), parity, ab)) return;
     const TileDesc& d = sm.desc[stage];
     const int flags = d.flags;
     if (flags & kFirst) {
-      load_queries<T>(a, d, q_tile, q_factor);
+      if (tile > 0) load_queries<T>(a, d, q_tile, q_factor);
       if (!join.wait(ab)) return;
+      const int row_first = d.row_tile * R;
+      seen.first = d.first, seen.end = d.end;
+      seen.all = a.causal ? min(d.end, d.pos0 + row_first / a.group + 1) : d.end;
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          st.m[nt][e] = -INFINITY;
+          const int row = row_first + row_off + nt * 8 + 2 * (lane & 3) + e;
+          sees[nt][e] = a.causal ? min(d.end, d.pos0 + row / a.group + 1) : d.end;
+          st.m[nt][e] = kNoReference;
           st.l[nt][e] = 0.f;
           if constexpr (T::FP8) qf[nt][e] = q_factor[row_off + nt * 8 + 2 * (lane & 3) + e];
         }
@@ -492,8 +550,8 @@ __device__ __forceinline__ void compute_tiles(const StepArgs& args, SmallSmem& s
     }
     if (!(flags & kNoKeys)) {
       const uint32_t k_tile = ring + stage * T::STAGE, v_tile = k_tile + T::TILE;
-      const int key0 = d.key0, row_first = d.row_tile * R;
-      const bool guard = key0 < d.first || key0 + kKeys > d.end || (a.causal && key0 + kKeys - 1 > d.pos0 + row_first / a.group);
+      const int key0 = d.key0, group64 = T::KEYS > kScaleTokens ? key_off / kScaleTokens : 0;
+      const bool guard = key0 < seen.first || key0 + T::KEYS > seen.all;
       // logits of the warp's keys and rows
       float z[KT][NT][4];
 #pragma unroll
@@ -530,68 +588,68 @@ __device__ __forceinline__ void compute_tiles(const StepArgs& args, SmallSmem& s
               }
           }
       }
-      // base-2 logits, masked
+      if (guard) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int key = key0 + key_off + kt * 16 + key_of<T>(lane, e >> 1);
+              if (key < seen.first || key >= sees[nt][e & 1]) z[kt][nt][e] = -INFINITY;
+            }
+      }
+      // base-2 logits are z f + add; the largest decides whether a row's reference moves
+      const float add = T::FP8 ? d.v_log2[group64] : 0.f, k_scale = T::FP8 ? d.k_scale[group64] : a.c;
+      float f[NT][2], top[NT][2];
       bool over = false;
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          const float f = T::FP8 ? d.k_scale * qf[nt][e] : a.c;
-          const float add = T::FP8 ? d.v_log2 : 0.f;
-          int hi = d.end;
-          if (guard && a.causal) hi = min(hi, d.pos0 + (row_first + row_off + nt * 8 + 2 * (lane & 3) + e) / a.group + 1);
-          const float limit = st.m[nt][e] + kLazy;
+          f[nt][e] = T::FP8 ? k_scale * qf[nt][e] : k_scale;
+          float t = fmaxf(z[0][nt][e], z[0][nt][2 + e]);
 #pragma unroll
-          for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              float x = T::FP8 ? fmaf(z[kt][nt][2 * h + e], f, add) : z[kt][nt][2 * h + e] * f;
-              if (guard) {
-                const int key = key0 + key_off + kt * 16 + key_of<T>(lane, h);
-                if (key < d.first || key >= hi) x = -INFINITY;
-              }
-              z[kt][nt][2 * h + e] = x;
-              over |= x > limit;
-            }
+          for (int kt = 1; kt < KT; ++kt) t = max3(t, z[kt][nt][e], z[kt][nt][2 + e]);
+          top[nt][e] = fmaf(t, f[nt][e], add);
+          over |= top[nt][e] > st.m[nt][e] + kLazy;
         }
       if (__any_sync(0xffffffffu, over)) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            float top = st.m[nt][e];
+            float t = fmaxf(st.m[nt][e], top[nt][e]);
 #pragma unroll
-            for (int kt = 0; kt < KT; ++kt) top = fmaxf(top, fmaxf(z[kt][nt][e], z[kt][nt][2 + e]));
+            for (int o = 4; o < 32; o <<= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, o));
+            const float scale = fast_exp2(st.m[nt][e] - t);
+            st.m[nt][e] = t;
+            st.l[nt][e] *= scale;
 #pragma unroll
-            for (int o = 4; o < 32; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-            const float f = top == st.m[nt][e] ? 1.f : fast_exp2(st.m[nt][e] - top);
-            st.m[nt][e] = top;
-            st.l[nt][e] *= f;
-#pragma unroll
-            for (int m = 0; m < D / 16; ++m) st.o[m][nt][e] *= f, st.o[m][nt][2 + e] *= f;
+            for (int m = 0; m < D / 16; ++m) st.o[m][nt][e] *= scale, st.o[m][nt][2 + e] *= scale;
           }
       }
       uint32_t p[KT][NT][2];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
-        float ref[2], sum[2] = {0.f, 0.f};
+        float off[2], sum[2] = {0.f, 0.f};
 #pragma unroll
-        for (int e = 0; e < 2; ++e) ref[e] = (st.m[nt][e] == -INFINITY ? 0.f : st.m[nt][e]) - (T::FP8 ? kShift : 0.f);
+        for (int e = 0; e < 2; ++e) off[e] = add - (st.m[nt][e] - (T::FP8 ? kShift : 0.f));
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            const float x = fast_exp2(z[kt][nt][2 * h] - ref[0]), y = fast_exp2(z[kt][nt][2 * h + 1] - ref[1]);
+            const float x = fast_exp2(fmaf(z[kt][nt][2 * h], f[nt][0], off[0])), y = fast_exp2(fmaf(z[kt][nt][2 * h + 1], f[nt][1], off[1]));
             sum[0] += x;
             sum[1] += y;
             p[kt][nt][h] = transpose8(T::FP8 ? pack_f16(x, y) : pack_bf16(x, y));
           }
 #pragma unroll
-        for (int e = 0; e < 2; ++e) st.l[nt][e] = T::FP8 ? fmaf(sum[e], d.v_inverse, st.l[nt][e]) : st.l[nt][e] + sum[e];
+        for (int e = 0; e < 2; ++e) st.l[nt][e] = T::FP8 ? fmaf(sum[e], d.v_inverse[group64], st.l[nt][e]) : st.l[nt][e] + sum[e];
       }
-#pragma unroll
-      for (int kt = 0; kt < KT; ++kt)
-        add_values<T>(st, p[kt], v_tile, key_off + kt * 16, key0, d, a.group, a.causal, row_first + row_off, guard, lane);
+      if (!guard) add_values<T, false>(st, p, v_tile, key_off, key0, seen, lane);
+      else if (seen.all >= seen.end || !odd_values<T>(v_tile, key_off, key0, seen.all, seen.end, lane)) add_values<T, true>(st, p, v_tile, key_off, key0, seen, lane);
+      else add_odd_values<T>(st, p, v_tile, key_off, key0, seen, d, a.group, a.causal, d.row_tile * R + row_off, lane);
     }
     if (flags & kLast) {
       // the warps' sums of a row, each against its own reference
@@ -611,10 +669,10 @@ __device__ __forceinline__ void compute_tiles(const StepArgs& args, SmallSmem& s
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           const int r = row_off + nt * 8 + 2 * (lane & 3) + e;
-          float top = -INFINITY;
+          float top = kNoReference;
 #pragma unroll
           for (int w = 0; w < T::WK; ++w) top = fmaxf(top, sm.stats[w][r].x);
-          f[nt][e] = st.m[nt][e] == -INFINITY ? 0.f : fast_exp2(st.m[nt][e] - top);
+          f[nt][e] = fast_exp2(st.m[nt][e] - top);
         }
       const bool whole = (flags & kFromStart) && (flags & kToEnd);
       const int slot = 2 * blockIdx.x + ((flags & kFromStart) ? 1 : 0);
@@ -646,12 +704,11 @@ __device__ __forceinline__ void compute_tiles(const StepArgs& args, SmallSmem& s
             const float4 u = src[0], v = src[1];
             x[0] += u.x, x[1] += u.y, x[2] += u.z, x[3] += u.w, x[4] += v.x, x[5] += v.y, x[6] += v.z, x[7] += v.w;
           }
-          float top = -INFINITY, l = 0.f;
+          float top = kNoReference, l = 0.f;
 #pragma unroll
           for (int w = 0; w < T::WK; ++w) top = fmaxf(top, sm.stats[w][r].x);
 #pragma unroll
-          for (int w = 0; w < T::WK; ++w)
-            if (sm.stats[w][r].x != -INFINITY) l += sm.stats[w][r].y * fast_exp2(sm.stats[w][r].x - top);
+          for (int w = 0; w < T::WK; ++w) l += sm.stats[w][r].y * fast_exp2(sm.stats[w][r].x - top);
           if (whole) {
             const int rr = d.row_tile * R + r;
             const int64_t row = d.row0 + rr / a.group;
@@ -705,13 +762,13 @@ __global__ void __launch_bounds__(Traits<D, FP8, R>::THREADS, Traits<D, FP8, R>:
   find_start<T>(args, sm);                               // ends with a barrier of the CTA
   grid_launch_dependents();                              // every CTA of this kernel has started: the joining one can take its place
   const int64_t total = sm.total;
-  const int64_t per = max((int64_t)args.min_tiles, (total + gridDim.x - 1) / gridDim.x);
+  const int64_t per = (total + gridDim.x - 1) / gridDim.x;
   const int64_t w0 = per * blockIdx.x, w1 = min(w0 + per, total);
   if (w0 < w1) {
     const Abort ab{&sm.abort, args.a.dev_status};
     if (threadIdx.x < kWarps * 32) {
       if constexpr (T::LEND) reg_inc<kComputeRegs>();
-      compute_tiles<T>(args, sm, ring_ptr, smem_u32(ring_ptr), q_tile, w1 - w0, ab);
+      compute_tiles<T>(args, sm, ring_ptr, smem_u32(ring_ptr), q_tile, w0, w1 - w0, ab);
     } else {
       if constexpr (T::LEND) reg_dec<kOtherRegs>();
       if (threadIdx.x < (kWarps + 1) * 32) copy_tiles<T>(args, sm, smem_u32(ring_ptr), w0, w1, per, ab);
@@ -727,23 +784,25 @@ int tile_rows(int group, int max_new) {
 int ctas_per_sm(int rows) { return rows <= 8 ? 3 : 2; }
 
 template <int D, bool FP8, int R>
-int32_t launch_step(const StepArgs& args, int ctas, cudaStream_t stream) {
+int32_t launch_step(StepArgs& args, const spf_kv_cache* cache, int live, int ctas, cudaStream_t stream) {
   using T = Traits<D, FP8, R>;
   static ContextSet done;
-  const int32_t st = allow_shared_memory(reinterpret_cast<const void*>(attend_step_kernel<D, FP8, R>), smem_bytes<T>(), done);
+  int32_t st = encode_pool_map("spf_attend", cache, cache->k_pool, T::KEYS, &args.k_map);
+  if (st == SPF_OK) st = encode_pool_map("spf_attend", cache, cache->v_pool, T::KEYS, &args.v_map);
+  if (st == SPF_OK) st = allow_shared_memory(reinterpret_cast<const void*>(attend_step_kernel<D, FP8, R>), smem_bytes<T>(), done);
   if (st != SPF_OK) return st;
   attend_step_kernel<D, FP8, R><<<ctas, T::THREADS, smem_bytes<T>(), stream>>>(args);
   SPF_CUDA_CHECK(cudaGetLastError());
-  return attend_join_launch(args.a, args.parts, R, D, FP8, ctas, stream);
+  return attend_join_launch(args.a, args.parts, R, live, D, FP8, ctas, stream);
 }
 
 template <int D, bool FP8>
-int32_t launch_rows(const StepArgs& args, int rows, int ctas, cudaStream_t stream) {
+int32_t launch_rows(StepArgs& args, const spf_kv_cache* cache, int rows, int live, int ctas, cudaStream_t stream) {
   switch (rows) {
-    case 8: return launch_step<D, FP8, 8>(args, ctas, stream);
-    case 16: return launch_step<D, FP8, 16>(args, ctas, stream);
-    case 32: return launch_step<D, FP8, 32>(args, ctas, stream);
-    default: return launch_step<D, FP8, 64>(args, ctas, stream);
+    case 8: return launch_step<D, FP8, 8>(args, cache, live, ctas, stream);
+    case 16: return launch_step<D, FP8, 16>(args, cache, live, ctas, stream);
+    case 32: return launch_step<D, FP8, 32>(args, cache, live, ctas, stream);
+    default: return launch_step<D, FP8, 64>(args, cache, live, ctas, stream);
   }
 }
 
@@ -760,15 +819,11 @@ size_t attend_step_workspace_bytes(const spf_kv_cache* cache, int group, int max
 int32_t attend_step_launch(const AttendArgs& a, const spf_kv_cache* cache, int max_new, int sm_count, void* workspace, cudaStream_t stream) {
   StepArgs args{};
   args.a = a;
-  const int rows = tile_rows(a.group, max_new), ctas = sm_count * ctas_per_sm(rows);
+  const int rows = tile_rows(a.group, max_new), live = (int)std::min<int64_t>((int64_t)a.group * max_new, rows), ctas = sm_count * ctas_per_sm(rows);
   args.parts = parts_at(workspace, rows, cache->head_dim, ctas);
-  args.min_tiles = 2;
-  int32_t st = encode_pool_map("spf_attend", cache, cache->k_pool, kKeys, &args.k_map);
-  if (st == SPF_OK) st = encode_pool_map("spf_attend", cache, cache->v_pool, kKeys, &args.v_map);
-  if (st != SPF_OK) return st;
-  const bool fp8 = cache->k_scale != nullptr;
-  if (cache->head_dim == 64) return fp8 ? launch_rows<64, true>(args, rows, ctas, stream) : launch_rows<64, false>(args, rows, ctas, stream);
-  return fp8 ? launch_rows<128, true>(args, rows, ctas, stream) : launch_rows<128, false>(args, rows, ctas, stream);
+    const bool fp8 = cache->k_scale != nullptr;
+  if (cache->head_dim == 64) return fp8 ? launch_rows<64, true>(args, cache, rows, live, ctas, stream) : launch_rows<64, false>(args, cache, rows, live, ctas, stream);
+  return fp8 ? launch_rows<128, true>(args, cache, rows, live, ctas, stream) : launch_rows<128, false>(args, cache, rows, live, ctas, stream);
 }
 
 }  // namespace spf
