@@ -228,6 +228,14 @@ __device__ __forceinline__ void copy_tiles(const PromptArgs& args, Smem& sm, uin
   }
 }
 
+struct Ring {
+  int stage;
+  uint32_t parity;
+  __device__ __forceinline__ void advance(int stages) {
+    if (++stage == stages) stage = 0, parity ^= 1u;
+  }
+};
+
 // The next part, nullptr when there is none (or the CTA gives up).
 struct PartReader {
   int n = 0;
@@ -385,10 +393,29 @@ __device__ __forceinline__ void prepare_values(const AttendArgs& a, Smem& sm, un
 }
 
 // ---------------------------------------------------------------------------------------------- products
+// The issuing warp goes through its loop as a whole and one lane's predicate is on the instructions alone: operands then are values
+// that the whole warp shares, which is where the instructions want them.  (One thread in a branch of its own had to bring each of an
+// instruction's six operand registers there: 75 to 115 cycles an instruction that takes the tensor cores 64.)
+//
+// D[128 x N] (+)= A . B^T, both operands in shared memory: 16 bf16, or 32 bytes, of a row.
+template <bool FP8>
+__device__ __forceinline__ void mma_from_smem(uint32_t lane_on, uint32_t d, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+#define SPF_MMA(KIND)                                                                                                                  \
+  asm volatile("{\n.reg .pred p, q;\nsetp.ne.b32 p, %4, 0;\nsetp.ne.b32 q, %5, 0;\n@q tcgen05.mma.cta_group::1.kind::" KIND              \
+               " [%0], %1, %2, %3, p;\n}" ::"r"(d), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(lane_on)                \
+               : "memory")
+  if constexpr (FP8) SPF_MMA("f8f6f4");
+  else SPF_MMA("f16");
+#undef SPF_MMA
+}
 // D[128 x N] (+)= A[128 x 16] . B: A from tensor memory, 16 bits.
-__device__ __forceinline__ void mma_from_tmem(uint32_t d, uint32_t a, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
-  asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(d), "r"(a), "l"(b_desc),
-               "r"(idesc), "r"(accumulate)
+__device__ __forceinline__ void mma_from_tmem(uint32_t lane_on, uint32_t d, uint32_t a, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile("{\n.reg .pred p, q;\nsetp.ne.b32 p, %4, 0;\nsetp.ne.b32 q, %5, 0;\n@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(d),
+               "r"(a), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(lane_on)
+               : "memory");
+}
+__device__ __forceinline__ void commit(uint32_t lane_on, uint32_t bar) {
+  asm volatile("{\n.reg .pred q;\nsetp.ne.b32 q, %1, 0;\n@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}" ::"r"(bar), "r"(lane_on)
                : "memory");
 }
 // Operand whose columns (dimensions) are contiguous: blocks of 64 of them, kKeys rows of 128 bytes each (128-byte swizzle), one
@@ -404,7 +431,7 @@ __device__ __forceinline__ uint64_t value_desc(uint32_t addr) {
 }
 
 template <class T>
-__device__ __forceinline__ void logits(uint32_t s, uint32_t q, uint32_t k) {
+__device__ __forceinline__ void logits(uint32_t lane_on, uint32_t s, uint64_t q, uint64_t k) {
   constexpr uint32_t idesc = instr_desc(128, kKeys, T::FP8);
   if constexpr (T::FP8) {
     // the second term's format is E5M2
@@ -412,78 +439,86 @@ __device__ __forceinline__ void logits(uint32_t s, uint32_t q, uint32_t k) {
     for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int ks = 0; ks < T::SPAN / 32; ++ks)
-        tc_mma<true, false>(s, smem_desc<T::SPAN>(q + t * (128 * T::D)) + 2u * ks, smem_desc<T::SPAN>(k) + 2u * ks, t == 0 ? idesc : idesc | (1u << 7),
+        mma_from_smem<true>(lane_on, s, q + (uint32_t)(t * (128 * T::D >> 4) + 2 * ks), k + 2u * ks, t == 0 ? idesc : idesc | (1u << 7),
                             (uint32_t)((t | ks) != 0));
   } else {
 #pragma unroll
-    for (int b = 0; b < T::D / 64; ++b)
-#pragma unroll
-      for (int ks = 0; ks < 4; ++ks)
-        tc_mma<false, false>(s, smem_desc<T::SPAN>(q + b * (128 * 128)) + 2u * ks, smem_desc<T::SPAN>(k + b * (kKeys * 128)) + 2u * ks, idesc,
-                             (uint32_t)((b | ks) != 0));
+    for (int i = 0; i < T::D / 16; ++i) {
+      const uint32_t at = (uint32_t)((i >> 2) * (128 * 128 >> 4) + 2 * (i & 3));
+      mma_from_smem<false>(lane_on, s, q + at, k + at, idesc, (uint32_t)(i != 0));
+    }
   }
 }
 template <class T>
-__device__ __forceinline__ void weigh(uint32_t o, uint32_t p, uint32_t v, bool first) {
+__device__ __forceinline__ void weigh(uint32_t lane_on, uint32_t o, uint32_t p, uint64_t v, uint32_t accumulate) {
   constexpr uint32_t type = T::FP8 ? 0u : 1u;            // fp16 or bf16; the right operand's columns are contiguous (bit 16)
   constexpr uint32_t idesc = (1u << 4) | (type << 7) | (type << 10) | (1u << 16) | ((uint32_t)(T::D >> 3) << 17) | (8u << 24);
 #pragma unroll
-  for (int ks = 0; ks < kKeys / 16; ++ks) mma_from_tmem(o, p + 8 * ks, value_desc(v + ks * 2048), idesc, (uint32_t)(!first || ks != 0));
+  for (int ks = 0; ks < kKeys / 16; ++ks)
+    mma_from_tmem(lane_on, o, p + 8 * ks, v + (uint32_t)(ks * (2048 >> 4)), idesc, ks == 0 ? accumulate : 1u);
 }
 
 template <class T>
 __device__ __forceinline__ void issue_products(Smem& sm, uint32_t tmem, uint32_t q_tiles, uint32_t k_ring, uint32_t v_ring, const Abort& ab) {
+  const uint32_t on = elect_one() ? 1u : 0u;
   int n_parts = 0, with_keys = 0, with_tile[2] = {0, 0};
-  int64_t used = 0, done[2] = {0, 0};
-  bool fine = true;
-  while (fine) {
-    if (!mbar_wait(smem_u32(&sm.part_full[n_parts & 1]), (uint32_t)(n_parts >> 1) & 1u, ab)) break;
+  uint32_t done[2] = {0, 0};
+  Ring now{0, 0}, next{0, 0};                            // stages of tile j and tile j + 1
+  const uint64_t q_desc = smem_desc<T::SPAN>(q_tiles), k_desc = smem_desc<T::SPAN>(k_ring), v_desc = value_desc(v_ring);
+  for (;;) {
+    if (!mbar_wait_warp(smem_u32(&sm.part_full[n_parts & 1]), (uint32_t)(n_parts >> 1) & 1u, ab)) break;
     const Part& p = sm.part[n_parts & 1];
     if (p.live <= 0) break;
     const int n = p.n_tiles, tiles = p.live > 128 ? 2 : 1;
     if (n > 0) {
-      fine = mbar_wait(smem_u32(&sm.q_ready), (uint32_t)with_keys & 1u, ab);
+      if (!mbar_wait_warp(smem_u32(&sm.q_ready), (uint32_t)with_keys & 1u, ab)) break;
       ++with_keys;
+      bool fine = true;
+#pragma unroll 1
       for (int j = -1; fine && j < n; ++j) {
         // tile j's weights times values, then the logits of tile j + 1, for one row tile after the other
-        const int stage = (int)((used + j) % T::STAGES), next = (int)((used + j + 1) % T::STAGES);
-        for (int x = 0; fine && x < tiles; ++x) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          if (x == tiles || !fine) break;
           const uint32_t s = tmem + 128 * x, o = tmem + 256 + 128 * x;
           if (j >= 0) {
-            fine = mbar_wait(smem_u32(&sm.p_ready[x]), (uint32_t)done[x] & 1u, ab);
-            if (fine && x == 0) fine = mbar_wait(smem_u32(&sm.v_ready[stage]), (uint32_t)((used + j) / T::STAGES) & 1u, ab);
-            if (fine && j == 0 && with_tile[x] > 0) fine = mbar_wait(smem_u32(&sm.o_free[x]), (uint32_t)(with_tile[x] - 1) & 1u, ab);
+            if (x == 0) fine = mbar_wait_warp(smem_u32(&sm.v_ready[now.stage]), now.parity, ab);
+            if (fine && j == 0 && with_tile[x] > 0) fine = mbar_wait_warp(smem_u32(&sm.o_free[x]), (uint32_t)(with_tile[x] - 1) & 1u, ab);
+            if (fine) fine = mbar_wait_warp(smem_u32(&sm.p_ready[x]), done[x] & 1u, ab);
             if (!fine) break;
             tc_fence_after();
-            weigh<T>(o, s, v_ring + stage * T::VTILE, j == 0);
-            tc_commit(smem_u32(&sm.o_done[x]));
+            weigh<T>(on, o, s, v_desc + (uint32_t)(now.stage * (T::VTILE >> 4)), j == 0 ? 0u : 1u);
+            commit(on, smem_u32(&sm.o_done[x]));
             ++done[x];
-            if (x == tiles - 1) tc_commit(smem_u32(&sm.v_empty[stage]));
+            if (x == tiles - 1) commit(on, smem_u32(&sm.v_empty[now.stage]));
           }
           if (j + 1 < n) {
-            if (x == 0) fine = mbar_wait(smem_u32(&sm.k_full[next]), (uint32_t)((used + j + 1) / T::STAGES) & 1u, ab);
+            if (x == 0) fine = mbar_wait_warp(smem_u32(&sm.k_full[next.stage]), next.parity, ab);
             // its columns hold the weights that the product before reads
-            if (fine && done[x] > 0) fine = mbar_wait(smem_u32(&sm.o_done[x]), (uint32_t)(done[x] - 1) & 1u, ab);
+            if (fine && done[x] > 0) fine = mbar_wait_warp(smem_u32(&sm.o_done[x]), (done[x] - 1) & 1u, ab);
             if (!fine) break;
             tc_fence_after();
-            logits<T>(s, q_tiles + x * T::QTILE, k_ring + next * T::KTILE);
-            tc_commit(smem_u32(&sm.s_full[x]));
-            mbar_arrive(smem_u32(&sm.s_full[x]));        // hands on what this thread has seen: the tile's scales, the rows' factors
+            logits<T>(on, s, q_desc + (uint32_t)(x * (T::QTILE >> 4)), k_desc + (uint32_t)(next.stage * (T::KTILE >> 4)));
+            commit(on, smem_u32(&sm.s_full[x]));
+            if (on) mbar_arrive(smem_u32(&sm.s_full[x]));   // hands on what this warp has seen: the tile's scales, the rows' factors
             if (x == tiles - 1) {
-              tc_commit(smem_u32(&sm.k_empty[next]));
-              if (j + 2 == n) tc_commit(smem_u32(&sm.q_free));
+              commit(on, smem_u32(&sm.k_empty[next.stage]));
+              if (j + 2 == n) commit(on, smem_u32(&sm.q_free));
             }
           }
         }
+        if (j >= 0) now.advance(T::STAGES);
+        if (j + 1 < n) next.advance(T::STAGES);
       }
+      if (!fine) break;
       for (int x = 0; x < tiles; ++x) ++with_tile[x];
-      used += n;
     }
-    mbar_arrive(smem_u32(&sm.part_empty[n_parts & 1]));
+    __syncwarp();
+    if (on) mbar_arrive(smem_u32(&sm.part_empty[n_parts & 1]));
     ++n_parts;
   }
-  tc_commit(smem_u32(&sm.mma_done));
-  mbar_wait(smem_u32(&sm.mma_done), 0u, ab);
+  commit(on, smem_u32(&sm.mma_done));
+  mbar_wait_warp(smem_u32(&sm.mma_done), 0u, ab);
 }
 
 // ---------------------------------------------------------------------------------------------- softmax and output
@@ -714,7 +749,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
     if (warp < 8) softmax_rows<T>(args, sm, tmem, ab);
     else if (warp < 12) prepare_values<T>(args.a, sm, q_tiles, v8_ring, v_ring, ab);
     else if (warp == 12) copy_tiles<T>(args, sm, smem_u32(k_ring), smem_u32(FP8 ? v8_ring : v_ring), w0, w1, per, ab);
-    else if (warp == 13 && (threadIdx.x & 31) == 0) issue_products<T>(sm, tmem, smem_u32(q_tiles), smem_u32(k_ring), smem_u32(v_ring), ab);
+    else if (warp == 13) issue_products<T>(sm, tmem, smem_u32(q_tiles), smem_u32(k_ring), smem_u32(v_ring), ab);
   }
   tc_fence_before();
   __syncthreads();
