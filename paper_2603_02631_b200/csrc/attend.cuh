@@ -73,6 +73,7 @@ int32_t encode_pool_map(const char* who, const spf_kv_cache* cache, void* pool, 
 
 // ---------------------------------------------------------------------------------------------- what both kernels compute with
 constexpr float kLazy = 8.f;            // how far logits may exceed their reference
+constexpr float kNoReference = -1.5e38f;   // of a row that has seen no key: finite, so that no difference of two is NaN
 constexpr float kShift = 7.f;           // 8-bit values: weights reach 2^(kLazy + kShift) = 2^15, below fp16's 65504
 
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {

@@ -28,7 +28,7 @@ namespace spf {
 namespace {
 
 constexpr int kRows = 256, kKeys = 128, kThreads = 512;
-constexpr int kSoftmaxRegs = 176, kOtherRegs = 72;    // of 128 a thread at launch: 256 x (176 + 72) <= 512 x 128
+constexpr int kSoftmaxRegs = 184, kOtherRegs = 72;    // of 128 a thread at launch: 256 x (184 + 72) = 512 x 128
 constexpr int kInfo = 8;                              // tiles' scales kept: more than may be under way between copy and softmax
 constexpr int kNever = 0x7fffffff;
 
@@ -40,6 +40,10 @@ struct Traits {
   static constexpr int QTILE = 128 * D * 2;                                     // bf16, or two 8-bit terms
   static constexpr int KTILE = kKeys * ROWB, V8TILE = FP8 ? kKeys * D : 0, VTILE = kKeys * D * 2;
   static constexpr int STAGES = D == 64 ? 3 : 2;
+  // Tensor memory, 512 columns: S_X 128 each, O_X D each.  With 64 dimensions there is room for P_X (64 each) beside S_X, and the
+  // next keys' logits are made while these are being turned into weights; with 128, P_X lies over S_X.
+  static constexpr bool APART = D == 64;
+  static constexpr uint32_t O_COL = 256, P_COL = APART ? 384 : 0, P_STEP = APART ? 64 : 128;
   static constexpr int BYTES = 2 * QTILE + STAGES * (KTILE + V8TILE + VTILE);
 };
 
@@ -57,7 +61,7 @@ struct TileInfo {
 };
 
 struct Smem {
-  unsigned long long s_full[2], p_ready[2], o_done[2], o_free[2], q_ready, q_free, part_full[2], part_empty[2], values_done[2], mma_done;
+  unsigned long long s_full[2], s_free[2], p_ready[2], o_done[2], o_free[2], q_ready, q_free, part_full[2], part_empty[2], values_done[2], mma_done;
   unsigned long long k_full[3], k_empty[3], v_full[3], v_ready[3], v_empty[3], v8_empty[3];
   TileInfo info[kInfo];
   Part part[2];
@@ -227,14 +231,6 @@ __device__ __forceinline__ void copy_tiles(const PromptArgs& args, Smem& sm, uin
     mbar_arrive(smem_u32(&sm.part_full[slot]));
   }
 }
-
-struct Ring {
-  int stage;
-  uint32_t parity;
-  __device__ __forceinline__ void advance(int stages) {
-    if (++stage == stages) stage = 0, parity ^= 1u;
-  }
-};
 
 // The next part, nullptr when there is none (or the CTA gives up).
 struct PartReader {
@@ -458,66 +454,98 @@ __device__ __forceinline__ void weigh(uint32_t lane_on, uint32_t o, uint32_t p, 
     mma_from_tmem(lane_on, o, p + 8 * ks, v + (uint32_t)(ks * (2048 >> 4)), idesc, ks == 0 ? accumulate : 1u);
 }
 
+// The order of the products.  Where weights lie over logits: per row tile, tile j's values, then tile j + 1's logits; the other row
+// tile's threads are busy meanwhile.  Where they lie apart, each row tile's logits go ahead of the OTHER one's values, which is the
+// order in which what they wait for is there when the two are half a tile apart.  (Asking for whichever can be made, by polling: 631
+// instead of 513 us with 128 dimensions, where each product's start is on the critical path.)
+template <class T>
+struct Products {
+  Smem& sm;
+  const Abort& ab;
+  uint32_t tmem, on;
+  uint64_t q_desc, k_desc, v_desc;
+  uint32_t done[2] = {0, 0}, asked[2] = {0, 0};          // products of either kind
+  int with_tile[2] = {0, 0};
+  uint32_t used = 0;                                     // tiles of the parts before
+  int n = 0, tiles = 0;                                  // of this part
+  bool fine = true;
+
+  __device__ __forceinline__ void wait(unsigned long long* bar, uint32_t parity) { fine = fine && mbar_wait_warp(smem_u32(bar), parity & 1u, ab); }
+
+  __device__ __forceinline__ void ask(int x, int j) {
+    if (j >= n || !fine) return;
+    const uint32_t tile = used + (uint32_t)j, stage = tile % T::STAGES;
+    if (x == 0) wait(&sm.k_full[stage], tile / T::STAGES);
+    // the columns hold logits until they have been read, or the weights that the product before reads
+    if (asked[x] > 0) wait(T::APART ? &sm.s_free[x] : &sm.o_done[x], asked[x] - 1);
+    if (!fine) return;
+    tc_fence_after();
+    logits<T>(on, tmem + 128 * x, q_desc + (uint32_t)(x * (T::QTILE >> 4)), k_desc + stage * (T::KTILE >> 4));
+    commit(on, smem_u32(&sm.s_full[x]));
+    if (on) mbar_arrive(smem_u32(&sm.s_full[x]));         // hands on what this warp has seen: the tile's scales, the rows' factors
+    ++asked[x];
+    if (x == tiles - 1) {
+      commit(on, smem_u32(&sm.k_empty[stage]));
+      if (j + 1 == n) commit(on, smem_u32(&sm.q_free));
+    }
+  }
+  __device__ __forceinline__ void add(int x, int j) {
+    if (j < 0 || j >= n || !fine) return;
+    const uint32_t tile = used + (uint32_t)j, stage = tile % T::STAGES;
+    if (x == 0) wait(&sm.v_ready[stage], tile / T::STAGES);
+    if (j == 0 && with_tile[x] > 0) wait(&sm.o_free[x], (uint32_t)(with_tile[x] - 1));
+    wait(&sm.p_ready[x], done[x]);
+    if (!fine) return;
+    tc_fence_after();
+    weigh<T>(on, tmem + T::O_COL + T::D * x, tmem + T::P_COL + T::P_STEP * x, v_desc + stage * (T::VTILE >> 4), j > 0 ? 1u : 0u);
+    commit(on, smem_u32(&sm.o_done[x]));
+    ++done[x];
+    if (x == tiles - 1) commit(on, smem_u32(&sm.v_empty[stage]));
+  }
+};
+
 template <class T>
 __device__ __forceinline__ void issue_products(Smem& sm, uint32_t tmem, uint32_t q_tiles, uint32_t k_ring, uint32_t v_ring, const Abort& ab) {
-  const uint32_t on = elect_one() ? 1u : 0u;
-  int n_parts = 0, with_keys = 0, with_tile[2] = {0, 0};
-  uint32_t done[2] = {0, 0};
-  Ring now{0, 0}, next{0, 0};                            // stages of tile j and tile j + 1
-  const uint64_t q_desc = smem_desc<T::SPAN>(q_tiles), k_desc = smem_desc<T::SPAN>(k_ring), v_desc = value_desc(v_ring);
+  Products<T> p{sm, ab, tmem, elect_one() ? 1u : 0u, smem_desc<T::SPAN>(q_tiles), smem_desc<T::SPAN>(k_ring), value_desc(v_ring)};
+  int n_parts = 0, with_keys = 0;
   for (;;) {
-    if (!mbar_wait_warp(smem_u32(&sm.part_full[n_parts & 1]), (uint32_t)(n_parts >> 1) & 1u, ab)) break;
-    const Part& p = sm.part[n_parts & 1];
-    if (p.live <= 0) break;
-    const int n = p.n_tiles, tiles = p.live > 128 ? 2 : 1;
-    if (n > 0) {
-      if (!mbar_wait_warp(smem_u32(&sm.q_ready), (uint32_t)with_keys & 1u, ab)) break;
+    p.wait(&sm.part_full[n_parts & 1], (uint32_t)(n_parts >> 1));
+    if (!p.fine || sm.part[n_parts & 1].live <= 0) break;
+    p.n = sm.part[n_parts & 1].n_tiles;
+    p.tiles = sm.part[n_parts & 1].live > 128 ? 2 : 1;
+    if (p.n > 0) {
+      p.wait(&sm.q_ready, (uint32_t)with_keys);
       ++with_keys;
-      bool fine = true;
+      if (!T::APART) {
 #pragma unroll 1
-      for (int j = -1; fine && j < n; ++j) {
-        // tile j's weights times values, then the logits of tile j + 1, for one row tile after the other
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          if (x == tiles || !fine) break;
-          const uint32_t s = tmem + 128 * x, o = tmem + 256 + 128 * x;
-          if (j >= 0) {
-            if (x == 0) fine = mbar_wait_warp(smem_u32(&sm.v_ready[now.stage]), now.parity, ab);
-            if (fine && j == 0 && with_tile[x] > 0) fine = mbar_wait_warp(smem_u32(&sm.o_free[x]), (uint32_t)(with_tile[x] - 1) & 1u, ab);
-            if (fine) fine = mbar_wait_warp(smem_u32(&sm.p_ready[x]), done[x] & 1u, ab);
-            if (!fine) break;
-            tc_fence_after();
-            weigh<T>(on, o, s, v_desc + (uint32_t)(now.stage * (T::VTILE >> 4)), j == 0 ? 0u : 1u);
-            commit(on, smem_u32(&sm.o_done[x]));
-            ++done[x];
-            if (x == tiles - 1) commit(on, smem_u32(&sm.v_empty[now.stage]));
-          }
-          if (j + 1 < n) {
-            if (x == 0) fine = mbar_wait_warp(smem_u32(&sm.k_full[next.stage]), next.parity, ab);
-            // its columns hold the weights that the product before reads
-            if (fine && done[x] > 0) fine = mbar_wait_warp(smem_u32(&sm.o_done[x]), (done[x] - 1) & 1u, ab);
-            if (!fine) break;
-            tc_fence_after();
-            logits<T>(on, s, q_desc + (uint32_t)(x * (T::QTILE >> 4)), k_desc + (uint32_t)(next.stage * (T::KTILE >> 4)));
-            commit(on, smem_u32(&sm.s_full[x]));
-            if (on) mbar_arrive(smem_u32(&sm.s_full[x]));   // hands on what this warp has seen: the tile's scales, the rows' factors
-            if (x == tiles - 1) {
-              commit(on, smem_u32(&sm.k_empty[next.stage]));
-              if (j + 2 == n) commit(on, smem_u32(&sm.q_free));
-            }
+        for (int j = -1; p.fine && j < p.n; ++j) {
+          p.add(0, j);
+          p.ask(0, j + 1);
+          if (p.tiles == 2) {
+            p.add(1, j);
+            p.ask(1, j + 1);
           }
         }
-        if (j >= 0) now.advance(T::STAGES);
-        if (j + 1 < n) next.advance(T::STAGES);
+      } else {
+#pragma unroll 1
+        for (int j = -1; p.fine && j <= p.n; ++j) {
+          p.ask(0, j + 1);
+          if (p.tiles == 2) {
+            p.add(1, j - 1);
+            p.ask(1, j + 1);
+          }
+          p.add(0, j);
+        }
       }
-      if (!fine) break;
-      for (int x = 0; x < tiles; ++x) ++with_tile[x];
+      for (int x = 0; x < p.tiles; ++x) ++p.with_tile[x];
+      p.used += (uint32_t)p.n;
+      if (!p.fine) break;
     }
     __syncwarp();
-    if (on) mbar_arrive(smem_u32(&sm.part_empty[n_parts & 1]));
+    if (p.on) mbar_arrive(smem_u32(&sm.part_empty[n_parts & 1]));
     ++n_parts;
   }
-  commit(on, smem_u32(&sm.mma_done));
+  commit(p.on, smem_u32(&sm.mma_done));
   mbar_wait_warp(smem_u32(&sm.mma_done), 0u, ab);
 }
 
@@ -577,7 +605,8 @@ __device__ __forceinline__ void softmax_rows(const PromptArgs& args, Smem& sm, u
   constexpr int D = T::D;
   const AttendArgs& a = args.a;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, x = warp >> 2;
-  const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, s_addr = tmem + 128 * x + lanes, o_addr = tmem + 256 + 128 * x + lanes;
+  const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, s_addr = tmem + 128 * x + lanes, o_addr = tmem + T::O_COL + D * x + lanes,
+                 p_addr = tmem + T::P_COL + T::P_STEP * x + lanes;
   const int r = x * 128 + (warp & 3) * 32 + lane;        // the thread's row of the part
   PartReader reader;
   int64_t seen = 0;                                      // tiles of this row tile
@@ -586,7 +615,7 @@ __device__ __forceinline__ void softmax_rows(const PromptArgs& args, Smem& sm, u
     const Part& p = *pp;
     const bool mine = x * 128 < p.live;
     const int n = p.n_tiles;
-    float m = -INFINITY, l = 0.f;
+    float m = kNoReference, l = 0.f;
     if (mine && n > 0) {
       const int token = (int)(((int64_t)p.row_tile * kRows + r) / a.group);
       const int hi = a.causal ? min(p.end, p.pos0 + token + 1) : p.end, first = p.first;
@@ -619,7 +648,13 @@ __device__ __forceinline__ void softmax_rows(const PromptArgs& args, Smem& sm, u
             for (int i = 0; i < 32; ++i)
               if (32 * c + i < lo_i || 32 * c + i >= hi_i) s[c][i] = 0xff800000u;
         }
-        // the row's largest logit (scales are positive)
+        if constexpr (T::APART) {
+          tc_fence_before();                             // the logits are in registers
+          __syncwarp();
+          if (lane == 0) mbar_arrive(smem_u32(&sm.s_free[x]));
+        }
+        // the row's largest logit (scales are positive); on the way through the exponentials below it would cost registers that
+        // are not there (554 instead of 513 us)
         float top = -INFINITY;
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
@@ -631,12 +666,17 @@ __device__ __forceinline__ void softmax_rows(const PromptArgs& args, Smem& sm, u
               t[(i >> 1) & 3] = max3(t[(i >> 1) & 3], __uint_as_float(s[2 * g + c][i]), __uint_as_float(s[2 * g + c][i + 1]));
           top = fmaxf(top, fmaf(fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])), f[g], add[g]));
         }
+        if constexpr (T::APART) {
+          // the weights go where the product with the tile before may still read
+          if (seen > 0 && !mbar_wait_warp(smem_u32(&sm.o_done[x]), (uint32_t)(seen - 1) & 1u, ab)) return;
+          tc_fence_after();
+        }
         if (__any_sync(0xffffffffu, top > m + kLazy)) {
-          const float now = fmaxf(m, top), scale = now == m ? 1.f : fast_exp2(m - now);
+          const float now = fmaxf(m, top), scale = fast_exp2(m - now);
           m = now;
           l *= scale;
           if (j > 0) {
-            // the product with the tile before is done: it was waited for before these logits' product
+            // the product with the tile before is done: it was waited for above, or before these logits' product
 #pragma unroll 1
             for (int c = 0; c < D; c += 16) {
               uint32_t o[16];
@@ -647,10 +687,9 @@ __device__ __forceinline__ void softmax_rows(const PromptArgs& args, Smem& sm, u
               for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * scale);
               tmem_store<16>(o_addr + c, o);
             }
-            tmem_store_wait();
           }
         }
-        const float ref = (m == -INFINITY ? 0.f : m) - (T::FP8 ? kShift : 0.f);
+        const float ref = m - (T::FP8 ? kShift : 0.f);
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
           const uint64_t ff = pack2(f[g], f[g]), off = pack2(add[g] - ref, add[g] - ref);
@@ -667,7 +706,7 @@ __device__ __forceinline__ void softmax_rows(const PromptArgs& args, Smem& sm, u
               sum[c] = add2(sum[c], pack2(u, v));
               w[16 * c + (i >> 1)] = T::FP8 ? pack_f16(u, v) : pack_bf16(u, v);
             }
-          tmem_store<32>(s_addr + 32 * g, w);
+          tmem_store<32>(p_addr + 32 * g, w);
           float u, v;
           unpack2(add2(sum[0], sum[1]), u, v);
           l = T::FP8 ? fmaf(u + v, inverse[g], l) : l + (u + v);
@@ -710,6 +749,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
   if (threadIdx.x == 0) {
     for (int i = 0; i < 2; ++i) {
       mbar_init(smem_u32(&sm.s_full[i]), 2);
+      mbar_init(smem_u32(&sm.s_free[i]), 4);
       mbar_init(smem_u32(&sm.p_ready[i]), 4);
       mbar_init(smem_u32(&sm.o_done[i]), 1);
       mbar_init(smem_u32(&sm.o_free[i]), 4);

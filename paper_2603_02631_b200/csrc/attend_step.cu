@@ -44,7 +44,6 @@ constexpr int kWarps = 4;               // that compute
 // 128 x (192 + 64) = 256 x 128.
 constexpr int kComputeRegs = 192, kOtherRegs = 64;
 constexpr int kMaxStages = 8;
-constexpr float kNoReference = -1.5e38f;   // of a row that has seen no key: finite, so that no difference of two is NaN
 
 
 // What the copying warp tells the computing ones about a stage.
