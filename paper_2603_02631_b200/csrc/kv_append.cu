@@ -15,11 +15,12 @@
 #include <cuda_fp16.h>
 
 #include "kv.cuh"
+#include "tc_ptx.cuh"
 
 namespace spf {
 namespace {
 
-constexpr int kAppendThreads = 128;
+constexpr int kAppendThreads = 256;
 
 struct AppendArgs {
   KvView kv;
@@ -88,6 +89,17 @@ __device__ __forceinline__ void turn(float& x, float& y, float c, float s) {
   y = __fadd_rn(__fmul_rn(y, c), __fmul_rn(x, s));
   x = nx;
 }
+// Two at once, with the same roundings.
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ void turn2(float* x, float* y, const float* c, const float* s) {
+  const uint64_t xx = pack2(x[0], x[1]), yy = pack2(y[0], y[1]), cc = pack2(c[0], c[1]), ss = pack2(s[0], s[1]);
+  unpack2(fma2(mul2(yy, ss), pack2(-1.f, -1.f), mul2(xx, cc)), x[0], x[1]);
+  unpack2(add2(mul2(yy, cc), mul2(xx, ss)), y[0], y[1]);
+}
 __device__ __forceinline__ void rotate(float (&a)[8], float (&b)[8], const Angles& t, int interleaved) {
   if (interleaved) {
 #pragma unroll
@@ -97,7 +109,7 @@ __device__ __forceinline__ void rotate(float (&a)[8], float (&b)[8], const Angle
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) turn(a[i], b[i], t.c[i], t.s[i]);
+    for (int i = 0; i < 8; i += 2) turn2(a + i, b + i, t.c + i, t.s + i);
   }
 }
 
@@ -210,23 +222,37 @@ __device__ __forceinline__ float2 e4m3_pair_value(uint32_t two) {
   return __half22float2(*reinterpret_cast<const __half2*>(&h2));
 }
 
-// x / scale: a product where the scale is a power of two (as every scale that this kernel makes), which is the same value.
-struct Divider {
-  float scale, inverse;
-  bool exact;
-  __device__ __forceinline__ float operator()(float x) const { return exact ? x * inverse : __fdiv_rn(x, scale); }
-};
-
-__device__ __forceinline__ uint2 bytes8(const float (&x)[8], const Divider& by) {
+__device__ __forceinline__ uint2 bytes8(const float (&x)[8], float inverse) {
   uint2 r;
-  r.x = e4m3_pair(by(x[0]), by(x[1])) | (e4m3_pair(by(x[2]), by(x[3])) << 16);
-  r.y = e4m3_pair(by(x[4]), by(x[5])) | (e4m3_pair(by(x[6]), by(x[7])) << 16);
+  r.x = e4m3_pair(x[0] * inverse, x[1] * inverse) | (e4m3_pair(x[2] * inverse, x[3] * inverse) << 16);
+  r.y = e4m3_pair(x[4] * inverse, x[5] * inverse) | (e4m3_pair(x[6] * inverse, x[7] * inverse) << 16);
   return r;
 }
 
 __device__ __forceinline__ float finite_magnitude(float x) {
   const float m = fabsf(x);
   return m <= 3.402823466e38f ? m : 0.f;            // neither infinities nor NaN set a scale
+}
+// Largest of `top` and the magnitudes, those that are not finite apart if FINITE (else NaN only).
+template <bool FINITE>
+__device__ __forceinline__ float largest(const float (&x)[2][8], float top) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int e = 0; e < 8; e += 2)
+      top = FINITE ? fmaxf(top, fmaxf(finite_magnitude(x[h][e]), finite_magnitude(x[h][e + 1]))) : max3(top, fabsf(x[h][e]), fabsf(x[h][e + 1]));
+  return top;
+}
+// The largest of all threads' values.
+__device__ __forceinline__ float largest_of_cta(float top, float* warp_max) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+  __syncthreads();                                  // of values of another call, and of what was read before it
+  if ((threadIdx.x & 31) == 0) warp_max[threadIdx.x >> 5] = top;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kAppendThreads / 32; ++w) top = fmaxf(top, warp_max[w]);
+  return top;
 }
 
 // One group of 64 tokens (of a sequence, in a pool block), one head, keys or values.  Group slots of the grid: sequence b owns
@@ -291,20 +317,32 @@ __device__ __forceinline__ void fill_group(const AppendArgs& a) {
       load_angles(a.rope, angle_row, a.rot_dim, u.angle, t);
       rotate(x[i][0], x[i][1], t, a.interleaved);
     }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) top = fmaxf(top, fmaxf(finite_magnitude(x[i][0][e]), finite_magnitude(x[i][1][e])));
+    top = largest<false>(x[i], top);
   }
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-  if ((threadIdx.x & 31) == 0) warp_max[threadIdx.x >> 5] = top;
   const bool partly = lo > first;                   // the group holds tokens from before the step
-  const float held = partly ? *scale_at : 0.f;
-  __syncthreads();                                  // every thread has the old scale before one of them writes the new one
+  const float held = partly ? *scale_at : 0.f;      // every thread has it before one of them writes the new one: barriers follow
+  top = largest_of_cta(top, warp_max);
+  if (!(top <= 3.402823466e38f)) {
+    top = 0.f;                                      // some are infinite: once more without them
 #pragma unroll
-  for (int w = 0; w < kAppendThreads / 32; ++w) top = fmaxf(top, warp_max[w]);
+    for (int i = 0; i < kPer; ++i)
+      if (live[i]) top = largest<true>(x[i], top);
+    top = largest_of_cta(top, warp_max);
+  }
   const float scale = fmaxf(held, scale_for(top));
   if (threadIdx.x == 0 && scale != held) *scale_at = scale;
-  const Divider by{scale, 1.f / scale, (__float_as_uint(scale) & 0x7fffffu) == 0};
+  // x / scale is a product where the scale is a power of two, as every scale that this kernel makes; else the quotients are made here
+  float inverse = 1.f / scale;
+  if ((__float_as_uint(scale) & 0x7fffffu) != 0) {
+#pragma unroll 1
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int i = 0; i < kPer; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (live[i]) (h == 0 ? x[i][0][e] : x[i][1][e]) = __fdiv_rn(h == 0 ? x[i][0][e] : x[i][1][e], scale);
+    inverse = 1.f;
+  }
   if (partly && scale != held) {
     const float ratio = __fdiv_rn(held, scale);
     for (int i = threadIdx.x; i < (lo - first) * (D / 16); i += kAppendThreads) {
@@ -325,13 +363,13 @@ __device__ __forceinline__ void fill_group(const AppendArgs& a) {
     const int item = i * kAppendThreads + threadIdx.x;
     const Unit u = unit_of(item % kUnits, rot_dim, a.interleaved);
     uint8_t* dst = cells + (item / kUnits) * D;
-    *reinterpret_cast<uint2*>(dst + u.first) = bytes8(x[i][0], by);
-    *reinterpret_cast<uint2*>(dst + u.second) = bytes8(x[i][1], by);
+    *reinterpret_cast<uint2*>(dst + u.first) = bytes8(x[i][0], inverse);
+    *reinterpret_cast<uint2*>(dst + u.second) = bytes8(x[i][1], inverse);
   }
 }
 
 template <int D, int HPT, bool FP8>
-__global__ void __launch_bounds__(kAppendThreads) append_kernel(const __grid_constant__ AppendArgs a) {
+__global__ void __launch_bounds__(kAppendThreads, 4) append_kernel(const __grid_constant__ AppendArgs a) {
   if (FP8 && (int)blockIdx.x >= a.rotate_ctas) fill_group<D>(a);
   else move_rows<D, HPT, FP8>(a);
 }
@@ -339,17 +377,17 @@ __global__ void __launch_bounds__(kAppendThreads) append_kernel(const __grid_con
 template <int D, bool FP8>
 int32_t launch_append(AppendArgs& a, cudaStream_t stream) {
   const int turned = a.n_q_heads + (FP8 ? 0 : a.kv.n_kv_heads), copied = FP8 ? 0 : a.kv.n_kv_heads;
-  // one head a thread while that does not fill the chip, four where it does: a row's angles are then read once for four heads
+  // one head a thread while that does not fill the chip, two where it does: a row's angles are then read once for two heads
   const int64_t items1 = (int64_t)a.step.n_rows * (turned + copied) * (D / 16);
   const bool many = items1 > 148 * 2048;
-  const int hpt = many ? 4 : 1;
+  const int hpt = many ? 2 : 1;
   const int64_t items = (int64_t)a.step.n_rows * (ceil_div(turned, hpt) + ceil_div(copied, hpt)) * (D / 16);
   const int64_t rotate = ceil_div(items, kAppendThreads);
   const int64_t groups = FP8 ? (a.step.n_rows / kScaleTokens + 2 * (int64_t)a.step.n_seqs) * 2 * a.kv.n_kv_heads : 0;
   if (rotate + groups > 0x7fffffffLL) return fail(SPF_ERR_UNSUPPORTED, "spf_kv_append: too many rows for one launch");
   if (rotate + groups == 0) return SPF_OK;
   a.rotate_ctas = (int)rotate;
-  if (many) append_kernel<D, 4, FP8><<<(unsigned)(rotate + groups), kAppendThreads, 0, stream>>>(a);
+  if (many) append_kernel<D, 2, FP8><<<(unsigned)(rotate + groups), kAppendThreads, 0, stream>>>(a);
   else append_kernel<D, 1, FP8><<<(unsigned)(rotate + groups), kAppendThreads, 0, stream>>>(a);
   SPF_CUDA_CHECK(cudaGetLastError());
   return SPF_OK;
