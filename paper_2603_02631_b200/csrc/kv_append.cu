@@ -21,6 +21,7 @@ namespace spf {
 namespace {
 
 constexpr int kAppendThreads = 256;
+constexpr int kManyJobs = 4;
 
 struct AppendArgs {
   KvView kv;
@@ -31,6 +32,7 @@ struct AppendArgs {
   int n_positions, rot_dim, interleaved;
   int n_q_heads;                // 0: no queries in this call
   int rotate_ctas;              // CTAs that move whole rows; behind them, those that fill 8-bit groups
+  uint64_t per_row_inverse;     // 2^64 / (threads of a row), rounded up
   int32_t* dev_status;
 };
 
@@ -132,15 +134,18 @@ __device__ __forceinline__ void move_rows(const AppendArgs& a) {
   const int turned_groups = (turned + HPT - 1) / HPT, groups = turned_groups + (copied + HPT - 1) / HPT;
   const int per_row = groups * kUnits;
   const int64_t first = (int64_t)blockIdx.x * kAppendThreads, item = first + threadIdx.x;
+  // n / per_row = high word of n ceil(2^64 / per_row) while n per_row < 2^64 (here below 2^39 and 2^20): a 64-bit division by a
+  // value that is not known when this is compiled takes some hundred instructions, more than everything else here
+  auto row_of = [&](int64_t n) { return (int)__umul64hi((uint64_t)n, a.per_row_inverse); };
   // the sequences of the CTA's first and last row, by one look of all threads at the starts; a thread's own lies between
-  const int row_lo = (int)(first / per_row), row_hi = (int)min((first + kAppendThreads - 1) / per_row, (int64_t)a.step.n_rows - 1);
+  const int row_lo = row_of(first), row_hi = min(row_of(first + kAppendThreads - 1), a.step.n_rows - 1);
   int lo = 0, hi = 0;
   for (int b = 0; b < a.step.n_seqs; b += kAppendThreads) {
     const int start = b + (int)threadIdx.x < a.step.n_seqs ? __ldg(a.step.row_start + b + threadIdx.x) : 0x7fffffff;
     lo += __syncthreads_count(start <= row_lo);
     hi += __syncthreads_count(start <= row_hi);
   }
-  const int row = (int)(item / per_row);
+  const int row = row_of(item);
   if (row >= a.step.n_rows || row >= __ldg(a.step.row_start + a.step.n_seqs)) return;
   while (lo < hi) {
     const int mid = (lo + hi) >> 1;
@@ -210,10 +215,12 @@ __device__ __forceinline__ float scale_for(float m) {
   return __uint_as_float((uint32_t)(e + 127) << 23);
 }
 
-// Two values as E4M3 bytes, to nearest, clipped at 448 (NaN: 0x7F).
-__device__ __forceinline__ uint32_t e4m3_pair(float lo, float hi) {
-  uint16_t r;
-  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+// Four values as E4M3 bytes, to nearest, clipped at 448 (NaN: 0x7F).
+__device__ __forceinline__ uint32_t e4m3_four(float a, float b, float c, float d) {
+  uint32_t r;
+  asm("{\n.reg .b16 lo, hi;\ncvt.rn.satfinite.e4m3x2.f32 lo, %2, %1;\ncvt.rn.satfinite.e4m3x2.f32 hi, %4, %3;\nmov.b32 %0, {lo, hi};\n}"
+      : "=r"(r)
+      : "f"(a), "f"(b), "f"(c), "f"(d));
   return r;
 }
 __device__ __forceinline__ float2 e4m3_pair_value(uint32_t two) {
@@ -223,10 +230,8 @@ __device__ __forceinline__ float2 e4m3_pair_value(uint32_t two) {
 }
 
 __device__ __forceinline__ uint2 bytes8(const float (&x)[8], float inverse) {
-  uint2 r;
-  r.x = e4m3_pair(x[0] * inverse, x[1] * inverse) | (e4m3_pair(x[2] * inverse, x[3] * inverse) << 16);
-  r.y = e4m3_pair(x[4] * inverse, x[5] * inverse) | (e4m3_pair(x[6] * inverse, x[7] * inverse) << 16);
-  return r;
+  return make_uint2(e4m3_four(x[0] * inverse, x[1] * inverse, x[2] * inverse, x[3] * inverse),
+                    e4m3_four(x[4] * inverse, x[5] * inverse, x[6] * inverse, x[7] * inverse));
 }
 
 __device__ __forceinline__ float finite_magnitude(float x) {
@@ -240,7 +245,7 @@ __device__ __forceinline__ float largest(const float (&x)[2][8], float top) {
   for (int h = 0; h < 2; ++h)
 #pragma unroll
     for (int e = 0; e < 8; e += 2)
-      top = FINITE ? fmaxf(top, fmaxf(finite_magnitude(x[h][e]), finite_magnitude(x[h][e + 1]))) : max3(top, fabsf(x[h][e]), fabsf(x[h][e + 1]));
+      top = FINITE ? fmaxf(top, fmaxf(finite_magnitude(x[h][e]), finite_magnitude(x[h][e + 1]))) : fmaxf(top, fmaxf(fabsf(x[h][e]), fabsf(x[h][e + 1])));
   return top;
 }
 // The largest of all threads' values.
@@ -255,15 +260,16 @@ __device__ __forceinline__ float largest_of_cta(float top, float* warp_max) {
   return top;
 }
 
-// One group of 64 tokens (of a sequence, in a pool block), one head, keys or values.  Group slots of the grid: sequence b owns
-// those from row_start[b] / 64 + 2 b on, which is at least as many as its new tokens can touch (n tokens touch at most
-// n / 64 + 2 groups).
-template <int D>
+// A group of 64 tokens (of a sequence, in a pool block), for `jobs` of its heads' keys and values in turn: while one is made, the
+// next one's rows are on their way.  Group slots of the grid: sequence b owns those from row_start[b] / 64 + 2 b on, which is at
+// least as many as its new tokens can touch (n tokens touch at most n / 64 + 2 groups).
+template <int D, bool MANY>
 __device__ __forceinline__ void fill_group(const AppendArgs& a) {
   constexpr int kUnits = D / 16, kPer = kScaleTokens * kUnits / kAppendThreads;
   __shared__ float warp_max[kAppendThreads / 32];
-  const int index = (int)blockIdx.x - a.rotate_ctas;
-  const int lanes = 2 * a.kv.n_kv_heads, slot = index / lanes, head = (index % lanes) >> 1, is_v = index & 1;
+  constexpr int kJobs = MANY ? kManyJobs : 1;
+  const int lanes = 2 * a.kv.n_kv_heads, pieces = (lanes + kJobs - 1) / kJobs;
+  const int index = (int)blockIdx.x - a.rotate_ctas, slot = index / pieces, job0 = (index - slot * pieces) * kJobs, job1 = min(job0 + kJobs, lanes);
   int count = 0;
   for (int b = 0; b < a.step.n_seqs; b += kAppendThreads) {
     const int at = b + (int)threadIdx.x;
@@ -271,8 +277,8 @@ __device__ __forceinline__ void fill_group(const AppendArgs& a) {
   }
   const int seq = count - 1;
   if (seq < 0) return;
-  const int start = __ldg(a.step.row_start + seq), end = min(__ldg(a.step.row_start + seq + 1), a.step.n_rows), len = __ldg(a.step.seq_lens + seq);
-  const int behind = __ldg(a.step.row_start + seq + 1);
+  const int start = __ldg(a.step.row_start + seq), behind = __ldg(a.step.row_start + seq + 1), len = __ldg(a.step.seq_lens + seq);
+  const int end = min(behind, a.step.n_rows);
   const int old_len = len - (behind - start);        // tokens before the step
   const int group = max(old_len, 0) / kScaleTokens + slot - (start / kScaleTokens + 2 * seq);
   const int first = group * kScaleTokens;           // position of the group's first token
@@ -287,106 +293,136 @@ __device__ __forceinline__ void fill_group(const AppendArgs& a) {
     if (block < 0) return;
   }
   const int off = first % a.kv.block_tokens;
-  const int64_t slab = block * a.kv.n_kv_heads + head;
-  uint8_t* cells = (is_v ? a.kv.v : a.kv.k) + (slab * a.kv.block_tokens + off) * D;
-  float* scale_at = (is_v ? a.kv.v_scale : a.kv.k_scale) + slab * (a.kv.block_tokens / kScaleTokens) + off / kScaleTokens;
-  const RowsView& rows = is_v ? a.v : a.k;
-  const int rot_dim = !is_v && a.rope != nullptr ? a.rot_dim : 0;
 
-  float x[kPer][2][8];
+  // the thread's units: unit threadIdx.x mod units of every (threads / units)-th token
+  const int unit = threadIdx.x % kUnits, token0 = threadIdx.x / kUnits;
+  constexpr int kTokenStep = kAppendThreads / kUnits;
+  const int row0 = start + (first + token0 - old_len);
   bool live[kPer];
-  float top = 0.f;
+  int64_t angle_row[kPer];
 #pragma unroll
   for (int i = 0; i < kPer; ++i) {
-    const int item = i * kAppendThreads + threadIdx.x, pos = first + item / kUnits;
-    const int row = start + (pos - old_len);
+    const int pos = first + token0 + i * kTokenStep;
     live[i] = pos >= lo && pos < hi;
-    if (!live[i]) continue;
-    const Unit u = unit_of(item % kUnits, rot_dim, a.interleaved);
-    const int64_t angle_row = a.positions != nullptr ? __ldg(a.positions + row) : pos;
-    if (a.rope != nullptr && (angle_row < 0 || angle_row >= a.n_positions)) {
-      live[i] = false;
-      report_cache(a.dev_status);
-      continue;
+    angle_row[i] = pos;
+    if (live[i] && a.rope != nullptr) {
+      if (a.positions != nullptr) angle_row[i] = __ldg(a.positions + row0 + i * kTokenStep);
+      if (angle_row[i] < 0 || angle_row[i] >= a.n_positions) {
+        live[i] = false;
+        report_cache(a.dev_status);
+      }
     }
-    const __nv_bfloat16* src = rows.data + row * rows.stride_row + head * rows.stride_head;
-    widen8(load_raw(src + u.first), x[i][0]);
-    widen8(load_raw(src + u.second), x[i][1]);
-    if (u.angle >= 0) {
-      Angles t;
-      load_angles(a.rope, angle_row, a.rot_dim, u.angle, t);
-      rotate(x[i][0], x[i][1], t, a.interleaved);
-    }
-    top = largest<false>(x[i], top);
   }
-  const bool partly = lo > first;                   // the group holds tokens from before the step
-  const float held = partly ? *scale_at : 0.f;      // every thread has it before one of them writes the new one: barriers follow
-  top = largest_of_cta(top, warp_max);
-  if (!(top <= 3.402823466e38f)) {
-    top = 0.f;                                      // some are infinite: once more without them
+  auto fetch = [&](int job, uint4 (&raw)[kPer][2]) {
+    const bool is_v = job >= a.kv.n_kv_heads;
+    const RowsView& rows = is_v ? a.v : a.k;
+    const Unit u = unit_of(unit, !is_v && a.rope != nullptr ? a.rot_dim : 0, a.interleaved);
+    const __nv_bfloat16* src = rows.data + row0 * rows.stride_row + (is_v ? job - a.kv.n_kv_heads : job) * rows.stride_head;
 #pragma unroll
-    for (int i = 0; i < kPer; ++i)
-      if (live[i]) top = largest<true>(x[i], top);
+    for (int i = 0; i < kPer; ++i) {
+      raw[i][0] = raw[i][1] = make_uint4(0, 0, 0, 0);
+      if (live[i]) {
+        raw[i][0] = load_raw(src + i * kTokenStep * rows.stride_row + u.first);
+        raw[i][1] = load_raw(src + i * kTokenStep * rows.stride_row + u.second);
+      }
+    }
+  };
+  uint4 raw[kPer][2];
+  fetch(job0, raw);
+  for (int job = job0; MANY ? job < job1 : job == job0; ++job) {
+    const bool is_v = job >= a.kv.n_kv_heads;
+    const int head = is_v ? job - a.kv.n_kv_heads : job;
+    const int64_t slab = block * a.kv.n_kv_heads + head;
+    uint8_t* cells = (is_v ? a.kv.v : a.kv.k) + (slab * a.kv.block_tokens + off) * D;
+    float* scale_at = (is_v ? a.kv.v_scale : a.kv.k_scale) + slab * (a.kv.block_tokens / kScaleTokens) + off / kScaleTokens;
+    const Unit u = unit_of(unit, !is_v && a.rope != nullptr ? a.rot_dim : 0, a.interleaved);
+    const bool partly = lo > first;                 // the group holds tokens from before the step
+    const float held = partly ? *scale_at : 0.f;    // every thread has it before one of them writes the new one: barriers follow
+    float x[kPer][2][8];
+    float top = 0.f;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      widen8(raw[i][0], x[i][0]);
+      widen8(raw[i][1], x[i][1]);
+    }
+    if (MANY && job + 1 < job1) fetch(job + 1, raw);
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      if (u.angle >= 0 && live[i]) {
+        Angles t;
+        load_angles(a.rope, angle_row[i], a.rot_dim, u.angle, t);
+        rotate(x[i][0], x[i][1], t, a.interleaved);
+      }
+      top = largest<false>(x[i], top);              // rows that are not there are zeros
+    }
     top = largest_of_cta(top, warp_max);
-  }
-  const float scale = fmaxf(held, scale_for(top));
-  if (threadIdx.x == 0 && scale != held) *scale_at = scale;
-  // x / scale is a product where the scale is a power of two, as every scale that this kernel makes; else the quotients are made here
-  float inverse = 1.f / scale;
-  if ((__float_as_uint(scale) & 0x7fffffu) != 0) {
-#pragma unroll 1
-    for (int h = 0; h < 2; ++h)
+    if (!(top <= 3.402823466e38f)) {
+      top = 0.f;                                    // some are infinite: once more without them
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) top = largest<true>(x[i], top);
+      top = largest_of_cta(top, warp_max);
+    }
+    const float scale = fmaxf(held, scale_for(top));
+    if (threadIdx.x == 0 && scale != held) *scale_at = scale;
+    // x / scale is a product where the scale is a power of two, as every scale that this kernel makes; else the quotients are made here
+    float inverse = 1.f / scale;
+    if ((__float_as_uint(scale) & 0x7fffffu) != 0) {
 #pragma unroll
       for (int i = 0; i < kPer; ++i)
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (live[i]) (h == 0 ? x[i][0][e] : x[i][1][e]) = __fdiv_rn(h == 0 ? x[i][0][e] : x[i][1][e], scale);
-    inverse = 1.f;
-  }
-  if (partly && scale != held) {
-    const float ratio = __fdiv_rn(held, scale);
-    for (int i = threadIdx.x; i < (lo - first) * (D / 16); i += kAppendThreads) {
-      uint4* at = reinterpret_cast<uint4*>(cells) + i;
-      uint4 v = *at;
-      uint32_t* w = &v.x;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const float2 p = e4m3_pair_value(w[j] & 0xffffu), r = e4m3_pair_value(w[j] >> 16);
-        w[j] = e4m3_pair(p.x * ratio, p.y * ratio) | (e4m3_pair(r.x * ratio, r.y * ratio) << 16);
-      }
-      *at = v;
+        for (int e = 0; e < 8; ++e) {
+          x[i][0][e] = __fdiv_rn(x[i][0][e], scale);
+          x[i][1][e] = __fdiv_rn(x[i][1][e], scale);
+        }
+      inverse = 1.f;
     }
-  }
+    if (partly && scale != held) {
+      const float ratio = __fdiv_rn(held, scale);
+      for (int i = threadIdx.x; i < (lo - first) * (D / 16); i += kAppendThreads) {
+        uint4* at = reinterpret_cast<uint4*>(cells) + i;
+        uint4 v = *at;
+        uint32_t* w = &v.x;
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) {
-    if (!live[i]) continue;
-    const int item = i * kAppendThreads + threadIdx.x;
-    const Unit u = unit_of(item % kUnits, rot_dim, a.interleaved);
-    uint8_t* dst = cells + (item / kUnits) * D;
-    *reinterpret_cast<uint2*>(dst + u.first) = bytes8(x[i][0], inverse);
-    *reinterpret_cast<uint2*>(dst + u.second) = bytes8(x[i][1], inverse);
+        for (int j = 0; j < 4; ++j) {
+          const float2 p = e4m3_pair_value(w[j] & 0xffffu), r = e4m3_pair_value(w[j] >> 16);
+          w[j] = e4m3_four(p.x * ratio, p.y * ratio, r.x * ratio, r.y * ratio);
+        }
+        *at = v;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      if (!live[i]) continue;
+      uint8_t* dst = cells + (token0 + i * kTokenStep) * D;
+      *reinterpret_cast<uint2*>(dst + u.first) = bytes8(x[i][0], inverse);
+      *reinterpret_cast<uint2*>(dst + u.second) = bytes8(x[i][1], inverse);
+    }
   }
 }
 
 template <int D, int HPT, bool FP8>
-__global__ void __launch_bounds__(kAppendThreads, 4) append_kernel(const __grid_constant__ AppendArgs a) {
-  if (FP8 && (int)blockIdx.x >= a.rotate_ctas) fill_group<D>(a);
+__global__ void __launch_bounds__(kAppendThreads, FP8 ? 3 : 4) append_kernel(const __grid_constant__ AppendArgs a) {
+  if (FP8 && (int)blockIdx.x >= a.rotate_ctas) fill_group<D, (HPT > 1)>(a);
   else move_rows<D, HPT, FP8>(a);
 }
 
 template <int D, bool FP8>
 int32_t launch_append(AppendArgs& a, cudaStream_t stream) {
   const int turned = a.n_q_heads + (FP8 ? 0 : a.kv.n_kv_heads), copied = FP8 ? 0 : a.kv.n_kv_heads;
-  // one head a thread while that does not fill the chip, two where it does: a row's angles are then read once for two heads
-  const int64_t items1 = (int64_t)a.step.n_rows * (turned + copied) * (D / 16);
-  const bool many = items1 > 148 * 2048;
+  // Few rows: a head to a thread, a head's group to a CTA, so that everything is under way at once.  Where that more than fills the
+  // chip: two heads to a thread, which read a row's angles once, and four heads' groups to a CTA, which finds its place once and
+  // fetches the next one's rows while it makes one.
+  const int64_t slots = FP8 ? a.step.n_rows / kScaleTokens + 2 * (int64_t)a.step.n_seqs : 0, lanes = 2 * (int64_t)a.kv.n_kv_heads;
+  const bool many = (int64_t)a.step.n_rows * (a.n_q_heads + lanes) * (D / 16) > 148 * 2048;
   const int hpt = many ? 2 : 1;
   const int64_t items = (int64_t)a.step.n_rows * (ceil_div(turned, hpt) + ceil_div(copied, hpt)) * (D / 16);
-  const int64_t rotate = ceil_div(items, kAppendThreads);
-  const int64_t groups = FP8 ? (a.step.n_rows / kScaleTokens + 2 * (int64_t)a.step.n_seqs) * 2 * a.kv.n_kv_heads : 0;
+  const int64_t rotate = ceil_div(items, kAppendThreads), groups = slots * ceil_div(lanes, many ? kManyJobs : 1);
   if (rotate + groups > 0x7fffffffLL) return fail(SPF_ERR_UNSUPPORTED, "spf_kv_append: too many rows for one launch");
   if (rotate + groups == 0) return SPF_OK;
   a.rotate_ctas = (int)rotate;
+  const int64_t per_row = (ceil_div(turned, hpt) + ceil_div(copied, hpt)) * (D / 16);
+  if (per_row >= (1 << 20)) return fail(SPF_ERR_UNSUPPORTED, "spf_kv_append: too many heads");
+  a.per_row_inverse = per_row > 0 ? ~0ull / (uint64_t)per_row + 1 : 0;
   if (many) append_kernel<D, 2, FP8><<<(unsigned)(rotate + groups), kAppendThreads, 0, stream>>>(a);
   else append_kernel<D, 1, FP8><<<(unsigned)(rotate + groups), kAppendThreads, 0, stream>>>(a);
   SPF_CUDA_CHECK(cudaGetLastError());
