@@ -89,7 +89,6 @@ int32_t launch_rows(const AttendArgs& a, const AttendParts& parts, int rows, int
     case 8: return launch<D, FP8, 8>(a, parts, live, ctas, stream);
     case 16: return launch<D, FP8, 16>(a, parts, live, ctas, stream);
     case 32: return launch<D, FP8, 32>(a, parts, live, ctas, stream);
-    case 64: return launch<D, FP8, 64>(a, parts, live, ctas, stream);
     default: return launch<D, FP8, 256>(a, parts, live, ctas, stream);
   }
 }

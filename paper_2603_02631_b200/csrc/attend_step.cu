@@ -40,8 +40,7 @@ namespace spf {
 namespace {
 
 constexpr int kWarps = 4;               // that compute
-// From 16 rows on a second warpgroup, whose first warp copies, lends registers of the 128 a thread that the launch has,
-// 128 x (192 + 64) = 256 x 128.
+// A second warpgroup, whose first warp copies, lends registers of the 128 a thread that the launch has: 128 x (192 + 64) = 256 x 128.
 constexpr int kComputeRegs = 192, kOtherRegs = 64;
 constexpr int kMaxStages = 8;
 
@@ -58,18 +57,19 @@ template <int D_, bool FP8_, int R_>
 struct Traits {
   static constexpr int D = D_, R = R_;
   static constexpr bool FP8 = FP8_;
-  // warps over rows (16 rows of 128 dimensions, 32 of 64, are 64 registers of outputs), and over keys
-  static constexpr int WR = R * D <= 2048 ? 1 : R * D / 2048, WK = kWarps / WR;
+  // Warps over rows and over keys: a warp's outputs are 32 registers (8 rows of 128 dimensions, 16 of 64).  With 64 of them, 32 rows
+  // of 64 dimensions took 69 instead of 61 us (131072 keys, 8 heads), though each key is then read by half as many warps.
+  static constexpr int WR = R * D <= 1024 ? 1 : R * D / 1024, WK = kWarps / WR;
   static constexpr int NT = R / (8 * WR);                             // 8-row tiles of a warp
   // Keys of a tile: 128 where their rows are short, so that a warp has two sixteens of them at a time.  (One sixteen is a chain of
   // dependent steps: with tiles of 64 keys 32 sequences of up to 16k tokens on an 8-bit cache took 136 instead of 111 us, four of up to
   // 250k 384 instead of 292, eight lookahead tokens over 131072 keys of 64 dimensions 92 instead of 70.)  A warp's keys share a scale, so they are 64 at most.
   static constexpr int KEYS = (FP8 ? D : 2 * D) <= 128 && WK > 1 ? 128 : 64;
   static constexpr int KW = KEYS / WK, KT = KW / 16;                  // keys of a warp in a tile, in sixteens
-  static constexpr bool LEND = R >= 16;                               // registers move between warpgroups
+  static constexpr bool LEND = R >= 16 && R * D < 4096;               // registers move between warpgroups
   static constexpr int THREADS = LEND ? 2 * kWarps * 32 : (kWarps + 1) * 32;
   static constexpr int CTAS = R == 8 ? 3 : 2;                         // per SM
-  static constexpr bool QREGS = R <= 16;                              // queries stay in registers
+  static constexpr bool QREGS = NT <= 2;                              // queries stay in registers
   static constexpr int ROWB = FP8 ? D : 2 * D, SPAN = ROWB < 128 ? ROWB : 128;
   static constexpr int TILE = KEYS * ROWB, STAGE = 2 * TILE;
   static constexpr int QBYTES = R * D * 2;
@@ -83,7 +83,7 @@ enum : int { kFirst = 1, kLast = 2, kNoKeys = 4, kFromStart = 8, kToEnd = 16 };
 struct SmallSmem {
   unsigned long long full[kMaxStages], empty[kMaxStages], join;
   TileDesc desc[kMaxStages];
-  float2 stats[kWarps][64];             // (m, l) of the warps' rows
+  float2 stats[kWarps][32];             // (m, l) of the warps' rows
   int64_t scan[2 * kWarps];
   int64_t total, start_base;
   int start_seq;
@@ -775,10 +775,10 @@ __global__ void __launch_bounds__(Traits<D, FP8, R>::THREADS, Traits<D, FP8, R>:
   }
 }
 
-// Rows of a tile: the fewest that hold the rows of a sequence and key head, up to 64.
+// Rows of a tile: the fewest that hold the rows of a sequence and key head.
 int tile_rows(int group, int max_new) {
   const int64_t rows = (int64_t)group * max_new;
-  return rows <= 8 ? 8 : rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
+  return rows <= 8 ? 8 : rows <= 16 ? 16 : 32;
 }
 int ctas_per_sm(int rows) { return rows <= 8 ? 3 : 2; }
 
@@ -800,8 +800,7 @@ int32_t launch_rows(StepArgs& args, const spf_kv_cache* cache, int rows, int liv
   switch (rows) {
     case 8: return launch_step<D, FP8, 8>(args, cache, live, ctas, stream);
     case 16: return launch_step<D, FP8, 16>(args, cache, live, ctas, stream);
-    case 32: return launch_step<D, FP8, 32>(args, cache, live, ctas, stream);
-    default: return launch_step<D, FP8, 64>(args, cache, live, ctas, stream);
+    default: return launch_step<D, FP8, 32>(args, cache, live, ctas, stream);
   }
 }
 
