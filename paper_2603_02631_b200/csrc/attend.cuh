@@ -50,9 +50,10 @@ __device__ __forceinline__ int pool_row(const AttendArgs& a, int seq, int head, 
   return (int)((block * a.kv.n_kv_heads + head) * a.kv.block_tokens + pos % a.kv.block_tokens);
 }
 
-// Factor of a group of 64 tokens, 1 outside the pool (its bytes then read as zeros).
-__device__ __forceinline__ float group_scale(const float* scale, int pool_row, int64_t rows) {
-  return pool_row < rows ? __ldg(scale + pool_row / kScaleTokens) : 1.f;
+// Factor of the group of 64 tokens at `key` (pool row `row`): 1 outside the pool, whose bytes then read as zeros, and for groups that
+// no row sees, whose factor may be anything.
+__device__ __forceinline__ float group_scale(const float* scale, const SeqSpan& s, int key, int row, int64_t rows) {
+  return row < rows && key < s.end && key + kScaleTokens > s.first ? __ldg(scale + row / kScaleTokens) : 1.f;
 }
 
 // One copy of a tile of pool rows, all spans of them, completing `bar`.

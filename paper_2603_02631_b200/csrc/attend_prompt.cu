@@ -196,8 +196,9 @@ __device__ __forceinline__ void copy_tiles(const PromptArgs& args, Smem& sm, uin
         if constexpr (T::FP8) {
 #pragma unroll
           for (int g = 0; g < 2; ++g) {
-            const float v = group_scale(a.kv.v_scale, row + 64 * g, pool_rows);
-            info.k_scale[g] = a.c * group_scale(a.kv.k_scale, row + 64 * g, pool_rows);
+            const int key = (tile0 + j0 + lane) * kKeys + g * kScaleTokens, at = row + g * kScaleTokens;
+            const float v = group_scale(a.kv.v_scale, s, key, at, pool_rows);
+            info.k_scale[g] = a.c * group_scale(a.kv.k_scale, s, key, at, pool_rows);
             info.v_log2[g] = log2f(v);
             info.v_inverse[g] = kWiden / v;
           }

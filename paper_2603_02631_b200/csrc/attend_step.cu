@@ -247,8 +247,9 @@ __device__ __forceinline__ void copy_tiles(const StepArgs& args, SmallSmem& sm, 
         if constexpr (T::FP8) {
 #pragma unroll
           for (int g = 0; g < T::KEYS / kScaleTokens; ++g) {
-            const float v = group_scale(a.kv.v_scale, row + g * kScaleTokens, pool_rows);
-            d.k_scale[g] = a.c * group_scale(a.kv.k_scale, row + g * kScaleTokens, pool_rows);
+            const int key = d.key0 + g * kScaleTokens, at = row + g * kScaleTokens;
+            const float v = group_scale(a.kv.v_scale, s, key, at, pool_rows);
+            d.k_scale[g] = a.c * group_scale(a.kv.k_scale, s, key, at, pool_rows);
             d.v_log2[g] = log2f(v);
             d.v_inverse[g] = kWiden / v;                  // l comes out times kWiden, as the values do
           }

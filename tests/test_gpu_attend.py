@@ -116,6 +116,25 @@ def test_what_no_row_may_see_does_not_matter(bits, new):
             pool.copy_(keep)
 
 
+@pytest.mark.parametrize("new", [1, 6, 90])
+def test_scales_of_groups_that_no_row_sees_do_not_matter(new):
+    import paper_2603_02631_b200 as spf
+    old, first = [230, 80], [70, 3]                         # the group of tokens 0 to 63 of the first is seen by nobody
+    s = make_step(8, 2, 64, 128, old, [new, new], 8, seed=4)
+    clean = run(spf, s, first=first)
+    used = torch.zeros(s.k_scale.shape[:1] + s.k_scale.shape[2:], dtype=torch.bool)
+    for b in range(2):
+        for pos in range(first[b], old[b] + new):
+            used[int(s.table[b, pos // 128]), pos % 128 // 64] = True
+    for scale in (s.k_scale, s.v_scale):
+        for value in (0.0, float("nan"), float("inf"), -1.0):
+            keep = scale.clone()
+            scale.masked_fill_(~used.cuda()[:, None], value)
+            dirty = run(spf, s, first=first)
+            assert torch.equal(clean[0], dirty[0]) and torch.equal(clean[1], dirty[1])
+            scale.copy_(keep)
+
+
 @pytest.mark.parametrize("bits", [16, 8])
 @pytest.mark.parametrize("new", [6, 100])
 def test_values_that_are_not_finite_reach_the_rows_that_see_them_and_no_others(bits, new):
