@@ -15,7 +15,6 @@
 #include <cuda_fp16.h>
 
 #include "kv.cuh"
-#include "tc_ptx.cuh"
 
 namespace spf {
 namespace {
@@ -86,21 +85,11 @@ __device__ __forceinline__ void load_angles(const float* table, int64_t row, int
   }
 }
 
+// (Packed pairs, mul.rn.f32x2 and add.rn.f32x2, gave other last bits: the two were made one instruction.)
 __device__ __forceinline__ void turn(float& x, float& y, float c, float s) {
   const float nx = __fsub_rn(__fmul_rn(x, c), __fmul_rn(y, s));
   y = __fadd_rn(__fmul_rn(y, c), __fmul_rn(x, s));
   x = nx;
-}
-// Two at once, with the same roundings.
-__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
-  uint64_t d;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
-}
-__device__ __forceinline__ void turn2(float* x, float* y, const float* c, const float* s) {
-  const uint64_t xx = pack2(x[0], x[1]), yy = pack2(y[0], y[1]), cc = pack2(c[0], c[1]), ss = pack2(s[0], s[1]);
-  unpack2(fma2(mul2(yy, ss), pack2(-1.f, -1.f), mul2(xx, cc)), x[0], x[1]);
-  unpack2(add2(mul2(yy, cc), mul2(xx, ss)), y[0], y[1]);
 }
 __device__ __forceinline__ void rotate(float (&a)[8], float (&b)[8], const Angles& t, int interleaved) {
   if (interleaved) {
@@ -111,7 +100,7 @@ __device__ __forceinline__ void rotate(float (&a)[8], float (&b)[8], const Angle
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; i += 2) turn2(a + i, b + i, t.c + i, t.s + i);
+    for (int i = 0; i < 8; ++i) turn(a[i], b[i], t.c[i], t.s[i]);
   }
 }
 
