@@ -71,18 +71,13 @@ __device__ __forceinline__ Unit unit_of(int u, int rot_dim, int interleaved) {
   return Unit{u * 8, rot_dim / 2 + u * 8, u * 8};
 }
 
+// Cosines and sines of four of a unit's eight pairs, the first four or the others.
 struct Angles {
-  float c[8], s[8];
+  float4 c, s;
 };
-__device__ __forceinline__ void load_angles(const float* table, int64_t row, int rot_dim, int angle, Angles& a) {
-  const float4* c = reinterpret_cast<const float4*>(table + row * rot_dim + angle);
-  const float4* s = reinterpret_cast<const float4*>(table + row * rot_dim + rot_dim / 2 + angle);
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const float4 x = __ldg(c + i), y = __ldg(s + i);
-    a.c[4 * i] = x.x, a.c[4 * i + 1] = x.y, a.c[4 * i + 2] = x.z, a.c[4 * i + 3] = x.w;
-    a.s[4 * i] = y.x, a.s[4 * i + 1] = y.y, a.s[4 * i + 2] = y.z, a.s[4 * i + 3] = y.w;
-  }
+__device__ __forceinline__ Angles load_angles(const float* table, int64_t row, int rot_dim, int angle) {
+  const float* at = table + row * rot_dim + angle;
+  return Angles{__ldg(reinterpret_cast<const float4*>(at)), __ldg(reinterpret_cast<const float4*>(at + rot_dim / 2))};
 }
 
 // (Packed pairs, mul.rn.f32x2 and add.rn.f32x2, gave other last bits: the two were made one instruction.)
@@ -91,16 +86,13 @@ __device__ __forceinline__ void turn(float& x, float& y, float c, float s) {
   y = __fadd_rn(__fmul_rn(y, c), __fmul_rn(x, s));
   x = nx;
 }
-__device__ __forceinline__ void rotate(float (&a)[8], float (&b)[8], const Angles& t, int interleaved) {
-  if (interleaved) {
+__device__ __forceinline__ void rotate(float (&a)[8], float (&b)[8], const Angles& t, int half, int interleaved) {
+  const float c[4] = {t.c.x, t.c.y, t.c.z, t.c.w}, s[4] = {t.s.x, t.s.y, t.s.z, t.s.w};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      turn(a[2 * i], a[2 * i + 1], t.c[i], t.s[i]);
-      turn(b[2 * i], b[2 * i + 1], t.c[4 + i], t.s[4 + i]);
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) turn(a[i], b[i], t.c[i], t.s[i]);
+  for (int i = 0; i < 4; ++i) {
+    if (!interleaved) turn(a[4 * half + i], b[4 * half + i], c[i], s[i]);
+    else if (half == 0) turn(a[2 * i], a[2 * i + 1], c[i], s[i]);
+    else turn(b[2 * i], b[2 * i + 1], c[i], s[i]);
   }
 }
 
@@ -160,8 +152,11 @@ __device__ __forceinline__ void move_rows(const AppendArgs& a) {
   const int64_t cell = (block * a.kv.n_kv_heads * a.kv.block_tokens + pos % a.kv.block_tokens) * D;
   const bool turns = !copy && u.angle >= 0;
   uint4 x[HPT][2];                                  // what is not turned is copied as it is
-  Angles t;
-  if (turns) load_angles(a.rope, angle_row, a.rot_dim, u.angle, t);
+  Angles t[2];
+  if (turns) {
+#pragma unroll
+    for (int half = 0; half < 2; ++half) t[half] = load_angles(a.rope, angle_row, a.rot_dim, u.angle + 4 * half);
+  }
 #pragma unroll
   for (int i = 0; i < HPT; ++i) {
     const int h = head0 + i;
@@ -181,7 +176,8 @@ __device__ __forceinline__ void move_rows(const AppendArgs& a) {
         float f[8], g[8];
         widen8(x[i][0], f);
         widen8(x[i][1], g);
-        rotate(f, g, t, a.interleaved);
+#pragma unroll
+        for (int half = 0; half < 2; ++half) rotate(f, g, t[half], half, a.interleaved);
         x[i][0] = narrow8(f);
         x[i][1] = narrow8(g);
       }
@@ -288,7 +284,7 @@ __device__ __forceinline__ void fill_group(const AppendArgs& a) {
   constexpr int kTokenStep = kAppendThreads / kUnits;
   const int row0 = start + (first + token0 - old_len);
   bool live[kPer];
-  int64_t angle_row[kPer];
+  int angle_row[kPer];
 #pragma unroll
   for (int i = 0; i < kPer; ++i) {
     const int pos = first + token0 + i * kTokenStep;
@@ -338,9 +334,11 @@ __device__ __forceinline__ void fill_group(const AppendArgs& a) {
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       if (u.angle >= 0 && live[i]) {
-        Angles t;
-        load_angles(a.rope, angle_row[i], a.rot_dim, u.angle, t);
-        rotate(x[i][0], x[i][1], t, a.interleaved);
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          const Angles t = load_angles(a.rope, angle_row[i], a.rot_dim, u.angle + 4 * half);
+          rotate(x[i][0], x[i][1], t, half, a.interleaved);
+        }
       }
       top = largest<false>(x[i], top);              // rows that are not there are zeros
     }
