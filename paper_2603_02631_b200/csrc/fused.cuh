@@ -1294,11 +1294,13 @@ __global__ void __launch_bounds__(kFusedThreads, 1) score_fused_kernel(const __g
 struct FusedLaunch {
   int ncols, padded_group, n_cta, smem_bytes;
   bool once;
+  bool scale_groups;              // 8-bit keys: scales for groups of 64 keys
 };
 int32_t fused_launch_d64(const FusedArgs& args, const FusedLaunch& l, cudaStream_t stream);
 int32_t fused_launch_d128(const FusedArgs& args, const FusedLaunch& l, cudaStream_t stream);
 int32_t fused_launch_d64_fp8(const FusedArgs& args, const FusedLaunch& l, cudaStream_t stream);
 int32_t fused_launch_d128_fp8(const FusedArgs& args, const FusedLaunch& l, cudaStream_t stream);
+// what the two above hand launches with scale_groups to
 int32_t fused_launch_d64_fp8_groups(const FusedArgs& args, const FusedLaunch& l, cudaStream_t stream);
 int32_t fused_launch_d128_fp8_groups(const FusedArgs& args, const FusedLaunch& l, cudaStream_t stream);
 

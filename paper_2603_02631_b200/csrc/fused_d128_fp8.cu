@@ -2,5 +2,7 @@
 #include "fused.cuh"
 
 namespace spf {
-int32_t fused_launch_d128_fp8(const FusedArgs& args, const FusedLaunch& l, cudaStream_t stream) { return fused_launch<128, 1>(args, l, stream); }
+int32_t fused_launch_d128_fp8(const FusedArgs& args, const FusedLaunch& l, cudaStream_t stream) {
+  return l.scale_groups ? fused_launch_d128_fp8_groups(args, l, stream) : fused_launch<128, 1>(args, l, stream);
+}
 }  // namespace spf

@@ -579,7 +579,7 @@ int32_t launch_group(const ScoreProblem* p, int n, const Geometry* geometries, c
   args.n_layers = p0.n_layers;
   args.mode = mode;
   args.dev_status = dev_status;
-  FusedLaunch l{g.ncols, g.padded_group, 0, 0, g.once};
+  FusedLaunch l{g.ncols, g.padded_group, 0, 0, g.once, GROUPS};
   int most_tiles = 1;
   for (int i = 0; i < n; ++i) {
     const ScoreProblem& q = p[i];
@@ -644,7 +644,6 @@ int32_t launch_group(const ScoreProblem* p, int n, const Geometry* geometries, c
     return fail(SPF_ERR_UNSUPPORTED, "spf_score: shape not covered by the fused path");
   const int32_t st = launch_prep<N, GROUPS>(prep, p0.head_dim, g.fp8, g.n_slabs, n, stream);
   if (st != SPF_OK) return st;
-  if constexpr (GROUPS) return p0.head_dim == 64 ? fused_launch_d64_fp8_groups(args, l, stream) : fused_launch_d128_fp8_groups(args, l, stream);
   if (p0.head_dim == 64) return g.fp8 ? fused_launch_d64_fp8(args, l, stream) : fused_launch_d64(args, l, stream);
   return g.fp8 ? fused_launch_d128_fp8(args, l, stream) : fused_launch_d128(args, l, stream);
 }
