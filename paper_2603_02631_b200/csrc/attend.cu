@@ -83,8 +83,8 @@ extern "C" int32_t spf_attend(const spf_kv_cache* cache, const spf_kv_step* step
   if (st != SPF_OK) return st;
   if (q->data == out->data) return fail(SPF_ERR_INVALID_ARG, "%s: out must not be q", who);
   const float scale = softmax_scale > 0.f ? softmax_scale : 1.0f / std::sqrt((float)cache->head_dim);
-  if (!std::isfinite(scale)) return fail(SPF_ERR_INVALID_ARG, "%s: softmax_scale is not finite", who);
   a.c = scale * kLog2e;
+  if (!std::isfinite(a.c)) return fail(SPF_ERR_INVALID_ARG, "%s: softmax_scale is too large", who);
   a.causal = 1;
   if (options != nullptr) {
     a.causal = options->see_all == 0;

@@ -40,12 +40,12 @@ __device__ __forceinline__ SeqSpan seq_span(const AttendArgs& a, int b) {
 }
 
 // Row of the pool (as the tensor maps count them, over blocks and heads) of a token's key; a place outside the pool is a row
-// outside the map, which reads as zeros.
+// outside every map (pools have at most 2^31 - 128 rows), which reads as zeros.
 __device__ __forceinline__ int pool_row(const AttendArgs& a, int seq, int head, int pos) {
   const int64_t block = pool_block(a.kv, a.step, seq, pos);
   if (block < 0) {
     report_cache(a.dev_status);
-    return 0x7fffff00;
+    return 0x7fffff80;
   }
   return (int)((block * a.kv.n_kv_heads + head) * a.kv.block_tokens + pos % a.kv.block_tokens);
 }

@@ -649,6 +649,7 @@ PyObject* score_paged_fp8_workspace_bytes(PyObject*, PyObject* const* args, Py_s
     const double scale = PyFloat_AsDouble(args[1]);
     if (PyErr_Occurred()) throw PyFailure{};
     const PagedFp8Call call(args[0], scale);
+    const c10::cuda::CUDAGuard guard(call.held.front().device());
     return PyLong_FromSize_t(spf_score_paged_fp8_workspace_bytes(&call.shape, call.prompts.data(), (int32_t)call.prompts.size()));
   } catch (const PyFailure&) {
     return nullptr;
@@ -669,6 +670,7 @@ PyObject* score_paged_fp8(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
     if (!ws.is_cuda()) raise(PyExc_TypeError, "workspace must be a CUDA tensor");
     at::Tensor status;
     if (args[3] != Py_None) status = device_tensor(args[3], at::kInt, "dev_status");
+    const c10::cuda::CUDAGuard guard(call.held.front().device());      // the prompts' device, not the current one
     void* stream = stream_of(args[4]);
     void* ws_ptr = ws.data_ptr();
     const size_t ws_bytes = (size_t)ws.numel() * ws.element_size();
