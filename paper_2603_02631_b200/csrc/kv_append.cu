@@ -11,16 +11,17 @@
 //
 // Bounds: bytes for a prompt, a launch and four dependent loads (row_start, seq_lens, table, the data) for single tokens.
 #include <algorithm>
+#include <type_traits>
 
 #include <cuda_fp16.h>
 
 #include "kv.cuh"
+#include "tc_ptx.cuh"
 
 namespace spf {
 namespace {
 
 constexpr int kAppendThreads = 256;
-constexpr int kManyJobs = 4;
 
 struct AppendArgs {
   KvView kv;
@@ -30,7 +31,8 @@ struct AppendArgs {
   const int32_t* positions;     // null: a token's place in its sequence
   int n_positions, rot_dim, interleaved;
   int n_q_heads;                // 0: no queries in this call
-  int rotate_ctas;              // CTAs that move whole rows; behind them, those that fill 8-bit groups
+  int rotate_ctas;              // CTAs that move whole rows; before them, those that fill 8-bit groups
+  int fill_heads;               // heads whose keys and values such a CTA fills (where there are many)
   uint64_t per_row_inverse;     // 2^64 / (threads of a row), rounded up
   int32_t* dev_status;
 };
@@ -80,6 +82,10 @@ __device__ __forceinline__ Angles load_angles(const float* table, int64_t row, i
   return Angles{__ldg(reinterpret_cast<const float4*>(at)), __ldg(reinterpret_cast<const float4*>(at + rot_dim / 2))};
 }
 
+__device__ __forceinline__ void copy_async(uint32_t dst, const void* src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+
 // (Packed pairs, mul.rn.f32x2 and add.rn.f32x2, gave other last bits: the two were made one instruction.)
 __device__ __forceinline__ void turn(float& x, float& y, float c, float s) {
   const float nx = __fsub_rn(__fmul_rn(x, c), __fmul_rn(y, s));
@@ -109,12 +115,12 @@ __device__ __forceinline__ bool place_of(const AppendArgs& a, int seq, int row, 
 // Rows as they are: queries (always), keys and values (bf16 pools).  A thread has one unit of HPT heads of a row, so that a
 // row's angles are read once for HPT heads.
 template <int D, int HPT, bool FP8>
-__device__ __forceinline__ void move_rows(const AppendArgs& a) {
+__device__ __forceinline__ void move_rows(const AppendArgs& a, int cta) {
   constexpr int kUnits = D / 16;
   const int turned = a.n_q_heads + (FP8 ? 0 : a.kv.n_kv_heads), copied = FP8 ? 0 : a.kv.n_kv_heads;
   const int turned_groups = (turned + HPT - 1) / HPT, groups = turned_groups + (copied + HPT - 1) / HPT;
   const int per_row = groups * kUnits;
-  const int64_t first = (int64_t)blockIdx.x * kAppendThreads, item = first + threadIdx.x;
+  const int64_t first = (int64_t)cta * kAppendThreads, item = first + threadIdx.x;
   // n / per_row = high word of n ceil(2^64 / per_row) while n per_row < 2^64 (here below 2^39 and 2^20): a 64-bit division by a
   // value that is not known when this is compiled takes some hundred instructions, more than everything else here
   auto row_of = [&](int64_t n) { return (int)__umul64hi((uint64_t)n, a.per_row_inverse); };
@@ -230,7 +236,7 @@ __device__ __forceinline__ float largest(const float (&x)[2][8], float top) {
   for (int h = 0; h < 2; ++h)
 #pragma unroll
     for (int e = 0; e < 8; e += 2)
-      top = FINITE ? fmaxf(top, fmaxf(finite_magnitude(x[h][e]), finite_magnitude(x[h][e + 1]))) : fmaxf(top, fmaxf(fabsf(x[h][e]), fabsf(x[h][e + 1])));
+      top = FINITE ? fmaxf(top, fmaxf(finite_magnitude(x[h][e]), finite_magnitude(x[h][e + 1]))) : max3(top, fabsf(x[h][e]), fabsf(x[h][e + 1]));
   return top;
 }
 // The largest of all threads' values.
@@ -245,16 +251,18 @@ __device__ __forceinline__ float largest_of_cta(float top, float* warp_max) {
   return top;
 }
 
-// A group of 64 tokens (of a sequence, in a pool block), for `jobs` of its heads' keys and values in turn: while one is made, the
-// next one's rows are on their way.  Group slots of the grid: sequence b owns those from row_start[b] / 64 + 2 b on, which is at
+// A group of 64 tokens (of a sequence, in a pool block): keys and values of some of its heads in turn; while ones are made, the next
+// ones' rows are on their way.  Group slots of the grid: sequence b owns those from row_start[b] / 64 + 2 b on, which is at
 // least as many as its new tokens can touch (n tokens touch at most n / 64 + 2 groups).
 template <int D, bool MANY>
-__device__ __forceinline__ void fill_group(const AppendArgs& a) {
+__device__ __forceinline__ void fill_group(const AppendArgs& a, int index) {
   constexpr int kUnits = D / 16, kPer = kScaleTokens * kUnits / kAppendThreads;
   __shared__ float warp_max[kAppendThreads / 32];
-  constexpr int kJobs = MANY ? kManyJobs : 1;
-  const int lanes = 2 * a.kv.n_kv_heads, pieces = (lanes + kJobs - 1) / kJobs;
-  const int index = (int)blockIdx.x - a.rotate_ctas, slot = index / pieces, job0 = (index - slot * pieces) * kJobs, job1 = min(job0 + kJobs, lanes);
+  // a CTA's share of the group: keys and values of some heads, or one head's keys or values
+  const int pieces = MANY ? (a.kv.n_kv_heads + a.fill_heads - 1) / a.fill_heads : 2 * a.kv.n_kv_heads;
+  const int slot = index / pieces, piece = index - slot * pieces;
+  const bool only_v = !MANY && piece >= a.kv.n_kv_heads;
+  const int head0 = MANY ? piece * a.fill_heads : only_v ? piece - a.kv.n_kv_heads : piece, head1 = min(head0 + (MANY ? a.fill_heads : 1), a.kv.n_kv_heads);
   int count = 0;
   for (int b = 0; b < a.step.n_seqs; b += kAppendThreads) {
     const int at = b + (int)threadIdx.x;
@@ -298,30 +306,43 @@ __device__ __forceinline__ void fill_group(const AppendArgs& a) {
       }
     }
   }
-  auto fetch = [&](int job, uint4 (&raw)[kPer][2]) {
-    const bool is_v = job >= a.kv.n_kv_heads;
-    const RowsView& rows = is_v ? a.v : a.k;
-    const Unit u = unit_of(unit, !is_v && a.rope != nullptr ? a.rot_dim : 0, a.interleaved);
-    const __nv_bfloat16* src = rows.data + row0 * rows.stride_row + (is_v ? job - a.kv.n_kv_heads : job) * rows.stride_head;
+  const Unit turned = unit_of(unit, a.rope != nullptr ? a.rot_dim : 0, a.interleaved), straight{unit * 16, unit * 16 + 8, -1};
+  auto fetch = [&](const __nv_bfloat16* src, int64_t stride_row, const Unit& u, uint4 (&raw)[kPer][2]) {
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       raw[i][0] = raw[i][1] = make_uint4(0, 0, 0, 0);
       if (live[i]) {
-        raw[i][0] = load_raw(src + i * kTokenStep * rows.stride_row + u.first);
-        raw[i][1] = load_raw(src + i * kTokenStep * rows.stride_row + u.second);
+        raw[i][0] = load_raw(src + i * kTokenStep * stride_row + u.first);
+        raw[i][1] = load_raw(src + i * kTokenStep * stride_row + u.second);
       }
     }
   };
+  const __nv_bfloat16* k_src = a.k.data + row0 * a.k.stride_row + head0 * a.k.stride_head;
+  const __nv_bfloat16* v_src = a.v.data + row0 * a.v.stride_row + head0 * a.v.stride_head;
+  // places of the thread's first token and of the group's scale in the pools, the same for keys and values
+  int64_t cell = ((block * a.kv.n_kv_heads + head0) * a.kv.block_tokens + off) * D;
+  int64_t scale_cell = (block * a.kv.n_kv_heads + head0) * (a.kv.block_tokens / kScaleTokens) + off / kScaleTokens;
+  const bool partly = lo > first;                   // the group holds tokens from before the step
   uint4 raw[kPer][2];
-  fetch(job0, raw);
-  for (int job = job0; MANY ? job < job1 : job == job0; ++job) {
-    const bool is_v = job >= a.kv.n_kv_heads;
-    const int head = is_v ? job - a.kv.n_kv_heads : job;
-    const int64_t slab = block * a.kv.n_kv_heads + head;
-    uint8_t* cells = (is_v ? a.kv.v : a.kv.k) + (slab * a.kv.block_tokens + off) * D;
-    float* scale_at = (is_v ? a.kv.v_scale : a.kv.k_scale) + slab * (a.kv.block_tokens / kScaleTokens) + off / kScaleTokens;
-    const Unit u = unit_of(unit, !is_v && a.rope != nullptr ? a.rot_dim : 0, a.interleaved);
-    const bool partly = lo > first;                 // the group holds tokens from before the step
+  // The thread's angles wait in shared memory, where their copy is on its way with the first rows: in registers there is no room, and
+  // loaded when the rows are there they are waited for once more.
+  __shared__ float4 angles[kPer][4][kAppendThreads];
+  const bool with_angles = !only_v && turned.angle >= 0;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    if (with_angles && live[i]) {
+      const float* at = a.rope + (int64_t)angle_row[i] * a.rot_dim + turned.angle;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) copy_async(smem_u32(&angles[i][j][threadIdx.x]), at + (j >> 1) * (a.rot_dim / 2) + 4 * (j & 1));
+    }
+  }
+
+  // Makes the bytes of what `raw` holds; `next` fetches the rows after these.
+  auto fill = [&](auto is_v, auto next) {
+    constexpr bool kValues = decltype(is_v)::value;
+    uint8_t* cells = (kValues ? a.kv.v : a.kv.k) + cell;
+    float* scale_at = (kValues ? a.kv.v_scale : a.kv.k_scale) + scale_cell;
+    const Unit u = kValues ? straight : turned;
     const float held = partly ? *scale_at : 0.f;    // every thread has it before one of them writes the new one: barriers follow
     float x[kPer][2][8];
     float top = 0.f;
@@ -330,15 +351,14 @@ __device__ __forceinline__ void fill_group(const AppendArgs& a) {
       widen8(raw[i][0], x[i][0]);
       widen8(raw[i][1], x[i][1]);
     }
-    if (MANY && job + 1 < job1) fetch(job + 1, raw);
+    next();
+    if (!kValues) asm volatile("cp.async.wait_all;" ::: "memory");
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-      if (u.angle >= 0 && live[i]) {
+      if (!kValues && with_angles && live[i]) {
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          const Angles t = load_angles(a.rope, angle_row[i], a.rot_dim, u.angle + 4 * half);
-          rotate(x[i][0], x[i][1], t, half, a.interleaved);
-        }
+        for (int half = 0; half < 2; ++half)
+          rotate(x[i][0], x[i][1], Angles{angles[i][half][threadIdx.x], angles[i][2 + half][threadIdx.x]}, half, a.interleaved);
       }
       top = largest<false>(x[i], top);              // rows that are not there are zeros
     }
@@ -351,9 +371,11 @@ __device__ __forceinline__ void fill_group(const AppendArgs& a) {
     }
     const float scale = fmaxf(held, scale_for(top));
     if (threadIdx.x == 0 && scale != held) *scale_at = scale;
-    // x / scale is a product where the scale is a power of two, as every scale that this kernel makes; else the quotients are made here
-    float inverse = 1.f / scale;
-    if ((__float_as_uint(scale) & 0x7fffffu) != 0) {
+    // x / scale is a product where the scale is a power of two (whose inverse is one too), as every scale that this kernel makes; else
+    // the quotients are made here
+    const uint32_t bits = __float_as_uint(scale);
+    float inverse = __uint_as_float((254u << 23) - bits);
+    if ((bits & 0x7fffffu) != 0 || bits >= 254u << 23) {
 #pragma unroll
       for (int i = 0; i < kPer; ++i)
 #pragma unroll
@@ -384,26 +406,54 @@ __device__ __forceinline__ void fill_group(const AppendArgs& a) {
       *reinterpret_cast<uint2*>(dst + u.first) = bytes8(x[i][0], inverse);
       *reinterpret_cast<uint2*>(dst + u.second) = bytes8(x[i][1], inverse);
     }
+  };
+  const std::integral_constant<bool, false> keys;
+  const std::integral_constant<bool, true> values;
+  if constexpr (!MANY) {
+    if (only_v) {
+      fetch(v_src, a.v.stride_row, straight, raw);
+      fill(values, [] {});
+    } else {
+      fetch(k_src, a.k.stride_row, turned, raw);
+      fill(keys, [] {});
+    }
+  } else {
+    fetch(k_src, a.k.stride_row, turned, raw);
+    for (int head = head0; head < head1; ++head) {
+      fill(keys, [&] { fetch(v_src, a.v.stride_row, straight, raw); });
+      k_src += a.k.stride_head;
+      v_src += a.v.stride_head;
+      fill(values, [&] {
+        if (head + 1 < head1) fetch(k_src, a.k.stride_row, turned, raw);
+      });
+      cell += (int64_t)a.kv.block_tokens * D;
+      scale_cell += a.kv.block_tokens / kScaleTokens;
+    }
   }
 }
 
 template <int D, int HPT, bool FP8>
 __global__ void __launch_bounds__(kAppendThreads, FP8 ? 3 : 4) append_kernel(const __grid_constant__ AppendArgs a) {
-  if (FP8 && (int)blockIdx.x >= a.rotate_ctas) fill_group<D, (HPT > 1)>(a);
-  else move_rows<D, HPT, FP8>(a);
+  const int fills = (int)gridDim.x - a.rotate_ctas;
+  if (FP8 && (int)blockIdx.x < fills) fill_group<D, (HPT > 1)>(a, (int)blockIdx.x);
+  else move_rows<D, HPT, FP8>(a, (int)blockIdx.x - (FP8 ? fills : 0));
 }
 
 template <int D, bool FP8>
 int32_t launch_append(AppendArgs& a, cudaStream_t stream) {
   const int turned = a.n_q_heads + (FP8 ? 0 : a.kv.n_kv_heads), copied = FP8 ? 0 : a.kv.n_kv_heads;
-  // Few rows: a head to a thread, a head's group to a CTA, so that everything is under way at once.  Where that more than fills the
-  // chip: two heads to a thread, which read a row's angles once, and four heads' groups to a CTA, which finds its place once and
-  // fetches the next one's rows while it makes one.
+  // Few rows: a head to a thread, a head's keys or values of a group to a CTA, so that everything is under way at once.  Where that
+  // more than fills the chip: two heads to a thread, which read a row's angles once, and keys and values of several heads of a group to
+  // a CTA, which finds its place once, keeps the angles and fetches the next rows while it makes these.
   const int64_t slots = FP8 ? a.step.n_rows / kScaleTokens + 2 * (int64_t)a.step.n_seqs : 0, lanes = 2 * (int64_t)a.kv.n_kv_heads;
   const bool many = (int64_t)a.step.n_rows * (a.n_q_heads + lanes) * (D / 16) > 148 * 2048;
   const int hpt = many ? 2 : 1;
   const int64_t items = (int64_t)a.step.n_rows * (ceil_div(turned, hpt) + ceil_div(copied, hpt)) * (D / 16);
-  const int64_t rotate = ceil_div(items, kAppendThreads), groups = slots * ceil_div(lanes, many ? kManyJobs : 1);
+  // Eight such heads, fewer where that would leave SMs without a CTA.  8 heads of 128 dimensions: 54k tokens 198 us (with two heads 210),
+  // 8192 tokens 27.8 (wanting three CTAs an SM 29.5, half of one 33.2), 4096 tokens 13.0 (14.7, 14.2).
+  a.fill_heads = 8;
+  while (a.fill_heads > 1 && slots * ceil_div(a.kv.n_kv_heads, a.fill_heads) < 148) a.fill_heads /= 2;
+  const int64_t rotate = ceil_div(items, kAppendThreads), groups = slots * (many ? ceil_div(a.kv.n_kv_heads, a.fill_heads) : lanes);
   if (rotate + groups > 0x7fffffffLL) return fail(SPF_ERR_UNSUPPORTED, "spf_kv_append: too many rows for one launch");
   if (rotate + groups == 0) return SPF_OK;
   a.rotate_ctas = (int)rotate;

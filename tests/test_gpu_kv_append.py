@@ -217,3 +217,11 @@ def test_many_sequences_and_a_graph_that_is_replayed_with_other_lengths(bits):
     alone = ids[count == 1].long()
     assert torch.equal(by_graph[0][alone], s.k_pool[alone]) and torch.equal(by_graph[1][alone], s.v_pool[alone])
     assert torch.equal(by_graph[2], q_out)
+
+
+@pytest.mark.parametrize("Hkv,rot_dim", [(3, 64), (8, 32), (12, 64)])
+def test_several_heads_of_a_group_to_a_cta(Hkv, rot_dim):
+    """Enough 8-bit groups that a CTA makes several heads' keys and values of one, a number that does not divide the heads among them."""
+    import paper_2603_02631_b200 as spf
+    s = make_step(2 * Hkv, Hkv, 64, 128, [70, 0], [4500, 5000], 8, seed=Hkv)
+    _check(spf, s, rope_table(6000, rot_dim))
