@@ -110,19 +110,18 @@ __device__ __forceinline__ void two_terms(const float (&f)[8], float top, int* e
   const uint32_t bits = __float_as_uint(top);
   const int e = top > 0.f && top < INFINITY ? min(max(135 - (int)(bits >> 23) - ((bits & 0x7fffffu) > 0x600000u ? 1 : 0), -120), 120) : 0;
   const float up = __uint_as_float((uint32_t)(e + 127) << 23);
-  uint32_t hi[2] = {0, 0}, lo[2] = {0, 0};
+  uint32_t hi[4], lo[4];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float x = f[i] * up;
-    const uint32_t t = float_to_e4m3(x);
-    uint32_t rest;
-    asm("{\n.reg .b16 r;\ncvt.rn.satfinite.e5m2x2.f32 r, %1, %2;\ncvt.u32.u16 %0, r;\n}" : "=r"(rest) : "f"(0.f), "f"(x - e4m3_to_float(t)));
-    hi[i >> 2] |= t << (8 * (i & 3));
-    lo[i >> 2] |= (rest & 0xffu) << (8 * (i & 3));
+  for (int i = 0; i < 4; ++i) {
+    const float x = f[2 * i] * up, y = f[2 * i + 1] * up;
+    uint32_t near;
+    asm("{\n.reg .b16 t;\ncvt.rn.satfinite.e4m3x2.f32 t, %3, %2;\ncvt.u32.u16 %0, t;\ncvt.rn.f16x2.e4m3x2 %1, t;\n}" : "=r"(hi[i]), "=r"(near) : "f"(x), "f"(y));
+    const float2 t = __half22float2(*reinterpret_cast<const __half2*>(&near));
+    asm("{\n.reg .b16 t;\ncvt.rn.satfinite.e5m2x2.f32 t, %2, %1;\ncvt.u32.u16 %0, t;\n}" : "=r"(lo[i]) : "f"(x - t.x), "f"(y - t.y));
   }
   *e_out = e;
-  *hi_out = make_uint2(hi[0], hi[1]);
-  *lo_out = make_uint2(lo[0], lo[1]);
+  *hi_out = make_uint2(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16);
+  *lo_out = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
 }
 
 // Log-sum-exp (natural) of a row from its reference and sum.

@@ -40,11 +40,12 @@ struct Traits {
   static constexpr int QTILE = 128 * D * 2;                                     // bf16, or two 8-bit terms
   static constexpr int KTILE = kKeys * ROWB, V8TILE = FP8 ? kKeys * D : 0, VTILE = kKeys * D * 2;
   static constexpr int STAGES = D == 64 ? 3 : 2;
+  static constexpr int QBUFS = D == 64 ? 2 : 1;                                 // where there is room, the next part's queries are fetched ahead
   // Tensor memory, 512 columns: S_X 128 each, O_X D each.  With 64 dimensions there is room for P_X (64 each) beside S_X, and the
   // next keys' logits are made while these are being turned into weights; with 128, P_X lies over S_X.
   static constexpr bool APART = D == 64;
   static constexpr uint32_t O_COL = 256, P_COL = APART ? 384 : 0, P_STEP = APART ? 64 : 128;
-  static constexpr int BYTES = 2 * QTILE + STAGES * (KTILE + V8TILE + VTILE);
+  static constexpr int BYTES = QBUFS * 2 * QTILE + STAGES * (KTILE + V8TILE + VTILE);
 };
 
 // What the copying warp tells the others about a part of a triple.
@@ -61,7 +62,7 @@ struct TileInfo {
 };
 
 struct Smem {
-  unsigned long long s_full[2], s_free[2], p_ready[2], o_done[2], o_free[2], q_ready, q_free, part_full[2], part_empty[2], values_done[2], mma_done;
+  unsigned long long s_full[2], s_free[2], p_ready[2], o_done[2], o_free[2], q_ready[2], q_free[2], part_full[2], part_empty[2], values_done[2], mma_done;
   unsigned long long k_full[3], k_empty[3], v_full[3], v_ready[3], v_empty[3], v8_empty[3];
   TileInfo info[kInfo];
   Part part[2];
@@ -252,46 +253,73 @@ struct PartReader {
 // ---------------------------------------------------------------------------------------------- queries and values
 template <class T>
 __device__ __forceinline__ void load_queries(const AttendArgs& a, Part& p, unsigned char* q_tiles, int thread) {
-  constexpr int D = T::D, kLanes = D / 8;
-  const int total = p.n_new * a.group;
-  for (int item = thread; item < kRows * kLanes; item += 128) {
-    const int r = item / kLanes, part = item % kLanes, x = r >> 7, in = r & 127;
-    const int64_t rr = (int64_t)p.row_tile * kRows + r;
-    union { uint4 u; __nv_bfloat162 h[4]; } v;
-    v.u = make_uint4(0, 0, 0, 0);
-    if (rr < total) {
-      const int token = (int)(rr / a.group), g = (int)(rr - (int64_t)token * a.group);
-      v.u = __ldg(reinterpret_cast<const uint4*>(a.q.data + (int64_t)(p.row0 + token) * a.q.stride_row + (int64_t)(p.head * a.group + g) * a.q.stride_head) + part);
+  constexpr int D = T::D, kLanes = D / 8, kBatch = T::FP8 ? 2 : 8;
+  static_assert(kRows * kLanes % (128 * kBatch) == 0);
+  const uint32_t group = (uint32_t)a.group, first = (uint32_t)p.row_tile * kRows, total = (uint32_t)p.n_new * group;
+  const int part = thread % kLanes;
+  const __nv_bfloat16* heads = a.q.data + (int64_t)p.row0 * a.q.stride_row + (int64_t)p.head * a.group * a.q.stride_head + 8 * part;
+#pragma unroll 1
+  for (int r0 = thread / kLanes; r0 < kRows; r0 += kBatch * (128 / kLanes)) {
+    union { uint4 u; __nv_bfloat162 h[4]; } v[kBatch];
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      const uint32_t rr = first + (uint32_t)(r0 + i * (128 / kLanes)), token = rr / group, g = rr - token * group;
+      v[i].u = make_uint4(0, 0, 0, 0);
+      if (rr < total) v[i].u = __ldg(reinterpret_cast<const uint4*>(heads + token * a.q.stride_row + g * a.q.stride_head));
     }
-    unsigned char* tile = q_tiles + x * T::QTILE;
-    if constexpr (!T::FP8) {
-      *reinterpret_cast<uint4*>(tile + (part >> 3) * (128 * 128) + in * 128 + ((part ^ in) & 7) * 16) = v.u;
-    } else {
-      float f[8], top = 0.f;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float2 t = __bfloat1622float2(v.h[i]);
-        f[2 * i] = t.x, f[2 * i + 1] = t.y;
-        top = fmaxf(top, fmaxf(fabsf(t.x), fabsf(t.y)));
+    for (int i = 0; i < kBatch; ++i) {
+      const int r = r0 + i * (128 / kLanes), x = r >> 7, in = r & 127;
+      unsigned char* tile = q_tiles + x * T::QTILE;
+      if constexpr (!T::FP8) {
+        *reinterpret_cast<uint4*>(tile + (part >> 3) * (128 * 128) + in * 128 + ((part ^ in) & 7) * 16) = v[i].u;
+      } else {
+        float f[8], top = 0.f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float2 t = __bfloat1622float2(v[i].h[j]);
+          f[2 * j] = t.x, f[2 * j + 1] = t.y;
+          top = fmaxf(top, fmaxf(fabsf(t.x), fabsf(t.y)));
+        }
+#pragma unroll
+        for (int o = kLanes / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o, kLanes));
+        int e;
+        uint2 hi, lo;
+        two_terms(f, top, &e, &hi, &lo);
+        const int chunk = part >> 1;
+        unsigned char* at = tile + (D == 128 ? in * 128 + ((chunk ^ in) & 7) * 16 : in * 64 + ((chunk ^ (in >> 1)) & 3) * 16) + 8 * (part & 1);
+        *reinterpret_cast<uint2*>(at) = hi;
+        *reinterpret_cast<uint2*>(at + 128 * D) = lo;
+        if (part == 0) p.q_factor[r] = __uint_as_float((uint32_t)(127 - e) << 23);
       }
-#pragma unroll
-      for (int o = kLanes / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o, kLanes));
-      int e;
-      uint2 hi, lo;
-      two_terms(f, top, &e, &hi, &lo);
-      const int chunk = part >> 1;
-      unsigned char* at = tile + (D == 128 ? in * 128 + ((chunk ^ in) & 7) * 16 : in * 64 + ((chunk ^ (in >> 1)) & 3) * 16) + 8 * (part & 1);
-      *reinterpret_cast<uint2*>(at) = hi;
-      *reinterpret_cast<uint2*>(at + 128 * D) = lo;
-      if (part == 0) p.q_factor[r] = __uint_as_float((uint32_t)(127 - e) << 23);
     }
   }
 }
 
-// Puts a value that is not finite down and returns whether it is to be cleared.
-__device__ __forceinline__ void put_down(Part& p, int dim, int key, bool nan, bool negative) {
-  atomicMin(&p.bad[nan ? 0 : negative ? 2 : 1][dim], key);
-  p.dirty = 1;
+// Clears what is not finite among 16 bytes of values (of a key, from dimension `dim` on) and puts it down.  Apart from the loop that
+// looks for such bytes, so that what is hardly ever needed does not crowd its instructions out.
+template <bool FP8>
+__device__ __noinline__ uint4 put_down(Part& p, uint4 raw, int dim, int key) {
+  uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+#pragma unroll 1
+    for (int i = 0; i < (FP8 ? 4 : 2); ++i) {
+      const uint32_t bits = FP8 ? 0xffu << (8 * i) : 0xffffu << (16 * i), v = (w[j] & bits) >> (FP8 ? 8 * i : 16 * i);
+      const bool nan = FP8 ? (v & 0x7fu) == 0x7fu : (v & 0x7fffu) > 0x7f80u, infinite = !FP8 && (v & 0x7fffu) == 0x7f80u;
+      if (nan || infinite) {
+        atomicMin(&p.bad[nan ? 0 : (v & 0x8000u) ? 2 : 1][dim + (FP8 ? 4 : 2) * j + i], key);
+        p.dirty = 1;
+        w[j] &= ~bits;
+      }
+    }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+// Whether any of 16 bytes of values is not finite: the exponent (E4M3: all but the sign) of ones overflows into the sign's place.
+template <bool FP8>
+__device__ __forceinline__ bool any_not_finite(const uint4& v) {
+  constexpr uint32_t kBits = FP8 ? 0x7f7f7f7fu : 0x7f807f80u, kOne = FP8 ? 0x01010101u : 0x00800080u, kSign = FP8 ? 0x80808080u : 0x80008000u;
+  return ((((v.x & kBits) + kOne) | ((v.y & kBits) + kOne) | ((v.z & kBits) + kOne) | ((v.w & kBits) + kOne)) & kSign) != 0;
 }
 
 template <class T>
@@ -305,12 +333,13 @@ __device__ __forceinline__ void prepare_values(const AttendArgs& a, Smem& sm, un
   while (Part* pp = reader.next(sm, ab)) {
     Part& p = *pp;
     if (p.n_tiles > 0) {
-      if (with_keys > 0 && !mbar_wait_warp(smem_u32(&sm.q_free), (uint32_t)(with_keys - 1) & 1u, ab)) return;
+      const int buf = with_keys % T::QBUFS, round = with_keys / T::QBUFS;
+      if (round > 0 && !mbar_wait_warp(smem_u32(&sm.q_free[buf]), (uint32_t)(round - 1) & 1u, ab)) return;
       ++with_keys;
-      load_queries<T>(a, p, q_tiles, thread);
+      load_queries<T>(a, p, q_tiles + buf * 2 * T::QTILE, thread);
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&sm.q_ready));
+      if (lane == 0) mbar_arrive(smem_u32(&sm.q_ready[buf]));
     }
     const int seen_by_all = a.causal ? p.pos0 + (int)((int64_t)p.row_tile * kRows / a.group) + 1 : p.end;   // keys below this one
     for (int j = 0; j < p.n_tiles; ++j, ++used) {
@@ -330,15 +359,7 @@ __device__ __forceinline__ void prepare_values(const AttendArgs& a, Smem& sm, un
           const int k = item / (D / 16), c = item % (D / 16), key = key0 + k;
           uint4 raw = *reinterpret_cast<const uint4*>(src + (D == 128 ? k * 128 + ((c ^ k) & 7) * 16 : k * 64 + ((c ^ (k >> 1)) & 3) * 16));
           if (ends && (key < p.first || key >= p.end)) raw = make_uint4(0, 0, 0, 0);
-          if (later && key >= seen_by_all) {
-            uint32_t* w = &raw.x;
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-              if (((w[i >> 2] >> (8 * (i & 3))) & 0x7fu) == 0x7fu) {
-                put_down(p, c * 16 + i, key, true, false);
-                w[i >> 2] &= ~(0xffu << (8 * (i & 3)));
-              }
-          }
+          if (later && key >= seen_by_all && any_not_finite<true>(raw)) raw = put_down<true>(p, raw, c * 16, key);
           uint32_t o[8];
           const uint32_t* w = &raw.x;
 #pragma unroll
@@ -360,19 +381,8 @@ __device__ __forceinline__ void prepare_values(const AttendArgs& a, Smem& sm, un
           if (key < p.first || key >= p.end) {
             *at = make_uint4(0, 0, 0, 0);
           } else if (key >= seen_by_all) {
-            uint4 raw = *at;
-            uint32_t* w = &raw.x;
-            bool changed = false;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const uint32_t half = (w[i >> 1] >> (16 * (i & 1))) & 0xffffu;
-              if ((half & 0x7f80u) == 0x7f80u) {
-                put_down(p, c * 8 + i, key, (half & 0x7fu) != 0, (half & 0x8000u) != 0);
-                w[i >> 1] &= (i & 1) ? 0x0000ffffu : 0xffff0000u;
-                changed = true;
-              }
-            }
-            if (changed) *at = raw;
+            const uint4 raw = *at;
+            if (any_not_finite<false>(raw)) *at = put_down<false>(p, raw, c * 8, key);
           }
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -468,6 +478,7 @@ struct Products {
   uint32_t done[2] = {0, 0}, asked[2] = {0, 0};          // products of either kind
   int with_tile[2] = {0, 0};
   uint32_t used = 0;                                     // tiles of the parts before
+  uint32_t q_buf = 0;                                    // where this part's queries lie
   int n = 0, tiles = 0;                                  // of this part
   bool fine = true;
 
@@ -481,13 +492,13 @@ struct Products {
     if (asked[x] > 0) wait(T::APART ? &sm.s_free[x] : &sm.o_done[x], asked[x] - 1);
     if (!fine) return;
     tc_fence_after();
-    logits<T>(on, tmem + 128 * x, q_desc + (uint32_t)(x * (T::QTILE >> 4)), k_desc + stage * (T::KTILE >> 4));
+    logits<T>(on, tmem + 128 * x, q_desc + (2 * q_buf + (uint32_t)x) * (T::QTILE >> 4), k_desc + stage * (T::KTILE >> 4));
     commit(on, smem_u32(&sm.s_full[x]));
     if (on) mbar_arrive(smem_u32(&sm.s_full[x]));         // hands on what this warp has seen: the tile's scales, the rows' factors
     ++asked[x];
     if (x == tiles - 1) {
       commit(on, smem_u32(&sm.k_empty[stage]));
-      if (j + 1 == n) commit(on, smem_u32(&sm.q_free));
+      if (j + 1 == n) commit(on, smem_u32(&sm.q_free[q_buf]));
     }
   }
   __device__ __forceinline__ void add(int x, int j) {
@@ -515,7 +526,8 @@ __device__ __forceinline__ void issue_products(Smem& sm, uint32_t tmem, uint32_t
     p.n = sm.part[n_parts & 1].n_tiles;
     p.tiles = sm.part[n_parts & 1].live > 128 ? 2 : 1;
     if (p.n > 0) {
-      p.wait(&sm.q_ready, (uint32_t)with_keys);
+      p.q_buf = (uint32_t)(with_keys % T::QBUFS);
+      p.wait(&sm.q_ready[p.q_buf], (uint32_t)(with_keys / T::QBUFS));
       ++with_keys;
       if (!T::APART) {
 #pragma unroll 1
@@ -556,8 +568,8 @@ __device__ __forceinline__ void write_rows(const PromptArgs& args, const Part& p
   constexpr int D = T::D;
   const AttendArgs& a = args.a;
   const bool whole = (p.flags & kFromStart) && (p.flags & kToEnd), live = r < p.live;
-  const int64_t rr = (int64_t)p.row_tile * kRows + r;
-  const int token = (int)(rr / a.group), head = p.head * a.group + (int)(rr - (int64_t)token * a.group), slot = 2 * blockIdx.x + ((p.flags & kFromStart) ? 1 : 0);
+  const uint32_t rr = (uint32_t)p.row_tile * kRows + (uint32_t)r;
+  const int token = (int)(rr / (uint32_t)a.group), head = p.head * a.group + (int)(rr - (uint32_t)token * (uint32_t)a.group), slot = 2 * blockIdx.x + ((p.flags & kFromStart) ? 1 : 0);
   const int64_t row = p.row0 + token;
   const float inv = l == 0.f ? 0.f : 1.f / l;
   const int pos = p.pos0 + token, dirty = p.dirty;
@@ -572,9 +584,10 @@ __device__ __forceinline__ void write_rows(const PromptArgs& args, const Part& p
     }
     float x[32];
 #pragma unroll
-    for (int i = 0; i < 32; ++i) {
-      x[i] = any ? __uint_as_float(raw[i]) : 0.f;
-      if (dirty) {
+    for (int i = 0; i < 32; ++i) x[i] = any ? __uint_as_float(raw[i]) : 0.f;
+    if (dirty) {
+#pragma unroll
+      for (int i = 0; i < 32; ++i) {
         const bool nan = p.bad[0][c + i] <= pos, plus = p.bad[1][c + i] <= pos, minus = p.bad[2][c + i] <= pos;
         if (nan || (plus && minus)) x[i] = __int_as_float(0x7fffffff);
         else if (plus || minus) x[i] += plus ? INFINITY : -INFINITY;
@@ -618,7 +631,7 @@ __device__ __forceinline__ void softmax_rows(const PromptArgs& args, Smem& sm, u
     const int n = p.n_tiles;
     float m = kNoReference, l = 0.f;
     if (mine && n > 0) {
-      const int token = (int)(((int64_t)p.row_tile * kRows + r) / a.group);
+      const int token = (int)(((uint32_t)p.row_tile * kRows + (uint32_t)r) / (uint32_t)a.group);
       const int hi = a.causal ? min(p.end, p.pos0 + token + 1) : p.end, first = p.first;
       float qf = 1.f;
       for (int j = 0; j < n; ++j, ++seen) {
@@ -742,7 +755,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
   using T = Traits<D, FP8>;
   extern __shared__ unsigned char smem_raw[];
   unsigned char* q_tiles = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
-  unsigned char* k_ring = q_tiles + 2 * T::QTILE;
+  unsigned char* k_ring = q_tiles + T::QBUFS * 2 * T::QTILE;
   unsigned char* v8_ring = k_ring + T::STAGES * T::KTILE;
   unsigned char* v_ring = v8_ring + T::STAGES * T::V8TILE;
   Smem& sm = *reinterpret_cast<Smem*>(v_ring + T::STAGES * T::VTILE);
@@ -757,9 +770,9 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
       mbar_init(smem_u32(&sm.part_full[i]), 1);
       mbar_init(smem_u32(&sm.part_empty[i]), 13);        // warps 0-11 and the one that issues products
       mbar_init(smem_u32(&sm.values_done[i]), 4);
+      mbar_init(smem_u32(&sm.q_ready[i]), 4);
+      mbar_init(smem_u32(&sm.q_free[i]), 1);
     }
-    mbar_init(smem_u32(&sm.q_ready), 4);
-    mbar_init(smem_u32(&sm.q_free), 1);
     mbar_init(smem_u32(&sm.mma_done), 1);
     for (int i = 0; i < T::STAGES; ++i) {
       mbar_init(smem_u32(&sm.k_full[i]), 1);
