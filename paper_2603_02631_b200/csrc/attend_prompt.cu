@@ -12,6 +12,11 @@
 // The work is dealt out as for few rows: the list of all key tiles of all (sequence, row tile, key head) triples, up to a row tile's
 // last visible key, is cut into one part for each SM; parts of a triple meet in a second kernel.
 //
+// Two row tiles and 128 keys take about 3400 cycles at 128 dimensions, of which the tensor cores are busy 2048 and the exponential unit
+// 2048 (2048 new of 32k tokens: 510 us, 1050 TFLOP/s, at the clock that the power limit leaves).  Not taken, all slower there: a part
+// of the exponentials as polynomials on the multiply-add units, products with the first half of the weights while the second is made,
+// logits read in two halves, exponentials of the two row tiles strictly in turns.
+//
 // Warps: 0-3 and 4-7 the rows of the two tiles (softmax, rescaling of O where a reference moves, output), 8-11 queries and values
 // (below), 12 copies, 13 issues the products.
 //
@@ -253,7 +258,7 @@ struct PartReader {
 // ---------------------------------------------------------------------------------------------- queries and values
 template <class T>
 __device__ __forceinline__ void load_queries(const AttendArgs& a, Part& p, unsigned char* q_tiles, int thread) {
-  constexpr int D = T::D, kLanes = D / 8, kBatch = T::FP8 ? 2 : 8;
+  constexpr int D = T::D, kLanes = D / 8, kBatch = T::FP8 ? 2 : 8;    // loads in flight (8 bits: their conversions are long; 8: 600 instead of 550 us)
   static_assert(kRows * kLanes % (128 * kBatch) == 0);
   const uint32_t group = (uint32_t)a.group, first = (uint32_t)p.row_tile * kRows, total = (uint32_t)p.n_new * group;
   const int part = thread % kLanes;
@@ -354,7 +359,8 @@ __device__ __forceinline__ void prepare_values(const AttendArgs& a, Smem& sm, un
       unsigned char* tile = v_ring + stage * T::VTILE;
       if constexpr (T::FP8) {
         const unsigned char* src = v8_ring + stage * T::V8TILE;
-#pragma unroll 2
+        // One piece at a time: the roles' instructions share a cache, and four at a time took 496 instead of 465 us (two: 478).
+#pragma unroll 1
         for (int item = thread; item < kKeys * (D / 16); item += 128) {
           const int k = item / (D / 16), c = item % (D / 16), key = key0 + k;
           uint4 raw = *reinterpret_cast<const uint4*>(src + (D == 128 ? k * 128 + ((c ^ k) & 7) * 16 : k * 64 + ((c ^ (k >> 1)) & 3) * 16));
