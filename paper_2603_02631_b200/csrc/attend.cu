@@ -31,7 +31,7 @@ int32_t check_heads(const char* who, const spf_kv_cache* cache, int32_t n_q_head
 // Enough for every step with up to `max_new` new tokens a sequence.
 size_t workspace_for(const spf_kv_cache* cache, int group, int max_new, int sm_count) {
   const size_t few = attend_step_workspace_bytes(cache, group, max_new, sm_count);
-  return (int64_t)group * max_new > kStepRows ? std::max(few, attend_prompt_workspace_bytes(cache, sm_count)) : few;
+  return (int64_t)group * max_new > step_rows(cache) ? std::max(few, attend_prompt_workspace_bytes(cache, sm_count)) : few;
 }
 
 }  // namespace
@@ -104,6 +104,6 @@ extern "C" int32_t spf_attend(const spf_kv_cache* cache, const spf_kv_step* step
     return fail(SPF_ERR_WORKSPACE, "%s: workspace is null or not 256-byte aligned", who);
   if (workspace_bytes < need) return fail(SPF_ERR_WORKSPACE, "%s: workspace has %zu bytes, %zu needed", who, workspace_bytes, need);
   const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-  if ((int64_t)a.group * step->max_new > kStepRows) return attend_prompt_launch(a, cache, sm_count, workspace, stream);
+  if ((int64_t)a.group * step->max_new > step_rows(cache)) return attend_prompt_launch(a, cache, sm_count, workspace, stream);
   return attend_step_launch(a, cache, step->max_new, sm_count, workspace, stream);
 }

@@ -161,10 +161,10 @@ int32_t attend_join_launch(const AttendArgs& a, const AttendParts& parts, int ro
 // The two kernels: a few rows a head and sequence, keys split over the chip; many rows.
 size_t attend_prompt_workspace_bytes(const spf_kv_cache* cache, int sm_count);
 int32_t attend_prompt_launch(const AttendArgs& a, const spf_kv_cache* cache, int sm_count, void* workspace, cudaStream_t stream);
-// Rows a key head and sequence up to which the first is taken.  With 64 rows and 131072 keys the second takes 90 us against 93
-// (64 dimensions; 8 bits: 100 against 138) and 129 against 145 (128; 157 against 275), with 32 rows 85 against 61 (94 against 77) and
-// 120 against 109 (148 against 155).
-constexpr int kStepRows = 32;
+// Rows a key head and sequence up to which the first is taken.  Over 131072 keys and 8 heads, first against second, 32 rows: 61 us
+// against 80 (64 dimensions), 76 against 88 (64, 8 bits), 108 against 112 (128), 157 against 139 (128, 8 bits, whose values' widening
+// then takes longer than their read); 64 rows: 99 against 85, 128 against 95, 187 against 118, 281 against 148.
+inline int step_rows(const spf_kv_cache* cache) { return cache->k_scale != nullptr && cache->head_dim == 128 ? 16 : 32; }
 size_t attend_step_workspace_bytes(const spf_kv_cache* cache, int group, int max_new, int sm_count);
 int32_t attend_step_launch(const AttendArgs& a, const spf_kv_cache* cache, int max_new, int sm_count, void* workspace, cudaStream_t stream);
 

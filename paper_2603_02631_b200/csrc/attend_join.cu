@@ -88,9 +88,11 @@ int32_t launch_rows(const AttendArgs& a, const AttendParts& parts, int rows, int
   switch (rows) {
     case 8: return launch<D, FP8, 8>(a, parts, live, ctas, stream);
     case 16: return launch<D, FP8, 16>(a, parts, live, ctas, stream);
-    case 32: return launch<D, FP8, 32>(a, parts, live, ctas, stream);
-    default: return launch<D, FP8, 256>(a, parts, live, ctas, stream);
+    case 32:
+      if constexpr (!(D == 128 && FP8)) return launch<D, FP8, 32>(a, parts, live, ctas, stream);   // else such steps have their tiles of 256
+      break;
   }
+  return launch<D, FP8, 256>(a, parts, live, ctas, stream);
 }
 
 }  // namespace

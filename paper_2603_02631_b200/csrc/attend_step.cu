@@ -777,9 +777,9 @@ __global__ void __launch_bounds__(Traits<D, FP8, R>::THREADS, Traits<D, FP8, R>:
 }
 
 // Rows of a tile: the fewest that hold the rows of a sequence and key head.
-int tile_rows(int group, int max_new) {
+int tile_rows(const spf_kv_cache* cache, int group, int max_new) {
   const int64_t rows = (int64_t)group * max_new;
-  return rows <= 8 ? 8 : rows <= 16 ? 16 : 32;
+  return rows <= 8 ? 8 : rows <= 16 ? 16 : step_rows(cache);
 }
 int ctas_per_sm(int rows) { return rows <= 8 ? 3 : 2; }
 
@@ -800,9 +800,11 @@ template <int D, bool FP8>
 int32_t launch_rows(StepArgs& args, const spf_kv_cache* cache, int rows, int live, int ctas, cudaStream_t stream) {
   switch (rows) {
     case 8: return launch_step<D, FP8, 8>(args, cache, live, ctas, stream);
-    case 16: return launch_step<D, FP8, 16>(args, cache, live, ctas, stream);
-    default: return launch_step<D, FP8, 32>(args, cache, live, ctas, stream);
+    case 16: break;
+    default:
+      if constexpr (!(D == 128 && FP8)) return launch_step<D, FP8, 32>(args, cache, live, ctas, stream);
   }
+  return launch_step<D, FP8, 16>(args, cache, live, ctas, stream);
 }
 
 }  // namespace
@@ -810,7 +812,7 @@ int32_t launch_rows(StepArgs& args, const spf_kv_cache* cache, int rows, int liv
 size_t attend_step_workspace_bytes(const spf_kv_cache* cache, int group, int max_new, int sm_count) {
   // a step with fewer rows has more CTAs: the most that any with up to this many takes
   size_t most = 0;
-  for (int rows = 8; rows <= tile_rows(group, max_new); rows *= 2)
+  for (int rows = 8; rows <= tile_rows(cache, group, max_new); rows *= 2)
     most = std::max(most, parts_layout(rows, cache->head_dim, sm_count * ctas_per_sm(rows)).total);
   return most;
 }
@@ -818,9 +820,9 @@ size_t attend_step_workspace_bytes(const spf_kv_cache* cache, int group, int max
 int32_t attend_step_launch(const AttendArgs& a, const spf_kv_cache* cache, int max_new, int sm_count, void* workspace, cudaStream_t stream) {
   StepArgs args{};
   args.a = a;
-  const int rows = tile_rows(a.group, max_new), live = (int)std::min<int64_t>((int64_t)a.group * max_new, rows), ctas = sm_count * ctas_per_sm(rows);
+  const int rows = tile_rows(cache, a.group, max_new), live = (int)std::min<int64_t>((int64_t)a.group * max_new, rows), ctas = sm_count * ctas_per_sm(rows);
   args.parts = parts_at(workspace, rows, cache->head_dim, ctas);
-    const bool fp8 = cache->k_scale != nullptr;
+  const bool fp8 = cache->k_scale != nullptr;
   if (cache->head_dim == 64) return fp8 ? launch_rows<64, true>(args, cache, rows, live, ctas, stream) : launch_rows<64, false>(args, cache, rows, live, ctas, stream);
   return fp8 ? launch_rows<128, true>(args, cache, rows, live, ctas, stream) : launch_rows<128, false>(args, cache, rows, live, ctas, stream);
 }

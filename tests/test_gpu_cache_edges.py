@@ -10,9 +10,9 @@ pytestmark = pytest.mark.gpu
 
 
 @pytest.mark.parametrize("bits", [16, 8])
-@pytest.mark.parametrize("Hq,Hkv,d,old,new", [(33, 1, 64, [150, 3], [1, 1]), (64, 1, 128, [500], [1]), (40, 1, 64, [130], [7]), (12, 12, 128, [70], [300])])
+@pytest.mark.parametrize("Hq,Hkv,d,old,new", [(33, 1, 64, [150, 3], [1, 1]), (64, 1, 128, [500], [1]), (40, 1, 64, [130], [7]), (16, 2, 128, [300, 40], [3, 2]), (12, 12, 128, [70], [300])])
 def test_wide_groups_and_single_heads(Hq, Hkv, d, old, new, bits):
-    """33, 64 and 280 rows of one key head (the kernel for many rows, few tokens); one row a head of a prompt."""
+    """33, 64, 280 and 24 rows of a key head (the kernel for many rows, few tokens); one row a head of a prompt."""
     import paper_2603_02631_b200 as spf
     s = make_step(Hq, Hkv, d, 128, old, new, bits, seed=Hq, behind=1)
     compare(s, *run(spf, s))
