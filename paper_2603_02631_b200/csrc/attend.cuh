@@ -109,7 +109,8 @@ __device__ __forceinline__ float nan_if_infinite(float x) {
 __device__ __forceinline__ void two_terms(const float (&f)[8], float top, int* e_out, uint2* hi_out, uint2* lo_out) {
   const uint32_t bits = __float_as_uint(top);
   const int e = top > 0.f && top < INFINITY ? min(max(135 - (int)(bits >> 23) - ((bits & 0x7fffffu) > 0x600000u ? 1 : 0), -120), 120) : 0;
-  const float up = __uint_as_float((uint32_t)(e + 127) << 23);
+  // a row with an infinite element has no softmax: NaN, not the largest finite byte
+  const float up = __uint_as_float(top == INFINITY ? 0x7fffffffu : (uint32_t)(e + 127) << 23);
   uint32_t hi[4], lo[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {

@@ -32,6 +32,22 @@ def test_a_step_in_which_no_sequence_has_tokens(bits, max_new):
     assert all(torch.equal(a, b) for a, b in zip(before, (s.k_pool, s.v_pool)))
 
 
+@pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("what", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("d,new", [(64, 6), (128, 2), (64, 60), (128, 60)])
+def test_queries_that_are_not_finite_spoil_their_own_row_alone(d, new, what, bits):
+    import paper_2603_02631_b200 as spf
+    s = make_step(4, 2, d, 128, [300], [new], bits, seed=8)
+    clean, clean_lse = run(spf, s)
+    element = s.q[1, 2, 5].clone()
+    s.q[1, 2, 5] = what
+    out, lse = run(spf, s)
+    assert out[1, 2].isnan().all() and lse[1, 2].isnan()
+    s.q[1, 2, 5] = element                                  # the other rows: as the reference has them
+    out[1, 2], lse[1, 2] = clean[1, 2], clean_lse[1, 2]
+    compare(s, out, lse)
+
+
 def test_a_step_of_no_rows():
     import paper_2603_02631_b200 as spf
     s = make_step(4, 2, 64, 128, [100], [0], 16, seed=2)
