@@ -75,7 +75,8 @@ int32_t encode_pool_map(const char* who, const spf_kv_cache* cache, void* pool, 
 // ---------------------------------------------------------------------------------------------- what both kernels compute with
 constexpr float kLazy = 8.f;            // how far logits may exceed their reference
 constexpr float kNoReference = -1.5e38f;   // of a row that has seen no key: finite, so that no difference of two is NaN
-constexpr float kShift = 7.f;           // 8-bit values: weights reach 2^(kLazy + kShift) = 2^15, below fp16's 65504
+constexpr float kShift = 7.f;           // 8-bit values: their reference is that much lower: weights reach 2^15, below fp16's 65504
+constexpr float kFar = 64.f;            // 8-bit values: how far the sum's weights may be above the products' and be made of them (RowStats)
 
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
@@ -89,7 +90,7 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
 // Four E4M3 bytes as two pairs of fp16, bytes 0 and 2, bytes 1 and 3, each times kWiden.  A byte s eeee mmm moved to the bits
 // s 0eeee mmm0000000 of a half is its value times 2^-8, subnormals included.  The product with 9 * 2^12 (exact: 4 + 4 significant
 // bits) leaves 448 at 64512, inside fp16, and takes the NaN patterns, which look like 480, to infinity.
-constexpr float kWiden = 144.f, kLog2Widen = 7.169925001442312f;
+constexpr float kWiden = 144.f;
 __device__ __forceinline__ void widen4(uint32_t four, uint32_t& even, uint32_t& odd) {
   const __half2 up = __half2half2(__ushort_as_half(0x7880));
   const uint32_t e = (four & 0x00ff00ffu) * 128u + (four & 0x00800080u) * 128u;
@@ -125,18 +126,32 @@ __device__ __forceinline__ void two_terms(const float (&f)[8], float top, int* e
   *lo_out = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
 }
 
-// Log-sum-exp (natural) of a row from its reference and sum.
+// A row's references and the sum of its weights.  bf16: weights are 2^(z - m) in the products and in the sum, m_sum is m.  8 bits: they
+// are 2^(z + log2 s_v - m) in the products, s_v being the scale of a group's values, and 2^(z - m_sum) in the sum.  Value scales may lie
+// 2^200 apart (that of zeros is 2^-100), so that no reference holds both in fp32's range.  A group's sum of the former times
+// 2^above_weights() is its part of the latter; where that factor is above 2^kFar, weights that fp32 has flushed to zero (below 2^-126)
+// could matter, and the part is made of exponentials of its own.
+struct RowStats {
+  float m, m_sum, l;
+};
+// `off`: what a group's logits have added in the exponents of the products' weights.
+__device__ __forceinline__ float above_weights(float off, float m_sum) { return -off - m_sum; }
+
+// What a row's weighted values are multiplied by besides 1 / l.
 template <bool FP8>
-__device__ __forceinline__ float row_lse(float m, float l) {
-  return l == 0.f ? -INFINITY : (m - (FP8 ? kShift + kLog2Widen : 0.f) + log2f(l)) * kLn2;
+__device__ __forceinline__ float output_factor(const RowStats& s) {
+  return FP8 ? fast_exp2(above_weights(-s.m, s.m_sum)) * (1.f / kWiden) : 1.f;
 }
+
+// Log-sum-exp (natural) of a row.
+__device__ __forceinline__ float row_lse(const RowStats& s) { return s.l == 0.f ? -INFINITY : (s.m_sum + log2f(s.l)) * kLn2; }
 
 // ---------------------------------------------------------------------------------------------- parts of a triple
 // A triple (sequence, row tile, key head) whose tiles several CTAs share leaves partial sums: slot 2 c of CTA c for what an earlier
 // CTA began, slot 2 c + 1 for what it began itself.
 struct AttendParts {
   float* sums;                    // [2 ctas][R][D]
-  float2* stats;                  // [2 ctas][R] reference and sum of weights
+  float4* stats;                  // [2 ctas][R] RowStats
   int4* headers;                  // [ctas][2]: CTAs behind this one with parts of its last triple (0: none), row0, head, row tile; rows
 };
 struct PartsLayout {
@@ -146,14 +161,14 @@ inline PartsLayout parts_layout(int rows, int d, int ctas) {
   PartsLayout w;
   w.sums = 0;
   w.stats = align_up((size_t)2 * ctas * rows * d * sizeof(float), 256);
-  w.headers = w.stats + align_up((size_t)2 * ctas * rows * sizeof(float2), 256);
+  w.headers = w.stats + align_up((size_t)2 * ctas * rows * sizeof(float4), 256);
   w.total = w.headers + align_up((size_t)2 * ctas * sizeof(int4), 256);
   return w;
 }
 inline AttendParts parts_at(void* workspace, int rows, int d, int ctas) {
   const PartsLayout w = parts_layout(rows, d, ctas);
   char* base = static_cast<char*>(workspace);
-  return AttendParts{reinterpret_cast<float*>(base + w.sums), reinterpret_cast<float2*>(base + w.stats), reinterpret_cast<int4*>(base + w.headers)};
+  return AttendParts{reinterpret_cast<float*>(base + w.sums), reinterpret_cast<float4*>(base + w.stats), reinterpret_cast<int4*>(base + w.headers)};
 }
 // Launches the kernel that joins parts, behind the one that leaves them.  `live`: rows that a tile of `rows` is expected to have at
 // most; with more the kernel does its work in several rounds.

@@ -19,17 +19,27 @@ __global__ void __launch_bounds__(128) attend_join_kernel(const __grid_constant_
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   auto slot = [&](int i) { return i == 0 ? 2 * (int)blockIdx.x + 1 : 2 * ((int)blockIdx.x + i); };
   for (int r = blockIdx.y; r < live; r += gridDim.y) {
-    float top = -INFINITY;
-    for (int i = lane; i < parts; i += 32) top = fmaxf(top, __ldcg(&args.stats[slot(i) * R + r].x));
+    RowStats all{-INFINITY, -INFINITY, 0.f};             // references are finite, also of parts whose keys the row does not see
+    for (int i = lane; i < parts; i += 32) {
+      const float2 s = __ldcg(reinterpret_cast<const float2*>(&args.stats[slot(i) * R + r]));
+      all.m = fmaxf(all.m, s.x);
+      all.m_sum = fmaxf(all.m_sum, s.y);
+    }
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    for (int o = 16; o > 0; o >>= 1) {
+      all.m = fmaxf(all.m, __shfl_xor_sync(0xffffffffu, all.m, o));
+      if (FP8) all.m_sum = fmaxf(all.m_sum, __shfl_xor_sync(0xffffffffu, all.m_sum, o));
+    }
+    if (!FP8) all.m_sum = all.m;
     float x[V] = {}, l = 0.f;
     for (int i0 = warp; i0 < parts; i0 += 128) {
       // the warp's parts i0, i0 + 4, ...: a lane has the statistics of one of 32
-      float2 s = make_float2(0.f, 0.f);
-      if (i0 + 4 * lane < parts) s = __ldcg(&args.stats[slot(i0 + 4 * lane) * R + r]);
-      const float f = i0 + 4 * lane < parts && s.x != -INFINITY ? fast_exp2(s.x - top) : 0.f;
-      l += s.y * f;
+      float f = 0.f;
+      if (i0 + 4 * lane < parts) {
+        const float4 s = __ldcg(&args.stats[slot(i0 + 4 * lane) * R + r]);
+        f = fast_exp2(s.x - all.m);
+        l += s.z * (FP8 ? fast_exp2(s.y - all.m_sum) : f);
+      }
 #pragma unroll 8
       for (int i = 0; i < 32 && i0 + 4 * i < parts; ++i) {
         const float w = __shfl_sync(0xffffffffu, f, i);
@@ -52,18 +62,18 @@ __global__ void __launch_bounds__(128) attend_join_kernel(const __grid_constant_
     for (int j = 0; j < V; ++j) sums[warp][lane * V + j] = x[j];
     if (lane == 0) weights[warp] = l;
     __syncthreads();
-    l = (weights[0] + weights[1]) + (weights[2] + weights[3]);
+    all.l = (weights[0] + weights[1]) + (weights[2] + weights[3]);
     const int rr = head.w * R + r, t = 2 * threadIdx.x;
     const int64_t row = head.y + rr / a.group;
     const int h = head.z * a.group + rr % a.group;
-    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const float inv = all.l == 0.f ? 0.f : 1.f / all.l, factor = output_factor<FP8>(all);
     if (t < D) {
       const float u = (sums[0][t] + sums[1][t]) + (sums[2][t] + sums[3][t]);
       const float v = (sums[0][t + 1] + sums[1][t + 1]) + (sums[2][t + 1] + sums[3][t + 1]);
       *reinterpret_cast<uint32_t*>(a.out.data + row * a.out.stride_row + h * a.out.stride_head + t) =
-          pack_bf16(nan_if_infinite<FP8>(u) * inv, nan_if_infinite<FP8>(v) * inv);
+          pack_bf16(nan_if_infinite<FP8>(u) * inv * factor, nan_if_infinite<FP8>(v) * inv * factor);
     }
-    if (a.lse != nullptr && threadIdx.x == 0) a.lse[row * a.lse_stride_row + h * a.lse_stride_head] = row_lse<FP8>(top, l);
+    if (a.lse != nullptr && threadIdx.x == 0) a.lse[row * a.lse_stride_row + h * a.lse_stride_head] = row_lse(all);
     __syncthreads();
   }
 }

@@ -63,7 +63,7 @@ struct Part {
 enum : int { kFromStart = 1, kToEnd = 2 };
 
 struct TileInfo {
-  float k_scale[2], v_log2[2], v_inverse[2];   // of the tile's two groups of 64 keys
+  float k_scale[2], v_log2[2];         // of the tile's two groups of 64 keys
 };
 
 struct Smem {
@@ -203,10 +203,8 @@ __device__ __forceinline__ void copy_tiles(const PromptArgs& args, Smem& sm, uin
 #pragma unroll
           for (int g = 0; g < 2; ++g) {
             const int key = (tile0 + j0 + lane) * kKeys + g * kScaleTokens, at = row + g * kScaleTokens;
-            const float v = group_scale(a.kv.v_scale, s, key, at, pool_rows);
             info.k_scale[g] = a.c * group_scale(a.kv.k_scale, s, key, at, pool_rows);
-            info.v_log2[g] = log2f(v);
-            info.v_inverse[g] = kWiden / v;
+            info.v_log2[g] = log2f(group_scale(a.kv.v_scale, s, key, at, pool_rows));
           }
         }
       }
@@ -570,14 +568,14 @@ __device__ __forceinline__ void issue_products(Smem& sm, uint32_t tmem, uint32_t
 
 // ---------------------------------------------------------------------------------------------- softmax and output
 template <class T>
-__device__ __forceinline__ void write_rows(const PromptArgs& args, const Part& p, int r, uint32_t o_addr, float m, float l, bool any) {
+__device__ __forceinline__ void write_rows(const PromptArgs& args, const Part& p, int r, uint32_t o_addr, const RowStats& stats, bool any) {
   constexpr int D = T::D;
   const AttendArgs& a = args.a;
   const bool whole = (p.flags & kFromStart) && (p.flags & kToEnd), live = r < p.live;
   const uint32_t rr = (uint32_t)p.row_tile * kRows + (uint32_t)r;
   const int token = (int)(rr / (uint32_t)a.group), head = p.head * a.group + (int)(rr - (uint32_t)token * (uint32_t)a.group), slot = 2 * blockIdx.x + ((p.flags & kFromStart) ? 1 : 0);
   const int64_t row = p.row0 + token;
-  const float inv = l == 0.f ? 0.f : 1.f / l;
+  const float inv = stats.l == 0.f ? 0.f : 1.f / stats.l, factor = output_factor<T::FP8>(stats);
   const int pos = p.pos0 + token, dirty = p.dirty;
 #pragma unroll 1
   for (int c = 0; c < D; c += 32) {
@@ -604,7 +602,7 @@ __device__ __forceinline__ void write_rows(const PromptArgs& args, const Part& p
     } else if (whole) {
       uint4* dst = reinterpret_cast<uint4*>(a.out.data + row * a.out.stride_row + head * a.out.stride_head + c);
 #pragma unroll
-      for (int i = 0; i < 32; ++i) x[i] = nan_if_infinite<T::FP8>(x[i]) * inv;
+      for (int i = 0; i < 32; ++i) x[i] = nan_if_infinite<T::FP8>(x[i]) * inv * factor;
 #pragma unroll
       for (int i = 0; i < 4; ++i)
         dst[i] = make_uint4(pack_bf16(x[8 * i], x[8 * i + 1]), pack_bf16(x[8 * i + 2], x[8 * i + 3]), pack_bf16(x[8 * i + 4], x[8 * i + 5]),
@@ -616,8 +614,8 @@ __device__ __forceinline__ void write_rows(const PromptArgs& args, const Part& p
     }
   }
   if (!live) return;
-  if (!whole) args.parts.stats[slot * kRows + r] = make_float2(m, l);
-  else if (a.lse != nullptr) a.lse[row * a.lse_stride_row + head * a.lse_stride_head] = row_lse<T::FP8>(m, l);
+  if (!whole) args.parts.stats[slot * kRows + r] = make_float4(stats.m, stats.m_sum, stats.l, 0.f);
+  else if (a.lse != nullptr) a.lse[row * a.lse_stride_row + head * a.lse_stride_head] = row_lse(stats);
 }
 
 template <class T>
@@ -635,7 +633,7 @@ __device__ __forceinline__ void softmax_rows(const PromptArgs& args, Smem& sm, u
     const Part& p = *pp;
     const bool mine = x * 128 < p.live;
     const int n = p.n_tiles;
-    float m = kNoReference, l = 0.f;
+    float m = kNoReference, m_sum = kNoReference, l = 0.f;   // m_sum: 8 bits
     if (mine && n > 0) {
       const int token = (int)(((uint32_t)p.row_tile * kRows + (uint32_t)r) / (uint32_t)a.group);
       const int hi = a.causal ? min(p.end, p.pos0 + token + 1) : p.end, first = p.first;
@@ -647,15 +645,15 @@ __device__ __forceinline__ void softmax_rows(const PromptArgs& args, Smem& sm, u
         uint32_t s[4][32];
 #pragma unroll
         for (int c = 0; c < 4; ++c) tmem_issue<32>(s_addr + 32 * c, s[c]);
-        float f[2], add[2], inverse[2];
+        float f[2], add[2];
         if constexpr (T::FP8) {
           const TileInfo& info = sm.info[(info_at + j) % kInfo];
           if (j == 0) qf = p.q_factor[r];
 #pragma unroll
-          for (int g = 0; g < 2; ++g) f[g] = info.k_scale[g] * qf, add[g] = info.v_log2[g], inverse[g] = info.v_inverse[g];
+          for (int g = 0; g < 2; ++g) f[g] = info.k_scale[g] * qf, add[g] = info.v_log2[g];
         } else {
 #pragma unroll
-          for (int g = 0; g < 2; ++g) f[g] = a.c, add[g] = 0.f, inverse[g] = 1.f;
+          for (int g = 0; g < 2; ++g) f[g] = a.c, add[g] = 0.f;
         }
         tmem_load_wait();
 #pragma unroll
@@ -675,7 +673,7 @@ __device__ __forceinline__ void softmax_rows(const PromptArgs& args, Smem& sm, u
         }
         // the row's largest logit (scales are positive); on the way through the exponentials below it would cost registers that
         // are not there (554 instead of 513 us)
-        float top = -INFINITY;
+        float top = -INFINITY, top_sum = -INFINITY;      // with the values' scales, and without
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
           float t[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
@@ -684,17 +682,38 @@ __device__ __forceinline__ void softmax_rows(const PromptArgs& args, Smem& sm, u
 #pragma unroll
             for (int i = 0; i < 32; i += 2)
               t[(i >> 1) & 3] = max3(t[(i >> 1) & 3], __uint_as_float(s[2 * g + c][i]), __uint_as_float(s[2 * g + c][i + 1]));
-          top = fmaxf(top, fmaf(fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])), f[g], add[g]));
+          const float largest = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])) * f[g];
+          top = fmaxf(top, largest + add[g]);
+          top_sum = fmaxf(top_sum, largest);
         }
+        auto above = [&](int g) { return above_weights(add[g] - m, m_sum); };
+        bool over = T::FP8 ? top - m > kLazy + kShift : top > m + kLazy;
+        if constexpr (T::FP8) over |= top_sum - m_sum > kLazy || above(0) > kFar || above(1) > kFar;
         if constexpr (T::APART) {
           // the weights go where the product with the tile before may still read
           if (seen > 0 && !mbar_wait_warp(smem_u32(&sm.o_done[x]), (uint32_t)(seen - 1) & 1u, ab)) return;
           tc_fence_after();
         }
-        if (__any_sync(0xffffffffu, top > m + kLazy)) {
-          const float now = fmaxf(m, top), scale = fast_exp2(m - now);
+        if (__any_sync(0xffffffffu, over)) {
+          const float now = fmaxf(m, T::FP8 ? top - kShift : top), scale = fast_exp2(m - now);
           m = now;
-          l *= scale;
+          if constexpr (T::FP8) {
+            const float now_sum = fmaxf(m_sum, top_sum);
+            l *= fast_exp2(m_sum - now_sum);
+            m_sum = now_sum;
+#pragma unroll
+            for (int g = 0; g < 2; ++g) {
+              if (!__any_sync(0xffffffffu, above(g) > kFar)) continue;
+              float own = 0.f;
+#pragma unroll
+              for (int c = 0; c < 2; ++c)
+#pragma unroll
+                for (int i = 0; i < 32; ++i) own += fast_exp2(fmaf(__uint_as_float(s[2 * g + c][i]), f[g], -m_sum));
+              if (above(g) > kFar) l += own;
+            }
+          } else {
+            l *= scale;
+          }
           if (j > 0) {
             // the product with the tile before is done: it was waited for above, or before these logits' product
 #pragma unroll 1
@@ -709,10 +728,9 @@ __device__ __forceinline__ void softmax_rows(const PromptArgs& args, Smem& sm, u
             }
           }
         }
-        const float ref = m - (T::FP8 ? kShift : 0.f);
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
-          const uint64_t ff = pack2(f[g], f[g]), off = pack2(add[g] - ref, add[g] - ref);
+          const uint64_t ff = pack2(f[g], f[g]), off = pack2(add[g] - m, add[g] - m);
           uint64_t sum[2] = {0ull, 0ull};
           uint32_t w[32];
 #pragma unroll
@@ -729,7 +747,8 @@ __device__ __forceinline__ void softmax_rows(const PromptArgs& args, Smem& sm, u
           tmem_store<32>(p_addr + 32 * g, w);
           float u, v;
           unpack2(add2(sum[0], sum[1]), u, v);
-          l = T::FP8 ? fmaf(u + v, inverse[g], l) : l + (u + v);
+          if constexpr (T::FP8) l = fmaf(u + v, above(g) > kFar ? 0.f : fast_exp2(above(g)), l);
+          else l += u + v;
         }
         tmem_store_wait();
         tc_fence_before();
@@ -741,7 +760,7 @@ __device__ __forceinline__ void softmax_rows(const PromptArgs& args, Smem& sm, u
     }
     if (mine) {
       if (!mbar_wait_warp(smem_u32(&sm.values_done[reader.n & 1]), (uint32_t)(reader.n >> 1) & 1u, ab)) return;
-      write_rows<T>(args, p, r, o_addr, m, l, n > 0);
+      write_rows<T>(args, p, r, o_addr, RowStats{m, T::FP8 ? m_sum : m, l}, n > 0);
       tc_fence_before();
       __syncwarp();
       if (n > 0 && lane == 0) mbar_arrive(smem_u32(&sm.o_free[x]));

@@ -25,9 +25,10 @@
 // two e of a row that takes its largest element to (224, 448].  Exact for elements within 2^13 of that one, off by at most 2^-21 of
 // it below: hi has 4 significant bits, what it leaves is at most half its step and fits lo's 3.
 // 8 bits, values: widened to fp16, exactly, next to the products (widen4; both operands by the conversion instruction, which is
-// slow: 697 instead of 384 us for four sequences of 131 to 250 thousand tokens).  A tile's value scale s_v joins its logits, so that the weights are p s_v / (the largest such so far) and never
-// leave fp16's range, and l takes them divided by s_v again:
-//   z'[r,s] = z[r,s] + log2 s_v,  w = 2^(z' - m' + 7),  out = sum w byte / l,  l = sum w / s_v,  lse = (m' - 7 + log2 l) ln 2.
+// slow: 697 instead of 384 us for four sequences of 131 to 250 thousand tokens).  A tile's value scale s_v joins its logits, so that the
+// weights are p s_v / (the largest such so far) and never leave fp16's range; their sum l has a reference of its own (RowStats):
+//   z'[r,s] = z[r,s] + log2 s_v,  w = 2^(z' - m'),  l = sum 2^(z - m),  out = 2^(m' - m) sum w byte / l,  lse = (m + log2 l) ln 2.
+// m' lies 7 below the largest z' seen (but for the 8 above), which leaves small weights more of fp16's range.
 //
 // Keys that no row may see (behind the sequence's end, before its first key) take part with logits of -inf and values of zero,
 // whatever the pool holds there.  Keys that only later rows of the step may see have weight zero; if their values are not
@@ -48,7 +49,7 @@ constexpr int kMaxStages = 8;
 // What the copying warp tells the computing ones about a stage.
 struct TileDesc {
   int row0, n_new, pos0, first, end, head, row_tile, key0;
-  float k_scale[2], v_log2[2], v_inverse[2];   // 8 bits: of the tile's groups of 64 keys
+  float k_scale[2], v_log2[2];          // 8 bits: of the tile's groups of 64 keys
   int flags;                            // kFirst, kLast, kNoKeys; bits 8 ...: CTAs behind this one with parts of the triple
 };
 
@@ -83,7 +84,7 @@ enum : int { kFirst = 1, kLast = 2, kNoKeys = 4, kFromStart = 8, kToEnd = 16 };
 struct SmallSmem {
   unsigned long long full[kMaxStages], empty[kMaxStages], join;
   TileDesc desc[kMaxStages];
-  float2 stats[kWarps][32];             // (m, l) of the warps' rows
+  RowStats stats[kWarps][32];           // of the warps' rows
   int64_t scan[2 * kWarps];
   int64_t total, start_base;
   int start_seq;
@@ -248,10 +249,8 @@ __device__ __forceinline__ void copy_tiles(const StepArgs& args, SmallSmem& sm, 
 #pragma unroll
           for (int g = 0; g < T::KEYS / kScaleTokens; ++g) {
             const int key = d.key0 + g * kScaleTokens, at = row + g * kScaleTokens;
-            const float v = group_scale(a.kv.v_scale, s, key, at, pool_rows);
             d.k_scale[g] = a.c * group_scale(a.kv.k_scale, s, key, at, pool_rows);
-            d.v_log2[g] = log2f(v);
-            d.v_inverse[g] = kWiden / v;                  // l comes out times kWiden, as the values do
+            d.v_log2[g] = log2f(group_scale(a.kv.v_scale, s, key, at, pool_rows));
           }
         }
       }
@@ -399,6 +398,7 @@ template <class T>
 struct State {
   float o[T::D / 16][T::NT][4];
   float m[T::NT][2], l[T::NT][2];
+  float m_sum[T::FP8 ? T::NT : 1][2];                    // 8 bits
 };
 
 // Keys of a triple that its rows see: [first, end) that some do, below `all` that every one does.
@@ -532,6 +532,7 @@ __device__ __forceinline__ void compute_tiles(const StepArgs& args, SmallSmem& s
           sees[nt][e] = a.causal ? min(d.end, d.pos0 + row / a.group + 1) : d.end;
           st.m[nt][e] = kNoReference;
           st.l[nt][e] = 0.f;
+          if constexpr (T::FP8) st.m_sum[nt][e] = kNoReference;
           if constexpr (T::FP8) qf[nt][e] = q_factor[row_off + nt * 8 + 2 * (lane & 3) + e];
         }
 #pragma unroll
@@ -602,6 +603,7 @@ __device__ __forceinline__ void compute_tiles(const StepArgs& args, SmallSmem& s
       // base-2 logits are z f + add; the largest decides whether a row's reference moves
       const float add = T::FP8 ? d.v_log2[group64] : 0.f, k_scale = T::FP8 ? d.k_scale[group64] : a.c;
       float f[NT][2], top[NT][2];
+      auto offset = [&](int nt, int e) { return add - st.m[nt][e]; };
       bool over = false;
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
@@ -611,22 +613,39 @@ __device__ __forceinline__ void compute_tiles(const StepArgs& args, SmallSmem& s
           float t = fmaxf(z[0][nt][e], z[0][nt][2 + e]);
 #pragma unroll
           for (int kt = 1; kt < KT; ++kt) t = max3(t, z[kt][nt][e], z[kt][nt][2 + e]);
-          top[nt][e] = fmaf(t, f[nt][e], add);
-          over |= top[nt][e] > st.m[nt][e] + kLazy;
+          top[nt][e] = t * f[nt][e];
+          if constexpr (T::FP8) {
+            const float off = offset(nt, e);
+            over |= top[nt][e] + off > kLazy + kShift || top[nt][e] - st.m_sum[nt][e] > kLazy || above_weights(off, st.m_sum[nt][e]) > kFar;
+          } else {
+            over |= top[nt][e] > st.m[nt][e] + kLazy;
+          }
         }
       if (__any_sync(0xffffffffu, over)) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            float t = fmaxf(st.m[nt][e], top[nt][e]);
+            float largest = top[nt][e];
 #pragma unroll
-            for (int o = 4; o < 32; o <<= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, o));
-            const float scale = fast_exp2(st.m[nt][e] - t);
-            st.m[nt][e] = t;
-            st.l[nt][e] *= scale;
+            for (int o = 4; o < 32; o <<= 1) largest = fmaxf(largest, __shfl_xor_sync(0xffffffffu, largest, o));
+            const float m = fmaxf(st.m[nt][e], T::FP8 ? largest + add - kShift : largest), scale = fast_exp2(st.m[nt][e] - m);
+            st.m[nt][e] = m;
 #pragma unroll
-            for (int m = 0; m < D / 16; ++m) st.o[m][nt][e] *= scale, st.o[m][nt][2 + e] *= scale;
+            for (int i = 0; i < D / 16; ++i) st.o[i][nt][e] *= scale, st.o[i][nt][2 + e] *= scale;
+            if constexpr (T::FP8) {
+              const float m_sum = fmaxf(st.m_sum[nt][e], largest);
+              st.l[nt][e] *= fast_exp2(st.m_sum[nt][e] - m_sum);
+              st.m_sum[nt][e] = m_sum;
+              if (above_weights(offset(nt, e), m_sum) > kFar) {
+#pragma unroll
+                for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+                  for (int h = 0; h < 2; ++h) st.l[nt][e] += fast_exp2(fmaf(z[kt][nt][2 * h + e], f[nt][e], -m_sum));
+              }
+            } else {
+              st.l[nt][e] *= scale;
+            }
           }
       }
       uint32_t p[KT][NT][2];
@@ -634,7 +653,7 @@ __device__ __forceinline__ void compute_tiles(const StepArgs& args, SmallSmem& s
       for (int nt = 0; nt < NT; ++nt) {
         float off[2], sum[2] = {0.f, 0.f};
 #pragma unroll
-        for (int e = 0; e < 2; ++e) off[e] = add - (st.m[nt][e] - (T::FP8 ? kShift : 0.f));
+        for (int e = 0; e < 2; ++e) off[e] = offset(nt, e);
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
@@ -645,7 +664,14 @@ __device__ __forceinline__ void compute_tiles(const StepArgs& args, SmallSmem& s
             p[kt][nt][h] = transpose8(T::FP8 ? pack_f16(x, y) : pack_bf16(x, y));
           }
 #pragma unroll
-        for (int e = 0; e < 2; ++e) st.l[nt][e] = T::FP8 ? fmaf(sum[e], d.v_inverse[group64], st.l[nt][e]) : st.l[nt][e] + sum[e];
+        for (int e = 0; e < 2; ++e) {
+          if constexpr (T::FP8) {
+            const float above = above_weights(off[e], st.m_sum[nt][e]);
+            st.l[nt][e] = fmaf(sum[e], above > kFar ? 0.f : fast_exp2(above), st.l[nt][e]);
+          } else {
+            st.l[nt][e] += sum[e];
+          }
+        }
       }
       if (!guard) add_values<T, false>(st, p, v_tile, key_off, key0, seen, lane);
       else if (seen.all >= seen.end || !odd_values<T>(v_tile, key_off, key0, seen.all, seen.end, lane)) add_values<T, true>(st, p, v_tile, key_off, key0, seen, lane);
@@ -660,7 +686,7 @@ __device__ __forceinline__ void compute_tiles(const StepArgs& args, SmallSmem& s
           float l = st.l[nt][e];
 #pragma unroll
           for (int o = 4; o < 32; o <<= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
-          if (lane < 4) sm.stats[key_warp][row_off + nt * 8 + 2 * lane + e] = make_float2(st.m[nt][e], l);
+          if (lane < 4) sm.stats[key_warp][row_off + nt * 8 + 2 * lane + e] = RowStats{st.m[nt][e], T::FP8 ? st.m_sum[nt][e] : st.m[nt][e], l};
         }
       if (!join.wait(ab)) return;                        // statistics are there, and the stage's tile is read
       float f[NT][2];
@@ -671,7 +697,7 @@ __device__ __forceinline__ void compute_tiles(const StepArgs& args, SmallSmem& s
           const int r = row_off + nt * 8 + 2 * (lane & 3) + e;
           float top = kNoReference;
 #pragma unroll
-          for (int w = 0; w < T::WK; ++w) top = fmaxf(top, sm.stats[w][r].x);
+          for (int w = 0; w < T::WK; ++w) top = fmaxf(top, sm.stats[w][r].m);
           f[nt][e] = fast_exp2(st.m[nt][e] - top);
         }
       const bool whole = (flags & kFromStart) && (flags & kToEnd);
@@ -704,28 +730,28 @@ __device__ __forceinline__ void compute_tiles(const StepArgs& args, SmallSmem& s
             const float4 u = src[0], v = src[1];
             x[0] += u.x, x[1] += u.y, x[2] += u.z, x[3] += u.w, x[4] += v.x, x[5] += v.y, x[6] += v.z, x[7] += v.w;
           }
-          float top = kNoReference, l = 0.f;
+          RowStats all{kNoReference, kNoReference, 0.f};
 #pragma unroll
-          for (int w = 0; w < T::WK; ++w) top = fmaxf(top, sm.stats[w][r].x);
+          for (int w = 0; w < T::WK; ++w) all.m = fmaxf(all.m, sm.stats[w][r].m), all.m_sum = fmaxf(all.m_sum, sm.stats[w][r].m_sum);
 #pragma unroll
-          for (int w = 0; w < T::WK; ++w) l += sm.stats[w][r].y * fast_exp2(sm.stats[w][r].x - top);
+          for (int w = 0; w < T::WK; ++w) all.l += sm.stats[w][r].l * fast_exp2(sm.stats[w][r].m_sum - all.m_sum);
           if (whole) {
             const int rr = d.row_tile * R + r;
             const int64_t row = d.row0 + rr / a.group;
             const int head = d.head * a.group + rr % a.group;
-            const float inv = l == 0.f ? 0.f : 1.f / l;
+            const float inv = all.l == 0.f ? 0.f : 1.f / all.l, factor = output_factor<T::FP8>(all);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = nan_if_infinite<T::FP8>(x[i]) * inv;
+            for (int i = 0; i < 8; ++i) x[i] = nan_if_infinite<T::FP8>(x[i]) * inv * factor;
             uint4 v;
             v.x = pack_bf16(x[0], x[1]), v.y = pack_bf16(x[2], x[3]);
             v.z = pack_bf16(x[4], x[5]), v.w = pack_bf16(x[6], x[7]);
             *reinterpret_cast<uint4*>(a.out.data + row * a.out.stride_row + head * a.out.stride_head + c0 + col) = v;
-            if (a.lse != nullptr && c0 + col == 0) a.lse[row * a.lse_stride_row + head * a.lse_stride_head] = row_lse<T::FP8>(top, l);
+            if (a.lse != nullptr && c0 + col == 0) a.lse[row * a.lse_stride_row + head * a.lse_stride_head] = row_lse(all);
           } else {
             float4* dst = reinterpret_cast<float4*>(args.parts.sums + ((int64_t)slot * R + r) * D + c0 + col);
             dst[0] = make_float4(x[0], x[1], x[2], x[3]);
             dst[1] = make_float4(x[4], x[5], x[6], x[7]);
-            if (c0 + col == 0) args.parts.stats[slot * R + r] = make_float2(top, l);
+            if (c0 + col == 0) args.parts.stats[slot * R + r] = make_float4(all.m, all.m_sum, all.l, 0.f);
           }
         }
         if (!join.wait(ab)) return;
