@@ -143,6 +143,15 @@ __device__ __forceinline__ float output_factor(const RowStats& s) {
   return FP8 ? fast_exp2(above_weights(-s.m, s.m_sum)) * (1.f / kWiden) : 1.f;
 }
 
+// 8 bits: factor from a row's accumulated products to base-2 logits.  Keys of the smallest scale under a tiny query take it below fp32's
+// range, where it would make NaN of the -inf of masked keys, and the largest beyond it, where it would of zeros: it stays inside.
+__device__ __forceinline__ float logit_factor(float k_scale, float q_factor) {
+  float f;                                               // a NaN scale stays one
+  asm("max.NaN.f32 %0, %1, 0f00800000;" : "=f"(f) : "f"(k_scale * q_factor));
+  asm("min.NaN.f32 %0, %1, 0f7F7FFFFF;" : "=f"(f) : "f"(f));
+  return f;
+}
+
 // Log-sum-exp (natural) of a row.
 __device__ __forceinline__ float row_lse(const RowStats& s) { return s.l == 0.f ? -INFINITY : (s.m_sum + log2f(s.l)) * kLn2; }
 

@@ -650,7 +650,7 @@ __device__ __forceinline__ void softmax_rows(const PromptArgs& args, Smem& sm, u
           const TileInfo& info = sm.info[(info_at + j) % kInfo];
           if (j == 0) qf = p.q_factor[r];
 #pragma unroll
-          for (int g = 0; g < 2; ++g) f[g] = info.k_scale[g] * qf, add[g] = info.v_log2[g];
+          for (int g = 0; g < 2; ++g) f[g] = logit_factor(info.k_scale[g], qf), add[g] = info.v_log2[g];
         } else {
 #pragma unroll
           for (int g = 0; g < 2; ++g) f[g] = a.c, add[g] = 0.f;

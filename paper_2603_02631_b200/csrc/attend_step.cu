@@ -609,7 +609,7 @@ __device__ __forceinline__ void compute_tiles(const StepArgs& args, SmallSmem& s
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          f[nt][e] = T::FP8 ? k_scale * qf[nt][e] : k_scale;
+          f[nt][e] = T::FP8 ? logit_factor(k_scale, qf[nt][e]) : k_scale;
           float t = fmaxf(z[0][nt][e], z[0][nt][2 + e]);
 #pragma unroll
           for (int kt = 1; kt < KT; ++kt) t = max3(t, z[kt][nt][e], z[kt][nt][2 + e]);
