@@ -58,6 +58,11 @@ const at::Tensor& device_tensor(PyObject* o, at::ScalarType dtype, const char* n
   return t;
 }
 
+// A tensor that a call reads or writes next to `first`, which fixes the call's device.
+void on_device_of(const at::Tensor& first, const at::Tensor& t, const char* first_name, const char* name) {
+  if (t.device() != first.device()) raise(PyExc_ValueError, std::string(name) + " is on another device than " + first_name);
+}
+
 // Attribute names, interned once.
 struct Names {
   PyObject *importance, *lse, *chunk_scores, *kept, *out_ids, *out_pos, *tok_spans, *char_spans, *counts, *dev_status, *workspace, *chunk,
@@ -109,7 +114,8 @@ struct Inputs {
 };
 
 // Checks q and the layers' key tensors; the first prompt of a call fixes the shape.  `n_paged`: tokens of a paged prompt.  `aux`: the
-// block table (paged), the key scales (8 bits), or a tuple of the block table and a sequence of the layers' scales (both).
+// block table (paged), the key scales (8 bits), or a tuple of the block table and a sequence of the layers' scales (both; these lie on
+// q's device, which is looked at before any pointer is).
 void read_inputs(Kind kind, PyObject* q_obj, PyObject* layers_obj, PyObject* aux_obj, int64_t n_paged, double scale, bool first,
                  spf_shape* shape, Inputs* in) {
   const at::Tensor& q = device_tensor(q_obj, at::kBFloat16, "q");
@@ -138,11 +144,12 @@ void read_inputs(Kind kind, PyObject* q_obj, PyObject* layers_obj, PyObject* aux
     raise(PyExc_ValueError, "q must be contiguous [L, Hq, m, d], the same shape for all prompts");
   if (count != shape->n_layers) raise(PyExc_ValueError, "k_layers must hold one tensor per layer");
   in->layers.resize((size_t)count);
-  in->held.reserve((size_t)count + 2);
+  in->held.reserve((size_t)(kind == kPagedFp8 ? 2 * count : count) + 2);
   in->held.push_back(q);
   for (Py_ssize_t l = 0; l < count; ++l) {
     const at::Tensor& kl = device_tensor(items[l], dtype, "k_layers[l]");
     in->held.push_back(kl);
+    if (kind == kPagedFp8) on_device_of(q, kl, "q", "k_pools[l]");
     bool fine = kl.dim() == dims && kl.sizes() == k0.sizes() && kl.size(dims - 1) == shape->head_dim && hkv == shape->n_kv_heads;
     if (paged) fine = fine && kl.is_contiguous();
     else fine = fine && kl.stride(2) == 1 && kl.strides() == k0.strides();
@@ -150,9 +157,7 @@ void read_inputs(Kind kind, PyObject* q_obj, PyObject* layers_obj, PyObject* aux
       raise(PyExc_ValueError, kind == kPaged      ? "every pool must be contiguous bf16 [n_pool_blocks, Hkv, block_tokens, d]"
                               : kind == kPagedFp8 ? "every pool must be contiguous uint8 [n_pool_blocks, Hkv, block_tokens, d]"
                                                   : "every k_layers[l] must be [Hkv, N, d] with a contiguous last dim and equal strides");
-    in->layers[(size_t)l] = kl.data_ptr();
   }
-  in->q = q.data_ptr();
   if (paged) {
     PyObject* table_obj = aux_obj;
     if (kind == kPagedFp8) {
@@ -165,12 +170,13 @@ void read_inputs(Kind kind, PyObject* q_obj, PyObject* layers_obj, PyObject* aux
       for (Py_ssize_t l = 0; l < count; ++l) {
         const at::Tensor& t = device_tensor(PySequence_Fast_GET_ITEM(scales.p, l), at::kFloat, "k_scales[l]");
         in->held.push_back(t);
+        on_device_of(q, t, "q", "k_scales[l]");
         if (t.dim() != 3 || !t.is_contiguous() || t.size(0) != k0.size(0) || t.size(1) != hkv || t.size(2) != k0.size(2) / SPF_KV_SCALE_TOKENS)
           raise(PyExc_ValueError, "every k_scales[l] must be contiguous fp32 [n_pool_blocks, Hkv, block_tokens / 64]");
-        in->scales.push_back(t.data_ptr<float>());
       }
     }
     const at::Tensor& table = device_tensor(table_obj, at::kInt, "block_table");
+    if (kind == kPagedFp8) on_device_of(q, table, "q", "block_table");
     in->n = n_paged;
     in->block_tokens = (int)k0.size(2);
     in->pool_blocks = k0.size(0);
@@ -191,6 +197,10 @@ void read_inputs(Kind kind, PyObject* q_obj, PyObject* layers_obj, PyObject* aux
       in->held.push_back(scales);
     }
   }
+  in->q = q.data_ptr();
+  for (size_t l = 0; l < (size_t)count; ++l) in->layers[l] = in->held[1 + l].data_ptr();
+  if (kind == kPagedFp8)
+    for (size_t l = 0; l < (size_t)count; ++l) in->scales.push_back(in->held[1 + count + l].data_ptr<float>());
 }
 
 // What a Selector brings for one prompt, and the prompt's token arrays (`held`: as in Inputs).
@@ -482,8 +492,7 @@ PyObject* compress_host(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
 struct Held {
   std::vector<at::Tensor> tensors;
   const at::Tensor& keep(const at::Tensor& t, const char* name) {
-    if (!tensors.empty() && t.device() != tensors.front().device())
-      raise(PyExc_ValueError, std::string(name) + " is on another device than the cache");
+    if (!tensors.empty()) on_device_of(tensors.front(), t, "the cache", name);
     tensors.push_back(t);
     return tensors.back();
   }
@@ -610,26 +619,36 @@ PyObject* kv_append(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
   }
 }
 
-// The prompts of a call on 8-bit block pools (PagedFp8PromptBuffers).
+// The prompts of a call on 8-bit block pools (PagedFp8PromptBuffers), all of whose tensors lie on the first one's device.
 struct PagedFp8Call {
   spf_shape shape{};
   std::vector<Inputs> in;
   std::vector<spf_paged_fp8_prompt> prompts;
-  std::vector<at::Tensor> held;
-  PagedFp8Call(PyObject* list, double scale) {
+  std::vector<at::Tensor> held;                // the prompts' q, then the outputs
+  // `workspace` and `status`: those of the call, undefined where it has none
+  PagedFp8Call(PyObject* list, double scale, const at::Tensor& workspace = at::Tensor(), const at::Tensor& status = at::Tensor()) {
     Ref seq(PySequence_Fast(list, "prompts must be a sequence"));
     const size_t count = (size_t)PySequence_Fast_GET_SIZE(seq.p);
     if (count == 0) raise(PyExc_IndexError, "no prompts");
     in.resize(count);
     prompts.resize(count);
+    held.reserve(3 * count);
+    for (size_t i = 0; i < count; ++i) {
+      held.push_back(attr_tensor(PySequence_Fast_GET_ITEM(seq.p, (Py_ssize_t)i), N.q, at::kBFloat16, "q"));
+      on_device_of(held.front(), held.back(), "the first prompt's", "q");
+    }
+    if (workspace.defined()) on_device_of(held.front(), workspace, "q", "workspace");
+    if (status.defined()) on_device_of(held.front(), status, "q", "dev_status");
     for (size_t i = 0; i < count; ++i) {
       PyObject* o = PySequence_Fast_GET_ITEM(seq.p, (Py_ssize_t)i);
-      const Ref q(attr(o, N.q)), pools(attr(o, N.k_pools)), table(attr(o, N.block_table)), scales(attr(o, N.k_scales));
+      const Ref q(THPVariable_Wrap(held[i])), pools(attr(o, N.k_pools)), table(attr(o, N.block_table)), scales(attr(o, N.k_scales));
       const Ref aux(PyTuple_Pack(2, table.p, scales.p));
       const int64_t n = attr_int(o, N.n_tokens);
       if (n < 0) raise(PyExc_ValueError, "n_tokens must not be negative");
-      read_inputs(kPagedFp8, q.p, pools.p, aux.p, n, scale, i == 0, &shape, &in[i]);
       const at::Tensor importance = attr_tensor(o, N.importance, at::kFloat, "importance"), lse = attr_tensor_or_none(o, N.lse, at::kFloat, "lse");
+      on_device_of(held[i], importance, "q", "importance");
+      if (lse.defined()) on_device_of(held[i], lse, "q", "lse");
+      read_inputs(kPagedFp8, q.p, pools.p, aux.p, n, scale, i == 0, &shape, &in[i]);
       if (importance.numel() != n || !importance.is_contiguous()) raise(PyExc_ValueError, "block_table or importance has the wrong size");
       if (lse.defined() && (lse.numel() != (int64_t)shape.n_layers * shape.n_q_heads * shape.n_lookahead || !lse.is_contiguous()))
         raise(PyExc_ValueError, "lse must be contiguous fp32 [L, Hq, m]");
@@ -665,11 +684,12 @@ PyObject* score_paged_fp8(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
     if (n_args != 5) raise(PyExc_TypeError, "score_paged_fp8 takes 5 arguments");
     const double scale = PyFloat_AsDouble(args[2]);
     if (PyErr_Occurred()) throw PyFailure{};
-    const PagedFp8Call call(args[0], scale);
     const at::Tensor ws = tensor(args[1], "workspace");
-    if (!ws.is_cuda()) raise(PyExc_TypeError, "workspace must be a CUDA tensor");
+    if (!ws.is_cuda() || !ws.is_contiguous()) raise(PyExc_TypeError, "workspace must be a contiguous CUDA tensor");
     at::Tensor status;
     if (args[3] != Py_None) status = device_tensor(args[3], at::kInt, "dev_status");
+    if (status.defined() && status.numel() < 1) raise(PyExc_ValueError, "dev_status must hold one int32");
+    const PagedFp8Call call(args[0], scale, ws, status);
     const c10::cuda::CUDAGuard guard(call.held.front().device());      // the prompts' device, not the current one
     void* stream = stream_of(args[4]);
     void* ws_ptr = ws.data_ptr();
