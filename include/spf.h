@@ -293,7 +293,7 @@ typedef struct {
  * Appends a step's keys and values to the cache, rotating keys (and queries) on the way.
  *   k, v          bf16, n_kv_heads heads a row
  *   q, q_out      bf16, n_q_heads heads a row: the rotated queries go to q_out, which may be q itself (same strides) and must
- *                 not overlap it otherwise; both NULL: the step's queries are handled elsewhere
+ *                 overlap neither it otherwise nor k or v; both NULL: the step's queries are handled elsewhere
  *   rope          NULL: nothing is rotated (q, where given, is copied)
  * bf16 pools: rotated values are rounded to bf16 once.  8-bit pools, for each group of SPF_KV_SCALE_TOKENS tokens and head that
  * receives tokens: scale = the smallest power of two that keeps the new tokens' finite values within 448 times it (at least

@@ -81,7 +81,7 @@ extern "C" int32_t spf_attend(const spf_kv_cache* cache, const spf_kv_step* step
   st = check_rows(who, "q", q, n_q_heads, cache->head_dim, false, &a.q);
   if (st == SPF_OK) st = check_rows(who, "out", out, n_q_heads, cache->head_dim, true, &a.out);
   if (st != SPF_OK) return st;
-  if (q->data == out->data) return fail(SPF_ERR_INVALID_ARG, "%s: out must not be q", who);
+  if (rows_meet(a.q, n_q_heads, a.out, n_q_heads, step->n_rows, cache->head_dim)) return fail(SPF_ERR_INVALID_ARG, "%s: out overlaps q", who);
   const float scale = softmax_scale > 0.f ? softmax_scale : 1.0f / std::sqrt((float)cache->head_dim);
   a.c = scale * kLog2e;
   if (!std::isfinite(a.c)) return fail(SPF_ERR_INVALID_ARG, "%s: softmax_scale is too large", who);

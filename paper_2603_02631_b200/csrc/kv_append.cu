@@ -511,6 +511,32 @@ int32_t check_rows(const char* who, const char* name, const spf_rows* r, int n_h
   return SPF_OK;
 }
 
+// Slices of one buffer lie in one range of memory without meeting, so ranges alone decide only where they are apart.  Else each run of a's
+// elements is held against b's rows: of a row i of b, of w elements, [i S, i S + w), the first that ends behind the run's start decides.
+// With equal strides of rows (slices of one buffer) one row of a stands for all, rows of b before it being negative ones.
+bool rows_meet(const RowsView& a, int a_heads, const RowsView& b, int b_heads, int n_rows, int head_dim) {
+  struct Runs {
+    int64_t heads, width, stride_head, extent;
+  };
+  const int64_t rows = n_rows;
+  auto runs_of = [&](const RowsView& v, int heads) {
+    const bool joined = heads == 1 || v.stride_head == head_dim;       // a row's heads are one run
+    return Runs{joined ? 1 : heads, joined ? (int64_t)heads * head_dim : head_dim, v.stride_head, (rows - 1) * v.stride_row + (heads - 1) * v.stride_head + head_dim};
+  };
+  const Runs ra = runs_of(a, a_heads), rb = runs_of(b, b_heads);
+  const int64_t apart = (int64_t)(reinterpret_cast<intptr_t>(a.data) - reinterpret_cast<intptr_t>(b.data)) / (int64_t)sizeof(__nv_bfloat16);
+  if (apart >= rb.extent || apart + ra.extent <= 0) return false;
+  const bool same = a.stride_row == b.stride_row;
+  for (int64_t r = 0; r < (same || a.stride_row == 0 ? 1 : rows); ++r)
+    for (int64_t h = 0; h < ra.heads; ++h)
+      for (int64_t g = 0; g < rb.heads; ++g) {
+        const int64_t x = apart + r * a.stride_row + h * ra.stride_head - g * rb.stride_head, y = x - rb.width, S = b.stride_row;   // S > 0: b is written
+        const int64_t first = std::max((y >= 0 ? y / S : -((-y + S - 1) / S)) + 1, same ? 1 - rows : 0);
+        if (first < rows && first * S < x + ra.width) return true;
+      }
+  return false;
+}
+
 }  // namespace spf
 
 using namespace spf;
@@ -533,8 +559,12 @@ extern "C" int32_t spf_kv_append(const spf_kv_cache* cache, const spf_kv_step* s
     st = check_rows(who, "q", q, n_q_heads, cache->head_dim, false, &a.q);
     if (st == SPF_OK) st = check_rows(who, "q_out", q_out, n_q_heads, cache->head_dim, true, &a.q_out);
     if (st != SPF_OK) return st;
-    if (q->data == q_out->data && (q->stride_row != q_out->stride_row || q->stride_head != q_out->stride_head))
-      return fail(SPF_ERR_INVALID_ARG, "%s: q_out overlaps q with other strides", who);
+    const bool in_place = q->data == q_out->data && q->stride_row == q_out->stride_row && q->stride_head == q_out->stride_head;
+    if (!in_place && rows_meet(a.q, n_q_heads, a.q_out, n_q_heads, step->n_rows, cache->head_dim))
+      return fail(SPF_ERR_INVALID_ARG, "%s: q_out overlaps q and is not q", who);
+    if (rows_meet(a.k, cache->n_kv_heads, a.q_out, n_q_heads, step->n_rows, cache->head_dim) ||
+        rows_meet(a.v, cache->n_kv_heads, a.q_out, n_q_heads, step->n_rows, cache->head_dim))
+      return fail(SPF_ERR_INVALID_ARG, "%s: q_out overlaps k or v", who);
     a.n_q_heads = n_q_heads;
   }
   if (rope != nullptr) {
