@@ -29,17 +29,6 @@ __device__ __forceinline__ void report_cache(int32_t* dev_status) {
   if (dev_status != nullptr) atomicCAS(dev_status, 0, (int32_t)SPF_ERR_CACHE);
 }
 
-// The sequence of a row: the last one that starts at or before it (-1: none does).  Empty sequences start where the next does.
-__device__ __forceinline__ int sequence_of(const StepView& st, int row) {
-  int lo = 0, hi = st.n_seqs;                       // the answer is below hi, and at least lo - 1
-  while (lo < hi) {
-    const int mid = (lo + hi) >> 1;
-    if (__ldg(st.row_start + mid) <= row) lo = mid + 1;
-    else hi = mid;
-  }
-  return lo - 1;
-}
-
 // Pool block of a token, -1 where the table or the pool has no such place.
 __device__ __forceinline__ int64_t pool_block(const KvView& kv, const StepView& st, int seq, int pos) {
   const int j = pos / kv.block_tokens;
