@@ -718,7 +718,8 @@ PyObject* attend_workspace_bytes(PyObject*, PyObject* const* args, Py_ssize_t n_
     if (q.dim() != 3) raise(PyExc_ValueError, "q must be [rows, heads, d] of the step and the cache, the last dimension contiguous");
     const int64_t max_new = attr_int(args[1], N.max_new);
     const c10::cuda::CUDAGuard guard(held.tensors.front().device());
-    return PyLong_FromSize_t(spf_attend_workspace_bytes(&cache, (int32_t)q.size(1), (int32_t)std::min<int64_t>(max_new, INT32_MAX)));
+    if (max_new < 1 || max_new > INT32_MAX || q.size(1) > INT32_MAX) raise(PyExc_ValueError, "max_new must be positive, and the step smaller");
+    return PyLong_FromSize_t(spf_attend_workspace_bytes(&cache, (int32_t)q.size(1), (int32_t)max_new));
   } catch (const PyFailure&) {
     return nullptr;
   } catch (const std::exception& e) {
