@@ -18,8 +18,10 @@
 // rows and queries as columns; a weight is wanted the other way round, which one movmatrix per 8 x 8 does.
 //
 // The reference m_r moves only when a logit exceeds it by 8 (2^8 is far from any format's limit): most tiles need no exchange
-// of maxima and no rescaling of the output.  Weights are rounded to the format of the second product's operands: bf16 (8 bits;
-// the output is bf16 too) over bf16 values, fp16 (11 bits) over 8-bit ones; their sum l is taken in fp32 before that.
+// of maxima and no rescaling of the output.  Weights are rounded to the format of the second product's operands, fp16 (11 bits) over
+// 8-bit values, bf16 (8 bits; the output is bf16 too) over bf16 ones; their sum l is taken in fp32 before that.  Up to 8 rows over a bf16
+// cache, where the read leaves time, weights are two bf16 terms (off by 2^-16): 16 sequences of 4 to 32k tokens take 172 us with either
+// one or two, one short prompt 11.2 instead of 10.8.  Two terms would cost 32 rows 8 % (64 dimensions, bf16) and 8-bit caches 16 %.
 //
 // 8 bits, keys: multiplied as they are (m16n8k32, E4M3) by queries in two terms, E4M3 and E5M2: q 2^e = hi + lo, with the power of
 // two e of a row that takes its largest element to (224, 448].  Exact for elements within 2^13 of that one, off by at most 2^-21 of
@@ -70,6 +72,7 @@ struct Traits {
   static constexpr bool LEND = R >= 16 && R * D < 4096;               // registers move between warpgroups
   static constexpr int THREADS = LEND ? 2 * kWarps * 32 : (kWarps + 1) * 32;
   static constexpr int CTAS = R == 8 ? 3 : 2;                         // per SM
+  static constexpr int WTERMS = !FP8 && R == 8 ? 2 : 1;               // of a weight
   static constexpr bool QREGS = NT <= 2;                              // queries stay in registers
   static constexpr int ROWB = FP8 ? D : 2 * D, SPAN = ROWB < 128 ? ROWB : 128;
   static constexpr int TILE = KEYS * ROWB, STAGE = 2 * TILE;
@@ -406,10 +409,10 @@ struct Seen {
   int first, end, all;
 };
 
-// out += values . weights of the warp's keys from `key` (of the tile, which begins at key0) on, p[kt][nt] being the weights of
-// sixteen keys and eight rows.  GUARD: the tile has keys outside [first, end), whose values are taken as zeros.
+// out += values . weights of the warp's keys from `key` (of the tile, which begins at key0) on, p[t][kt][nt] being a term of the weights
+// of sixteen keys and eight rows.  GUARD: the tile has keys outside [first, end), whose values are taken as zeros.
 template <class T, bool GUARD>
-__device__ __forceinline__ void add_values(State<T>& st, const uint32_t (&p)[T::KT][T::NT][2], uint32_t v_tile, int key, int key0, const Seen& seen,
+__device__ __forceinline__ void add_values(State<T>& st, const uint32_t (&p)[T::WTERMS][T::KT][T::NT][2], uint32_t v_tile, int key, int key0, const Seen& seen,
                                            int lane) {
   constexpr int kStep = T::FP8 ? 2 : 1;
 #pragma unroll
@@ -429,7 +432,9 @@ __device__ __forceinline__ void add_values(State<T>& st, const uint32_t (&p)[T::
 #pragma unroll
       for (int i = 0; i < kStep; ++i)
 #pragma unroll
-        for (int nt = 0; nt < T::NT; ++nt) mma16<T::FP8>(st.o[m0 + i][nt], v[i], p[kt][nt][0], p[kt][nt][1]);
+        for (int nt = 0; nt < T::NT; ++nt)
+#pragma unroll
+          for (int t = 0; t < T::WTERMS; ++t) mma16<T::FP8>(st.o[m0 + i][nt], v[i], p[t][kt][nt][0], p[t][kt][nt][1]);
     }
 }
 
@@ -454,7 +459,7 @@ __device__ __noinline__ bool odd_values(uint32_t v_tile, int key, int key0, int 
 
 // add_values where there are such: row by row, each with the values that it sees.
 template <class T>
-__device__ __forceinline__ void add_odd_values(State<T>& st, const uint32_t (&p)[T::KT][T::NT][2], uint32_t v_tile, int key, int key0, const Seen& seen,
+__device__ __forceinline__ void add_odd_values(State<T>& st, const uint32_t (&p)[T::WTERMS][T::KT][T::NT][2], uint32_t v_tile, int key, int key0, const Seen& seen,
                                                const TileDesc& d, int group, int causal, int row_in_triple, int lane) {
   constexpr int kStep = T::FP8 ? 2 : 1;
 #pragma unroll 1
@@ -476,7 +481,8 @@ __device__ __forceinline__ void add_odd_values(State<T>& st, const uint32_t (&p)
             uint32_t vr[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) vr[e] = keep_keys(v[i][e], base + value_key<T>(lane, e, 0), base + value_key<T>(lane, e, 1), seen.first, hi);
-            mma16<T::FP8>(part, vr, mine ? p[kt][nt][0] : 0u, mine ? p[kt][nt][1] : 0u);
+#pragma unroll
+            for (int t = 0; t < T::WTERMS; ++t) mma16<T::FP8>(part, vr, mine ? p[t][kt][nt][0] : 0u, mine ? p[t][kt][nt][1] : 0u);
 #pragma unroll
             for (int e = 0; e < 4; ++e)
               if (2 * (lane & 3) + (e & 1) == r) st.o[m0 + i][nt][e] += part[e];
@@ -648,7 +654,7 @@ __device__ __forceinline__ void compute_tiles(const StepArgs& args, SmallSmem& s
             }
           }
       }
-      uint32_t p[KT][NT][2];
+      uint32_t p[T::WTERMS][KT][NT][2];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         float off[2], sum[2] = {0.f, 0.f};
@@ -661,7 +667,9 @@ __device__ __forceinline__ void compute_tiles(const StepArgs& args, SmallSmem& s
             const float x = fast_exp2(fmaf(z[kt][nt][2 * h], f[nt][0], off[0])), y = fast_exp2(fmaf(z[kt][nt][2 * h + 1], f[nt][1], off[1]));
             sum[0] += x;
             sum[1] += y;
-            p[kt][nt][h] = transpose8(T::FP8 ? pack_f16(x, y) : pack_bf16(x, y));
+            const uint32_t w = T::FP8 ? pack_f16(x, y) : pack_bf16(x, y);
+            p[0][kt][nt][h] = transpose8(w);
+            if constexpr (T::WTERMS == 2) p[1][kt][nt][h] = transpose8(pack_bf16(x - __uint_as_float(w << 16), y - __uint_as_float(w & 0xffff0000u)));
           }
 #pragma unroll
         for (int e = 0; e < 2; ++e) {

@@ -69,11 +69,12 @@ def reference(s, b, head, first=0, causal=True, scale=None, tokens=None):
     return torch.einsum("tgn,nd->tgd", p, v), lse, torch.einsum("tgn,nd->tgd", p, v.abs()), terms
 
 
-def check(s, out, lse, causal=True, first=None, scale=None, heads=None, tokens=None):
+def check(s, out, lse, causal=True, first=None, scale=None, heads=None, tokens=None, operand=None):
     """Compares rows of every sequence with the reference.  Tolerances as derived in test_gpu_attend.compare: a logit is an fp32 sum
     of exact products, off by less than 2^-16 sum |scale q k|; weights by that twice (the sum of them has it too), by ex2's 2^-21 and by
     half a step of the second product's operands (bf16 2^-8, fp16 2^-11); the output by half a step of bf16."""
-    operand = 2.0 ** -8 if s.k_scale is None else 2.0 ** -11
+    if operand is None:
+        operand = 2.0 ** -8 if s.k_scale is None else 2.0 ** -11
     group = s.Hq // s.Hkv
     for b, new in enumerate(s.new):
         if new == 0:
