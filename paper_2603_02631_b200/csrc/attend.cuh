@@ -32,7 +32,7 @@ __device__ __forceinline__ SeqSpan seq_span(const AttendArgs& a, int b) {
   s.row0 = max(__ldg(a.step.row_start + b), 0);
   s.n_new = max(min(__ldg(a.step.row_start + b + 1), a.step.n_rows) - s.row0, 0);
   const int len = __ldg(a.step.seq_lens + b);
-  s.pos0 = len - (__ldg(a.step.row_start + b + 1) - s.row0);
+  s.pos0 = place_from_end(len, (int64_t)__ldg(a.step.row_start + b + 1) - s.row0);
   s.end = max((int)min((int64_t)len, (int64_t)a.step.table_stride * a.kv.block_tokens), 0);
   s.first = a.first_keys != nullptr ? min(max(__ldg(a.first_keys + b), 0), s.end) : 0;
   if (s.n_new > 0 && (s.end != len || s.pos0 < 0)) report_cache(a.dev_status);

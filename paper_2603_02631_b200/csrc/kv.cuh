@@ -29,6 +29,10 @@ __device__ __forceinline__ void report_cache(int32_t* dev_status) {
   if (dev_status != nullptr) atomicCAS(dev_status, 0, (int32_t)SPF_ERR_CACHE);
 }
 
+// Place in its sequence of a token that has `behind` tokens from it on: below zero where the sequence is shorter than that, and kept where
+// 2^30 rows more stay below zero, whatever the length says.
+__device__ __forceinline__ int place_from_end(int len, int64_t behind) { return (int)min(max(len - behind, -(int64_t)(1 << 30)), (int64_t)0x7fffffff); }
+
 // Pool block of a token, -1 where the table or the pool has no such place.
 __device__ __forceinline__ int64_t pool_block(const KvView& kv, const StepView& st, int seq, int pos) {
   const int j = pos / kv.block_tokens;

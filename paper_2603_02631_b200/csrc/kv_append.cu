@@ -105,7 +105,7 @@ __device__ __forceinline__ void rotate(float (&a)[8], float (&b)[8], const Angle
 // Position in the sequence and row of the angles' table; false (and reported) where one lies outside.
 __device__ __forceinline__ bool place_of(const AppendArgs& a, int seq, int row, int* pos, int64_t* angle_row) {
   const int start = __ldg(a.step.row_start + seq), end = __ldg(a.step.row_start + seq + 1), len = __ldg(a.step.seq_lens + seq);
-  *pos = len - (end - row);
+  *pos = place_from_end(len, (int64_t)end - row);
   *angle_row = a.positions != nullptr ? __ldg(a.positions + row) : *pos;
   const bool fine = row >= start && *pos >= 0 && (a.rope == nullptr || (*angle_row >= 0 && *angle_row < a.n_positions));
   if (!fine) report_cache(a.dev_status);
@@ -272,11 +272,12 @@ __device__ __forceinline__ void fill_group(const AppendArgs& a, int index) {
   if (seq < 0) return;
   const int start = __ldg(a.step.row_start + seq), behind = __ldg(a.step.row_start + seq + 1), len = __ldg(a.step.seq_lens + seq);
   const int end = min(behind, a.step.n_rows);
-  const int old_len = len - (behind - start);        // tokens before the step
-  const int group = max(old_len, 0) / kScaleTokens + slot - (start / kScaleTokens + 2 * seq);
-  const int first = group * kScaleTokens;           // position of the group's first token
-  const int lo = max(first, max(old_len, 0)), hi = min(first + kScaleTokens, min(len, old_len + (end - start)));
-  if (start < 0 || lo >= hi) {
+  const int old_len = place_from_end(len, (int64_t)behind - start);      // tokens before the step
+  // the group's first token, and its tokens of the step, by position (64 bits: a length may be anything)
+  const int64_t from = ((int64_t)(max(old_len, 0) / kScaleTokens) + slot - (start / kScaleTokens + 2 * seq)) * kScaleTokens;
+  const int64_t begin = max(from, (int64_t)max(old_len, 0)), upto = min(from + kScaleTokens, min((int64_t)len, (int64_t)old_len + end - start));
+  const int first = (int)from, lo = (int)begin, hi = (int)upto;
+  if (start < 0 || begin >= upto) {
     if (threadIdx.x == 0 && old_len < 0) report_cache(a.dev_status);
     return;
   }
