@@ -708,7 +708,8 @@ class KvCache:
 @dataclasses.dataclass
 class KvStep:
     """The new tokens of a step (see spf_kv_step in include/spf.h): rows row_start[b] .. row_start[b + 1] - 1 of the step's arrays
-    are the last of sequence b's seq_lens[b] tokens."""
+    are the last of sequence b's seq_lens[b] tokens.  A step of more than one new token a sequence says so in ``max_new``: spf_attend
+    picks its kernel by it, and a chunk of 2048 tokens that is passed as a step of one is right but takes six times as long."""
     row_start: torch.Tensor                   # int32 [n_seqs + 1]
     seq_lens: torch.Tensor                    # int32 [n_seqs]
     block_table: torch.Tensor                 # int32 [n_seqs, blocks]

@@ -187,8 +187,13 @@ int32_t attend_join_launch(const AttendArgs& a, const AttendParts& parts, int ro
 size_t attend_prompt_workspace_bytes(const spf_kv_cache* cache, int sm_count);
 int32_t attend_prompt_launch(const AttendArgs& a, const spf_kv_cache* cache, int sm_count, void* workspace, cudaStream_t stream);
 // Rows a key head and sequence up to which the first is taken.  Over 131072 keys and 8 heads, first against second, 32 rows: 61 us
-// against 80 (64 dimensions), 76 against 88 (64, 8 bits), 108 against 112 (128), 157 against 139 (128, 8 bits, whose values' widening
-// then takes longer than their read); 64 rows: 99 against 85, 128 against 95, 187 against 118, 281 against 148.
+// against 81 (64 dimensions), 80 against 91 (64, 8 bits), 109 against 114 (128), 157 against 139 (128, 8 bits, whose values' widening
+// then takes longer than their read); 64 rows: 99 against 85, 134 against 97, 189 against 119, 281 against 148.  32 rows elsewhere, 8 heads,
+// in the same order but for the last form, of which the first kernel has none: 32 sequences of 2000 keys 42 against 53, 52 against 63,
+// 73 against 73; of 16000 keys 176 against 269, 246 against 302, 375 against 445; 256 sequences of 500 keys 87 against 119, 122 against 142,
+// 165 against 153.  One sequence of 2000 keys and one of 16000 differ by 2 us or less but with 128 dimensions (18 against 16.5, 30 against 27).  With
+// one key head, over 2000 to 131072 keys of one sequence, the second is up to 9 us the quicker one (34 against 25: 128 dimensions, 16000).
+// 16 rows, 128 dimensions, 8 bits: 88 against 138 over 131072 keys, 288 against 473 for 32 sequences of 16000, 16 against 21 for one of 2000.
 inline int step_rows(const spf_kv_cache* cache) { return cache->k_scale != nullptr && cache->head_dim == 128 ? 16 : 32; }
 size_t attend_step_workspace_bytes(const spf_kv_cache* cache, int group, int max_new, int sm_count);
 int32_t attend_step_launch(const AttendArgs& a, const spf_kv_cache* cache, int max_new, int sm_count, void* workspace, cudaStream_t stream);

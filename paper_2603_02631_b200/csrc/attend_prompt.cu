@@ -13,7 +13,7 @@
 // last visible key, is cut into one part for each SM; parts of a triple meet in a second kernel.
 //
 // Two row tiles and 128 keys take about 3400 cycles at 128 dimensions, of which the tensor cores are busy 2048 and the exponential unit
-// 2048 (2048 new of 32k tokens: 510 us, 1050 TFLOP/s, at the clock that the power limit leaves).  Not taken, all slower there: a part
+// 2048 (2048 new of 32k tokens, calls back to back: 505 us, 1055 TFLOP/s, at the clock that the power limit leaves).  Not taken, all slower there: a part
 // of the exponentials as polynomials on the multiply-add units, products with the first half of the weights while the second is made,
 // logits read in two halves, exponentials of the two row tiles strictly in turns.
 //
