@@ -221,23 +221,31 @@ SPF_API int32_t spf_score_fp8(const spf_shape* shape, const spf_fp8_prompt* prom
  * is the pool that spf_score_paged (bf16) and spf_score_paged_fp8 (8 bits) score.
  *
  *   k_pool, v_pool     DEVICE, contiguous [n_pool_blocks][Hkv][block_tokens][d], 16-byte aligned; keys after the rotation.
- *                      bf16 when the scales are NULL, else E4M3 bytes (see spf_score_fp8)
- *   k_scale, v_scale   DEVICE fp32 [n_pool_blocks][Hkv][block_tokens / SPF_KV_SCALE_TOKENS]: what the bytes of that many
- *                      consecutive tokens of a block and head are multiplied by, positive and finite; both NULL: bf16 pools
+ *                      16 bits: bf16.  8 bits: E4M3 bytes (see spf_score_fp8).  4 bits: codes 0 ... 15, two to a byte ([...][d / 2] bytes),
+ *                      element 2 j in the low half of byte j, 2 j + 1 in the high one
+ *   k_scale, v_scale   16 bits: both NULL.
+ *                      8 bits: DEVICE fp32 [n_pool_blocks][Hkv][block_tokens / SPF_KV_SCALE_TOKENS]: what the bytes of that many
+ *                      consecutive tokens of a block and head are multiplied by, positive and finite.
+ *                      4 bits: DEVICE bf16 [n_pool_blocks][Hkv][block_tokens][d / SPF_KV_SCALE_DIMS], 16-byte aligned: an element is worth
+ *                      scale * (code - 8), the scale being that of its SPF_KV_SCALE_DIMS consecutive elements of the token; positive and
+ *                      finite, with at most five significant bits (an element then is a bf16 number)
  *   block_tokens       a positive multiple of 128
  *   head_dim           d: 64 or 128
+ *   bits               of an element: 16, 8 or 4; 0: 16 without scales, 8 with them
  * Limit: n_pool_blocks * Hkv * block_tokens < 2^31.
  */
 #define SPF_KV_SCALE_TOKENS 64
+#define SPF_KV_SCALE_DIMS 32
 typedef struct {
   void* k_pool;
   void* v_pool;
-  float* k_scale;
-  float* v_scale;
+  void* k_scale;
+  void* v_scale;
   int64_t n_pool_blocks;
   int32_t block_tokens;
   int32_t n_kv_heads;
   int32_t head_dim;
+  int32_t bits;
 } spf_kv_cache;
 
 /*
@@ -300,6 +308,9 @@ typedef struct {
  * 2^-100), and no smaller than the scale that tokens of the group from before the step have; where it grows, their bytes are
  * rounded again to the new scale (exact unless they become subnormal).  New values are rounded once, from fp32; infinities
  * become +-448 times the scale, NaN stays NaN (0x7F).
+ * 4-bit pools, for each SPF_KV_SCALE_DIMS elements x of a new token and head: scale = the smallest number of five significant bits that
+ * keeps the finite ones within 7 times it (at least 2^-100), code = 8 + x * (1 / scale) rounded to the nearest whole number, ties to
+ * even, -7 ... 7; fp32 throughout.  Infinities become +-7 times the scale, NaN makes the scale NaN.
  * A block that receives tokens belongs to one sequence of the step only (two that write the same block race).
  * Device conditions: SPF_ERR_CACHE in dev_status (may be NULL) for a row whose position, table row or block lies outside; that
  * row is left out, the others are not affected.
@@ -327,7 +338,9 @@ SPF_API int32_t spf_kv_append(const spf_kv_cache* cache, const spf_kv_step* step
  *                 contents irrelevant on entry, unspecified on exit.  Calls that share one must be ordered on one stream.
  * What the pools hold behind a sequence's tokens, or before its first key, does not matter.
  * Roundings: weights of the sum over values are bf16 over bf16 pools (16 bits with up to 8 rows a key head and sequence), fp16 over
- * 8-bit ones; the sum of the weights is fp32.
+ * 8-bit ones, bf16, with the values' scales in them, over 4-bit ones (from 33 rows on, 17 with 128 dimensions: as over bf16 pools); the
+ * sum of the weights is fp32.
+ * 4-bit pools: elements are exact.  Elements of a query should lie below 2^114 in magnitude, value scales within 2^-40 ... 2^50.
  * 8-bit pools: values of bytes times scales are exact; their scales should lie within 2^-100 ... 2^100.  Elements of a query row are exact
  * within 2^13 of its largest and off by at most 2^-21 of that below.  Weights below 2^-21 of the row's largest (each times its value
  * scale) are off by up to 2^-32 of it.

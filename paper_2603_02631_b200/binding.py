@@ -75,7 +75,7 @@ class _PagedFp8Prompt(ctypes.Structure):
 class _KvCache(ctypes.Structure):
     _fields_ = [("k_pool", ctypes.c_void_p), ("v_pool", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
                 ("n_pool_blocks", ctypes.c_int64), ("block_tokens", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
-                ("head_dim", ctypes.c_int32)]
+                ("head_dim", ctypes.c_int32), ("bits", ctypes.c_int32)]
 
 
 class _KvStep(ctypes.Structure):
@@ -698,10 +698,11 @@ def spf_compress_host(q: torch.Tensor, k_layers: Sequence[torch.Tensor], token_i
 
 @dataclasses.dataclass
 class KvCache:
-    """One layer's paged cache (see spf_kv_cache in include/spf.h): bf16 pools, or uint8 pools (E4M3 bytes) with their scales."""
-    k_pool: torch.Tensor                      # [n_pool_blocks, Hkv, block_tokens, d], contiguous
+    """One layer's paged cache (see spf_kv_cache in include/spf.h): bf16 pools, uint8 pools of E4M3 bytes with fp32 scales, or uint8 pools
+    of 4-bit codes, two to a byte, with bf16 scales."""
+    k_pool: torch.Tensor                      # [n_pool_blocks, Hkv, block_tokens, d], contiguous; 4 bits: d / 2 bytes
     v_pool: torch.Tensor
-    k_scale: Optional[torch.Tensor] = None    # fp32 [n_pool_blocks, Hkv, block_tokens / 64]
+    k_scale: Optional[torch.Tensor] = None    # fp32 [n_pool_blocks, Hkv, block_tokens / 64]; 4 bits: bf16 [..., block_tokens, d / 32]
     v_scale: Optional[torch.Tensor] = None
 
 

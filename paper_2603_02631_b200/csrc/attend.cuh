@@ -71,6 +71,13 @@ __device__ __forceinline__ void drain_copy(uint32_t bar, uint32_t parity) {
 
 // Tensor map of a pool: rows of d elements seen as spans of at most 128 bytes, `tile_rows` rows a copy.
 int32_t encode_pool_map(const char* who, const spf_kv_cache* cache, void* pool, int tile_rows, CUtensorMap* map);
+// 4 bits: of the scales of a pool, a row of the map being those of 128 tokens (blocks are multiples of them).
+int32_t encode_scale_map(const char* who, const spf_kv_cache* cache, void* scales, CUtensorMap* map);
+__device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map, int c0, int c1, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+               ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(bar)
+               : "memory");
+}
 
 // ---------------------------------------------------------------------------------------------- what both kernels compute with
 constexpr float kLazy = 8.f;            // how far logits may exceed their reference
@@ -194,7 +201,7 @@ int32_t attend_prompt_launch(const AttendArgs& a, const spf_kv_cache* cache, int
 // 165 against 153.  One sequence of 2000 keys and one of 16000 differ by 2 us or less but with 128 dimensions (18 against 16.5, 30 against 27).  With
 // one key head, over 2000 to 131072 keys of one sequence, the second is up to 9 us the quicker one (34 against 25: 128 dimensions, 16000).
 // 16 rows, 128 dimensions, 8 bits: 88 against 138 over 131072 keys, 288 against 473 for 32 sequences of 16000, 16 against 21 for one of 2000.
-inline int step_rows(const spf_kv_cache* cache) { return cache->k_scale != nullptr && cache->head_dim == 128 ? 16 : 32; }
+inline int step_rows(const spf_kv_cache* cache) { return cache_bits(cache) != 16 && cache->head_dim == 128 ? 16 : 32; }
 size_t attend_step_workspace_bytes(const spf_kv_cache* cache, int group, int max_new, int sm_count);
 int32_t attend_step_launch(const AttendArgs& a, const spf_kv_cache* cache, int max_new, int sm_count, void* workspace, cudaStream_t stream);
 

@@ -1,4 +1,4 @@
-// Attention of a step with many rows per key head (chunks of prompts) over the paged cache, bf16 or 8 bits: the formulas, masks and
+// Attention of a step with many rows per key head (chunks of prompts) over the paged cache, bf16, 8 or 4 bits: the formulas, masks and
 // references of the kernel for few rows, with the products on the big tensor-core instruction.
 //
 // A CTA works on 256 rows of a (sequence, key head), two tiles X of 128, against tiles of 128 keys.  Per tile of keys
@@ -21,7 +21,8 @@
 // (below), 12 copies, 13 issues the products.
 //
 // Queries: read once per triple by warps 8-11; 8 bits: as an E4M3 and an E5M2 term, as for few rows, so that 8-bit keys are
-// multiplied as they are.  Values of 8-bit caches are widened to fp16 by these warps between their copy and their product.
+// multiplied as they are.  Values of 8-bit caches are widened to fp16 by these warps between their copy and their product; keys and values of
+// 4-bit caches to bf16, which holds scale times (code - 8) exactly, so that everything else is as over a bf16 cache.
 // Values of bf16 caches go straight from the copy to the product, but for tiles at the ends of a sequence's range, where
 // what lies outside is cleared (a weight of zero would make NaN of NaN), and tiles whose last keys only later rows may see: values
 // there that are not finite are cleared and put down with their place, and the output's rows that do see them get them back.
@@ -37,20 +38,23 @@ constexpr int kSoftmaxRegs = 184, kOtherRegs = 72;    // of 128 a thread at laun
 constexpr int kInfo = 8;                              // tiles' scales kept: more than may be under way between copy and softmax
 constexpr int kNever = 0x7fffffff;
 
-template <int D_, bool FP8_>
+template <int D_, int BITS_>
 struct Traits {
   static constexpr int D = D_;
-  static constexpr bool FP8 = FP8_;
-  static constexpr int ROWB = FP8 ? D : 2 * D, SPAN = ROWB < 128 ? ROWB : 128;   // bytes of a cache row, and of the swizzle's span
+  static constexpr bool FP8 = BITS_ == 8, INT4 = BITS_ == 4;
+  static constexpr int ROWB = FP8 ? D : 2 * D, SPAN = ROWB < 128 ? ROWB : 128;   // bytes of a row of keys in the products, and of the swizzle's span
   static constexpr int QTILE = 128 * D * 2;                                     // bf16, or two 8-bit terms
   static constexpr int KTILE = kKeys * ROWB, V8TILE = FP8 ? kKeys * D : 0, VTILE = kKeys * D * 2;
   static constexpr int STAGES = D == 64 ? 3 : 2;
+  // 4 bits: a copied tile of keys or of values, the scales behind the codes, and how many of either are under way (one where there is no room
+  // for more: it is widened in a tenth of the time that the products of a tile take, which is left for the next copy)
+  static constexpr int PARTS = D / kScaleDims, CODES = kKeys * D / 2, RAW = INT4 ? CODES + kKeys * PARTS * 2 : 0, RAWS = D == 64 ? 3 : 1;
   static constexpr int QBUFS = D == 64 ? 2 : 1;                                 // where there is room, the next part's queries are fetched ahead
   // Tensor memory, 512 columns: S_X 128 each, O_X D each.  With 64 dimensions there is room for P_X (64 each) beside S_X, and the
   // next keys' logits are made while these are being turned into weights; with 128, P_X lies over S_X.
   static constexpr bool APART = D == 64;
   static constexpr uint32_t O_COL = 256, P_COL = APART ? 384 : 0, P_STEP = APART ? 64 : 128;
-  static constexpr int BYTES = QBUFS * 2 * QTILE + STAGES * (KTILE + V8TILE + VTILE);
+  static constexpr int BYTES = QBUFS * 2 * QTILE + STAGES * (KTILE + V8TILE + VTILE) + RAWS * 2 * RAW;
 };
 
 // What the copying warp tells the others about a part of a triple.
@@ -68,7 +72,7 @@ struct TileInfo {
 
 struct Smem {
   unsigned long long s_full[2], s_free[2], p_ready[2], o_done[2], o_free[2], q_ready[2], q_free[2], part_full[2], part_empty[2], values_done[2], mma_done;
-  unsigned long long k_full[3], k_empty[3], v_full[3], v_ready[3], v_empty[3], v8_empty[3];
+  unsigned long long k_full[3], k_empty[3], v_full[3], v_ready[3], v_empty[3], v8_empty[3], k4_full[3], k4_empty[3];
   TileInfo info[kInfo];
   Part part[2];
   int64_t scan[kThreads / 32];
@@ -84,6 +88,7 @@ constexpr int smem_bytes() { return T::BYTES + (int)sizeof(Smem) + 1024; }
 struct PromptArgs {
   AttendArgs a;
   CUtensorMap k_map, v_map;
+  CUtensorMap k_scale_map, v_scale_map;                // 4 bits
   AttendParts parts;
 };
 
@@ -209,6 +214,25 @@ __device__ __forceinline__ void copy_tiles(const PromptArgs& args, Smem& sm, uin
         }
       }
       for (int j = 0; j < min(32, count - j0); ++j, ++issued) {
+        if constexpr (T::INT4) {
+          const int raw = (int)(issued % T::RAWS);
+          const uint32_t before = ((uint32_t)(issued / T::RAWS) & 1u) ^ 1u;
+          if (!mbar_wait_warp(smem_u32(&sm.k4_empty[raw]), before, ab)) return;
+          if (lane == j) {
+            const uint32_t bar = smem_u32(&sm.k4_full[raw]), at = v_ring + 2 * raw * T::RAW;
+            mbar_expect_tx(bar, T::RAW);
+            tma_load_3d(at, &args.k_map, 0, row, 0, bar);
+            tma_load_2d(at + T::CODES, &args.k_scale_map, 0, row / kKeys, bar);
+          }
+          if (!mbar_wait_warp(smem_u32(&sm.v8_empty[raw]), before, ab)) return;
+          if (lane == j) {
+            const uint32_t bar = smem_u32(&sm.v_full[raw]), at = v_ring + (2 * raw + 1) * T::RAW;
+            mbar_expect_tx(bar, T::RAW);
+            tma_load_3d(at, &args.v_map, 0, row, 0, bar);
+            tma_load_2d(at + T::CODES, &args.v_scale_map, 0, row / kKeys, bar);
+          }
+          continue;
+        }
         const int stage = (int)(issued % T::STAGES);
         const uint32_t parity = (uint32_t)(issued / T::STAGES) & 1u;
         if (!mbar_wait_warp(smem_u32(&sm.k_empty[stage]), parity ^ 1u, ab)) return;
@@ -254,6 +278,52 @@ struct PartReader {
 };
 
 // ---------------------------------------------------------------------------------------------- queries and values
+// Eight bf16 elements in the order in which codes come out of a word: 0 4 1 5 2 6 3 7.
+__device__ __forceinline__ uint4 code_order(const uint4& v) {
+  return make_uint4(__byte_perm(v.x, v.z, 0x5410), __byte_perm(v.x, v.z, 0x7632), __byte_perm(v.y, v.w, 0x5410), __byte_perm(v.y, v.w, 0x7632));
+}
+__device__ __forceinline__ constexpr int code_place(int i) { return (i & ~7) + ((i & 1) << 2) + ((i & 7) >> 1); }   // element in place i of that order
+
+// Eight codes as bf16 elements, in that order.  A code shifted to the upper bits of 16.0's mantissa makes 16 + code, exactly, and so is its
+// product with the scale less 24 scales (at most five significant bits in a scale, eight in either term's and the result's).
+__device__ __forceinline__ uint4 widen_codes(uint32_t w, uint32_t scales, uint32_t less) {
+  uint32_t r[4] = {w << 3, w >> 1, w >> 5, w >> 9};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    r[i] = (r[i] & 0x00780078u) | 0x41804180u;
+    asm("fma.rn.bf16x2 %0, %0, %1, %2;" : "+r"(r[i]) : "r"(scales), "r"(less));
+  }
+  return make_uint4(r[0], r[1], r[2], r[3]);
+}
+
+// Widens a tile of codes, rows of 2 D bytes in spans of 128 as the products read them.  VALUES: keys outside [first, end) become zeros, and
+// elements that are not finite (those of a scale that is not) of keys from `all` on are cleared and put down.
+template <class T, bool VALUES>
+__device__ __forceinline__ void widen_tile(Part& p, const unsigned char* raw, unsigned char* tile, int thread, int key0, int first, int end, int all) {
+#pragma unroll 2
+  for (int item = thread; item < kKeys * T::PARTS; item += 128) {
+    const int k = item / T::PARTS, c = item % T::PARTS, key = key0 + k;
+    const uint4 codes = *reinterpret_cast<const uint4*>(raw + (T::D == 128 ? k * 64 + ((c ^ (k >> 1)) & 3) * 16 : k * 32 + ((c ^ (k >> 2)) & 1) * 16));
+    uint32_t scale = *reinterpret_cast<const uint16_t*>(raw + T::CODES + (k * T::PARTS + c) * 2);
+    if (VALUES) {
+      if (key < first || key >= end) {
+        scale = 0;
+      } else if (key >= all && (scale & 0x7f80u) == 0x7f80u) {
+        for (int i = 0; i < kScaleDims; ++i) atomicMin(&p.bad[0][c * kScaleDims + i], key);
+        p.dirty = 1;
+        scale = 0;
+      }
+    }
+    const uint32_t both = scale | scale << 16;
+    uint32_t less;
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(less) : "r"(both), "r"(0xc1c0c1c0u));      // -24
+    unsigned char* dst = tile + (c >> 1) * (kKeys * 128) + k * 128;
+    const uint32_t w[4] = {codes.x, codes.y, codes.z, codes.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4*>(dst + (((4 * c + i) ^ k) & 7) * 16) = widen_codes(w[i], both, less);
+  }
+}
+
 template <class T>
 __device__ __forceinline__ void load_queries(const AttendArgs& a, Part& p, unsigned char* q_tiles, int thread) {
   constexpr int D = T::D, kLanes = D / 8, kBatch = T::FP8 ? 2 : 8;    // loads in flight (8 bits: their conversions are long; 8: 600 instead of 550 us)
@@ -275,6 +345,7 @@ __device__ __forceinline__ void load_queries(const AttendArgs& a, Part& p, unsig
       const int r = r0 + i * (128 / kLanes), x = r >> 7, in = r & 127;
       unsigned char* tile = q_tiles + x * T::QTILE;
       if constexpr (!T::FP8) {
+        if constexpr (T::INT4) v[i].u = code_order(v[i].u);
         *reinterpret_cast<uint4*>(tile + (part >> 3) * (128 * 128) + in * 128 + ((part ^ in) & 7) * 16) = v[i].u;
       } else {
         float f[8], top = 0.f;
@@ -326,8 +397,8 @@ __device__ __forceinline__ bool any_not_finite(const uint4& v) {
 }
 
 template <class T>
-__device__ __forceinline__ void prepare_values(const AttendArgs& a, Smem& sm, unsigned char* q_tiles, unsigned char* v8_ring, unsigned char* v_ring,
-                                               const Abort& ab) {
+__device__ __forceinline__ void prepare_values(const AttendArgs& a, Smem& sm, unsigned char* q_tiles, unsigned char* k_ring, unsigned char* v8_ring,
+                                               unsigned char* v_ring, const Abort& ab) {
   constexpr int D = T::D;
   const int thread = threadIdx.x - 256, lane = threadIdx.x & 31;
   PartReader reader;
@@ -348,6 +419,29 @@ __device__ __forceinline__ void prepare_values(const AttendArgs& a, Smem& sm, un
     for (int j = 0; j < p.n_tiles; ++j, ++used) {
       const int stage = (int)(used % T::STAGES);
       const uint32_t parity = (uint32_t)(used / T::STAGES) & 1u;
+      if constexpr (T::INT4) {
+        const int raw = (int)(used % T::RAWS), key0 = (p.tile0 + j) * kKeys;
+        const uint32_t raw_parity = (uint32_t)(used / T::RAWS) & 1u;
+        if (!mbar_wait_warp(smem_u32(&sm.k4_full[raw]), raw_parity, ab)) return;
+        if (!mbar_wait_warp(smem_u32(&sm.k_empty[stage]), parity ^ 1u, ab)) return;
+        widen_tile<T, false>(p, v8_ring + 2 * raw * T::RAW, k_ring + stage * T::KTILE, thread, key0, p.first, p.end, seen_by_all);
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(smem_u32(&sm.k_full[stage]));
+          mbar_arrive(smem_u32(&sm.k4_empty[raw]));
+        }
+        if (!mbar_wait_warp(smem_u32(&sm.v_full[raw]), raw_parity, ab)) return;
+        if (!mbar_wait_warp(smem_u32(&sm.v_empty[stage]), parity ^ 1u, ab)) return;
+        widen_tile<T, true>(p, v8_ring + (2 * raw + 1) * T::RAW, v_ring + stage * T::VTILE, thread, key0, p.first, p.end, seen_by_all);
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(smem_u32(&sm.v_ready[stage]));
+          mbar_arrive(smem_u32(&sm.v8_empty[raw]));
+        }
+        continue;
+      }
       if (!mbar_wait_warp(smem_u32(&sm.v_full[stage]), parity, ab)) return;
       if constexpr (T::FP8) {
         if (!mbar_wait_warp(smem_u32(&sm.v_empty[stage]), parity ^ 1u, ab)) return;
@@ -588,7 +682,7 @@ __device__ __forceinline__ void write_rows(const PromptArgs& args, const Part& p
     }
     float x[32];
 #pragma unroll
-    for (int i = 0; i < 32; ++i) x[i] = any ? __uint_as_float(raw[i]) : 0.f;
+    for (int i = 0; i < 32; ++i) x[T::INT4 ? code_place(i) : i] = any ? __uint_as_float(raw[i]) : 0.f;
     if (dirty) {
 #pragma unroll
       for (int i = 0; i < 32; ++i) {
@@ -775,14 +869,14 @@ __device__ __forceinline__ void softmax_rows(const PromptArgs& args, Smem& sm, u
 }
 
 // ---------------------------------------------------------------------------------------------- kernel
-template <int D, bool FP8>
+template <int D, int BITS>
 __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid_constant__ PromptArgs args) {
-  using T = Traits<D, FP8>;
+  using T = Traits<D, BITS>;
   extern __shared__ unsigned char smem_raw[];
   unsigned char* q_tiles = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
   unsigned char* k_ring = q_tiles + T::QBUFS * 2 * T::QTILE;
-  unsigned char* v8_ring = k_ring + T::STAGES * T::KTILE;
-  unsigned char* v_ring = v8_ring + T::STAGES * T::V8TILE;
+  unsigned char* v8_ring = k_ring + T::STAGES * T::KTILE;   // what is copied to be widened
+  unsigned char* v_ring = v8_ring + T::STAGES * T::V8TILE + T::RAWS * 2 * T::RAW;
   Smem& sm = *reinterpret_cast<Smem*>(v_ring + T::STAGES * T::VTILE);
   const int warp = threadIdx.x >> 5;
   if (threadIdx.x == 0) {
@@ -800,12 +894,14 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
     }
     mbar_init(smem_u32(&sm.mma_done), 1);
     for (int i = 0; i < T::STAGES; ++i) {
-      mbar_init(smem_u32(&sm.k_full[i]), 1);
+      mbar_init(smem_u32(&sm.k_full[i]), T::INT4 ? 4 : 1);
       mbar_init(smem_u32(&sm.k_empty[i]), 1);
       mbar_init(smem_u32(&sm.v_full[i]), 1);
       mbar_init(smem_u32(&sm.v_ready[i]), 4);
       mbar_init(smem_u32(&sm.v_empty[i]), 1);
       mbar_init(smem_u32(&sm.v8_empty[i]), 4);
+      mbar_init(smem_u32(&sm.k4_full[i]), 1);
+      mbar_init(smem_u32(&sm.k4_empty[i]), 4);
     }
     sm.abort = 0;
     args.parts.headers[2 * blockIdx.x] = make_int4(0, 0, 0, 0);
@@ -826,8 +922,8 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
   else reg_dec<kOtherRegs>();
   if (w0 < w1) {
     if (warp < 8) softmax_rows<T>(args, sm, tmem, ab);
-    else if (warp < 12) prepare_values<T>(args.a, sm, q_tiles, v8_ring, v_ring, ab);
-    else if (warp == 12) copy_tiles<T>(args, sm, smem_u32(k_ring), smem_u32(FP8 ? v8_ring : v_ring), w0, w1, per, ab);
+    else if (warp < 12) prepare_values<T>(args.a, sm, q_tiles, k_ring, v8_ring, v_ring, ab);
+    else if (warp == 12) copy_tiles<T>(args, sm, smem_u32(k_ring), smem_u32(BITS == 16 ? v_ring : v8_ring), w0, w1, per, ab);
     else if (warp == 13) issue_products<T>(sm, tmem, smem_u32(q_tiles), smem_u32(k_ring), smem_u32(v_ring), ab);
   }
   tc_fence_before();
@@ -844,15 +940,16 @@ __global__ void __launch_bounds__(kThreads, 1) attend_prompt_kernel(const __grid
   }
 }
 
-template <int D, bool FP8>
+template <int D, int BITS>
 int32_t launch(const PromptArgs& args, int ctas, cudaStream_t stream) {
-  using T = Traits<D, FP8>;
+  using T = Traits<D, BITS>;
+  static_assert(smem_bytes<T>() <= 227 * 1024);
   static ContextSet done;
-  const int32_t st = allow_shared_memory(reinterpret_cast<const void*>(attend_prompt_kernel<D, FP8>), smem_bytes<T>(), done);
+  const int32_t st = allow_shared_memory(reinterpret_cast<const void*>(attend_prompt_kernel<D, BITS>), smem_bytes<T>(), done);
   if (st != SPF_OK) return st;
-  attend_prompt_kernel<D, FP8><<<ctas, kThreads, smem_bytes<T>(), stream>>>(args);
+  attend_prompt_kernel<D, BITS><<<ctas, kThreads, smem_bytes<T>(), stream>>>(args);
   SPF_CUDA_CHECK(cudaGetLastError());
-  return attend_join_launch(args.a, args.parts, kRows, kRows, D, FP8, ctas, stream);
+  return attend_join_launch(args.a, args.parts, kRows, kRows, D, T::FP8, ctas, stream);
 }
 
 }  // namespace
@@ -866,9 +963,16 @@ int32_t attend_prompt_launch(const AttendArgs& a, const spf_kv_cache* cache, int
   int32_t st = encode_pool_map("spf_attend", cache, cache->k_pool, kKeys, &args.k_map);
   if (st == SPF_OK) st = encode_pool_map("spf_attend", cache, cache->v_pool, kKeys, &args.v_map);
   if (st != SPF_OK) return st;
-  const bool fp8 = cache->k_scale != nullptr;
-  if (cache->head_dim == 64) return fp8 ? launch<64, true>(args, sm_count, stream) : launch<64, false>(args, sm_count, stream);
-  return fp8 ? launch<128, true>(args, sm_count, stream) : launch<128, false>(args, sm_count, stream);
+  const bool d64 = cache->head_dim == 64;
+  switch (a.kv.bits) {
+    case 4:
+      st = encode_scale_map("spf_attend", cache, cache->k_scale, &args.k_scale_map);
+      if (st == SPF_OK) st = encode_scale_map("spf_attend", cache, cache->v_scale, &args.v_scale_map);
+      if (st != SPF_OK) return st;
+      return d64 ? launch<64, 4>(args, sm_count, stream) : launch<128, 4>(args, sm_count, stream);
+    case 8: return d64 ? launch<64, 8>(args, sm_count, stream) : launch<128, 8>(args, sm_count, stream);
+    default: return d64 ? launch<64, 16>(args, sm_count, stream) : launch<128, 16>(args, sm_count, stream);
+  }
 }
 
 }  // namespace spf

@@ -37,122 +37,22 @@
 // finite, the tile's second product is made row by row, so that they reach the rows that see them and no others.
 #include <algorithm>
 
-#include "attend.cuh"
+#include "attend_step.cuh"
 
 namespace spf {
 namespace {
 
-constexpr int kWarps = 4;               // that compute
-// A second warpgroup, whose first warp copies, lends registers of the 128 a thread that the launch has: 128 x (192 + 64) = 256 x 128.
-constexpr int kComputeRegs = 192, kOtherRegs = 64;
-constexpr int kMaxStages = 8;
-
-
-// What the copying warp tells the computing ones about a stage.
-struct TileDesc {
-  int row0, n_new, pos0, first, end, head, row_tile, key0;
-  float k_scale[2], v_log2[2];          // 8 bits: of the tile's groups of 64 keys
-  int flags;                            // kFirst, kLast, kNoKeys; bits 8 ...: CTAs behind this one with parts of the triple
-};
-
-
-template <int D_, bool FP8_, int R_>
-struct Traits {
-  static constexpr int D = D_, R = R_;
-  static constexpr bool FP8 = FP8_;
-  // Warps over rows and over keys: a warp's outputs are 32 registers (8 rows of 128 dimensions, 16 of 64).  With 64 of them, 32 rows
-  // of 64 dimensions took 69 instead of 61 us (131072 keys, 8 heads), though each key is then read by half as many warps.
-  static constexpr int WR = R * D <= 1024 ? 1 : R * D / 1024, WK = kWarps / WR;
-  static constexpr int NT = R / (8 * WR);                             // 8-row tiles of a warp
-  // Keys of a tile: 128 where their rows are short, so that a warp has two sixteens of them at a time.  (One sixteen is a chain of
-  // dependent steps: with tiles of 64 keys 32 sequences of up to 16k tokens on an 8-bit cache took 136 instead of 111 us, four of up to
-  // 250k 384 instead of 292, eight lookahead tokens over 131072 keys of 64 dimensions 92 instead of 70.)  A warp's keys share a scale, so they are 64 at most.
-  static constexpr int KEYS = (FP8 ? D : 2 * D) <= 128 && WK > 1 ? 128 : 64;
-  static constexpr int KW = KEYS / WK, KT = KW / 16;                  // keys of a warp in a tile, in sixteens
-  static constexpr bool LEND = R >= 16 && R * D < 4096;               // registers move between warpgroups
-  static constexpr int THREADS = LEND ? 2 * kWarps * 32 : (kWarps + 1) * 32;
-  static constexpr int CTAS = R == 8 ? 3 : 2;                         // per SM
-  static constexpr int WTERMS = !FP8 && R == 8 ? 2 : 1;               // of a weight
-  static constexpr bool QREGS = NT <= 2;                              // queries stay in registers
-  static constexpr int ROWB = FP8 ? D : 2 * D, SPAN = ROWB < 128 ? ROWB : 128;
-  static constexpr int TILE = KEYS * ROWB, STAGE = 2 * TILE;
-  static constexpr int QBYTES = R * D * 2;
-  static constexpr int FIT = ((CTAS == 3 ? 74 : 112) * 1024 - 4096 - QBYTES) / STAGE;
-  static constexpr int STAGES = FIT < kMaxStages ? FIT : kMaxStages;
-  static constexpr int JOIN = D * WK * R * 4 <= STAGE ? D : STAGE / (WK * R * 4);   // output columns joined at a time
-};
-
-enum : int { kFirst = 1, kLast = 2, kNoKeys = 4, kFromStart = 8, kToEnd = 16 };
-
-struct SmallSmem {
-  unsigned long long full[kMaxStages], empty[kMaxStages], join;
-  TileDesc desc[kMaxStages];
-  RowStats stats[kWarps][32];           // of the warps' rows
-  int64_t scan[2 * kWarps];
-  int64_t total, start_base;
-  int start_seq;
-  int abort;
-};
-
-template <class T>
-constexpr int smem_bytes() { return T::STAGES * T::STAGE + T::QBYTES + (int)sizeof(SmallSmem) + 1024; }
-
 struct StepArgs {
   AttendArgs a;
   CUtensorMap k_map, v_map;
+  CUtensorMap k_scale_map, v_scale_map;   // 4 bits
   AttendParts parts;
 };
 
-__device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t (&r)[4]) {
-  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
-}
-__device__ __forceinline__ void ldsm4_t(uint32_t addr, uint32_t (&r)[4]) {
-  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
-}
-
-template <bool FP8>
-__device__ __forceinline__ void mma16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  if constexpr (FP8)
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-  else
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-
-// 8-bit keys by the E4M3 (LOW: E5M2) term of 8-bit queries.
-template <bool LOW>
-__device__ __forceinline__ void mma32(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  if constexpr (LOW)
-    asm volatile("mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e5m2.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-  else
-    asm volatile("mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-
-// Byte offset of the 16-byte chunk `chunk` of row `row` in a tile, as the copies' swizzle lays it: spans of 128 (or 64) bytes
-// one after the other, the chunk's place in its span exchanged by the row.
-template <class T>
-__device__ __forceinline__ uint32_t tile_chunk(int row, int chunk) {
-  if constexpr (T::SPAN == 64) return (uint32_t)(row * 64 + ((chunk ^ (row >> 1)) & 3) * 16);
-  return (uint32_t)((chunk >> 3) * (T::KEYS * 128) + row * 128 + ((chunk ^ row) & 7) * 16);
-}
-// The same for the query tile, rows of 2 D bytes.
-template <class T>
-__device__ __forceinline__ uint32_t q_chunk(int row, int chunk) {
-  return (uint32_t)(row * (2 * T::D) + ((chunk & ~7) | ((chunk ^ row) & 7)) * 16);
-}
-
-// One term of 8-bit queries, rows of D bytes: eight rows' chunks of one column on banks of their own.
-template <class T>
-__device__ __forceinline__ uint32_t q8_chunk(int row, int chunk) {
-  if constexpr (T::D == 64) return (uint32_t)(row * 64 + ((chunk ^ (row >> 1)) & 3) * 16);
-  return (uint32_t)(row * 128 + ((chunk ^ row) & 7) * 16);
+__device__ __forceinline__ uint32_t transpose8(uint32_t x) {
+  uint32_t y;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
 }
 
 // ---------------------------------------------------------------------------------------------- the list of tiles
@@ -276,6 +176,10 @@ __device__ __forceinline__ void copy_tiles(const StepArgs& args, SmallSmem& sm, 
           mbar_expect_tx(bar, T::STAGE);
           tma_load_3d(at, &args.k_map, 0, row, 0, bar);
           tma_load_3d(at + T::TILE, &args.v_map, 0, row, 0, bar);
+          if constexpr (T::INT4) {
+            tma_load_2d(at + 2 * T::TILE, &args.k_scale_map, 0, row / 128, bar);
+            tma_load_2d(at + 2 * T::TILE + T::SCALES, &args.v_scale_map, 0, row / 128, bar);
+          }
         }
       }
       if (++stage == T::STAGES) stage = 0, parity ^= 1;
@@ -298,64 +202,12 @@ struct Join {
   }
 };
 
-// The triple's query rows into shared memory, rows that do not exist as zeros.  8 bits: the two terms, one tile behind the other, and
-// the rows' factors 2^-e.
-template <class T>
-__device__ __forceinline__ void load_queries(const AttendArgs& a, const TileDesc& d, unsigned char* q_tile, float* q_factor) {
-  constexpr int kLanes = T::D / 8;                       // threads of a row
-  const int total = d.n_new * a.group;
-  for (int item = threadIdx.x; item < T::R * kLanes; item += kWarps * 32) {
-    const int r = item / kLanes, part = item % kLanes, rr = d.row_tile * T::R + r;
-    const __nv_bfloat16* src = a.q.data + (int64_t)(d.row0 + rr / a.group) * a.q.stride_row + (int64_t)(d.head * a.group + rr % a.group) * a.q.stride_head;
-    union { uint4 u; __nv_bfloat162 h[4]; } v;
-    v.u = make_uint4(0, 0, 0, 0);
-    if (rr < total) v.u = __ldg(reinterpret_cast<const uint4*>(src) + part);
-    if constexpr (!T::FP8) {
-      *reinterpret_cast<uint4*>(q_tile + q_chunk<T>(r, part)) = v.u;
-    } else {
-      float f[8];
-      float top = 0.f;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float2 p = __bfloat1622float2(v.h[i]);
-        f[2 * i] = p.x, f[2 * i + 1] = p.y;
-        top = fmaxf(top, fmaxf(fabsf(p.x), fabsf(p.y)));
-      }
-#pragma unroll
-      for (int o = kLanes / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o, kLanes));
-      int e;
-      uint2 hi, lo;
-      two_terms(f, top, &e, &hi, &lo);
-      *reinterpret_cast<uint2*>(q_tile + q8_chunk<T>(r, part >> 1) + 8 * (part & 1)) = hi;
-      *reinterpret_cast<uint2*>(q_tile + T::R * T::D + q8_chunk<T>(r, part >> 1) + 8 * (part & 1)) = lo;
-      if (part == 0) q_factor[r] = __uint_as_float((uint32_t)(127 - e) << 23);
-    }
-  }
-}
-
-// The queries of 8 rows as right operands for 32 (8 bits: 64) dimensions: b[0..1] of two products; 8 bits: first[0..1], second[2..3]
-// of one term.
-template <class T>
-__device__ __forceinline__ void query_operand(uint32_t q_addr, int row, int step, int lane, uint32_t (&b)[4]) {
-  if constexpr (T::FP8) ldsm4(q_addr + q8_chunk<T>(row + (lane & 7), 4 * step + (lane >> 3)), b);
-  else ldsm4(q_addr + q_chunk<T>(row + (lane & 7), 4 * step + (lane >> 3)), b);
-}
-
-// The 16 keys from `key` on as the left operand: bf16 16 dimensions (of chunk pair `step`), 8 bits 32.  Rows 0-7 and 8-15 of the
-// operand are keys 0-7 and 8-15; 8 bits: the even and the odd keys, as the values' bytes come.
-template <class T>
-__device__ __forceinline__ void key_operand(uint32_t k_tile, int key, int step, int lane, uint32_t (&a)[4]) {
-  const int in8 = lane & 7, second = (lane >> 3) & 1;
-  ldsm4(k_tile + tile_chunk<T>(key + (T::FP8 ? 2 * in8 + second : 8 * second + in8), 2 * step + (lane >> 4)), a);
-}
-// The key (from the warp's sixteen) of a thread's logits 0, 1 (half = 0) and 2, 3 (half = 1).
-template <class T>
-__device__ __forceinline__ int key_of(int lane, int half) { return T::FP8 ? 2 * (lane >> 2) + half : (lane >> 2) + 8 * half; }
-
 // 16 dimensions of the values of 16 keys as the left operand: a[0], a[2] dimensions 0-7, a[1], a[3] 8-15.  The halves of a register
-// are two keys (value_key).  8 bits: two such, for the 16 dimensions behind as well.
+// are two keys (value_key).  8 bits: two such, for the 16 dimensions behind as well; 4 bits: two such of 32 dimensions that share scales, rows
+// 0-7 the even dimensions, 8-15 the odd ones.
 template <class T>
 __device__ __forceinline__ void value_operand(uint32_t v_tile, int key, int mt, int lane, uint32_t (&a)[T::FP8 ? 2 : 1][4]) {
+  static_assert(!T::INT4);
   if constexpr (T::FP8) {
     uint32_t r[4];
     // two 16 x 16 byte matrices, transposed: r[0] the four keys 4 c ... of dimension lane / 4, r[1] of the one 8 behind it
@@ -389,17 +241,12 @@ __device__ __forceinline__ bool not_finite(uint32_t pair) {
   return (pair & kExp) == kExp || ((pair >> 16) & kExp) == kExp;
 }
 
-__device__ __forceinline__ uint32_t transpose8(uint32_t x) {
-  uint32_t y;
-  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
-  return y;
-}
-
 // What a warp has of a triple: outputs (dimensions lane / 4 and 8 behind it of every 16, query rows 2 (lane % 4) and the next of
 // every 8), references and sums of its rows.
 template <class T>
 struct State {
   float o[T::D / 16][T::NT][4];
+  float eight[T::INT4 ? T::PARTS : 1][T::INT4 ? T::NT : 1][4];   // 4 bits: what 8 in place of the codes would give
   float m[T::NT][2], l[T::NT][2];
   float m_sum[T::FP8 ? T::NT : 1][2];                    // 8 bits
 };
@@ -436,6 +283,54 @@ __device__ __forceinline__ void add_values(State<T>& st, const uint32_t (&p)[T::
 #pragma unroll
           for (int t = 0; t < T::WTERMS; ++t) mma16<T::FP8>(st.o[m0 + i][nt], v[i], p[t][kt][nt][0], p[t][kt][nt][1]);
     }
+}
+
+// 4 bits: out += scales . codes . weights.  Codes are multiplied as subnormal numbers, as those of the keys are (tile_logits); scales go into
+// the weights, rounded once to bf16, and 8 times the sum of these is subtracted at the triple's end.  x[kt][nt][h]: the weights in fp32.
+// Values of keys that a row does not see count as zeros (GUARD), whatever their scales.
+template <class T, bool GUARD>
+__device__ __forceinline__ void add_codes(State<T>& st, const float (&x)[T::KT][T::NT][2][2], const int (&sees)[T::NT][2], uint32_t v_tile, uint32_t scales, int key,
+                                          int key0, int first, int lane) {
+#pragma unroll
+  for (int kt = 0; kt < T::KT; ++kt) {
+    float s[2][T::PARTS];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) load_scales<T>(scales, key + kt * 16 + key_of<T>(lane, h), s[h]);
+#pragma unroll
+    for (int m0 = 0; m0 < T::PARTS; m0 += 2) {
+      // two 16 x 16 byte matrices, transposed: w[2 i] the four keys of rows 4 c ... and byte lane / 4, w[2 i + 1] of the byte 8 behind it
+      uint32_t w[4];
+      const int r = lane & 15;
+      asm volatile("ldmatrix.sync.aligned.m16n16.x2.trans.shared.b8 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
+                   : "r"(v_tile + tile_chunk<T>(key + kt * 16 + operand_key<T>(2 * (r >> 2) + ((r >> 1) & 1), r & 1), m0 + (lane >> 4))));
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int part = m0 + i;
+#pragma unroll
+        for (int nt = 0; nt < T::NT; ++nt) {
+          uint32_t p[2];
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            float u = x[kt][nt][h][0] * s[h][part], v = x[kt][nt][h][1] * s[h][part];
+            if (GUARD) {
+              const int at = key0 + key + kt * 16 + key_of<T>(lane, h);
+              if (at < first || at >= sees[nt][0]) u = 0.f;
+              if (at < first || at >= sees[nt][1]) v = 0.f;
+            }
+            p[h] = transpose8(pack_bf16(u, v));
+          }
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const uint32_t word = w[2 * i + j];
+            const uint32_t codes[4] = {word & 0x000f000fu, word & 0x00f000f0u, (word >> 8) & 0x000f000fu, (word >> 8) & 0x00f000f0u};
+            mma16<false>(st.o[2 * part + j][nt], codes, p[0], p[1]);
+          }
+          const uint32_t eights[4] = {0x00080008u, 0x00800080u, 0x00080008u, 0x00800080u};
+          mma16<false>(st.eight[part][nt], eights, p[0], p[1]);
+        }
+      }
+    }
+  }
 }
 
 // Whether the warp has values that are not finite of keys that some row sees and others do not.
@@ -496,18 +391,18 @@ template <class T>
 __device__ __forceinline__ void compute_tiles(const StepArgs& args, SmallSmem& sm, unsigned char* ring_ptr, uint32_t ring, unsigned char* q_tile,
                                               int64_t w0, int64_t n_tiles, const Abort& ab) {
   constexpr int D = T::D, R = T::R, NT = T::NT, KT = T::KT;
-  constexpr int kTerms = T::FP8 ? 2 : 1, kSteps = T::FP8 ? D / 64 : D / 32;   // four registers of queries each
+  // 4 bits: the reference lies 2^64 below the largest weight, so that codes of 2^-133 times weights and scales make normal numbers
+  constexpr float kBelow = T::INT4 ? 64.f : 0.f;
   const AttendArgs& a = args.a;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int row_off = warp % T::WR * NT * 8, key_warp = warp / T::WR, key_off = key_warp * T::KW;
   const uint32_t q_addr = smem_u32(q_tile);
-  __shared__ float q_factor[R];
+  __shared__ QueryNotes<T> notes;
   Join join{smem_u32(&sm.join), 0};
   State<T> st;
-  float qf[NT][2];
   int sees[NT][2];                                       // the key behind the last one that a row sees
   Seen seen{0, 0, 0};
-  uint32_t q[T::QREGS ? kTerms * kSteps * NT : 1][4];
+  Queries<T> queries;
   int stage = 0;
   uint32_t parity = 0;
   {
@@ -518,14 +413,14 @@ __device__ __forceinline__ void compute_tiles(const StepArgs& args, SmallSmem& s
     d.row0 = s.row0, d.n_new = s.n_new;
     d.head = (int)(triple / row_tiles_of<T>(a, s));
     d.row_tile = (int)(triple - (int64_t)d.head * row_tiles_of<T>(a, s));
-    load_queries<T>(a, d, q_tile, q_factor);
+    load_queries<T>(a, d, q_tile, notes);
   }
   for (int64_t tile = 0; tile < n_tiles; ++tile) {
     if (!mbar_wait_warp(smem_u32(&sm.full[stage]), parity, ab)) return;
     const TileDesc& d = sm.desc[stage];
     const int flags = d.flags;
     if (flags & kFirst) {
-      if (tile > 0) load_queries<T>(a, d, q_tile, q_factor);
+      if (tile > 0) load_queries<T>(a, d, q_tile, notes);
       if (!join.wait(ab)) return;
       const int row_first = d.row_tile * R;
       seen.first = d.first, seen.end = d.end;
@@ -539,21 +434,21 @@ __device__ __forceinline__ void compute_tiles(const StepArgs& args, SmallSmem& s
           st.m[nt][e] = kNoReference;
           st.l[nt][e] = 0.f;
           if constexpr (T::FP8) st.m_sum[nt][e] = kNoReference;
-          if constexpr (T::FP8) qf[nt][e] = q_factor[row_off + nt * 8 + 2 * (lane & 3) + e];
         }
 #pragma unroll
         for (int m = 0; m < D / 16; ++m)
 #pragma unroll
           for (int e = 0; e < 4; ++e) st.o[m][nt][e] = 0.f;
       }
-      if constexpr (T::QREGS) {
+      if constexpr (T::INT4) {
 #pragma unroll
-        for (int t = 0; t < kTerms; ++t)
+        for (int p = 0; p < T::PARTS; ++p)
 #pragma unroll
-          for (int x = 0; x < kSteps; ++x)
+          for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) query_operand<T>(q_addr + t * R * D, row_off + nt * 8, x, lane, q[(t * kSteps + x) * NT + nt]);
+            for (int e = 0; e < 4; ++e) st.eight[p][nt][e] = 0.f;
       }
+      queries.load(q_addr, notes, row_off, lane);
     }
     if (!(flags & kNoKeys)) {
       const uint32_t k_tile = ring + stage * T::STAGE, v_tile = k_tile + T::TILE;
@@ -561,40 +456,7 @@ __device__ __forceinline__ void compute_tiles(const StepArgs& args, SmallSmem& s
       const bool guard = key0 < seen.first || key0 + T::KEYS > seen.all;
       // logits of the warp's keys and rows
       float z[KT][NT][4];
-#pragma unroll
-      for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) z[kt][nt][e] = 0.f;
-#pragma unroll
-      for (int x = 0; x < kSteps; ++x) {
-        uint32_t k[KT][2][4];
-#pragma unroll
-        for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-          for (int h = 0; h < 2; ++h) key_operand<T>(k_tile, key_off + kt * 16, 2 * x + h, lane, k[kt][h]);
-#pragma unroll
-        for (int t = 0; t < kTerms; ++t)
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-            uint32_t b[4];
-            if constexpr (T::QREGS) {
-#pragma unroll
-              for (int e = 0; e < 4; ++e) b[e] = q[(t * kSteps + x) * NT + nt][e];
-            } else {
-              query_operand<T>(q_addr + t * R * D, row_off + nt * 8, x, lane, b);
-            }
-#pragma unroll
-            for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-              for (int h = 0; h < 2; ++h) {
-                if constexpr (!T::FP8) mma16<false>(z[kt][nt], k[kt][h], b[2 * h], b[2 * h + 1]);
-                else if (t == 0) mma32<false>(z[kt][nt], k[kt][h], b[2 * h], b[2 * h + 1]);
-                else mma32<true>(z[kt][nt], k[kt][h], b[2 * h], b[2 * h + 1]);
-              }
-          }
-      }
+      tile_logits<T>(z, queries, q_addr, row_off, k_tile, k_tile + 2 * T::TILE, key_off, lane);
       if (guard) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
@@ -615,7 +477,7 @@ __device__ __forceinline__ void compute_tiles(const StepArgs& args, SmallSmem& s
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          f[nt][e] = T::FP8 ? logit_factor(k_scale, qf[nt][e]) : k_scale;
+          f[nt][e] = T::FP8 ? logit_factor(k_scale, queries.factor[nt][e]) : T::INT4 ? queries.factor[nt][e] : k_scale;
           float t = fmaxf(z[0][nt][e], z[0][nt][2 + e]);
 #pragma unroll
           for (int kt = 1; kt < KT; ++kt) t = max3(t, z[kt][nt][e], z[kt][nt][2 + e]);
@@ -624,7 +486,7 @@ __device__ __forceinline__ void compute_tiles(const StepArgs& args, SmallSmem& s
             const float off = offset(nt, e);
             over |= top[nt][e] + off > kLazy + kShift || top[nt][e] - st.m_sum[nt][e] > kLazy || above_weights(off, st.m_sum[nt][e]) > kFar;
           } else {
-            over |= top[nt][e] > st.m[nt][e] + kLazy;
+            over |= top[nt][e] > st.m[nt][e] + (kLazy + kBelow);
           }
         }
       if (__any_sync(0xffffffffu, over)) {
@@ -635,10 +497,14 @@ __device__ __forceinline__ void compute_tiles(const StepArgs& args, SmallSmem& s
             float largest = top[nt][e];
 #pragma unroll
             for (int o = 4; o < 32; o <<= 1) largest = fmaxf(largest, __shfl_xor_sync(0xffffffffu, largest, o));
-            const float m = fmaxf(st.m[nt][e], T::FP8 ? largest + add - kShift : largest), scale = fast_exp2(st.m[nt][e] - m);
+            const float m = fmaxf(st.m[nt][e], T::FP8 ? largest + add - kShift : largest - kBelow), scale = fast_exp2(st.m[nt][e] - m);
             st.m[nt][e] = m;
 #pragma unroll
             for (int i = 0; i < D / 16; ++i) st.o[i][nt][e] *= scale, st.o[i][nt][2 + e] *= scale;
+            if constexpr (T::INT4) {
+#pragma unroll
+              for (int p = 0; p < T::PARTS; ++p) st.eight[p][nt][e] *= scale, st.eight[p][nt][2 + e] *= scale;
+            }
             if constexpr (T::FP8) {
               const float m_sum = fmaxf(st.m_sum[nt][e], largest);
               st.l[nt][e] *= fast_exp2(st.m_sum[nt][e] - m_sum);
@@ -654,7 +520,8 @@ __device__ __forceinline__ void compute_tiles(const StepArgs& args, SmallSmem& s
             }
           }
       }
-      uint32_t p[T::WTERMS][KT][NT][2];
+      uint32_t p[T::WTERMS][KT][NT][2];                  // not for 4 bits
+      float weight[T::INT4 ? KT : 1][NT][2][2];          // 4 bits
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         float off[2], sum[2] = {0.f, 0.f};
@@ -667,6 +534,10 @@ __device__ __forceinline__ void compute_tiles(const StepArgs& args, SmallSmem& s
             const float x = fast_exp2(fmaf(z[kt][nt][2 * h], f[nt][0], off[0])), y = fast_exp2(fmaf(z[kt][nt][2 * h + 1], f[nt][1], off[1]));
             sum[0] += x;
             sum[1] += y;
+            if constexpr (T::INT4) {
+              weight[kt][nt][h][0] = x, weight[kt][nt][h][1] = y;
+              continue;
+            }
             const uint32_t w = T::FP8 ? pack_f16(x, y) : pack_bf16(x, y);
             p[0][kt][nt][h] = transpose8(w);
             if constexpr (T::WTERMS == 2) p[1][kt][nt][h] = transpose8(pack_bf16(x - __uint_as_float(w << 16), y - __uint_as_float(w & 0xffff0000u)));
@@ -681,11 +552,27 @@ __device__ __forceinline__ void compute_tiles(const StepArgs& args, SmallSmem& s
           }
         }
       }
-      if (!guard) add_values<T, false>(st, p, v_tile, key_off, key0, seen, lane);
+      if constexpr (T::INT4) {
+        const uint32_t v_scales = k_tile + 2 * T::TILE + T::SCALES;
+        if (!guard) add_codes<T, false>(st, weight, sees, v_tile, v_scales, key_off, key0, seen.first, lane);
+        else add_codes<T, true>(st, weight, sees, v_tile, v_scales, key_off, key0, seen.first, lane);
+      } else if (!guard) add_values<T, false>(st, p, v_tile, key_off, key0, seen, lane);
       else if (seen.all >= seen.end || !odd_values<T>(v_tile, key_off, key0, seen.all, seen.end, lane)) add_values<T, true>(st, p, v_tile, key_off, key0, seen, lane);
       else add_odd_values<T>(st, p, v_tile, key_off, key0, seen, d, a.group, a.causal, d.row_tile * R + row_off, lane);
     }
     if (flags & kLast) {
+      if constexpr (T::INT4) {
+        // codes less 8, and both powers of two taken out: of the codes' places and of the reference
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int m = 0; m < D / 16; ++m) st.o[m][nt][e] = (st.o[m][nt][e] - st.eight[m / 2][nt][e]) * (e < 2 ? 0x1p69f : 0x1p65f);
+#pragma unroll
+          for (int e = 0; e < 2; ++e) st.l[nt][e] *= 0x1p-64f, st.m[nt][e] += kBelow;
+        }
+      }
       // the warps' sums of a row, each against its own reference
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
@@ -722,7 +609,7 @@ __device__ __forceinline__ void compute_tiles(const StepArgs& args, SmallSmem& s
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              const int r = row_off + nt * 8 + 2 * (lane & 3) + (e & 1), col = 16 * m - c0 + (lane >> 2) + 8 * (e >> 1);
+              const int r = row_off + nt * 8 + 2 * (lane & 3) + (e & 1), col = 16 * m - c0 + (T::INT4 ? 2 * (lane >> 2) + (e >> 1) : (lane >> 2) + 8 * (e >> 1));
               buf[(key_warp * R + r) * T::JOIN + (col ^ (((r >> 1) & kSwizzle) << 3))] = st.o[m][nt][e] * f[nt][e & 1];
             }
         }
@@ -776,9 +663,9 @@ __device__ __forceinline__ void compute_tiles(const StepArgs& args, SmallSmem& s
   }
 }
 
-template <int D, bool FP8, int R>
-__global__ void __launch_bounds__(Traits<D, FP8, R>::THREADS, Traits<D, FP8, R>::CTAS) attend_step_kernel(const __grid_constant__ StepArgs args) {
-  using T = Traits<D, FP8, R>;
+template <int D, int BITS, int R>
+__global__ void __launch_bounds__(Traits<D, BITS, R>::THREADS, Traits<D, BITS, R>::CTAS) attend_step_kernel(const __grid_constant__ StepArgs args) {
+  using T = Traits<D, BITS, R>;
   extern __shared__ unsigned char smem_raw[];
   unsigned char* ring_ptr = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
   unsigned char* q_tile = ring_ptr + T::STAGES * T::STAGE;
@@ -817,28 +704,32 @@ int tile_rows(const spf_kv_cache* cache, int group, int max_new) {
 }
 int ctas_per_sm(int rows) { return rows <= 8 ? 3 : 2; }
 
-template <int D, bool FP8, int R>
+template <int D, int BITS, int R>
 int32_t launch_step(StepArgs& args, const spf_kv_cache* cache, int live, int ctas, cudaStream_t stream) {
-  using T = Traits<D, FP8, R>;
+  using T = Traits<D, BITS, R>;
   static ContextSet done;
   int32_t st = encode_pool_map("spf_attend", cache, cache->k_pool, T::KEYS, &args.k_map);
   if (st == SPF_OK) st = encode_pool_map("spf_attend", cache, cache->v_pool, T::KEYS, &args.v_map);
-  if (st == SPF_OK) st = allow_shared_memory(reinterpret_cast<const void*>(attend_step_kernel<D, FP8, R>), smem_bytes<T>(), done);
+  if constexpr (T::INT4) {
+    if (st == SPF_OK) st = encode_scale_map("spf_attend", cache, cache->k_scale, &args.k_scale_map);
+    if (st == SPF_OK) st = encode_scale_map("spf_attend", cache, cache->v_scale, &args.v_scale_map);
+  }
+  if (st == SPF_OK) st = allow_shared_memory(reinterpret_cast<const void*>(attend_step_kernel<D, BITS, R>), smem_bytes<T>(), done);
   if (st != SPF_OK) return st;
-  attend_step_kernel<D, FP8, R><<<ctas, T::THREADS, smem_bytes<T>(), stream>>>(args);
+  attend_step_kernel<D, BITS, R><<<ctas, T::THREADS, smem_bytes<T>(), stream>>>(args);
   SPF_CUDA_CHECK(cudaGetLastError());
-  return attend_join_launch(args.a, args.parts, R, live, D, FP8, ctas, stream);
+  return attend_join_launch(args.a, args.parts, R, live, D, T::FP8, ctas, stream);
 }
 
-template <int D, bool FP8>
+template <int D, int BITS>
 int32_t launch_rows(StepArgs& args, const spf_kv_cache* cache, int rows, int live, int ctas, cudaStream_t stream) {
   switch (rows) {
-    case 8: return launch_step<D, FP8, 8>(args, cache, live, ctas, stream);
+    case 8: return launch_step<D, BITS, 8>(args, cache, live, ctas, stream);
     case 16: break;
     default:
-      if constexpr (!(D == 128 && FP8)) return launch_step<D, FP8, 32>(args, cache, live, ctas, stream);
+      if constexpr (D == 64 || BITS == 16) return launch_step<D, BITS, 32>(args, cache, live, ctas, stream);
   }
-  return launch_step<D, FP8, 16>(args, cache, live, ctas, stream);
+  return launch_step<D, BITS, 16>(args, cache, live, ctas, stream);
 }
 
 }  // namespace
@@ -856,9 +747,12 @@ int32_t attend_step_launch(const AttendArgs& a, const spf_kv_cache* cache, int m
   args.a = a;
   const int rows = tile_rows(cache, a.group, max_new), live = (int)std::min<int64_t>((int64_t)a.group * max_new, rows), ctas = sm_count * ctas_per_sm(rows);
   args.parts = parts_at(workspace, rows, cache->head_dim, ctas);
-  const bool fp8 = cache->k_scale != nullptr;
-  if (cache->head_dim == 64) return fp8 ? launch_rows<64, true>(args, cache, rows, live, ctas, stream) : launch_rows<64, false>(args, cache, rows, live, ctas, stream);
-  return fp8 ? launch_rows<128, true>(args, cache, rows, live, ctas, stream) : launch_rows<128, false>(args, cache, rows, live, ctas, stream);
+  const bool d64 = cache->head_dim == 64;
+  switch (a.kv.bits) {
+    case 4: return d64 ? launch_rows<64, 4>(args, cache, rows, live, ctas, stream) : launch_rows<128, 4>(args, cache, rows, live, ctas, stream);
+    case 8: return d64 ? launch_rows<64, 8>(args, cache, rows, live, ctas, stream) : launch_rows<128, 8>(args, cache, rows, live, ctas, stream);
+    default: return d64 ? launch_rows<64, 16>(args, cache, rows, live, ctas, stream) : launch_rows<128, 16>(args, cache, rows, live, ctas, stream);
+  }
 }
 
 }  // namespace spf

@@ -5,13 +5,15 @@
 
 namespace spf {
 
-constexpr int kScaleTokens = SPF_KV_SCALE_TOKENS;
+constexpr int kScaleTokens = SPF_KV_SCALE_TOKENS, kScaleDims = SPF_KV_SCALE_DIMS;
 
 struct KvView {
-  uint8_t *k, *v;              // pools: bf16 or E4M3 [n_blocks][n_kv_heads][block_tokens][d]
+  uint8_t *k, *v;              // pools: bf16, E4M3 or codes [n_blocks][n_kv_heads][block_tokens][d]
   float *k_scale, *v_scale;    // 8-bit pools: [n_blocks][n_kv_heads][block_tokens / 64]
+  uint16_t *k_scale4, *v_scale4;    // 4-bit pools: bf16 [n_blocks][n_kv_heads][block_tokens][d / 32]
   int64_t n_blocks;
   int block_tokens, n_kv_heads;
+  int bits;                    // 16, 8 or 4
 };
 
 struct StepView {
@@ -40,6 +42,9 @@ __device__ __forceinline__ int64_t pool_block(const KvView& kv, const StepView& 
   const int b = __ldg(st.table + (int64_t)seq * st.table_stride + j);
   return b >= 0 && b < kv.n_blocks ? b : -1;
 }
+
+// Bits of a cache's elements; the caller has checked it.
+inline int cache_bits(const spf_kv_cache* c) { return c->bits != 0 ? c->bits : c->k_scale != nullptr ? 8 : 16; }
 
 // Host checks, shared by the calls on the cache; they leave the reason in the error text.
 int32_t check_cache(const char* who, const spf_kv_cache* cache, KvView* out);

@@ -7,7 +7,10 @@
 // one CTA makes the new tokens of such a group, their largest magnitude, the scale, and the bytes:
 //   s' = max(s of the tokens that the group holds already, 2^ceil(log2(max |x| / 448))),   byte = E4M3(x / s'),
 // and rounds the bytes held already from s to s' where it grew.  Powers of two: that second rounding is then exact but for
-// bytes that become subnormal.
+// bytes that become subnormal.  4-bit pools: a token's 32 consecutive elements of a head have a scale of their own,
+//   s = the smallest number of five significant bits with 7 s >= max |x|,   code = 8 + rint(x (1 / s)),
+// so that tokens are independent, as with bf16, and a row is moved by the same threads: the D / 16 lanes that have a head's elements
+// exchange their largest magnitudes, and each writes the codes of its two runs of 8, 4 bytes each.
 //
 // Bounds: bytes for a prompt, a launch and four dependent loads (row_start, seq_lens, table, the data) for single tokens.
 #include <algorithm>
@@ -112,12 +115,71 @@ __device__ __forceinline__ bool place_of(const AppendArgs& a, int seq, int row, 
   return fine;
 }
 
-// Rows as they are: queries (always), keys and values (bf16 pools).  A thread has one unit of HPT heads of a row, so that a
+// ---------------------------------------------------------------------------------------------- 4-bit rows
+// Largest magnitude of eight elements, as bits that order like it: infinities as zeros, NaN above every number.
+__device__ __forceinline__ uint32_t largest_bits(const float (&x)[8]) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint32_t m = __float_as_uint(x[i]) & 0x7fffffffu;
+    top = max(top, m == 0x7f800000u ? 0u : m);
+  }
+  return top;
+}
+// The smallest number of five significant bits s >= 2^-100 with 7 s >= the magnitude; NaN for NaN.
+__device__ __forceinline__ float short_scale(uint32_t magnitude) {
+  if (magnitude > 0x7f800000u) return __uint_as_float(0x7fc00000u);
+  const float top = __uint_as_float(magnitude);
+  uint32_t s = __float_as_uint(__fdiv_rn(top, 7.f)) & 0xfff80000u;
+  if (__uint_as_float(s) * 7.f < top) s += 0x80000u;     // the product is exact: 3 + 5 bits
+  return fmaxf(__uint_as_float(s), 0x1p-100f);
+}
+// Codes of eight elements, the first in the lowest four bits.
+__device__ __forceinline__ uint32_t codes8(const float (&x)[8], float inverse) {
+  uint32_t r = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float t = fminf(fmaxf(__fmul_rn(x[i], inverse), -7.f), 7.f);
+    r |= (__float_as_uint(__fadd_rn(t, 12582920.f)) & 15u) << (4 * i);   // 1.5 * 2^23 + 8: the sum's last bits are the code
+  }
+  return r;
+}
+// A head's row of a 4-bit pool: its D / 16 lanes, neighbours in a warp, have a unit each.
+template <int D>
+__device__ __forceinline__ void write_codes(uint8_t* row, uint16_t* scales, const float (&f)[8], const float (&g)[8], const Unit& u) {
+  constexpr int kUnits = D / 16, kParts = D / kScaleDims;
+  const int lane = threadIdx.x & 31;
+  const uint32_t lanes = ((1u << kUnits) - 1u) << (lane & ~(kUnits - 1));
+  const uint32_t mf = largest_bits(f), mg = largest_bits(g);
+  float scale[kParts];
+#pragma unroll
+  for (int p = 0; p < kParts; ++p) {
+    uint32_t m = max(u.first / kScaleDims == p ? mf : 0u, u.second / kScaleDims == p ? mg : 0u);
+#pragma unroll
+    for (int o = 1; o < kUnits; o <<= 1) m = max(m, __shfl_xor_sync(lanes, m, o));
+    scale[p] = short_scale(m);
+  }
+  float sf = scale[0], sg = scale[0];
+#pragma unroll
+  for (int p = 1; p < kParts; ++p) {
+    if (u.first / kScaleDims == p) sf = scale[p];
+    if (u.second / kScaleDims == p) sg = scale[p];
+  }
+  *reinterpret_cast<uint32_t*>(row + u.first / 2) = codes8(f, __frcp_rn(sf));
+  *reinterpret_cast<uint32_t*>(row + u.second / 2) = codes8(g, __frcp_rn(sg));
+  if ((lane & (kUnits - 1)) == 0) {
+#pragma unroll
+    for (int p = 0; p < kParts; p += 2)
+      *reinterpret_cast<uint32_t*>(scales + p) = (__float_as_uint(scale[p]) >> 16) | (__float_as_uint(scale[p + 1]) & 0xffff0000u);
+  }
+}
+
+// Rows one by one: queries (always), keys and values (bf16 and 4-bit pools).  A thread has one unit of HPT heads of a row, so that a
 // row's angles are read once for HPT heads.
-template <int D, int HPT, bool FP8>
+template <int D, int HPT, int BITS>
 __device__ __forceinline__ void move_rows(const AppendArgs& a, int cta) {
   constexpr int kUnits = D / 16;
-  const int turned = a.n_q_heads + (FP8 ? 0 : a.kv.n_kv_heads), copied = FP8 ? 0 : a.kv.n_kv_heads;
+  const int turned = a.n_q_heads + (BITS == 8 ? 0 : a.kv.n_kv_heads), copied = BITS == 8 ? 0 : a.kv.n_kv_heads;
   const int turned_groups = (turned + HPT - 1) / HPT, groups = turned_groups + (copied + HPT - 1) / HPT;
   const int per_row = groups * kUnits;
   const int64_t first = (int64_t)cta * kAppendThreads, item = first + threadIdx.x;
@@ -154,8 +216,8 @@ __device__ __forceinline__ void move_rows(const AppendArgs& a, int cta) {
     report_cache(a.dev_status);
     return;
   }
-  // offset of the token's row in a bf16 pool, but for the head
-  const int64_t cell = (block * a.kv.n_kv_heads * a.kv.block_tokens + pos % a.kv.block_tokens) * D;
+  // the token's row in a pool, but for the head
+  const int64_t cell = block * a.kv.n_kv_heads * a.kv.block_tokens + pos % a.kv.block_tokens;
   const bool turns = !copy && u.angle >= 0;
   uint4 x[HPT][2];                                  // what is not turned is copied as it is
   Angles t[2];
@@ -178,6 +240,18 @@ __device__ __forceinline__ void move_rows(const AppendArgs& a, int cta) {
   for (int i = 0; i < HPT; ++i) {
     const int h = head0 + i;
     if (h < heads) {
+      if (BITS == 4 && (copy || h >= a.n_q_heads)) {
+        float f[8], g[8];
+        widen8(x[i][0], f);
+        widen8(x[i][1], g);
+        if (turns) {
+#pragma unroll
+          for (int half = 0; half < 2; ++half) rotate(f, g, t[half], half, a.interleaved);
+        }
+        const int64_t row4 = cell + (int64_t)(copy ? h : h - a.n_q_heads) * a.kv.block_tokens;
+        write_codes<D>((copy ? a.kv.v : a.kv.k) + row4 * (D / 2), (copy ? a.kv.v_scale4 : a.kv.k_scale4) + row4 * (D / kScaleDims), f, g, u);
+        continue;
+      }
       if (turns) {
         float f[8], g[8];
         widen8(x[i][0], f);
@@ -188,9 +262,9 @@ __device__ __forceinline__ void move_rows(const AppendArgs& a, int cta) {
         x[i][1] = narrow8(g);
       }
       __nv_bfloat16* dst;
-      if (copy) dst = reinterpret_cast<__nv_bfloat16*>(a.kv.v) + cell + (int64_t)h * a.kv.block_tokens * D;
+      if (copy) dst = reinterpret_cast<__nv_bfloat16*>(a.kv.v) + (cell + (int64_t)h * a.kv.block_tokens) * D;
       else if (h < a.n_q_heads) dst = a.q_out.data + row * a.q_out.stride_row + h * a.q_out.stride_head;
-      else dst = reinterpret_cast<__nv_bfloat16*>(a.kv.k) + cell + (int64_t)(h - a.n_q_heads) * a.kv.block_tokens * D;
+      else dst = reinterpret_cast<__nv_bfloat16*>(a.kv.k) + (cell + (int64_t)(h - a.n_q_heads) * a.kv.block_tokens) * D;
       *reinterpret_cast<uint4*>(dst + u.first) = x[i][0];
       *reinterpret_cast<uint4*>(dst + u.second) = x[i][1];
     }
@@ -433,15 +507,16 @@ __device__ __forceinline__ void fill_group(const AppendArgs& a, int index) {
   }
 }
 
-template <int D, int HPT, bool FP8>
-__global__ void __launch_bounds__(kAppendThreads, FP8 ? 3 : 4) append_kernel(const __grid_constant__ AppendArgs a) {
+template <int D, int HPT, int BITS>
+__global__ void __launch_bounds__(kAppendThreads, BITS == 8 ? 3 : 4) append_kernel(const __grid_constant__ AppendArgs a) {
   const int fills = (int)gridDim.x - a.rotate_ctas;
-  if (FP8 && (int)blockIdx.x < fills) fill_group<D, (HPT > 1)>(a, (int)blockIdx.x);
-  else move_rows<D, HPT, FP8>(a, (int)blockIdx.x - (FP8 ? fills : 0));
+  if (BITS == 8 && (int)blockIdx.x < fills) fill_group<D, (HPT > 1)>(a, (int)blockIdx.x);
+  else move_rows<D, HPT, BITS>(a, (int)blockIdx.x - (BITS == 8 ? fills : 0));
 }
 
-template <int D, bool FP8>
+template <int D, int BITS>
 int32_t launch_append(AppendArgs& a, cudaStream_t stream) {
+  constexpr bool FP8 = BITS == 8;
   const int turned = a.n_q_heads + (FP8 ? 0 : a.kv.n_kv_heads), copied = FP8 ? 0 : a.kv.n_kv_heads;
   // Few rows: a head to a thread, a head's keys or values of a group to a CTA, so that everything is under way at once.  Where that
   // more than fills the chip: two heads to a thread, which read a row's angles once, and keys and values of several heads of a group to
@@ -461,8 +536,8 @@ int32_t launch_append(AppendArgs& a, cudaStream_t stream) {
   const int64_t per_row = (ceil_div(turned, hpt) + ceil_div(copied, hpt)) * (D / 16);
   if (per_row >= (1 << 20)) return fail(SPF_ERR_UNSUPPORTED, "spf_kv_append: too many heads");
   a.per_row_inverse = per_row > 0 ? ~0ull / (uint64_t)per_row + 1 : 0;
-  if (many) append_kernel<D, 2, FP8><<<(unsigned)(rotate + groups), kAppendThreads, 0, stream>>>(a);
-  else append_kernel<D, 1, FP8><<<(unsigned)(rotate + groups), kAppendThreads, 0, stream>>>(a);
+  if (many) append_kernel<D, 2, BITS><<<(unsigned)(rotate + groups), kAppendThreads, 0, stream>>>(a);
+  else append_kernel<D, 1, BITS><<<(unsigned)(rotate + groups), kAppendThreads, 0, stream>>>(a);
   SPF_CUDA_CHECK(cudaGetLastError());
   return SPF_OK;
 }
@@ -473,11 +548,15 @@ int32_t check_cache(const char* who, const spf_kv_cache* c, KvView* out) {
   if (c == nullptr) return fail(SPF_ERR_INVALID_ARG, "%s: cache is null", who);
   if (c->k_pool == nullptr || c->v_pool == nullptr) return fail(SPF_ERR_INVALID_ARG, "%s: k_pool or v_pool is null", who);
   if ((c->k_scale == nullptr) != (c->v_scale == nullptr))
-    return fail(SPF_ERR_INVALID_ARG, "%s: k_scale and v_scale are both given (8-bit pools) or both null (bf16 pools)", who);
+    return fail(SPF_ERR_INVALID_ARG, "%s: k_scale and v_scale are both given (8-bit and 4-bit pools) or both null (bf16 pools)", who);
+  if (c->bits != 0 && c->bits != 4 && c->bits != 8 && c->bits != 16) return fail(SPF_ERR_INVALID_ARG, "%s: bits must be 4, 8, 16 or 0 (got %d)", who, c->bits);
+  const int bits = cache_bits(c);
+  if ((bits == 16) != (c->k_scale == nullptr)) return fail(SPF_ERR_INVALID_ARG, "%s: pools of 4 and 8 bits have scales, bf16 pools none", who);
   if (reinterpret_cast<uintptr_t>(c->k_pool) % 16 != 0 || reinterpret_cast<uintptr_t>(c->v_pool) % 16 != 0)
     return fail(SPF_ERR_INVALID_ARG, "%s: k_pool or v_pool is not 16-byte aligned", who);
-  if (reinterpret_cast<uintptr_t>(c->k_scale) % 4 != 0 || reinterpret_cast<uintptr_t>(c->v_scale) % 4 != 0)
-    return fail(SPF_ERR_INVALID_ARG, "%s: k_scale or v_scale is not 4-byte aligned", who);
+  const uintptr_t aligned = bits == 4 ? 16 : 4;
+  if (reinterpret_cast<uintptr_t>(c->k_scale) % aligned != 0 || reinterpret_cast<uintptr_t>(c->v_scale) % aligned != 0)
+    return fail(SPF_ERR_INVALID_ARG, "%s: k_scale or v_scale is not %d-byte aligned", who, (int)aligned);
   if (c->n_pool_blocks < 1 || c->n_kv_heads < 1) return fail(SPF_ERR_INVALID_ARG, "%s: the pool has no blocks or no heads", who);
   if (c->block_tokens < 128 || c->block_tokens % 128 != 0)
     return fail(SPF_ERR_INVALID_ARG, "%s: block_tokens must be a positive multiple of 128 (got %d)", who, c->block_tokens);
@@ -486,8 +565,10 @@ int32_t check_cache(const char* who, const spf_kv_cache* c, KvView* out) {
   const int64_t per_block = (int64_t)c->n_kv_heads * c->block_tokens;
   if (per_block > 0x7fffffffLL || c->n_pool_blocks > 0x7fffffffLL / per_block)
     return fail(SPF_ERR_UNSUPPORTED, "%s: n_pool_blocks * n_kv_heads * block_tokens is 2^31 or more", who);
-  *out = KvView{static_cast<uint8_t*>(c->k_pool), static_cast<uint8_t*>(c->v_pool), c->k_scale, c->v_scale, c->n_pool_blocks,
-                c->block_tokens, c->n_kv_heads};
+  *out = KvView{static_cast<uint8_t*>(c->k_pool), static_cast<uint8_t*>(c->v_pool), nullptr, nullptr, nullptr, nullptr, c->n_pool_blocks,
+                c->block_tokens, c->n_kv_heads, bits};
+  if (bits == 8) out->k_scale = static_cast<float*>(c->k_scale), out->v_scale = static_cast<float*>(c->v_scale);
+  if (bits == 4) out->k_scale4 = static_cast<uint16_t*>(c->k_scale), out->v_scale4 = static_cast<uint16_t*>(c->v_scale);
   return SPF_OK;
 }
 
@@ -581,6 +662,10 @@ extern "C" int32_t spf_kv_append(const spf_kv_cache* cache, const spf_kv_step* s
   }
   a.dev_status = dev_status;
   const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-  if (cache->k_scale != nullptr) return cache->head_dim == 64 ? launch_append<64, true>(a, stream) : launch_append<128, true>(a, stream);
-  return cache->head_dim == 64 ? launch_append<64, false>(a, stream) : launch_append<128, false>(a, stream);
+  const bool d64 = cache->head_dim == 64;
+  switch (a.kv.bits) {
+    case 4: return d64 ? launch_append<64, 4>(a, stream) : launch_append<128, 4>(a, stream);
+    case 8: return d64 ? launch_append<64, 8>(a, stream) : launch_append<128, 8>(a, stream);
+    default: return d64 ? launch_append<64, 16>(a, stream) : launch_append<128, 16>(a, stream);
+  }
 }

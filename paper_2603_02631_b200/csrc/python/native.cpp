@@ -504,29 +504,37 @@ struct Held {
 spf_kv_cache read_cache(PyObject* o, Held* held) {
   spf_kv_cache c{};
   const Ref scale(attr(o, N.k_scale)), v_scale(attr(o, N.v_scale));
-  if ((scale.p == Py_None) != (v_scale.p == Py_None)) raise(PyExc_ValueError, "k_scale and v_scale are both given (8-bit pools) or both None (bf16 pools)");
-  const bool bits8 = scale.p != Py_None;
-  const at::ScalarType type = bits8 ? at::kByte : at::kBFloat16;
+  if ((scale.p == Py_None) != (v_scale.p == Py_None)) raise(PyExc_ValueError, "k_scale and v_scale are both given (8-bit and 4-bit pools) or both None (bf16 pools)");
+  const bool scaled = scale.p != Py_None, bits4 = scaled && THPVariable_Check(scale.p) && THPVariable_Unpack(scale.p).scalar_type() == at::kBFloat16;
+  const at::ScalarType type = scaled ? at::kByte : at::kBFloat16;
   held->tensors.reserve(16);
   const at::Tensor& k = held->keep_attr(o, N.k_pool, type, "k_pool");
   const at::Tensor& v = held->keep_attr(o, N.v_pool, type, "v_pool");
   if (k.dim() != 4 || k.sizes() != v.sizes() || !k.is_contiguous() || !v.is_contiguous())
     raise(PyExc_ValueError, "k_pool and v_pool must be contiguous [n_pool_blocks, Hkv, block_tokens, d] of one shape");
-  if (k.size(1) > INT32_MAX || k.size(2) > INT32_MAX || k.size(3) > INT32_MAX) raise(PyExc_ValueError, "the pool is too large");
+  if (k.size(1) > INT32_MAX || k.size(2) > INT32_MAX || k.size(3) > INT32_MAX / 2) raise(PyExc_ValueError, "the pool is too large");
   c.k_pool = k.data_ptr();
   c.v_pool = v.data_ptr();
   c.n_pool_blocks = k.size(0);
   c.n_kv_heads = (int32_t)k.size(1);
   c.block_tokens = (int32_t)k.size(2);
-  c.head_dim = (int32_t)k.size(3);
-  if (bits8) {
-    const at::Tensor* scales[2] = {&held->keep(device_tensor(scale.p, at::kFloat, "k_scale"), "k_scale"),
-                                   &held->keep(device_tensor(v_scale.p, at::kFloat, "v_scale"), "v_scale")};
-    for (const at::Tensor* t : scales)
+  c.head_dim = (int32_t)k.size(3) * (bits4 ? 2 : 1);
+  c.bits = bits4 ? 4 : scaled ? 8 : 16;
+  if (scaled) {
+    const at::ScalarType scale_type = bits4 ? at::kBFloat16 : at::kFloat;
+    const at::Tensor* scales[2] = {&held->keep(device_tensor(scale.p, scale_type, "k_scale"), "k_scale"),
+                                   &held->keep(device_tensor(v_scale.p, scale_type, "v_scale"), "v_scale")};
+    for (const at::Tensor* t : scales) {
+      if (bits4) {
+        if (t->dim() != 4 || !t->is_contiguous() || t->size(0) != k.size(0) || t->size(1) != k.size(1) || t->size(2) != k.size(2) || t->size(3) != c.head_dim / SPF_KV_SCALE_DIMS)
+          raise(PyExc_ValueError, "k_scale and v_scale must be contiguous bf16 [n_pool_blocks, Hkv, block_tokens, d / 32]");
+        continue;
+      }
       if (t->dim() != 3 || !t->is_contiguous() || t->size(0) != k.size(0) || t->size(1) != k.size(1) || t->size(2) != k.size(2) / SPF_KV_SCALE_TOKENS)
         raise(PyExc_ValueError, "k_scale and v_scale must be contiguous fp32 [n_pool_blocks, Hkv, block_tokens / 64]");
-    c.k_scale = scales[0]->data_ptr<float>();
-    c.v_scale = scales[1]->data_ptr<float>();
+    }
+    c.k_scale = scales[0]->data_ptr();
+    c.v_scale = scales[1]->data_ptr();
   }
   return c;
 }
