@@ -362,6 +362,91 @@ SPF_API int32_t spf_attend(const spf_kv_cache* cache, const spf_kv_step* step, c
                            size_t workspace_bytes, int32_t* dev_status, void* cuda_stream);
 
 /*
+ * What a cut of the cache goes by, beside one layer's cache of any format: for each token of a block and head
+ *   weight        DEVICE fp32 [n_pool_blocks][Hkv][block_tokens]: the attention weight that the token has received (spf_kv_weigh)
+ *   position      DEVICE int32, the same: the token's position in its sequence, whatever was cut before it; NULL: nothing was ever cut, a
+ *                 token's position is its place
+ */
+typedef struct {
+  float* weight;
+  int32_t* position;
+} spf_kv_ledger;
+
+/*
+ * Adds to the ledger the attention weights of a step's rows (spf_kv_append and spf_attend of the step come first).  For each key s and
+ * key head h of every sequence that has new tokens:
+ *     weight[h, s] = decay * weight[h, s] + sum over rows t that see s, heads g of the group of exp(softmax_scale * q[t,g] . K[h, s] - lse[t,g]),
+ * where a new token's weight from before is 0.  Rows see keys as in spf_attend.
+ *   q             as for spf_attend
+ *   attend        as the step's spf_attend had it; lse is required, and read
+ *   ledger        position may be NULL; else the new tokens' positions are written to it
+ *   options       NULL: decay 1, all rows, a token's place as its position
+ *     decay       finite, not negative
+ *     last_rows   only the last so many new tokens of a sequence count as rows (0: all of them)
+ *     positions   DEVICE int32 [n_rows], the positions of the step's tokens; NULL: a token's place in its sequence
+ * A block belongs to one sequence of the step (two that share one race).
+ * Sums are fp32, taken in an order that does not change from run to run.  A row whose lse is -inf (it saw no key) adds nothing; one with NaN
+ * makes NaN of the weights of the keys that it sees.
+ * Device conditions: SPF_ERR_CACHE in dev_status (may be NULL) as for spf_attend; keys in a block outside the pool are left out.
+ * SPF_ERR_TIMEOUT as for spf_score.
+ * Errors: SPF_ERR_INVALID_ARG, SPF_ERR_UNSUPPORTED (as for spf_attend), SPF_ERR_CUDA.
+ */
+typedef struct {
+  float decay;
+  int32_t last_rows;
+  const int32_t* positions;
+} spf_kv_weigh_options;
+
+SPF_API int32_t spf_kv_weigh(const spf_kv_cache* cache, const spf_kv_step* step, const spf_rows* q, int32_t n_q_heads,
+                             float softmax_scale, const spf_attend_options* attend, const spf_kv_ledger* ledger,
+                             const spf_kv_weigh_options* options, int32_t* dev_status, void* cuda_stream);
+
+/*
+ * Cuts sequences to a budget: copies what is kept of them, keys, values, their scales and the ledger, to other blocks of the same pools.
+ * For each sequence b of seq_lens[b] = n tokens and each key head, min(n, keep[b]) tokens are kept (n if keep[b] is more, none if it is
+ * negative) and put one after the other, in the order of their places, into the blocks of to_table.  Kept are those with a position below
+ * n_first, or of n_seen[b] - n_recent and above, then those of the largest weight; of equals, and of the former where they are too many, those
+ * of the lowest places.  NaN ranks below every number.  Heads keep different tokens; a sequence's length, the same for all of them, goes to to_lens.
+ * The blocks that the call reads are left as they were, and may be given up, or kept (a prefix that other sequences share).
+ *
+ *   n_seqs        1 ... 2^20
+ *   seq_lens      DEVICE int32 [n_seqs], at most table_stride * block_tokens
+ *   block_table   DEVICE int32 [n_seqs][table_stride], as in spf_kv_step
+ *   keep          DEVICE int32 [n_seqs]; at most to_stride * block_tokens of a sequence's tokens are kept
+ *   to_table      DEVICE int32 [n_seqs][to_stride]: the blocks that receive the tokens, none of which is one that the call reads, each in one
+ *                 place only (blocks that are read and written race)
+ *   to_lens       DEVICE int32 [n_seqs], out; may be seq_lens
+ *   n_first, n_recent   0 or more
+ *   n_seen        DEVICE int32 [n_seqs], how many tokens the sequences have had, or NULL: seq_lens
+ *   workspace     DEVICE, 256-byte aligned, spf_kv_evict_workspace_bytes(); contents irrelevant on entry, unspecified on exit.  Calls
+ *                 that share one must be ordered on one stream.
+ * Places behind a sequence's new length are left as they were.  8-bit pools: a group of SPF_KV_SCALE_TOKENS tokens gets the largest scale of
+ * those that its tokens come from, and their bytes are rounded to it (exact between powers of two unless they become subnormal).
+ * Device conditions: SPF_ERR_CACHE in dev_status (may be NULL): a length below zero or beyond the table (it is taken to be 0), or a block outside the
+ * pool: tokens that should be read from one count as tokens of weight 0 and position 0 and are left out of the copy, as are those that should
+ * be written to one.
+ * Errors: SPF_ERR_INVALID_ARG, SPF_ERR_UNSUPPORTED (head_dim, the cache's limit, more than 2^20 sequences times heads, tables of more than
+ * 2^30 tokens a sequence), SPF_ERR_WORKSPACE, SPF_ERR_CUDA.
+ */
+typedef struct {
+  int32_t n_seqs;
+  int32_t table_stride;
+  int32_t to_stride;
+  int32_t n_first;
+  int32_t n_recent;
+  const int32_t* seq_lens;
+  const int32_t* block_table;
+  const int32_t* keep;
+  const int32_t* to_table;
+  int32_t* to_lens;
+  const int32_t* n_seen;
+} spf_kv_cut;
+
+SPF_API size_t spf_kv_evict_workspace_bytes(const spf_kv_cache* cache, int32_t n_seqs, int32_t to_stride);
+SPF_API int32_t spf_kv_evict(const spf_kv_cache* cache, const spf_kv_ledger* ledger, const spf_kv_cut* cut, void* workspace,
+                             size_t workspace_bytes, int32_t* dev_status, void* cuda_stream);
+
+/*
  * spf_score on a PAGED 8-bit key cache, as spf_kv_append writes it: blocks as for spf_score_paged, key s of a prompt, in block
  * block_table[s / block_tokens], worth
  *     k_scales[l][block][hk][(s % block_tokens) / SPF_KV_SCALE_TOKENS] * E4M3(byte).

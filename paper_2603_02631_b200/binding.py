@@ -97,6 +97,20 @@ class _AttendOptions(ctypes.Structure):
                 ("first_keys", ctypes.c_void_p), ("see_all", ctypes.c_int32)]
 
 
+class _KvLedger(ctypes.Structure):
+    _fields_ = [("weight", ctypes.c_void_p), ("position", ctypes.c_void_p)]
+
+
+class _KvWeighOptions(ctypes.Structure):
+    _fields_ = [("decay", ctypes.c_float), ("last_rows", ctypes.c_int32), ("positions", ctypes.c_void_p)]
+
+
+class _KvCut(ctypes.Structure):
+    _fields_ = [("n_seqs", ctypes.c_int32), ("table_stride", ctypes.c_int32), ("to_stride", ctypes.c_int32), ("n_first", ctypes.c_int32),
+                ("n_recent", ctypes.c_int32), ("seq_lens", ctypes.c_void_p), ("block_table", ctypes.c_void_p), ("keep", ctypes.c_void_p),
+                ("to_table", ctypes.c_void_p), ("to_lens", ctypes.c_void_p), ("n_seen", ctypes.c_void_p)]
+
+
 def _load() -> ctypes.CDLL:
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"{LIB_PATH} is missing: build it with `python -m paper_2603_02631_b200.build` "
@@ -166,6 +180,13 @@ def _load() -> ctypes.CDLL:
     dll.spf_attend.restype = i32
     dll.spf_attend.argtypes = [ctypes.POINTER(_KvCache), ctypes.POINTER(_KvStep), ctypes.POINTER(_Rows), ctypes.POINTER(_Rows), i32,
                                ctypes.c_float, ctypes.POINTER(_AttendOptions), vp, ctypes.c_size_t, vp, vp]
+    dll.spf_kv_weigh.restype = i32
+    dll.spf_kv_weigh.argtypes = [ctypes.POINTER(_KvCache), ctypes.POINTER(_KvStep), ctypes.POINTER(_Rows), i32, ctypes.c_float,
+                                 ctypes.POINTER(_AttendOptions), ctypes.POINTER(_KvLedger), ctypes.POINTER(_KvWeighOptions), vp, vp]
+    dll.spf_kv_evict_workspace_bytes.restype = ctypes.c_size_t
+    dll.spf_kv_evict_workspace_bytes.argtypes = [ctypes.POINTER(_KvCache), i32, i32]
+    dll.spf_kv_evict.restype = i32
+    dll.spf_kv_evict.argtypes = [ctypes.POINTER(_KvCache), ctypes.POINTER(_KvLedger), ctypes.POINTER(_KvCut), vp, ctypes.c_size_t, vp, vp]
     dll.spf_keep_count.restype = i64
     dll.spf_keep_count.argtypes = [i64, ctypes.c_double]
     dll.spf_keep_rate.restype = ctypes.c_double
@@ -748,6 +769,43 @@ def spf_attend(cache: KvCache, step: KvStep, q: torch.Tensor, out: torch.Tensor,
     """Attention of a step's tokens over the cache, their own keys and values (spf_kv_append) included.  q, out: bf16
     [rows, Hq, d]; lse: fp32 [rows, Hq] of any strides; first_keys: int32 [n_seqs], the first key that a sequence's rows see."""
     _check(_native.attend(cache, step, q, out, workspace, lse, first_keys, causal, softmax_scale, dev_status, stream), "spf_attend")
+
+
+@dataclasses.dataclass
+class KvLedger:
+    """What a cut of the cache goes by (see spf_kv_ledger in include/spf.h), beside one layer's cache of any format."""
+    weight: torch.Tensor                      # fp32 [n_pool_blocks, Hkv, block_tokens]: attention weight that a token has received
+    position: Optional[torch.Tensor] = None   # int32, the same: its position in its sequence; None: nothing was ever cut
+
+
+def spf_kv_weigh(cache: KvCache, step: KvStep, q: torch.Tensor, lse: torch.Tensor, ledger: KvLedger,
+                 positions: Optional[torch.Tensor] = None, first_keys: Optional[torch.Tensor] = None, causal: bool = True,
+                 last_rows: int = 0, decay: float = 1.0, softmax_scale: float = 0.0, dev_status: Optional[torch.Tensor] = None,
+                 stream: Optional[torch.cuda.Stream] = None) -> None:
+    """Adds to the ledger the attention weights of a step's rows, after spf_attend, whose ``lse`` is read.  positions: int32 [rows], the
+    positions of the step's tokens (None: their places); last_rows: only the last so many new tokens of a sequence count (0: all); decay:
+    what weights from before the step are multiplied by."""
+    _check(_native.kv_weigh(cache, step, q, lse, ledger, positions, first_keys, causal, last_rows, decay, softmax_scale, dev_status, stream),
+           "spf_kv_weigh")
+
+
+def spf_kv_evict_workspace_bytes(cache: KvCache, to_table: torch.Tensor) -> int:
+    """Bytes of workspace for cuts to tables of this size."""
+    n = int(_native.kv_evict_workspace_bytes(cache, to_table))
+    if n == 0:
+        raise SpfError(-1, "spf_kv_evict_workspace_bytes", spf_last_error())
+    return n
+
+
+def spf_kv_evict(cache: KvCache, ledger: KvLedger, seq_lens: torch.Tensor, block_table: torch.Tensor, keep: torch.Tensor,
+                 to_table: torch.Tensor, to_lens: torch.Tensor, workspace: torch.Tensor, n_first: int = 0, n_recent: int = 0,
+                 n_seen: Optional[torch.Tensor] = None, dev_status: Optional[torch.Tensor] = None,
+                 stream: Optional[torch.cuda.Stream] = None) -> None:
+    """Copies what is kept of sequences (keys, values, ledger) to the blocks of ``to_table``: of each key head's tokens ``keep[b]``, the first
+    ``n_first`` and the last ``n_recent`` among them, the others those that have received the largest weights.  The new lengths go to
+    ``to_lens``, which may be ``seq_lens``; n_seen: int32 [n_seqs], the tokens that the sequences have had (None: seq_lens)."""
+    _check(_native.kv_evict(cache, ledger, seq_lens, block_table, keep, to_table, to_lens, workspace, n_first, n_recent, n_seen, dev_status, stream),
+           "spf_kv_evict")
 
 
 @dataclasses.dataclass

@@ -20,6 +20,14 @@ EncodeFn encoder() {
   return fn;
 }
 
+// Enough for every step with up to `max_new` new tokens a sequence.
+size_t workspace_for(const spf_kv_cache* cache, int group, int max_new, int sm_count) {
+  const size_t few = attend_step_workspace_bytes(cache, group, max_new, sm_count);
+  return (int64_t)group * max_new > step_rows(cache) ? std::max(few, attend_prompt_workspace_bytes(cache, sm_count)) : few;
+}
+
+}  // namespace
+
 int32_t check_heads(const char* who, const spf_kv_cache* cache, int32_t n_q_heads, int* group) {
   if (n_q_heads < 1) return fail(SPF_ERR_INVALID_ARG, "%s: n_q_heads must be positive", who);
   if (n_q_heads % cache->n_kv_heads != 0)
@@ -28,13 +36,23 @@ int32_t check_heads(const char* who, const spf_kv_cache* cache, int32_t n_q_head
   return SPF_OK;
 }
 
-// Enough for every step with up to `max_new` new tokens a sequence.
-size_t workspace_for(const spf_kv_cache* cache, int group, int max_new, int sm_count) {
-  const size_t few = attend_step_workspace_bytes(cache, group, max_new, sm_count);
-  return (int64_t)group * max_new > step_rows(cache) ? std::max(few, attend_prompt_workspace_bytes(cache, sm_count)) : few;
+int32_t attend_settings(const char* who, const spf_kv_cache* cache, const spf_kv_step* step, int32_t n_q_heads, float softmax_scale,
+                        const spf_attend_options* options, AttendArgs* a) {
+  const float scale = softmax_scale > 0.f ? softmax_scale : 1.0f / std::sqrt((float)cache->head_dim);
+  a->c = scale * kLog2e;
+  if (!std::isfinite(a->c)) return fail(SPF_ERR_INVALID_ARG, "%s: softmax_scale is too large", who);
+  a->causal = 1;
+  if (options != nullptr) {
+    a->causal = options->see_all == 0;
+    a->first_keys = options->first_keys;
+    a->lse = options->lse;
+    a->lse_stride_row = options->lse_stride_row;
+    a->lse_stride_head = options->lse_stride_head;
+    if (a->lse != nullptr && (a->lse_stride_row < 0 || a->lse_stride_head < 0 || (n_q_heads > 1 && a->lse_stride_head < 1) || (step->n_rows > 1 && a->lse_stride_row < 1)))
+      return fail(SPF_ERR_INVALID_ARG, "%s: the strides of lse must be positive", who);
+  }
+  return SPF_OK;
 }
-
-}  // namespace
 
 int32_t encode_pool_map(const char* who, const spf_kv_cache* cache, void* pool, int tile_rows, CUtensorMap* map) {
   const EncodeFn encode = encoder();
@@ -98,19 +116,8 @@ extern "C" int32_t spf_attend(const spf_kv_cache* cache, const spf_kv_step* step
   if (st == SPF_OK) st = check_rows(who, "out", out, n_q_heads, cache->head_dim, true, &a.out);
   if (st != SPF_OK) return st;
   if (rows_meet(a.q, n_q_heads, a.out, n_q_heads, step->n_rows, cache->head_dim)) return fail(SPF_ERR_INVALID_ARG, "%s: out overlaps q", who);
-  const float scale = softmax_scale > 0.f ? softmax_scale : 1.0f / std::sqrt((float)cache->head_dim);
-  a.c = scale * kLog2e;
-  if (!std::isfinite(a.c)) return fail(SPF_ERR_INVALID_ARG, "%s: softmax_scale is too large", who);
-  a.causal = 1;
-  if (options != nullptr) {
-    a.causal = options->see_all == 0;
-    a.first_keys = options->first_keys;
-    a.lse = options->lse;
-    a.lse_stride_row = options->lse_stride_row;
-    a.lse_stride_head = options->lse_stride_head;
-    if (a.lse != nullptr && (a.lse_stride_row < 0 || a.lse_stride_head < 0 || (n_q_heads > 1 && a.lse_stride_head < 1) || (step->n_rows > 1 && a.lse_stride_row < 1)))
-      return fail(SPF_ERR_INVALID_ARG, "%s: the strides of lse must be positive", who);
-  }
+  st = attend_settings(who, cache, step, n_q_heads, softmax_scale, options, &a);
+  if (st != SPF_OK) return st;
   a.dev_status = dev_status;
   int sm_count = 0;
   st = device_sm_count(&sm_count);

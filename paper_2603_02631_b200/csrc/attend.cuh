@@ -69,6 +69,11 @@ __device__ __forceinline__ void drain_copy(uint32_t bar, uint32_t parity) {
   while (!mbar_test_wait(bar, parity) && global_timer() - t0 < 1000000000ull) {}
 }
 
+// Host checks that the calls with query rows share: heads, and the settings of the softmax.
+int32_t check_heads(const char* who, const spf_kv_cache* cache, int32_t n_q_heads, int* group);
+int32_t attend_settings(const char* who, const spf_kv_cache* cache, const spf_kv_step* step, int32_t n_q_heads, float softmax_scale,
+                        const spf_attend_options* options, AttendArgs* a);
+
 // Tensor map of a pool: rows of d elements seen as spans of at most 128 bytes, `tile_rows` rows a copy.
 int32_t encode_pool_map(const char* who, const spf_kv_cache* cache, void* pool, int tile_rows, CUtensorMap* map);
 // 4 bits: of the scales of a pool, a row of the map being those of 128 tokens (blocks are multiples of them).

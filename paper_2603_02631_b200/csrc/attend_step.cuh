@@ -42,6 +42,11 @@ struct Traits {
   static constexpr int ROWB = D * BITS / 8, SPAN = ROWB < 128 ? ROWB : 128;
   // A stage: the keys, the values; 4 bits: their scales behind them.
   static constexpr int PARTS = D / kScaleDims, TILE = KEYS * ROWB, SCALES = INT4 ? KEYS * PARTS * 2 : 0, STAGE = (VALUES ? 2 : 1) * (TILE + SCALES);
+  // 8-bit keys are multiplied as they are, by queries in two 8-bit terms, where their logits make an attention; where weights are an output
+  // of their own (no values), in bf16: sums of 8-bit products are cut off earlier and left 1.3e-6 in them, also with a third term, and
+  // bf16 ones 6e-8.
+  static constexpr bool WIDE = FP8 && !VALUES;
+  static constexpr int TERMS = FP8 && !WIDE ? 2 : 1;
   static constexpr int QBYTES = R * D * 2;
   static constexpr int FIT = ((CTAS == 3 ? 74 : 112) * 1024 - 4096 - QBYTES) / STAGE;
   static constexpr int STAGES = FIT < kMaxStages ? FIT : kMaxStages;
@@ -124,12 +129,13 @@ __device__ __forceinline__ int code_exponent(float top) { return min(max(247 - (
 // What a row's logits need besides its elements.
 template <class T>
 struct QueryNotes {
-  float factor[T::R];                                    // 8 bits: 2^-e; 4 bits: c 2^(133 - e)
+  float factor[T::R];                                    // 8 bits: 2^-e (in bf16: 2^(120 - e)); 4 bits: c 2^(133 - e)
   float base[T::INT4 ? T::PARTS : 1][T::R];              // 4 bits: -8 2^-133 times the sum of 32 scaled elements
 };
 
 // The triple's query rows into shared memory, rows that do not exist as zeros.  8 bits: the two terms, one tile behind the other.  4
-// bits: scaled by 2^e, eight elements in the order 0 4 2 6 1 5 3 7 in which codes come out of a word, the latter four by 1/16 of that.
+// bits: scaled by 2^e, eight elements in the order 0 4 2 6 1 5 3 7 in which codes come out of a word, the latter four by 1/16 of that; 8 bits in
+// bf16: scaled too, four elements in the order 0 2 1 3 in which bytes do.
 template <class T>
 __device__ __forceinline__ void load_queries(const AttendArgs& a, const TileDesc& d, unsigned char* q_tile, QueryNotes<T>& notes) {
   constexpr int kLanes = T::D / 8;                       // threads of a row
@@ -153,7 +159,7 @@ __device__ __forceinline__ void load_queries(const AttendArgs& a, const TileDesc
       }
 #pragma unroll
       for (int o = kLanes / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o, kLanes));
-      if constexpr (T::FP8) {
+      if constexpr (T::TERMS == 2) {
         int e;
         uint2 hi, lo;
         two_terms(f, top, &e, &hi, &lo);
@@ -163,6 +169,16 @@ __device__ __forceinline__ void load_queries(const AttendArgs& a, const TileDesc
       } else {
         const int e = code_exponent(top);
         const float up = __uint_as_float(top == INFINITY ? 0x7fffffffu : (uint32_t)(e + 127) << 23), up16 = up * 0.0625f;
+        if constexpr (T::WIDE) {
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const int o = 8 * (part & 3) + 4 * i;        // of the 32 dimensions: lane (o % 16) / 4 has four of either 16
+            *reinterpret_cast<uint2*>(q_tile + q_chunk<T>(r, (part & ~3) + ((o & 15) >> 2)) + 8 * (o >> 4)) =
+                make_uint2(pack_bf16(f[4 * i] * up, f[4 * i + 2] * up), pack_bf16(f[4 * i + 1] * up, f[4 * i + 3] * up));
+          }
+          if (part == 0) notes.factor[r] = __uint_as_float((uint32_t)(120 - e + 127) << 23);
+          continue;
+        }
         *reinterpret_cast<uint4*>(q_tile + q_chunk<T>(r, part)) = make_uint4(pack_bf16(f[0] * up, f[4] * up), pack_bf16(f[2] * up, f[6] * up),
                                                                            pack_bf16(f[1] * up16, f[5] * up16), pack_bf16(f[3] * up16, f[7] * up16));
         float sum = ((f[0] + f[1]) + (f[2] + f[3])) + ((f[4] + f[5]) + (f[6] + f[7]));
@@ -179,8 +195,8 @@ __device__ __forceinline__ void load_queries(const AttendArgs& a, const TileDesc
 // of one term.
 template <class T>
 __device__ __forceinline__ void query_operand(uint32_t q_addr, int row, int step, int lane, uint32_t (&b)[4]) {
-  if constexpr (T::INT4) {
-    // four lanes have the 32 elements of a scale, a row of eight each
+  if constexpr (T::INT4 || T::WIDE) {
+    // four lanes have 32 elements, eight each, one behind the other
     asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(b[0]), "=r"(b[1]), "=r"(b[2]), "=r"(b[3])
                  : "r"(q_addr + q_chunk<T>(row + (lane >> 2), 4 * step + (lane & 3))));
   } else if constexpr (T::FP8) ldsm4(q_addr + q8_chunk<T>(row + (lane & 7), 4 * step + (lane >> 3)), b);
@@ -193,7 +209,7 @@ __device__ __forceinline__ void query_operand(uint32_t q_addr, int row, int step
 template <class T>
 __device__ __forceinline__ int operand_key(int r, int half) {
   if constexpr (T::INT4) return half ? r + 4 : r + 2 * (r & 4);
-  return T::FP8 ? 2 * r + half : r + 8 * half;
+  return T::FP8 && T::VALUES ? 2 * r + half : r + 8 * half;
 }
 // The 16 keys from `key` on as the left operand: bf16 16 dimensions (of chunk pair `step`), 8 bits 32; 4 bits: words of eight codes of two
 // times 32 dimensions.
@@ -208,7 +224,7 @@ __device__ __forceinline__ int key_of(int lane, int half) { return operand_key<T
 // What a thread keeps of a triple's queries.
 template <class T>
 struct Queries {
-  static constexpr int kTerms = T::FP8 ? 2 : 1, kSteps = T::FP8 ? T::D / 64 : T::D / 32;   // four registers each
+  static constexpr int kTerms = T::TERMS, kSteps = kTerms == 2 ? T::D / 64 : T::D / 32;   // four registers each
   uint32_t q[T::QREGS ? kTerms * kSteps * T::NT : 1][4];
   float factor[T::NT][2];                                // of its rows, 2 (lane % 4) and the next of every 8
   float base[T::INT4 ? T::PARTS : 1][T::INT4 ? T::NT : 1][2];
@@ -296,6 +312,50 @@ __device__ __forceinline__ void tile_logits(float (&z)[T::KT][T::NT][4], const Q
         }
       }
     }
+  } else if constexpr (T::WIDE) {
+    // A byte s eeee mmm moved to the bits s 0000eeee mmm0000 of a bf16 number is its value times 2^-120, subnormals included.  The NaN patterns
+    // look like 480 then, so they are looked for.
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) z[kt][nt][e] = 0.f;
+    uint32_t nan[KT][2] = {};
+#pragma unroll
+    for (int x = 0; x < kSteps; ++x) {
+      uint32_t w[KT][4];
+#pragma unroll
+      for (int kt = 0; kt < KT; ++kt) {
+        key_operand<T>(k_tile, key + kt * 16, x, lane, w[kt]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) nan[kt][i & 1] |= (w[kt][i] & 0x7f7f7f7fu) + 0x01010101u;
+      }
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        uint32_t b[4];
+        queries.operand(q_addr, row_off, 0, x, nt, lane, b);
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const uint32_t lo = w[kt][2 * h], hi = w[kt][2 * h + 1];
+            const uint32_t a[4] = {((lo << 8) & 0x80008000u) | ((lo << 4) & 0x07f007f0u), ((hi << 8) & 0x80008000u) | ((hi << 4) & 0x07f007f0u),
+                                   (lo & 0x80008000u) | ((lo >> 4) & 0x07f007f0u), (hi & 0x80008000u) | ((hi >> 4) & 0x07f007f0u)};
+            mma16<false>(z[kt][nt], a, b[2 * h], b[2 * h + 1]);
+          }
+      }
+    }
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        if (!__any_sync(0xffffffffu, (nan[kt][h] & 0x80808080u) != 0)) continue;
+        const uint32_t row = 0xfu << (lane & 28);        // the four lanes of a key
+        if ((__ballot_sync(0xffffffffu, (nan[kt][h] & 0x80808080u) != 0) & row) == 0) continue;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) z[kt][nt][2 * h] = z[kt][nt][2 * h + 1] = __uint_as_float(0x7fffffffu);
+      }
   } else {
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt)

@@ -1,0 +1,399 @@
+// Cuts sequences of a cache to a budget: of each key head's tokens the first, the last and those of the largest weights, copied in order to
+// other blocks.
+//
+// Two kernels.  The first ranks: a cluster of CTAs has a (sequence, key head), each a part of its places.  Weights become 32-bit numbers that
+// order like them (NaN lowest; what is kept in any case highest), which stay in shared memory; a radix selection of 11 + 11 + 10 bits finds the
+// last number that is kept and how many of its equals are, each pass with one exchange of the counts over the cluster; then every warp
+// knows how many kept places lie before its own and writes them to a list.  No order of atomics shows in it.
+// The second copies: 64 places of the list (a group, which shares a scale in an 8-bit pool) are a CTA's, rows in pieces of 16 bytes.
+//
+// What bounds them: latency (three passes, four exchanges) the first, the rows' bytes the second.
+#include <cooperative_groups.h>
+#include <cuda_fp16.h>
+
+#include <algorithm>
+
+#include "kv.cuh"
+#include "tc_ptx.cuh"
+
+namespace spf {
+namespace {
+
+namespace cg = cooperative_groups;
+
+constexpr int kRankThreads = 512, kRankWarps = kRankThreads / 32, kBins = 2048;
+constexpr int kHeld = 36864;              // numbers that a CTA of the first kernel keeps (with more, they are made anew in every pass)
+constexpr int kMoveThreads = 128;
+constexpr uint32_t kAlways = 0xffffffffu;
+constexpr int64_t kMostPlaces = 1 << 30;  // of a sequence, so that a place and what is added to it stay in 32 bits
+
+struct EvictArgs {
+  KvView kv;
+  const int32_t *lens, *table, *keep, *to_table, *n_seen;
+  int32_t* to_lens;
+  int n_seqs, table_stride, to_stride, n_first, n_recent;
+  float* weight;
+  int32_t* position;
+  int32_t* list;                          // [n_seqs][n_kv_heads][to_stride * block_tokens]: kept places
+  int32_t* counts;                        // [n_seqs][n_kv_heads]
+  int32_t* dev_status;
+  int held;                               // numbers that fit into the first kernel's shared memory
+};
+
+__device__ __forceinline__ int64_t block_at(const KvView& kv, const int32_t* table, int stride, int seq, int pos) {
+  const int b = __ldg(table + (int64_t)seq * stride + pos / kv.block_tokens);
+  return b >= 0 && b < kv.n_blocks ? b : -1;
+}
+// Row of a place in the pools and the ledger, -1 outside.
+__device__ __forceinline__ int64_t row_at(const KvView& kv, const int32_t* table, int stride, int seq, int head, int pos) {
+  const int64_t b = block_at(kv, table, stride, seq, pos);
+  return b < 0 ? -1 : (b * kv.n_kv_heads + head) * kv.block_tokens + pos % kv.block_tokens;
+}
+
+// A token's rank as a number.
+__device__ __forceinline__ uint32_t rank_of(const EvictArgs& a, int seq, int head, int pos, int64_t recent) {
+  const int64_t row = row_at(a.kv, a.table, a.table_stride, seq, head, pos);
+  float w = 0.f;
+  int position = 0;
+  if (row >= 0) {
+    w = __ldg(a.weight + row);
+    position = a.position != nullptr ? __ldg(a.position + row) : pos;
+  } else {
+    report_cache(a.dev_status);
+  }
+  if (position < a.n_first || position >= recent) return kAlways;
+  if (w != w) return 0u;
+  const uint32_t bits = __float_as_uint(w + 0.f);        // -0 becomes 0
+  return bits ^ ((bits >> 31) != 0 ? 0xffffffffu : 0x80000000u);
+}
+
+struct RankSmem {
+  uint32_t bins[3][kBins];
+  uint32_t sums[kRankWarps];
+  uint32_t found[2];                      // bin, and what is left to be taken in it
+  uint32_t above[kRankWarps + 1], equal[kRankWarps + 1];   // kept for certain, and candidates, before each warp; the last: of the CTA
+};
+
+__global__ void __launch_bounds__(kRankThreads) rank_kernel(const __grid_constant__ EvictArgs a) {
+  extern __shared__ uint32_t held[];
+  __shared__ RankSmem sm;
+  cg::cluster_group cluster = cg::this_cluster();
+  const int parts = (int)cluster.num_blocks(), part = (int)cluster.block_rank();
+  const int pair = (int)(blockIdx.x / parts), seq = pair / a.kv.n_kv_heads, head = pair - seq * a.kv.n_kv_heads;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int64_t room = (int64_t)a.to_stride * a.kv.block_tokens;
+  int n = __ldg(a.lens + seq);
+  if (n < 0 || n > (int64_t)a.table_stride * a.kv.block_tokens) {
+    if (threadIdx.x == 0) report_cache(a.dev_status);
+    n = 0;
+  }
+  const int left = (int)min((int64_t)min(n, max(__ldg(a.keep + seq), 0)), room);
+  int32_t* list = a.list + (int64_t)pair * room;
+  if (part == 0 && threadIdx.x == 0) a.counts[pair] = left;
+  grid_launch_dependents();
+  if (left == 0) return;
+  const int each = ((n + parts - 1) / parts + 31) & ~31, lo = min(part * each, n), hi = min(lo + each, n);
+  if (left == n) {
+    for (int i = lo + (int)threadIdx.x; i < hi; i += kRankThreads) list[i] = i;
+    return;
+  }
+  const int64_t recent = (int64_t)(a.n_seen != nullptr ? __ldg(a.n_seen + seq) : n) - a.n_recent;
+  const bool fits = each <= a.held;
+  auto rank = [&](int i) { return fits ? held[i - lo] : rank_of(a, seq, head, i, recent); };
+  for (int i = threadIdx.x; i < 3 * kBins; i += kRankThreads) (&sm.bins[0][0])[i] = 0;
+  __syncthreads();
+  uint32_t prefix = 0, take = (uint32_t)left;             // the last kept number's upper bits; kept ones among those that have them
+#pragma unroll 1
+  for (int pass = 0; pass < 3; ++pass) {
+    const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
+    for (int i0 = lo; i0 < hi; i0 += kRankThreads) {
+      const int i = i0 + (int)threadIdx.x;
+      uint32_t r = 0;
+      if (i < hi) {
+        if (pass == 0) {
+          r = rank_of(a, seq, head, i, recent);
+          if (fits) held[i - lo] = r;
+        } else {
+          r = rank(i);
+        }
+      }
+      const bool counts = i < hi && (pass == 0 || (r >> (shift + bits)) == prefix);
+      const uint32_t bin = (r >> shift) & ((1u << bits) - 1u), mask = __ballot_sync(0xffffffffu, counts);
+      if (mask == 0) continue;
+      // many equal weights would be as many additions to one counter
+      const uint32_t first = __shfl_sync(0xffffffffu, bin, __ffs((int)mask) - 1);
+      if (__all_sync(0xffffffffu, !counts || bin == first)) {
+        if (lane == 0) atomicAdd(&sm.bins[pass][first], (uint32_t)__popc(mask));
+      } else if (counts) {
+        atomicAdd(&sm.bins[pass][bin], 1u);
+      }
+    }
+    cluster.sync();
+    // every CTA adds up everybody's counts and finds the bin, from the highest number down
+    constexpr int kPer = kBins / kRankThreads;
+    uint32_t own[kPer], sum = 0;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+      own[j] = 0;
+      for (int p = 0; p < parts; ++p) own[j] += cluster.map_shared_rank(&sm.bins[pass][0], p)[kBins - 1 - (int)(threadIdx.x * kPer + j)];
+      sum += own[j];
+    }
+    uint32_t upto = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint32_t v = __shfl_up_sync(0xffffffffu, upto, o);
+      if (lane >= o) upto += v;
+    }
+    if (lane == 31) sm.sums[warp] = upto;
+    __syncthreads();
+    for (int w = 0; w < warp; ++w) upto += sm.sums[w];
+    uint32_t before = upto - sum;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+      if (before < take && take <= before + own[j]) {
+        sm.found[0] = (uint32_t)(kBins - 1 - (int)(threadIdx.x * kPer + j));
+        sm.found[1] = take - before;
+      }
+      before += own[j];
+    }
+    __syncthreads();
+    prefix = prefix << bits | sm.found[0];
+    take = sm.found[1];
+  }
+  // kept: every number above `prefix`, and the first `take` that equal it
+  const int run = ((each / 32 + kRankWarps - 1) / kRankWarps) * 32, from = min(lo + warp * run, hi), to = min(from + run, hi);
+  uint32_t above = 0, equal = 0;
+  for (int i0 = from; i0 < to; i0 += 32) {
+    const int i = i0 + lane;
+    const uint32_t r = i < to ? rank(i) : 0u;
+    above += (uint32_t)__popc(__ballot_sync(0xffffffffu, i < to && r > prefix));
+    equal += (uint32_t)__popc(__ballot_sync(0xffffffffu, i < to && r == prefix));
+  }
+  if (lane == 0) sm.above[warp] = above, sm.equal[warp] = equal;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    uint32_t u = 0, e = 0;
+    for (int w = 0; w < kRankWarps; ++w) {
+      const uint32_t du = sm.above[w], de = sm.equal[w];
+      sm.above[w] = u, sm.equal[w] = e;
+      u += du, e += de;
+    }
+    sm.above[kRankWarps] = u, sm.equal[kRankWarps] = e;
+  }
+  cluster.sync();
+  above = sm.above[warp], equal = sm.equal[warp];
+  for (int p = 0; p < part; ++p) {
+    const RankSmem* other = cluster.map_shared_rank(&sm, p);
+    above += other->above[kRankWarps], equal += other->equal[kRankWarps];
+  }
+  cluster.sync();                                         // nobody leaves while its counts are read
+  for (int i0 = from; i0 < to; i0 += 32) {
+    const int i = i0 + lane;
+    const uint32_t r = i < to ? rank(i) : 0u;
+    const uint32_t more = __ballot_sync(0xffffffffu, i < to && r > prefix), same = __ballot_sync(0xffffffffu, i < to && r == prefix);
+    const uint32_t mine = (1u << lane) - 1u, u = above + (uint32_t)__popc(more & mine), e = equal + (uint32_t)__popc(same & mine);
+    if (i < to && (r > prefix || (r == prefix && e < take))) list[u + min(e, take)] = i;
+    above += (uint32_t)__popc(more), equal += (uint32_t)__popc(same);
+  }
+}
+
+// Four E4M3 bytes times a ratio, rounded to nearest, clipped at 448 (NaN: 0x7F).
+__device__ __forceinline__ uint32_t scale_bytes(uint32_t four, float ratio) {
+  uint32_t lo, hi, r;
+  asm("{\n.reg .b16 a, b;\nmov.b32 {a, b}, %2;\ncvt.rn.f16x2.e4m3x2 %0, a;\ncvt.rn.f16x2.e4m3x2 %1, b;\n}" : "=r"(lo), "=r"(hi) : "r"(four));
+  const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&lo)), y = __half22float2(*reinterpret_cast<const __half2*>(&hi));
+  asm("{\n.reg .b16 a, b;\ncvt.rn.satfinite.e4m3x2.f32 a, %2, %1;\ncvt.rn.satfinite.e4m3x2.f32 b, %4, %3;\nmov.b32 %0, {a, b};\n}"
+      : "=r"(r)
+      : "f"(x.x * ratio), "f"(x.y * ratio), "f"(y.x * ratio), "f"(y.y * ratio));
+  return r;
+}
+
+template <int D, int BITS>
+__global__ void __launch_bounds__(kMoveThreads) move_kernel(const __grid_constant__ EvictArgs a) {
+  constexpr int kRow = D * BITS / 8, kPieces = kRow / 16, kLoads = 8;
+  __shared__ int64_t from[kScaleTokens];                  // the tokens' rows in the pools, below zero: left out
+  __shared__ float scale[2][kScaleTokens], top[2];
+  grid_wait();
+  const int room_groups = a.to_stride * (a.kv.block_tokens / kScaleTokens);
+  const int64_t room = (int64_t)room_groups * kScaleTokens, items = (int64_t)a.n_seqs * a.kv.n_kv_heads * room_groups;
+  for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
+    const int pair = (int)(item / room_groups), group = (int)(item - (int64_t)pair * room_groups);
+    const int seq = pair / a.kv.n_kv_heads, head = pair - seq * a.kv.n_kv_heads, count = __ldg(a.counts + pair);
+    if (group == 0 && head == 0 && threadIdx.x == 0) a.to_lens[seq] = count;
+    const int live = min(count - group * kScaleTokens, kScaleTokens);
+    if (live <= 0) continue;
+    const int64_t to = row_at(a.kv, a.to_table, a.to_stride, seq, head, group * kScaleTokens);
+    if (to < 0) {
+      if (threadIdx.x == 0) report_cache(a.dev_status);
+      continue;
+    }
+    __syncthreads();                                      // the item before is done with shared memory
+    if (threadIdx.x < kScaleTokens) {
+      int64_t row = -1;
+      if ((int)threadIdx.x < live) {
+        const int pos = __ldg(a.list + (int64_t)pair * room + group * kScaleTokens + threadIdx.x);
+        row = row_at(a.kv, a.table, a.table_stride, seq, head, pos);
+        if (row < 0) report_cache(a.dev_status);
+      }
+      from[threadIdx.x] = row;
+      if (row >= 0) {
+        a.weight[to + threadIdx.x] = __ldg(a.weight + row);
+        if (a.position != nullptr) a.position[to + threadIdx.x] = __ldg(a.position + row);
+      }
+      if constexpr (BITS == 8) {
+#pragma unroll
+        for (int v = 0; v < 2; ++v) scale[v][threadIdx.x] = row >= 0 ? __ldg((v ? a.kv.v_scale : a.kv.k_scale) + row / kScaleTokens) : 0.f;
+      }
+    }
+    __syncthreads();
+    if constexpr (BITS == 8) {
+      if (threadIdx.x < 64) {
+        const int v = threadIdx.x >> 5, lane = threadIdx.x & 31;
+        float m = fmaxf(scale[v][lane], scale[v][lane + 32]);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+        if (lane == 0) {
+          top[v] = m;
+          if (m > 0.f) (v ? a.kv.v_scale : a.kv.k_scale)[to / kScaleTokens] = m;
+        }
+      }
+      __syncthreads();
+    }
+    const int pieces = 2 * live * kPieces;                // of keys, then of values
+    for (int i0 = threadIdx.x; i0 < pieces; i0 += kLoads * kMoveThreads) {
+      uint4 x[kLoads];
+      int64_t dst[kLoads];
+#pragma unroll
+      for (int j = 0; j < kLoads; ++j) {
+        const int i = i0 + j * kMoveThreads, v = i >= live * kPieces, token = (i - v * live * kPieces) / kPieces, piece = i % kPieces;
+        dst[j] = -1;
+        if (i < pieces && from[token] >= 0) {
+          dst[j] = (to + token) * kRow + piece * 16;
+          x[j] = __ldg(reinterpret_cast<const uint4*>((v ? a.kv.v : a.kv.k) + from[token] * kRow + piece * 16));
+          if constexpr (BITS == 8) {
+            const float ratio = __fdiv_rn(scale[v][token], top[v]);
+            if (ratio != 1.f) {
+              x[j].x = scale_bytes(x[j].x, ratio), x[j].y = scale_bytes(x[j].y, ratio);
+              x[j].z = scale_bytes(x[j].z, ratio), x[j].w = scale_bytes(x[j].w, ratio);
+            }
+          }
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < kLoads; ++j)
+        if (dst[j] >= 0) *reinterpret_cast<uint4*>((i0 + j * kMoveThreads >= live * kPieces ? a.kv.v : a.kv.k) + dst[j]) = x[j];
+    }
+    if constexpr (BITS == 4) {
+      constexpr int kWords = D / kScaleDims / 2;          // of a token's scales
+      for (int i = threadIdx.x; i < 2 * live * kWords; i += kMoveThreads) {
+        const int v = i >= live * kWords, j = i - v * live * kWords, token = j / kWords;
+        uint32_t* scales = reinterpret_cast<uint32_t*>(v ? a.kv.v_scale4 : a.kv.k_scale4);
+        if (from[token] >= 0) scales[to * kWords + j] = __ldg(scales + from[token] * kWords + j % kWords);
+      }
+    }
+  }
+}
+
+size_t list_bytes(const KvView& kv, int64_t n_seqs, int64_t to_stride) {
+  return align_up((size_t)(n_seqs * kv.n_kv_heads) * (size_t)(to_stride * kv.block_tokens) * sizeof(int32_t), 256);
+}
+size_t evict_workspace(const KvView& kv, int64_t n_seqs, int64_t to_stride) {
+  return list_bytes(kv, n_seqs, to_stride) + align_up((size_t)(n_seqs * kv.n_kv_heads) * sizeof(int32_t), 256);
+}
+
+int32_t check_cut(const char* who, const KvView& kv, int64_t n_seqs, int64_t to_stride) {
+  if (n_seqs < 1 || n_seqs > (1 << 20) || to_stride < 1) return fail(SPF_ERR_INVALID_ARG, "%s: n_seqs and to_stride must be positive (n_seqs at most 2^20)", who);
+  if (n_seqs * kv.n_kv_heads > (1 << 20)) return fail(SPF_ERR_UNSUPPORTED, "%s: more than 2^20 sequences times heads", who);
+  if (to_stride * kv.block_tokens > kMostPlaces) return fail(SPF_ERR_UNSUPPORTED, "%s: to_stride * block_tokens is more than 2^30", who);
+  return SPF_OK;
+}
+
+template <int D, int BITS>
+int32_t launch_evict(EvictArgs& a, cudaStream_t stream) {
+  // CTAs of a (sequence, key head): by the places that its table has room for
+  const int64_t places = (int64_t)a.table_stride * a.kv.block_tokens, pairs = (int64_t)a.n_seqs * a.kv.n_kv_heads;
+  const int parts = places <= 4096 ? 1 : places <= 8192 ? 2 : places <= 32768 ? 4 : 8;
+  a.held = (int)std::min<int64_t>(align_up((size_t)ceil_div(places, parts), 32), kHeld);
+  static ContextSet done;
+  const int32_t st = allow_shared_memory(reinterpret_cast<const void*>(rank_kernel), kHeld * 4, done);
+  if (st != SPF_OK) return st;
+  cudaLaunchConfig_t config{};
+  cudaLaunchAttribute attr{};
+  config.gridDim = dim3((unsigned)(pairs * parts));
+  config.blockDim = dim3(kRankThreads);
+  config.dynamicSmemBytes = (size_t)a.held * 4;
+  config.stream = stream;
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = (unsigned)parts;
+  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+  config.attrs = &attr;
+  config.numAttrs = 1;
+  SPF_CUDA_CHECK(cudaLaunchKernelEx(&config, rank_kernel, a));
+  int sm_count = 0;
+  if (const int32_t bad = device_sm_count(&sm_count); bad != SPF_OK) return bad;
+  const int64_t items = pairs * a.to_stride * (a.kv.block_tokens / kScaleTokens);
+  config.gridDim = dim3((unsigned)std::min<int64_t>(items, (int64_t)sm_count * 12));
+  config.blockDim = dim3(kMoveThreads);
+  config.dynamicSmemBytes = 0;
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  SPF_CUDA_CHECK(cudaLaunchKernelEx(&config, move_kernel<D, BITS>, a));
+  return SPF_OK;
+}
+
+}  // namespace
+
+int32_t check_ledger(const char* who, const spf_kv_ledger* ledger) {
+  if (ledger == nullptr || ledger->weight == nullptr) return fail(SPF_ERR_INVALID_ARG, "%s: ledger or its weight is null", who);
+  if (reinterpret_cast<uintptr_t>(ledger->weight) % 4 != 0 || reinterpret_cast<uintptr_t>(ledger->position) % 4 != 0)
+    return fail(SPF_ERR_INVALID_ARG, "%s: the ledger is not 4-byte aligned", who);
+  return SPF_OK;
+}
+
+}  // namespace spf
+
+using namespace spf;
+
+extern "C" size_t spf_kv_evict_workspace_bytes(const spf_kv_cache* cache, int32_t n_seqs, int32_t to_stride) {
+  const char* who = "spf_kv_evict_workspace_bytes";
+  clear_error();
+  KvView kv;
+  if (check_cache(who, cache, &kv) != SPF_OK || check_cut(who, kv, n_seqs, to_stride) != SPF_OK) return 0;
+  return evict_workspace(kv, n_seqs, to_stride);
+}
+
+extern "C" int32_t spf_kv_evict(const spf_kv_cache* cache, const spf_kv_ledger* ledger, const spf_kv_cut* cut, void* workspace, size_t workspace_bytes,
+                                int32_t* dev_status, void* cuda_stream) {
+  const char* who = "spf_kv_evict";
+  clear_error();
+  EvictArgs a{};
+  int32_t st = check_cache(who, cache, &a.kv);
+  if (st == SPF_OK) st = check_ledger(who, ledger);
+  if (st != SPF_OK) return st;
+  if (cut == nullptr) return fail(SPF_ERR_INVALID_ARG, "%s: cut is null", who);
+  st = check_cut(who, a.kv, cut->n_seqs, cut->to_stride);
+  if (st != SPF_OK) return st;
+  if (cut->table_stride < 1) return fail(SPF_ERR_INVALID_ARG, "%s: table_stride must be positive", who);
+  if ((int64_t)cut->table_stride * a.kv.block_tokens > kMostPlaces) return fail(SPF_ERR_UNSUPPORTED, "%s: table_stride * block_tokens is more than 2^30", who);
+  if (cut->n_first < 0 || cut->n_recent < 0) return fail(SPF_ERR_INVALID_ARG, "%s: n_first and n_recent must not be negative", who);
+  if (cut->seq_lens == nullptr || cut->block_table == nullptr || cut->keep == nullptr || cut->to_table == nullptr || cut->to_lens == nullptr)
+    return fail(SPF_ERR_INVALID_ARG, "%s: seq_lens, block_table, keep, to_table or to_lens is null", who);
+  const size_t need = evict_workspace(a.kv, cut->n_seqs, cut->to_stride);
+  if (workspace == nullptr || reinterpret_cast<uintptr_t>(workspace) % 256 != 0)
+    return fail(SPF_ERR_WORKSPACE, "%s: workspace is null or not 256-byte aligned", who);
+  if (workspace_bytes < need) return fail(SPF_ERR_WORKSPACE, "%s: workspace has %zu bytes, %zu needed", who, workspace_bytes, need);
+  a.lens = cut->seq_lens, a.table = cut->block_table, a.keep = cut->keep, a.to_table = cut->to_table, a.n_seen = cut->n_seen;
+  a.to_lens = cut->to_lens;
+  a.n_seqs = cut->n_seqs, a.table_stride = cut->table_stride, a.to_stride = cut->to_stride, a.n_first = cut->n_first, a.n_recent = cut->n_recent;
+  a.weight = ledger->weight, a.position = ledger->position;
+  a.list = static_cast<int32_t*>(workspace);
+  a.counts = reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + list_bytes(a.kv, cut->n_seqs, cut->to_stride));
+  a.dev_status = dev_status;
+  const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+  const bool d64 = cache->head_dim == 64;
+  switch (a.kv.bits) {
+    case 4: return d64 ? launch_evict<64, 4>(a, stream) : launch_evict<128, 4>(a, stream);
+    case 8: return d64 ? launch_evict<64, 8>(a, stream) : launch_evict<128, 8>(a, stream);
+    default: return d64 ? launch_evict<64, 16>(a, stream) : launch_evict<128, 16>(a, stream);
+  }
+}

@@ -49,6 +49,7 @@ inline int cache_bits(const spf_kv_cache* c) { return c->bits != 0 ? c->bits : c
 // Host checks, shared by the calls on the cache; they leave the reason in the error text.
 int32_t check_cache(const char* who, const spf_kv_cache* cache, KvView* out);
 int32_t check_step(const char* who, const spf_kv_step* step, StepView* out);
+int32_t check_ledger(const char* who, const spf_kv_ledger* ledger);
 int32_t check_rows(const char* who, const char* name, const spf_rows* rows, int n_heads, int head_dim, bool written, RowsView* out);
 // Whether rows `a` that a call reads and rows `b` that it writes (`n_rows` of either, of so many heads) have an element in common.
 bool rows_meet(const RowsView& a, int a_heads, const RowsView& b, int b_heads, int n_rows, int head_dim);

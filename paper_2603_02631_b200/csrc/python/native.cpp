@@ -68,7 +68,7 @@ struct Names {
   PyObject *importance, *lse, *chunk_scores, *kept, *out_ids, *out_pos, *tok_spans, *char_spans, *counts, *dev_status, *workspace, *chunk,
       *pool_kernel, *softmax_scale, *pool_edge_rule, *force_first, *force_last, *max_tokens, *slots, *q, *k, *token_ids, *char_start,
       *char_end, *n_tokens, *k_pool, *v_pool, *k_scale, *v_scale, *row_start, *seq_lens, *block_table, *max_new, *table, *positions, *interleaved,
-      *k_pools, *k_scales;
+      *k_pools, *k_scales, *weight, *position;
 };
 Names N;
 
@@ -779,7 +779,132 @@ PyObject* attend(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
   }
 }
 
+// A ledger beside a cache: fp32 weights and int32 positions (or None), [n_pool_blocks, Hkv, block_tokens].
+spf_kv_ledger read_ledger(PyObject* o, const spf_kv_cache& cache, Held* held) {
+  spf_kv_ledger l{};
+  const at::Tensor& weight = held->keep_attr(o, N.weight, at::kFloat, "ledger.weight");
+  const Ref position(attr(o, N.position));
+  const at::Tensor* tensors[2] = {&weight, position.p != Py_None ? &held->keep(device_tensor(position.p, at::kInt, "ledger.position"), "ledger.position") : nullptr};
+  for (const at::Tensor* t : tensors)
+    if (t != nullptr && (t->dim() != 3 || !t->is_contiguous() || t->size(0) != cache.n_pool_blocks || t->size(1) != cache.n_kv_heads || t->size(2) != cache.block_tokens))
+      raise(PyExc_ValueError, "ledger.weight and ledger.position must be contiguous [n_pool_blocks, Hkv, block_tokens]");
+  l.weight = weight.data_ptr<float>();
+  l.position = tensors[1] != nullptr ? tensors[1]->data_ptr<int32_t>() : nullptr;
+  return l;
+}
+
+// Contiguous int32 [count] or None.
+const int32_t* read_ints(PyObject* o, const char* name, int64_t count, Held* held) {
+  if (o == Py_None) return nullptr;
+  const at::Tensor& t = held->keep(device_tensor(o, at::kInt, name), name);
+  if (t.dim() != 1 || t.numel() != count || !t.is_contiguous()) raise(PyExc_ValueError, std::string(name) + " must be contiguous int32, one of every row or sequence");
+  return t.data_ptr<int32_t>();
+}
+
+// kv_weigh(cache, step, q, lse, ledger, positions, first_keys, causal, last_rows, decay, softmax_scale, dev_status, stream) -> status
+PyObject* kv_weigh(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
+  try {
+    if (n_args != 13) raise(PyExc_TypeError, "kv_weigh takes 13 arguments");
+    Held held;
+    const spf_kv_cache cache = read_cache(args[0], &held);
+    const at::Tensor& q0 = device_tensor(args[2], at::kBFloat16, "q");
+    const int64_t n_rows = q0.dim() > 0 ? q0.size(0) : 0, heads = q0.dim() > 1 ? q0.size(1) : 0;
+    const spf_kv_step step = read_step(args[1], n_rows, &held);
+    const spf_rows q = read_rows(args[2], "q", n_rows, heads, cache.head_dim, &held);
+    const at::Tensor& lse = held.keep(device_tensor(args[3], at::kFloat, "lse"), "lse");
+    if (lse.dim() != 2 || lse.size(0) != n_rows || lse.size(1) != heads) raise(PyExc_ValueError, "lse must be fp32 [rows, heads]");
+    spf_attend_options attended{};
+    attended.lse = lse.data_ptr<float>();
+    attended.lse_stride_row = n_rows > 1 ? lse.stride(0) : 1;
+    attended.lse_stride_head = heads > 1 ? lse.stride(1) : 1;
+    attended.first_keys = read_ints(args[6], "first_keys", step.n_seqs, &held);
+    const spf_kv_ledger ledger = read_ledger(args[4], cache, &held);
+    const int causal = PyObject_IsTrue(args[7]);
+    const long long last_rows = PyLong_AsLongLong(args[8]);
+    const double decay = PyFloat_AsDouble(args[9]), scale = PyFloat_AsDouble(args[10]);
+    if (PyErr_Occurred()) throw PyFailure{};
+    if (last_rows < 0 || last_rows > INT32_MAX) raise(PyExc_ValueError, "last_rows must not be negative");
+    attended.see_all = !causal;
+    const spf_kv_weigh_options options{(float)decay, (int32_t)last_rows, read_ints(args[5], "positions", n_rows, &held)};
+    int32_t* status = read_status(args[11], &held);
+    const c10::cuda::CUDAGuard guard(held.tensors.front().device());
+    void* stream = stream_on(args[12], held);
+    return PyLong_FromLong(spf_kv_weigh(&cache, &step, &q, (int32_t)heads, (float)scale, &attended, &ledger, &options, status, stream));
+  } catch (const PyFailure&) {
+    return nullptr;
+  } catch (const std::exception& e) {
+    PyErr_SetString(PyExc_RuntimeError, e.what());
+    return nullptr;
+  }
+}
+
+// kv_evict_workspace_bytes(cache, to_table) -> bytes (0: the reason is in spf_last_error())
+PyObject* kv_evict_workspace_bytes(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
+  try {
+    if (n_args != 2) raise(PyExc_TypeError, "kv_evict_workspace_bytes takes 2 arguments");
+    Held held;
+    const spf_kv_cache cache = read_cache(args[0], &held);
+    const at::Tensor& to = held.keep(device_tensor(args[1], at::kInt, "to_table"), "to_table");
+    if (to.dim() != 2 || to.size(0) > INT32_MAX || to.size(1) > INT32_MAX) raise(PyExc_ValueError, "to_table must be [n_seqs, blocks]");
+    return PyLong_FromSize_t(spf_kv_evict_workspace_bytes(&cache, (int32_t)to.size(0), (int32_t)to.size(1)));
+  } catch (const PyFailure&) {
+    return nullptr;
+  } catch (const std::exception& e) {
+    PyErr_SetString(PyExc_RuntimeError, e.what());
+    return nullptr;
+  }
+}
+
+// kv_evict(cache, ledger, seq_lens, block_table, keep, to_table, to_lens, workspace, n_first, n_recent, n_seen, dev_status, stream) -> status
+PyObject* kv_evict(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
+  try {
+    if (n_args != 13) raise(PyExc_TypeError, "kv_evict takes 13 arguments");
+    Held held;
+    const spf_kv_cache cache = read_cache(args[0], &held);
+    const spf_kv_ledger ledger = read_ledger(args[1], cache, &held);
+    const at::Tensor& lens = held.keep(device_tensor(args[2], at::kInt, "seq_lens"), "seq_lens");
+    const int64_t n = lens.numel();
+    const at::Tensor* tables[2] = {&held.keep(device_tensor(args[3], at::kInt, "block_table"), "block_table"),
+                                   &held.keep(device_tensor(args[5], at::kInt, "to_table"), "to_table")};
+    if (lens.dim() != 1 || !lens.is_contiguous() || n > INT32_MAX) raise(PyExc_ValueError, "seq_lens must be contiguous int32 [n_seqs]");
+    for (const at::Tensor* t : tables)
+      if (t->dim() != 2 || t->size(0) != n || !t->is_contiguous() || t->size(1) > INT32_MAX)
+        raise(PyExc_ValueError, "block_table and to_table must be contiguous [n_seqs, blocks]");
+    spf_kv_cut cut{};
+    cut.n_seqs = (int32_t)n;
+    cut.table_stride = (int32_t)tables[0]->size(1);
+    cut.to_stride = (int32_t)tables[1]->size(1);
+    cut.seq_lens = lens.data_ptr<int32_t>();
+    cut.block_table = tables[0]->data_ptr<int32_t>();
+    cut.to_table = tables[1]->data_ptr<int32_t>();
+    if (args[4] == Py_None || args[6] == Py_None) raise(PyExc_TypeError, "keep and to_lens must be CUDA tensors");
+    cut.keep = read_ints(args[4], "keep", n, &held);
+    cut.to_lens = const_cast<int32_t*>(read_ints(args[6], "to_lens", n, &held));
+    const at::Tensor& ws = held.keep(tensor(args[7], "workspace"), "workspace");
+    if (!ws.is_cuda() || !ws.is_contiguous()) raise(PyExc_TypeError, "workspace must be a contiguous CUDA tensor");
+    const long long first = PyLong_AsLongLong(args[8]), recent = PyLong_AsLongLong(args[9]);
+    if (PyErr_Occurred()) throw PyFailure{};
+    if (first < 0 || first > INT32_MAX || recent < 0 || recent > INT32_MAX) raise(PyExc_ValueError, "n_first and n_recent must not be negative");
+    cut.n_first = (int32_t)first;
+    cut.n_recent = (int32_t)recent;
+    cut.n_seen = read_ints(args[10], "n_seen", n, &held);
+    int32_t* status = read_status(args[11], &held);
+    const c10::cuda::CUDAGuard guard(held.tensors.front().device());
+    void* stream = stream_on(args[12], held);
+    return PyLong_FromLong(spf_kv_evict(&cache, &ledger, &cut, ws.data_ptr(), (size_t)ws.numel() * ws.element_size(), status, stream));
+  } catch (const PyFailure&) {
+    return nullptr;
+  } catch (const std::exception& e) {
+    PyErr_SetString(PyExc_RuntimeError, e.what());
+    return nullptr;
+  }
+}
+
 PyMethodDef kMethods[] = {
+    {"kv_weigh", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(kv_weigh)), METH_FASTCALL, "A step's attention weights into the ledger."},
+    {"kv_evict", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(kv_evict)), METH_FASTCALL, "Cuts sequences to a budget."},
+    {"kv_evict_workspace_bytes", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(kv_evict_workspace_bytes)), METH_FASTCALL,
+     "Workspace of kv_evict."},
     {"score_paged_fp8_workspace_bytes", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(score_paged_fp8_workspace_bytes)), METH_FASTCALL,
      "Workspace of score_paged_fp8."},
     {"score_paged_fp8", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(score_paged_fp8)), METH_FASTCALL, "Scores prompts in 8-bit block pools."},
@@ -803,7 +928,7 @@ PyMODINIT_FUNC PyInit__native() {
   SPF_NAME(q); SPF_NAME(k); SPF_NAME(token_ids); SPF_NAME(char_start); SPF_NAME(char_end); SPF_NAME(n_tokens);
   SPF_NAME(k_pool); SPF_NAME(v_pool); SPF_NAME(k_scale); SPF_NAME(v_scale); SPF_NAME(row_start); SPF_NAME(seq_lens); SPF_NAME(block_table);
   SPF_NAME(max_new); SPF_NAME(table); SPF_NAME(positions); SPF_NAME(interleaved);
-  SPF_NAME(k_pools); SPF_NAME(k_scales);
+  SPF_NAME(k_pools); SPF_NAME(k_scales); SPF_NAME(weight); SPF_NAME(position);
 #undef SPF_NAME
   return PyModule_Create(&kModule);
 }

@@ -1,0 +1,53 @@
+// The attention weights that a cache's tokens receive from a step's rows: what its kernels share.
+#pragma once
+
+#include "attend.cuh"
+
+namespace spf {
+
+struct WeighArgs {
+  AttendArgs a;                   // its lse is read; `out` is not used
+  CUtensorMap k_map, k_scale_map; // the latter: 4 bits
+  float* weight;                  // [n_blocks][n_kv_heads][block_tokens]
+  int32_t* position;              // the same; may be null
+  const int32_t* positions;       // [n_rows]; null: a token's place
+  float decay;
+  int last_rows;                  // of a sequence's new tokens, those that count; 0: all
+};
+
+// A sequence's part in the call: its rows that count, and the places of its new tokens.
+struct WeighSpan {
+  SeqSpan rows;                   // row0, n_new and pos0 of the rows that count
+  int fresh, fresh_row;           // place and row of the first new token
+};
+__device__ __forceinline__ WeighSpan weigh_span(const WeighArgs& w, int b) {
+  WeighSpan s;
+  s.rows = seq_span(w.a, b);
+  s.fresh = s.rows.pos0;
+  s.fresh_row = s.rows.row0;
+  const int skip = w.last_rows > 0 ? max(s.rows.n_new - w.last_rows, 0) : 0;
+  s.rows.row0 += skip;
+  s.rows.pos0 += skip;
+  s.rows.n_new -= skip;
+  return s;
+}
+
+// Base-2 log-sum-exp of a row, +inf (which makes every weight zero) for rows that do not exist or saw no key.
+__device__ __forceinline__ float row_lse2(const AttendArgs& a, int row, int head, bool exists) {
+  if (!exists) return INFINITY;
+  const float lse = __ldg(a.lse + (int64_t)row * a.lse_stride_row + (int64_t)head * a.lse_stride_head);
+  return lse == -INFINITY ? INFINITY : lse * kLog2e;
+}
+
+// What a key has received: `got` joins what the ledger holds, or replaces it where the token is one of the step's.
+__device__ __forceinline__ void book(const WeighArgs& w, int64_t cell, float held, float got, int key, int fresh, int fresh_row) {
+  if (key < fresh) {
+    w.weight[cell] = fmaf(held, w.decay, got);
+    return;
+  }
+  w.weight[cell] = got;
+  const int64_t row = (int64_t)fresh_row + key - fresh;
+  if (w.position != nullptr) w.position[cell] = w.positions != nullptr && row < w.a.step.n_rows ? __ldg(w.positions + row) : key;
+}
+
+}  // namespace spf
