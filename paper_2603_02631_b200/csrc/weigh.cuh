@@ -50,4 +50,7 @@ __device__ __forceinline__ void book(const WeighArgs& w, int64_t cell, float hel
   if (w.position != nullptr) w.position[cell] = w.positions != nullptr && row < w.a.step.n_rows ? __ldg(w.positions + row) : key;
 }
 
+// The kernel for many rows a key head and sequence; that for few is weigh.cu's own.
+int32_t weigh_prompt_launch(const WeighArgs& w, int head_dim, int sm_count, cudaStream_t stream);
+
 }  // namespace spf
