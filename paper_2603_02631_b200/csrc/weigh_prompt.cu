@@ -18,15 +18,17 @@
 namespace spf {
 namespace {
 
-constexpr int kThreads = 512, kKeys = 128, kRows = 128, kStages = 3, kKeyGroups = 4, kRowGroups = 4;
+constexpr int kThreads = 512, kKeys = 128, kStages = 3, kKeyGroups = 4, kRowGroups = 4;
+constexpr int kGroupRows = 64, kRows = kRowGroups * kGroupRows, kGroupThreads = kThreads / kRowGroups;
 
 template <int D_, int BITS_>
 struct Traits {
-  static constexpr int D = D_, BITS = BITS_, BLOCKS = D / 32, QSTAGE = kRows * D * 2;
+  static constexpr int D = D_, BITS = BITS_, BLOCKS = D / 32, QSTAGE = kGroupRows * D * 2;
+  static constexpr int STEP = D == 64 ? 2 : 1;            // eights of rows whose products are under way together
 };
 
 struct Smem {
-  float lse2[kStages][kRows];
+  float below[kRowGroups][kStages][kGroupRows];           // the rows' base-2 log-sum-exps, negated
   float sums[kRowGroups][kKeys];
   int64_t scan[kThreads / 32];
   int64_t total, start_base;
@@ -44,7 +46,7 @@ __device__ __forceinline__ int stages_of(const WeighArgs& w, const SeqSpan& s, i
   if (key0 + kKeys <= s.first) return 0;
   return (int)(((int64_t)s.n_new * w.a.group - first_row(w, s, key0) + kRows - 1) / kRows);
 }
-// Length of a (sequence, key head) in the list: a stage, and one more an item for its beginning and end.
+// Length of a (sequence, key head) in the list: its stages, and one more an item for its beginning and end.
 __device__ __forceinline__ int64_t head_cost(const WeighArgs& w, const SeqSpan& s) {
   const int tiles = (s.end + kKeys - 1) / kKeys;
   // keys before the first that every row sees, and those from the first row's on
@@ -160,33 +162,43 @@ __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uin
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+// The same with nothing to add to.
+__device__ __forceinline__ void mma_first(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+}
 // Byte offset of a row's 16-byte chunk in a stage: rows in turns begin with either half of 128 bytes, so that two rows' four chunks touch every bank.
 template <class T>
 __device__ __forceinline__ uint32_t row_chunk(int row, int chunk) { return (uint32_t)(row * (2 * T::D) + (chunk ^ ((row & 1) << 2)) * 16); }
 
-// Asks for the rows of a stage (rr: the first one's number in the sequence and key head); returns the thread's row's base-2 log-sum-exp.
+// A row of a sequence and key head as (token, head of the group), and the step to one further on, without a division.
+struct RowAt {
+  int token, g;
+  __device__ __forceinline__ RowAt(int64_t rr, int group) : token((int)(rr / group)), g((int)(rr - (int64_t)token * group)) {}
+  __device__ __forceinline__ RowAt after(const RowAt& step, int group) const {
+    RowAt r = *this;
+    r.token += step.token, r.g += step.g;
+    if (r.g >= group) r.g -= group, ++r.token;
+    return r;
+  }
+};
+
+// Asks for the rows of a stage, from (token, g) `at` on, the thread's first; `lse_at` is that of the thread's log-sum-exp, which is returned.
 template <class T>
-__device__ __forceinline__ float fetch_rows(const WeighArgs& w, const SeqSpan& s, int head, int64_t rr, uint32_t to) {
+__device__ __forceinline__ float fetch_rows(const WeighArgs& w, const SeqSpan& s, int head, RowAt at, const RowAt& lse_at, const RowAt& step, uint32_t to) {
   constexpr int kChunks = T::D / 8;
   const AttendArgs& a = w.a;
-  const uint32_t group = (uint32_t)a.group;
-  const int64_t total = (int64_t)s.n_new * a.group;
+  const int thread = (int)threadIdx.x % kGroupThreads, first = thread / kChunks, chunk = thread % kChunks;
+  const __nv_bfloat16* base = a.q.data + s.row0 * a.q.stride_row + (int64_t)head * a.group * a.q.stride_head + 8 * chunk;
 #pragma unroll
-  for (int i = 0; i < kRows * kChunks / kThreads; ++i) {
-    const int item = (int)threadIdx.x + i * kThreads, r = item / kChunks, chunk = item % kChunks;
-    const bool exists = rr + r < total;
-    const uint32_t at = exists ? (uint32_t)(rr + r) : 0u, token = at / group, g = at - token * group;
-    const __nv_bfloat16* src = a.q.data + (int64_t)(s.row0 + (int)token) * a.q.stride_row + (int64_t)(head * a.group + (int)g) * a.q.stride_head + 8 * chunk;
-    const int bytes = exists ? 16 : 0;                    // the others are zeros
+  for (int i = 0; i < kGroupRows * kChunks / kGroupThreads; ++i) {
+    const int r = first + i * (kGroupThreads / kChunks), bytes = at.token < s.n_new ? 16 : 0;     // rows that do not exist are zeros
+    const __nv_bfloat16* src = base + (bytes ? at.token * a.q.stride_row + at.g * a.q.stride_head : 0);
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + row_chunk<T>(r, chunk)), "l"(src), "r"(bytes) : "memory");
+    at = at.after(step, a.group);
   }
-  float lse2 = INFINITY;
-  if (threadIdx.x < kRows) {
-    const bool exists = rr + threadIdx.x < total;
-    const uint32_t at = exists ? (uint32_t)(rr + threadIdx.x) : 0u, token = at / group, g = at - token * group;
-    lse2 = row_lse2(a, s.row0 + (int)token, head * a.group + (int)g, exists);
-  }
-  return lse2;
+  return thread < kGroupRows ? row_lse2(a, s.row0 + lse_at.token, head * a.group + lse_at.g, lse_at.token < s.n_new) : 0.f;
 }
 
 template <int D, int BITS>
@@ -199,8 +211,11 @@ __global__ void __launch_bounds__(kThreads, 1) weigh_prompt_kernel(const __grid_
   const int64_t per = (sm.total + gridDim.x - 1) / gridDim.x, w0 = per * blockIdx.x, w1 = min(w0 + per, sm.total);
   if (w0 >= w1) return;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, key_group = warp % kKeyGroups, row_group = warp / kKeyGroups, c = lane & 3;
-  const uint32_t q_addr = smem_u32(q_rows);
+  const int in_group = (int)threadIdx.x % kGroupThreads;
+  const unsigned char* group_rows = q_rows + row_group * kStages * T::QSTAGE;
+  const uint32_t q_addr = smem_u32(group_rows);           // of the copies
   const int64_t pool_rows = a.kv.n_blocks * a.kv.n_kv_heads * a.kv.block_tokens;
+  const RowAt copy_step(kGroupThreads / (D / 8), a.group), stage_step(kRows, a.group);   // from a thread's row to its next, from a stage to the next
   Cursor cur = first_item(w, sm, w0);
   WeighSpan span = weigh_span(w, cur.seq);
   while (cur.at < w1) {
@@ -215,13 +230,20 @@ __global__ void __launch_bounds__(kThreads, 1) weigh_prompt_kernel(const __grid_
     }
     const SeqSpan& s = span.rows;
     const int key0 = cur.tile * kKeys, stages = stages_of(w, s, key0);
-    const int64_t row_first = first_row(w, s, key0);
+    const int row_first = first_row(w, s, key0);
     const int pool_at = pool_row(a, cur.seq, cur.head, key0);
     const bool inside = pool_at < pool_rows;
     float lse2[2];                                        // of the stages under way
+    const int group_first = row_first + row_group * kGroupRows;
+    RowAt copy_at(group_first + in_group / (D / 8), a.group), lse_at(group_first + in_group % kGroupRows, a.group);
+    auto fetch = [&](int slot) {
+      const float x = fetch_rows<T>(w, s, cur.head, copy_at, lse_at, copy_step, q_addr + slot * T::QSTAGE);
+      copy_at = copy_at.after(stage_step, a.group), lse_at = lse_at.after(stage_step, a.group);
+      return x;
+    };
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      lse2[i] = i < stages ? fetch_rows<T>(w, s, cur.head, row_first + i * kRows, q_addr + i * T::QSTAGE) : 0.f;
+      lse2[i] = i < stages ? fetch(i) : 0.f;
       asm volatile("cp.async.commit_group;" ::: "memory");
     }
     float held = 0.f;
@@ -249,56 +271,79 @@ __global__ void __launch_bounds__(kThreads, 1) weigh_prompt_kernel(const __grid_
     guard_below = __reduce_max_sync(0xffffffffu, guard_below);
     float f = a.c;
     if constexpr (BITS == 8) f = logit_factor(a.c * group_scale(a.kv.k_scale, s, (key0 + key_group * 32) & ~(kScaleTokens - 1), (pool_at + key_group * 32) & ~(kScaleTokens - 1), pool_rows), 1.f);
+    const uint64_t ff = pack2(f, f);
     float sum[2][2] = {}, lost[2][2] = {};
 #pragma unroll 1
     for (int stage = 0; stage < stages; ++stage) {
       const int slot = stage % kStages;
-      if (threadIdx.x < kRows) sm.lse2[slot][threadIdx.x] = lse2[0];
+      if (in_group < kGroupRows) sm.below[row_group][slot][in_group] = -lse2[0];
       lse2[0] = lse2[1];
       asm volatile("cp.async.wait_group 1;" ::: "memory");
-      __syncthreads();                                    // the stage is there, and the one before it is read
-      if (stage + 2 < stages) lse2[1] = fetch_rows<T>(w, s, cur.head, row_first + (int64_t)(stage + 2) * kRows, q_addr + (stage + 2) % kStages * T::QSTAGE);
+      asm volatile("bar.sync %0, %1;" ::"r"(1 + row_group), "n"(kGroupThreads) : "memory");   // the stage is there, and the one before it is read
+      if (stage + 2 < stages) lse2[1] = fetch((stage + 2) % kStages);
       asm volatile("cp.async.commit_group;" ::: "memory");
-      float part[2][2] = {};
-#pragma unroll 2
-      for (int rt = 0; rt < 4; ++rt) {
-        const int r = row_group * 32 + rt * 8;
-        float z[2][4] = {};
+      uint64_t part[2][2] = {};                           // pairs: of either of the thread's rows of eight
+      // Products of some eights of rows, one instruction at a time (kProducts): they are issued in turns with the exponentials of the rows
+      // before, so that neither unit waits while all warps want the other.
+      constexpr int kStep = T::STEP, kSteps = kGroupRows / 8 / kStep, kChains = 2 * kStep, kProducts = 2 * T::BLOCKS * kChains;
+      float z[2][kStep][2][4];
+      uint4 q[kStep];
+      auto product = [&](int step, int i) {
+        const int b = i / (2 * kChains), second = i / kChains & 1, j = i % kChains >> 1, kt = i & 1;
+        float (&to)[4] = z[step & 1][j][kt];
+        if (kt == 0 && second == 0)
+          q[j] = *reinterpret_cast<const uint4*>(group_rows + slot * T::QSTAGE + row_chunk<T>((step * kStep + j) * 8 + (lane >> 2), 4 * b + c));
+        if (i < kChains) mma_first(to, k[kt][b][0][0], k[kt][b][1][0], k[kt][b][0][1], k[kt][b][1][1], q[j].x, q[j].y);
+        else if (second == 0) mma(to, k[kt][b][0][0], k[kt][b][1][0], k[kt][b][0][1], k[kt][b][1][1], q[j].x, q[j].y);
+        else mma(to, k[kt][b][0][2], k[kt][b][1][2], k[kt][b][0][3], k[kt][b][1][3], q[j].z, q[j].w);
+      };
 #pragma unroll
-        for (int b = 0; b < T::BLOCKS; ++b) {
-          uint32_t q[4];
-          asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(q[0]), "=r"(q[1]), "=r"(q[2]), "=r"(q[3])
-                       : "r"(q_addr + slot * T::QSTAGE + row_chunk<T>(r + (lane >> 2), 4 * b + c)));
+      for (int i = 0; i < kProducts; ++i) product(0, i);
 #pragma unroll
-          for (int kt = 0; kt < 2; ++kt) {
-            mma(z[kt], k[kt][b][0][0], k[kt][b][1][0], k[kt][b][0][1], k[kt][b][1][1], q[0], q[1]);
-            mma(z[kt], k[kt][b][0][2], k[kt][b][1][2], k[kt][b][0][3], k[kt][b][1][3], q[2], q[3]);
-          }
-        }
-        const float2 below = *reinterpret_cast<const float2*>(&sm.lse2[slot][r + 2 * c]);
-        const int64_t rr = row_first + (int64_t)stage * kRows + r;
-        float p[2][4];
+      for (int step = 0; step < kSteps; ++step) {
+        const int rr = group_first + stage * kRows + step * 8 * kStep;
+        float x[kStep][2][4];
 #pragma unroll
-        for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) p[kt][e] = fast_exp2(fmaf(z[kt][e], f, -((e & 1) ? below.y : below.x)));
-        if (rr < guard_below) {
+        for (int j = 0; j < kStep; ++j) {
+          const uint64_t below = *reinterpret_cast<const uint64_t*>(&sm.below[row_group][slot][(step * kStep + j) * 8 + 2 * c]);
 #pragma unroll
           for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (rr + 2 * c + (e & 1) < from[kt][e >> 1]) p[kt][e] = 0.f;
+            for (int h = 0; h < 2; ++h)
+              unpack2(fma2(pack2(z[step & 1][j][kt][2 * h], z[step & 1][j][kt][2 * h + 1]), ff, below), x[j][kt][2 * h], x[j][kt][2 * h + 1]);
         }
 #pragma unroll
-        for (int kt = 0; kt < 2; ++kt)
+        for (int i = 0; i < 8 * kStep; ++i) {
+          if (step + 1 < kSteps) {
 #pragma unroll
-          for (int h = 0; h < 2; ++h) part[kt][h] += p[kt][2 * h] + p[kt][2 * h + 1];
+            for (int n = 0; n < kProducts / (8 * kStep); ++n) product(step + 1, i * (kProducts / (8 * kStep)) + n);
+          }
+          float& e = x[i >> 3][i >> 2 & 1][i & 3];
+          asm volatile("ex2.approx.ftz.f32 %0, %0;" : "+f"(e));
+        }
+        if (rr < guard_below) {
+#pragma unroll
+          for (int j = 0; j < kStep; ++j)
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                if (rr + 8 * j + 2 * c + (e & 1) < from[kt][e >> 1]) x[j][kt][e] = 0.f;
+        }
+#pragma unroll
+        for (int j = 0; j < kStep; ++j)
+#pragma unroll
+          for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) part[kt][h] = add2(part[kt][h], pack2(x[j][kt][2 * h], x[j][kt][2 * h + 1]));
       }
 #pragma unroll
       for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const float y = __fsub_rn(part[kt][h], lost[kt][h]), t = __fadd_rn(sum[kt][h], y);
+          float u, v;
+          unpack2(part[kt][h], u, v);
+          const float y = __fsub_rn(u + v, lost[kt][h]), t = __fadd_rn(sum[kt][h], y);
           lost[kt][h] = __fsub_rn(__fsub_rn(t, sum[kt][h]), y);
           sum[kt][h] = t;
         }
@@ -328,7 +373,7 @@ __global__ void __launch_bounds__(kThreads, 1) weigh_prompt_kernel(const __grid_
 
 template <int D, int BITS>
 int32_t launch(const WeighArgs& w, int sm_count, cudaStream_t stream) {
-  constexpr int kBytes = kStages * Traits<D, BITS>::QSTAGE;
+  constexpr int kBytes = kRowGroups * kStages * Traits<D, BITS>::QSTAGE;
   static ContextSet done;
   const int32_t st = allow_shared_memory(reinterpret_cast<const void*>(weigh_prompt_kernel<D, BITS>), kBytes, done);
   if (st != SPF_OK) return st;
