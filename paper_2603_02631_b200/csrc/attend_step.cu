@@ -285,11 +285,74 @@ __device__ __forceinline__ void add_values(State<T>& st, const uint32_t (&p)[T::
     }
 }
 
+// Codes of 16 keys' values in two times 32 dimensions, transposed: w[2 i] the four keys of rows 4 c ... and byte lane / 4, w[2 i + 1] of the
+// byte 8 behind it.
+template <class T>
+__device__ __forceinline__ void code_operand(uint32_t v_tile, int key, int m0, int lane, uint32_t (&w)[4]) {
+  const int r = lane & 15;
+  asm volatile("ldmatrix.sync.aligned.m16n16.x2.trans.shared.b8 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
+               : "r"(v_tile + tile_chunk<T>(key + operand_key<T>(2 * (r >> 2) + ((r >> 1) & 1), r & 1), m0 + (lane >> 4))));
+}
+// The products of 32 dimensions' codes, two words, and of eights in their places.
+template <class T>
+__device__ __forceinline__ void multiply_codes(State<T>& st, uint32_t w0, uint32_t w1, int part, int nt, const uint32_t (&p)[2]) {
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const uint32_t word = j ? w1 : w0;
+    const uint32_t codes[4] = {word & 0x000f000fu, word & 0x00f000f0u, (word >> 8) & 0x000f000fu, (word >> 8) & 0x00f000f0u};
+    mma16<false>(st.o[2 * part + j][nt], codes, p[0], p[1]);
+  }
+  const uint32_t eights[4] = {0x00080008u, 0x00800080u, 0x00080008u, 0x00800080u};
+  mma16<false>(st.eight[part][nt], eights, p[0], p[1]);
+}
+
 // 4 bits: out += scales . codes . weights.  Codes are multiplied as subnormal numbers, as those of the keys are (tile_logits); scales go into
-// the weights, rounded once to bf16, and 8 times the sum of these is subtracted at the triple's end.  x[kt][nt][h]: the weights in fp32.
-// Values of keys that a row does not see count as zeros (GUARD), whatever their scales.
-template <class T, bool GUARD>
-__device__ __forceinline__ void add_codes(State<T>& st, const float (&x)[T::KT][T::NT][2][2], const int (&sees)[T::NT][2], uint32_t v_tile, uint32_t scales, int key,
+// the weights, and 8 times the sum of these is subtracted at the triple's end.  x[kt][nt][h]: the weights in fp32.
+//
+// Weights are rounded to bf16 and turned as they are, once for all scales, and multiplied by pairs of scales as bf16 pairs, which rounds them
+// again (both together off by up to 2^-8); scaled in fp32 first, each scale would have a rounding, a packing and a turn of its own (86 us
+// instead of 79 for 32 sequences of up to 16k tokens).  Where some keys are not seen by some rows (add_some_codes) that is what is done:
+// values of keys that a row does not see count as zeros, whatever their scales.
+template <class T>
+__device__ __forceinline__ void add_codes(State<T>& st, const float (&x)[T::KT][T::NT][2][2], uint32_t v_tile, uint32_t scales, int key, int lane) {
+#pragma unroll
+  for (int kt = 0; kt < T::KT; ++kt) {
+    // scales of the two keys in a register of the right operand, rows 2 c and 2 c + 1 of either half: neighbours
+    uint32_t pairs[2][T::PARTS];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int at = key + kt * 16 + operand_key<T>(2 * (lane & 3), h);
+      uint32_t w[T::PARTS];
+      if constexpr (T::PARTS == 4) asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(scales + at * 8));
+      else asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(scales + at * 4));
+#pragma unroll
+      for (int p = 0; p < T::PARTS; ++p) pairs[h][p] = __byte_perm(w[p / 2], w[T::PARTS / 2 + p / 2], p & 1 ? 0x7632 : 0x5410);
+    }
+    uint32_t turned[T::NT][2];
+#pragma unroll
+    for (int nt = 0; nt < T::NT; ++nt)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) turned[nt][h] = transpose8(pack_bf16(x[kt][nt][h][0], x[kt][nt][h][1]));
+#pragma unroll
+    for (int m0 = 0; m0 < T::PARTS; m0 += 2) {
+      uint32_t w[4];
+      code_operand<T>(v_tile, key + kt * 16, m0, lane, w);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int part = m0 + i;
+#pragma unroll
+        for (int nt = 0; nt < T::NT; ++nt) {
+          uint32_t p[2];
+#pragma unroll
+          for (int h = 0; h < 2; ++h) asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(p[h]) : "r"(turned[nt][h]), "r"(pairs[h][part]));
+          multiply_codes<T>(st, w[2 * i], w[2 * i + 1], part, nt, p);
+        }
+      }
+    }
+  }
+}
+template <class T>
+__device__ __forceinline__ void add_some_codes(State<T>& st, const float (&x)[T::KT][T::NT][2][2], const int (&sees)[T::NT][2], uint32_t v_tile, uint32_t scales, int key,
                                           int key0, int first, int lane) {
 #pragma unroll
   for (int kt = 0; kt < T::KT; ++kt) {
@@ -298,11 +361,8 @@ __device__ __forceinline__ void add_codes(State<T>& st, const float (&x)[T::KT][
     for (int h = 0; h < 2; ++h) load_scales<T>(scales, key + kt * 16 + key_of<T>(lane, h), s[h]);
 #pragma unroll
     for (int m0 = 0; m0 < T::PARTS; m0 += 2) {
-      // two 16 x 16 byte matrices, transposed: w[2 i] the four keys of rows 4 c ... and byte lane / 4, w[2 i + 1] of the byte 8 behind it
       uint32_t w[4];
-      const int r = lane & 15;
-      asm volatile("ldmatrix.sync.aligned.m16n16.x2.trans.shared.b8 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
-                   : "r"(v_tile + tile_chunk<T>(key + kt * 16 + operand_key<T>(2 * (r >> 2) + ((r >> 1) & 1), r & 1), m0 + (lane >> 4))));
+      code_operand<T>(v_tile, key + kt * 16, m0, lane, w);
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const int part = m0 + i;
@@ -312,21 +372,12 @@ __device__ __forceinline__ void add_codes(State<T>& st, const float (&x)[T::KT][
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             float u = x[kt][nt][h][0] * s[h][part], v = x[kt][nt][h][1] * s[h][part];
-            if (GUARD) {
-              const int at = key0 + key + kt * 16 + key_of<T>(lane, h);
-              if (at < first || at >= sees[nt][0]) u = 0.f;
-              if (at < first || at >= sees[nt][1]) v = 0.f;
-            }
+            const int at = key0 + key + kt * 16 + key_of<T>(lane, h);
+            if (at < first || at >= sees[nt][0]) u = 0.f;
+            if (at < first || at >= sees[nt][1]) v = 0.f;
             p[h] = transpose8(pack_bf16(u, v));
           }
-#pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            const uint32_t word = w[2 * i + j];
-            const uint32_t codes[4] = {word & 0x000f000fu, word & 0x00f000f0u, (word >> 8) & 0x000f000fu, (word >> 8) & 0x00f000f0u};
-            mma16<false>(st.o[2 * part + j][nt], codes, p[0], p[1]);
-          }
-          const uint32_t eights[4] = {0x00080008u, 0x00800080u, 0x00080008u, 0x00800080u};
-          mma16<false>(st.eight[part][nt], eights, p[0], p[1]);
+          multiply_codes<T>(st, w[2 * i], w[2 * i + 1], part, nt, p);
         }
       }
     }
@@ -554,8 +605,8 @@ __device__ __forceinline__ void compute_tiles(const StepArgs& args, SmallSmem& s
       }
       if constexpr (T::INT4) {
         const uint32_t v_scales = k_tile + 2 * T::TILE + T::SCALES;
-        if (!guard) add_codes<T, false>(st, weight, sees, v_tile, v_scales, key_off, key0, seen.first, lane);
-        else add_codes<T, true>(st, weight, sees, v_tile, v_scales, key_off, key0, seen.first, lane);
+        if (!guard) add_codes<T>(st, weight, v_tile, v_scales, key_off, lane);
+        else add_some_codes<T>(st, weight, sees, v_tile, v_scales, key_off, key0, seen.first, lane);
       } else if (!guard) add_values<T, false>(st, p, v_tile, key_off, key0, seen, lane);
       else if (seen.all >= seen.end || !odd_values<T>(v_tile, key_off, key0, seen.all, seen.end, lane)) add_values<T, true>(st, p, v_tile, key_off, key0, seen, lane);
       else add_odd_values<T>(st, p, v_tile, key_off, key0, seen, d, a.group, a.causal, d.row_tile * R + row_off, lane);

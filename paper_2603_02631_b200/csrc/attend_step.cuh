@@ -87,6 +87,13 @@ __device__ __forceinline__ void mma16(float (&d)[4], const uint32_t (&a)[4], uin
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
+// The same onto other sums, bf16.
+__device__ __forceinline__ void mma16_from(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, const float (&c)[4]) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(c[0]), "f"(c[1]), "f"(c[2]), "f"(c[3]));
+}
+
 // 8-bit keys by the E4M3 (LOW: E5M2) term of 8-bit queries.
 template <bool LOW>
 __device__ __forceinline__ void mma32(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
@@ -303,8 +310,9 @@ __device__ __forceinline__ void tile_logits(float (&z)[T::KT][T::NT][4], const Q
             const uint32_t lo = w[kt][2 * h], hi = w[kt][2 * h + 1];
             const uint32_t first[4] = {lo & 0x000f000fu, hi & 0x000f000fu, (lo >> 8) & 0x000f000fu, (hi >> 8) & 0x000f000fu},
                            second[4] = {lo & 0x00f000f0u, hi & 0x00f000f0u, (lo >> 8) & 0x00f000f0u, (hi >> 8) & 0x00f000f0u};
-            float acc[4] = {queries.base[p][nt][0], queries.base[p][nt][1], queries.base[p][nt][0], queries.base[p][nt][1]};
-            mma16<false>(acc, first, b[0], b[1]);
+            const float base[4] = {queries.base[p][nt][0], queries.base[p][nt][1], queries.base[p][nt][0], queries.base[p][nt][1]};
+            float acc[4];
+            mma16_from(acc, first, b[0], b[1], base);
             mma16<false>(acc, second, b[2], b[3]);
 #pragma unroll
             for (int e = 0; e < 4; ++e) z[kt][nt][e] = p == 0 ? s[kt][e >> 1][p] * acc[e] : fmaf(s[kt][e >> 1][p], acc[e], z[kt][nt][e]);

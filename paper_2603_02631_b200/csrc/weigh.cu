@@ -153,6 +153,7 @@ __device__ __forceinline__ void weigh_tiles_of_cta(const WeighArgs& w, WeighSmem
   __shared__ float lse2[R];
   Queries<T> queries;
   float below[NT][2];                                    // the rows' log-sum-exps
+  int first_token = 0, last_token = 0;                   // of the rows of the tile
   int stage = 0;
   uint32_t parity = 0, join_parity = 0;
   auto join = [&] {
@@ -194,9 +195,10 @@ __device__ __forceinline__ void weigh_tiles_of_cta(const WeighArgs& w, WeighSmem
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
           for (int e = 0; e < 2; ++e) below[nt][e] = lse2[nt * 8 + 2 * (lane & 3) + e];
+        first_token = rt * R / a.group, last_token = min(d.n_new - 1, (rt * R + R - 1) / a.group);
       }
-      const int row_first = rt * R, seen_by_all = a.causal ? min(end, d.pos0 + row_first / a.group + 1) : end;
-      if (a.causal && d.pos0 + min(d.n_new - 1, (row_first + R - 1) / a.group) < key0) continue;    // no row of the tile sees any of these keys
+      const int row_first = rt * R, seen_by_all = a.causal ? min(end, d.pos0 + first_token + 1) : end;
+      if (a.causal && d.pos0 + last_token < key0) continue;    // no row of the tile sees any of these keys
       const bool guard = key0 < first || key0 + T::KEYS > seen_by_all;
       const uint32_t k_tile = ring + stage * T::STAGE;
       const float k_scale = T::FP8 ? d.k_scale[T::KEYS > kScaleTokens ? key_off / kScaleTokens : 0] : a.c;
