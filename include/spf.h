@@ -362,7 +362,7 @@ SPF_API int32_t spf_attend(const spf_kv_cache* cache, const spf_kv_step* step, c
                            size_t workspace_bytes, int32_t* dev_status, void* cuda_stream);
 
 /*
- * What a cut of the cache goes by, beside one layer's cache of any format: for each token of a block and head
+ * What a cut of the cache goes by, beside one layer's cache of any format, 16-byte aligned: for each token of a block and head
  *   weight        DEVICE fp32 [n_pool_blocks][Hkv][block_tokens]: the attention weight that the token has received (spf_kv_weigh)
  *   position      DEVICE int32, the same: the token's position in its sequence, whatever was cut before it; NULL: nothing was ever cut, a
  *                 token's position is its place

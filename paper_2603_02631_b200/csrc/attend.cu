@@ -54,12 +54,16 @@ int32_t attend_settings(const char* who, const spf_kv_cache* cache, const spf_kv
   return SPF_OK;
 }
 
+static cuuint64_t pool_rows(const spf_kv_cache* cache) {
+  return (cuuint64_t)cache->n_pool_blocks * (cuuint64_t)cache->n_kv_heads * (cuuint64_t)cache->block_tokens;
+}
+
 int32_t encode_pool_map(const char* who, const spf_kv_cache* cache, void* pool, int tile_rows, CUtensorMap* map) {
   const EncodeFn encode = encoder();
   if (encode == nullptr) return fail(SPF_ERR_CUDA, "%s: cuTensorMapEncodeTiled is not available from the driver", who);
   const int bits = cache_bits(cache);
   const int es = bits == 16 ? 2 : 1, row = cache->head_dim * bits / 8, span = std::min(row, 128);
-  const cuuint64_t rows = (cuuint64_t)cache->n_pool_blocks * (cuuint64_t)cache->n_kv_heads * (cuuint64_t)cache->block_tokens;
+  const cuuint64_t rows = pool_rows(cache);
   const cuuint64_t dims[3] = {(cuuint64_t)(span / es), rows, (cuuint64_t)(row / span)};
   const cuuint64_t strides[2] = {(cuuint64_t)row, (cuuint64_t)span};
   const cuuint32_t box[3] = {(cuuint32_t)(span / es), (cuuint32_t)tile_rows, (cuuint32_t)(row / span)}, ones[3] = {1, 1, 1};
@@ -73,17 +77,22 @@ int32_t encode_pool_map(const char* who, const spf_kv_cache* cache, void* pool, 
   return SPF_OK;
 }
 
-int32_t encode_scale_map(const char* who, const spf_kv_cache* cache, void* scales, CUtensorMap* map) {
+// Rows of `words` 32-bit words, one behind the other.
+static int32_t encode_words(const char* who, void* data, cuuint64_t words, cuuint64_t rows, CUtensorMap* map) {
   const EncodeFn encode = encoder();
   if (encode == nullptr) return fail(SPF_ERR_CUDA, "%s: cuTensorMapEncodeTiled is not available from the driver", who);
-  const cuuint64_t rows = (cuuint64_t)cache->n_pool_blocks * (cuuint64_t)cache->n_kv_heads * (cuuint64_t)cache->block_tokens;
-  const cuuint64_t words = (cuuint64_t)(128 * cache->head_dim / kScaleDims / 2);       // of 128 tokens
-  const cuuint64_t dims[2] = {words, rows / 128}, strides[1] = {words * 4};
+  const cuuint64_t dims[2] = {words, rows}, strides[1] = {words * 4};
   const cuuint32_t box[2] = {(cuuint32_t)words, 1}, ones[2] = {1, 1};
-  const CUresult r = encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT32, 2, scales, dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+  const CUresult r = encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT32, 2, data, dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
                             CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-  if (r != CUDA_SUCCESS) return fail(SPF_ERR_CUDA, "%s: encoding a tensor map of scales failed (CUresult %d)", who, (int)r);
+  if (r != CUDA_SUCCESS) return fail(SPF_ERR_CUDA, "%s: encoding a tensor map of scales or weights failed (CUresult %d)", who, (int)r);
   return SPF_OK;
+}
+int32_t encode_scale_map(const char* who, const spf_kv_cache* cache, void* scales, CUtensorMap* map) {
+  return encode_words(who, scales, (cuuint64_t)(128 * cache->head_dim / kScaleDims / 2), pool_rows(cache) / 128, map);
+}
+int32_t encode_ledger_map(const char* who, const spf_kv_cache* cache, float* numbers, int tile_rows, CUtensorMap* map) {
+  return encode_words(who, numbers, (cuuint64_t)tile_rows, pool_rows(cache) / (cuuint64_t)tile_rows, map);
 }
 
 }  // namespace spf

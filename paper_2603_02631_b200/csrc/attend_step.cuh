@@ -36,9 +36,9 @@ struct Traits {
   static constexpr int KW = KEYS / WK, KT = KW / 16;                  // keys of a warp in a tile, in sixteens
   static constexpr bool LEND = VALUES && R >= 16 && R * D < 4096;     // registers move between warpgroups
   static constexpr int THREADS = LEND ? 2 * kWarps * 32 : (kWarps + 1) * 32;
-  static constexpr int CTAS = R == 8 ? 3 : 2;                         // per SM
+  static constexpr int CTAS = R == 8 ? (VALUES ? 3 : 4) : 2;                         // per SM
   static constexpr int WTERMS = BITS == 16 && R == 8 ? 2 : 1;               // of a weight
-  static constexpr bool QREGS = NT <= 2;                              // queries stay in registers
+  static constexpr bool QREGS = NT <= 2 && !(VALUES && INT4 && R * D == 1024);   // queries stay in registers, where there is room (4 bits, 128 dimensions: 77 us without, 85 with them)
   static constexpr int ROWB = D * BITS / 8, SPAN = ROWB < 128 ? ROWB : 128;
   // A stage: the keys, the values; 4 bits: their scales behind them.
   static constexpr int PARTS = D / kScaleDims, TILE = KEYS * ROWB, SCALES = INT4 ? KEYS * PARTS * 2 : 0, STAGE = (VALUES ? 2 : 1) * (TILE + SCALES);
@@ -48,7 +48,7 @@ struct Traits {
   static constexpr bool WIDE = FP8 && !VALUES;
   static constexpr int TERMS = FP8 && !WIDE ? 2 : 1;
   static constexpr int QBYTES = R * D * 2;
-  static constexpr int FIT = ((CTAS == 3 ? 74 : 112) * 1024 - 4096 - QBYTES) / STAGE;
+  static constexpr int FIT = ((CTAS == 4 ? 55 : CTAS == 3 ? 74 : 112) * 1024 - 4096 - QBYTES) / STAGE;
   static constexpr int STAGES = FIT < kMaxStages ? FIT : kMaxStages;
   static constexpr int JOIN = D * WK * R * 4 <= 2 * TILE ? D : 2 * TILE / (WK * R * 4);   // output columns joined at a time
 };

@@ -345,8 +345,8 @@ int32_t launch_evict(EvictArgs& a, cudaStream_t stream) {
 
 int32_t check_ledger(const char* who, const spf_kv_ledger* ledger) {
   if (ledger == nullptr || ledger->weight == nullptr) return fail(SPF_ERR_INVALID_ARG, "%s: ledger or its weight is null", who);
-  if (reinterpret_cast<uintptr_t>(ledger->weight) % 4 != 0 || reinterpret_cast<uintptr_t>(ledger->position) % 4 != 0)
-    return fail(SPF_ERR_INVALID_ARG, "%s: the ledger is not 4-byte aligned", who);
+  if (reinterpret_cast<uintptr_t>(ledger->weight) % 16 != 0 || reinterpret_cast<uintptr_t>(ledger->position) % 16 != 0)
+    return fail(SPF_ERR_INVALID_ARG, "%s: the ledger is not 16-byte aligned", who);
   return SPF_OK;
 }
 

@@ -24,7 +24,9 @@ struct WeighDesc {
   int new_rows;                         // the stage's rows are not those of the stage before
 };
 
+template <class T>
 struct WeighSmem {
+  float held[T::STAGES][T::KEYS];       // what the ledger holds of the stages' keys
   unsigned long long full[kMaxStages], empty[kMaxStages], join;
   WeighDesc desc[kMaxStages];
   int64_t scan[kWarps + 1];
@@ -34,7 +36,7 @@ struct WeighSmem {
 };
 
 template <class T>
-constexpr int weigh_smem_bytes() { return T::STAGES * T::STAGE + T::QBYTES + (int)sizeof(WeighSmem) + 1024; }
+constexpr int weigh_smem_bytes() { return T::STAGES * T::STAGE + T::QBYTES + (int)sizeof(WeighSmem<T>) + 1024; }
 
 // Tiles of a (sequence, key head): all keys, since what no row sees is still multiplied by the decay.
 template <class T>
@@ -47,7 +49,7 @@ __device__ __forceinline__ int64_t weigh_cost(const WeighArgs& w, int b) {
 
 // Length of the list, and the sequence that holds the CTA's first tile.
 template <class T>
-__device__ __forceinline__ void weigh_start(const WeighArgs& w, WeighSmem& sm) {
+__device__ __forceinline__ void weigh_start(const WeighArgs& w, WeighSmem<T>& sm) {
   const int n_seqs = w.a.step.n_seqs, run = (n_seqs + T::THREADS - 1) / T::THREADS, lo = min((int)threadIdx.x * run, n_seqs), hi = min(lo + run, n_seqs);
   int64_t mine = 0;
   for (int b = lo; b < hi; ++b) mine += weigh_cost<T>(w, b);
@@ -83,7 +85,7 @@ __device__ __forceinline__ void weigh_start(const WeighArgs& w, WeighSmem& sm) {
 }
 
 template <class T>
-__device__ __forceinline__ void copy_keys(const WeighArgs& w, WeighSmem& sm, uint32_t ring, int64_t w0, int64_t w1, const Abort& ab) {
+__device__ __forceinline__ void copy_keys(const WeighArgs& w, WeighSmem<T>& sm, uint32_t ring, int64_t w0, int64_t w1, const Abort& ab) {
   const AttendArgs& a = w.a;
   const int lane = threadIdx.x & 31;
   const int64_t pool_rows = a.kv.n_blocks * a.kv.n_kv_heads * a.kv.block_tokens;
@@ -131,8 +133,9 @@ __device__ __forceinline__ void copy_keys(const WeighArgs& w, WeighSmem& sm, uin
       if (lane == j) {
         sm.desc[stage] = d;
         const uint32_t bar = smem_u32(&sm.full[stage]), to = ring + stage * T::STAGE;
-        mbar_expect_tx(bar, T::STAGE);
+        mbar_expect_tx(bar, T::STAGE + T::KEYS * 4);
         tma_load_3d(to, &w.k_map, 0, row, 0, bar);
+        tma_load_2d(smem_u32(sm.held[stage]), &w.weight_map, 0, row / T::KEYS, bar);
         if constexpr (T::INT4) tma_load_2d(to + T::TILE, &w.k_scale_map, 0, row / 128, bar);
       }
       if (++stage == T::STAGES) stage = 0, parity ^= 1;
@@ -143,7 +146,7 @@ __device__ __forceinline__ void copy_keys(const WeighArgs& w, WeighSmem& sm, uin
 }
 
 template <class T>
-__device__ __forceinline__ void weigh_tiles_of_cta(const WeighArgs& w, WeighSmem& sm, uint32_t ring, unsigned char* q_tile, int64_t n_tiles, const Abort& ab) {
+__device__ __forceinline__ void weigh_tiles_of_cta(const WeighArgs& w, WeighSmem<T>& sm, uint32_t ring, unsigned char* q_tile, int64_t n_tiles, const Abort& ab) {
   constexpr int R = T::R, NT = T::NT, KT = T::KT;
   static_assert(T::WR == 1 && KT <= 2);
   const AttendArgs& a = w.a;
@@ -172,8 +175,6 @@ __device__ __forceinline__ void weigh_tiles_of_cta(const WeighArgs& w, WeighSmem
     const int key0 = d.key0, end = d.end, first = d.first, own_key = key0 + own;
     const bool writes = books && d.cell >= 0 && own_key < end;
     const int64_t cell = (int64_t)d.cell + own;
-    float held = 0.f;
-    if (writes && own_key < d.fresh) held = w.weight[cell];
     const int row_tiles = (int)(((int64_t)d.n_new * a.group + R - 1) / R);
     float got[KT][2] = {};
     for (int rt = 0; rt < row_tiles; ++rt) {
@@ -235,7 +236,7 @@ __device__ __forceinline__ void weigh_tiles_of_cta(const WeighArgs& w, WeighSmem
       sum = (odd ? got[0][1] : got[0][0]) + __shfl_xor_sync(0xffffffffu, odd ? got[0][0] : got[0][1], 1);
       sum += __shfl_xor_sync(0xffffffffu, sum, 2);
     }
-    if (writes) book(w, cell, held, sum, own_key, d.fresh, d.fresh_row);
+    if (writes) book(w, cell, sm.held[stage][own], sum, own_key, d.fresh, d.fresh_row);
     __syncwarp();
     if (lane == 0) mbar_arrive(smem_u32(&sm.empty[stage]));
     if (++stage == T::STAGES) stage = 0, parity ^= 1;
@@ -247,7 +248,7 @@ __global__ void __launch_bounds__(T::THREADS, T::CTAS) weigh_step_kernel(const _
   extern __shared__ unsigned char smem_raw[];
   unsigned char* ring_ptr = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
   unsigned char* q_tile = ring_ptr + T::STAGES * T::STAGE;
-  WeighSmem& sm = *reinterpret_cast<WeighSmem*>(q_tile + T::QBYTES);
+  WeighSmem<T>& sm = *reinterpret_cast<WeighSmem<T>*>(q_tile + T::QBYTES);
   if (threadIdx.x == 0) {
     for (int i = 0; i < T::STAGES; ++i) {
       mbar_init(smem_u32(&sm.full[i]), 1);
@@ -270,6 +271,7 @@ int32_t launch_weigh(WeighArgs& w, const spf_kv_cache* cache, int sm_count, cuda
   using T = Traits<D, BITS, R, false>;
   static ContextSet done;
   int32_t st = encode_pool_map("spf_kv_weigh", cache, cache->k_pool, T::KEYS, &w.k_map);
+  if (st == SPF_OK) st = encode_ledger_map("spf_kv_weigh", cache, w.weight, T::KEYS, &w.weight_map);
   if constexpr (T::INT4) {
     if (st == SPF_OK) st = encode_scale_map("spf_kv_weigh", cache, cache->k_scale, &w.k_scale_map);
   }

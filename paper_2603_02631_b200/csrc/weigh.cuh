@@ -7,7 +7,7 @@ namespace spf {
 
 struct WeighArgs {
   AttendArgs a;                   // its lse is read; `out` is not used
-  CUtensorMap k_map, k_scale_map; // the latter: 4 bits
+  CUtensorMap k_map, k_scale_map, weight_map;   // few rows; the second: 4 bits
   float* weight;                  // [n_blocks][n_kv_heads][block_tokens]
   int32_t* position;              // the same; may be null
   const int32_t* positions;       // [n_rows]; null: a token's place
