@@ -120,58 +120,76 @@ __device__ __forceinline__ bool place_of(const AppendArgs& a, int seq, int row, 
 __device__ __forceinline__ uint32_t largest_bits(const float (&x)[8]) {
   uint32_t top = 0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const uint32_t m = __float_as_uint(x[i]) & 0x7fffffffu;
-    top = max(top, m == 0x7f800000u ? 0u : m);
+  for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
+  if (top == 0x7f800000u) {
+    top = 0;                                        // some are infinite, none is NaN: once more without them
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t m = __float_as_uint(x[i]) & 0x7fffffffu;
+      top = max(top, m == 0x7f800000u ? 0u : m);
+    }
   }
   return top;
 }
 // The smallest number of five significant bits s >= 2^-100 with 7 s >= the magnitude; NaN for NaN.
 __device__ __forceinline__ float short_scale(uint32_t magnitude) {
   if (magnitude > 0x7f800000u) return __uint_as_float(0x7fc00000u);
+  // a seventh but for a rounding, cut to five bits, is that number or the one below it, and 7 times either is exact (3 + 5 bits)
   const float top = __uint_as_float(magnitude);
-  uint32_t s = __float_as_uint(__fdiv_rn(top, 7.f)) & 0xfff80000u;
-  if (__uint_as_float(s) * 7.f < top) s += 0x80000u;     // the product is exact: 3 + 5 bits
+  uint32_t s = __float_as_uint(top * (1.f / 7.f)) & 0xfff80000u;
+  if (__uint_as_float(s) * 7.f < top) s += 0x80000u;
   return fmaxf(__uint_as_float(s), 0x1p-100f);
 }
 // Codes of eight elements, the first in the lowest four bits.
 __device__ __forceinline__ uint32_t codes8(const float (&x)[8], float inverse) {
-  uint32_t r = 0;
+  uint32_t two[4];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float t = fminf(fmaxf(__fmul_rn(x[i], inverse), -7.f), 7.f);
-    r |= (__float_as_uint(__fadd_rn(t, 12582920.f)) & 15u) << (4 * i);   // 1.5 * 2^23 + 8: the sum's last bits are the code
+  for (int i = 0; i < 4; ++i) {
+    uint32_t c[2];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const float t = fminf(fmaxf(__fmul_rn(x[2 * i + e], inverse), -7.f), 7.f);
+      c[e] = __float_as_uint(__fadd_rn(t, 12582920.f));   // 1.5 * 2^23 + 8: the sum's last byte is the code
+    }
+    two[i] = c[0] + 16u * c[1];
   }
-  return r;
+  return __byte_perm(__byte_perm(two[0], two[1], 0x0040), __byte_perm(two[2], two[3], 0x0040), 0x5410);
 }
-// A head's row of a 4-bit pool: its D / 16 lanes, neighbours in a warp, have a unit each.
+// A head's row of a 4-bit pool: its D / 16 lanes, neighbours in a warp, have a unit each.  `whole`: units are those of a head that is
+// rotated as a whole, in the split form (1), or two runs side by side (2); else (0) they may be either.
 template <int D>
-__device__ __forceinline__ void write_codes(uint8_t* row, uint16_t* scales, const float (&f)[8], const float (&g)[8], const Unit& u) {
+__device__ __forceinline__ void write_codes(uint8_t* row, uint16_t* scales, const float (&f)[8], const float (&g)[8], const Unit& u, int whole) {
   constexpr int kUnits = D / 16, kParts = D / kScaleDims;
-  const int lane = threadIdx.x & 31;
-  const uint32_t lanes = ((1u << kUnits) - 1u) << (lane & ~(kUnits - 1));
-  const uint32_t mf = largest_bits(f), mg = largest_bits(g);
-  float scale[kParts];
+  const uint32_t lanes = ((1u << kUnits) - 1u) << (threadIdx.x & 31 & ~(kUnits - 1));
+  uint32_t mf = largest_bits(f), mg = largest_bits(g);
+  if (whole == 1) {
+    // four neighbours have the first, and the second, runs of 32 elements each
 #pragma unroll
-  for (int p = 0; p < kParts; ++p) {
-    uint32_t m = max(u.first / kScaleDims == p ? mf : 0u, u.second / kScaleDims == p ? mg : 0u);
+    for (int o = 1; o < 4; o <<= 1) {
+      mf = max(mf, __shfl_xor_sync(lanes, mf, o));
+      mg = max(mg, __shfl_xor_sync(lanes, mg, o));
+    }
+  } else if (whole == 2) {
+    mf = max(mf, mg);                               // two neighbours have 32 elements
+    mf = mg = max(mf, __shfl_xor_sync(lanes, mf, 1));
+  } else {
+    uint32_t of_f = 0, of_g = 0;
 #pragma unroll
-    for (int o = 1; o < kUnits; o <<= 1) m = max(m, __shfl_xor_sync(lanes, m, o));
-    scale[p] = short_scale(m);
+    for (int p = 0; p < kParts; ++p) {
+      uint32_t m = max(u.first / kScaleDims == p ? mf : 0u, u.second / kScaleDims == p ? mg : 0u);
+#pragma unroll
+      for (int o = 1; o < kUnits; o <<= 1) m = max(m, __shfl_xor_sync(lanes, m, o));
+      if (u.first / kScaleDims == p) of_f = m;
+      if (u.second / kScaleDims == p) of_g = m;
+    }
+    mf = of_f, mg = of_g;
   }
-  float sf = scale[0], sg = scale[0];
-#pragma unroll
-  for (int p = 1; p < kParts; ++p) {
-    if (u.first / kScaleDims == p) sf = scale[p];
-    if (u.second / kScaleDims == p) sg = scale[p];
-  }
-  *reinterpret_cast<uint32_t*>(row + u.first / 2) = codes8(f, __frcp_rn(sf));
-  *reinterpret_cast<uint32_t*>(row + u.second / 2) = codes8(g, __frcp_rn(sg));
-  if ((lane & (kUnits - 1)) == 0) {
-#pragma unroll
-    for (int p = 0; p < kParts; p += 2)
-      *reinterpret_cast<uint32_t*>(scales + p) = (__float_as_uint(scale[p]) >> 16) | (__float_as_uint(scale[p + 1]) & 0xffff0000u);
-  }
+  const float sf = short_scale(mf), sg = whole == 2 ? sf : short_scale(mg), inverse = __frcp_rn(sf);
+  *reinterpret_cast<uint32_t*>(row + u.first / 2) = codes8(f, inverse);
+  *reinterpret_cast<uint32_t*>(row + u.second / 2) = codes8(g, whole == 2 ? inverse : __frcp_rn(sg));
+  // who has the first run of 32 elements writes their scale
+  if (u.first % kScaleDims == 0) scales[u.first / kScaleDims] = (uint16_t)(__float_as_uint(sf) >> 16);
+  if (u.second % kScaleDims == 0) scales[u.second / kScaleDims] = (uint16_t)(__float_as_uint(sg) >> 16);
 }
 
 // Rows one by one: queries (always), keys and values (bf16 and 4-bit pools).  A thread has one unit of HPT heads of a row, so that a
@@ -209,6 +227,7 @@ __device__ __forceinline__ void move_rows(const AppendArgs& a, int cta) {
   const int in_row = (int)(item - (int64_t)row * per_row), group = in_row / kUnits;
   const Unit u = unit_of(in_row % kUnits, a.rope != nullptr ? a.rot_dim : 0, a.interleaved);
   const bool copy = group >= turned_groups;
+  const int whole = a.rope == nullptr ? 2 : a.rot_dim < D ? 0 : a.interleaved ? 2 : 1;   // 4 bits
   const int head0 = (copy ? group - turned_groups : group) * HPT, heads = copy ? copied : turned;
 
   const int64_t block = pool_block(a.kv, a.step, seq, pos);
@@ -249,7 +268,7 @@ __device__ __forceinline__ void move_rows(const AppendArgs& a, int cta) {
           for (int half = 0; half < 2; ++half) rotate(f, g, t[half], half, a.interleaved);
         }
         const int64_t row4 = cell + (int64_t)(copy ? h : h - a.n_q_heads) * a.kv.block_tokens;
-        write_codes<D>((copy ? a.kv.v : a.kv.k) + row4 * (D / 2), (copy ? a.kv.v_scale4 : a.kv.k_scale4) + row4 * (D / kScaleDims), f, g, u);
+        write_codes<D>((copy ? a.kv.v : a.kv.k) + row4 * (D / 2), (copy ? a.kv.v_scale4 : a.kv.k_scale4) + row4 * (D / kScaleDims), f, g, u, whole);
         continue;
       }
       if (turns) {
