@@ -48,7 +48,9 @@ struct Traits {
   static constexpr bool WIDE = FP8 && !VALUES;
   static constexpr int TERMS = FP8 && !WIDE ? 2 : 1;
   static constexpr int QBYTES = R * D * 2;
-  static constexpr int FIT = ((CTAS == 4 ? 55 : CTAS == 3 ? 74 : 112) * 1024 - 4096 - QBYTES) / STAGE;
+  // Row tiles whose queries are kept: without values, where nothing is left behind for a row, keys wait for all of them.
+  static constexpr int TILES_HELD = !VALUES && R == 32 ? 4 : 1;
+  static constexpr int FIT = ((CTAS == 4 ? 55 : CTAS == 3 ? 74 : 112) * 1024 - 4096 - TILES_HELD * QBYTES) / STAGE;
   static constexpr int STAGES = FIT < kMaxStages ? FIT : kMaxStages;
   static constexpr int JOIN = D * WK * R * 4 <= 2 * TILE ? D : 2 * TILE / (WK * R * 4);   // output columns joined at a time
 };

@@ -6,7 +6,7 @@
 // of keys are independent of one another.  The work is the list of all key tiles of all (sequence, key head), cut into one part for each CTA.
 // Copies, products and the 4-bit and 8-bit keys' arithmetic are those of the attention for few rows; a thread's weights of a key are summed
 // over its rows, the four lanes that share a key exchange sums, and each of them books one key.  With more rows than a tile of R the tile of keys
-// stays where it is while the rows go by.  What bounds it with few rows is the read of the keys.
+// stays where it is while the rows go by, up to 128 of them from shared memory.  What bounds it with few rows is the read of the keys.
 #include <algorithm>
 #include <cmath>
 
@@ -36,7 +36,7 @@ struct WeighSmem {
 };
 
 template <class T>
-constexpr int weigh_smem_bytes() { return T::STAGES * T::STAGE + T::QBYTES + (int)sizeof(WeighSmem<T>) + 1024; }
+constexpr int weigh_smem_bytes() { return T::STAGES * T::STAGE + T::TILES_HELD * T::QBYTES + (int)sizeof(WeighSmem<T>) + 1024; }
 
 // Tiles of a (sequence, key head): all keys, since what no row sees is still multiplied by the decay.
 template <class T>
@@ -152,8 +152,9 @@ __device__ __forceinline__ void weigh_tiles_of_cta(const WeighArgs& w, WeighSmem
   const AttendArgs& a = w.a;
   const int lane = threadIdx.x & 31, key_off = (threadIdx.x >> 5) * T::KW;
   const uint32_t q_addr = smem_u32(q_tile);
-  __shared__ QueryNotes<T> notes;
-  __shared__ float lse2[R];
+  constexpr int kHeld = T::TILES_HELD;
+  __shared__ QueryNotes<T> notes[kHeld];
+  __shared__ float lse2[kHeld][R];
   Queries<T> queries;
   float below[NT][2];                                    // the rows' log-sum-exps
   int first_token = 0, last_token = 0;                   // of the rows of the tile
@@ -178,24 +179,29 @@ __device__ __forceinline__ void weigh_tiles_of_cta(const WeighArgs& w, WeighSmem
     const int row_tiles = (int)(((int64_t)d.n_new * a.group + R - 1) / R);
     float got[KT][2] = {};
     for (int rt = 0; rt < row_tiles; ++rt) {
-      if (d.new_rows || row_tiles > 1) {
+      const int slot = rt % kHeld;
+      if (slot == 0 && (d.new_rows || row_tiles > kHeld)) {
         // the warps are through with the rows before these, then they have all brought these
         if (tile > 0 || rt > 0) {
           if (!join()) return;
         }
-        TileDesc t;
-        t.row0 = d.row0, t.n_new = d.n_new, t.head = d.head, t.row_tile = rt;
-        load_queries<T>(a, t, q_tile, notes);
-        for (int r = threadIdx.x; r < R; r += kWarps * 32) {
-          const int rr = rt * R + r;
-          lse2[r] = row_lse2(a, d.row0 + rr / a.group, d.head * a.group + rr % a.group, rr < d.n_new * a.group);
+        for (int i = 0; i < min(kHeld, row_tiles - rt); ++i) {
+          TileDesc t;
+          t.row0 = d.row0, t.n_new = d.n_new, t.head = d.head, t.row_tile = rt + i;
+          load_queries<T>(a, t, q_tile + i * T::QBYTES, notes[i]);
+          for (int r = threadIdx.x; r < R; r += kWarps * 32) {
+            const int rr = (rt + i) * R + r;
+            lse2[i][r] = row_lse2(a, d.row0 + rr / a.group, d.head * a.group + rr % a.group, rr < d.n_new * a.group);
+          }
         }
         if (!join()) return;
-        queries.load(q_addr, notes, 0, lane);
+      }
+      if (d.new_rows || row_tiles > 1) {
+        queries.load(q_addr + slot * T::QBYTES, notes[slot], 0, lane);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int e = 0; e < 2; ++e) below[nt][e] = lse2[nt * 8 + 2 * (lane & 3) + e];
+          for (int e = 0; e < 2; ++e) below[nt][e] = lse2[slot][nt * 8 + 2 * (lane & 3) + e];
         first_token = rt * R / a.group, last_token = min(d.n_new - 1, (rt * R + R - 1) / a.group);
       }
       const int row_first = rt * R, seen_by_all = a.causal ? min(end, d.pos0 + first_token + 1) : end;
@@ -204,7 +210,7 @@ __device__ __forceinline__ void weigh_tiles_of_cta(const WeighArgs& w, WeighSmem
       const uint32_t k_tile = ring + stage * T::STAGE;
       const float k_scale = T::FP8 ? d.k_scale[T::KEYS > kScaleTokens ? key_off / kScaleTokens : 0] : a.c;
       float z[KT][NT][4];
-      tile_logits<T>(z, queries, q_addr, 0, k_tile, k_tile + T::TILE, key_off, lane);
+      tile_logits<T>(z, queries, q_addr + slot * T::QBYTES, 0, k_tile, k_tile + T::TILE, key_off, lane);
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         float f[2];
@@ -213,16 +219,29 @@ __device__ __forceinline__ void weigh_tiles_of_cta(const WeighArgs& w, WeighSmem
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            float p = fast_exp2(fmaf(z[kt][nt][e], f[e & 1], -below[nt][e & 1]));
-            if (guard) {
-              const int key = key0 + key_off + kt * 16 + key_of<T>(lane, e >> 1);
-              const int hi = a.causal ? min(end, d.pos0 + (row_first + nt * 8 + 2 * (lane & 3) + (e & 1)) / a.group + 1) : end;
-              if (key < first || key >= hi) p = 0.f;
-            }
-            got[kt][e >> 1] += p;
+          for (int e = 0; e < 4; ++e) z[kt][nt][e] = fast_exp2(fmaf(z[kt][nt][e], f[e & 1], -below[nt][e & 1]));
+      }
+      if (guard) {
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            // rows from (key - pos0) group on see a key
+            const int key = key0 + key_off + kt * 16 + key_of<T>(lane, h);
+            const int64_t from = key < first || key >= end ? INT64_MAX : a.causal ? ((int64_t)key - d.pos0) * a.group : 0;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+              for (int e = 0; e < 2; ++e)
+                if (row_first + nt * 8 + 2 * (lane & 3) + e < from) z[kt][nt][2 * h + e] = 0.f;
           }
       }
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) got[kt][h] += z[kt][nt][2 * h] + z[kt][nt][2 * h + 1];
     }
     // sums over the four lanes of a key, each of which ends with one key's
     float sum;
@@ -248,7 +267,7 @@ __global__ void __launch_bounds__(T::THREADS, T::CTAS) weigh_step_kernel(const _
   extern __shared__ unsigned char smem_raw[];
   unsigned char* ring_ptr = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
   unsigned char* q_tile = ring_ptr + T::STAGES * T::STAGE;
-  WeighSmem<T>& sm = *reinterpret_cast<WeighSmem<T>*>(q_tile + T::QBYTES);
+  WeighSmem<T>& sm = *reinterpret_cast<WeighSmem<T>*>(q_tile + T::TILES_HELD * T::QBYTES);
   if (threadIdx.x == 0) {
     for (int i = 0; i < T::STAGES; ++i) {
       mbar_init(smem_u32(&sm.full[i]), 1);
