@@ -5,7 +5,7 @@
 // order like them (NaN lowest; what is kept in any case highest), which stay in shared memory; a radix selection of 11 + 11 + 10 bits finds the
 // last number that is kept and how many of its equals are, each pass with one exchange of the counts over the cluster; then every warp
 // knows how many kept places lie before its own and writes them to a list.  No order of atomics shows in it.
-// The second copies: 64 places of the list (a group, which shares a scale in an 8-bit pool) are a CTA's, rows in pieces of 16 bytes.
+// The second copies: 64 places of the list (a group, which shares a scale in an 8-bit pool) are a warp's, rows in pieces of 16 bytes.
 //
 // What bounds them: latency (three passes, four exchanges) the first, the rows' bytes the second.
 #include <cooperative_groups.h>
@@ -51,20 +51,24 @@ __device__ __forceinline__ int64_t row_at(const KvView& kv, const int32_t* table
 }
 
 // A token's rank as a number.
-__device__ __forceinline__ uint32_t rank_of(const EvictArgs& a, int seq, int head, int pos, int64_t recent) {
-  const int64_t row = row_at(a.kv, a.table, a.table_stride, seq, head, pos);
-  float w = 0.f;
-  int position = 0;
-  if (row >= 0) {
-    w = __ldg(a.weight + row);
-    position = a.position != nullptr ? __ldg(a.position + row) : pos;
-  } else {
-    report_cache(a.dev_status);
-  }
+__device__ __forceinline__ uint32_t rank_of(const EvictArgs& a, float w, int position, int64_t recent) {
   if (position < a.n_first || position >= recent) return kAlways;
   if (w != w) return 0u;
   const uint32_t bits = __float_as_uint(w + 0.f);        // -0 becomes 0
   return bits ^ ((bits >> 31) != 0 ? 0xffffffffu : 0x80000000u);
+}
+// The ranks of four tokens from place pos on, a multiple of 4 (blocks are multiples of 128).
+__device__ __forceinline__ uint4 ranks_at(const EvictArgs& a, int seq, int head, int pos, int64_t recent) {
+  const int64_t row = row_at(a.kv, a.table, a.table_stride, seq, head, pos);
+  float4 w = make_float4(0.f, 0.f, 0.f, 0.f);
+  int4 at = make_int4(0, 0, 0, 0);
+  if (row >= 0) {
+    w = __ldg(reinterpret_cast<const float4*>(a.weight + row));
+    at = a.position != nullptr ? __ldg(reinterpret_cast<const int4*>(a.position + row)) : make_int4(pos, pos + 1, pos + 2, pos + 3);
+  } else {
+    report_cache(a.dev_status);
+  }
+  return make_uint4(rank_of(a, w.x, at.x, recent), rank_of(a, w.y, at.y, recent), rank_of(a, w.z, at.z, recent), rank_of(a, w.w, at.w, recent));
 }
 
 struct RankSmem {
@@ -75,7 +79,7 @@ struct RankSmem {
 };
 
 __global__ void __launch_bounds__(kRankThreads) rank_kernel(const __grid_constant__ EvictArgs a) {
-  extern __shared__ uint32_t held[];
+  extern __shared__ __align__(16) uint32_t held[];
   __shared__ RankSmem sm;
   cg::cluster_group cluster = cg::this_cluster();
   const int parts = (int)cluster.num_blocks(), part = (int)cluster.block_rank();
@@ -92,40 +96,60 @@ __global__ void __launch_bounds__(kRankThreads) rank_kernel(const __grid_constan
   if (part == 0 && threadIdx.x == 0) a.counts[pair] = left;
   grid_launch_dependents();
   if (left == 0) return;
-  const int each = ((n + parts - 1) / parts + 31) & ~31, lo = min(part * each, n), hi = min(lo + each, n);
+  // the CTA's places: chunks of 128, four to a lane
+  const int each = ((n + parts - 1) / parts + 127) & ~127, lo = min(part * each, n), hi = min(lo + each, n);
   if (left == n) {
     for (int i = lo + (int)threadIdx.x; i < hi; i += kRankThreads) list[i] = i;
     return;
   }
   const int64_t recent = (int64_t)(a.n_seen != nullptr ? __ldg(a.n_seen + seq) : n) - a.n_recent;
   const bool fits = each <= a.held;
-  auto rank = [&](int i) { return fits ? held[i - lo] : rank_of(a, seq, head, i, recent); };
+  uint4* held4 = reinterpret_cast<uint4*>(held);
+  auto ranks = [&](int i) { return fits ? held4[(i - lo) / 4] : ranks_at(a, seq, head, i, recent); };
   for (int i = threadIdx.x; i < 3 * kBins; i += kRankThreads) (&sm.bins[0][0])[i] = 0;
   __syncthreads();
   uint32_t prefix = 0, take = (uint32_t)left;             // the last kept number's upper bits; kept ones among those that have them
 #pragma unroll 1
   for (int pass = 0; pass < 3; ++pass) {
     const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
-    for (int i0 = lo; i0 < hi; i0 += kRankThreads) {
-      const int i = i0 + (int)threadIdx.x;
-      uint32_t r = 0;
-      if (i < hi) {
-        if (pass == 0) {
-          r = rank_of(a, seq, head, i, recent);
-          if (fits) held[i - lo] = r;
-        } else {
-          r = rank(i);
+    auto count = [&](int i, const uint4& four) {
+      const uint32_t r[4] = {four.x, four.y, four.z, four.w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const bool counts = i + j < hi && (pass == 0 || (r[j] >> (shift + bits)) == prefix);
+        const uint32_t bin = (r[j] >> shift) & ((1u << bits) - 1u), mask = __ballot_sync(0xffffffffu, counts);
+        if (mask == 0) continue;
+        // many equal weights would be as many additions to one counter
+        const uint32_t first = __shfl_sync(0xffffffffu, bin, __ffs((int)mask) - 1);
+        if (__all_sync(0xffffffffu, !counts || bin == first)) {
+          if (lane == 0) atomicAdd(&sm.bins[pass][first], (uint32_t)__popc(mask));
+        } else if (counts) {
+          atomicAdd(&sm.bins[pass][bin], 1u);
         }
       }
-      const bool counts = i < hi && (pass == 0 || (r >> (shift + bits)) == prefix);
-      const uint32_t bin = (r >> shift) & ((1u << bits) - 1u), mask = __ballot_sync(0xffffffffu, counts);
-      if (mask == 0) continue;
-      // many equal weights would be as many additions to one counter
-      const uint32_t first = __shfl_sync(0xffffffffu, bin, __ffs((int)mask) - 1);
-      if (__all_sync(0xffffffffu, !counts || bin == first)) {
-        if (lane == 0) atomicAdd(&sm.bins[pass][first], (uint32_t)__popc(mask));
-      } else if (counts) {
-        atomicAdd(&sm.bins[pass][bin], 1u);
+    };
+    if (pass == 0) {
+      // loads of four chunks in flight
+      constexpr int kAhead = 4;
+      for (int i0 = lo + warp * 128; i0 < hi; i0 += kAhead * kRankThreads * 4) {
+        uint4 four[kAhead];
+#pragma unroll
+        for (int c = 0; c < kAhead; ++c) {
+          const int i = i0 + c * kRankThreads * 4 + 4 * lane;
+          four[c] = i < hi ? ranks_at(a, seq, head, i, recent) : make_uint4(0u, 0u, 0u, 0u);
+        }
+#pragma unroll
+        for (int c = 0; c < kAhead; ++c) {
+          const int i = i0 + c * kRankThreads * 4 + 4 * lane;
+          if (i - 4 * lane >= hi) break;
+          if (fits && i < hi) held4[(i - lo) / 4] = four[c];
+          count(i, four[c]);
+        }
+      }
+    } else {
+      for (int i0 = lo + warp * 128; i0 < hi; i0 += kRankThreads * 4) {
+        const int i = i0 + 4 * lane;
+        count(i, i < hi ? ranks(i) : make_uint4(0u, 0u, 0u, 0u));
       }
     }
     cluster.sync();
@@ -161,14 +185,24 @@ __global__ void __launch_bounds__(kRankThreads) rank_kernel(const __grid_constan
     take = sm.found[1];
   }
   // kept: every number above `prefix`, and the first `take` that equal it
-  const int run = ((each / 32 + kRankWarps - 1) / kRankWarps) * 32, from = min(lo + warp * run, hi), to = min(from + run, hi);
+  __syncthreads();                                        // all numbers are held
+  const int run = ((each / 128 + kRankWarps - 1) / kRankWarps) * 128, from = min(lo + warp * run, hi), to = min(from + run, hi);
+  // of a lane's four: those above the number in the lower half, its equals in the upper one
+  auto tally = [&](int i, const uint4& four) {
+    uint32_t t = 0;
+    const uint32_t r[4] = {four.x, four.y, four.z, four.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) t += i + j >= to ? 0u : r[j] > prefix ? 1u : r[j] == prefix ? 0x10000u : 0u;
+    return t;
+  };
   uint32_t above = 0, equal = 0;
-  for (int i0 = from; i0 < to; i0 += 32) {
-    const int i = i0 + lane;
-    const uint32_t r = i < to ? rank(i) : 0u;
-    above += (uint32_t)__popc(__ballot_sync(0xffffffffu, i < to && r > prefix));
-    equal += (uint32_t)__popc(__ballot_sync(0xffffffffu, i < to && r == prefix));
+  for (int i0 = from; i0 < to; i0 += 128) {
+    const int i = i0 + 4 * lane;
+    const uint32_t t = i < to ? tally(i, ranks(i)) : 0u;
+    above += t & 0xffffu, equal += t >> 16;
   }
+  above = __reduce_add_sync(0xffffffffu, above);
+  equal = __reduce_add_sync(0xffffffffu, equal);
   if (lane == 0) sm.above[warp] = above, sm.equal[warp] = equal;
   __syncthreads();
   if (threadIdx.x == 0) {
@@ -187,13 +221,28 @@ __global__ void __launch_bounds__(kRankThreads) rank_kernel(const __grid_constan
     above += other->above[kRankWarps], equal += other->equal[kRankWarps];
   }
   cluster.sync();                                         // nobody leaves while its counts are read
-  for (int i0 = from; i0 < to; i0 += 32) {
-    const int i = i0 + lane;
-    const uint32_t r = i < to ? rank(i) : 0u;
-    const uint32_t more = __ballot_sync(0xffffffffu, i < to && r > prefix), same = __ballot_sync(0xffffffffu, i < to && r == prefix);
-    const uint32_t mine = (1u << lane) - 1u, u = above + (uint32_t)__popc(more & mine), e = equal + (uint32_t)__popc(same & mine);
-    if (i < to && (r > prefix || (r == prefix && e < take))) list[u + min(e, take)] = i;
-    above += (uint32_t)__popc(more), equal += (uint32_t)__popc(same);
+  for (int i0 = from; i0 < to; i0 += 128) {
+    const int i = i0 + 4 * lane;
+    const uint4 four = i < to ? ranks(i) : make_uint4(0u, 0u, 0u, 0u);
+    const uint32_t t = i < to ? tally(i, four) : 0u;
+    uint32_t upto = t;                                    // over the lanes up to this one: at most 128 of either
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint32_t v = __shfl_up_sync(0xffffffffu, upto, o);
+      if (lane >= o) upto += v;
+    }
+    uint32_t u = above + ((upto - t) & 0xffffu), e = equal + ((upto - t) >> 16);
+    const uint32_t r[4] = {four.x, four.y, four.z, four.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (i + j >= to || r[j] < prefix) continue;
+      const bool more = r[j] > prefix;
+      if (more || e < take) list[u + min(e, take)] = i + j;
+      if (more) ++u;
+      else ++e;
+    }
+    const uint32_t all = __shfl_sync(0xffffffffu, upto, 31);
+    above += all & 0xffffu, equal += all >> 16;
   }
 }
 
@@ -210,85 +259,100 @@ __device__ __forceinline__ uint32_t scale_bytes(uint32_t four, float ratio) {
 
 template <int D, int BITS>
 __global__ void __launch_bounds__(kMoveThreads) move_kernel(const __grid_constant__ EvictArgs a) {
-  constexpr int kRow = D * BITS / 8, kPieces = kRow / 16, kLoads = 8;
-  __shared__ int64_t from[kScaleTokens];                  // the tokens' rows in the pools, below zero: left out
-  __shared__ float scale[2][kScaleTokens], top[2];
+  constexpr int kRow = D * BITS / 8, kPieces = kRow / 16, kLoads = 8, kWarps = kMoveThreads / 32;
+  const int lane = threadIdx.x & 31;
   grid_wait();
   const int room_groups = a.to_stride * (a.kv.block_tokens / kScaleTokens);
   const int64_t room = (int64_t)room_groups * kScaleTokens, items = (int64_t)a.n_seqs * a.kv.n_kv_heads * room_groups;
-  for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
+  // warps on their own: an item is a chain of dependent loads (counts, table, list, table, rows), so the more are under way the better
+  for (int64_t item = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5); item < items; item += (int64_t)gridDim.x * kWarps) {
     const int pair = (int)(item / room_groups), group = (int)(item - (int64_t)pair * room_groups);
     const int seq = pair / a.kv.n_kv_heads, head = pair - seq * a.kv.n_kv_heads, count = __ldg(a.counts + pair);
-    if (group == 0 && head == 0 && threadIdx.x == 0) a.to_lens[seq] = count;
+    if (group == 0 && head == 0 && lane == 0) a.to_lens[seq] = count;
     const int live = min(count - group * kScaleTokens, kScaleTokens);
     if (live <= 0) continue;
     const int64_t to = row_at(a.kv, a.to_table, a.to_stride, seq, head, group * kScaleTokens);
     if (to < 0) {
-      if (threadIdx.x == 0) report_cache(a.dev_status);
+      if (lane == 0) report_cache(a.dev_status);
       continue;
     }
-    __syncthreads();                                      // the item before is done with shared memory
-    if (threadIdx.x < kScaleTokens) {
-      int64_t row = -1;
-      if ((int)threadIdx.x < live) {
-        const int pos = __ldg(a.list + (int64_t)pair * room + group * kScaleTokens + threadIdx.x);
-        row = row_at(a.kv, a.table, a.table_stride, seq, head, pos);
-        if (row < 0) report_cache(a.dev_status);
+    int from[2];                                          // the rows in the pools of tokens lane and lane + 32, below zero: left out
+    float scale[2][2], top[2];                            // 8 bits: of keys and values; the group's
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int token = lane + 32 * h;
+      from[h] = -1;
+      if (token < live) {
+        const int pos = __ldg(a.list + (int64_t)pair * room + group * kScaleTokens + token);
+        from[h] = (int)row_at(a.kv, a.table, a.table_stride, seq, head, pos);
+        if (from[h] < 0) report_cache(a.dev_status);
       }
-      from[threadIdx.x] = row;
-      if (row >= 0) {
-        a.weight[to + threadIdx.x] = __ldg(a.weight + row);
-        if (a.position != nullptr) a.position[to + threadIdx.x] = __ldg(a.position + row);
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      if (from[h] >= 0) {
+        const int64_t cell = to + lane + 32 * h;
+        const float weight = __ldg(a.weight + from[h]);
+        const int position = a.position != nullptr ? __ldg(a.position + from[h]) : 0;
+        a.weight[cell] = weight;
+        if (a.position != nullptr) a.position[cell] = position;
       }
       if constexpr (BITS == 8) {
 #pragma unroll
-        for (int v = 0; v < 2; ++v) scale[v][threadIdx.x] = row >= 0 ? __ldg((v ? a.kv.v_scale : a.kv.k_scale) + row / kScaleTokens) : 0.f;
+        for (int v = 0; v < 2; ++v) scale[v][h] = from[h] >= 0 ? __ldg((v ? a.kv.v_scale : a.kv.k_scale) + from[h] / kScaleTokens) : 0.f;
       }
     }
-    __syncthreads();
     if constexpr (BITS == 8) {
-      if (threadIdx.x < 64) {
-        const int v = threadIdx.x >> 5, lane = threadIdx.x & 31;
-        float m = fmaxf(scale[v][lane], scale[v][lane + 32]);
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-        if (lane == 0) {
-          top[v] = m;
-          if (m > 0.f) (v ? a.kv.v_scale : a.kv.k_scale)[to / kScaleTokens] = m;
-        }
+      for (int v = 0; v < 2; ++v) {
+        top[v] = fmaxf(scale[v][0], scale[v][1]);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) top[v] = fmaxf(top[v], __shfl_xor_sync(0xffffffffu, top[v], o));
+        if (lane == 0 && top[v] > 0.f) (v ? a.kv.v_scale : a.kv.k_scale)[to / kScaleTokens] = top[v];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) scale[v][h] = __fdiv_rn(scale[v][h], top[v]);      // what the tokens' bytes are multiplied by
       }
-      __syncthreads();
     }
-    const int pieces = 2 * live * kPieces;                // of keys, then of values
-    for (int i0 = threadIdx.x; i0 < pieces; i0 += kLoads * kMoveThreads) {
-      uint4 x[kLoads];
-      int64_t dst[kLoads];
 #pragma unroll
-      for (int j = 0; j < kLoads; ++j) {
-        const int i = i0 + j * kMoveThreads, v = i >= live * kPieces, token = (i - v * live * kPieces) / kPieces, piece = i % kPieces;
-        dst[j] = -1;
-        if (i < pieces && from[token] >= 0) {
-          dst[j] = (to + token) * kRow + piece * 16;
-          x[j] = __ldg(reinterpret_cast<const uint4*>((v ? a.kv.v : a.kv.k) + from[token] * kRow + piece * 16));
-          if constexpr (BITS == 8) {
-            const float ratio = __fdiv_rn(scale[v][token], top[v]);
-            if (ratio != 1.f) {
-              x[j].x = scale_bytes(x[j].x, ratio), x[j].y = scale_bytes(x[j].y, ratio);
-              x[j].z = scale_bytes(x[j].z, ratio), x[j].w = scale_bytes(x[j].w, ratio);
+    for (int v = 0; v < 2; ++v) {
+      uint8_t* pool = v ? a.kv.v : a.kv.k;
+#pragma unroll 1
+      for (int i0 = 0; i0 < live * kPieces; i0 += kLoads * 32) {
+        uint4 x[kLoads];
+        bool there[kLoads];
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) {
+          const int i = i0 + j * 32 + lane, token = i / kPieces;
+          // kPieces divides 32 or is divided by it: the lanes' tokens of one j lie in one half
+          const int first = i0 + j * 32 < kPieces * 32 ? from[0] : from[1];
+          const int row = __shfl_sync(0xffffffffu, first, token & 31);
+          float ratio = 1.f;
+          if constexpr (BITS == 8) ratio = __shfl_sync(0xffffffffu, i0 + j * 32 < kPieces * 32 ? scale[v][0] : scale[v][1], token & 31);
+          there[j] = i < live * kPieces && row >= 0;
+          if (there[j]) {
+            x[j] = __ldg(reinterpret_cast<const uint4*>(pool + (int64_t)row * kRow) + i % kPieces);
+            if constexpr (BITS == 8) {
+              if (ratio != 1.f) {
+                x[j].x = scale_bytes(x[j].x, ratio), x[j].y = scale_bytes(x[j].y, ratio);
+                x[j].z = scale_bytes(x[j].z, ratio), x[j].w = scale_bytes(x[j].w, ratio);
+              }
             }
           }
         }
-      }
 #pragma unroll
-      for (int j = 0; j < kLoads; ++j)
-        if (dst[j] >= 0) *reinterpret_cast<uint4*>((i0 + j * kMoveThreads >= live * kPieces ? a.kv.v : a.kv.k) + dst[j]) = x[j];
-    }
-    if constexpr (BITS == 4) {
-      constexpr int kWords = D / kScaleDims / 2;          // of a token's scales
-      for (int i = threadIdx.x; i < 2 * live * kWords; i += kMoveThreads) {
-        const int v = i >= live * kWords, j = i - v * live * kWords, token = j / kWords;
+        for (int j = 0; j < kLoads; ++j)
+          if (there[j]) reinterpret_cast<uint4*>(pool + to * kRow)[i0 + j * 32 + lane] = x[j];
+      }
+      if constexpr (BITS == 4) {
+        constexpr int kWords = D / kScaleDims / 2;        // of a token's scales
         uint32_t* scales = reinterpret_cast<uint32_t*>(v ? a.kv.v_scale4 : a.kv.k_scale4);
-        if (from[token] >= 0) scales[to * kWords + j] = __ldg(scales + from[token] * kWords + j % kWords);
+        uint32_t x[2 * kWords];
+#pragma unroll
+        for (int j = 0; j < 2 * kWords; ++j) {
+          const int i = j * 32 + lane, row = __shfl_sync(0xffffffffu, j < kWords ? from[0] : from[1], (i / kWords) & 31);
+          x[j] = row >= 0 ? __ldg(scales + (int64_t)row * kWords + i % kWords) : 0u;
+          if (row >= 0) scales[to * kWords + i] = x[j];
+        }
       }
     }
   }
@@ -313,7 +377,7 @@ int32_t launch_evict(EvictArgs& a, cudaStream_t stream) {
   // CTAs of a (sequence, key head): by the places that its table has room for
   const int64_t places = (int64_t)a.table_stride * a.kv.block_tokens, pairs = (int64_t)a.n_seqs * a.kv.n_kv_heads;
   const int parts = places <= 4096 ? 1 : places <= 8192 ? 2 : places <= 32768 ? 4 : 8;
-  a.held = (int)std::min<int64_t>(align_up((size_t)ceil_div(places, parts), 32), kHeld);
+  a.held = (int)std::min<int64_t>(align_up((size_t)ceil_div(places, parts), 128), kHeld);
   static ContextSet done;
   const int32_t st = allow_shared_memory(reinterpret_cast<const void*>(rank_kernel), kHeld * 4, done);
   if (st != SPF_OK) return st;
@@ -332,7 +396,7 @@ int32_t launch_evict(EvictArgs& a, cudaStream_t stream) {
   int sm_count = 0;
   if (const int32_t bad = device_sm_count(&sm_count); bad != SPF_OK) return bad;
   const int64_t items = pairs * a.to_stride * (a.kv.block_tokens / kScaleTokens);
-  config.gridDim = dim3((unsigned)std::min<int64_t>(items, (int64_t)sm_count * 12));
+  config.gridDim = dim3((unsigned)std::min<int64_t>(ceil_div(items, kMoveThreads / 32), (int64_t)sm_count * 8));
   config.blockDim = dim3(kMoveThreads);
   config.dynamicSmemBytes = 0;
   attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
