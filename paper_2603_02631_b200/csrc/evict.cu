@@ -21,7 +21,7 @@ namespace {
 
 namespace cg = cooperative_groups;
 
-constexpr int kRankThreads = 512, kRankWarps = kRankThreads / 32, kBins = 2048;
+constexpr int kMostParts = 8, kBins = 2048;
 constexpr int kHeld = 36864;              // numbers that a CTA of the first kernel keeps (with more, they are made anew in every pass)
 constexpr int kMoveThreads = 128;
 constexpr uint32_t kAlways = 0xffffffffu;
@@ -71,16 +71,20 @@ __device__ __forceinline__ uint4 ranks_at(const EvictArgs& a, int seq, int head,
   return make_uint4(rank_of(a, w.x, at.x, recent), rank_of(a, w.y, at.y, recent), rank_of(a, w.z, at.z, recent), rank_of(a, w.w, at.w, recent));
 }
 
+template <int kRankThreads>
 struct RankSmem {
-  uint32_t bins[3][kBins];
+  static constexpr int kRankWarps = kRankThreads / 32;
+  alignas(16) uint32_t bins[3][kBins];
   uint32_t sums[kRankWarps];
   uint32_t found[2];                      // bin, and what is left to be taken in it
   uint32_t above[kRankWarps + 1], equal[kRankWarps + 1];   // kept for certain, and candidates, before each warp; the last: of the CTA
 };
 
+template <int kRankThreads>
 __global__ void __launch_bounds__(kRankThreads) rank_kernel(const __grid_constant__ EvictArgs a) {
+  constexpr int kRankWarps = kRankThreads / 32;
   extern __shared__ __align__(16) uint32_t held[];
-  __shared__ RankSmem sm;
+  __shared__ RankSmem<kRankThreads> sm;
   cg::cluster_group cluster = cg::this_cluster();
   const int parts = (int)cluster.num_blocks(), part = (int)cluster.block_rank();
   const int pair = (int)(blockIdx.x / parts), seq = pair / a.kv.n_kv_heads, head = pair - seq * a.kv.n_kv_heads;
@@ -129,8 +133,8 @@ __global__ void __launch_bounds__(kRankThreads) rank_kernel(const __grid_constan
       }
     };
     if (pass == 0) {
-      // loads of four chunks in flight
-      constexpr int kAhead = 4;
+      // loads of two chunks in flight
+      constexpr int kAhead = 2;
       for (int i0 = lo + warp * 128; i0 < hi; i0 += kAhead * kRankThreads * 4) {
         uint4 four[kAhead];
 #pragma unroll
@@ -154,13 +158,18 @@ __global__ void __launch_bounds__(kRankThreads) rank_kernel(const __grid_constan
     }
     cluster.sync();
     // every CTA adds up everybody's counts and finds the bin, from the highest number down
-    constexpr int kPer = kBins / kRankThreads;
-    uint32_t own[kPer], sum = 0;
+    constexpr int kPer = kBins / kRankThreads, kPairs = kPer / 2;
+    uint32_t own[kPer] = {}, sum = 0;
 #pragma unroll
-    for (int j = 0; j < kPer; ++j) {
-      own[j] = 0;
-      for (int p = 0; p < parts; ++p) own[j] += cluster.map_shared_rank(&sm.bins[pass][0], p)[kBins - 1 - (int)(threadIdx.x * kPer + j)];
-      sum += own[j];
+    for (int pair = 0; pair < kPairs; ++pair) {
+      const int at = kBins / 2 - 1 - ((int)threadIdx.x * kPairs + pair);
+      uint2 counts[kMostParts];
+#pragma unroll
+      for (int p = 0; p < kMostParts; ++p)                // loads from all of them in flight together
+        counts[p] = p < parts ? reinterpret_cast<const uint2*>(cluster.map_shared_rank(&sm.bins[pass][0], p))[at] : make_uint2(0u, 0u);
+#pragma unroll
+      for (int p = 0; p < kMostParts; ++p) own[2 * pair] += counts[p].y, own[2 * pair + 1] += counts[p].x;
+      sum += own[2 * pair] + own[2 * pair + 1];
     }
     uint32_t upto = sum;
 #pragma unroll
@@ -217,7 +226,7 @@ __global__ void __launch_bounds__(kRankThreads) rank_kernel(const __grid_constan
   cluster.sync();
   above = sm.above[warp], equal = sm.equal[warp];
   for (int p = 0; p < part; ++p) {
-    const RankSmem* other = cluster.map_shared_rank(&sm, p);
+    const RankSmem<kRankThreads>* other = cluster.map_shared_rank(&sm, p);
     above += other->above[kRankWarps], equal += other->equal[kRankWarps];
   }
   cluster.sync();                                         // nobody leaves while its counts are read
@@ -260,17 +269,20 @@ __device__ __forceinline__ uint32_t scale_bytes(uint32_t four, float ratio) {
 template <int D, int BITS>
 __global__ void __launch_bounds__(kMoveThreads) move_kernel(const __grid_constant__ EvictArgs a) {
   constexpr int kRow = D * BITS / 8, kPieces = kRow / 16, kLoads = 8, kWarps = kMoveThreads / 32;
+  constexpr int kShares = kRow > 64 ? kRow / 64 : 1, kTokens = kScaleTokens / kShares;   // long rows: warps that share a group
   const int lane = threadIdx.x & 31;
   grid_wait();
   const int room_groups = a.to_stride * (a.kv.block_tokens / kScaleTokens);
-  const int64_t room = (int64_t)room_groups * kScaleTokens, items = (int64_t)a.n_seqs * a.kv.n_kv_heads * room_groups;
+  const int64_t room = (int64_t)room_groups * kScaleTokens, items = (int64_t)a.n_seqs * a.kv.n_kv_heads * room_groups * kShares;
   // warps on their own: an item is a chain of dependent loads (counts, table, list, table, rows), so the more are under way the better
   for (int64_t item = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5); item < items; item += (int64_t)gridDim.x * kWarps) {
-    const int pair = (int)(item / room_groups), group = (int)(item - (int64_t)pair * room_groups);
+    const int share = (int)(item % kShares);
+    const int64_t whole = item / kShares;
+    const int pair = (int)(whole / room_groups), group = (int)(whole - (int64_t)pair * room_groups);
     const int seq = pair / a.kv.n_kv_heads, head = pair - seq * a.kv.n_kv_heads, count = __ldg(a.counts + pair);
-    if (group == 0 && head == 0 && lane == 0) a.to_lens[seq] = count;
-    const int live = min(count - group * kScaleTokens, kScaleTokens);
-    if (live <= 0) continue;
+    if (group == 0 && head == 0 && share == 0 && lane == 0) a.to_lens[seq] = count;
+    const int live = min(count - group * kScaleTokens, kScaleTokens), token0 = share * kTokens, token1 = min(token0 + kTokens, live);
+    if (token0 >= token1) continue;
     const int64_t to = row_at(a.kv, a.to_table, a.to_stride, seq, head, group * kScaleTokens);
     if (to < 0) {
       if (lane == 0) report_cache(a.dev_status);
@@ -282,7 +294,7 @@ __global__ void __launch_bounds__(kMoveThreads) move_kernel(const __grid_constan
     for (int h = 0; h < 2; ++h) {
       const int token = lane + 32 * h;
       from[h] = -1;
-      if (token < live) {
+      if (BITS == 8 ? token < live : token >= token0 && token < token1) {
         const int pos = __ldg(a.list + (int64_t)pair * room + group * kScaleTokens + token);
         from[h] = (int)row_at(a.kv, a.table, a.table_stride, seq, head, pos);
         if (from[h] < 0) report_cache(a.dev_status);
@@ -290,7 +302,7 @@ __global__ void __launch_bounds__(kMoveThreads) move_kernel(const __grid_constan
     }
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      if (from[h] >= 0) {
+      if (from[h] >= 0 && lane + 32 * h >= token0 && lane + 32 * h < token1) {
         const int64_t cell = to + lane + 32 * h;
         const float weight = __ldg(a.weight + from[h]);
         const int position = a.position != nullptr ? __ldg(a.position + from[h]) : 0;
@@ -308,7 +320,7 @@ __global__ void __launch_bounds__(kMoveThreads) move_kernel(const __grid_constan
         top[v] = fmaxf(scale[v][0], scale[v][1]);
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) top[v] = fmaxf(top[v], __shfl_xor_sync(0xffffffffu, top[v], o));
-        if (lane == 0 && top[v] > 0.f) (v ? a.kv.v_scale : a.kv.k_scale)[to / kScaleTokens] = top[v];
+        if (lane == 0 && share == 0 && top[v] > 0.f) (v ? a.kv.v_scale : a.kv.k_scale)[to / kScaleTokens] = top[v];
 #pragma unroll
         for (int h = 0; h < 2; ++h) scale[v][h] = __fdiv_rn(scale[v][h], top[v]);      // what the tokens' bytes are multiplied by
       }
@@ -317,7 +329,7 @@ __global__ void __launch_bounds__(kMoveThreads) move_kernel(const __grid_constan
     for (int v = 0; v < 2; ++v) {
       uint8_t* pool = v ? a.kv.v : a.kv.k;
 #pragma unroll 1
-      for (int i0 = 0; i0 < live * kPieces; i0 += kLoads * 32) {
+      for (int i0 = token0 * kPieces; i0 < token1 * kPieces; i0 += kLoads * 32) {
         uint4 x[kLoads];
         bool there[kLoads];
 #pragma unroll
@@ -328,7 +340,7 @@ __global__ void __launch_bounds__(kMoveThreads) move_kernel(const __grid_constan
           const int row = __shfl_sync(0xffffffffu, first, token & 31);
           float ratio = 1.f;
           if constexpr (BITS == 8) ratio = __shfl_sync(0xffffffffu, i0 + j * 32 < kPieces * 32 ? scale[v][0] : scale[v][1], token & 31);
-          there[j] = i < live * kPieces && row >= 0;
+          there[j] = i < token1 * kPieces && row >= 0;
           if (there[j]) {
             x[j] = __ldg(reinterpret_cast<const uint4*>(pool + (int64_t)row * kRow) + i % kPieces);
             if constexpr (BITS == 8) {
@@ -376,15 +388,19 @@ template <int D, int BITS>
 int32_t launch_evict(EvictArgs& a, cudaStream_t stream) {
   // CTAs of a (sequence, key head): by the places that its table has room for
   const int64_t places = (int64_t)a.table_stride * a.kv.block_tokens, pairs = (int64_t)a.n_seqs * a.kv.n_kv_heads;
-  const int parts = places <= 4096 ? 1 : places <= 8192 ? 2 : places <= 32768 ? 4 : 8;
+  const int parts = places <= 4096 ? 1 : places <= 8192 ? 2 : places <= 32768 ? 4 : kMostParts;
   a.held = (int)std::min<int64_t>(align_up((size_t)ceil_div(places, parts), 128), kHeld);
+  // Few places: small CTAs, so that many sequences' run at the same time (256 of 2200 tokens: 256 threads 20 us, 1024 threads 23)
   static ContextSet done;
-  const int32_t st = allow_shared_memory(reinterpret_cast<const void*>(rank_kernel), kHeld * 4, done);
-  if (st != SPF_OK) return st;
+  const auto rank = parts == 1 ? rank_kernel<256> : rank_kernel<1024>;
+  if (parts > 1) {
+    const int32_t st = allow_shared_memory(reinterpret_cast<const void*>(rank_kernel<1024>), kHeld * 4, done);
+    if (st != SPF_OK) return st;
+  }
   cudaLaunchConfig_t config{};
   cudaLaunchAttribute attr{};
   config.gridDim = dim3((unsigned)(pairs * parts));
-  config.blockDim = dim3(kRankThreads);
+  config.blockDim = dim3(parts == 1 ? 256 : 1024);
   config.dynamicSmemBytes = (size_t)a.held * 4;
   config.stream = stream;
   attr.id = cudaLaunchAttributeClusterDimension;
@@ -392,10 +408,10 @@ int32_t launch_evict(EvictArgs& a, cudaStream_t stream) {
   attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
   config.attrs = &attr;
   config.numAttrs = 1;
-  SPF_CUDA_CHECK(cudaLaunchKernelEx(&config, rank_kernel, a));
+  SPF_CUDA_CHECK(cudaLaunchKernelEx(&config, rank, a));
   int sm_count = 0;
   if (const int32_t bad = device_sm_count(&sm_count); bad != SPF_OK) return bad;
-  const int64_t items = pairs * a.to_stride * (a.kv.block_tokens / kScaleTokens);
+  const int64_t items = pairs * a.to_stride * (a.kv.block_tokens / kScaleTokens) * std::max(D * BITS / 8 / 64, 1);
   config.gridDim = dim3((unsigned)std::min<int64_t>(ceil_div(items, kMoveThreads / 32), (int64_t)sm_count * 8));
   config.blockDim = dim3(kMoveThreads);
   config.dynamicSmemBytes = 0;
