@@ -2,15 +2,20 @@
 //
 //   W[h, s] = decay W[h, s] + sum over rows r that see s of 2^(f_s q[r] . k[s] - lse2[r])
 //
-// Here the exponentials bound it (128 rows by 128 keys take the exponential unit 1024 cycles, the warp-level products of 128 dimensions as
-// long, the big instruction's a quarter), so a weight should cost little else.  A CTA has 128 keys of a (sequence, key head) in registers, as
-// left operands of warp-level products, widened to bf16 once (exactly: 8-bit values, and 4-bit codes times scales of five bits), and the
-// rows go by in stages of 128.  A warp has 32 keys and every fourth 32 rows: logits have keys as rows and query rows as columns, so a thread's
-// weights of a key add up in registers, and only at the end do the lanes and warps that share a key exchange sums.  Sums of a stage are
-// added with what the additions lose (thousands of rows make 1.7e-6 of a weight otherwise).
+// A weight is one product of D dimensions and one exponential, and the exponentials bound it: 128 keys by 128 rows take the exponential unit
+// 1024 cycles, the tensor cores 128 (64 dimensions) or 256.  So the products are the big instruction's, into tensor memory, with keys as the 128
+// lanes and rows as the columns: a thread of the two sets of four warps that take the exponentials has one key, whose weights it adds up in a
+// register over all rows, with no exchange between threads; per exponential it spends half a multiply-add, half an addition and a quarter of a
+// read of log-sum-exps from shared memory.  (Warp-level products, keys in registers, took 648 us where this takes 290: two units in turns in
+// each of few warps.)  Sums of a tile are added with what the additions lose (thousands of rows make 1.7e-6 of a weight otherwise).
 //
-// The list of all (sequence, key head, 128 keys), each as long as the stages of rows that see any of its keys, is cut into one part for each SM; an
-// item belongs to the part that its beginning lies in.
+// Keys are brought once for all rows of an item (a sequence, key head and 128 keys) and widened to bf16 on the way (exactly: 8-bit values, and
+// 4-bit codes times scales of five bits), the next item's while this one's last rows are being made; rows go by in tiles of 128.
+//
+// The list of all items, each as long as the tiles of rows that see any of its keys, is cut into one part for each SM; an item belongs to the
+// part that its beginning lies in.
+//
+// Warps: 0-3 and 4-7 the exponentials, of the even and the odd tiles; 8-11 keys, rows and log-sum-exps; 12 issues the products.
 #include <climits>
 
 #include "weigh.cuh"
@@ -18,22 +23,27 @@
 namespace spf {
 namespace {
 
-constexpr int kThreads = 512, kKeys = 128, kStages = 3, kKeyGroups = 4, kRowGroups = 4;
-constexpr int kGroupRows = 64, kRows = kRowGroups * kGroupRows, kGroupThreads = kThreads / kRowGroups;
+constexpr int kThreads = 416, kKeys = 128, kRows = 128, kEnds = 2;
+constexpr int kAccs = 4, kBelow = 16;                     // accumulators in tensor memory; tiles whose log-sum-exps are kept: more than may be under way
 
 template <int D_, int BITS_>
 struct Traits {
-  static constexpr int D = D_, BITS = BITS_, BLOCKS = D / 32, QSTAGE = kGroupRows * D * 2;
-  static constexpr int STEP = D == 64 ? 2 : 1;            // eights of rows whose products are under way together
+  static constexpr int D = D_, BITS = BITS_, TILE = 128 * D * 2, STAGES = D == 64 ? 6 : 4;
 };
 
 struct Smem {
-  float below[kRowGroups][kStages][kGroupRows];           // the rows' base-2 log-sum-exps, negated
-  float sums[kRowGroups][kKeys];
+  unsigned long long q_full[6], q_empty[6], k_full[2], k_empty[2], acc_full[kAccs], acc_empty[kAccs], summed, mma_done;
+  float below[kBelow][kRows];                             // the rows' base-2 log-sum-exps, negated
+  float sums[2][kKeys];                                   // of the odd tiles
   int64_t scan[kThreads / 32];
   int64_t total, start_base;
   int start_seq;
+  int abort;
+  uint32_t tmem;
 };
+
+template <class T>
+constexpr int smem_bytes() { return (2 + T::STAGES) * T::TILE + (int)sizeof(Smem) + 1024; }
 
 // ---------------------------------------------------------------------------------------------- the list of items
 // Rows of a sequence and key head, from the first that sees key0 on (a multiple of 8).
@@ -42,18 +52,18 @@ __device__ __forceinline__ int first_row(const WeighArgs& w, const SeqSpan& s, i
   const int64_t r = ((int64_t)key0 - s.pos0) * w.a.group;
   return (int)min(max(r, (int64_t)0), (int64_t)s.n_new * w.a.group) & ~7;
 }
-__device__ __forceinline__ int stages_of(const WeighArgs& w, const SeqSpan& s, int key0) {
+__device__ __forceinline__ int tiles_of(const WeighArgs& w, const SeqSpan& s, int key0) {
   if (key0 + kKeys <= s.first) return 0;
   return (int)(((int64_t)s.n_new * w.a.group - first_row(w, s, key0) + kRows - 1) / kRows);
 }
-// Length of a (sequence, key head) in the list: its stages, and one more an item for its beginning and end.
+// Length of a (sequence, key head) in the list: its tiles of rows, and for an item's beginning and end as long as kEnds of them.
 __device__ __forceinline__ int64_t head_cost(const WeighArgs& w, const SeqSpan& s) {
   const int tiles = (s.end + kKeys - 1) / kKeys;
   // keys before the first that every row sees, and those from the first row's on
   const int before = s.first / kKeys, all = w.a.causal ? min(max(s.pos0, 0) / kKeys, tiles) : tiles;
-  int64_t cost = tiles;
-  if (all > before) cost += (int64_t)(all - before) * stages_of(w, s, before * kKeys);
-  for (int t = max(all, before); t < tiles; ++t) cost += stages_of(w, s, t * kKeys);
+  int64_t cost = (int64_t)kEnds * tiles;
+  if (all > before) cost += (int64_t)(all - before) * tiles_of(w, s, before * kKeys);
+  for (int t = max(all, before); t < tiles; ++t) cost += tiles_of(w, s, t * kKeys);
   return cost;
 }
 
@@ -109,15 +119,46 @@ __device__ __forceinline__ Cursor first_item(const WeighArgs& w, const Smem& sm,
   c.head = (int)((w0 - c.at) / per_head);
   c.at += c.head * per_head;
   const int tiles = (s.end + kKeys - 1) / kKeys, before = s.first / kKeys, all = w.a.causal ? min(max(s.pos0, 0) / kKeys, tiles) : tiles;
-  if (all > before && w0 > c.at + before) {
+  if (all > before && w0 > c.at + kEnds * before) {
     // among the items of equal length, without looking at each
-    const int64_t each = stages_of(w, s, before * kKeys) + 1, skip = min((w0 - c.at - before) / each, (int64_t)(all - before));
+    const int64_t each = tiles_of(w, s, before * kKeys) + kEnds, skip = min((w0 - c.at - kEnds * before) / each, (int64_t)(all - before));
     c.tile = before + (int)skip;
-    c.at += before + skip * each;
+    c.at += kEnds * before + skip * each;
   }
-  while (c.at < w0) c.at += stages_of(w, s, c.tile++ * kKeys) + 1;
+  while (c.at < w0) c.at += tiles_of(w, s, c.tile++ * kKeys) + kEnds;
   return c;
 }
+
+// A CTA's items one after the other, as every role walks through them.
+struct Walk {
+  Cursor at;
+  WeighSpan span;
+  int64_t end;
+  int key0, tiles, row_first;                             // of the item; row_first: the first row of its first tile
+  int pool_at;                                            // the first key's row in the pool
+  bool inside;
+
+  __device__ __forceinline__ Walk(const WeighArgs& w, const Smem& sm, int64_t w0, int64_t w1) : at(first_item(w, sm, w0)), span(weigh_span(w, at.seq)), end(w1) {}
+  __device__ __forceinline__ bool next(const WeighArgs& w) {
+    if (at.at >= end) return false;
+    while (span.rows.n_new <= 0 || at.tile * kKeys >= span.rows.end) {
+      at.tile = 0;
+      if (span.rows.n_new <= 0 || span.rows.end == 0 || ++at.head >= w.a.kv.n_kv_heads) {
+        at.head = 0;
+        if (++at.seq >= w.a.step.n_seqs) return false;
+        span = weigh_span(w, at.seq);
+      }
+    }
+    key0 = at.tile * kKeys;
+    tiles = tiles_of(w, span.rows, key0);
+    row_first = first_row(w, span.rows, key0);
+    pool_at = pool_row(w.a, at.seq, at.head, key0);
+    inside = pool_at < w.a.kv.n_blocks * w.a.kv.n_kv_heads * w.a.kv.block_tokens;
+    at.at += tiles + kEnds;
+    ++at.tile;
+    return true;
+  }
+};
 
 // ---------------------------------------------------------------------------------------------- keys
 __device__ __forceinline__ uint32_t mul_bf16(uint32_t a, uint32_t b) {
@@ -146,7 +187,7 @@ __device__ __forceinline__ void load_eight(const KvView& kv, int64_t row, int j,
     }
   } else {
     const uint32_t word = __ldg(reinterpret_cast<const uint32_t*>(kv.k + row * (T::D / 2)) + j);
-    const uint32_t s = __ldg(kv.k_scale4 + row * T::BLOCKS + j / 4), both = s | s << 16, less = mul_bf16(both, 0xc1c0c1c0u);   // -24 scales
+    const uint32_t s = __ldg(kv.k_scale4 + row * (T::D / kScaleDims) + j / 4), both = s | s << 16, less = mul_bf16(both, 0xc1c0c1c0u);   // -24 scales
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const uint32_t two = word >> (8 * i);
@@ -155,22 +196,6 @@ __device__ __forceinline__ void load_eight(const KvView& kv, int64_t row, int j,
     }
   }
 }
-
-// ---------------------------------------------------------------------------------------------- rows
-__device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
-// The same with nothing to add to.
-__device__ __forceinline__ void mma_first(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
-      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
-      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
-}
-// Byte offset of a row's 16-byte chunk in a stage: rows in turns begin with either half of 128 bytes, so that two rows' four chunks touch every bank.
-template <class T>
-__device__ __forceinline__ uint32_t row_chunk(int row, int chunk) { return (uint32_t)(row * (2 * T::D) + (chunk ^ ((row & 1) << 2)) * 16); }
 
 // A row of a sequence and key head as (token, head of the group), and the step to one further on, without a division.
 struct RowAt {
@@ -184,196 +209,252 @@ struct RowAt {
   }
 };
 
-// Asks for the rows of a stage, from (token, g) `at` on, the thread's first; `lse_at` is that of the thread's log-sum-exp, which is returned.
+// ---------------------------------------------------------------------------------------------- keys and rows into shared memory
+// Byte offset of the 16-byte chunk of a row of keys or queries, as the products read them: spans of 128 bytes, swizzled.
+__device__ __forceinline__ uint32_t tile_chunk(int row, int chunk) { return (uint32_t)((chunk >> 3) * (128 * 128) + row * 128 + ((chunk ^ row) & 7) * 16); }
+
 template <class T>
-__device__ __forceinline__ float fetch_rows(const WeighArgs& w, const SeqSpan& s, int head, RowAt at, const RowAt& lse_at, const RowAt& step, uint32_t to) {
-  constexpr int kChunks = T::D / 8;
+__device__ __forceinline__ void bring(const WeighArgs& w, Smem& sm, unsigned char* k_tiles, uint32_t q_ring, int64_t w0, int64_t w1, const Abort& ab) {
+  constexpr int kChunks = T::D / 8, kLines = 128 / kChunks;
   const AttendArgs& a = w.a;
-  const int thread = (int)threadIdx.x % kGroupThreads, first = thread / kChunks, chunk = thread % kChunks;
-  const __nv_bfloat16* base = a.q.data + s.row0 * a.q.stride_row + (int64_t)head * a.group * a.q.stride_head + 8 * chunk;
+  const int thread = (int)threadIdx.x - 256, lane = threadIdx.x & 31, first = thread / kChunks, chunk = thread % kChunks;
+  const RowAt line_step(kLines, a.group), tile_step(kRows, a.group);
+  Walk walk(w, sm, w0, w1);
+  uint32_t done = 0, items = 0;                           // tiles and items brought
+  uint32_t handed = 0;                                    // tiles handed over: their copies have landed
+  auto hand_over = [&](uint32_t upto) {
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+    for (; handed < upto; ++handed)
+      if (lane == 0) mbar_arrive(smem_u32(&sm.q_full[handed % T::STAGES]));
+  };
+  while (walk.next(w)) {
+    if (walk.tiles == 0) continue;
+    const SeqSpan& s = walk.span.rows;
+    const int head = walk.at.head;
+    const uint32_t buf = items & 1u;
+    if (!mbar_wait_warp(smem_u32(&sm.k_empty[buf]), ((items >> 1) & 1u) ^ 1u, ab)) return;
+    unsigned char* k_tile = k_tiles + buf * T::TILE;
+#pragma unroll 4
+    for (int i = 0; i < 128 / kLines; ++i) {
+      const int in = first + i * kLines;
+      uint32_t r[4] = {0u, 0u, 0u, 0u};
+      if (walk.inside) load_eight<T>(a.kv, (int64_t)walk.pool_at + in, chunk, r);
+      *reinterpret_cast<uint4*>(k_tile + tile_chunk(in, chunk)) = make_uint4(r[0], r[1], r[2], r[3]);
+    }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+    if (lane == 0) mbar_arrive(smem_u32(&sm.k_full[buf]));
+    ++items;
+    const __nv_bfloat16* base = a.q.data + s.row0 * a.q.stride_row + (int64_t)head * a.group * a.q.stride_head + 8 * chunk;
+    RowAt copy_at(walk.row_first + first, a.group), lse_at(walk.row_first + thread, a.group);
+    auto lse2 = [&] { return row_lse2(a, s.row0 + lse_at.token, head * a.group + lse_at.g, lse_at.token < s.n_new); };
+    float own = lse2();
+    for (int j = 0; j < walk.tiles; ++j, ++done) {
+      const uint32_t slot = done % T::STAGES;
+      lse_at = lse_at.after(tile_step, a.group);
+      const float later = j + 1 < walk.tiles ? lse2() : 0.f;
+      if (!mbar_wait_warp(smem_u32(&sm.q_empty[slot]), ((done / T::STAGES) & 1u) ^ 1u, ab)) return;
+      RowAt r = copy_at;
 #pragma unroll
-  for (int i = 0; i < kGroupRows * kChunks / kGroupThreads; ++i) {
-    const int r = first + i * (kGroupThreads / kChunks), bytes = at.token < s.n_new ? 16 : 0;     // rows that do not exist are zeros
-    const __nv_bfloat16* src = base + (bytes ? at.token * a.q.stride_row + at.g * a.q.stride_head : 0);
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + row_chunk<T>(r, chunk)), "l"(src), "r"(bytes) : "memory");
-    at = at.after(step, a.group);
+      for (int i = 0; i < 128 / kLines; ++i) {
+        const int bytes = r.token < s.n_new ? 16 : 0;     // rows that do not exist are zeros
+        const __nv_bfloat16* src = base + (bytes ? r.token * a.q.stride_row + r.g * a.q.stride_head : 0);
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(q_ring + slot * T::TILE + tile_chunk(first + i * kLines, chunk)), "l"(src), "r"(bytes)
+                     : "memory");
+        r = r.after(line_step, a.group);
+      }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+      sm.below[done % kBelow][thread] = -own;
+      own = later;
+      copy_at = copy_at.after(tile_step, a.group);
+      if (done + 1 > handed + 2) {
+        asm volatile("cp.async.wait_group 2;" ::: "memory");
+        hand_over(done - 1);
+      }
+    }
+    // all of them, before a wait for what these have to bring about
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    hand_over(done);
   }
-  return thread < kGroupRows ? row_lse2(a, s.row0 + lse_at.token, head * a.group + lse_at.g, lse_at.token < s.n_new) : 0.f;
+}
+
+// ---------------------------------------------------------------------------------------------- products
+template <class T>
+__device__ __forceinline__ void multiply(const WeighArgs& w, Smem& sm, uint32_t tmem, uint32_t k_tiles, uint32_t q_ring, int64_t w0, int64_t w1, const Abort& ab) {
+  constexpr uint32_t idesc = instr_desc(128, 128, false);
+  const uint64_t k_desc = smem_desc<128>(k_tiles), q_desc = smem_desc<128>(q_ring);
+  const bool on = elect_one();
+  Walk walk(w, sm, w0, w1);
+  uint32_t done = 0, items = 0;
+  while (walk.next(w)) {
+    if (walk.tiles == 0) continue;
+    const uint32_t buf = items & 1u;
+    if (!mbar_wait_warp(smem_u32(&sm.k_full[buf]), (items >> 1) & 1u, ab)) break;
+    ++items;
+    bool fine = true;
+    for (int j = 0; j < walk.tiles; ++j, ++done) {
+      const uint32_t slot = done % T::STAGES, acc = done % kAccs;
+      fine = mbar_wait_warp(smem_u32(&sm.q_full[slot]), (done / T::STAGES) & 1u, ab) && mbar_wait_warp(smem_u32(&sm.acc_empty[acc]), ((done / kAccs) & 1u) ^ 1u, ab);
+      if (!fine) break;
+      tc_fence_after();
+      if (on) {
+#pragma unroll
+        for (int i = 0; i < T::D / 16; ++i) {
+          const uint32_t at = (uint32_t)((i >> 2) * (128 * 128 >> 4) + 2 * (i & 3));
+          tc_mma<false, false>(tmem + 128 * acc, k_desc + buf * (T::TILE >> 4) + at, q_desc + slot * (T::TILE >> 4) + at, idesc, (uint32_t)(i != 0));
+        }
+        tc_commit(smem_u32(&sm.q_empty[slot]));
+        tc_commit(smem_u32(&sm.acc_full[acc]));
+        mbar_arrive(smem_u32(&sm.acc_full[acc]));         // hands on what this warp has seen: the rows' log-sum-exps
+        if (j + 1 == walk.tiles) tc_commit(smem_u32(&sm.k_empty[buf]));
+      }
+      __syncwarp();
+    }
+    if (!fine) break;
+  }
+  if (on) tc_commit(smem_u32(&sm.mma_done));
+  __syncwarp();
+  mbar_wait_warp(smem_u32(&sm.mma_done), 0u, ab);
+}
+
+// ---------------------------------------------------------------------------------------------- weights
+template <class T>
+__device__ __forceinline__ void add_up(const WeighArgs& w, Smem& sm, uint32_t tmem, int64_t w0, int64_t w1, const Abort& ab) {
+  const AttendArgs& a = w.a;
+  const int lane = threadIdx.x & 31, set = (int)threadIdx.x >> 7, in = threadIdx.x & 127;
+  const uint32_t lanes = (uint32_t)(in & ~31) << 16;
+  const int64_t pool_rows = a.kv.n_blocks * a.kv.n_kv_heads * a.kv.block_tokens;
+  Walk walk(w, sm, w0, w1);
+  uint32_t done = 0, items = 0;                           // tiles before this item, items
+  while (walk.next(w)) {
+    const SeqSpan& s = walk.span.rows;
+    const int key = walk.key0 + in;
+    const bool books = set == 0 && walk.inside && key < s.end;
+    float held = 0.f;
+    if (books && key < walk.span.fresh) held = w.weight[(int64_t)walk.pool_at + in];
+    int from = INT_MIN;                                   // the first row that sees the key
+    if (key < s.first || key >= s.end) from = INT_MAX;
+    else if (a.causal) from = (int)max(min(((int64_t)key - s.pos0) * a.group, (int64_t)INT_MAX), (int64_t)INT_MIN);
+    float f = a.c;
+    if constexpr (T::BITS == 8) f = logit_factor(a.c * group_scale(a.kv.k_scale, s, key & ~(kScaleTokens - 1), (walk.pool_at + in) & ~(kScaleTokens - 1), pool_rows), 1.f);
+    const uint64_t ff = pack2(f, f);
+    float sum = 0.f, lost = 0.f;
+    for (int j = (int)((done + (uint32_t)set) & 1u); j < walk.tiles; j += 2) {
+      const uint32_t tile = done + (uint32_t)j, acc = tile % kAccs;
+      if (!mbar_wait_warp(smem_u32(&sm.acc_full[acc]), (tile / kAccs) & 1u, ab)) return;
+      tc_fence_after();
+      const float* below = sm.below[tile % kBelow];
+      const int rr = walk.row_first + j * kRows;
+      const bool guard = __any_sync(0xffffffffu, rr < from);
+      uint64_t part[2] = {0ull, 0ull};
+      uint32_t z[2][16];
+      tmem_issue<16>(tmem + 128 * acc + lanes, z[0]);
+#pragma unroll
+      for (int c = 0; c < 8; ++c) {
+        tmem_load_wait();
+        tmem_ready<16>(z[c & 1]);
+        if (c < 7) {
+          tmem_issue<16>(tmem + 128 * acc + lanes + 16 * (c + 1), z[(c + 1) & 1]);
+        } else {
+          tc_fence_before();                              // the accumulator is in registers
+          __syncwarp();
+          if (lane == 0) mbar_arrive(smem_u32(&sm.acc_empty[acc]));
+        }
+        float p[16];
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+          const float4 b = *reinterpret_cast<const float4*>(below + 16 * c + i);
+          unpack2(fma2(pack2(z[c & 1][i], z[c & 1][i + 1]), ff, pack2(b.x, b.y)), p[i], p[i + 1]);
+          unpack2(fma2(pack2(z[c & 1][i + 2], z[c & 1][i + 3]), ff, pack2(b.z, b.w)), p[i + 2], p[i + 3]);
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) p[i] = fast_exp2(p[i]);
+        if (guard) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (rr + 16 * c + i < from) p[i] = 0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < 16; i += 2) part[(i >> 1) & 1] = add2(part[(i >> 1) & 1], pack2(p[i], p[i + 1]));
+      }
+      float u, v;
+      unpack2(add2(part[0], part[1]), u, v);
+      const float y = __fsub_rn(u + v, lost), t = __fadd_rn(sum, y);
+      lost = __fsub_rn(__fsub_rn(t, sum), y);
+      sum = t;
+    }
+    done += (uint32_t)walk.tiles;
+    // both sets of warps meet; the sums of two items lie apart
+    float* other = sm.sums[items & 1u];
+    if (set == 1) other[in] = sum;
+    __syncwarp();
+    if (lane == 0) mbar_arrive(smem_u32(&sm.summed));
+    if (!mbar_wait_warp(smem_u32(&sm.summed), items & 1u, ab)) return;
+    ++items;
+    if (books) book(w, (int64_t)walk.pool_at + in, held, sum + other[in], key, walk.span.fresh, walk.span.fresh_row);
+  }
 }
 
 template <int D, int BITS>
 __global__ void __launch_bounds__(kThreads, 1) weigh_prompt_kernel(const __grid_constant__ WeighArgs w) {
   using T = Traits<D, BITS>;
-  extern __shared__ __align__(128) unsigned char q_rows[];
-  __shared__ Smem sm;
-  const AttendArgs& a = w.a;
-  find_start(w, sm);
-  const int64_t per = (sm.total + gridDim.x - 1) / gridDim.x, w0 = per * blockIdx.x, w1 = min(w0 + per, sm.total);
-  if (w0 >= w1) return;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, key_group = warp % kKeyGroups, row_group = warp / kKeyGroups, c = lane & 3;
-  const int in_group = (int)threadIdx.x % kGroupThreads;
-  const unsigned char* group_rows = q_rows + row_group * kStages * T::QSTAGE;
-  const uint32_t q_addr = smem_u32(group_rows);           // of the copies
-  const int64_t pool_rows = a.kv.n_blocks * a.kv.n_kv_heads * a.kv.block_tokens;
-  const RowAt copy_step(kGroupThreads / (D / 8), a.group), stage_step(kRows, a.group);   // from a thread's row to its next, from a stage to the next
-  Cursor cur = first_item(w, sm, w0);
-  WeighSpan span = weigh_span(w, cur.seq);
-  while (cur.at < w1) {
-    // the next item: heads and sequences behind one another
-    while (span.rows.n_new <= 0 || cur.tile * kKeys >= span.rows.end) {
-      cur.tile = 0;
-      if (span.rows.n_new <= 0 || span.rows.end == 0 || ++cur.head >= a.kv.n_kv_heads) {
-        cur.head = 0;
-        if (++cur.seq >= a.step.n_seqs) return;
-        span = weigh_span(w, cur.seq);
-      }
+  extern __shared__ unsigned char smem_raw[];
+  unsigned char* k_tiles = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
+  unsigned char* q_ring = k_tiles + 2 * T::TILE;
+  Smem& sm = *reinterpret_cast<Smem*>(q_ring + T::STAGES * T::TILE);
+  const int warp = threadIdx.x >> 5;
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < T::STAGES; ++i) {
+      mbar_init(smem_u32(&sm.q_full[i]), 4);
+      mbar_init(smem_u32(&sm.q_empty[i]), 1);
     }
-    const SeqSpan& s = span.rows;
-    const int key0 = cur.tile * kKeys, stages = stages_of(w, s, key0);
-    const int row_first = first_row(w, s, key0);
-    const int pool_at = pool_row(a, cur.seq, cur.head, key0);
-    const bool inside = pool_at < pool_rows;
-    float lse2[2];                                        // of the stages under way
-    const int group_first = row_first + row_group * kGroupRows;
-    RowAt copy_at(group_first + in_group / (D / 8), a.group), lse_at(group_first + in_group % kGroupRows, a.group);
-    auto fetch = [&](int slot) {
-      const float x = fetch_rows<T>(w, s, cur.head, copy_at, lse_at, copy_step, q_addr + slot * T::QSTAGE);
-      copy_at = copy_at.after(stage_step, a.group), lse_at = lse_at.after(stage_step, a.group);
-      return x;
-    };
-#pragma unroll
     for (int i = 0; i < 2; ++i) {
-      lse2[i] = i < stages ? fetch(i) : 0.f;
-      asm volatile("cp.async.commit_group;" ::: "memory");
+      mbar_init(smem_u32(&sm.k_full[i]), 4);
+      mbar_init(smem_u32(&sm.k_empty[i]), 1);
     }
-    float held = 0.f;
-    const int own = key0 + (int)threadIdx.x;
-    const bool books = threadIdx.x < kKeys && inside && own < s.end;
-    if (books && own < span.fresh) held = w.weight[(int64_t)pool_at + threadIdx.x];
-    // the warp's keys
-    uint32_t k[2][T::BLOCKS][2][4];
-    int from[2][2];                                       // the first row that sees a key
-    int guard_below = INT_MIN;
-#pragma unroll
-    for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int in = key_group * 32 + kt * 16 + h * 8 + (lane >> 2), key = key0 + in;
-#pragma unroll
-        for (int b = 0; b < T::BLOCKS; ++b) {
-          if (stages > 0 && inside) load_eight<T>(a.kv, (int64_t)pool_at + in, 4 * b + c, k[kt][b][h]);
-          else k[kt][b][h][0] = k[kt][b][h][1] = k[kt][b][h][2] = k[kt][b][h][3] = 0u;
-        }
-        if (key < s.first || key >= s.end) from[kt][h] = INT_MAX;
-        else from[kt][h] = a.causal ? (int)max(min(((int64_t)key - s.pos0) * a.group, (int64_t)INT_MAX), (int64_t)INT_MIN) : INT_MIN;
-        guard_below = max(guard_below, from[kt][h]);
-      }
-    guard_below = __reduce_max_sync(0xffffffffu, guard_below);
-    float f = a.c;
-    if constexpr (BITS == 8) f = logit_factor(a.c * group_scale(a.kv.k_scale, s, (key0 + key_group * 32) & ~(kScaleTokens - 1), (pool_at + key_group * 32) & ~(kScaleTokens - 1), pool_rows), 1.f);
-    const uint64_t ff = pack2(f, f);
-    float sum[2][2] = {}, lost[2][2] = {};
-#pragma unroll 1
-    for (int stage = 0; stage < stages; ++stage) {
-      const int slot = stage % kStages;
-      if (in_group < kGroupRows) sm.below[row_group][slot][in_group] = -lse2[0];
-      lse2[0] = lse2[1];
-      asm volatile("cp.async.wait_group 1;" ::: "memory");
-      asm volatile("bar.sync %0, %1;" ::"r"(1 + row_group), "n"(kGroupThreads) : "memory");   // the stage is there, and the one before it is read
-      if (stage + 2 < stages) lse2[1] = fetch((stage + 2) % kStages);
-      asm volatile("cp.async.commit_group;" ::: "memory");
-      uint64_t part[2][2] = {};                           // pairs: of either of the thread's rows of eight
-      // Products of some eights of rows, one instruction at a time (kProducts): they are issued in turns with the exponentials of the rows
-      // before, so that neither unit waits while all warps want the other.
-      constexpr int kStep = T::STEP, kSteps = kGroupRows / 8 / kStep, kChains = 2 * kStep, kProducts = 2 * T::BLOCKS * kChains;
-      float z[2][kStep][2][4];
-      uint4 q[kStep];
-      auto product = [&](int step, int i) {
-        const int b = i / (2 * kChains), second = i / kChains & 1, j = i % kChains >> 1, kt = i & 1;
-        float (&to)[4] = z[step & 1][j][kt];
-        if (kt == 0 && second == 0)
-          q[j] = *reinterpret_cast<const uint4*>(group_rows + slot * T::QSTAGE + row_chunk<T>((step * kStep + j) * 8 + (lane >> 2), 4 * b + c));
-        if (i < kChains) mma_first(to, k[kt][b][0][0], k[kt][b][1][0], k[kt][b][0][1], k[kt][b][1][1], q[j].x, q[j].y);
-        else if (second == 0) mma(to, k[kt][b][0][0], k[kt][b][1][0], k[kt][b][0][1], k[kt][b][1][1], q[j].x, q[j].y);
-        else mma(to, k[kt][b][0][2], k[kt][b][1][2], k[kt][b][0][3], k[kt][b][1][3], q[j].z, q[j].w);
-      };
-#pragma unroll
-      for (int i = 0; i < kProducts; ++i) product(0, i);
-#pragma unroll
-      for (int step = 0; step < kSteps; ++step) {
-        const int rr = group_first + stage * kRows + step * 8 * kStep;
-        float x[kStep][2][4];
-#pragma unroll
-        for (int j = 0; j < kStep; ++j) {
-          const uint64_t below = *reinterpret_cast<const uint64_t*>(&sm.below[row_group][slot][(step * kStep + j) * 8 + 2 * c]);
-#pragma unroll
-          for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-              unpack2(fma2(pack2(z[step & 1][j][kt][2 * h], z[step & 1][j][kt][2 * h + 1]), ff, below), x[j][kt][2 * h], x[j][kt][2 * h + 1]);
-        }
-#pragma unroll
-        for (int i = 0; i < 8 * kStep; ++i) {
-          if (step + 1 < kSteps) {
-#pragma unroll
-            for (int n = 0; n < kProducts / (8 * kStep); ++n) product(step + 1, i * (kProducts / (8 * kStep)) + n);
-          }
-          float& e = x[i >> 3][i >> 2 & 1][i & 3];
-          asm volatile("ex2.approx.ftz.f32 %0, %0;" : "+f"(e));
-        }
-        if (rr < guard_below) {
-#pragma unroll
-          for (int j = 0; j < kStep; ++j)
-#pragma unroll
-            for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-              for (int e = 0; e < 4; ++e)
-                if (rr + 8 * j + 2 * c + (e & 1) < from[kt][e >> 1]) x[j][kt][e] = 0.f;
-        }
-#pragma unroll
-        for (int j = 0; j < kStep; ++j)
-#pragma unroll
-          for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) part[kt][h] = add2(part[kt][h], pack2(x[j][kt][2 * h], x[j][kt][2 * h + 1]));
-      }
-#pragma unroll
-      for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          float u, v;
-          unpack2(part[kt][h], u, v);
-          const float y = __fsub_rn(u + v, lost[kt][h]), t = __fadd_rn(sum[kt][h], y);
-          lost[kt][h] = __fsub_rn(__fsub_rn(t, sum[kt][h]), y);
-          sum[kt][h] = t;
-        }
+    for (int i = 0; i < kAccs; ++i) {
+      mbar_init(smem_u32(&sm.acc_full[i]), 2);
+      mbar_init(smem_u32(&sm.acc_empty[i]), 4);
     }
-#pragma unroll
-    for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        float x = sum[kt][h];
-        x += __shfl_xor_sync(0xffffffffu, x, 1);
-        x += __shfl_xor_sync(0xffffffffu, x, 2);
-        if (c == 0) sm.sums[row_group][key_group * 32 + kt * 16 + h * 8 + (lane >> 2)] = x;
-      }
-    asm volatile("cp.async.wait_all;" ::: "memory");
-    __syncthreads();
-    if (books) {
-      float got = 0.f;
-#pragma unroll
-      for (int g = 0; g < kRowGroups; ++g) got += sm.sums[g][threadIdx.x];
-      book(w, (int64_t)pool_at + threadIdx.x, held, got, own, span.fresh, span.fresh_row);
-    }
-    __syncthreads();                                      // before the next item's rows and sums
-    cur.at += stages + 1;
-    ++cur.tile;
+    mbar_init(smem_u32(&sm.summed), 8);
+    mbar_init(smem_u32(&sm.mma_done), 1);
+    sm.abort = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 12) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&sm.tmem)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  find_start(w, sm);                                      // barriers of the CTA
+  tc_fence_after();
+  const uint32_t tmem = sm.tmem;
+  const int64_t per = (sm.total + gridDim.x - 1) / gridDim.x, w0 = per * blockIdx.x, w1 = min(w0 + per, sm.total);
+  const Abort ab{&sm.abort, w.a.dev_status};
+  if (w0 < w1) {
+    if (warp < 8) add_up<T>(w, sm, tmem, w0, w1, ab);
+    else if (warp < 12) bring<T>(w, sm, k_tiles, smem_u32(q_ring), w0, w1, ab);
+    else multiply<T>(w, sm, tmem, smem_u32(k_tiles), smem_u32(q_ring), w0, w1, ab);
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (sm.abort != 0) {
+    // a wait ran out: what is still in flight gets time to land before the memory is given back
+    const unsigned long long t0 = global_timer();
+    while (global_timer() - t0 < 2000000ull) __nanosleep(1000);
+  }
+  __syncthreads();
+  if (warp == 12) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
   }
 }
 
 template <int D, int BITS>
 int32_t launch(const WeighArgs& w, int sm_count, cudaStream_t stream) {
-  constexpr int kBytes = kRowGroups * kStages * Traits<D, BITS>::QSTAGE;
+  constexpr int kBytes = smem_bytes<Traits<D, BITS>>();
+  static_assert(kBytes <= 227 * 1024);
   static ContextSet done;
   const int32_t st = allow_shared_memory(reinterpret_cast<const void*>(weigh_prompt_kernel<D, BITS>), kBytes, done);
   if (st != SPF_OK) return st;
