@@ -15,7 +15,7 @@
 // The list of all items, each as long as the tiles of rows that see any of its keys, is cut into one part for each SM; an item belongs to the
 // part that its beginning lies in.
 //
-// Warps: 0-3 and 4-7 the exponentials, of the even and the odd tiles; 8-11 keys, rows and log-sum-exps; 12 issues the products.
+// Warps: sets of four for the exponentials, a tile each in turn; four for keys, rows and log-sum-exps; one issues the products.
 #include <climits>
 
 #include "weigh.cuh"
@@ -23,7 +23,7 @@
 namespace spf {
 namespace {
 
-constexpr int kThreads = 416, kKeys = 128, kRows = 128, kEnds = 2;
+constexpr int kSets = 2, kThreads = (4 * kSets + 5) * 32, kKeys = 128, kRows = 128, kEnds = 2;
 constexpr int kAccs = 4, kBelow = 16;                     // accumulators in tensor memory; tiles whose log-sum-exps are kept: more than may be under way
 
 template <int D_, int BITS_>
@@ -34,7 +34,7 @@ struct Traits {
 struct Smem {
   unsigned long long q_full[6], q_empty[6], k_full[2], k_empty[2], acc_full[kAccs], acc_empty[kAccs], summed, mma_done;
   float below[kBelow][kRows];                             // the rows' base-2 log-sum-exps, negated
-  float sums[2][kKeys];                                   // of the odd tiles
+  float sums[2][kSets - 1][kKeys];                        // of all sets but the first
   int64_t scan[kThreads / 32];
   int64_t total, start_base;
   int start_seq;
@@ -217,16 +217,20 @@ template <class T>
 __device__ __forceinline__ void bring(const WeighArgs& w, Smem& sm, unsigned char* k_tiles, uint32_t q_ring, int64_t w0, int64_t w1, const Abort& ab) {
   constexpr int kChunks = T::D / 8, kLines = 128 / kChunks;
   const AttendArgs& a = w.a;
-  const int thread = (int)threadIdx.x - 256, lane = threadIdx.x & 31, first = thread / kChunks, chunk = thread % kChunks;
+  const int thread = (int)threadIdx.x - 128 * kSets, lane = threadIdx.x & 31, first = thread / kChunks, chunk = thread % kChunks;
   const RowAt line_step(kLines, a.group), tile_step(kRows, a.group);
   Walk walk(w, sm, w0, w1);
   uint32_t done = 0, items = 0;                           // tiles and items brought
   uint32_t handed = 0;                                    // tiles handed over: their copies have landed
-  auto hand_over = [&](uint32_t upto) {
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-    __syncwarp();
-    for (; handed < upto; ++handed)
+  // Log-sum-exps are copied as they are and made what the exponentials want here: loaded into registers, each tile waited for its own.
+  auto hand_over = [&](uint32_t upto, int64_t row) {      // row: the thread's row of the first of them; beyond the last: of no effect
+    for (; handed < upto; ++handed, row += kRows) {
+      float& own = sm.below[handed % kBelow][thread];
+      own = row < (int64_t)walk.span.rows.n_new * a.group && own != -INFINITY ? -own * kLog2e : -INFINITY;
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&sm.q_full[handed % T::STAGES]));
+    }
   };
   while (walk.next(w)) {
     if (walk.tiles == 0) continue;
@@ -248,12 +252,10 @@ __device__ __forceinline__ void bring(const WeighArgs& w, Smem& sm, unsigned cha
     ++items;
     const __nv_bfloat16* base = a.q.data + s.row0 * a.q.stride_row + (int64_t)head * a.group * a.q.stride_head + 8 * chunk;
     RowAt copy_at(walk.row_first + first, a.group), lse_at(walk.row_first + thread, a.group);
-    auto lse2 = [&] { return row_lse2(a, s.row0 + lse_at.token, head * a.group + lse_at.g, lse_at.token < s.n_new); };
-    float own = lse2();
+    const float* lse = a.lse + s.row0 * a.lse_stride_row + (int64_t)head * a.group * a.lse_stride_head;
+    const int64_t own_row = (int64_t)walk.row_first + thread;
     for (int j = 0; j < walk.tiles; ++j, ++done) {
       const uint32_t slot = done % T::STAGES;
-      lse_at = lse_at.after(tile_step, a.group);
-      const float later = j + 1 < walk.tiles ? lse2() : 0.f;
       if (!mbar_wait_warp(smem_u32(&sm.q_empty[slot]), ((done / T::STAGES) & 1u) ^ 1u, ab)) return;
       RowAt r = copy_at;
 #pragma unroll
@@ -264,18 +266,21 @@ __device__ __forceinline__ void bring(const WeighArgs& w, Smem& sm, unsigned cha
                      : "memory");
         r = r.after(line_step, a.group);
       }
+      const int bytes = lse_at.token < s.n_new ? 4 : 0;
+      asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(smem_u32(&sm.below[done % kBelow][thread])),
+                   "l"(lse + (bytes ? lse_at.token * a.lse_stride_row + lse_at.g * a.lse_stride_head : 0)), "r"(bytes)
+                   : "memory");
       asm volatile("cp.async.commit_group;" ::: "memory");
-      sm.below[done % kBelow][thread] = -own;
-      own = later;
+      lse_at = lse_at.after(tile_step, a.group);
       copy_at = copy_at.after(tile_step, a.group);
       if (done + 1 > handed + 2) {
         asm volatile("cp.async.wait_group 2;" ::: "memory");
-        hand_over(done - 1);
+        hand_over(done - 1, own_row + (int64_t)(j - 2) * kRows);
       }
     }
     // all of them, before a wait for what these have to bring about
     asm volatile("cp.async.wait_all;" ::: "memory");
-    hand_over(done);
+    hand_over(done, own_row + ((int64_t)walk.tiles - (int64_t)(done - handed)) * kRows);
   }
 }
 
@@ -340,7 +345,7 @@ __device__ __forceinline__ void add_up(const WeighArgs& w, Smem& sm, uint32_t tm
     if constexpr (T::BITS == 8) f = logit_factor(a.c * group_scale(a.kv.k_scale, s, key & ~(kScaleTokens - 1), (walk.pool_at + in) & ~(kScaleTokens - 1), pool_rows), 1.f);
     const uint64_t ff = pack2(f, f);
     float sum = 0.f, lost = 0.f;
-    for (int j = (int)((done + (uint32_t)set) & 1u); j < walk.tiles; j += 2) {
+    for (int j = (int)(((uint32_t)set - done) % kSets); j < walk.tiles; j += kSets) {
       const uint32_t tile = done + (uint32_t)j, acc = tile % kAccs;
       if (!mbar_wait_warp(smem_u32(&sm.acc_full[acc]), (tile / kAccs) & 1u, ab)) return;
       tc_fence_after();
@@ -385,14 +390,18 @@ __device__ __forceinline__ void add_up(const WeighArgs& w, Smem& sm, uint32_t tm
       sum = t;
     }
     done += (uint32_t)walk.tiles;
-    // both sets of warps meet; the sums of two items lie apart
-    float* other = sm.sums[items & 1u];
-    if (set == 1) other[in] = sum;
+    // the sets meet; the sums of two items lie apart
+    float (&others)[kSets - 1][kKeys] = sm.sums[items & 1u];
+    if (set > 0) others[set - 1][in] = sum;
     __syncwarp();
     if (lane == 0) mbar_arrive(smem_u32(&sm.summed));
     if (!mbar_wait_warp(smem_u32(&sm.summed), items & 1u, ab)) return;
     ++items;
-    if (books) book(w, (int64_t)walk.pool_at + in, held, sum + other[in], key, walk.span.fresh, walk.span.fresh_row);
+    if (books) {
+#pragma unroll
+      for (int i = 0; i < kSets - 1; ++i) sum += others[i][in];
+      book(w, (int64_t)walk.pool_at + in, held, sum, key, walk.span.fresh, walk.span.fresh_row);
+    }
   }
 }
 
@@ -417,12 +426,12 @@ __global__ void __launch_bounds__(kThreads, 1) weigh_prompt_kernel(const __grid_
       mbar_init(smem_u32(&sm.acc_full[i]), 2);
       mbar_init(smem_u32(&sm.acc_empty[i]), 4);
     }
-    mbar_init(smem_u32(&sm.summed), 8);
+    mbar_init(smem_u32(&sm.summed), 4 * kSets);
     mbar_init(smem_u32(&sm.mma_done), 1);
     sm.abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == 12) {
+  if (warp == 4 * kSets + 4) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&sm.tmem)) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
@@ -433,8 +442,8 @@ __global__ void __launch_bounds__(kThreads, 1) weigh_prompt_kernel(const __grid_
   const int64_t per = (sm.total + gridDim.x - 1) / gridDim.x, w0 = per * blockIdx.x, w1 = min(w0 + per, sm.total);
   const Abort ab{&sm.abort, w.a.dev_status};
   if (w0 < w1) {
-    if (warp < 8) add_up<T>(w, sm, tmem, w0, w1, ab);
-    else if (warp < 12) bring<T>(w, sm, k_tiles, smem_u32(q_ring), w0, w1, ab);
+    if (warp < 4 * kSets) add_up<T>(w, sm, tmem, w0, w1, ab);
+    else if (warp < 4 * kSets + 4) bring<T>(w, sm, k_tiles, smem_u32(q_ring), w0, w1, ab);
     else multiply<T>(w, sm, tmem, smem_u32(k_tiles), smem_u32(q_ring), w0, w1, ab);
   }
   tc_fence_before();
@@ -445,7 +454,7 @@ __global__ void __launch_bounds__(kThreads, 1) weigh_prompt_kernel(const __grid_
     while (global_timer() - t0 < 2000000ull) __nanosleep(1000);
   }
   __syncthreads();
-  if (warp == 12) {
+  if (warp == 4 * kSets + 4) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
   }
