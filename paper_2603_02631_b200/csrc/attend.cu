@@ -77,6 +77,17 @@ int32_t encode_pool_map(const char* who, const spf_kv_cache* cache, void* pool, 
   return SPF_OK;
 }
 
+int32_t encode_rows_map(const char* who, const RowsView& rows, int n_rows, int n_heads, int head_dim, int tokens, int heads, CUtensorMap* map) {
+  const EncodeFn encode = encoder();
+  if (encode == nullptr) return fail(SPF_ERR_CUDA, "%s: cuTensorMapEncodeTiled is not available from the driver", who);
+  const cuuint64_t dims[3] = {(cuuint64_t)head_dim, (cuuint64_t)n_heads, (cuuint64_t)n_rows};
+  const cuuint64_t strides[2] = {(cuuint64_t)(n_heads > 1 ? rows.stride_head : head_dim) * 2, (cuuint64_t)(n_rows > 1 ? rows.stride_row : head_dim) * 2};
+  const cuuint32_t box[3] = {64, (cuuint32_t)heads, (cuuint32_t)tokens}, ones[3] = {1, 1, 1};
+  const CUresult r = encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, rows.data, dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) return fail(SPF_ERR_CUDA, "%s: encoding a tensor map of rows failed (CUresult %d)", who, (int)r);
+  return SPF_OK;
+}
 // Rows of `words` 32-bit words, one behind the other.
 static int32_t encode_words(const char* who, void* data, cuuint64_t words, cuuint64_t rows, CUtensorMap* map) {
   const EncodeFn encode = encoder();

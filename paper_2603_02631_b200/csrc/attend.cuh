@@ -76,6 +76,8 @@ int32_t attend_settings(const char* who, const spf_kv_cache* cache, const spf_kv
 
 // Tensor map of a pool: rows of d elements seen as spans of at most 128 bytes, `tile_rows` rows a copy.
 int32_t encode_pool_map(const char* who, const spf_kv_cache* cache, void* pool, int tile_rows, CUtensorMap* map);
+// Of a step's rows: a copy is `tokens` rows, `heads` heads and 64 dimensions of each.  Strides must not be zero.
+int32_t encode_rows_map(const char* who, const RowsView& rows, int n_rows, int n_heads, int head_dim, int tokens, int heads, CUtensorMap* map);
 // Of one fp32 number for each token, a row of the map being those of `tile_rows` of them.
 int32_t encode_ledger_map(const char* who, const spf_kv_cache* cache, float* numbers, int tile_rows, CUtensorMap* map);
 // 4 bits: of the scales of a pool, a row of the map being those of 128 tokens (blocks are multiples of them).

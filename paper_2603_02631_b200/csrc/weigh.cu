@@ -345,7 +345,7 @@ extern "C" int32_t spf_kv_weigh(const spf_kv_cache* cache, const spf_kv_step* st
   if (st != SPF_OK) return st;
   const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
   const int64_t rows = (int64_t)a.group * (w.last_rows > 0 ? std::min(w.last_rows, step->max_new) : step->max_new);
-  if (rows > 128) return weigh_prompt_launch(w, cache->head_dim, sm_count, stream);
+  if (rows > 128 && weigh_prompt_fits(w)) return weigh_prompt_launch(w, n_q_heads, cache->head_dim, sm_count, stream);
   const bool d64 = cache->head_dim == 64;
   switch (a.kv.bits) {
     case 4: return d64 ? launch_rows<64, 4>(w, cache, rows, sm_count, stream) : launch_rows<128, 4>(w, cache, rows, sm_count, stream);

@@ -8,6 +8,7 @@ namespace spf {
 struct WeighArgs {
   AttendArgs a;                   // its lse is read; `out` is not used
   CUtensorMap k_map, k_scale_map, weight_map;   // few rows; the second: 4 bits
+  CUtensorMap q_map;              // many rows
   float* weight;                  // [n_blocks][n_kv_heads][block_tokens]
   int32_t* position;              // the same; may be null
   const int32_t* positions;       // [n_rows]; null: a token's place
@@ -51,6 +52,7 @@ __device__ __forceinline__ void book(const WeighArgs& w, int64_t cell, float hel
 }
 
 // The kernel for many rows a key head and sequence; that for few is weigh.cu's own.
-int32_t weigh_prompt_launch(const WeighArgs& w, int head_dim, int sm_count, cudaStream_t stream);
+bool weigh_prompt_fits(const WeighArgs& w);       // whether its copies can read the queries
+int32_t weigh_prompt_launch(WeighArgs& w, int n_q_heads, int head_dim, int sm_count, cudaStream_t stream);
 
 }  // namespace spf

@@ -10,12 +10,13 @@
 // each of few warps.)  Sums of a tile are added with what the additions lose (thousands of rows make 1.7e-6 of a weight otherwise).
 //
 // Keys are brought once for all rows of an item (a sequence, key head and 128 keys) and widened to bf16 on the way (exactly: 8-bit values, and
-// 4-bit codes times scales of five bits), the next item's while this one's last rows are being made; rows go by in tiles of 128.
+// 4-bit codes times scales of five bits), the next item's while this one's last rows are being made.  Rows go by in tiles of as many tokens as fit whole into 128, a box of the queries each, whose
+// strides the tensor map has.
 //
 // The list of all items, each as long as the tiles of rows that see any of its keys, is cut into one part for each SM; an item belongs to the
 // part that its beginning lies in.
 //
-// Warps: sets of four for the exponentials, a tile each in turn; four for keys, rows and log-sum-exps; one issues the products.
+// Warps: sets of four for the exponentials, a tile each in turn; four for keys and log-sum-exps; one issues the products, one copies rows.
 #include <climits>
 
 #include "weigh.cuh"
@@ -23,7 +24,7 @@
 namespace spf {
 namespace {
 
-constexpr int kSets = 2, kThreads = (4 * kSets + 5) * 32, kKeys = 128, kRows = 128, kEnds = 2;
+constexpr int kSets = 2, kThreads = (4 * kSets + 6) * 32, kKeys = 128, kEnds = 2;
 constexpr int kAccs = 4, kBelow = 16;                     // accumulators in tensor memory; tiles whose log-sum-exps are kept: more than may be under way
 
 template <int D_, int BITS_>
@@ -32,8 +33,8 @@ struct Traits {
 };
 
 struct Smem {
-  unsigned long long q_full[6], q_empty[6], k_full[2], k_empty[2], acc_full[kAccs], acc_empty[kAccs], summed, mma_done;
-  float below[kBelow][kRows];                             // the rows' base-2 log-sum-exps, negated
+  unsigned long long q_full[6], q_empty[6], b_full[6], k_full[2], k_empty[2], acc_full[kAccs], acc_empty[kAccs], summed, mma_done;
+  float below[kBelow][128];                             // the rows' base-2 log-sum-exps, negated
   float sums[2][kSets - 1][kKeys];                        // of all sets but the first
   int64_t scan[kThreads / 32];
   int64_t total, start_base;
@@ -46,15 +47,15 @@ template <class T>
 constexpr int smem_bytes() { return (2 + T::STAGES) * T::TILE + (int)sizeof(Smem) + 1024; }
 
 // ---------------------------------------------------------------------------------------------- the list of items
-// Rows of a sequence and key head, from the first that sees key0 on (a multiple of 8).
-__device__ __forceinline__ int first_row(const WeighArgs& w, const SeqSpan& s, int key0) {
-  if (!w.a.causal) return 0;
-  const int64_t r = ((int64_t)key0 - s.pos0) * w.a.group;
-  return (int)min(max(r, (int64_t)0), (int64_t)s.n_new * w.a.group) & ~7;
+// Tokens whose rows make a tile: as many as fit whole.
+__device__ __forceinline__ int tile_tokens(const WeighArgs& w) { return 128 / w.a.group; }
+// Of a sequence's tokens the first that sees key0.
+__device__ __forceinline__ int first_token(const WeighArgs& w, const SeqSpan& s, int key0) {
+  return w.a.causal ? (int)min(max((int64_t)key0 - s.pos0, (int64_t)0), (int64_t)s.n_new) : 0;
 }
 __device__ __forceinline__ int tiles_of(const WeighArgs& w, const SeqSpan& s, int key0) {
   if (key0 + kKeys <= s.first) return 0;
-  return (int)(((int64_t)s.n_new * w.a.group - first_row(w, s, key0) + kRows - 1) / kRows);
+  return (s.n_new - first_token(w, s, key0) + tile_tokens(w) - 1) / tile_tokens(w);
 }
 // Length of a (sequence, key head) in the list: its tiles of rows, and for an item's beginning and end as long as kEnds of them.
 __device__ __forceinline__ int64_t head_cost(const WeighArgs& w, const SeqSpan& s) {
@@ -134,7 +135,7 @@ struct Walk {
   Cursor at;
   WeighSpan span;
   int64_t end;
-  int key0, tiles, row_first;                             // of the item; row_first: the first row of its first tile
+  int key0, tiles, token;                                 // of the item; token: the first of its first tile
   int pool_at;                                            // the first key's row in the pool
   bool inside;
 
@@ -151,7 +152,7 @@ struct Walk {
     }
     key0 = at.tile * kKeys;
     tiles = tiles_of(w, span.rows, key0);
-    row_first = first_row(w, span.rows, key0);
+    token = first_token(w, span.rows, key0);
     pool_at = pool_row(w.a, at.seq, at.head, key0);
     inside = pool_at < w.a.kv.n_blocks * w.a.kv.n_kv_heads * w.a.kv.block_tokens;
     at.at += tiles + kEnds;
@@ -197,45 +198,50 @@ __device__ __forceinline__ void load_eight(const KvView& kv, int64_t row, int j,
   }
 }
 
-// A row of a sequence and key head as (token, head of the group), and the step to one further on, without a division.
-struct RowAt {
-  int token, g;
-  __device__ __forceinline__ RowAt(int64_t rr, int group) : token((int)(rr / group)), g((int)(rr - (int64_t)token * group)) {}
-  __device__ __forceinline__ RowAt after(const RowAt& step, int group) const {
-    RowAt r = *this;
-    r.token += step.token, r.g += step.g;
-    if (r.g >= group) r.g -= group, ++r.token;
-    return r;
-  }
-};
-
 // ---------------------------------------------------------------------------------------------- keys and rows into shared memory
-// Byte offset of the 16-byte chunk of a row of keys or queries, as the products read them: spans of 128 bytes, swizzled.
+// The copying thread: a tile of rows is a box of the queries, spans of 64 dimensions x heads of the group x tokens.
+template <class T>
+__device__ __forceinline__ void copy_rows(const WeighArgs& w, Smem& sm, uint32_t q_ring, int64_t w0, int64_t w1, const Abort& ab) {
+  const int tokens = tile_tokens(w);
+  const uint32_t bytes = (uint32_t)(tokens * w.a.group * T::D * 2);
+  const bool on = elect_one();
+  Walk walk(w, sm, w0, w1);
+  uint32_t done = 0;
+  while (walk.next(w)) {
+    for (int j = 0; j < walk.tiles; ++j, ++done) {
+      const uint32_t slot = done % T::STAGES, bar = smem_u32(&sm.q_full[slot]);
+      if (!mbar_wait_warp(smem_u32(&sm.q_empty[slot]), ((done / T::STAGES) & 1u) ^ 1u, ab)) {
+        // a stage's last copy was its (done - stage) / STAGES-th, rounded up
+        const uint32_t stage = threadIdx.x & 31;
+        if (stage < T::STAGES && done > stage) drain_copy(smem_u32(&sm.q_full[stage]), ((done - stage + T::STAGES - 1) / T::STAGES - 1) & 1u);
+        return;
+      }
+      if (on) {
+        mbar_expect_tx(bar, bytes);
+#pragma unroll
+        for (int x = 0; x < T::D; x += 64)
+          tma_load_3d(q_ring + slot * T::TILE + x * 256, &w.q_map, x, walk.at.head * w.a.group, walk.span.rows.row0 + walk.token + j * tokens, bar);
+      }
+      __syncwarp();
+    }
+  }
+}
+
+// Byte offset of the 16-byte chunk of a row of keys, as the products read them: spans of 128 bytes, swizzled.
 __device__ __forceinline__ uint32_t tile_chunk(int row, int chunk) { return (uint32_t)((chunk >> 3) * (128 * 128) + row * 128 + ((chunk ^ row) & 7) * 16); }
 
+// Keys, widened, and log-sum-exps, made what the exponentials want; those of four tiles are loaded together.
 template <class T>
-__device__ __forceinline__ void bring(const WeighArgs& w, Smem& sm, unsigned char* k_tiles, uint32_t q_ring, int64_t w0, int64_t w1, const Abort& ab) {
-  constexpr int kChunks = T::D / 8, kLines = 128 / kChunks;
+__device__ __forceinline__ void bring(const WeighArgs& w, Smem& sm, unsigned char* k_tiles, int64_t w0, int64_t w1, const Abort& ab) {
+  constexpr int kChunks = T::D / 8, kLines = 128 / kChunks, kAhead = 4;
   const AttendArgs& a = w.a;
   const int thread = (int)threadIdx.x - 128 * kSets, lane = threadIdx.x & 31, first = thread / kChunks, chunk = thread % kChunks;
-  const RowAt line_step(kLines, a.group), tile_step(kRows, a.group);
+  const int tokens = tile_tokens(w), own_token = thread / a.group, own_head = thread - own_token * a.group;
   Walk walk(w, sm, w0, w1);
   uint32_t done = 0, items = 0;                           // tiles and items brought
-  uint32_t handed = 0;                                    // tiles handed over: their copies have landed
-  // Log-sum-exps are copied as they are and made what the exponentials want here: loaded into registers, each tile waited for its own.
-  auto hand_over = [&](uint32_t upto, int64_t row) {      // row: the thread's row of the first of them; beyond the last: of no effect
-    for (; handed < upto; ++handed, row += kRows) {
-      float& own = sm.below[handed % kBelow][thread];
-      own = row < (int64_t)walk.span.rows.n_new * a.group && own != -INFINITY ? -own * kLog2e : -INFINITY;
-      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-      __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&sm.q_full[handed % T::STAGES]));
-    }
-  };
   while (walk.next(w)) {
     if (walk.tiles == 0) continue;
     const SeqSpan& s = walk.span.rows;
-    const int head = walk.at.head;
     const uint32_t buf = items & 1u;
     if (!mbar_wait_warp(smem_u32(&sm.k_empty[buf]), ((items >> 1) & 1u) ^ 1u, ab)) return;
     unsigned char* k_tile = k_tiles + buf * T::TILE;
@@ -250,37 +256,28 @@ __device__ __forceinline__ void bring(const WeighArgs& w, Smem& sm, unsigned cha
     __syncwarp();
     if (lane == 0) mbar_arrive(smem_u32(&sm.k_full[buf]));
     ++items;
-    const __nv_bfloat16* base = a.q.data + s.row0 * a.q.stride_row + (int64_t)head * a.group * a.q.stride_head + 8 * chunk;
-    RowAt copy_at(walk.row_first + first, a.group), lse_at(walk.row_first + thread, a.group);
-    const float* lse = a.lse + s.row0 * a.lse_stride_row + (int64_t)head * a.group * a.lse_stride_head;
-    const int64_t own_row = (int64_t)walk.row_first + thread;
-    for (int j = 0; j < walk.tiles; ++j, ++done) {
-      const uint32_t slot = done % T::STAGES;
-      if (!mbar_wait_warp(smem_u32(&sm.q_empty[slot]), ((done / T::STAGES) & 1u) ^ 1u, ab)) return;
-      RowAt r = copy_at;
+    int token = walk.token + own_token;
+    const float* lse = a.lse + (int64_t)(s.row0 + token) * a.lse_stride_row + (int64_t)(walk.at.head * a.group + own_head) * a.lse_stride_head;
+    const int64_t step = tokens * a.lse_stride_row;
+    for (int j0 = 0; j0 < walk.tiles; j0 += kAhead) {
+      float own[kAhead];
 #pragma unroll
-      for (int i = 0; i < 128 / kLines; ++i) {
-        const int bytes = r.token < s.n_new ? 16 : 0;     // rows that do not exist are zeros
-        const __nv_bfloat16* src = base + (bytes ? r.token * a.q.stride_row + r.g * a.q.stride_head : 0);
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(q_ring + slot * T::TILE + tile_chunk(first + i * kLines, chunk)), "l"(src), "r"(bytes)
-                     : "memory");
-        r = r.after(line_step, a.group);
+      for (int i = 0; i < kAhead; ++i) {
+        own[i] = own_token < tokens && token < s.n_new ? __ldg(lse) : -INFINITY;   // rows that do not exist, or saw no key: nothing
+        token += tokens;
+        lse += step;
       }
-      const int bytes = lse_at.token < s.n_new ? 4 : 0;
-      asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(smem_u32(&sm.below[done % kBelow][thread])),
-                   "l"(lse + (bytes ? lse_at.token * a.lse_stride_row + lse_at.g * a.lse_stride_head : 0)), "r"(bytes)
-                   : "memory");
-      asm volatile("cp.async.commit_group;" ::: "memory");
-      lse_at = lse_at.after(tile_step, a.group);
-      copy_at = copy_at.after(tile_step, a.group);
-      if (done + 1 > handed + 2) {
-        asm volatile("cp.async.wait_group 2;" ::: "memory");
-        hand_over(done - 1, own_row + (int64_t)(j - 2) * kRows);
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        if (j0 + i >= walk.tiles) break;
+        const uint32_t slot = done % T::STAGES;
+        if (!mbar_wait_warp(smem_u32(&sm.q_empty[slot]), ((done / T::STAGES) & 1u) ^ 1u, ab)) return;
+        sm.below[done % kBelow][thread] = own[i] == -INFINITY ? -INFINITY : -own[i] * kLog2e;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&sm.b_full[slot]));
+        ++done;
       }
     }
-    // all of them, before a wait for what these have to bring about
-    asm volatile("cp.async.wait_all;" ::: "memory");
-    hand_over(done, own_row + ((int64_t)walk.tiles - (int64_t)(done - handed)) * kRows);
   }
 }
 
@@ -300,7 +297,8 @@ __device__ __forceinline__ void multiply(const WeighArgs& w, Smem& sm, uint32_t 
     bool fine = true;
     for (int j = 0; j < walk.tiles; ++j, ++done) {
       const uint32_t slot = done % T::STAGES, acc = done % kAccs;
-      fine = mbar_wait_warp(smem_u32(&sm.q_full[slot]), (done / T::STAGES) & 1u, ab) && mbar_wait_warp(smem_u32(&sm.acc_empty[acc]), ((done / kAccs) & 1u) ^ 1u, ab);
+      const uint32_t parity = (done / T::STAGES) & 1u;
+      fine = mbar_wait_warp(smem_u32(&sm.q_full[slot]), parity, ab) && mbar_wait_warp(smem_u32(&sm.b_full[slot]), parity, ab) && mbar_wait_warp(smem_u32(&sm.acc_empty[acc]), ((done / kAccs) & 1u) ^ 1u, ab);
       if (!fine) break;
       tc_fence_after();
       if (on) {
@@ -334,6 +332,7 @@ __device__ __forceinline__ void add_up(const WeighArgs& w, Smem& sm, uint32_t tm
   uint32_t done = 0, items = 0;                           // tiles before this item, items
   while (walk.next(w)) {
     const SeqSpan& s = walk.span.rows;
+    const int tile_rows = tile_tokens(w) * a.group, row_first = walk.token * a.group, rows = s.n_new * a.group;
     const int key = walk.key0 + in;
     const bool books = set == 0 && walk.inside && key < s.end;
     float held = 0.f;
@@ -350,8 +349,9 @@ __device__ __forceinline__ void add_up(const WeighArgs& w, Smem& sm, uint32_t tm
       if (!mbar_wait_warp(smem_u32(&sm.acc_full[acc]), (tile / kAccs) & 1u, ab)) return;
       tc_fence_after();
       const float* below = sm.below[tile % kBelow];
-      const int rr = walk.row_first + j * kRows;
-      const bool guard = __any_sync(0xffffffffu, rr < from);
+      const int rr = row_first + j * tile_rows;
+      // rows that do not see the key, and those behind the sequence's, which are other ones'
+      const bool guard = __any_sync(0xffffffffu, rr < from) || rr + 128 > rows;
       uint64_t part[2] = {0ull, 0ull};
       uint32_t z[2][16];
       tmem_issue<16>(tmem + 128 * acc + lanes, z[0]);
@@ -378,7 +378,7 @@ __device__ __forceinline__ void add_up(const WeighArgs& w, Smem& sm, uint32_t tm
         if (guard) {
 #pragma unroll
           for (int i = 0; i < 16; ++i)
-            if (rr + 16 * c + i < from) p[i] = 0.f;
+            if (rr + 16 * c + i < from || rr + 16 * c + i >= rows) p[i] = 0.f;
         }
 #pragma unroll
         for (int i = 0; i < 16; i += 2) part[(i >> 1) & 1] = add2(part[(i >> 1) & 1], pack2(p[i], p[i + 1]));
@@ -415,8 +415,9 @@ __global__ void __launch_bounds__(kThreads, 1) weigh_prompt_kernel(const __grid_
   const int warp = threadIdx.x >> 5;
   if (threadIdx.x == 0) {
     for (int i = 0; i < T::STAGES; ++i) {
-      mbar_init(smem_u32(&sm.q_full[i]), 4);
+      mbar_init(smem_u32(&sm.q_full[i]), 1);
       mbar_init(smem_u32(&sm.q_empty[i]), 1);
+      mbar_init(smem_u32(&sm.b_full[i]), 4);
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(smem_u32(&sm.k_full[i]), 4);
@@ -435,6 +436,10 @@ __global__ void __launch_bounds__(kThreads, 1) weigh_prompt_kernel(const __grid_
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&sm.tmem)) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
+  // what the copies leave of a tile: rows of zeros
+  for (int i = (tile_tokens(w) * w.a.group * 8) + (int)threadIdx.x; i < 128 * 8; i += kThreads)
+    for (int t = 0; t < T::STAGES * (D / 64); ++t) reinterpret_cast<uint4*>(q_ring + t * (128 * 128))[i] = make_uint4(0u, 0u, 0u, 0u);
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   tc_fence_before();
   find_start(w, sm);                                      // barriers of the CTA
   tc_fence_after();
@@ -443,7 +448,8 @@ __global__ void __launch_bounds__(kThreads, 1) weigh_prompt_kernel(const __grid_
   const Abort ab{&sm.abort, w.a.dev_status};
   if (w0 < w1) {
     if (warp < 4 * kSets) add_up<T>(w, sm, tmem, w0, w1, ab);
-    else if (warp < 4 * kSets + 4) bring<T>(w, sm, k_tiles, smem_u32(q_ring), w0, w1, ab);
+    else if (warp < 4 * kSets + 4) bring<T>(w, sm, k_tiles, w0, w1, ab);
+    else if (warp == 4 * kSets + 5) copy_rows<T>(w, sm, smem_u32(q_ring), w0, w1, ab);
     else multiply<T>(w, sm, tmem, smem_u32(k_tiles), smem_u32(q_ring), w0, w1, ab);
   }
   tc_fence_before();
@@ -474,7 +480,17 @@ int32_t launch(const WeighArgs& w, int sm_count, cudaStream_t stream) {
 
 }  // namespace
 
-int32_t weigh_prompt_launch(const WeighArgs& w, int head_dim, int sm_count, cudaStream_t stream) {
+// Strides of zero, which a row or a head for all has, and of 2^40 bytes and more are not a tensor map's; neither are more than 128 heads to a
+// key head a tile's.
+bool weigh_prompt_fits(const WeighArgs& w) {
+  const RowsView& q = w.a.q;
+  const int64_t most = (int64_t)1 << 38;
+  return w.a.group <= 128 && q.stride_row > 0 && q.stride_head > 0 && q.stride_row < most && q.stride_head < most;
+}
+
+int32_t weigh_prompt_launch(WeighArgs& w, int n_q_heads, int head_dim, int sm_count, cudaStream_t stream) {
+  const int32_t st = encode_rows_map("spf_kv_weigh", w.a.q, w.a.step.n_rows, n_q_heads, head_dim, 128 / w.a.group, w.a.group, &w.q_map);
+  if (st != SPF_OK) return st;
   const bool d64 = head_dim == 64;
   switch (w.a.kv.bits) {
     case 4: return d64 ? launch<64, 4>(w, sm_count, stream) : launch<128, 4>(w, sm_count, stream);
