@@ -4,7 +4,7 @@
 //
 // A weight is one product of D dimensions and one exponential, and the exponentials bound it: 128 keys by 128 rows take the exponential unit
 // 1024 cycles, the tensor cores 128 (64 dimensions) or 256.  So the products are the big instruction's, into tensor memory, with keys as the 128
-// lanes and rows as the columns: a thread of the two sets of four warps that take the exponentials has one key, whose weights it adds up in a
+// lanes and rows as the columns: a thread of the four sets of four warps that take the exponentials has one key, whose weights it adds up in a
 // register over all rows, with no exchange between threads; per exponential it spends half a multiply-add, half an addition and a quarter of a
 // read of log-sum-exps from shared memory.  (Warp-level products, keys in registers, took 648 us where this takes 290: two units in turns in
 // each of few warps.)  Sums of a tile are added with what the additions lose (thousands of rows make 1.7e-6 of a weight otherwise).
@@ -24,7 +24,7 @@
 namespace spf {
 namespace {
 
-constexpr int kSets = 2, kThreads = (4 * kSets + 6) * 32, kKeys = 128, kEnds = 2;
+constexpr int kSets = 4, kThreads = (4 * kSets + 6) * 32, kKeys = 128, kEnds = 4;
 constexpr int kAccs = 4, kBelow = 16;                     // accumulators in tensor memory; tiles whose log-sum-exps are kept: more than may be under way
 
 template <int D_, int BITS_>
