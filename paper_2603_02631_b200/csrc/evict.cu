@@ -118,23 +118,29 @@ __global__ void __launch_bounds__(kRankThreads) rank_kernel(const __grid_constan
     const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
     auto count = [&](int i, const uint4& four) {
       const uint32_t r[4] = {four.x, four.y, four.z, four.w};
+      uint32_t bin[4];
+      bool counts[4], all = true;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const bool counts = i + j < hi && (pass == 0 || (r[j] >> (shift + bits)) == prefix);
-        const uint32_t bin = (r[j] >> shift) & ((1u << bits) - 1u), mask = __ballot_sync(0xffffffffu, counts);
-        if (mask == 0) continue;
-        // many equal weights would be as many additions to one counter
-        const uint32_t first = __shfl_sync(0xffffffffu, bin, __ffs((int)mask) - 1);
-        if (__all_sync(0xffffffffu, !counts || bin == first)) {
-          if (lane == 0) atomicAdd(&sm.bins[pass][first], (uint32_t)__popc(mask));
-        } else if (counts) {
-          atomicAdd(&sm.bins[pass][bin], 1u);
-        }
+        counts[j] = i + j < hi && (pass == 0 || (r[j] >> (shift + bits)) == prefix);
+        bin[j] = (r[j] >> shift) & ((1u << bits) - 1u);
+        all = all && counts[j] && bin[j] == bin[0];
+      }
+      // equal weights would be as many additions to one counter
+      const uint32_t first = __shfl_sync(0xffffffffu, bin[0], 0);        // of every lane, not in a condition that some skip
+      if (__all_sync(0xffffffffu, all && bin[0] == first)) {
+        if (lane == 0) atomicAdd(&sm.bins[pass][bin[0]], 128u);
+      } else if (all) {
+        atomicAdd(&sm.bins[pass][bin[0]], 4u);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (counts[j]) atomicAdd(&sm.bins[pass][bin[j]], 1u);
       }
     };
     if (pass == 0) {
-      // loads of two chunks in flight
-      constexpr int kAhead = 2;
+      // loads of four chunks in flight
+      constexpr int kAhead = 4;
       for (int i0 = lo + warp * 128; i0 < hi; i0 += kAhead * kRankThreads * 4) {
         uint4 four[kAhead];
 #pragma unroll
@@ -244,11 +250,10 @@ __global__ void __launch_bounds__(kRankThreads) rank_kernel(const __grid_constan
     const uint32_t r[4] = {four.x, four.y, four.z, four.w};
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      if (i + j >= to || r[j] < prefix) continue;
-      const bool more = r[j] > prefix;
-      if (more || e < take) list[u + min(e, take)] = i + j;
-      if (more) ++u;
-      else ++e;
+      const bool more = i + j < to && r[j] > prefix, same = i + j < to && r[j] == prefix;
+      if (more || (same && e < take)) list[u + min(e, take)] = i + j;
+      u += more ? 1u : 0u;
+      e += same ? 1u : 0u;
     }
     const uint32_t all = __shfl_sync(0xffffffffu, upto, 31);
     above += all & 0xffffu, equal += all >> 16;
