@@ -168,35 +168,53 @@ __device__ __forceinline__ uint32_t mul_bf16(uint32_t a, uint32_t b) {
   return r;
 }
 
-// Eight elements of a key from dimension 8 j on as bf16 pairs; `row` is the key's row in the pool.
+// Eight elements of a key from dimension 8 j on as the cache has them (`row`: the key's row in the pool), and as bf16 pairs.
 template <class T>
-__device__ __forceinline__ void load_eight(const KvView& kv, int64_t row, int j, uint32_t (&r)[4]) {
-  if constexpr (T::BITS == 16) {
-    const uint4 v = __ldg(reinterpret_cast<const uint4*>(kv.k + row * (2 * T::D)) + j);
-    r[0] = v.x, r[1] = v.y, r[2] = v.z, r[3] = v.w;
-  } else if constexpr (T::BITS == 8) {
-    const uint2 v = __ldg(reinterpret_cast<const uint2*>(kv.k + row * T::D) + j);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint32_t word = i < 2 ? v.x : v.y, two = __byte_perm(word, 0, i & 1 ? 0x4342 : 0x4140);
-      // a byte s eeee mmm at the bits s 0000eeee mmm0000 is its value times 2^-120
-      r[i] = mul_bf16(((two << 8) & 0x80008000u) | ((two << 4) & 0x07f007f0u), 0x7b807b80u);
-      if ((((two & 0x007f007fu) + 0x00010001u) & 0x00800080u) != 0) {
-        if ((two & 0x7fu) == 0x7fu) r[i] |= 0x00007fffu;
-        if ((two & 0x7f0000u) == 0x7f0000u) r[i] |= 0x7fff0000u;
-      }
-    }
-  } else {
-    const uint32_t word = __ldg(reinterpret_cast<const uint32_t*>(kv.k + row * (T::D / 2)) + j);
-    const uint32_t s = __ldg(kv.k_scale4 + row * (T::D / kScaleDims) + j / 4), both = s | s << 16, less = mul_bf16(both, 0xc1c0c1c0u);   // -24 scales
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint32_t two = word >> (8 * i);
-      r[i] = ((two & 0xfu) << 3) | ((two & 0xf0u) << 15) | 0x41804180u;                                                        // 16 + code
-      asm("fma.rn.bf16x2 %0, %0, %1, %2;" : "+r"(r[i]) : "r"(both), "r"(less));
+struct Eight {
+  uint32_t raw[T::BITS / 4];
+  uint32_t scale;                                         // 4 bits
+
+  __device__ __forceinline__ void load(const KvView& kv, int64_t row, int j) {
+    if constexpr (T::BITS == 16) {
+      const uint4 v = __ldg(reinterpret_cast<const uint4*>(kv.k + row * (2 * T::D)) + j);
+      raw[0] = v.x, raw[1] = v.y, raw[2] = v.z, raw[3] = v.w;
+    } else if constexpr (T::BITS == 8) {
+      const uint2 v = __ldg(reinterpret_cast<const uint2*>(kv.k + row * T::D) + j);
+      raw[0] = v.x, raw[1] = v.y;
+    } else {
+      raw[0] = __ldg(reinterpret_cast<const uint32_t*>(kv.k + row * (T::D / 2)) + j);
+      scale = __ldg(kv.k_scale4 + row * (T::D / kScaleDims) + j / 4);
     }
   }
-}
+  __device__ __forceinline__ uint4 widen() const {
+    uint32_t r[4];
+    if constexpr (T::BITS == 16) {
+      return make_uint4(raw[0], raw[1], raw[2], raw[3]);
+    } else if constexpr (T::BITS == 8) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t two = __byte_perm(raw[i / 2], 0, i & 1 ? 0x4342 : 0x4140);
+        // a byte s eeee mmm at the bits s 0000eeee mmm0000 is its value times 2^-120
+        r[i] = mul_bf16(((two << 8) & 0x80008000u) | ((two << 4) & 0x07f007f0u), 0x7b807b80u);
+      }
+      if (((((raw[0] & 0x7f7f7f7fu) + 0x01010101u) | ((raw[1] & 0x7f7f7f7fu) + 0x01010101u)) & 0x80808080u) != 0) {
+        // NaN, which looks like 480
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (((raw[i / 4] >> (8 * (i & 3))) & 0x7fu) == 0x7fu) r[i / 2] |= 0x7fffu << (16 * (i & 1));
+      }
+    } else {
+      const uint32_t both = scale | scale << 16, less = mul_bf16(both, 0xc1c0c1c0u);                                          // -24 scales
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t two = raw[0] >> (8 * i);
+        r[i] = ((two & 0xfu) << 3) | ((two & 0xf0u) << 15) | 0x41804180u;                                                      // 16 + code
+        asm("fma.rn.bf16x2 %0, %0, %1, %2;" : "+r"(r[i]) : "r"(both), "r"(less));
+      }
+    }
+    return make_uint4(r[0], r[1], r[2], r[3]);
+  }
+};
 
 // ---------------------------------------------------------------------------------------------- keys and rows into shared memory
 // The copying thread: a tile of rows is a box of the queries, spans of 64 dimensions x heads of the group x tokens.
@@ -245,12 +263,15 @@ __device__ __forceinline__ void bring(const WeighArgs& w, Smem& sm, unsigned cha
     const uint32_t buf = items & 1u;
     if (!mbar_wait_warp(smem_u32(&sm.k_empty[buf]), ((items >> 1) & 1u) ^ 1u, ab)) return;
     unsigned char* k_tile = k_tiles + buf * T::TILE;
-#pragma unroll 4
-    for (int i = 0; i < 128 / kLines; ++i) {
-      const int in = first + i * kLines;
-      uint32_t r[4] = {0u, 0u, 0u, 0u};
-      if (walk.inside) load_eight<T>(a.kv, (int64_t)walk.pool_at + in, chunk, r);
-      *reinterpret_cast<uint4*>(k_tile + tile_chunk(in, chunk)) = make_uint4(r[0], r[1], r[2], r[3]);
+    constexpr int kBatch = 8;                             // loads in flight
+#pragma unroll 1
+    for (int i0 = 0; i0 < 128 / kLines; i0 += kBatch) {
+      Eight<T> eight[kBatch] = {};
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i)
+        if (walk.inside) eight[i].load(a.kv, (int64_t)walk.pool_at + first + (i0 + i) * kLines, chunk);
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) *reinterpret_cast<uint4*>(k_tile + tile_chunk(first + (i0 + i) * kLines, chunk)) = eight[i].widen();
     }
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     __syncwarp();
