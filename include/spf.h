@@ -12,7 +12,8 @@
  *   spf_compact_spans  Section 3.2 / Algorithm 1 "MergeAdjacentChunks" + "MapDraftChunksToTextSpans".
  *
  * Before them, on the draft model's side: spf_kv_append (rotates a step's queries and keys and writes a paged cache) and
- * spf_attend (the step's attention over it).  Around them: spf_keep_count / spf_keep_rate / spf_snap_budget (Section 3.1, keep rate) and spf_concat_with_delim
+ * spf_attend (the step's attention over it); spf_kv_weigh and spf_kv_evict (received attention weights, and cuts of the cache to a
+ * budget by them).  Around them: spf_keep_count / spf_keep_rate / spf_snap_budget (Section 3.1, keep rate) and spf_concat_with_delim
  * (Algorithm 1 "ConcatWithDelim") on the host; spf_score_paged (paged key cache), spf_score_fp8 (8-bit key cache), spf_score_paged_fp8 (both),
  * spf_score_shard_lse /
  * spf_score_shard_apply (one prompt's keys over several GPUs); spf_score_extra, spf_chunk_pool_edge,

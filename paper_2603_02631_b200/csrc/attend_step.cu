@@ -1,4 +1,4 @@
-// Attention of a step with few rows per key head (single tokens, lookahead tokens) over the paged cache, bf16 or 8 bits.
+// Attention of a step with few rows per key head (single tokens, lookahead tokens) over the paged cache, bf16, 8 or 4 bits.
 //
 //   z[r, s] = c q[r] . k[s]  (base-2 logits),   out[r] = sum_s 2^(z[r,s] - m_r) v[s] / l_r,   l_r = sum_s 2^(z[r,s] - m_r),
 //   lse[r] = (m_r + log2 l_r) ln 2;   rows r = (new token i, head g of the key head's group), r = i G + g, in tiles of R.
@@ -31,6 +31,15 @@
 // weights are p s_v / (the largest such so far) and never leave fp16's range; their sum l has a reference of its own (RowStats):
 //   z'[r,s] = z[r,s] + log2 s_v,  w = 2^(z' - m'),  l = sum 2^(z - m),  out = 2^(m' - m) sum w byte / l,  lse = (m + log2 l) ln 2.
 // m' lies 7 below the largest z' seen (but for the 8 above), which leaves small weights more of fp16's range.
+//
+// 4 bits: an element is s (code - 8), a scale for 32 dimensions of a token.  Widening them would take more instructions than the read of half as many
+// bytes leaves room for, so codes are multiplied without being converted: the four bits of a code in the lowest (or the next) four of a bf16 number's
+// are code 2^-133 (16 times that), a subnormal number, which the products take exactly; one instruction makes two of them.  The 8 is taken
+// off the sums: of 32 keys' elements by where the sum starts, of values by a product with eights in the codes' places.  Scales of keys multiply
+// the sums of their 32 dimensions, those of values the weights.  Powers of two in the queries, and in the reference of the weights, which
+// lies 2^64 below the largest, keep all sums in fp32's normal range.  32 sequences of up to 16k tokens, 8 heads of 128 dimensions, one token each:
+// 77 us, where the bytes take 49 (8 bits: 111, 88), and 58 without products; four of 131 to 250 thousand 189 (150).  What the rest goes to: the
+// chain of a warp's tile, of which three a scheduler run at a time at 128 registers (four at 96 spill: 93 us).
 //
 // Keys that no row may see (behind the sequence's end, before its first key) take part with logits of -inf and values of zero,
 // whatever the pool holds there.  Keys that only later rows of the step may see have weight zero; if their values are not
@@ -310,8 +319,8 @@ __device__ __forceinline__ void multiply_codes(State<T>& st, uint32_t w0, uint32
 // the weights, and 8 times the sum of these is subtracted at the triple's end.  x[kt][nt][h]: the weights in fp32.
 //
 // Weights are rounded to bf16 and turned as they are, once for all scales, and multiplied by pairs of scales as bf16 pairs, which rounds them
-// again (both together off by up to 2^-8); scaled in fp32 first, each scale would have a rounding, a packing and a turn of its own (86 us
-// instead of 79 for 32 sequences of up to 16k tokens).  Where some keys are not seen by some rows (add_some_codes) that is what is done:
+// again (both together off by up to 2^-8); scaled in fp32 first, each scale would have a rounding, a packing and a turn of its own, 28
+// instructions a sixteen of keys more.  Where some keys are not seen by some rows (add_some_codes) that is what is done:
 // values of keys that a row does not see count as zeros, whatever their scales.
 template <class T>
 __device__ __forceinline__ void add_codes(State<T>& st, const float (&x)[T::KT][T::NT][2][2], uint32_t v_tile, uint32_t scales, int key, int lane) {

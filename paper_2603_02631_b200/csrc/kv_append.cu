@@ -291,7 +291,8 @@ __device__ __forceinline__ void move_rows(const AppendArgs& a, int cta) {
 }
 
 // The same for many rows of a 4-bit cache: a warp has a row, all of its heads, four or eight at a time, so that a token's place and angles are
-// found once (with a thread for each unit of two heads, 238 instead of 172 us for 54k tokens).  The
+// found once (with a thread for each unit of two heads, 238 instead of 172 us for 54k tokens; with a thread for each unit, as for few rows: 2048 tokens 11.4
+// instead of 8.6 us, 1024 7.1 both, 512 4.3 instead of 6.7).  The
 // next heads' loads are under way while these are made.
 template <int D>
 __device__ __forceinline__ void move_whole_rows(const AppendArgs& a, int cta) {

@@ -4,9 +4,15 @@
 //
 // One pass over the keys: a row's log-sum-exp is known (its attention came first), so a weight is final as soon as its logit is there, and tiles
 // of keys are independent of one another.  The work is the list of all key tiles of all (sequence, key head), cut into one part for each CTA.
-// Copies, products and the 4-bit and 8-bit keys' arithmetic are those of the attention for few rows; a thread's weights of a key are summed
+// Copies, products and the 4-bit keys' arithmetic are those of the attention for few rows (8-bit keys are multiplied in bf16 here); a thread's weights of a key are summed
 // over its rows, the four lanes that share a key exchange sums, and each of them books one key.  With more rows than a tile of R the tile of keys
-// stays where it is while the rows go by, up to 128 of them from shared memory.  What bounds it with few rows is the read of the keys.
+// stays where it is while the rows go by, up to 128 of them from shared memory.
+//
+// What bounds it with few rows is the read of the keys, of which it misses half: one token for each of 32 sequences of up to 16k tokens on a 4-bit
+// cache, 8 heads of 128 dimensions, takes 51 us where the bytes take 27; without any product it takes 46, with 8 us of launch and first loads.
+// (Three CTAs an SM instead of four: 71 instead of 61 us; the ledger's weights loaded when they are wanted instead of copied with the keys: 61
+// instead of 58.)  Masks stand apart from the exponentials, in a block of their own: as a condition on each they made a branch of each (95 instead of
+// 36 us for 128 rows over 32k keys of 64 dimensions, whose exponentials take 8).
 #include <algorithm>
 #include <cmath>
 
@@ -345,7 +351,12 @@ extern "C" int32_t spf_kv_weigh(const spf_kv_cache* cache, const spf_kv_step* st
   if (st != SPF_OK) return st;
   const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
   const int64_t rows = (int64_t)a.group * (w.last_rows > 0 ? std::min(w.last_rows, step->max_new) : step->max_new);
-  if (rows > 128 && weigh_prompt_fits(w)) return weigh_prompt_launch(w, n_q_heads, cache->head_dim, sm_count, stream);
+  // Both over 131072 keys and over 8 sequences of 4000, 8 key heads, first against second kernel.  128 rows: bf16 104 against 168 us and 36 against 47
+  // (64 dimensions), 185 against 192 and 58 against 52 (128); 8 bits 132 against 218, 45 against 56 and 202 against 250, 66 against 65; 4 bits 125
+  // against 188, 44 against 51, but 277 against 200, 88 against 58 with 128 dimensions, whose codes are unpacked for each 32 rows anew (64 rows:
+  // 161 against 238, 52 against 66).  256 rows: 410 against 185 (bf16, 64 dimensions) to 1027 against 217 (4 bits, 128).
+  const int64_t few = a.kv.bits == 4 && cache->head_dim == 128 ? 64 : 128;
+  if (rows > few && weigh_prompt_fits(w)) return weigh_prompt_launch(w, n_q_heads, cache->head_dim, sm_count, stream);
   const bool d64 = cache->head_dim == 64;
   switch (a.kv.bits) {
     case 4: return d64 ? launch_rows<64, 4>(w, cache, rows, sm_count, stream) : launch_rows<128, 4>(w, cache, rows, sm_count, stream);

@@ -6,10 +6,12 @@
 // 1024 cycles, the tensor cores 128 (64 dimensions) or 256.  So the products are the big instruction's, into tensor memory, with keys as the 128
 // lanes and rows as the columns: a thread of the four sets of four warps that take the exponentials has one key, whose weights it adds up in a
 // register over all rows, with no exchange between threads; per exponential it spends half a multiply-add, half an addition and a quarter of a
-// read of log-sum-exps from shared memory.  (Warp-level products, keys in registers, took 648 us where this takes 290: two units in turns in
-// each of few warps.)  Sums of a tile are added with what the additions lose (thousands of rows make 1.7e-6 of a weight otherwise).
+// read of log-sum-exps from shared memory.  Three chunks of 836 to 2001 tokens behind 1300 to 9000 (32/8 heads of 64 dimensions, 8 bits) take
+// 339 us, 222 of them exponentials; warp-level products with keys in registers took 648: two units in turns in each of few warps.  Two sets of
+// warps for the exponentials instead of four: 385; rows brought by threads instead of tensor copies: 405, log-sum-exps loaded one tile at a time:
+// 447.  Sums of a tile are added with what the additions lose (thousands of rows make 1.7e-6 of a weight otherwise).
 //
-// Keys are brought once for all rows of an item (a sequence, key head and 128 keys) and widened to bf16 on the way (exactly: 8-bit values, and
+// Keys are brought once for all rows of an item (a sequence, key head and 128 keys), eight loads in flight, and widened to bf16 on the way (exactly: 8-bit values, and
 // 4-bit codes times scales of five bits), the next item's while this one's last rows are being made.  Rows go by in tiles of as many tokens as fit whole into 128, a box of the queries each, whose
 // strides the tensor map has.
 //
