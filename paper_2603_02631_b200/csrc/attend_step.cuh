@@ -36,7 +36,9 @@ struct Traits {
   static constexpr int KW = KEYS / WK, KT = KW / 16;                  // keys of a warp in a tile, in sixteens
   static constexpr bool LEND = VALUES && R >= 16 && R * D < 4096;     // registers move between warpgroups
   static constexpr int THREADS = LEND ? 2 * kWarps * 32 : (kWarps + 1) * 32;
-  static constexpr int CTAS = R == 8 ? (VALUES ? 3 : 4) : 2;                         // per SM
+  // Per SM.  Without values, whose sums are not there: 8 rows 61 us with four, 71 with three (a token of 32 sequences, 4 bits); 128 rows 92 with
+  // three, 104 with two (131072 keys of 64 dimensions, bf16).
+  static constexpr int CTAS = R == 8 ? (VALUES ? 3 : 4) : VALUES ? 2 : 3;
   static constexpr int WTERMS = BITS == 16 && R == 8 ? 2 : 1;               // of a weight
   static constexpr bool QREGS = NT <= 2 && !(VALUES && INT4 && R * D == 1024);   // queries stay in registers, where there is room (4 bits, 128 dimensions: 77 us without, 85 with them)
   static constexpr int ROWB = D * BITS / 8, SPAN = ROWB < 128 ? ROWB : 128;

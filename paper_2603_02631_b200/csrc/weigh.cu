@@ -10,9 +10,9 @@
 //
 // What bounds it with few rows is the read of the keys, of which it misses half: one token for each of 32 sequences of up to 16k tokens on a 4-bit
 // cache, 8 heads of 128 dimensions, takes 51 us where the bytes take 27; without any product it takes 46, with 8 us of launch and first loads.
-// (Three CTAs an SM instead of four: 71 instead of 61 us; the ledger's weights loaded when they are wanted instead of copied with the keys: 61
+// (The ledger's weights loaded when they are wanted instead of copied with the keys: 61
 // instead of 58.)  Masks stand apart from the exponentials, in a block of their own: as a condition on each they made a branch of each (95 instead of
-// 36 us for 128 rows over 32k keys of 64 dimensions, whose exponentials take 8).
+// 36 us for 128 rows over 32k keys of 64 dimensions, 33 now, whose exponentials take 8).
 #include <algorithm>
 #include <cmath>
 
@@ -351,10 +351,10 @@ extern "C" int32_t spf_kv_weigh(const spf_kv_cache* cache, const spf_kv_step* st
   if (st != SPF_OK) return st;
   const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
   const int64_t rows = (int64_t)a.group * (w.last_rows > 0 ? std::min(w.last_rows, step->max_new) : step->max_new);
-  // Both over 131072 keys and over 8 sequences of 4000, 8 key heads, first against second kernel.  128 rows: bf16 104 against 168 us and 36 against 47
-  // (64 dimensions), 185 against 192 and 58 against 52 (128); 8 bits 132 against 218, 45 against 56 and 202 against 250, 66 against 65; 4 bits 125
-  // against 188, 44 against 51, but 277 against 200, 88 against 58 with 128 dimensions, whose codes are unpacked for each 32 rows anew (64 rows:
-  // 161 against 238, 52 against 66).  256 rows: 410 against 185 (bf16, 64 dimensions) to 1027 against 217 (4 bits, 128).
+  // Both over 131072 keys and over 8 sequences of 4000, 8 key heads, first against second kernel.  128 rows: bf16 92 against 168 us and 34 against 47
+  // (64 dimensions), 151 against 192 and 53 against 52 (128); 8 bits 121 against 218, 44 against 56 and 184 against 250, 65 against 65; 4 bits 124
+  // against 188, 45 against 51, but 277 against 200, 88 against 58 with 128 dimensions, whose codes are unpacked for each 32 rows anew (64 rows:
+  // 143 against 238, 50 against 66).  256 rows: 410 against 185 (bf16, 64 dimensions) to 1027 against 217 (4 bits, 128).
   const int64_t few = a.kv.bits == 4 && cache->head_dim == 128 ? 64 : 128;
   if (rows > few && weigh_prompt_fits(w)) return weigh_prompt_launch(w, n_q_heads, cache->head_dim, sm_count, stream);
   const bool d64 = cache->head_dim == 64;
