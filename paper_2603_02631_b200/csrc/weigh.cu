@@ -356,7 +356,7 @@ extern "C" int32_t spf_kv_weigh(const spf_kv_cache* cache, const spf_kv_step* st
   // against 188, 45 against 51, but 277 against 200, 88 against 58 with 128 dimensions, whose codes are unpacked for each 32 rows anew (64 rows:
   // 143 against 238, 50 against 66).  256 rows: 410 against 185 (bf16, 64 dimensions) to 1027 against 217 (4 bits, 128).
   const int64_t few = a.kv.bits == 4 && cache->head_dim == 128 ? 64 : 128;
-  if (rows > few && weigh_prompt_fits(w)) return weigh_prompt_launch(w, n_q_heads, cache->head_dim, sm_count, stream);
+  if (rows > few && weigh_prompt_prepare(w, n_q_heads, cache->head_dim)) return weigh_prompt_launch(w, cache->head_dim, sm_count, stream);
   const bool d64 = cache->head_dim == 64;
   switch (a.kv.bits) {
     case 4: return d64 ? launch_rows<64, 4>(w, cache, rows, sm_count, stream) : launch_rows<128, 4>(w, cache, rows, sm_count, stream);

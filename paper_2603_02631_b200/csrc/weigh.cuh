@@ -52,7 +52,7 @@ __device__ __forceinline__ void book(const WeighArgs& w, int64_t cell, float hel
 }
 
 // The kernel for many rows a key head and sequence; that for few is weigh.cu's own.
-bool weigh_prompt_fits(const WeighArgs& w);       // whether its copies can read the queries
-int32_t weigh_prompt_launch(WeighArgs& w, int n_q_heads, int head_dim, int sm_count, cudaStream_t stream);
+bool weigh_prompt_prepare(WeighArgs& w, int n_q_heads, int head_dim);       // false: its copies cannot read the queries
+int32_t weigh_prompt_launch(const WeighArgs& w, int head_dim, int sm_count, cudaStream_t stream);
 
 }  // namespace spf

@@ -505,15 +505,16 @@ int32_t launch(const WeighArgs& w, int sm_count, cudaStream_t stream) {
 
 // Strides of zero, which a row or a head for all has, and of 2^40 bytes and more are not a tensor map's; neither are more than 128 heads to a
 // key head a tile's.
-bool weigh_prompt_fits(const WeighArgs& w) {
+bool weigh_prompt_prepare(WeighArgs& w, int n_q_heads, int head_dim) {
   const RowsView& q = w.a.q;
   const int64_t most = (int64_t)1 << 38;
-  return w.a.group <= 128 && q.stride_row > 0 && q.stride_head > 0 && q.stride_row < most && q.stride_head < most;
+  if (w.a.group > 128 || q.stride_row <= 0 || q.stride_head <= 0 || q.stride_row >= most || q.stride_head >= most) return false;
+  const bool fine = encode_rows_map("spf_kv_weigh", q, w.a.step.n_rows, n_q_heads, head_dim, 128 / w.a.group, w.a.group, &w.q_map) == SPF_OK;
+  if (!fine) clear_error();                               // the other kernel takes them
+  return fine;
 }
 
-int32_t weigh_prompt_launch(WeighArgs& w, int n_q_heads, int head_dim, int sm_count, cudaStream_t stream) {
-  const int32_t st = encode_rows_map("spf_kv_weigh", w.a.q, w.a.step.n_rows, n_q_heads, head_dim, 128 / w.a.group, w.a.group, &w.q_map);
-  if (st != SPF_OK) return st;
+int32_t weigh_prompt_launch(const WeighArgs& w, int head_dim, int sm_count, cudaStream_t stream) {
   const bool d64 = head_dim == 64;
   switch (w.a.kv.bits) {
     case 4: return d64 ? launch<64, 4>(w, sm_count, stream) : launch<128, 4>(w, sm_count, stream);

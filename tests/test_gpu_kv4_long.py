@@ -124,11 +124,14 @@ def test_received_weights_of_the_other_formats(Hq, Hkv, d, block, old, new, bits
 
 @pytest.mark.parametrize("bits", [16, 8, 4])
 def test_queries_with_rows_or_heads_for_all(bits):
-    """Strides of zero: one row for every token, one head for every head; with many rows these are not what a copy of a box can read."""
+    """Strides of zero (one row for every token, one head for every head; with many rows these are not what a copy of a box can read), rows that
+    overlap, and heads outside."""
     import paper_2603_02631_b200 as spf
     s = gpu_step4(8, 2, 64, 256, [500], [90], bits, seed=1)
     lse = torch.full((s.rows, 8), 2.0, device="cuda")
-    for q in (s.q[:1].expand(90, 8, 64), s.q[:, :1].expand(90, 8, 64)):
+    flat = s.q.contiguous().flatten()
+    for q in (s.q[:1].expand(90, 8, 64), s.q[:, :1].expand(90, 8, 64), flat.as_strided((90, 8, 64), (8, 64, 1)), flat.as_strided((90, 8, 64), (64, 16, 1)),
+              s.q.transpose(0, 1).contiguous().transpose(0, 1)):
         got = []
         for x in (q, q.contiguous()):
             weight = torch.zeros(s.k_pool.shape[:3], device="cuda")
