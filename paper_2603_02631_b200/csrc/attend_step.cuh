@@ -144,7 +144,8 @@ struct QueryNotes {
   float base[T::INT4 ? T::PARTS : 1][T::R];              // 4 bits: -8 2^-133 times the sum of 32 scaled elements
 };
 
-// The triple's query rows into shared memory, rows that do not exist as zeros.  8 bits: the two terms, one tile behind the other.  4
+// The triple's query rows into shared memory, rows that do not exist as zeros (without values, whose weights are added up over rows: as the last
+// one).  8 bits: the two terms, one tile behind the other.  4
 // bits: scaled by 2^e, eight elements in the order 0 4 2 6 1 5 3 7 in which codes come out of a word, the latter four by 1/16 of that; 8 bits in
 // bf16: scaled too, four elements in the order 0 2 1 3 in which bytes do.
 template <class T>
@@ -152,7 +153,7 @@ __device__ __forceinline__ void load_queries(const AttendArgs& a, const TileDesc
   constexpr int kLanes = T::D / 8;                       // threads of a row
   const int total = d.n_new * a.group;
   for (int item = threadIdx.x; item < T::R * kLanes; item += kWarps * 32) {
-    const int r = item / kLanes, part = item % kLanes, rr = d.row_tile * T::R + r;
+    const int r = item / kLanes, part = item % kLanes, rr = T::VALUES ? d.row_tile * T::R + r : min(d.row_tile * T::R + r, total - 1);
     const __nv_bfloat16* src = a.q.data + (int64_t)(d.row0 + rr / a.group) * a.q.stride_row + (int64_t)(d.head * a.group + rr % a.group) * a.q.stride_head;
     union { uint4 u; __nv_bfloat162 h[4]; } v;
     v.u = make_uint4(0, 0, 0, 0);

@@ -151,6 +151,15 @@ __device__ __forceinline__ void copy_keys(const WeighArgs& w, WeighSmem<T>& sm, 
   }
 }
 
+// Base-2 log-sum-exp of the row `row` of `total` that a sequence has for a key head, -inf for one that saw no key, whose weights are set to zero.
+// A tile is filled up with copies of the last row (load_queries), which sees every key that any row does, and the largest number as their
+// log-sum-exp: a copy adds 0, or the infinity or NaN that the row itself adds.  (Zeros in their place make NaN of a key with an infinite element.)
+__device__ __forceinline__ float row_lse2(const AttendArgs& a, const WeighDesc& d, int row, int total) {
+  const int r = min(row, total - 1);
+  const float lse = __ldg(a.lse + (int64_t)(d.row0 + r / a.group) * a.lse_stride_row + (int64_t)(d.head * a.group + r % a.group) * a.lse_stride_head);
+  return row < total || lse == -INFINITY ? lse * kLog2e : 3.402823466e38f;
+}
+
 template <class T>
 __device__ __forceinline__ void weigh_tiles_of_cta(const WeighArgs& w, WeighSmem<T>& sm, uint32_t ring, unsigned char* q_tile, int64_t n_tiles, const Abort& ab) {
   constexpr int R = T::R, NT = T::NT, KT = T::KT;
@@ -163,6 +172,7 @@ __device__ __forceinline__ void weigh_tiles_of_cta(const WeighArgs& w, WeighSmem
   __shared__ float lse2[kHeld][R];
   Queries<T> queries;
   float below[NT][2];                                    // the rows' log-sum-exps
+  uint32_t idle = 0;                                     // tiles of rows, of those held, with some that saw no key
   int first_token = 0, last_token = 0;                   // of the rows of the tile
   int stage = 0;
   uint32_t parity = 0, join_parity = 0;
@@ -195,12 +205,12 @@ __device__ __forceinline__ void weigh_tiles_of_cta(const WeighArgs& w, WeighSmem
           TileDesc t;
           t.row0 = d.row0, t.n_new = d.n_new, t.head = d.head, t.row_tile = rt + i;
           load_queries<T>(a, t, q_tile + i * T::QBYTES, notes[i]);
-          for (int r = threadIdx.x; r < R; r += kWarps * 32) {
-            const int rr = (rt + i) * R + r;
-            lse2[i][r] = row_lse2(a, d.row0 + rr / a.group, d.head * a.group + rr % a.group, rr < d.n_new * a.group);
-          }
+          for (int r = threadIdx.x; r < R; r += kWarps * 32) lse2[i][r] = row_lse2(a, d, (rt + i) * R + r, d.n_new * a.group);
         }
         if (!join()) return;
+        idle = 0;
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i) idle |= __any_sync(0xffffffffu, lse2[i][lane % R] == -INFINITY) ? 1u << i : 0u;
       }
       if (d.new_rows || row_tiles > 1) {
         queries.load(q_addr + slot * T::QBYTES, notes[slot], 0, lane);
@@ -226,6 +236,15 @@ __device__ __forceinline__ void weigh_tiles_of_cta(const WeighArgs& w, WeighSmem
         for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
           for (int e = 0; e < 4; ++e) z[kt][nt][e] = fast_exp2(fmaf(z[kt][nt][e], f[e & 1], -below[nt][e & 1]));
+      }
+      if ((idle >> slot & 1u) != 0) {
+        // by selection, whatever their products are
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) z[kt][nt][e] = below[nt][e & 1] == -INFINITY ? 0.f : z[kt][nt][e];
       }
       if (guard) {
 #pragma unroll

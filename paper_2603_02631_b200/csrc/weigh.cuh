@@ -33,13 +33,6 @@ __device__ __forceinline__ WeighSpan weigh_span(const WeighArgs& w, int b) {
   return s;
 }
 
-// Base-2 log-sum-exp of a row, +inf (which makes every weight zero) for rows that do not exist or saw no key.
-__device__ __forceinline__ float row_lse2(const AttendArgs& a, int row, int head, bool exists) {
-  if (!exists) return INFINITY;
-  const float lse = __ldg(a.lse + (int64_t)row * a.lse_stride_row + (int64_t)head * a.lse_stride_head);
-  return lse == -INFINITY ? INFINITY : lse * kLog2e;
-}
-
 // What a key has received: `got` joins what the ledger holds, or replaces it where the token is one of the step's.
 __device__ __forceinline__ void book(const WeighArgs& w, int64_t cell, float held, float got, int key, int fresh, int fresh_row) {
   if (key < fresh) {
