@@ -42,6 +42,7 @@ struct Smem {
   int64_t total, start_base;
   int start_seq;
   int abort;
+  int idle;                                             // some row of the CTA's saw no key
   uint32_t tmem;
 };
 
@@ -286,7 +287,7 @@ __device__ __forceinline__ void bring(const WeighArgs& w, Smem& sm, unsigned cha
       float own[kAhead];
 #pragma unroll
       for (int i = 0; i < kAhead; ++i) {
-        own[i] = own_token < tokens && token < s.n_new ? __ldg(lse) : -INFINITY;   // rows that do not exist, or saw no key: nothing
+        own[i] = own_token < tokens && token < s.n_new ? __ldg(lse) : INFINITY;    // columns without a row: nothing
         token += tokens;
         lse += step;
       }
@@ -295,7 +296,8 @@ __device__ __forceinline__ void bring(const WeighArgs& w, Smem& sm, unsigned cha
         if (j0 + i >= walk.tiles) break;
         const uint32_t slot = done % T::STAGES;
         if (!mbar_wait_warp(smem_u32(&sm.q_empty[slot]), ((done / T::STAGES) & 1u) ^ 1u, ab)) return;
-        sm.below[done % kBelow][thread] = own[i] == -INFINITY ? -INFINITY : -own[i] * kLog2e;
+        sm.below[done % kBelow][thread] = -own[i] * kLog2e;
+        if (own[i] == -INFINITY) sm.idle = 1;
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&sm.b_full[slot]));
         ++done;
@@ -376,35 +378,65 @@ __device__ __forceinline__ void add_up(const WeighArgs& w, Smem& sm, uint32_t tm
       // rows that do not see the key, and those behind the sequence's, which are other ones'
       const bool guard = __any_sync(0xffffffffu, rr < from) || rr + 128 > rows;
       uint64_t part[2] = {0ull, 0ull};
-      uint32_t z[2][16];
-      tmem_issue<16>(tmem + 128 * acc + lanes, z[0]);
+      if (*const_cast<const volatile int*>(&sm.idle) != 0) {
+        // Rows that saw no key add nothing, by selection, whatever their products are: apart from what follows, to which this added a twentieth.  Either
+        // gives other tiles the same bits, so that it does not matter when the flag is seen there.
+#pragma unroll 1
+        for (int c = 0; c < 8; ++c) {
+          uint32_t z[16];
+          tmem_issue<16>(tmem + 128 * acc + lanes + 16 * c, z);
+          tmem_load_wait();
+          tmem_ready<16>(z);
 #pragma unroll
-      for (int c = 0; c < 8; ++c) {
-        tmem_load_wait();
-        tmem_ready<16>(z[c & 1]);
-        if (c < 7) {
-          tmem_issue<16>(tmem + 128 * acc + lanes + 16 * (c + 1), z[(c + 1) & 1]);
-        } else {
-          tc_fence_before();                              // the accumulator is in registers
-          __syncwarp();
-          if (lane == 0) mbar_arrive(smem_u32(&sm.acc_empty[acc]));
+          for (int i = 0; i < 16; i += 2) {
+            float p[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const int column = 16 * c + i + e;
+              const float b = below[column];
+              p[e] = fast_exp2(fmaf(__uint_as_float(z[i + e]), f, b));
+              if (rr + column < from || rr + column >= min(rows, rr + tile_rows) || b == INFINITY) p[e] = 0.f;
+            }
+            part[(i >> 1) & 1] = add2(part[(i >> 1) & 1], pack2(p[0], p[1]));
+          }
         }
-        float p[16];
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&sm.acc_empty[acc]));
+      } else {
+        uint32_t z[2][16];
+        tmem_issue<16>(tmem + 128 * acc + lanes, z[0]);
 #pragma unroll
-        for (int i = 0; i < 16; i += 4) {
-          const float4 b = *reinterpret_cast<const float4*>(below + 16 * c + i);
-          unpack2(fma2(pack2(z[c & 1][i], z[c & 1][i + 1]), ff, pack2(b.x, b.y)), p[i], p[i + 1]);
-          unpack2(fma2(pack2(z[c & 1][i + 2], z[c & 1][i + 3]), ff, pack2(b.z, b.w)), p[i + 2], p[i + 3]);
+        for (int c = 0; c < 8; ++c) {
+          tmem_load_wait();
+          tmem_ready<16>(z[c & 1]);
+          if (c < 7) {
+            tmem_issue<16>(tmem + 128 * acc + lanes + 16 * (c + 1), z[(c + 1) & 1]);
+          } else {
+            tc_fence_before();                              // the accumulator is in registers
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&sm.acc_empty[acc]));
+          }
+          float p[16];
+#pragma unroll
+          for (int i = 0; i < 16; i += 4) {
+            const float4 b = *reinterpret_cast<const float4*>(below + 16 * c + i);
+            unpack2(fma2(pack2(z[c & 1][i], z[c & 1][i + 1]), ff, pack2(b.x, b.y)), p[i], p[i + 1]);
+            unpack2(fma2(pack2(z[c & 1][i + 2], z[c & 1][i + 3]), ff, pack2(b.z, b.w)), p[i + 2], p[i + 3]);
+          }
+#pragma unroll
+          for (int i = 0; i < 16; ++i) p[i] = fast_exp2(p[i]);
+          // Columns behind a tile's last whole token are zeros there, which a key with an infinite element makes NaN of: the last of these 16, if any
+          // is one, shows it.
+          if (guard || __any_sync(0xffffffffu, p[15] != p[15])) {
+            const int last = min(rows, rr + tile_rows);
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+              if (rr + 16 * c + i < from || rr + 16 * c + i >= last) p[i] = 0.f;
+          }
+#pragma unroll
+          for (int i = 0; i < 16; i += 2) part[(i >> 1) & 1] = add2(part[(i >> 1) & 1], pack2(p[i], p[i + 1]));
         }
-#pragma unroll
-        for (int i = 0; i < 16; ++i) p[i] = fast_exp2(p[i]);
-        if (guard) {
-#pragma unroll
-          for (int i = 0; i < 16; ++i)
-            if (rr + 16 * c + i < from || rr + 16 * c + i >= rows) p[i] = 0.f;
-        }
-#pragma unroll
-        for (int i = 0; i < 16; i += 2) part[(i >> 1) & 1] = add2(part[(i >> 1) & 1], pack2(p[i], p[i + 1]));
       }
       float u, v;
       unpack2(add2(part[0], part[1]), u, v);
@@ -453,6 +485,7 @@ __global__ void __launch_bounds__(kThreads, 1) weigh_prompt_kernel(const __grid_
     mbar_init(smem_u32(&sm.summed), 4 * kSets);
     mbar_init(smem_u32(&sm.mma_done), 1);
     sm.abort = 0;
+    sm.idle = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 4 * kSets + 4) {

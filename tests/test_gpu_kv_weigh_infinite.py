@@ -65,3 +65,29 @@ def test_a_row_that_saw_no_key_adds_nothing_to_keys_that_are_not_numbers():
         weigh(spf, s, lse, weight, None, decay=0.5)
         block = int(s.table[0, 0])
         assert torch.equal(weight[block, :, :100], before[block, :, :100] * 0.5) and (weight[block, :, 100:100 + new] == 0).all()
+
+
+@pytest.mark.parametrize("Hq,Hkv", [(3, 1), (10, 2), (6, 1), (7, 1), (9, 1), (70, 1)])
+@pytest.mark.parametrize("last", [0, 50])
+def test_many_rows_of_heads_that_do_not_fill_a_tile(Hq, Hkv, last):
+    """128 rows of a tile are as many tokens as fit whole: 3, 5, 6 ... heads leave columns without a row in each."""
+    import paper_2603_02631_b200 as spf
+    for d in (64, 128):
+        check(spf, infinite_step(Hq, Hkv, d, 128, [200, 5], [170, 65], d), 16, decay=0.5, last=last)
+
+
+def test_many_rows_of_which_some_saw_no_key():
+    """As test_a_row_that_saw_no_key_adds_nothing_to_keys_that_are_not_numbers, in a chunk: keys 40 and 41 are seen by rows without keys only."""
+    import paper_2603_02631_b200 as spf
+    s = make_step(4, 2, 64, 128, [100], [130], 16, 7)
+    s.k_pool[int(s.table[0, 0]), :, 40, 3], s.k_pool[int(s.table[0, 0]), :, 41, 3] = math.nan, math.inf
+    lse = torch.full((s.rows, 4), -math.inf, device="cuda")
+    weight, _ = ledger_of(s, 5)
+    before = weight.clone()
+    weigh(spf, s, lse, weight, None, decay=0.5)
+    block, second = int(s.table[0, 0]), int(s.table[0, 1])
+    assert torch.equal(weight[block, :, :100], before[block, :, :100] * 0.5) and (weight[block, :, 100:] == 0).all() and (weight[second, :, :102] == 0).all()
+
+
+def test_attention_of_a_chunk_and_what_follows_it():
+    assert attend_and_weigh(6, 2, 100) == [True] * 3
