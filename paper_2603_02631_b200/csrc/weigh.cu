@@ -22,6 +22,11 @@
 namespace spf {
 namespace {
 
+// Tiles of rows whose weights are added up plainly: up to 128 rows, for which the kernel is meant, have four.  With more (a hint that is too small,
+// rows that the other kernel does not take) sums carry what each addition loses, in a kernel of its own (MANY): there are no registers to spare for it
+// (a token of 32 sequences, 4 bits, 52.6 us instead of 51.2).
+constexpr int kPlain = 8;
+
 // What the copying warp tells the computing ones about a stage.
 struct WeighDesc {
   int row0, n_new, pos0, first, end, head, key0, fresh, fresh_row;
@@ -160,7 +165,7 @@ __device__ __forceinline__ float row_lse2(const AttendArgs& a, const WeighDesc& 
   return row < total || lse == -INFINITY ? lse * kLog2e : 3.402823466e38f;
 }
 
-template <class T>
+template <class T, bool MANY>
 __device__ __forceinline__ void weigh_tiles_of_cta(const WeighArgs& w, WeighSmem<T>& sm, uint32_t ring, unsigned char* q_tile, int64_t n_tiles, const Abort& ab) {
   constexpr int R = T::R, NT = T::NT, KT = T::KT;
   static_assert(T::WR == 1 && KT <= 2);
@@ -193,7 +198,7 @@ __device__ __forceinline__ void weigh_tiles_of_cta(const WeighArgs& w, WeighSmem
     const bool writes = books && d.cell >= 0 && own_key < end;
     const int64_t cell = (int64_t)d.cell + own;
     const int row_tiles = (int)(((int64_t)d.n_new * a.group + R - 1) / R);
-    float got[KT][2] = {};
+    float got[KT][2] = {}, lost[MANY ? KT : 1][2] = {};   // sums over tiles of rows, and what their additions lose
     for (int rt = 0; rt < row_tiles; ++rt) {
       const int slot = rt % kHeld;
       if (slot == 0 && (d.new_rows || row_tiles > kHeld)) {
@@ -261,12 +266,23 @@ __device__ __forceinline__ void weigh_tiles_of_cta(const WeighArgs& w, WeighSmem
                 if (row_first + nt * 8 + 2 * (lane & 3) + e < from) z[kt][nt][2 * h + e] = 0.f;
           }
       }
+      float part[KT][2] = {};
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
-          for (int h = 0; h < 2; ++h) got[kt][h] += z[kt][nt][2 * h] + z[kt][nt][2 * h + 1];
+          for (int h = 0; h < 2; ++h) (MANY ? part : got)[kt][h] += z[kt][nt][2 * h] + z[kt][nt][2 * h + 1];
+      if constexpr (MANY) {
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const float y = __fsub_rn(part[kt][h], lost[kt][h]), t = __fadd_rn(got[kt][h], y);
+            lost[kt][h] = __fsub_rn(__fsub_rn(t, got[kt][h]), y);
+            got[kt][h] = t;
+          }
+      }
     }
     // sums over the four lanes of a key, each of which ends with one key's
     float sum;
@@ -287,7 +303,7 @@ __device__ __forceinline__ void weigh_tiles_of_cta(const WeighArgs& w, WeighSmem
   }
 }
 
-template <class T>
+template <class T, bool MANY>
 __global__ void __launch_bounds__(T::THREADS, T::CTAS) weigh_step_kernel(const __grid_constant__ WeighArgs w) {
   extern __shared__ unsigned char smem_raw[];
   unsigned char* ring_ptr = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
@@ -306,30 +322,36 @@ __global__ void __launch_bounds__(T::THREADS, T::CTAS) weigh_step_kernel(const _
   const int64_t total = sm.total, per = (total + gridDim.x - 1) / gridDim.x, w0 = per * blockIdx.x, w1 = min(w0 + per, total);
   if (w0 >= w1) return;
   const Abort ab{&sm.abort, w.a.dev_status};
-  if (threadIdx.x < kWarps * 32) weigh_tiles_of_cta<T>(w, sm, smem_u32(ring_ptr), q_tile, w1 - w0, ab);
+  if (threadIdx.x < kWarps * 32) weigh_tiles_of_cta<T, MANY>(w, sm, smem_u32(ring_ptr), q_tile, w1 - w0, ab);
   else copy_keys<T>(w, sm, smem_u32(ring_ptr), w0, w1, ab);
 }
 
-template <int D, int BITS, int R>
-int32_t launch_weigh(WeighArgs& w, const spf_kv_cache* cache, int sm_count, cudaStream_t stream) {
-  using T = Traits<D, BITS, R, false>;
+template <class T, bool MANY>
+int32_t launch_kernel(const WeighArgs& w, int sm_count, cudaStream_t stream) {
   static ContextSet done;
+  const int32_t st = allow_shared_memory(reinterpret_cast<const void*>(weigh_step_kernel<T, MANY>), weigh_smem_bytes<T>(), done);
+  if (st != SPF_OK) return st;
+  weigh_step_kernel<T, MANY><<<sm_count * T::CTAS, T::THREADS, weigh_smem_bytes<T>(), stream>>>(w);
+  SPF_CUDA_CHECK(cudaGetLastError());
+  return SPF_OK;
+}
+// `most`: rows that a key head and sequence may have.
+template <int D, int BITS, int R>
+int32_t launch_weigh(WeighArgs& w, const spf_kv_cache* cache, int64_t most, int sm_count, cudaStream_t stream) {
+  using T = Traits<D, BITS, R, false>;
   int32_t st = encode_pool_map("spf_kv_weigh", cache, cache->k_pool, T::KEYS, &w.k_map);
   if (st == SPF_OK) st = encode_ledger_map("spf_kv_weigh", cache, w.weight, T::KEYS, &w.weight_map);
   if constexpr (T::INT4) {
     if (st == SPF_OK) st = encode_scale_map("spf_kv_weigh", cache, cache->k_scale, &w.k_scale_map);
   }
-  if (st == SPF_OK) st = allow_shared_memory(reinterpret_cast<const void*>(weigh_step_kernel<T>), weigh_smem_bytes<T>(), done);
   if (st != SPF_OK) return st;
-  weigh_step_kernel<T><<<sm_count * T::CTAS, T::THREADS, weigh_smem_bytes<T>(), stream>>>(w);
-  SPF_CUDA_CHECK(cudaGetLastError());
-  return SPF_OK;
+  return most > kPlain * R ? launch_kernel<T, true>(w, sm_count, stream) : launch_kernel<T, false>(w, sm_count, stream);
 }
 template <int D, int BITS>
-int32_t launch_rows(WeighArgs& w, const spf_kv_cache* cache, int64_t rows, int sm_count, cudaStream_t stream) {
-  if (rows <= 8) return launch_weigh<D, BITS, 8>(w, cache, sm_count, stream);
-  if (rows <= 16) return launch_weigh<D, BITS, 16>(w, cache, sm_count, stream);
-  return launch_weigh<D, BITS, 32>(w, cache, sm_count, stream);
+int32_t launch_rows(WeighArgs& w, const spf_kv_cache* cache, int64_t rows, int64_t most, int sm_count, cudaStream_t stream) {
+  if (rows <= 8) return launch_weigh<D, BITS, 8>(w, cache, most, sm_count, stream);
+  if (rows <= 16) return launch_weigh<D, BITS, 16>(w, cache, most, sm_count, stream);
+  return launch_weigh<D, BITS, 32>(w, cache, most, sm_count, stream);
 }
 
 }  // namespace
@@ -369,7 +391,11 @@ extern "C" int32_t spf_kv_weigh(const spf_kv_cache* cache, const spf_kv_step* st
   st = device_sm_count(&sm_count);
   if (st != SPF_OK) return st;
   const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-  const int64_t rows = (int64_t)a.group * (w.last_rows > 0 ? std::min(w.last_rows, step->max_new) : step->max_new);
+  auto rows_of = [&](int64_t tokens) { return a.group * (w.last_rows > 0 ? std::min<int64_t>(w.last_rows, tokens) : tokens); };
+  const int64_t rows = rows_of(step->max_new);
+  // Rows that the sequences cannot have by the hint: then some may have all of them.  (Fewer, in one sequence, may be more than it says too: not more
+  // than the hint allows all sequences together.)
+  const int64_t most = step->n_rows > (int64_t)step->n_seqs * step->max_new ? std::max(rows, rows_of(step->n_rows)) : rows;
   // Both over 131072 keys and over 8 sequences of 4000, 8 key heads, first against second kernel.  128 rows: bf16 92 against 168 us and 34 against 47
   // (64 dimensions), 151 against 192 and 53 against 52 (128); 8 bits 121 against 218, 44 against 56 and 184 against 250, 65 against 65; 4 bits 124
   // against 188, 45 against 51, but 277 against 200, 88 against 58 with 128 dimensions, whose codes are unpacked for each 32 rows anew (64 rows:
@@ -378,8 +404,8 @@ extern "C" int32_t spf_kv_weigh(const spf_kv_cache* cache, const spf_kv_step* st
   if (rows > few && weigh_prompt_prepare(w, n_q_heads, cache->head_dim)) return weigh_prompt_launch(w, cache->head_dim, sm_count, stream);
   const bool d64 = cache->head_dim == 64;
   switch (a.kv.bits) {
-    case 4: return d64 ? launch_rows<64, 4>(w, cache, rows, sm_count, stream) : launch_rows<128, 4>(w, cache, rows, sm_count, stream);
-    case 8: return d64 ? launch_rows<64, 8>(w, cache, rows, sm_count, stream) : launch_rows<128, 8>(w, cache, rows, sm_count, stream);
-    default: return d64 ? launch_rows<64, 16>(w, cache, rows, sm_count, stream) : launch_rows<128, 16>(w, cache, rows, sm_count, stream);
+    case 4: return d64 ? launch_rows<64, 4>(w, cache, rows, most, sm_count, stream) : launch_rows<128, 4>(w, cache, rows, most, sm_count, stream);
+    case 8: return d64 ? launch_rows<64, 8>(w, cache, rows, most, sm_count, stream) : launch_rows<128, 8>(w, cache, rows, most, sm_count, stream);
+    default: return d64 ? launch_rows<64, 16>(w, cache, rows, most, sm_count, stream) : launch_rows<128, 16>(w, cache, rows, most, sm_count, stream);
   }
 }
