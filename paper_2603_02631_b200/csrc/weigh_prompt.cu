@@ -382,23 +382,20 @@ __device__ __forceinline__ void add_up(const WeighArgs& w, Smem& sm, uint32_t tm
         // Rows that saw no key add nothing, by selection, whatever their products are: apart from what follows, to which this added a twentieth.  Either
         // gives other tiles the same bits, so that it does not matter when the flag is seen there.
 #pragma unroll 1
-        for (int c = 0; c < 8; ++c) {
-          uint32_t z[16];
-          tmem_issue<16>(tmem + 128 * acc + lanes + 16 * c, z);
+        for (int c = 0; c < 128; c += 4) {
+          uint32_t z[4];
+          tmem_issue<4>(tmem + 128 * acc + lanes + c, z);
           tmem_load_wait();
-          tmem_ready<16>(z);
+          tmem_ready<4>(z);
+          float p[4];
 #pragma unroll
-          for (int i = 0; i < 16; i += 2) {
-            float p[2];
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const int column = 16 * c + i + e;
-              const float b = below[column];
-              p[e] = fast_exp2(fmaf(__uint_as_float(z[i + e]), f, b));
-              if (rr + column < from || rr + column >= min(rows, rr + tile_rows) || b == INFINITY) p[e] = 0.f;
-            }
-            part[(i >> 1) & 1] = add2(part[(i >> 1) & 1], pack2(p[0], p[1]));
+          for (int i = 0; i < 4; ++i) {
+            const float b = below[c + i];
+            p[i] = fast_exp2(fmaf(__uint_as_float(z[i]), f, b));
+            if (rr + c + i < from || rr + c + i >= min(rows, rr + tile_rows) || b == INFINITY) p[i] = 0.f;
           }
+          part[0] = add2(part[0], pack2(p[0], p[1]));
+          part[1] = add2(part[1], pack2(p[2], p[3]));
         }
         tc_fence_before();
         __syncwarp();
@@ -427,8 +424,8 @@ __device__ __forceinline__ void add_up(const WeighArgs& w, Smem& sm, uint32_t tm
 #pragma unroll
           for (int i = 0; i < 16; ++i) p[i] = fast_exp2(p[i]);
           // Columns behind a tile's last whole token are zeros there, which a key with an infinite element makes NaN of: the last of these 16, if any
-          // is one, shows it.
-          if (guard || __any_sync(0xffffffffu, p[15] != p[15])) {
+          // is one, shows it.  (8- and 4-bit elements are finite or NaN, and of NaN the rows that see the key make NaN too.)
+          if (guard || (T::BITS == 16 && __any_sync(0xffffffffu, p[15] != p[15]))) {
             const int last = min(rows, rr + tile_rows);
 #pragma unroll
             for (int i = 0; i < 16; ++i)
