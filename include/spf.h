@@ -382,7 +382,7 @@ typedef struct {
  *   attend        as the step's spf_attend had it; lse is required, and read
  *   ledger        position may be NULL; else the new tokens' positions are written to it
  *   options       NULL: decay 1, all rows, a token's place as its position
- *     decay       finite, not negative
+ *     decay       finite, not negative; 0: what the ledger holds is replaced, whatever it is
  *     last_rows   only the last so many new tokens of a sequence count as rows (0: all of them)
  *     positions   DEVICE int32 [n_rows], the positions of the step's tokens; NULL: a token's place in its sequence
  * A block belongs to one sequence of the step (two that share one race).

@@ -36,7 +36,7 @@ __device__ __forceinline__ WeighSpan weigh_span(const WeighArgs& w, int b) {
 // What a key has received: `got` joins what the ledger holds, or replaces it where the token is one of the step's.
 __device__ __forceinline__ void book(const WeighArgs& w, int64_t cell, float held, float got, int key, int fresh, int fresh_row) {
   if (key < fresh) {
-    w.weight[cell] = fmaf(held, w.decay, got);
+    w.weight[cell] = w.decay != 0.f ? fmaf(held, w.decay, got) : got;      // memory that was never written may hold NaN
     return;
   }
   w.weight[cell] = got;
