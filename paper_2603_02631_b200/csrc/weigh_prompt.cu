@@ -347,6 +347,33 @@ __device__ __forceinline__ void multiply(const WeighArgs& w, Smem& sm, uint32_t 
 }
 
 // ---------------------------------------------------------------------------------------------- weights
+// A tile's weights of a key where that is seldom: some row of the CTA's saw no key, which adds nothing, or a key with an infinite element makes NaN of
+// the zeros behind a tile's last whole token.  Both by selection, whatever the products are, as for rows before `from`, and from `last` on, of the
+// tile.  Not inlined: beside the other code it cost that up to a twentieth.  Either gives other tiles the same bits, so that it does not matter when
+// a warp first sees the flag for the former.
+__device__ __noinline__ float2 add_seldom(uint32_t z_at, const float* below, float f, int from, int last) {
+  uint64_t part[2] = {0ull, 0ull};
+#pragma unroll 1
+  for (int c = 0; c < 128; c += 4) {
+    uint32_t four[4];
+    tmem_issue<4>(z_at + c, four);
+    tmem_load_wait();
+    tmem_ready<4>(four);
+    float p[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float b = below[c + i];
+      p[i] = fast_exp2(fmaf(__uint_as_float(four[i]), f, b));
+      if (c + i < from || c + i >= last || b == INFINITY) p[i] = 0.f;
+    }
+    part[0] = add2(part[0], pack2(p[0], p[1]));
+    part[1] = add2(part[1], pack2(p[2], p[3]));
+  }
+  float2 both;
+  unpack2(add2(part[0], part[1]), both.x, both.y);
+  return both;
+}
+
 template <class T>
 __device__ __forceinline__ void add_up(const WeighArgs& w, Smem& sm, uint32_t tmem, int64_t w0, int64_t w1, const Abort& ab) {
   const AttendArgs& a = w.a;
@@ -375,34 +402,31 @@ __device__ __forceinline__ void add_up(const WeighArgs& w, Smem& sm, uint32_t tm
       tc_fence_after();
       const float* below = sm.below[tile % kBelow];
       const int rr = row_first + j * tile_rows;
-      // rows that do not see the key, and those behind the sequence's, which are other ones'
-      const bool guard = __any_sync(0xffffffffu, rr < from) || rr + 128 > rows;
+      const int last = min(rows, rr + tile_rows);
       uint64_t part[2] = {0ull, 0ull};
-      if (*const_cast<const volatile int*>(&sm.idle) != 0) {
-        // Rows that saw no key add nothing, by selection, whatever their products are: apart from what follows, to which this added a twentieth.  Either
-        // gives other tiles the same bits, so that it does not matter when the flag is seen there.
-#pragma unroll 1
-        for (int c = 0; c < 128; c += 4) {
-          uint32_t z[4];
-          tmem_issue<4>(tmem + 128 * acc + lanes + c, z);
-          tmem_load_wait();
-          tmem_ready<4>(z);
-          float p[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float b = below[c + i];
-            p[i] = fast_exp2(fmaf(__uint_as_float(z[i]), f, b));
-            if (rr + c + i < from || rr + c + i >= min(rows, rr + tile_rows) || b == INFINITY) p[i] = 0.f;
-          }
-          part[0] = add2(part[0], pack2(p[0], p[1]));
-          part[1] = add2(part[1], pack2(p[2], p[3]));
-        }
+      uint32_t z[2][16];
+      tmem_issue<16>(tmem + 128 * acc + lanes, z[0]);
+      // Of a key with an infinite element the zeros behind a tile's last whole token make NaN, as its last column shows.  (8- and 4-bit elements are
+      // finite or NaN, and of NaN the rows that see the key make NaN too.)
+      bool seldom = *const_cast<const volatile int*>(&sm.idle) != 0;
+      if (T::BITS == 16 && tile_rows < 128) {
+        uint32_t end[2];
+        tmem_issue<2>(tmem + 128 * acc + lanes + 126, end);
+        tmem_load_wait();
+        tmem_ready<2>(end);
+        seldom = seldom || __uint_as_float(end[1]) != __uint_as_float(end[1]);
+      }
+      // rows that do not see the key, and those behind the sequence's, which are other ones'
+      const bool guard = __any_sync(0xffffffffu, rr < from || seldom) || rr + 128 > rows;
+      if (guard && __any_sync(0xffffffffu, seldom)) {
+        tmem_load_wait();
+        tmem_ready<16>(z[0]);
+        const float2 both = add_seldom(tmem + 128 * acc + lanes, below, f, max(from, 0) - rr, last - rr);
+        part[0] = pack2(both.x, both.y);
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&sm.acc_empty[acc]));
       } else {
-        uint32_t z[2][16];
-        tmem_issue<16>(tmem + 128 * acc + lanes, z[0]);
 #pragma unroll
         for (int c = 0; c < 8; ++c) {
           tmem_load_wait();
@@ -423,10 +447,7 @@ __device__ __forceinline__ void add_up(const WeighArgs& w, Smem& sm, uint32_t tm
           }
 #pragma unroll
           for (int i = 0; i < 16; ++i) p[i] = fast_exp2(p[i]);
-          // Columns behind a tile's last whole token are zeros there, which a key with an infinite element makes NaN of: the last of these 16, if any
-          // is one, shows it.  (8- and 4-bit elements are finite or NaN, and of NaN the rows that see the key make NaN too.)
-          if (guard || (T::BITS == 16 && __any_sync(0xffffffffu, p[15] != p[15]))) {
-            const int last = min(rows, rr + tile_rows);
+          if (guard) {
 #pragma unroll
             for (int i = 0; i < 16; ++i)
               if (rr + 16 * c + i < from || rr + 16 * c + i >= last) p[i] = 0.f;
