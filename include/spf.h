@@ -232,7 +232,8 @@ SPF_API int32_t spf_score_fp8(const spf_shape* shape, const spf_fp8_prompt* prom
  *                      finite, with at most five significant bits (an element then is a bf16 number)
  *   block_tokens       a positive multiple of 128
  *   head_dim           d: 64 or 128
- *   bits               of an element: 16, 8 or 4; 0: 16 without scales, 8 with them
+ *   bits               of an element: 16, 8 or 4; 0: 16 without scales, 8 with them.  (Since version 0.2.0, where the structure ended in four
+ *                      unused bytes, and k_scale and v_scale were float*: programs that do not set the bytes to zero have to be adapted)
  * Limit: n_pool_blocks * Hkv * block_tokens < 2^31.
  */
 #define SPF_KV_SCALE_TOKENS 64
@@ -339,8 +340,9 @@ SPF_API int32_t spf_kv_append(const spf_kv_cache* cache, const spf_kv_step* step
  *                 contents irrelevant on entry, unspecified on exit.  Calls that share one must be ordered on one stream.
  * What the pools hold behind a sequence's tokens, or before its first key, does not matter.
  * Roundings: weights of the sum over values are bf16 over bf16 pools (16 bits with up to 8 rows a key head and sequence), fp16 over
- * 8-bit ones, bf16, with the values' scales in them, over 4-bit ones (from 33 rows on, 17 with 128 dimensions: as over bf16 pools); the
- * sum of the weights is fp32.
+ * 8-bit ones; the sum of the weights is fp32, of weights that are not rounded.  4-bit pools, up to 32 rows (16 with 128 dimensions): weights are
+ * rounded to bf16, and once more with the values' scales in them, off by up to 2^-8 together; of 128 keys that not every row sees, once, with the
+ * scales in them (2^-9).  From 33 (17) rows on: as over bf16 pools.
  * 4-bit pools: elements are exact.  Elements of a query should lie below 2^114 in magnitude, value scales within 2^-40 ... 2^50.
  * 8-bit pools: values of bytes times scales are exact; their scales should lie within 2^-100 ... 2^100.  Elements of a query row are exact
  * within 2^13 of its largest and off by at most 2^-21 of that below.  Weights below 2^-21 of the row's largest (each times its value
@@ -367,6 +369,9 @@ SPF_API int32_t spf_attend(const spf_kv_cache* cache, const spf_kv_step* step, c
  *   weight        DEVICE fp32 [n_pool_blocks][Hkv][block_tokens]: the attention weight that the token has received (spf_kv_weigh)
  *   position      DEVICE int32, the same: the token's position in its sequence, whatever was cut before it; NULL: nothing was ever cut, a
  *                 token's position is its place
+ * Nothing has to be set beforehand where spf_kv_weigh is called for every step: it writes both for the step's tokens.  Only it does: where it is
+ * left out for some steps (chunks of a prompt before the window that a cut is decided by), their tokens' weights and positions are the caller's
+ * to set; with a decay of 0 their weights need not be, either.
  */
 typedef struct {
   float* weight;
@@ -386,8 +391,10 @@ typedef struct {
  *     last_rows   only the last so many new tokens of a sequence count as rows (0: all of them)
  *     positions   DEVICE int32 [n_rows], the positions of the step's tokens; NULL: a token's place in its sequence
  * A block belongs to one sequence of the step (two that share one race).
- * Sums are fp32, taken in an order that does not change from run to run.  A row whose lse is -inf (it saw no key) adds nothing; one with NaN
- * makes NaN of the weights of the keys that it sees.
+ * Sums are fp32, taken in an order that does not change from run to run; over many rows they carry what their additions lose.  (But for a
+ * sequence that has more rows than max_new announces, and no more than it announces for all sequences together: up to 2^-25 of a sum is lost for
+ * each 8 of them.)  Besides, weights are off by some 1e-7: the roundings of logits, of log-sum-exps and of ex2.
+ * A row whose lse is -inf (it saw no key) adds nothing, whatever the keys are; one with NaN makes NaN of the weights of the keys that it sees.
  * Device conditions: SPF_ERR_CACHE in dev_status (may be NULL) as for spf_attend; keys in a block outside the pool are left out.
  * SPF_ERR_TIMEOUT as for spf_score.
  * Errors: SPF_ERR_INVALID_ARG, SPF_ERR_UNSUPPORTED (as for spf_attend), SPF_ERR_CUDA.
@@ -409,6 +416,11 @@ SPF_API int32_t spf_kv_weigh(const spf_kv_cache* cache, const spf_kv_step* step,
  * n_first, or of n_seen[b] - n_recent and above, then those of the largest weight; of equals, and of the former where they are too many, those
  * of the lowest places.  NaN ranks below every number.  Heads keep different tokens; a sequence's length, the same for all of them, goes to to_lens.
  * The blocks that the call reads are left as they were, and may be given up, or kept (a prefix that other sequences share).
+ * A place then holds other tokens in each head and layer: such a cache is attended over, but not scored (spf_score_paged and
+ * spf_score_paged_fp8 go by places, and do not notice).
+ * The time goes by the room that the tables have too, not by the lengths alone, which the host does not see: 32 sequences of 1900 to 2500
+ * tokens (4 bits, 8 heads of 128 dimensions) take 55 us where block_table has room for 3072 tokens of each, 69 for 8192, 103 for 32768,
+ * 226 for 131072.
  *
  *   n_seqs        1 ... 2^20
  *   seq_lens      DEVICE int32 [n_seqs], at most table_stride * block_tokens
@@ -765,7 +777,7 @@ SPF_API int64_t spf_concat_with_delim(const char* text, int64_t text_bytes, cons
 SPF_API const char* spf_status_string(int32_t status);
 /* Text of the calling thread's most recent failure ("" if none).  Thread-local storage. */
 SPF_API const char* spf_last_error(void);
-/* Library version, e.g. "0.1.0". */
+/* Library version, e.g. "0.2.0". */
 SPF_API const char* spf_version(void);
 
 #ifdef __cplusplus

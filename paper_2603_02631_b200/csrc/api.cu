@@ -477,4 +477,4 @@ extern "C" const char* spf_status_string(int32_t status) {
 
 extern "C" const char* spf_last_error(void) { return g_error; }
 
-extern "C" const char* spf_version(void) { return "0.1.0"; }
+extern "C" const char* spf_version(void) { return "0.2.0"; }
