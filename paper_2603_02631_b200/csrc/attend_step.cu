@@ -4,13 +4,13 @@
 //   lse[r] = (m_r + log2 l_r) ln 2;   rows r = (new token i, head g of the key head's group), r = i G + g, in tiles of R.
 //
 // One pass over keys and values, each read once for all rows of a tile.  What bounds it is that read, so the work is dealt out
-// by key tiles, not by sequences: the tiles of all (sequence, row tile, key head) triples, 64 keys each, form one list, and CTA
+// by key tiles, not by sequences: the tiles of all (sequence, row tile, key head) triples, 64 or 128 keys each, form one list, and CTA
 // c takes its c-th part, wherever that begins and ends.  A triple that one CTA has from end to end is written at once; one that
 // several share leaves partial sums in the workspace, and a second kernel (launched behind the first without waiting for the
 // host) joins them in the order of the keys.  All of it is worked out on the device from the lengths there.
 //
-// A CTA: one warp copies tiles into a ring (TMA, 64 keys and their values a stage) and runs ahead across the triples' borders;
-// four warps compute, each on its own 16 keys of every tile (many rows: some of the rows and more of the keys), with maxima, sums
+// A CTA: one warp copies tiles into a ring (TMA, a tile's keys and their values a stage) and runs ahead across the triples' borders;
+// four warps compute, each on its own 16 or 32 keys of every tile (many rows: some of the rows and more of the keys), with maxima, sums
 // and outputs of their own in registers, so that nothing is exchanged between them until a triple ends.  Products are warp-level, with
 // the keys (then the dimensions of the values) as the 16 rows of the left operand and the query rows as the 8 columns of the right
 // one: a single token's few heads fill a product, where they would be half or less of the left operand's rows, and the tensor

@@ -7,9 +7,9 @@
 // knows how many kept places lie before its own and writes them to a list.  No order of atomics shows in it.
 // The second copies: 64 places of the list (a group, which shares a scale in an 8-bit pool) are a warp's, rows in pieces of 16 bytes.
 //
-// What bounds them: latency the first (a launch, two dependent loads, three passes with an exchange each: 17 us for 2200 places, 28 for 131072),
-// the rows' bytes the second, which are read where the kept tokens happen to lie.  32 sequences cut from 2500 to 2048 tokens, 8 heads of 128
-// dimensions, 4 bits: 56 us, 25 of bytes; 131072 tokens to a quarter, bf16: 88 us, 43 of bytes.
+// What bounds them: latency the first (a launch, two dependent loads, three passes with an exchange each: 19 us for 32 sequences of 1900 to 2500
+// places, 30 for one of 131072, 8 heads), the rows' bytes the second, which are read where the kept tokens happen to lie.  The former cut to 2048
+// tokens, 128 dimensions, 4 bits: 55 us in all, 25 of bytes; the latter to a quarter, bf16: 87 us, 43 of bytes.
 #include <cooperative_groups.h>
 #include <cuda_fp16.h>
 
@@ -393,12 +393,13 @@ int32_t check_cut(const char* who, const KvView& kv, int64_t n_seqs, int64_t to_
 
 template <int D, int BITS>
 int32_t launch_evict(EvictArgs& a, cudaStream_t stream) {
-  // CTAs of a (sequence, key head): by the places that its table has room for.  One and four for 3000 places: 19.4 and 19.1 us for a sequence, but 55
-  // and 134 for 32 of them; two and eight for 8000 places: 19 and 25 us, 150 and 393.
+  // CTAs of a (sequence, key head): by the places that its table has room for, which is what the host knows.  One and four for 3000 places (the whole
+  // call, 4 bits): 19 us either for a sequence, but 54 and 134 for 32 of them; two and eight for 8000 places: 19 and 23 us, 148 and 390.  A table wider
+  // than its sequences costs as much: 2500 places in room for 131072, 22 us for a sequence, 226 for 32.
   const int64_t places = (int64_t)a.table_stride * a.kv.block_tokens, pairs = (int64_t)a.n_seqs * a.kv.n_kv_heads;
   const int parts = places <= 4096 ? 1 : places <= 8192 ? 2 : places <= 32768 ? 4 : kMostParts;
   a.held = (int)std::min<int64_t>(align_up((size_t)ceil_div(places, parts), 128), kHeld);
-  // Few places: small CTAs, so that many sequences' run at the same time (256 of 2200 tokens: 256 threads 20 us, 1024 threads 23)
+  // Few places: small CTAs, so that many sequences' run at the same time (32 sequences of 3000 tokens, 8 heads, the whole call: 256 threads 54 us, 1024 threads 60)
   static ContextSet done;
   const auto rank = parts == 1 ? rank_kernel<256> : rank_kernel<1024>;
   if (parts > 1) {

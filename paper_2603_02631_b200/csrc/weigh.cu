@@ -9,9 +9,9 @@
 // stays where it is while the rows go by, up to 128 of them from shared memory.
 //
 // What bounds it with few rows is the read of the keys, of which it misses half: one token for each of 32 sequences of up to 16k tokens on a 4-bit
-// cache, 8 heads of 128 dimensions, takes 51 us where the bytes take 27; without any product it takes 46, with 8 us of launch and first loads.
-// (The ledger's weights loaded when they are wanted instead of copied with the keys: 61
-// instead of 58.)  Masks stand apart from the exponentials, in a block of their own: as a condition on each they made a branch of each (95 instead of
+// cache, 8 heads of 128 dimensions, takes 52 us where the bytes take 27; without any product it takes 46, with 8 us of launch and first loads.
+// (Where it took 58 it took 61 with the ledger's weights loaded when they are wanted, not copied with the keys.)
+// Masks stand apart from the exponentials, in a block of their own: as a condition on each they made a branch of each (95 instead of
 // 36 us for 128 rows over 32k keys of 64 dimensions, 33 now, whose exponentials take 8).
 #include <algorithm>
 #include <cmath>
@@ -396,10 +396,10 @@ extern "C" int32_t spf_kv_weigh(const spf_kv_cache* cache, const spf_kv_step* st
   // Rows that the sequences cannot have by the hint: then some may have all of them.  (Fewer, in one sequence, may be more than it says too: not more
   // than the hint allows all sequences together.)
   const int64_t most = step->n_rows > (int64_t)step->n_seqs * step->max_new ? std::max(rows, rows_of(step->n_rows)) : rows;
-  // Both over 131072 keys and over 8 sequences of 4000, 8 key heads, first against second kernel.  128 rows: bf16 92 against 168 us and 34 against 47
-  // (64 dimensions), 151 against 192 and 53 against 52 (128); 8 bits 121 against 218, 44 against 56 and 184 against 250, 65 against 65; 4 bits 124
-  // against 188, 45 against 51, but 277 against 200, 88 against 58 with 128 dimensions, whose codes are unpacked for each 32 rows anew (64 rows:
-  // 143 against 238, 50 against 66).  256 rows: 410 against 185 (bf16, 64 dimensions) to 1027 against 217 (4 bits, 128).
+  // Both over 131072 keys and over 8 sequences of 4000, 8 key heads, first against second kernel.  128 rows: bf16 95 against 174 us and 34 against 48
+  // (64 dimensions), 154 against 201 and 52 against 54 (128); 8 bits 121 against 225, 43 against 57 and 184 against 252, 63 against 66; 4 bits 126
+  // against 197, 46 against 52, but 254 against 213, 86 against 61 with 128 dimensions, whose codes are unpacked for each 32 rows anew (64 rows:
+  // 139 against 248, 48 against 69).  256 rows: 304 against 189 (bf16, 64 dimensions) to 819 against 226 (4 bits, 128).
   const int64_t few = a.kv.bits == 4 && cache->head_dim == 128 ? 64 : 128;
   if (rows > few && weigh_prompt_prepare(w, n_q_heads, cache->head_dim)) return weigh_prompt_launch(w, cache->head_dim, sm_count, stream);
   const bool d64 = cache->head_dim == 64;

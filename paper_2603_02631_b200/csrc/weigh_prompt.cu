@@ -7,9 +7,9 @@
 // lanes and rows as the columns: a thread of the four sets of four warps that take the exponentials has one key, whose weights it adds up in a
 // register over all rows, with no exchange between threads; per exponential it spends half a multiply-add, half an addition and a quarter of a
 // read of log-sum-exps from shared memory.  Three chunks of 836 to 2001 tokens behind 1300 to 9000 (32/8 heads of 64 dimensions, 8 bits) take
-// 339 us, 222 of them exponentials; warp-level products with keys in registers took 648: two units in turns in each of few warps.  Two sets of
+// 340 us, 222 of them exponentials; warp-level products with keys in registers took 648: two units in turns in each of few warps.  Two sets of
 // warps for the exponentials instead of four: 385; rows brought by threads instead of tensor copies: 405, log-sum-exps loaded one tile at a time:
-// 447.  Sums of a tile are added with what the additions lose (thousands of rows make 1.7e-6 of a weight otherwise).
+// 447.  Sums of tiles are added with what the additions lose (thousands of rows make 1.7e-6 of a weight otherwise).
 //
 // Keys are brought once for all rows of an item (a sequence, key head and 128 keys), eight loads in flight, and widened to bf16 on the way (exactly: 8-bit values, and
 // 4-bit codes times scales of five bits), the next item's while this one's last rows are being made.  Rows go by in tiles of as many tokens as fit whole into 128, a box of the queries each, whose
@@ -349,7 +349,7 @@ __device__ __forceinline__ void multiply(const WeighArgs& w, Smem& sm, uint32_t 
 // ---------------------------------------------------------------------------------------------- weights
 // A tile's weights of a key where that is seldom: some row of the CTA's saw no key, which adds nothing, or a key with an infinite element makes NaN of
 // the zeros behind a tile's last whole token.  Both by selection, whatever the products are, as for rows before `from`, and from `last` on, of the
-// tile.  Not inlined: beside the other code it cost that up to a twentieth.  Either gives other tiles the same bits, so that it does not matter when
+// tile.  A function of its own: beside the other code it cost that 4 to 9 %.  Either gives other tiles the same bits, so that it does not matter when
 // a warp first sees the flag for the former.
 __device__ __noinline__ float2 add_seldom(uint32_t z_at, const float* below, float f, int from, int last) {
   uint64_t part[2] = {0ull, 0ull};
