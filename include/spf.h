@@ -419,7 +419,7 @@ SPF_API int32_t spf_kv_weigh(const spf_kv_cache* cache, const spf_kv_step* step,
  * A place then holds other tokens in each head and layer: such a cache is attended over, but not scored (spf_score_paged and
  * spf_score_paged_fp8 go by places, and do not notice).
  * The time goes by the room that the tables have too, not by the lengths alone, which the host does not see: 32 sequences of 1900 to 2500
- * tokens (4 bits, 8 heads of 128 dimensions) take 55 us where block_table has room for 3072 tokens of each, 69 for 8192, 103 for 32768,
+ * tokens (4 bits, 8 heads of 128 dimensions) take 55 us where block_table has no more room than they need, 69 with room for 8192 of each, 103 for 32768,
  * 226 for 131072.
  *
  *   n_seqs        1 ... 2^20
